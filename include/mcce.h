@@ -44,7 +44,7 @@ enum {
   MCCE_ENONFINITE = -8 /* checked mode: a router logit was NaN or infinite                               */
 };
 
-enum { MCCE_F32 = 0, MCCE_BF16 = 1 };
+enum { MCCE_F32 = 0, MCCE_BF16 = 1, MCCE_E4M3 = 2 /* rows of mcce_dispatch only */ };
 enum { MCCE_DELTA_RUNNING = 0, MCCE_DELTA_FIXED = 1 };
 enum { MCCE_FFN_AUTO = 0, MCCE_FFN_SIMT = 1, MCCE_FFN_TENSOR = 2 };
 /* How the router's ranking r is changed in favour of cached experts (Sec. 3):
@@ -266,6 +266,105 @@ int mcce_get_grouping(mcce_ctx* ctx, int32_t* offsets, int32_t* perm);
 int mcce_belady_replay(const int32_t* sel_trace, int32_t n_tokens, int32_t n_layers, int32_t n_streams,
                        int32_t n_experts, int32_t top_k, const int32_t* capacities, int32_t n_capacities,
                        int32_t* next_use_scratch, int64_t* misses, void* cuda_stream);
+
+/* ---- operators around the experts ----------------------------------------------------------------------------
+ * What a decoder layer needs on either side of its experts, and the gradients for training it.  Context-free: the
+ * device that is current when the call is made is used, every buffer is the caller's, launches are asynchronous on
+ * the stream, nothing is allocated and nothing is kept between calls; a call may be captured into a graph.  A
+ * workspace is used only while the call's kernels run: calls that can overlap need one each.  Sums, statistics and
+ * weights are held in fp32; every result is rounded once, to nearest even, to the type of its buffer.  Results do
+ * not depend on the order in which threads run (no atomics on data): repeated calls give identical bits.
+ */
+
+/* Rows for mcce_rmsnorm and its gradient.  Row strides (ld_*) are in elements, 0 means d; the columns of a row are
+ * contiguous and rows of a tensor do not overlap. */
+typedef struct {
+  int64_t rows;          /* >= 0                                                                              */
+  int32_t d;             /* columns, 1..16384                                                                 */
+  int32_t dtype;         /* x, sum, out, and the gradients: MCCE_F32 or MCCE_BF16                             */
+  int32_t add_dtype;     /* MCCE_F32 (what mcce_moe_forward returns) or dtype                                 */
+  int32_t weight_dtype;  /* MCCE_F32 or dtype                                                                 */
+  int32_t quant_group;   /* columns that share a scale: 32, 64, 128, or 0 for one scale per row               */
+  float eps;             /* finite, >= 0                                                                      */
+  int64_t ld_x, ld_add, ld_sum, ld_out, ld_q;
+} mcce_norm;
+
+/* Root-mean-square norm of the residual stream, with the residual's addition:
+ *   h = x + add, rounded to dtype (h = x without add);    r = 1 / sqrt(mean_j h_j^2 + eps);    n_j = h_j r weight_j
+ *   sum = h;    out = n rounded to dtype;    for every group G of columns
+ *   scales_G = max(max_{j in G} |n_j|, 2^-100) / 448;    q_j = e4m3(n_j / scales_G)
+ *   x   DEVICE dtype [rows,d]; add DEVICE add_dtype [rows,d] or NULL; weight DEVICE weight_dtype [d]
+ *   sum DEVICE dtype [rows,d] out or NULL; may be x itself (same stride)
+ *   out DEVICE dtype [rows,d] out or NULL
+ *   q   DEVICE e4m3 (one byte: 4 exponent bits, 3 mantissa bits, largest value 448) [rows,d] out or NULL
+ *   scales DEVICE fp32 [rows, ceil(d / quant_group)] out, contiguous; given exactly when q is.  The last group of a
+ *       row may be shorter.  q_j * scales_G is within 2^-4 |n_j| (or half a subnormal step) of n_j.
+ * One of sum, out and q at least.  Apart from sum == x no output may overlap another tensor of the call.  A row that holds a NaN is
+ * NaN throughout; the sum of squares is formed in fp32, so one beyond 3.4e38 counts as infinite (r = 0). */
+int mcce_rmsnorm(const mcce_norm* n /*HOST*/, const void* x, const void* add, const void* weight, void* sum,
+                 void* out, void* q, float* scales, void* cuda_stream);
+
+/* Its gradient.  With g_j = dout_j weight_j and r as above, formed again from h:
+ *   dx_j = r g_j - h_j r^3 mean_i(h_i g_i) + dsum_j;    dweight_j = sum over the rows of dout_j h_j r
+ * dx is the gradient of x and of add alike (they enter as a sum).  The gradient of the 8-bit output is not part of
+ * it: hand in the gradient with respect to n as dout.
+ *   dout DEVICE dtype [rows,d], stride ld_out;    h DEVICE dtype [rows,d], stride ld_x: the `sum` of the forward call (x without add)
+ *   dsum DEVICE dtype [rows,d], stride ld_add, or NULL: the gradient that reaches h past the norm
+ *   dx   DEVICE dtype [rows,d] out, stride ld_sum; may be dout or dsum itself (same stride)
+ *   dweight DEVICE fp32 [d] out, or NULL: not wanted (no workspace needed then).  Rounded parts are added in a fixed order.
+ *   workspace DEVICE, 16-byte aligned, mcce_rmsnorm_backward_workspace_bytes(n) bytes (0 for an invalid n).
+ * add_dtype, quant_group and ld_q are ignored. */
+size_t mcce_rmsnorm_backward_workspace_bytes(const mcce_norm* n /*HOST*/);
+int mcce_rmsnorm_backward(const mcce_norm* n /*HOST*/, const void* dout, const void* h, const void* dsum,
+                          const void* weight, void* dx, float* dweight, void* workspace, size_t workspace_bytes,
+                          void* cuda_stream);
+
+/* Token rows for mcce_dispatch, mcce_combine and mcce_combine_backward: n_layers independent problems of n_tokens
+ * tokens with top_k (token, slot) pairs each, P = n_tokens * top_k <= 2^30 pairs per layer. */
+typedef struct {
+  int32_t n_layers;    /* 1..65535                                                                        */
+  int32_t n_tokens;    /* >= 0                                                                            */
+  int32_t top_k;       /* 1..16                                                                           */
+  int32_t n_experts;   /* 1..256 (mcce_dispatch)                                                          */
+  int32_t d;           /* columns of a row, >= 1                                                          */
+  int32_t dtype;       /* sorted rows: MCCE_F32 or MCCE_BF16; MCCE_E4M3 too in mcce_dispatch              */
+  int32_t token_dtype; /* y, add and dy: MCCE_F32, or dtype (mcce_combine and its gradient)               */
+  int32_t scale_cols;  /* fp32 scales that travel with a row, 0: none (mcce_dispatch)                     */
+  int64_t ld_token;    /* stride in elements of the token rows (x; y and dy), 0 means d; tokens of layer l start at row l * n_tokens */
+  int64_t ld_rows;     /* stride in elements of the sorted rows, 0 means d; layer l starts at row l * P   */
+} mcce_rows;
+
+/* Sorts token rows by expert: the pairs (t, k) of a layer, in the order t * top_k + k, go into their expert's bucket
+ * (a stable counting sort, the grouping of mcce_get_grouping).  A pair whose expert id is outside [0, n_experts) --
+ * padding, a dropped token -- goes nowhere.
+ *   sel_idx DEVICE int32 [L,T,K]
+ *   offsets DEVICE int32 [L,E+1] out: bucket e of layer l is positions offsets[l][e] .. offsets[l][e+1]
+ *   perm    DEVICE int32 [L,P] out: pair at every position, or NULL;    inv DEVICE int32 [L,T,K] out: position of every pair, -1 if it has none
+ *   x       DEVICE dtype [L,T,d] or NULL (only sort);    rows DEVICE dtype [L,P,d] out: rows[l][inv[l][t][k]] = x[l][t]
+ *   scales  DEVICE fp32 [L,T,scale_cols];    row_scales DEVICE fp32 [L,P,scale_cols] out: likewise; contiguous, NULL without scale_cols
+ * perm, rows and row_scales are left as they were behind position offsets[l][E].  A token's row is read once.
+ * The gradient with respect to x is mcce_combine without weights.
+ *   workspace DEVICE, 16-byte aligned, mcce_dispatch_workspace_bytes(r) bytes (0 is possible: it may be NULL then). */
+size_t mcce_dispatch_workspace_bytes(const mcce_rows* r /*HOST*/);
+int mcce_dispatch(const mcce_rows* r /*HOST*/, const int32_t* sel_idx, const void* x, const float* scales,
+                  int32_t* offsets, int32_t* perm, int32_t* inv, void* rows, float* row_scales, void* workspace,
+                  size_t workspace_bytes, void* cuda_stream);
+
+/* Brings rows back to their tokens (the weighted sum of Eq. 1):  y[l][t] = add[l][t] + sum_k sel_w[l][t][k] rows[l][inv[l][t][k]],
+ * added in slot order, then add.  A pair whose position is outside [0, P) contributes nothing, whatever its weight or
+ * any row holds; a token without pairs gets add, or 0.
+ *   rows DEVICE dtype [L,P,d];  inv DEVICE int32 [L,T,K];  sel_w DEVICE fp32 [L,T,K], or NULL: every weight is 1
+ *   add  DEVICE token_dtype [L,T,d], stride ld_token, or NULL;    y DEVICE token_dtype [L,T,d] out; may be add itself */
+int mcce_combine(const mcce_rows* r /*HOST*/, const void* rows, const int32_t* inv, const float* sel_w,
+                 const void* add, void* y, void* cuda_stream);
+
+/* Its gradient:  drows[l][inv[l][t][k]] = sel_w[l][t][k] dy[l][t];    dw[l][t][k] = sum_j dy[l][t][j] rows[l][inv[l][t][k]][j],
+ * 0 for a pair without a position.  (The gradient of add is dy.)  The positions of a layer must be distinct, as
+ * mcce_dispatch makes them; rows of drows at other positions are left as they were.
+ *   dy DEVICE token_dtype [L,T,d];  rows DEVICE dtype [L,P,d], NULL if dw is
+ *   drows DEVICE dtype [L,P,d] out, stride ld_rows; may be rows itself;    dw DEVICE fp32 [L,T,K] out, or NULL */
+int mcce_combine_backward(const mcce_rows* r /*HOST*/, const void* dy, const void* rows, const int32_t* inv,
+                          const float* sel_w, void* drows, float* dw, void* cuda_stream);
 
 /* Seeded synthetic inputs (counter-based: Philox4x32-10 keyed by (seed, 0), counter = (element
  * block, t, tensor_id), Box-Muller with fixed-order fp32 series); no counterpart in the paper, whose

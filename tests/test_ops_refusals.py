@@ -1,0 +1,154 @@
+"""What the operators around the experts (mcce_rmsnorm, mcce_dispatch, mcce_combine and the gradients) refuse: every
+check is on the host and comes before any launch, so the calls here use addresses that nothing ever reads."""
+import ctypes as C
+
+import pytest
+
+from paper_2412_00099_b200 import binding as mb
+from paper_2412_00099_b200 import build as mbuild
+
+EINVAL, ENOSPC = -1, -2
+P = [C.c_void_p(0x10000 * (i + 1)) for i in range(12)]     # distinct, 64 KB aligned, never dereferenced
+
+
+@pytest.fixture(scope="module")
+def lib():
+    mbuild.build()
+    return mb.load()
+
+
+def norm(**kw):
+    f = dict(rows=4, d=64, dtype=mb.BF16, add_dtype=mb.F32, weight_dtype=mb.F32, quant_group=32, eps=1e-6, ld_x=0,
+             ld_add=0, ld_sum=0, ld_out=0, ld_q=0)
+    f.update(kw)
+    return mb.Norm(**f)
+
+
+def rows(**kw):
+    f = dict(n_layers=2, n_tokens=10, top_k=4, n_experts=8, d=64, dtype=mb.BF16, token_dtype=mb.F32, scale_cols=0,
+             ld_token=0, ld_rows=0)
+    f.update(kw)
+    return mb.Rows(**f)
+
+
+def call_norm(lib, n, x=P[0], add=P[1], w=P[2], s=P[3], o=P[4], q=P[5], sc=P[6]):
+    return lib.mcce_rmsnorm(None if n is None else C.byref(n), x, add, w, s, o, q, sc, None)
+
+
+BAD_NORM = [dict(rows=-1), dict(rows=1 << 31), dict(d=0), dict(d=16385), dict(d=-8), dict(dtype=mb.E4M3), dict(dtype=7),
+            dict(weight_dtype=mb.E4M3), dict(dtype=mb.F32, weight_dtype=mb.BF16), dict(eps=-1e-6),
+            dict(eps=float("nan")), dict(eps=float("inf")), dict(ld_x=63), dict(ld_add=-64), dict(ld_sum=1),
+            dict(ld_out=63)]
+
+
+@pytest.mark.parametrize("bad", BAD_NORM, ids=str)
+def test_norm_descriptor(lib, bad):
+    n = norm(**bad)
+    assert call_norm(lib, n) == EINVAL
+    assert lib.mcce_rmsnorm_backward_workspace_bytes(C.byref(n)) == 0
+    assert lib.mcce_rmsnorm_backward(C.byref(n), P[0], P[1], P[2], P[3], P[4], P[5], P[6], 1 << 30, None) == EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(quant_group=16), dict(quant_group=-1), dict(quant_group=256), dict(ld_q=63),
+                                 dict(add_dtype=mb.E4M3), dict(dtype=mb.F32, add_dtype=mb.BF16)], ids=str)
+def test_norm_forward_only_fields(lib, bad):
+    assert call_norm(lib, norm(**bad)) == EINVAL
+
+
+def test_norm_buffers(lib):
+    n = norm()
+    assert call_norm(lib, None) == EINVAL
+    assert call_norm(lib, n, x=None) == EINVAL and call_norm(lib, n, w=None) == EINVAL
+    assert call_norm(lib, n, s=None, o=None, q=None, sc=None) == EINVAL           # nothing to compute
+    assert call_norm(lib, n, sc=None) == EINVAL and call_norm(lib, n, q=None) == EINVAL
+    odd = C.c_void_p(0x10001)
+    for name in ("x", "add", "w", "s", "o", "sc"):
+        assert call_norm(lib, n, **{name: odd}) == EINVAL, name
+    assert call_norm(lib, norm(ld_sum=128), s=P[0]) == EINVAL                      # in place with another stride
+    assert call_norm(lib, norm(rows=0), x=None, w=None) == 0                       # no rows: nothing to do
+
+
+def test_norm_backward_buffers(lib):
+    n = norm()
+    need = lib.mcce_rmsnorm_backward_workspace_bytes(C.byref(n))
+    assert need > 0 and lib.mcce_rmsnorm_backward_workspace_bytes(None) == 0
+
+    def call(dout=P[0], h=P[1], dsum=P[2], w=P[3], dx=P[4], dw=P[5], ws=P[6], nbytes=need, n=n):
+        return lib.mcce_rmsnorm_backward(C.byref(n), dout, h, dsum, w, dx, dw, ws, nbytes, None)
+    for name in ("dout", "h", "w", "dx", "ws"):
+        assert call(**{name: None}) == EINVAL, name
+    odd = C.c_void_p(0x10001)
+    for name in ("dout", "h", "dsum", "w", "dx", "dw", "ws"):
+        assert call(**{name: odd}) == EINVAL, name
+    assert call(nbytes=need - 1) == ENOSPC
+    assert call(dx=P[0], n=norm(ld_sum=128)) == EINVAL and call(dx=P[2], n=norm(ld_sum=128)) == EINVAL
+
+
+BAD_ROWS = [dict(n_layers=0), dict(n_layers=65536), dict(n_tokens=-1), dict(top_k=0), dict(top_k=17), dict(d=0),
+            dict(n_tokens=1 << 28, top_k=8), dict(ld_token=63), dict(ld_rows=1), dict(ld_rows=-64),
+            dict(scale_cols=-1), dict(dtype=3), dict(dtype=-1)]
+
+
+@pytest.mark.parametrize("bad", BAD_ROWS, ids=str)
+def test_rows_descriptor(lib, bad):
+    r = rows(**bad)
+    assert lib.mcce_dispatch_workspace_bytes(C.byref(r)) == 0
+    assert lib.mcce_dispatch(C.byref(r), P[0], P[1], None, P[2], P[3], P[4], P[5], None, P[6], 1 << 30, None) == EINVAL
+    assert lib.mcce_combine(C.byref(r), P[0], P[1], P[2], P[3], P[4], None) == EINVAL
+    assert lib.mcce_combine_backward(C.byref(r), P[0], P[1], P[2], P[3], P[4], P[5], None) == EINVAL
+
+
+def test_dispatch_refusals(lib):
+    def call(sel=P[0], x=P[1], sc=None, off=P[2], perm=P[3], inv=P[4], out=P[5], osc=None, ws=P[6], nbytes=1 << 30, **kw):
+        r = rows(**kw)
+        return lib.mcce_dispatch(C.byref(r), sel, x, sc, off, perm, inv, out, osc, ws, nbytes, None)
+    assert lib.mcce_dispatch_workspace_bytes(None) == 0
+    for name in ("sel", "x", "off", "inv", "out"):
+        assert call(**{name: None}) == EINVAL, name
+    assert call(n_experts=0) == EINVAL and call(n_experts=257) == EINVAL
+    assert call(scale_cols=2) == EINVAL and call(scale_cols=2, sc=P[7]) == EINVAL and call(sc=P[7], osc=P[8]) == EINVAL
+    odd = C.c_void_p(0x10001)
+    for name in ("sel", "x", "off", "perm", "inv", "out"):
+        assert call(**{name: odd}) == EINVAL, name
+    big = dict(n_tokens=100000)
+    need = lib.mcce_dispatch_workspace_bytes(C.byref(rows(**big)))
+    assert need > 0
+    assert call(ws=None, **big) == EINVAL and call(ws=C.c_void_p(0x10004), **big) == EINVAL
+    assert call(nbytes=need - 1, **big) == ENOSPC
+
+
+def test_combine_refusals(lib):
+    odd = C.c_void_p(0x10001)
+
+    def call(rows_=P[0], inv=P[1], w=P[2], add=P[3], y=P[4], **kw):
+        return lib.mcce_combine(C.byref(rows(**kw)), rows_, inv, w, add, y, None)
+    for name in ("rows_", "inv", "y"):
+        assert call(**{name: None}) == EINVAL, name
+    for name in ("rows_", "inv", "w", "add", "y"):
+        assert call(**{name: odd}) == EINVAL, name
+    for bad in (dict(dtype=mb.E4M3), dict(dtype=mb.F32, token_dtype=mb.BF16), dict(token_dtype=mb.E4M3)):
+        assert call(**bad) == EINVAL
+        assert lib.mcce_combine_backward(C.byref(rows(**bad)), P[0], P[1], P[2], P[3], P[4], P[5], None) == EINVAL
+    assert call(n_tokens=0, rows_=None, inv=None, y=None) == 0                     # no tokens: nothing to do
+
+    def back(dy=P[0], rows_=P[1], inv=P[2], w=P[3], dr=P[4], dw=P[5]):
+        return lib.mcce_combine_backward(C.byref(rows()), dy, rows_, inv, w, dr, dw, None)
+    for name in ("dy", "rows_", "inv", "dr"):
+        assert back(**{name: None}) == EINVAL, name
+    for name in ("dy", "rows_", "inv", "w", "dr", "dw"):
+        assert back(**{name: odd}) == EINVAL, name
+    assert lib.mcce_combine_backward(None, P[0], P[1], P[2], P[3], P[4], P[5], None) == EINVAL
+
+
+def test_binding_refuses_cpu_tensors():
+    import torch
+    with pytest.raises(mb.McceError, match="no CPU path"):
+        mb.rmsnorm(torch.zeros(2, 8), torch.ones(8))
+    with pytest.raises(mb.McceError, match="no CPU path"):
+        mb.rmsnorm_backward(torch.zeros(2, 8), torch.zeros(2, 8), torch.ones(8))
+    with pytest.raises(mb.McceError, match="no CPU path"):
+        mb.dispatch(torch.zeros(2, 2, dtype=torch.int32), 4)
+    with pytest.raises(mb.McceError, match="no CPU path"):
+        mb.combine(torch.zeros(4, 8), torch.zeros(2, 2, dtype=torch.int32))
+    with pytest.raises(mb.McceError, match="no CPU path"):
+        mb.combine_backward(torch.zeros(2, 8), torch.zeros(4, 8), torch.zeros(2, 2, dtype=torch.int32))
