@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include "common.cuh"
+#include "tc_common.cuh"
 #include "vec.cuh"
 
 namespace mcce {
@@ -11,50 +12,288 @@ namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
 constexpr int kMaxNormD = 16384;
-constexpr int kThreads = 256;
 constexpr float kE4m3Max = 448.f;
 constexpr uint32_t kAmaxFloor = 0x0d800000u;   // bits of 2^-100
 
+// ---- threads of a row: a power of two up to a warp (several rows per CTA), or the whole CTA -------------------
+struct RowThreads {
+  int tpr, t, slot;   // threads per row, this thread's index in its row, row of the CTA
+  __device__ __forceinline__ explicit RowThreads(int tpr_) : tpr(tpr_) {
+    if (tpr > 32) t = threadIdx.x, slot = 0;
+    else t = threadIdx.x & (tpr - 1), slot = threadIdx.x / (unsigned)tpr;
+  }
+};
+
+template <typename V, typename F>
+__device__ __forceinline__ V row_reduce(V v, int tpr, V* buf, V neutral, F op) {
+  if (tpr < 32) {
+    for (int o = tpr >> 1; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(kFull, v, o));
+    return v;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(kFull, v, o));
+  if (tpr == 32) return v;
+  const int lane = threadIdx.x & 31;
+  if (lane == 0) buf[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = lane < (int)(blockDim.x >> 5) ? buf[lane] : neutral;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(kFull, v, o));
+  return v;
+}
+// buf: one word per warp, not used again before the next barrier
+__device__ __forceinline__ float row_sum(float v, int tpr, float* buf) {
+  return row_reduce(v, tpr, buf, 0.f, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ uint32_t row_max(uint32_t v, int tpr, uint32_t* buf) {
+  return row_reduce(v, tpr, buf, 0u, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+
+// ---- forward ------------------------------------------------------------------------------------------------------
+enum Quant { kQuantRow = 1, kQuantLanes = 2, kQuantShared = 3 };   // how the largest magnitude of a group is found
+
 struct NormArgs {
   int64_t rows, ld_x, ld_add, ld_sum, ld_out, ld_q;
-  int d, group, n_groups, add_f32, weight_f32;
-  float eps;
+  int d, n_groups, group_log2, tpr, off, add_f32, weight_f32;
+  int quant;
+  float eps, inv_d;
   const void *x, *add, *weight;
   void *sum, *out;
   uint8_t* q;
   float* scales;
 };
 
-__device__ __forceinline__ float block_sum(float v, float* buf) {
+// r of the norm (rsqrtf is within 2 units in the last place)
+__device__ __forceinline__ float inv_rms(float sum_sq, float inv_d, float eps) { return rsqrtf(fmaf(sum_sq, inv_d, eps)); }
+// scale of a group from the bits of its largest magnitude, and what its values are multiplied by
+__device__ __forceinline__ float scale_of(uint32_t amax) { return __uint_as_float(amax) * (1.f / kE4m3Max); }
+__device__ __forceinline__ float back_of(float scale) { return __fdividef(1.f, scale); }   // scale is in [2^-109, 2^120]
+
+__device__ __forceinline__ uint8_t e4m3(float v) { return __nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3); }
+template <int N>
+__device__ __forceinline__ void store_e4m3(uint8_t* p, const float2 (&v)[N]) {
+  __nv_fp8x2_storage_t e[N];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
-  __syncthreads();
-  float s = 0.f;
-  for (int i = 0; i < kThreads / 32; ++i) s += buf[i];
-  return s;
+  for (int j = 0; j < N; ++j) e[j] = __nv_cvt_float2_to_fp8x2(v[j], __NV_SATFINITE, __NV_E4M3);
+  typename RawOf<2 * N>::type raw;
+  memcpy(&raw, e, sizeof(raw));
+  *(typename RawOf<2 * N>::type*)p = raw;
 }
+__device__ __forceinline__ uint32_t magnitude(float n) { return __float_as_uint(fabsf(n)); }   // NaN above everything
+
+// A row is read once: its units stay in registers from the addition to the last output, VPT of them per thread, so
+// that a thread has all its loads in flight before the point where the threads of a row meet.
+// RAGGED: rows start anywhere.  The units are those of the memory, up to U - 1 elements before the first and behind
+// the last one are single elements of the row's first U threads.
+template <typename T, typename A, typename W, int VPT, bool RAGGED>
+__global__ void __launch_bounds__(512) rmsnorm_kernel(const __grid_constant__ NormArgs a) {
+  constexpr int U = 16 / (int)sizeof(T);
+  __shared__ float buf[32];
+  __shared__ uint32_t buf_max[32];
+  __shared__ uint32_t amax[RAGGED ? kMaxNormD / 32 : 1];
+  const RowThreads th(a.tpr);
+  const int64_t r = a.tpr > 32 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (blockDim.x / a.tpr) + th.slot;
+  const int d = r < a.rows ? a.d : 0;
+  const int head = RAGGED ? min(d, (int)(-(r * a.ld_x + a.off) & (U - 1))) : 0;
+  const int whole = RAGGED ? (d - head) & ~(U - 1) : d;   // columns in units
+  const int c0 = th.t * U, step = a.tpr * U;
+  bool in[VPT];
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) in[i] = c0 + i * step < whole;
+  if (RAGGED && a.quant == kQuantShared) {
+    for (int g = threadIdx.x; g < (int)(blockDim.x / a.tpr) * a.n_groups; g += blockDim.x) amax[g] = kAmaxFloor;
+    __syncthreads();
+  }
+
+  // ---- h = x + add ------------------------------------------------------------------------------------------------
+  Pack<T, U> h[VPT];
+  const T* xr = (const T*)a.x + r * a.ld_x;
+  const A* ar = (const A*)a.add + r * a.ld_add;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    h[i].zero();
+    if (in[i]) h[i].load(xr + head + c0 + i * step);
+  }
+  if (a.add) {
+    Pack<A, U> y[VPT];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      y[i].zero();
+      if (in[i]) y[i].load(ar + head + c0 + i * step);
+    }
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      float2 v[U / 2], w[U / 2];
+      h[i].get(v);
+      y[i].get(w);
+#pragma unroll
+      for (int j = 0; j < U / 2; ++j) v[j] = add2(v[j], w[j]);
+      h[i].set(v);
+    }
+  }
+  // single elements: column t of the head, column t behind the units
+  const int tail = head + whole + th.t;
+  const bool in_head = RAGGED && th.t < head, in_tail = RAGGED && tail < d;
+  float h_head = 0.f, h_tail = 0.f;
+  if (RAGGED) {
+    auto one = [&](int c) {
+      const float v = wide(xr[c]);
+      return a.add ? wide(narrow<T>(v + wide(ar[c]))) : v;
+    };
+    if (in_head) h_head = one(th.t);
+    if (in_tail) h_tail = one(tail);
+  }
+  float2 ss2 = make_float2(h_head * h_head, h_tail * h_tail);
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    float2 v[U / 2];
+    h[i].get(v);
+#pragma unroll
+    for (int j = 0; j < U / 2; ++j) ss2 = fma2(v[j], v[j], ss2);
+  }
+  const float ss = ss2.x + ss2.y;
+  if (a.sum) {
+    T* sum = (T*)a.sum + r * a.ld_sum;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+      if (in[i]) h[i].store(sum + head + c0 + i * step);
+    if (in_head) sum[th.t] = narrow<T>(h_head);
+    if (in_tail) sum[tail] = narrow<T>(h_tail);
+  }
+  if (!a.out && !a.q) return;
+
+  // ---- n = h r weight ---------------------------------------------------------------------------------------------
+  const W* weight = (const W*)a.weight;
+  Pack<W, U> w[VPT];
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    w[i].zero();
+    if (in[i]) {
+      if constexpr (RAGGED) load_anywhere(w[i], weight + head + c0 + i * step, weight, weight + a.d);
+      else w[i].load_const(weight + c0 + i * step);
+    }
+  }
+  const float w_head = in_head ? wide(weight[th.t]) : 0.f, w_tail = in_tail ? wide(weight[tail]) : 0.f;
+  const float inv = inv_rms(row_sum(ss, a.tpr, buf), a.inv_d, a.eps);
+  const float n_head = h_head * inv * w_head, n_tail = h_tail * inv * w_tail;
+  auto norm_unit = [&](int i, float2 (&n)[U / 2]) {
+    float2 wv[U / 2];
+    h[i].get(n);
+    w[i].get(wv);
+#pragma unroll
+    for (int j = 0; j < U / 2; ++j) n[j] = mul2(mul2(n[j], both(inv)), wv[j]);
+  };
+  if (a.out) {
+    T* out = (T*)a.out + r * a.ld_out;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      float2 n[U / 2];
+      norm_unit(i, n);
+      Pack<T, U> o;
+      o.set(n);
+      if (in[i]) o.store(out + head + c0 + i * step);
+    }
+    if (in_head) out[th.t] = narrow<T>(n_head);
+    if (in_tail) out[tail] = narrow<T>(n_tail);
+  }
+  if (!a.q) return;
+
+  // ---- 8-bit rows -------------------------------------------------------------------------------------------------
+  uint8_t* q = a.q + r * a.ld_q;
+  float* scales = a.scales + r * a.n_groups;
+  if (a.quant == kQuantRow) {
+    uint32_t top = max(kAmaxFloor, max(magnitude(n_head), magnitude(n_tail)));
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      float2 n[U / 2];
+      norm_unit(i, n);
+#pragma unroll
+      for (int j = 0; j < U / 2; ++j) top = max(top, max(magnitude(n[j].x), magnitude(n[j].y)));
+    }
+    const float sc = scale_of(row_max(top, a.tpr, buf_max)), back = back_of(sc);
+    if (d && th.t == 0) scales[0] = sc;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      float2 n[U / 2];
+      norm_unit(i, n);
+#pragma unroll
+      for (int j = 0; j < U / 2; ++j) n[j] = mul2(n[j], both(back));
+      if (in[i]) store_e4m3(q + head + c0 + i * step, n);
+    }
+    if (in_head) q[th.t] = e4m3(n_head * back);
+    if (in_tail) q[tail] = e4m3(n_tail * back);
+  } else if (!RAGGED) {
+    // a group is a power of two of neighbouring lanes
+    const int lanes = (1 << a.group_log2) / U;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      float2 n[U / 2];
+      norm_unit(i, n);
+      uint32_t m = kAmaxFloor;
+#pragma unroll
+      for (int j = 0; j < U / 2; ++j) m = max(m, max(magnitude(n[j].x), magnitude(n[j].y)));
+      for (int o = lanes >> 1; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(kFull, m, o));
+      const float sc = scale_of(m), back = back_of(sc);
+#pragma unroll
+      for (int j = 0; j < U / 2; ++j) n[j] = mul2(n[j], both(back));
+      if (in[i]) {
+        store_e4m3(q + c0 + i * step, n);
+        if ((th.t & (lanes - 1)) == 0) scales[(c0 + i * step) >> a.group_log2] = sc;
+      }
+    }
+  } else {
+    // a unit's columns may belong to two groups
+    uint32_t* m = amax + th.slot * a.n_groups;
+    if (in_head) atomicMax(m, magnitude(n_head));   // the head is shorter than a group
+    if (in_tail) atomicMax(m + (tail >> a.group_log2), magnitude(n_tail));
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      if (!in[i]) continue;
+      float2 n[U / 2];
+      norm_unit(i, n);
+      const int c = head + c0 + i * step, g = c >> a.group_log2, cut = ((g + 1) << a.group_log2) - c;
+      uint32_t lo = 0, hi = 0;
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const uint32_t v = magnitude(j & 1 ? n[j / 2].y : n[j / 2].x);
+        if (j < cut) lo = max(lo, v);
+        else hi = max(hi, v);
+      }
+      atomicMax(m + g, lo);
+      if (cut < U) atomicMax(m + g + 1, hi);
+    }
+    __syncthreads();
+    if (d)
+      for (int g = th.t; g < a.n_groups; g += a.tpr) scales[g] = scale_of(m[g]);
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      if (!in[i]) continue;
+      float2 n[U / 2];
+      norm_unit(i, n);
+      const int c = head + c0 + i * step, g = c >> a.group_log2, cut = ((g + 1) << a.group_log2) - c;
+      const float b0 = back_of(scale_of(m[g])), b1 = cut < U ? back_of(scale_of(m[g + 1])) : b0;
+#pragma unroll
+      for (int j = 0; j < U / 2; ++j) n[j] = mul2(n[j], make_float2(2 * j < cut ? b0 : b1, 2 * j + 1 < cut ? b0 : b1));
+      store_e4m3(q + c, n);
+    }
+    if (in_head) q[th.t] = e4m3(n_head * back_of(scale_of(m[0])));
+    if (in_tail) q[tail] = e4m3(n_tail * back_of(scale_of(m[tail >> a.group_log2])));
+  }
+}
+
+// Tensors whose rows are not aligned alike (views with odd offsets or strides): element by element, three passes over a
+// row, which comes back from L1 in the second and third.
+constexpr int kThreads = 256;
 
 template <typename T>
 __device__ __forceinline__ float get1(const void* p, int64_t i, int f32) {
   if (f32 || sizeof(T) == 4) return ((const float*)p)[i];
   return __bfloat162float(((const __nv_bfloat16*)p)[i]);
 }
-template <typename T>
-__device__ __forceinline__ T round1(float v) {
-  if constexpr (sizeof(T) == 2) return __float2bfloat16_rn(v);
-  else return v;
-}
-template <typename T>
-__device__ __forceinline__ float wide1(T v) {
-  if constexpr (sizeof(T) == 2) return __bfloat162float(v);
-  else return v;
-}
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) rmsnorm_kernel(const NormArgs a) {
-  __shared__ float buf[kThreads / 32];
+__global__ void __launch_bounds__(kThreads) rmsnorm_scalar_kernel(const __grid_constant__ NormArgs a) {
+  __shared__ float buf[32];
   __shared__ uint32_t amax[kMaxNormD / 32];
   const int64_t r = blockIdx.x;
   const T* x = (const T*)a.x + r * a.ld_x;
@@ -62,77 +301,437 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_kernel(const NormArgs a) {
   for (int g = threadIdx.x; g < a.n_groups; g += kThreads) amax[g] = kAmaxFloor;
   float ss = 0.f;
   for (int j = threadIdx.x; j < a.d; j += kThreads) {
-    float h = wide1(x[j]);
-    if (a.add) h = wide1(round1<T>(h + get1<T>(a.add, r * a.ld_add + j, a.add_f32)));
-    if (sum) sum[j] = round1<T>(h);
+    float h = wide(x[j]);
+    if (a.add) h = wide(narrow<T>(h + get1<T>(a.add, r * a.ld_add + j, a.add_f32)));
+    if (sum) sum[j] = narrow<T>(h);
     ss = fmaf(h, h, ss);
   }
-  const float inv = 1.f / sqrtf(block_sum(ss, buf) / (float)a.d + a.eps);
+  const float inv = inv_rms(row_sum(ss, kThreads, buf), a.inv_d, a.eps);
   auto n_at = [&](int j) {
-    float h = sum ? wide1(sum[j]) : wide1(x[j]);
-    if (!sum && a.add) h = wide1(round1<T>(h + get1<T>(a.add, r * a.ld_add + j, a.add_f32)));
+    float h = sum ? wide(sum[j]) : wide(x[j]);
+    if (!sum && a.add) h = wide(narrow<T>(h + get1<T>(a.add, r * a.ld_add + j, a.add_f32)));
     return h * inv * get1<T>(a.weight, j, a.weight_f32);
   };
   for (int j = threadIdx.x; j < a.d; j += kThreads) {
     const float n = n_at(j);
-    if (a.out) ((T*)a.out)[r * a.ld_out + j] = round1<T>(n);
-    if (a.q) atomicMax(&amax[j / a.group], __float_as_uint(fabsf(n)));
+    if (a.out) ((T*)a.out)[r * a.ld_out + j] = narrow<T>(n);
+    if (a.q) atomicMax(&amax[j >> a.group_log2], magnitude(n));
   }
   if (!a.q) return;
   __syncthreads();
-  for (int g = threadIdx.x; g < a.n_groups; g += kThreads)
-    a.scales[r * a.n_groups + g] = __uint_as_float(amax[g]) / kE4m3Max;
-  for (int j = threadIdx.x; j < a.d; j += kThreads) {
-    const float s = __uint_as_float(amax[j / a.group]) / kE4m3Max;
-    a.q[r * a.ld_q + j] = __nv_cvt_float_to_fp8(n_at(j) / s, __NV_SATFINITE, __NV_E4M3);
+  for (int g = threadIdx.x; g < a.n_groups; g += kThreads) a.scales[r * a.n_groups + g] = scale_of(amax[g]);
+  for (int j = threadIdx.x; j < a.d; j += kThreads)
+    a.q[r * a.ld_q + j] = e4m3(n_at(j) * back_of(scale_of(amax[j >> a.group_log2])));
+}
+
+// How a row is laid over threads: `vpt` units for each of tpr threads.
+struct NormShape {
+  int tpr, vpt, threads;
+};
+
+int pow2_up(int v) {
+  int p = 1;
+  while (p < v) p *= 2;
+  return p;
+}
+
+NormShape shape_for(int units, int vpt, int least) {
+  const int need = (units + vpt - 1) / vpt > least ? (units + vpt - 1) / vpt : least;
+  NormShape s;
+  s.vpt = vpt;
+  s.tpr = need > 32 ? (need + 31) / 32 * 32 : pow2_up(need);
+  s.threads = s.tpr > 32 ? s.tpr : 128;
+  return s;
+}
+
+template <typename T, typename A, typename W, int VPT>
+cudaError_t launch_norm(NormArgs a, bool ragged, const NormShape& sh, cudaStream_t st) {
+  a.tpr = sh.tpr;
+  a.quant = !a.q ? 0 : a.n_groups == 1 ? kQuantRow : ragged ? kQuantShared : kQuantLanes;
+  const int rpb = sh.threads / a.tpr;
+  const unsigned grid = (unsigned)((a.rows + rpb - 1) / rpb);
+  if (ragged) rmsnorm_kernel<T, A, W, VPT, true><<<grid, sh.threads, 0, st>>>(a);
+  else rmsnorm_kernel<T, A, W, VPT, false><<<grid, sh.threads, 0, st>>>(a);
+  return cudaGetLastError();
+}
+template <typename T, typename A, typename W>
+cudaError_t launch_norm_vpt(const NormArgs& a, bool ragged, const NormShape& sh, cudaStream_t st) {
+  constexpr int kWide = sizeof(T) == 4 ? 8 : 4;
+  if (sh.vpt == 2) return launch_norm<T, A, W, 2>(a, ragged, sh, st);
+  return launch_norm<T, A, W, kWide>(a, ragged, sh, st);
+}
+cudaError_t launch_norm_types(const NormArgs& a, int dtype, bool ragged, const NormShape& sh, cudaStream_t st) {
+  using B = __nv_bfloat16;
+  if (dtype == MCCE_F32) return launch_norm_vpt<float, float, float>(a, ragged, sh, st);
+  if (a.add && a.add_f32) return a.weight_f32 ? launch_norm_vpt<B, float, float>(a, ragged, sh, st)
+                                              : launch_norm_vpt<B, float, B>(a, ragged, sh, st);
+  return a.weight_f32 ? launch_norm_vpt<B, B, float>(a, ragged, sh, st) : launch_norm_vpt<B, B, B>(a, ragged, sh, st);
+}
+
+// Two units per thread; 64 bytes of every tensor per thread (4 units of bf16, 8 of fp32) where two would need more than 512
+// threads for a row, and for many wide ragged rows, whose single elements and shifted weights cost a thread the
+// same for two units as for four.  Measured with the residual's addition, us, two / wide: 16384 x 4096 bf16 83.9 / 85.0
+// (0.98 of the copy bandwidth), with 8-bit rows 16384 x 2048 60.9 / 62.7, 131072 x 64 13.2 / 17.2; ragged 16384 x 4097 with 8-bit
+// rows 152 / 150, 16384 x 4098 101 / 99, 16384 x 4097 fp32 191 / 184 (between two events: 5 us are not the kernel's).
+// One unit per thread: 16384 x 4096 98.8, a single row of 2048 7.2 against 7.3.
+NormShape norm_shape(int64_t rows, int d, bool ragged, int elem_bytes, int group_log2) {
+  const int u = 16 / elem_bytes, units = d / u;
+  // a group of columns has to fit the lanes of one unit step; a ragged row needs a thread for every single element
+  const int least = ragged ? u : group_log2 < 30 ? (1 << group_log2) / u : 1;
+  const bool two = units <= 1024 && !(ragged && rows > 4096 && units > 256);
+  return shape_for(units, two ? 2 : elem_bytes == 4 ? 8 : 4, least);
+}
+
+// ---- gradient -----------------------------------------------------------------------------------------------------
+struct NormGradArgs {
+  int64_t rows, ld_dout, ld_h, ld_dsum, ld_dx;
+  int d, weight_f32, tpr, off, stages;
+  float eps, inv_d;
+  const void *dout, *h, *dsum, *weight;
+  void* dx;
+  float* part;   // [CTAs, d], or null: the weight's gradient is not wanted
+};
+
+// Both sums at once: the lower half of a group of lanes ends up with x, the upper half with y.
+__device__ __forceinline__ float half_sum2(float2 v, int lanes) {
+  const bool upper = threadIdx.x & (lanes >> 1);
+  const float got = __shfl_xor_sync(kFull, upper ? v.x : v.y, lanes >> 1);
+  float s = (upper ? v.y : v.x) + got;
+  for (int o = lanes >> 2; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+  return s;
+}
+__device__ __forceinline__ float2 row_sum2(float2 v, int tpr, float* buf) {   // buf: two words per warp
+  const int lane = threadIdx.x & 31;
+  if (tpr == 1) return v;
+  if (tpr < 32) {
+    const float s = half_sum2(v, tpr), other = __shfl_xor_sync(kFull, s, tpr >> 1);
+    return lane & (tpr >> 1) ? make_float2(other, s) : make_float2(s, other);
+  }
+  float s = half_sum2(v, 32);
+  if (tpr > 32) {   // sixteen warps at most: x of warp w in buf[w], y in buf[16 + w]
+    if ((lane & 15) == 0) buf[(lane & 16) + (threadIdx.x >> 5)] = s;
+    __syncthreads();
+    s = (lane & 15) < (int)(blockDim.x >> 5) ? buf[lane] : 0.f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+  }
+  return make_float2(__shfl_sync(kFull, s, 0), __shfl_sync(kFull, s, 16));
+}
+
+// 16 bytes from global to shared memory without passing through registers.  A thread reads only what it copied itself,
+// so waiting for its own copies is all the order that is needed.
+__device__ __forceinline__ void copy16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// A CTA takes rows blockIdx.x, + gridDim.x, ... (times the rows it holds at once).  The rows come through a ring of
+// `stages` slots in shared memory, filled stages - 1 rows ahead: a row's two passes (the sums, then dx) hang on one
+// another through a reduction over its threads, and only copies that are under way meanwhile keep the memory busy.
+// RAGGED: the step between a thread's rows is a multiple of U (or it has one row), so that every one of its rows starts at
+// the same place in a unit.  A thread therefore has the same columns in all its rows, aligned or not, and keeps their
+// weights and its part of the weights' gradient in registers.
+// Bound: HBM for aligned rows (16384 x 2048 bf16 with dsum: 42 us = 0.97 of the copy bandwidth, with the weight's gradient and
+// the second launch 43); ragged rows issue (16384 x 4097: 120 us = 0.68).  With the row in registers instead of the ring, loaded
+// when it was needed, the first took 62 us; with columns that move from row to row and sums in shared memory the second 148.
+template <typename T, typename W, int VPT, bool RAGGED>
+__global__ void __launch_bounds__(512) rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a) {
+  constexpr int U = 16 / (int)sizeof(T);
+  extern __shared__ __align__(16) uint8_t smem[];   // the ring; at the end [rows per CTA][d] sums
+  __shared__ float buf[2][32];
+  const RowThreads th(a.tpr);
+  const int rpb = blockDim.x / a.tpr;
+  const int64_t stride = (int64_t)gridDim.x * rpb, first = (int64_t)blockIdx.x * rpb + th.slot;
+  const int head = RAGGED ? min(a.d, (int)(-(first * a.ld_h + a.off) & (U - 1))) : 0;
+  const int whole = RAGGED ? (a.d - head) & ~(U - 1) : a.d;
+  const int c0 = th.t * U, step = a.tpr * U;
+  bool in[VPT];
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) in[i] = c0 + i * step < whole;
+  const int tensor_bytes = VPT * (int)blockDim.x * 16, stage_bytes = (a.dsum ? 3 : 2) * tensor_bytes;
+  uint8_t* ring = smem + threadIdx.x * 16;
+
+  const W* weight = (const W*)a.weight;
+  float2 w[VPT][U / 2], dw[VPT][U / 2];
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    Pack<W, U> p;
+    p.zero();
+    if (in[i]) {
+      if constexpr (RAGGED) load_anywhere(p, weight + head + c0 + i * step, weight, weight + a.d);
+      else p.load_const(weight + c0 + i * step);
+    }
+    p.get(w[i]);
+#pragma unroll
+    for (int j = 0; j < U / 2; ++j) dw[i][j] = both(0.f);
+  }
+  // single elements of a ragged row, of its first U threads: one before the units, one behind them
+  const int tail = head + whole + th.t;
+  const bool edges = RAGGED && th.t < U;
+  const bool there[2] = {RAGGED && th.t < head, RAGGED && tail < a.d};
+  const int col[2] = {th.t, tail};
+  const float we[2] = {there[0] ? wide(weight[col[0]]) : 0.f, there[1] ? wide(weight[col[1]]) : 0.f};
+  float dwe[2] = {0.f, 0.f};
+  struct Edge {
+    T h[2], g[2], s[2];   // as loaded: converting would wait for them
+  } edge{}, next{};
+  auto fetch_edge = [&](int64_t r) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (there[k] && r < a.rows) {
+        next.h[k] = ((const T*)a.h)[r * a.ld_h + col[k]];
+        next.g[k] = ((const T*)a.dout)[r * a.ld_dout + col[k]];
+        if (a.dsum) next.s[k] = ((const T*)a.dsum)[r * a.ld_dsum + col[k]];
+      }
+  };
+  auto fetch = [&](int64_t r, int stage) {
+    const bool row = r < a.rows;
+    const int64_t rr = row ? r : 0;
+    const int at = RAGGED && !row ? 0 : head;   // (another row's phase would leave the address unaligned)
+    const T *hr = (const T*)a.h + rr * a.ld_h + at, *gr = (const T*)a.dout + rr * a.ld_dout + at;
+    const T* sr = (const T*)a.dsum + rr * a.ld_dsum + at;
+    uint8_t* to = ring + stage * stage_bytes;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      if (!(row && in[i])) {   // what such a unit holds is never used, but has to be finite for the sums
+        *(uint4*)(to + i * (int)blockDim.x * 16) = *(uint4*)(to + tensor_bytes + i * (int)blockDim.x * 16) = make_uint4(0, 0, 0, 0);
+        continue;
+      }
+      const int c = c0 + i * step;
+      copy16(to + i * (int)blockDim.x * 16, hr + c);
+      copy16(to + tensor_bytes + i * (int)blockDim.x * 16, gr + c);
+      if (a.dsum) copy16(to + 2 * tensor_bytes + i * (int)blockDim.x * 16, sr + c);
+    }
+  };
+
+  for (int k = 0; k < a.stages - 1; ++k) {
+    fetch(first + k * stride, k);
+    copies_commit();
+  }
+  if (edges) fetch_edge(first);
+  int stage = 0, par = 0;
+  for (int64_t base = (int64_t)blockIdx.x * rpb; base < a.rows; base += stride, par ^= 1) {
+    const int64_t r = base + th.slot;
+    int into = stage + a.stages - 1;
+    if (into >= a.stages) into -= a.stages;
+    fetch(r + (a.stages - 1) * stride, into);
+    copies_commit();
+    float2 sum = both(0.f);   // of h^2, of h g
+    if (edges) {
+      edge = next;
+      fetch_edge(r + stride);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const float he = wide(edge.h[k]);
+        sum.x = fmaf(he, he, sum.x);
+        sum.y = fmaf(he, wide(edge.g[k]) * we[k], sum.y);
+      }
+    }
+    if (a.stages == 1) copies_wait<0>();
+    else if (a.stages == 2) copies_wait<1>();
+    else copies_wait<2>();
+    const uint8_t* row = ring + stage * stage_bytes;
+    float2 hh = both(0.f), hg = both(0.f);
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      Pack<T, U> h, g;
+      h.load((const T*)(row + i * (int)blockDim.x * 16)), g.load((const T*)(row + tensor_bytes + i * (int)blockDim.x * 16));
+      float2 hv[U / 2], gv[U / 2];
+      h.get(hv), g.get(gv);
+#pragma unroll
+      for (int j = 0; j < U / 2; ++j) {
+        hh = fma2(hv[j], hv[j], hh);
+        hg = fma2(hv[j], mul2(gv[j], w[i][j]), hg);
+      }
+    }
+    sum.x += hh.x + hh.y, sum.y += hg.x + hg.y;
+    sum = row_sum2(sum, a.tpr, buf[par]);
+    // dx = r g - (h r) (r^2 mean(h g)) + dsum
+    const float inv = r < a.rows ? inv_rms(sum.x, a.inv_d, a.eps) : 0.f, coef = -inv * inv * (sum.y * a.inv_d);
+    T* xr = (T*)a.dx + r * a.ld_dx + head;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      Pack<T, U> h, g, o;
+      h.load((const T*)(row + i * (int)blockDim.x * 16)), g.load((const T*)(row + tensor_bytes + i * (int)blockDim.x * 16));
+      o.zero();
+      if (a.dsum) o.load((const T*)(row + 2 * tensor_bytes + i * (int)blockDim.x * 16));
+      float2 hv[U / 2], gv[U / 2], v[U / 2];
+      h.get(hv), g.get(gv), o.get(v);
+#pragma unroll
+      for (int j = 0; j < U / 2; ++j) {
+        const float2 n = mul2(hv[j], both(inv));
+        dw[i][j] = fma2(gv[j], n, dw[i][j]);
+        v[j] = fma2(mul2(gv[j], w[i][j]), both(inv), fma2(n, both(coef), v[j]));
+      }
+      o.set(v);
+      if (in[i] && r < a.rows) o.store(xr + c0 + i * step);
+    }
+    if (edges && r < a.rows) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (!there[k]) continue;
+        const float he = wide(edge.h[k]), ge = wide(edge.g[k]);
+        xr[col[k] - head] = narrow<T>(fmaf(ge * we[k], inv, fmaf(he * inv, coef, a.dsum ? wide(edge.s[k]) : 0.f)));
+        dwe[k] = fmaf(ge, he * inv, dwe[k]);
+      }
+    }
+    if (++stage == a.stages) stage = 0;
+  }
+  copies_wait<0>();
+  if (!a.part) return;
+  float* part = a.part + (int64_t)blockIdx.x * a.d;
+  if (!RAGGED && rpb == 1) {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+      if (in[i])
+#pragma unroll
+        for (int j = 0; j < U / 2; j += 2)
+          *(float4*)(part + c0 + i * step + 2 * j) = make_float4(dw[i][j].x, dw[i][j].y, dw[i][j + 1].x, dw[i][j + 1].y);
+    return;
+  }
+  // several rows at once, or units across the columns' alignment: together through shared memory
+  __syncthreads();
+  float* mine = (float*)smem + (size_t)th.slot * a.d;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i)
+    if (in[i])
+#pragma unroll
+      for (int j = 0; j < U / 2; ++j) {
+        float* p = mine + head + c0 + i * step + 2 * j;
+        p[0] = dw[i][j].x, p[1] = dw[i][j].y;
+      }
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if (there[k]) mine[col[k]] = dwe[k];
+  __syncthreads();
+  for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
+    float v = 0.f;
+    for (int k = 0; k < rpb; ++k) v += ((const float*)smem)[(size_t)k * a.d + c];
+    part[c] = v;
   }
 }
 
-struct NormGradArgs {
-  int64_t rows, ld_dout, ld_h, ld_dsum, ld_dx;
-  int d, weight_f32, parts;
-  float eps;
-  const void *dout, *h, *dsum, *weight;
-  void* dx;
-  float* part;   // [parts, d]
-};
-
+// Tensors whose rows are not aligned alike: element by element, twice over a row.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) rmsnorm_grad_kernel(const NormGradArgs a) {
-  __shared__ float buf[kThreads / 32];
+__global__ void __launch_bounds__(kThreads) rmsnorm_grad_scalar_kernel(const __grid_constant__ NormGradArgs a) {
+  __shared__ float buf[2][32];
   float* part = a.part ? a.part + (int64_t)blockIdx.x * a.d : nullptr;
   if (part)
     for (int j = threadIdx.x; j < a.d; j += kThreads) part[j] = 0.f;
-  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+  int par = 0;
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, par ^= 1) {
     const T *g = (const T*)a.dout + r * a.ld_dout, *h = (const T*)a.h + r * a.ld_h;
-    float ss = 0.f, sg = 0.f;
+    float2 s = make_float2(0.f, 0.f);
     for (int j = threadIdx.x; j < a.d; j += kThreads) {
-      const float hj = wide1(h[j]);
-      ss = fmaf(hj, hj, ss);
-      sg = fmaf(hj, wide1(g[j]) * get1<T>(a.weight, j, a.weight_f32), sg);
+      const float hj = wide(h[j]);
+      s.x = fmaf(hj, hj, s.x);
+      s.y = fmaf(hj, wide(g[j]) * get1<T>(a.weight, j, a.weight_f32), s.y);
     }
-    const float inv = 1.f / sqrtf(block_sum(ss, buf) / (float)a.d + a.eps);
-    const float coef = inv * inv * inv * (block_sum(sg, buf) / (float)a.d);
+    s = row_sum2(s, kThreads, buf[par]);
+    const float inv = inv_rms(s.x, a.inv_d, a.eps), coef = inv * inv * inv * (s.y * a.inv_d);
     for (int j = threadIdx.x; j < a.d; j += kThreads) {
-      const float hj = wide1(h[j]), gj = wide1(g[j]);
-      float v = inv * (gj * get1<T>(a.weight, j, a.weight_f32)) - hj * coef;
-      if (a.dsum) v += wide1(((const T*)a.dsum)[r * a.ld_dsum + j]);
-      ((T*)a.dx)[r * a.ld_dx + j] = round1<T>(v);
-      if (part) part[j] += gj * (hj * inv);
+      const float hj = wide(h[j]), gj = wide(g[j]);
+      float v = fmaf(inv, gj * get1<T>(a.weight, j, a.weight_f32), -hj * coef);
+      if (a.dsum) v += wide(((const T*)a.dsum)[r * a.ld_dsum + j]);
+      ((T*)a.dx)[r * a.ld_dx + j] = narrow<T>(v);
+      if (part) part[j] = fmaf(gj, hj * inv, part[j]);
     }
   }
 }
 
-__global__ void dweight_kernel(const float* part, float* dweight, int parts, int d) {
-  const int j = blockIdx.x * blockDim.x + threadIdx.x;
-  if (j >= d) return;
+// dweight = the sum of the parts, in a fixed order: 32 columns per CTA, a warp takes every 32nd part.
+__global__ void __launch_bounds__(1024) dweight_kernel(const float* part, float* dweight, int parts, int d) {
+  __shared__ float sum[32][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   float s = 0.f;
-  for (int p = 0; p < parts; ++p) s += part[(int64_t)p * d + j];
-  dweight[j] = s;
+  cudaGridDependencySynchronize();   // launched before the kernel that writes the parts has ended
+  if (c < d) {
+#pragma unroll 8
+    for (int p = warp; p < parts; p += 32) s += part[(int64_t)p * d + c];
+  }
+  sum[warp][lane] = s;
+  __syncthreads();
+  s = sum[lane][warp];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+  if (lane == 0 && blockIdx.x * 32 + warp < d) dweight[blockIdx.x * 32 + warp] = s;
 }
 
-constexpr int kMaxParts = 592;
-int grad_parts(const mcce_norm& n) { return n.rows < kMaxParts ? (int)n.rows : kMaxParts; }
+cudaError_t launch_dweight(const float* part, float* dweight, int parts, int d, cudaStream_t st) {
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((d + 31) / 32), cfg.blockDim = dim3(1024), cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, dweight_kernel, part, dweight, parts, d);
+}
+
+constexpr int kSms = 148;
+
+struct GradShape {
+  NormShape s;
+  int ctas;     // also the number of parts
+  int stages;
+  size_t smem;
+};
+constexpr size_t kGradSmemMost = 226 * 1024;   // dynamic; the reduction buffers are static
+
+// Shared memory of the gradient kernel with a ring of `stages` rows (the layout of its declaration).
+size_t grad_smem(const NormShape& s, int stages, int d, bool ragged, bool dsum, bool dweight) {
+  const size_t ring = (size_t)stages * (dsum ? 3 : 2) * s.vpt * s.threads * 16, rpb = s.threads / s.tpr;
+  const size_t sums = dweight && (ragged || rpb > 1) ? rpb * d * 4 : 0;
+  return ring > sums ? ring : sums;
+}
+
+GradShape grad_shape(int64_t rows, int d, Layout3 lay, int elem_bytes, bool dsum, bool dweight) {
+  GradShape g;
+  if (lay == kScalar) {
+    g.s = NormShape{kThreads, 1, kThreads};
+    g.ctas = (int)(rows < 4 * kSms ? rows : 4 * kSms);
+    return g;
+  }
+  const bool ragged = lay == kRagged;
+  const int u = 16 / elem_bytes, units = d / u;
+  g.s = shape_for(units, units <= 1024 ? 2 : elem_bytes == 4 ? 8 : 4, ragged ? u : 1);
+  const int rpb = g.s.threads / g.s.tpr;
+  const int64_t all = (rows + rpb - 1) / rpb;
+  const int per_sm = 512 / g.s.threads < 1 ? 1 : 512 / g.s.threads;
+  g.stages = 3;
+  while (g.stages > 1 && grad_smem(g.s, g.stages, d, ragged, dsum, dweight) > kGradSmemMost / per_sm) --g.stages;
+  g.smem = grad_smem(g.s, g.stages, d, ragged, dsum, dweight);
+  int ctas = per_sm * kSms;
+  if (ragged) ctas = ctas / u * u;   // rows of a CTA: a multiple of u apart
+  g.ctas = (int)(all < ctas ? all : ctas);
+  return g;
+}
+int parts_most(const mcce_norm& n) {
+  const int64_t most = 8 * kSms;
+  return (int)(n.rows < 1 ? 1 : n.rows < most ? n.rows : most);
+}
+
+template <typename T, typename W, int VPT, bool RAGGED>
+cudaError_t launch_grad(NormGradArgs a, const GradShape& g, cudaStream_t st) {
+  static int cache[64] = {0};   // per kernel
+  int sms = 0;
+  const cudaError_t e = tc::sm_count_and_smem_optin(rmsnorm_grad_kernel<T, W, VPT, RAGGED>, kGradSmemMost, cache, &sms);
+  if (e != cudaSuccess) return e;
+  a.tpr = g.s.tpr, a.stages = g.stages;
+  rmsnorm_grad_kernel<T, W, VPT, RAGGED><<<g.ctas, g.s.threads, g.smem, st>>>(a);
+  return cudaGetLastError();
+}
+template <typename T, typename W>
+cudaError_t launch_grad_vpt(const NormGradArgs& a, bool ragged, const GradShape& g, cudaStream_t st) {
+  constexpr int kWide = sizeof(T) == 4 ? 8 : 4;
+  if (g.s.vpt == 2) return ragged ? launch_grad<T, W, 2, true>(a, g, st) : launch_grad<T, W, 2, false>(a, g, st);
+  return ragged ? launch_grad<T, W, kWide, true>(a, g, st) : launch_grad<T, W, kWide, false>(a, g, st);
+}
+cudaError_t launch_grad_types(const NormGradArgs& a, int dtype, bool ragged, const GradShape& g, cudaStream_t st) {
+  using B = __nv_bfloat16;
+  if (dtype == MCCE_F32) return launch_grad_vpt<float, float>(a, ragged, g, st);
+  return a.weight_f32 ? launch_grad_vpt<B, float>(a, ragged, g, st) : launch_grad_vpt<B, B>(a, ragged, g, st);
+}
 
 bool stride_ok(int64_t ld, int d) { return ld == 0 || ld >= d; }
 
@@ -163,38 +762,54 @@ extern "C" int mcce_rmsnorm(const mcce_norm* n, const void* x, const void* add, 
   if (add && n->add_dtype != MCCE_F32 && n->add_dtype != n->dtype) return MCCE_EINVAL;
   const int g = n->quant_group;
   if (q && ((g != 0 && g != 32 && g != 64 && g != 128) || !stride_ok(n->ld_q, n->d))) return MCCE_EINVAL;
-  const size_t e = elem(n->dtype);
-  if (!aligned(x, e) || !aligned(sum, e) || !aligned(out, e) || !aligned(weight, elem(n->weight_dtype)) ||
-      (add && !aligned(add, elem(n->add_dtype))) || !aligned(scales, 4))
+  const int e = elem(n->dtype), ea = elem(n->add_dtype), ew = elem(n->weight_dtype);
+  if (!aligned(x, e) || !aligned(sum, e) || !aligned(out, e) || !aligned(weight, ew) || (add && !aligned(add, ea)) ||
+      !aligned(scales, 4))
     return MCCE_EINVAL;
   if (sum == x && ld_or(n->ld_sum, n->d) != ld_or(n->ld_x, n->d)) return MCCE_EINVAL;
-  NormArgs a;
+  NormArgs a{};
   a.rows = n->rows, a.d = n->d, a.eps = n->eps;
   a.ld_x = ld_or(n->ld_x, n->d), a.ld_add = ld_or(n->ld_add, n->d), a.ld_sum = ld_or(n->ld_sum, n->d);
   a.ld_out = ld_or(n->ld_out, n->d), a.ld_q = ld_or(n->ld_q, n->d);
-  a.group = q ? (g ? g : n->d) : n->d, a.n_groups = q ? (n->d + a.group - 1) / a.group : 0;
-  a.add_f32 = n->add_dtype == MCCE_F32, a.weight_f32 = n->weight_dtype == MCCE_F32;
+  a.group_log2 = g == 0 ? 30 : g == 32 ? 5 : g == 64 ? 6 : 7;
+  a.n_groups = q ? (g ? (n->d + g - 1) / g : 1) : 0;
+  a.add_f32 = n->add_dtype == MCCE_F32, a.weight_f32 = n->weight_dtype == MCCE_F32, a.inv_d = 1.f / (float)n->d;
   a.x = x, a.add = add, a.weight = weight, a.sum = sum, a.out = out, a.q = (uint8_t*)q, a.scales = scales;
+  LayoutRule rule(n->d, 16 / e);
+  rule.tensor(x, a.ld_x, e);
+  rule.tensor(add, a.ld_add, ea);
+  rule.tensor(sum, a.ld_sum, e);
+  rule.tensor(out, a.ld_out, e);
+  rule.tensor(q, a.ld_q, 1);
+  const Layout3 lay = aligned(weight, 16) ? rule.layout() : kScalar;
+  a.off = rule.off;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  if (n->dtype == MCCE_F32) rmsnorm_kernel<float><<<(unsigned)n->rows, kThreads, 0, st>>>(a);
-  else rmsnorm_kernel<__nv_bfloat16><<<(unsigned)n->rows, kThreads, 0, st>>>(a);
-  return cudaGetLastError() == cudaSuccess ? MCCE_OK : MCCE_ECUDA;
+  cudaError_t err;
+  if (lay == kScalar) {
+    if (n->dtype == MCCE_F32) rmsnorm_scalar_kernel<float><<<(unsigned)n->rows, kThreads, 0, st>>>(a);
+    else rmsnorm_scalar_kernel<__nv_bfloat16><<<(unsigned)n->rows, kThreads, 0, st>>>(a);
+    err = cudaGetLastError();
+  } else {
+    const bool ragged = lay == kRagged;
+    err = launch_norm_types(a, n->dtype, ragged, norm_shape(n->rows, n->d, ragged, e, q ? a.group_log2 : 30), st);
+  }
+  return err == cudaSuccess ? MCCE_OK : MCCE_ECUDA;
 }
 
 extern "C" size_t mcce_rmsnorm_backward_workspace_bytes(const mcce_norm* n) {
-  return norm_ok(n) ? (size_t)(n->rows ? grad_parts(*n) : 1) * n->d * 4 : 0;
+  return norm_ok(n) ? (size_t)parts_most(*n) * n->d * 4 : 0;
 }
 
 extern "C" int mcce_rmsnorm_backward(const mcce_norm* n, const void* dout, const void* h, const void* dsum,
                                      const void* weight, void* dx, float* dweight, void* workspace,
                                      size_t workspace_bytes, void* cuda_stream) {
   if (!norm_ok(n) || (n->rows && (!dout || !h || !weight || !dx))) return MCCE_EINVAL;
-  const size_t e = elem(n->dtype);
+  const int e = elem(n->dtype);
   if (!aligned(dout, e) || !aligned(h, e) || !aligned(dsum, e) || !aligned(dx, e) ||
       !aligned(weight, elem(n->weight_dtype)) || !aligned(dweight, 4))
     return MCCE_EINVAL;
-  NormGradArgs a;
-  a.rows = n->rows, a.d = n->d, a.eps = n->eps, a.weight_f32 = n->weight_dtype == MCCE_F32;
+  NormGradArgs a{};
+  a.rows = n->rows, a.d = n->d, a.eps = n->eps, a.weight_f32 = n->weight_dtype == MCCE_F32, a.inv_d = 1.f / (float)n->d;
   a.ld_dout = ld_or(n->ld_out, n->d), a.ld_h = ld_or(n->ld_x, n->d), a.ld_dsum = ld_or(n->ld_add, n->d);
   a.ld_dx = ld_or(n->ld_sum, n->d);
   if ((dx == dout && a.ld_dx != a.ld_dout) || (dx == dsum && a.ld_dx != a.ld_dsum)) return MCCE_EINVAL;
@@ -203,12 +818,27 @@ extern "C" int mcce_rmsnorm_backward(const mcce_norm* n, const void* dout, const
     if (workspace_bytes < mcce_rmsnorm_backward_workspace_bytes(n)) return MCCE_ENOSPC;
   }
   cudaStream_t st = (cudaStream_t)cuda_stream;
+  if (n->rows == 0)
+    return !dweight || cudaMemsetAsync(dweight, 0, (size_t)n->d * 4, st) == cudaSuccess ? MCCE_OK : MCCE_ECUDA;
   a.dout = dout, a.h = h, a.dsum = dsum, a.weight = weight, a.dx = dx, a.part = dweight ? (float*)workspace : nullptr;
-  a.parts = grad_parts(*n);
-  if (a.parts) {
-    if (n->dtype == MCCE_F32) rmsnorm_grad_kernel<float><<<a.parts, kThreads, 0, st>>>(a);
-    else rmsnorm_grad_kernel<__nv_bfloat16><<<a.parts, kThreads, 0, st>>>(a);
+  LayoutRule rule(n->d, 16 / e);
+  rule.tensor(h, a.ld_h, e);
+  rule.tensor(dout, a.ld_dout, e);
+  rule.tensor(dsum, a.ld_dsum, e);
+  rule.tensor(dx, a.ld_dx, e);
+  const Layout3 lay = aligned(weight, 16) ? rule.layout() : kScalar;
+  a.off = rule.off;
+  const GradShape g = grad_shape(n->rows, n->d, lay, e, dsum != nullptr, dweight != nullptr);
+  cudaError_t err;
+  if (lay == kScalar) {
+    if (n->dtype == MCCE_F32) rmsnorm_grad_scalar_kernel<float><<<g.ctas, kThreads, 0, st>>>(a);
+    else rmsnorm_grad_scalar_kernel<__nv_bfloat16><<<g.ctas, kThreads, 0, st>>>(a);
+    err = cudaGetLastError();
+  } else {
+    err = launch_grad_types(a, n->dtype, lay == kRagged, g, st);
   }
-  if (dweight) dweight_kernel<<<(n->d + 127) / 128, 128, 0, st>>>(a.part, dweight, a.parts, n->d);
-  return cudaGetLastError() == cudaSuccess ? MCCE_OK : MCCE_ECUDA;
+  if (err == cudaSuccess && dweight) {
+    err = launch_dweight(a.part, dweight, g.ctas, n->d, st);
+  }
+  return err == cudaSuccess ? MCCE_OK : MCCE_ECUDA;
 }

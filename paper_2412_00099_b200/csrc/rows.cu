@@ -219,6 +219,20 @@ __global__ void __launch_bounds__(256) combine_rows_grad_kernel(const CombineArg
   }
 }
 
+struct UnitRule {
+  int u;
+  UnitRule(int d, int widest) : u(widest) {
+    while (d % u) u /= 2;
+  }
+  void tensor(const void* p, int64_t ld, int elem_bytes) {
+    while (p && u > 1) {
+      const int a = u * elem_bytes > 16 ? 16 : u * elem_bytes;
+      if ((uintptr_t)p % a == 0 && (ld * elem_bytes) % a == 0) return;
+      u /= 2;
+    }
+  }
+};
+
 bool rows_ok(const mcce_rows* r) {
   if (!r) return false;
   if (r->n_layers < 1 || r->n_layers > 65535 || r->n_tokens < 0 || r->top_k < 1 || r->top_k > kMaxK || r->d < 1) return false;
@@ -329,7 +343,7 @@ extern "C" int mcce_combine(const mcce_rows* r, const void* rows, const int32_t*
   if (!aligned(rows, e) || !aligned(inv, 4) || !aligned(sel_w, 4) || !aligned(add, ey) || !aligned(y, ey)) return MCCE_EINVAL;
   CombineArgs a = combine_args(*r);
   a.inv = inv, a.w = sel_w, a.rows = rows, a.add = add, a.y = y;
-  UnitRule u(r->d);
+  UnitRule u(r->d, 8);
   u.tensor(rows, a.ld_rows, e);
   u.tensor(add, a.ld_token, ey);
   u.tensor(y, a.ld_token, ey);
@@ -346,7 +360,7 @@ extern "C" int mcce_combine_backward(const mcce_rows* r, const void* dy, const v
     return MCCE_EINVAL;
   CombineArgs a = combine_args(*r);
   a.inv = inv, a.w = sel_w, a.rows = rows, a.dy = dy, a.drows = drows, a.dw = dw;
-  UnitRule u(r->d);
+  UnitRule u(r->d, 8);
   u.tensor(dw ? rows : nullptr, a.ld_rows, e);
   u.tensor(drows, a.ld_rows, e);
   u.tensor(dy, a.ld_token, ey);
