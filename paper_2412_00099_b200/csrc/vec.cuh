@@ -157,10 +157,10 @@ __device__ __forceinline__ void load_anywhere(Pack<T, U>& out, const T* p, const
   uint32_t w[4 * N + 4];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const uint4 q = __ldg(v + i);
+    const uint4 q = v[i];
     w[4 * i] = q.x, w[4 * i + 1] = q.y, w[4 * i + 2] = q.z, w[4 * i + 3] = q.w;
   }
-  const uint4 q = m ? __ldg(v + N) : make_uint4(0, 0, 0, 0);
+  const uint4 q = m ? v[N] : make_uint4(0, 0, 0, 0);
   w[4 * N] = q.x, w[4 * N + 1] = q.y, w[4 * N + 2] = q.z, w[4 * N + 3] = q.w;
   if (m & 4) {
 #pragma unroll
