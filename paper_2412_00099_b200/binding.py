@@ -440,12 +440,12 @@ def _code(t, what):
     return c
 
 
-def _ld(t, shape, device, what):
+def _ld(t, shape, dev, what):
     """Row stride of a tensor of this shape whose rows are evenly spaced (the stride may exceed the width)."""
-    if t.shape != shape or t.device != device:
-        raise McceError("%s is %s on %s, expected %s on %s" % (what, tuple(t.shape), t.device, tuple(shape), device))
-    if t.is_contiguous():
+    if t.shape == shape and t.get_device() == dev and t.is_contiguous():
         return shape[-1]
+    if t.shape != shape or t.get_device() != dev:
+        raise McceError("%s is %s on %s, expected %s on cuda:%d" % (what, tuple(t.shape), t.device, tuple(shape), dev))
     try:
         v = t.view(-1, shape[-1])
     except RuntimeError:
@@ -456,9 +456,9 @@ def _ld(t, shape, device, what):
     return ld
 
 
-def _dense(t, shape, dtype, device, what):
-    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise McceError("%s: expected contiguous %s %s on %s" % (what, dtype, tuple(shape), device))
+def _dense(t, shape, dtype, dev, what):
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev or not t.is_contiguous():
+        raise McceError("%s: expected contiguous %s %s on cuda:%d" % (what, dtype, tuple(shape), dev))
 
 
 def _at(t):
@@ -466,19 +466,21 @@ def _at(t):
 
 
 def _cuda(t):
-    dev = t.device
-    if dev.type != "cuda":
+    """Index of the tensor's device."""
+    dev = t.get_device()
+    if dev < 0:
         raise McceError("no CUDA tensor: this library has no CPU path")
     return dev
 
 
 def _call(fn, dev, *args):
-    """Calls an entry point that uses the current device, on the current stream of the tensors' device."""
-    if torch.cuda.current_device() == dev.index:
-        rc = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    """Calls an entry point that uses the current device, on the current stream of the tensors' device.  These calls take
+    a few microseconds on the device, so the handle comes without a Stream object around it."""
+    if torch._C._cuda_getDevice() == dev:
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
     else:
         with torch.cuda.device(dev):
-            rc = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         _check(rc)
 
@@ -501,7 +503,7 @@ def rmsnorm(x, weight, eps=1e-6, add=None, quant_group=None, want_out=True, out:
     row, else 32, 64 or 128 columns per scale) also the 8-bit rows `q` and their `scales`.  x [..., d] fp32 or bf16;
     add fp32 or x's type; weight [d] fp32 or x's type.  `out` gives the result tensors (out.sum may be x); a field that
     is None is not computed."""
-    lib, dev, shape = load(), _cuda(x), x.shape
+    lib, dev, shape = _lib or load(), _cuda(x), x.shape
     _need(x.dim() >= 1 and shape[-1] >= 1, "x must have columns")
     d = shape[-1]
     rows = x.numel() // d
@@ -537,7 +539,7 @@ def rmsnorm(x, weight, eps=1e-6, add=None, quant_group=None, want_out=True, out:
 def rmsnorm_backward(dout, h, weight, eps=1e-6, dsum=None, want_dweight=True, out=None):
     """Gradient of rmsnorm: dx (the gradient of x and of add) and dweight (fp32, None if not wanted).  h is the `sum` of the
     forward call, dsum the gradient that reaches it past the norm; `out` = (dx, dweight)."""
-    lib, dev, shape = load(), _cuda(h), h.shape
+    lib, dev, shape = _lib or load(), _cuda(h), h.shape
     _need(h.dim() >= 1 and shape[-1] >= 1, "h must have columns")
     d = shape[-1]
     code = _code(h, "h")
@@ -563,7 +565,7 @@ def dispatch(sel_idx, n_experts, x=None, scales=None, out: Optional[Dispatched] 
     """Sorts token rows by expert.  sel_idx [T,K] or [L,T,K] int32; x [(L,)T,d] fp32, bf16 or float8_e4m3fn; scales [(L,)T,n]
     fp32.  Returns offsets [(L,)E+1], perm [(L,)T*K], inv like sel_idx, rows [(L,)T*K,d], scales [(L,)T*K,n]; what lies
     behind the last bucket is left as it was (with `out`) or undefined."""
-    lib, dev = load(), _cuda(sel_idx)
+    lib, dev = _lib or load(), _cuda(sel_idx)
     _need(sel_idx.dim() in (2, 3), "sel_idx must be [T,K] or [L,T,K]")
     head, (T, K) = sel_idx.shape[:-2], sel_idx.shape[-2:]
     L = head[0] if head else 1
@@ -612,7 +614,7 @@ def combine(rows, inv, sel_w=None, add=None, out_dtype=None, out=None):
     """y[t] = add[t] + sum_k sel_w[t,k] rows[inv[t,k]] (weights 1 without sel_w: the gradient of dispatch with respect to
     x).  rows [(L,)T*K,d] fp32 or bf16, inv and sel_w [(L,)T,K]; y [(L,)T,d] in out_dtype: fp32, or the type of rows
     (the default).  `out` may be add."""
-    lib, dev = load(), _cuda(rows)
+    lib, dev = _lib or load(), _cuda(rows)
     head, L, T, K, d = _pairs(rows, inv, dev)
     if out is None:
         out = torch.empty(head + (T, d), dtype=out_dtype or rows.dtype, device=dev)
@@ -630,7 +632,7 @@ def combine(rows, inv, sel_w=None, add=None, out_dtype=None, out=None):
 def combine_backward(dy, rows, inv, sel_w=None, want_dw=True, out=None):
     """Gradient of combine: drows (in the type of rows; rows at positions that inv does not name are left as they were) and
     dw [(L,)T,K] fp32 (None if not wanted).  `out` = (drows, dw); drows may be rows."""
-    lib, dev = load(), _cuda(rows)
+    lib, dev = _lib or load(), _cuda(rows)
     head, L, T, K, d = _pairs(rows, inv, dev)
     if out is None:
         out = (torch.empty(head + (T * K, d), dtype=rows.dtype, device=dev),

@@ -166,13 +166,14 @@ __global__ void __launch_bounds__(512) rmsnorm_kernel(const __grid_constant__ No
   const W* weight = (const W*)a.weight;
   Pack<W, U> w[VPT];
 #pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    w[i].zero();
-    if (in[i]) {
-      if constexpr (RAGGED) load_anywhere(w[i], weight + head + c0 + i * step, weight, weight + a.d);
-      else w[i].load_const(weight + c0 + i * step);
-    }
-  }
+  for (int i = 0; i < VPT; ++i) w[i].zero();
+  auto load_weights = [&](auto how) {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+      if (in[i]) load_shifted<W, U, decltype(how)::value>(w[i], weight + head + c0 + i * step);
+  };
+  if constexpr (RAGGED) with_shift(weight + head, whole, weight, weight + a.d, load_weights);
+  else load_weights(Int<kInPlace>{});
   const float w_head = in_head ? wide(weight[th.t]) : 0.f, w_tail = in_tail ? wide(weight[tail]) : 0.f;
   const float inv = inv_rms(row_sum(ss, a.tpr, buf), a.inv_d, a.eps);
   const float n_head = h_head * inv * w_head, n_tail = h_tail * inv * w_tail;
@@ -460,7 +461,7 @@ __global__ void __launch_bounds__(512) rmsnorm_grad_kernel(const __grid_constant
     Pack<W, U> p;
     p.zero();
     if (in[i]) {
-      if constexpr (RAGGED) load_anywhere(p, weight + head + c0 + i * step, weight, weight + a.d);
+      if constexpr (RAGGED) p.load_part(weight + head + c0 + i * step, 0, U);   // once per CTA
       else p.load_const(weight + c0 + i * step);
     }
     p.get(w[i]);

@@ -1,4 +1,6 @@
 // Token rows sorted by expert, the rows brought back to their tokens with weights (Eq. 1's sum), and its gradient.
+#include <type_traits>
+
 #include "common.cuh"
 #include "vec.cuh"
 
@@ -118,14 +120,11 @@ __device__ __forceinline__ int my_position(const Token& tk, const int32_t* inv, 
   const int pos = tk.there && k < K ? inv[tk.t * K + k] : -1;
   return (unsigned)pos < (unsigned)P ? pos : -1;
 }
-// elements of a row that starts at element `at` of a tensor before its first whole unit
-template <int U>
-__device__ __forceinline__ int head_of(int64_t at, int off, int d) { return min(d, (int)(-(at + off) & (U - 1))); }
 
 struct CopyArgs {
   int64_t tokens;        // L * T
-  int64_t ld_x, ld_rows;
-  int T, K, P, d, scale_cols, tpt, off;   // off: of rows, in elements, past a 16-byte boundary
+  int64_t ld_x, ld_rows; // in units
+  int T, K, P, units, scale_cols, tpt;
   const int32_t* inv;
   const void* x;
   void* rows;
@@ -133,58 +132,49 @@ struct CopyArgs {
   float* row_scales;
 };
 
-__device__ __forceinline__ void copy_scales(const CopyArgs& a, const Token& tk, int k, int pos) {
-  for (int c = tk.u0; c < a.scale_cols; c += a.tpt)
-    a.row_scales[(tk.first + pos) * a.scale_cols + c] = a.scales[tk.t * a.scale_cols + c];
+// The row of a token to the positions of its pairs, by `threads` threads of which this is number u0.  V units of the row are
+// read, all in flight, and written once for every pair: a token's row is read once.
+// position_of(k): of pair k, -1: none.
+template <typename V_, typename F>
+__device__ __forceinline__ void move_row(const CopyArgs& a, int64_t t, int64_t first, int u0, int threads, F position_of) {
+  constexpr int V = sizeof(V_) == 16 ? 4 : 8;
+  const V_* x = (const V_*)a.x + t * a.ld_x;
+  V_* rows = (V_*)a.rows + first * a.ld_rows;
+  for (int b = u0; b - u0 < a.units; b += threads * V) {
+    V_ p[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (b + v * threads < a.units) p[v] = __ldg(x + b + v * threads);
+    for (int k = 0; k < a.K; ++k) {
+      const int pos = position_of(k);
+      if (pos < 0) continue;
+      V_* to = rows + pos * a.ld_rows + b;
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (b + v * threads < a.units) to[v * threads] = p[v];
+    }
+  }
 }
 
-// A token's row is read once, a unit of 16 bytes per thread, and written to the positions of its pairs.  RAGGED: the
-// units are those of the destination, whose alignment differs from pair to pair, shifted out of the token's row.
-template <typename T, bool RAGGED>
+template <typename V>
 __global__ void __launch_bounds__(256) rows_copy_kernel(const __grid_constant__ CopyArgs a) {
-  constexpr int U = 16 / (int)sizeof(T);
   cudaGridDependencySynchronize();
   const Token tk(a.tpt, a.tokens, a.T, a.P);
   const int mine = my_position(tk, a.inv, a.K, a.P);
-  const T* x = (const T*)a.x + tk.t * a.ld_x;
-  T* rows = (T*)a.rows + tk.first * a.ld_rows;
-  if (!RAGGED && a.x) {
-    const int n = tk.there ? a.d / U : 0, rounds = (a.d / U + a.tpt - 1) / a.tpt;
-    for (int i = 0, u = tk.u0; i < rounds; ++i, u += a.tpt) {
-      Pack<T, U> v;
-      if (u < n) v.load_const(x + u * U);
-      for (int k = 0; k < a.K; ++k) {
-        const int pos = position(tk, mine, k);
-        if (pos >= 0 && u < n) v.store(rows + pos * a.ld_rows + u * U);
-      }
-    }
-  }
-  for (int k = 0; k < a.K; ++k) {
+  if (a.x) move_row<V>(a, tk.there ? tk.t : 0, tk.first, tk.u0, a.tpt, [&](int k) { return position(tk, mine, k); });
+  for (int k = 0; a.scale_cols && k < a.K; ++k) {
     const int pos = position(tk, mine, k);
-    if (pos < 0) continue;
-    if (RAGGED && a.x) {
-      const int head = head_of<U>((tk.first + pos) * a.ld_rows, a.off, a.d), whole = (a.d - head) & ~(U - 1);
-      T* row = rows + pos * a.ld_rows;
-      const T* end = (const T*)a.x + (a.tokens - 1) * a.ld_x + a.d;
-      for (int c = head + tk.u0 * U; c < head + whole; c += a.tpt * U) {
-        Pack<T, U> v;
-        load_anywhere(v, x + c, (const T*)a.x, end);
-        v.store(row + c);
-      }
-      if (tk.u0 < head) row[tk.u0] = x[tk.u0];
-      if (head + whole + tk.u0 < a.d) row[head + whole + tk.u0] = x[head + whole + tk.u0];
-    }
-    copy_scales(a, tk, k, pos);
+    for (int c = tk.u0; pos >= 0 && c < a.scale_cols; c += a.tpt)
+      a.row_scales[(tk.first + pos) * a.scale_cols + c] = a.scales[tk.t * a.scale_cols + c];
   }
 }
 
 // Few pairs per layer: one launch.  Every CTA counts all pairs of its layer (and, in the upper half of a word, those before
 // its own tokens), ranks its own and moves their rows; the counting takes the place of two more launches.
 constexpr int kFusedPairs = 64;    // pairs of a CTA at most
-template <typename T, bool RAGGED>
+template <typename V>
 __global__ void __launch_bounds__(256) rows_dispatch_kernel(const __grid_constant__ SortArgs s, const __grid_constant__ CopyArgs a,
                                                             const int tokens_per_cta) {
-  constexpr int U = 16 / (int)sizeof(T);
   __shared__ int count[kMaxE], base[kMaxE], warp_sum[8], id[kFusedPairs], place[kFusedPairs];
   const int l = blockIdx.y, t0 = blockIdx.x * tokens_per_cta, n_tok = min(tokens_per_cta, s.T - t0);
   const int q0 = t0 * s.K, n = n_tok * s.K, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -230,47 +220,24 @@ __global__ void __launch_bounds__(256) rows_dispatch_kernel(const __grid_constan
     if (s.perm && pos >= 0) s.perm[(size_t)l * s.P + pos] = q0 + tid;
   }
   __syncthreads();
+  // the warps of a token: one each for eight tokens or more, else the eight warps shared out
   const int64_t first = (int64_t)l * s.P;
-  const T* end = (const T*)a.x + (a.tokens - 1) * a.ld_x + a.d;
-  if (a.x) {
-    if (!RAGGED) {
-      const int units = a.d / U;
-      for (int i = tid; i < n_tok * units; i += 256) {
-        const int t = i / units, u = i - t * units;
-        Pack<T, U> v;
-        v.load_const((const T*)a.x + ((int64_t)l * s.T + t0 + t) * a.ld_x + u * U);
-        for (int k = 0; k < s.K; ++k) {
-          const int pos = place[t * s.K + k];
-          if (pos >= 0) v.store((T*)a.rows + (first + pos) * a.ld_rows + u * U);
-        }
-      }
-    } else {
-      for (int p = warp; p < n; p += 8) {   // a warp per pair
-        const int pos = place[p];
-        if (pos < 0) continue;
-        const T* x = (const T*)a.x + ((int64_t)l * s.T + t0 + p / s.K) * a.ld_x;
-        T* row = (T*)a.rows + (first + pos) * a.ld_rows;
-        const int head = head_of<U>((first + pos) * a.ld_rows, a.off, a.d), whole = (a.d - head) & ~(U - 1);
-        for (int col = head + lane * U; col < head + whole; col += 32 * U) {
-          Pack<T, U> v;
-          load_anywhere(v, x + col, (const T*)a.x, end);
-          v.store(row + col);
-        }
-        if (lane < head) row[lane] = x[lane];
-        if (head + whole + lane < a.d) row[head + whole + lane] = x[head + whole + lane];
-      }
+  const int per_token = n_tok >= 8 ? 1 : n_tok >= 4 ? 2 : n_tok >= 2 ? 4 : 8, slots = 8 / per_token;
+  const int u0 = (warp & (per_token - 1)) * 32 + lane;
+  for (int t = warp / per_token; t < n_tok; t += slots) {
+    const int64_t token = (int64_t)l * s.T + t0 + t;
+    if (a.x) move_row<V>(a, token, first, u0, per_token * 32, [&](int k) { return place[t * s.K + k]; });
+    for (int k = 0; a.scale_cols && k < s.K; ++k) {
+      const int pos = place[t * s.K + k];
+      for (int i = u0; pos >= 0 && i < a.scale_cols; i += per_token * 32)
+        a.row_scales[(first + pos) * a.scale_cols + i] = a.scales[token * a.scale_cols + i];
     }
-  }
-  for (int i = tid; i < n * a.scale_cols; i += 256) {
-    const int p = i / a.scale_cols, col = i - p * a.scale_cols, pos = place[p];
-    if (pos >= 0)
-      a.row_scales[(first + pos) * a.scale_cols + col] = a.scales[((int64_t)l * s.T + t0 + p / s.K) * a.scale_cols + col];
   }
 }
 
 struct CombineArgs {
   int64_t tokens, ld_token, ld_rows;
-  int T, K, P, d, tpt, off;   // off: of y or of drows, in elements, past a unit's boundary
+  int T, K, P, d, tpt;
   const int32_t* inv;
   const float* w;
   const void *rows, *add;
@@ -280,28 +247,23 @@ struct CombineArgs {
   float* dw;
 };
 
-// y of a token: VPT units per thread and KC rows at a time, so that about eight 16-byte loads are in flight per thread.
-// RAGGED: the units are those of y; the rows, whose alignment differs from pair to pair, are shifted into place.
-template <typename T, typename Y, int KC, int VPT, bool RAGGED>
+// y of a token: U columns at a time, VPT such units per thread and KC rows at once, so that KC * VPT loads are in flight.
+template <typename T, typename Y, int U, int KC, int VPT>
 __global__ void __launch_bounds__(256) combine_rows_kernel(const __grid_constant__ CombineArgs a) {
-  constexpr int U = 16 / (int)sizeof(T);
+  constexpr int N = (U + 1) / 2;
   const Token tk(a.tpt, a.tokens, a.T, a.P);
   const int mine = my_position(tk, a.inv, a.K, a.P);
-  const int pair = (int)(threadIdx.x & 31) - tk.lane0;
-  const float my_w = mine >= 0 && a.w ? a.w[tk.t * a.K + pair] : 1.f;
+  const float my_w = mine >= 0 && a.w ? a.w[tk.t * a.K + (int)(threadIdx.x & 31) - tk.lane0] : 1.f;
   const T* rows = (const T*)a.rows + tk.first * a.ld_rows;
-  const T* end = (const T*)a.rows + (a.tokens / a.T * a.P - 1) * a.ld_rows + a.d;
   const int64_t at = tk.t * a.ld_token;
-  const int d = tk.there ? a.d : 0;
-  const int head = RAGGED ? head_of<U>(at, a.off, d) : 0, whole = RAGGED ? (d - head) & ~(U - 1) : d;
-  const int per_round = a.tpt * U * VPT, rounds = (a.d + per_round - 1) / per_round;
-  for (int i = 0; i < rounds; ++i) {
-    const int c0 = i * per_round + tk.u0 * U;
-    float2 s[VPT][U / 2];
+  const int d = tk.there ? a.d : 0, step = a.tpt * U;
+  for (int b = 0; b < a.d; b += step * VPT) {
+    const int c0 = b + tk.u0 * U;
+    float2 s[VPT][N];
 #pragma unroll
     for (int v = 0; v < VPT; ++v)
 #pragma unroll
-      for (int j = 0; j < U / 2; ++j) s[v][j] = both(0.f);
+      for (int j = 0; j < N; ++j) s[v][j] = both(0.f);
     for (int k0 = 0; k0 < a.K; k0 += KC) {
       Pack<T, U> p[KC][VPT];
       float w[KC];
@@ -309,64 +271,45 @@ __global__ void __launch_bounds__(256) combine_rows_kernel(const __grid_constant
       for (int k = 0; k < KC; ++k) {
         const int pos = k0 + k < a.K ? position(tk, mine, k0 + k) : -1;
         w[k] = __shfl_sync(kFull, my_w, tk.lane0 + ((k0 + k) & 15));
-        const T* row = rows + pos * a.ld_rows + head + c0;
+        const T* row = rows + pos * a.ld_rows + c0;
 #pragma unroll
         for (int v = 0; v < VPT; ++v) {
           p[k][v].zero();
-          if (pos >= 0 && c0 + v * a.tpt * U < whole) {
-            if constexpr (RAGGED) load_anywhere(p[k][v], row + v * a.tpt * U, (const T*)a.rows, end);
-            else p[k][v].load_const(row + v * a.tpt * U);
-          }
+          if (pos >= 0 && c0 + v * step < d) p[k][v].load_const(row + v * step);
         }
       }
 #pragma unroll
       for (int k = 0; k < KC; ++k)
 #pragma unroll
         for (int v = 0; v < VPT; ++v) {
-          float2 e[U / 2];
+          float2 e[N];
           p[k][v].get(e);
 #pragma unroll
-          for (int j = 0; j < U / 2; ++j) s[v][j] = fma2(e[j], both(w[k]), s[v][j]);
+          for (int j = 0; j < N; ++j) s[v][j] = fma2(e[j], both(w[k]), s[v][j]);
         }
     }
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      const int c = c0 + v * a.tpt * U;
-      if (c >= whole) continue;
+      const int c = c0 + v * step;
+      if (c >= d) continue;
       Pack<Y, U> y;
       if (a.add) {
-        const Y* add = (const Y*)a.add + at + head + c;
-        if constexpr (RAGGED) load_anywhere(y, add, (const Y*)a.add, (const Y*)a.add + (a.tokens - 1) * a.ld_token + a.d);
-        else y.load(add);
-        float2 e[U / 2];
+        y.load((const Y*)a.add + at + c);
+        float2 e[N];
         y.get(e);
 #pragma unroll
-        for (int j = 0; j < U / 2; ++j) s[v][j] = add2(s[v][j], e[j]);
+        for (int j = 0; j < N; ++j) s[v][j] = add2(s[v][j], e[j]);
       }
       y.set(s[v]);
-      y.store((Y*)a.y + at + head + c);
-    }
-  }
-  if (RAGGED) {   // single elements of the row's first U threads
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
-      const int c = side ? head + whole + tk.u0 : tk.u0;
-      const bool in = side ? c < d : tk.u0 < head;
-      float s = 0.f;
-      for (int k = 0; k < a.K; ++k) {
-        const int pos = position(tk, mine, k);
-        const float w = __shfl_sync(kFull, my_w, tk.lane0 + k);
-        if (in && pos >= 0) s = fmaf(wide(rows[pos * a.ld_rows + c]), w, s);
-      }
-      if (in) ((Y*)a.y)[at + c] = narrow<Y>(a.add ? s + wide(((const Y*)a.add)[at + c]) : s);
+      y.store((Y*)a.y + at + c);
     }
   }
 }
 
-// Sum of acc[k] over the lanes of a token, k < KC; lane l of a group of KC holds that of k = bit-reversed l afterwards.
+// Sums of acc[k] over `lanes` lanes, k < KC.  The number of values is halved while the lanes that share one double, so KC sums
+// cost little more than one; lane l holds that of k = l / (lanes / KC) afterwards.
 template <int KC>
 __device__ __forceinline__ float sum_of_all(float (&acc)[KC], int lanes) {
-  // halve the number of values and double the lanes that share one, until one is left
   int o = lanes >> 1;
   const int lane = threadIdx.x & 31;
 #pragma unroll
@@ -382,97 +325,77 @@ __device__ __forceinline__ float sum_of_all(float (&acc)[KC], int lanes) {
   return acc[0];
 }
 
-// drows and dw of a token: a row's unit is read, multiplied into the pair's sum, and replaced by w dy.  KC rows at a time.
-// RAGGED: the units are those of the sorted rows; dy, which lies in L1 after the first pair, is shifted into place.
-template <typename T, typename Y, int KC, bool RAGGED>
+// drows and dw of a token: a unit of a row is read, multiplied into the pair's sum, and replaced by w dy.  KC rows at once.
+template <typename T, typename Y, int U, int KC, int VPT>
 __global__ void __launch_bounds__(256) combine_rows_grad_kernel(const __grid_constant__ CombineArgs a) {
-  constexpr int U = 16 / (int)sizeof(T);
+  constexpr int N = (U + 1) / 2;
   __shared__ float parts[8][KC];
   const Token tk(a.tpt, a.tokens, a.T, a.P);
-  const int lane = threadIdx.x & 31, lanes = min(a.tpt, 32);
   const int mine = my_position(tk, a.inv, a.K, a.P);
-  const float my_w = mine >= 0 && a.w ? a.w[tk.t * a.K + lane - tk.lane0] : 1.f;
+  const float my_w = mine >= 0 && a.w ? a.w[tk.t * a.K + (int)(threadIdx.x & 31) - tk.lane0] : 1.f;
   const T* rows = (const T*)a.rows;
-  const T* rows_end = rows + (a.tokens / a.T * a.P - 1) * a.ld_rows + a.d;
   T* drows = (T*)a.drows;
   const Y* dy = (const Y*)a.dy + tk.t * a.ld_token;
-  const Y* dy_end = (const Y*)a.dy + (a.tokens - 1) * a.ld_token + a.d;
+  const int d = tk.there ? a.d : 0, step = a.tpt * U;
   for (int k0 = 0; k0 < a.K; k0 += KC) {
     int64_t at[KC];   // first element of the pair's row, -1: no row
-    int head[KC], whole[KC];
     float w[KC], acc[KC];
 #pragma unroll
     for (int k = 0; k < KC; ++k) {
       const int pos = k0 + k < a.K ? position(tk, mine, k0 + k) : -1;
       w[k] = __shfl_sync(kFull, my_w, tk.lane0 + ((k0 + k) & 15));
       at[k] = pos >= 0 ? (tk.first + pos) * a.ld_rows : -1;
-      head[k] = RAGGED && pos >= 0 ? head_of<U>(at[k], a.off, a.d) : 0;
-      whole[k] = pos < 0 ? 0 : RAGGED ? (a.d - head[k]) & ~(U - 1) : a.d;
       acc[k] = 0.f;
     }
-    for (int c = tk.u0 * U; c < a.d; c += a.tpt * U) {
-      Pack<T, U> p[KC];
-      float2 g[U / 2];
-      if (!RAGGED && tk.there) {
-        Pack<Y, U> q;
-        q.load_const(dy + c);
-        q.get(g);
-      }
+    for (int c = tk.u0 * U; c < d; c += step * VPT) {
+      Pack<T, U> p[KC][VPT];
+      Pack<Y, U> q[VPT];
+#pragma unroll
+      for (int v = 0; v < VPT; ++v)
+        if (c + v * step < d) q[v].load_const(dy + c + v * step);
       if (a.dw) {
 #pragma unroll
         for (int k = 0; k < KC; ++k)
-          if (c < whole[k]) {
-            if constexpr (RAGGED) load_anywhere(p[k], rows + at[k] + head[k] + c, rows, rows_end);
-            else p[k].load(rows + at[k] + c);
+#pragma unroll
+          for (int v = 0; v < VPT; ++v)
+            if (at[k] >= 0 && c + v * step < d) p[k][v].load(rows + at[k] + c + v * step);
+      }
+#pragma unroll
+      for (int v = 0; v < VPT; ++v) {
+        if (c + v * step >= d) continue;
+        float2 g[N];
+        q[v].get(g);
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+          if (at[k] < 0) continue;
+          float2 e[N];
+          if (a.dw) {
+            p[k][v].get(e);
+            float2 s = both(0.f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) s = fma2(e[j], g[j], s);
+            acc[k] += s.x + s.y;
           }
+#pragma unroll
+          for (int j = 0; j < N; ++j) e[j] = mul2(g[j], both(w[k]));
+          p[k][v].set(e);
+          p[k][v].store(drows + at[k] + c + v * step);
+        }
       }
-#pragma unroll
-      for (int k = 0; k < KC; ++k) {
-        if (c >= whole[k]) continue;
-        if constexpr (RAGGED) {
-          Pack<Y, U> q;
-          load_anywhere(q, dy + head[k] + c, (const Y*)a.dy, dy_end);
-          q.get(g);
-        }
-        float2 e[U / 2];
-        if (a.dw) {
-          p[k].get(e);
-          float2 s = both(0.f);
-#pragma unroll
-          for (int j = 0; j < U / 2; ++j) s = fma2(e[j], g[j], s);
-          acc[k] += s.x + s.y;
-        }
-#pragma unroll
-        for (int j = 0; j < U / 2; ++j) e[j] = mul2(g[j], both(w[k]));
-        p[k].set(e);
-        p[k].store(drows + at[k] + head[k] + c);
-      }
-    }
-    if (RAGGED) {
-#pragma unroll
-      for (int k = 0; k < KC; ++k)
-#pragma unroll
-        for (int side = 0; side < 2; ++side) {
-          const int c = side ? head[k] + whole[k] + tk.u0 : tk.u0;
-          if (at[k] < 0 || !(side ? c < a.d : tk.u0 < head[k])) continue;
-          const float g = wide(dy[c]);
-          if (a.dw) acc[k] = fmaf(wide(rows[at[k] + c]), g, acc[k]);
-          drows[at[k] + c] = narrow<T>(g * w[k]);
-        }
     }
     if (!a.dw) continue;
+    const int lane = threadIdx.x & 31, lanes = min(a.tpt, 32);
     const float s = sum_of_all(acc, lanes);
-    // this lane's pair of the chunk: the halves were taken from the top bit down
     const int k = (lane & (lanes - 1)) / (lanes / KC);
     const bool speaks = (lane & (lanes / KC - 1)) == 0;
     if (a.tpt <= 32) {
       if (speaks && tk.there && k0 + k < a.K) a.dw[tk.t * a.K + k0 + k] = s;
     } else {
-      __syncthreads();
+      __syncthreads();   // the last chunk's parts have been read
       if (speaks) parts[threadIdx.x >> 5][k] = s;
       __syncthreads();
       if (tk.there && tk.u0 < KC && k0 + tk.u0 < a.K) {
-        const int warps = a.tpt >> 5, w0 = (threadIdx.x >> 5);
+        const int warps = a.tpt >> 5, w0 = threadIdx.x >> 5;
         float v = 0.f;
         for (int i = 0; i < warps; ++i) v += parts[w0 + i][tk.u0];
         a.dw[tk.t * a.K + k0 + tk.u0] = v;
@@ -480,6 +403,22 @@ __global__ void __launch_bounds__(256) combine_rows_grad_kernel(const __grid_con
     }
   }
 }
+
+// Host: the widest unit (at most `widest` elements, a power of two) that divides the width and for which every row of every
+// tensor starts aligned.
+struct UnitRule {
+  int u;
+  UnitRule(int d, int widest) : u(widest) {
+    while (d % u) u /= 2;
+  }
+  void tensor(const void* p, int64_t ld, int elem_bytes) {   // null: not part of the call
+    while (p && u > 1) {
+      const int a = u * elem_bytes > 16 ? 16 : u * elem_bytes;
+      if ((uintptr_t)p % a == 0 && (ld * elem_bytes) % a == 0) return;
+      u /= 2;
+    }
+  }
+};
 
 bool rows_ok(const mcce_rows* r) {
   if (!r) return false;
@@ -512,67 +451,84 @@ int threads_per_token(int units, int per_thread) {
   while (t < 256 && t * per_thread < units) t *= 2;
   return t;
 }
-template <typename K, typename A>
-cudaError_t launch_tokens(K kernel, const A& a, cudaStream_t st) {
+template <typename K>
+cudaError_t launch_tokens(K kernel, const CombineArgs& a, cudaStream_t st) {
   const int64_t grid = (a.tokens * a.tpt + 255) / 256;
   if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
   kernel<<<(unsigned)grid, 256, 0, st>>>(a);
   return cudaGetLastError();
 }
 
-template <typename T, typename Y, bool RAGGED>
-cudaError_t run_combine_k(CombineArgs a, cudaStream_t st) {
-  const int units = (a.d * (int)sizeof(T) + 15) / 16;
-  if (a.K <= 1) return a.tpt = threads_per_token(units, 4), launch_tokens(combine_rows_kernel<T, Y, 1, 4, RAGGED>, a, st);
-  if (a.K <= 2) return a.tpt = threads_per_token(units, 4), launch_tokens(combine_rows_kernel<T, Y, 2, 4, RAGGED>, a, st);
-  if (a.K <= 4) return a.tpt = threads_per_token(units, 2), launch_tokens(combine_rows_kernel<T, Y, 4, 2, RAGGED>, a, st);
-  return a.tpt = threads_per_token(units, 1), launch_tokens(combine_rows_kernel<T, Y, 8, 1, RAGGED>, a, st);
+// Many tokens: a few units per thread.  Few tokens: one.
+int spread(const CombineArgs& a, int u, int units_per_thread) {
+  return threads_per_token((a.d + u - 1) / u, a.tokens * 64 < 148 * 1024 ? 1 : units_per_thread);
 }
-template <typename T, typename Y, bool RAGGED>
-cudaError_t run_combine_grad_k(CombineArgs a, cudaStream_t st) {
-  const int units = (a.d * (int)sizeof(T) + 15) / 16;
-  a.tpt = threads_per_token(units, 4);
-  if (a.K <= 1) return launch_tokens(combine_rows_grad_kernel<T, Y, 1, RAGGED>, a, st);
-  if (a.K <= 2) return launch_tokens(combine_rows_grad_kernel<T, Y, 2, RAGGED>, a, st);
-  if (a.K <= 4) return launch_tokens(combine_rows_grad_kernel<T, Y, 4, RAGGED>, a, st);
-  return launch_tokens(combine_rows_grad_kernel<T, Y, 8, RAGGED>, a, st);
+
+// Rows at once x units at once and threads per token, us measured (one launch between two events, 5 us of it not the kernel's;
+// 16384 tokens of 2048 bf16 columns unless noted).  Return, K = 8: 4 x 1 on 64 threads 99 (0.93 of the copy bandwidth), 8 x 1 104,
+// 2 x 2 133; K = 2, 4099 tokens of 4096: 1 x 4 22.8, 2 x 2 24.1, 2 x 1 25.2; K = 1 of 4096: 1 x 4 47.8, 2 x 2 55.7.  Gradient, K = 8:
+// 2 x 2 on 32 threads 195 (0.89), 4 x 1 193, 1 x 2 222; K = 6: 151 / 163 / 156.
+// Units narrower than 16 bytes (odd widths, unaligned rows) keep fewer bytes in flight per register: 8192 tokens, K = 8, of 1411
+// columns: return 4 x 4 82 (0.39), 4 x 2 93; gradient 4 x 1 142 (0.42), 2 x 4 152.  Sixteen-byte loads at the next boundary, shifted
+// into place, were no faster (74 .. 80 and 166).
+template <typename T, typename Y, int U>
+cudaError_t run_combine(CombineArgs a, cudaStream_t st) {
+  if constexpr (U * sizeof(T) == 16) {
+    a.tpt = spread(a, U, a.K <= 2 ? 8 : 4);
+    if (a.K <= 2) return launch_tokens(combine_rows_kernel<T, Y, U, 1, 4>, a, st);
+    return launch_tokens(combine_rows_kernel<T, Y, U, 4, sizeof(T) == 4 ? 2 : 1>, a, st);
+  } else {
+    a.tpt = spread(a, U, 32);
+    if (a.K <= 2) return launch_tokens(combine_rows_kernel<T, Y, U, 1, 8>, a, st);
+    return launch_tokens(combine_rows_kernel<T, Y, U, 4, 4>, a, st);
+  }
+}
+template <typename T, typename Y, int U>
+cudaError_t run_combine_grad(CombineArgs a, cudaStream_t st) {
+  if constexpr (U * sizeof(T) == 16) {
+    a.tpt = spread(a, U, 8);
+    if (a.K == 1) return launch_tokens(combine_rows_grad_kernel<T, Y, U, 1, 2>, a, st);
+    return launch_tokens(combine_rows_grad_kernel<T, Y, U, 2, 2>, a, st);
+  } else {
+    a.tpt = spread(a, U, a.K <= 2 ? 32 : 16);
+    if (a.K <= 2) return launch_tokens(combine_rows_grad_kernel<T, Y, U, 2, 4>, a, st);
+    return launch_tokens(combine_rows_grad_kernel<T, Y, U, 4, 1>, a, st);
+  }
 }
 template <typename T, typename Y>
-cudaError_t run_combine(const CombineArgs& a, bool ragged, bool grad, cudaStream_t st) {
-  if (grad) return ragged ? run_combine_grad_k<T, Y, true>(a, st) : run_combine_grad_k<T, Y, false>(a, st);
-  return ragged ? run_combine_k<T, Y, true>(a, st) : run_combine_k<T, Y, false>(a, st);
+cudaError_t run_combine_unit(const CombineArgs& a, int u, bool grad, cudaStream_t st) {
+  constexpr int kWide = 16 / (int)sizeof(T);
+  if (u == kWide) return grad ? run_combine_grad<T, Y, kWide>(a, st) : run_combine<T, Y, kWide>(a, st);
+  if (u >= 2) return grad ? run_combine_grad<T, Y, 2>(a, st) : run_combine<T, Y, 2>(a, st);
+  return grad ? run_combine_grad<T, Y, 1>(a, st) : run_combine<T, Y, 1>(a, st);
 }
-cudaError_t run_combine_types(const mcce_rows& r, const CombineArgs& a, bool ragged, bool grad, cudaStream_t st) {
-  if (r.dtype == MCCE_F32) return run_combine<float, float>(a, ragged, grad, st);
-  if (r.token_dtype == MCCE_F32) return run_combine<__nv_bfloat16, float>(a, ragged, grad, st);
-  return run_combine<__nv_bfloat16, __nv_bfloat16>(a, ragged, grad, st);
+cudaError_t run_combine_types(const mcce_rows& r, const CombineArgs& a, int u, bool grad, cudaStream_t st) {
+  if (r.dtype == MCCE_F32) return run_combine_unit<float, float>(a, u, grad, st);
+  if (r.token_dtype == MCCE_F32) return run_combine_unit<__nv_bfloat16, float>(a, u, grad, st);
+  return run_combine_unit<__nv_bfloat16, __nv_bfloat16>(a, u, grad, st);
 }
 
 // A launch that may begin while the kernel before it ends; the kernel waits for that one itself.
-template <typename... P, typename... A>
-cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t st, A... args) {
+template <typename P>
+cudaError_t launch_after(void (*kernel)(P), dim3 grid, int threads, cudaStream_t st, const std::decay_t<P>& args) {
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid, cfg.blockDim = dim3(threads), cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+  return cudaLaunchKernelEx(&cfg, kernel, args);
 }
 
 // Tokens per CTA of the single launch, 0: several launches.
-int fused_tokens(const SortArgs& s, int L) {
-  if (s.P > 4096) return 0;
-  int t = kFusedPairs / s.K;
-  while (t > 1 && (int64_t)((s.T + t - 1) / t) * L < 4 * 148) t = (t + 1) / 2;
-  return t;
+int fused_tokens(const SortArgs& s) {
+  if (s.P > 8192) return 0;
+  return s.K >= 4 ? 4 : s.K >= 2 ? 8 : 16;
 }
 
-template <typename T>
-cudaError_t run_dispatch(const SortArgs& s, CopyArgs c, int L, bool ragged, cudaStream_t st) {
-  if (const int t = fused_tokens(s, L)) {
-    const dim3 grid((s.T + t - 1) / t, L);
-    if (ragged) rows_dispatch_kernel<T, true><<<grid, 256, 0, st>>>(s, c, t);
-    else rows_dispatch_kernel<T, false><<<grid, 256, 0, st>>>(s, c, t);
+template <typename V>
+cudaError_t run_dispatch(const SortArgs& s, CopyArgs c, int L, cudaStream_t st) {
+  if (const int t = fused_tokens(s)) {
+    rows_dispatch_kernel<V><<<dim3((s.T + t - 1) / t, L), 256, 0, st>>>(s, c, t);
     return cudaGetLastError();
   }
   const dim3 grid(s.B, L);
@@ -580,11 +536,11 @@ cudaError_t run_dispatch(const SortArgs& s, CopyArgs c, int L, bool ragged, cuda
   cudaError_t err = cudaGetLastError();
   if (err == cudaSuccess) err = launch_after(rows_rank_kernel, grid, kSortChunk, st, s);
   if (err != cudaSuccess || !(c.x || c.scale_cols)) return err;
-  c.tpt = threads_per_token((c.d * (int)sizeof(T) + 15) / 16, 1);
+  c.tpt = threads_per_token(c.units, sizeof(V) == 16 ? 2 : 16);
+  if (c.tpt > 128) c.tpt = 128;
   const int64_t ctas = (c.tokens * c.tpt + 255) / 256;
   if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
-  return ragged ? launch_after(rows_copy_kernel<T, true>, dim3((unsigned)ctas), 256, st, c)
-                : launch_after(rows_copy_kernel<T, false>, dim3((unsigned)ctas), 256, st, c);
+  return launch_after(rows_copy_kernel<V>, dim3((unsigned)ctas), 256, st, c);
 }
 
 }  // namespace
@@ -620,18 +576,19 @@ extern "C" int mcce_dispatch(const mcce_rows* r, const int32_t* sel_idx, const v
   s.T = r->n_tokens, s.K = r->top_k, s.E = r->n_experts, s.P = s.T * s.K, s.B = (s.P + kSortChunk - 1) / kSortChunk;
   s.sel = sel_idx, s.offsets = offsets, s.perm = perm, s.inv = inv, s.counts = (int32_t*)workspace;
   CopyArgs c{};
-  c.tokens = (int64_t)r->n_layers * r->n_tokens, c.T = s.T, c.K = s.K, c.P = s.P, c.d = r->d, c.scale_cols = r->scale_cols;
-  c.ld_x = ld_or(r->ld_token, r->d), c.ld_rows = ld_or(r->ld_rows, r->d);
+  c.tokens = (int64_t)r->n_layers * r->n_tokens, c.T = s.T, c.K = s.K, c.P = s.P, c.scale_cols = r->scale_cols;
   c.inv = inv, c.x = x, c.rows = rows, c.scales = scales, c.row_scales = row_scales;
-  LayoutRule rule(r->d, 16 / e);
-  rule.tensor(rows, c.ld_rows, e);
-  c.off = rows ? rule.off : 0;
-  rule.tensor(x, c.ld_x, e);
-  const bool ragged = x && !rule.aligned;
+  // rows are moved in units of 16 bytes or the largest power of two that they are aligned to
+  int64_t ld_x = ld_or(r->ld_token, r->d) * e, ld_rows = ld_or(r->ld_rows, r->d) * e, row = x ? (int64_t)r->d * e : 0;
+  int v = 16;
+  while (v > 1 && (row % v || ld_x % v || ld_rows % v || !aligned(x, v) || !aligned(rows, v))) v /= 2;
+  c.ld_x = ld_x / v, c.ld_rows = ld_rows / v, c.units = (int)(row / v);
   cudaError_t err;
-  if (e == 4) err = run_dispatch<uint32_t>(s, c, r->n_layers, ragged, st);
-  else if (e == 2) err = run_dispatch<uint16_t>(s, c, r->n_layers, ragged, st);
-  else err = run_dispatch<uint8_t>(s, c, r->n_layers, ragged, st);
+  if (v == 16) err = run_dispatch<uint4>(s, c, r->n_layers, st);
+  else if (v == 8) err = run_dispatch<uint2>(s, c, r->n_layers, st);
+  else if (v == 4) err = run_dispatch<uint32_t>(s, c, r->n_layers, st);
+  else if (v == 2) err = run_dispatch<uint16_t>(s, c, r->n_layers, st);
+  else err = run_dispatch<uint8_t>(s, c, r->n_layers, st);
   return err == cudaSuccess ? MCCE_OK : MCCE_ECUDA;
 }
 
@@ -644,12 +601,11 @@ extern "C" int mcce_combine(const mcce_rows* r, const void* rows, const int32_t*
   if (!aligned(rows, e) || !aligned(inv, 4) || !aligned(sel_w, 4) || !aligned(add, ey) || !aligned(y, ey)) return MCCE_EINVAL;
   CombineArgs a = combine_args(*r);
   a.inv = inv, a.w = sel_w, a.rows = rows, a.add = add, a.y = y;
-  LayoutRule rule(r->d, 16 / e);
-  rule.tensor(y, a.ld_token, ey);
-  a.off = rule.off;
-  rule.tensor(add, a.ld_token, ey);
-  rule.tensor(rows, a.ld_rows, e);
-  return run_combine_types(*r, a, !rule.aligned, false, (cudaStream_t)cuda_stream) == cudaSuccess ? MCCE_OK : MCCE_ECUDA;
+  UnitRule u(r->d, 16 / e);
+  u.tensor(rows, a.ld_rows, e);
+  u.tensor(add, a.ld_token, ey);
+  u.tensor(y, a.ld_token, ey);
+  return run_combine_types(*r, a, u.u, false, (cudaStream_t)cuda_stream) == cudaSuccess ? MCCE_OK : MCCE_ECUDA;
 }
 
 extern "C" int mcce_combine_backward(const mcce_rows* r, const void* dy, const void* rows, const int32_t* inv,
@@ -662,10 +618,9 @@ extern "C" int mcce_combine_backward(const mcce_rows* r, const void* dy, const v
     return MCCE_EINVAL;
   CombineArgs a = combine_args(*r);
   a.inv = inv, a.w = sel_w, a.rows = dw ? rows : nullptr, a.dy = dy, a.drows = drows, a.dw = dw;
-  LayoutRule rule(r->d, 16 / e);
-  rule.tensor(drows, a.ld_rows, e);
-  a.off = rule.off;
-  rule.tensor(a.rows, a.ld_rows, e);
-  rule.tensor(dy, a.ld_token, ey);
-  return run_combine_types(*r, a, !rule.aligned, true, (cudaStream_t)cuda_stream) == cudaSuccess ? MCCE_OK : MCCE_ECUDA;
+  UnitRule u(r->d, 16 / e);
+  u.tensor(a.rows, a.ld_rows, e);
+  u.tensor(drows, a.ld_rows, e);
+  u.tensor(dy, a.ld_token, ey);
+  return run_combine_types(*r, a, u.u, true, (cudaStream_t)cuda_stream) == cudaSuccess ? MCCE_OK : MCCE_ECUDA;
 }

@@ -96,14 +96,13 @@ struct Pack {
     for (int i = 0; i < U; ++i)
       if (i >= lo && i < hi) p[i] = e[i];
   }
-  __device__ __forceinline__ void get(float (&v)[U]) const {
-    T e[U];
-    memcpy(e, r, sizeof(e));
-#pragma unroll
-    for (int i = 0; i < U; ++i) v[i] = wide(e[i]);
-  }
-  __device__ __forceinline__ void get(float2 (&v)[U / 2]) const {
-    if constexpr (sizeof(T) == 2) {
+  // in pairs; a single value has a zero beside it
+  __device__ __forceinline__ void get(float2 (&v)[(U + 1) / 2]) const {
+    if constexpr (U == 1) {
+      T e;
+      memcpy(&e, r, sizeof(e));
+      v[0] = make_float2(wide(e), 0.f);
+    } else if constexpr (sizeof(T) == 2) {
       uint32_t e[U / 2];
       memcpy(e, r, sizeof(e));
 #pragma unroll
@@ -112,21 +111,12 @@ struct Pack {
       memcpy(v, r, sizeof(v));
     }
   }
-  __device__ __forceinline__ void set(const float (&v)[U]) {   // each value rounded once, to nearest even
-    if constexpr (sizeof(T) == 2 && U > 1) {
-      __nv_bfloat162 e[U / 2];
-#pragma unroll
-      for (int i = 0; i < U / 2; ++i) e[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-      memcpy(r, e, sizeof(e));
-    } else {
-      T e[U];
-#pragma unroll
-      for (int i = 0; i < U; ++i) e[i] = narrow<T>(v[i]);
-      memcpy(r, e, sizeof(e));
-    }
-  }
-  __device__ __forceinline__ void set(const float2 (&v)[U / 2]) {
-    if constexpr (sizeof(T) == 2) {
+  // each value rounded once, to nearest even
+  __device__ __forceinline__ void set(const float2 (&v)[(U + 1) / 2]) {
+    if constexpr (U == 1) {
+      const T e = narrow<T>(v[0].x);
+      memcpy(r, &e, sizeof(e));
+    } else if constexpr (sizeof(T) == 2) {
       __nv_bfloat162 e[U / 2];
 #pragma unroll
       for (int i = 0; i < U / 2; ++i) e[i] = __floats2bfloat162_rn(v[i].x, v[i].y);
@@ -141,39 +131,52 @@ struct Pack {
   }
 };
 
-// U consecutive elements at any element's address: the aligned vectors around them, shifted into place.  Reads nothing
-// outside [base, end), which the elements must lie in; vectors that would are replaced by single elements.
-template <typename T, int U>
-__device__ __forceinline__ void load_anywhere(Pack<T, U>& out, const T* p, const T* base, const T* end) {
+// Units of a row whose first one lies at any element's address: the aligned vectors around a unit, shifted into place.
+// The shift is the same for every unit of the row, so the words to skip are a compile-time number, chosen once per row.
+//   with_shift(first, n, base, end, f) calls f(how), and load_shifted<how> loads a unit; [base, end) is the tensor, outside of
+//   which nothing is read (a row at its edge is read element by element), n the elements of the row from `first` on.
+constexpr int kElements = -2, kInPlace = -1;   // else: whole words to skip, 0 .. 3
+
+template <typename T, int U, int HOW>
+__device__ __forceinline__ void load_shifted(Pack<T, U>& out, const T* p) {
   constexpr int N = U * (int)sizeof(T) / 16;
   static_assert(N >= 1, "whole vectors");
-  const uintptr_t at = (uintptr_t)p;
-  const int m = (int)(at & 15);
-  const uint4* v = (const uint4*)(at - m);
-  if ((const char*)v < (const char*)base || (const char*)(v + N + (m != 0)) > (const char*)end) {
+  if constexpr (HOW == kElements) {
     out.load_part(p, 0, U);
-    return;
-  }
-  uint32_t w[4 * N + 4];
+  } else if constexpr (HOW == kInPlace) {
+    out.load(p);
+  } else {
+    const uint4* v = (const uint4*)((uintptr_t)p & ~(uintptr_t)15);
+    uint32_t w[4 * N + 4];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const uint4 q = v[i];
-    w[4 * i] = q.x, w[4 * i + 1] = q.y, w[4 * i + 2] = q.z, w[4 * i + 3] = q.w;
-  }
-  const uint4 q = m ? v[N] : make_uint4(0, 0, 0, 0);
-  w[4 * N] = q.x, w[4 * N + 1] = q.y, w[4 * N + 2] = q.z, w[4 * N + 3] = q.w;
-  if (m & 4) {
+    for (int i = 0; i <= N; ++i) {
+      const uint4 q = v[i];
+      w[4 * i] = q.x, w[4 * i + 1] = q.y, w[4 * i + 2] = q.z, w[4 * i + 3] = q.w;
+    }
+    uint32_t o[4 * N];
 #pragma unroll
-    for (int i = 0; i < 4 * N + 3; ++i) w[i] = w[i + 1];
+    for (int i = 0; i < 4 * N; ++i) {
+      if constexpr (sizeof(T) == 4) o[i] = w[HOW + i];
+      else o[i] = __funnelshift_r(w[HOW + i], w[HOW + i + 1], ((uintptr_t)p & 3) * 8);
+    }
+    memcpy(out.r, o, sizeof(o));
   }
-  if (m & 8) {
-#pragma unroll
-    for (int i = 0; i < 4 * N + 2; ++i) w[i] = w[i + 2];
-  }
-  uint32_t o[4 * N];
-#pragma unroll
-  for (int i = 0; i < 4 * N; ++i) o[i] = __funnelshift_r(w[i], w[i + 1], (m & 3) * 8);
-  memcpy(out.r, o, sizeof(o));
+}
+
+template <int V>
+struct Int {
+  static constexpr int value = V;
+};
+template <typename T, typename F>
+__device__ __forceinline__ void with_shift(const T* first, int n, const T* base, const T* end, F f) {
+  const uintptr_t at = (uintptr_t)first, lo = at & ~(uintptr_t)15, hi = ((uintptr_t)(first + n) + 15) & ~(uintptr_t)15;
+  const int m = (int)(at & 15);
+  if (m == 0) f(Int<kInPlace>{});
+  else if (lo < (uintptr_t)base || hi > (uintptr_t)end) f(Int<kElements>{});
+  else if (m < 4) f(Int<0>{});
+  else if (m < 8) f(Int<1>{});
+  else if (m < 12) f(Int<2>{});
+  else f(Int<3>{});
 }
 
 // Host: which layout the tensors of a call allow.  `unit` is U; add every tensor (null: not part of the call).
