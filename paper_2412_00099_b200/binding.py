@@ -6,7 +6,6 @@ the library's CUDA kernels.  There is no CPU fallback; a missing library or devi
 from __future__ import annotations
 
 import ctypes as C
-import functools
 import os
 from typing import NamedTuple, Optional
 
@@ -408,7 +407,23 @@ def belady_replay(sel_trace: torch.Tensor, n_experts: int, capacities) -> torch.
 
 
 # -- operators around the experts ------------------------------------------------------------------------------
-_CODE = {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
+_fast = None
+
+
+def _marshal():
+    """The extension module that checks the tensors and calls the library, connected to it on first use."""
+    global _fast
+    if _fast is None:
+        lib = load()
+        path = os.path.join(_HERE, "_marshal.so")
+        if not os.path.exists(path):
+            raise McceError("_marshal.so is missing: build it with `python -m paper_2412_00099_b200.build`")
+        from . import _marshal as m
+        m.connect(McceError, *[C.cast(getattr(lib, n), C.c_void_p).value for n in (
+            "mcce_rmsnorm", "mcce_rmsnorm_backward_workspace_bytes", "mcce_rmsnorm_backward", "mcce_dispatch_workspace_bytes",
+            "mcce_dispatch", "mcce_combine", "mcce_combine_backward", "mcce_strerror")])
+        _fast = m
+    return _fast
 
 
 class NormOut(NamedTuple):
@@ -433,131 +448,39 @@ def _need(ok, msg):
         raise McceError(msg)
 
 
-def _code(t, what):
-    c = _CODE.get(t.dtype)
-    if c is None:
-        raise McceError("%s has dtype %s" % (what, t.dtype))
-    return c
-
-
-def _ld(t, shape, dev, what):
-    """Row stride of a tensor of this shape whose rows are evenly spaced (the stride may exceed the width)."""
-    if t.shape == shape and t.get_device() == dev and t.is_contiguous():
-        return shape[-1]
-    if t.shape != shape or t.get_device() != dev:
-        raise McceError("%s is %s on %s, expected %s on cuda:%d" % (what, tuple(t.shape), t.device, tuple(shape), dev))
-    try:
-        v = t.view(-1, shape[-1])
-    except RuntimeError:
-        raise McceError("%s: rows must be evenly spaced" % what) from None
-    ld = v.stride(0) if v.shape[0] > 1 else shape[-1]
-    _need(v.stride(1) == 1 or shape[-1] == 1, "%s: the columns of a row must be contiguous" % what)
-    _need(ld >= shape[-1], "%s: rows overlap" % what)
-    return ld
-
-
-def _dense(t, shape, dtype, dev, what):
-    if t.shape != shape or t.dtype != dtype or t.get_device() != dev or not t.is_contiguous():
-        raise McceError("%s: expected contiguous %s %s on cuda:%d" % (what, dtype, tuple(shape), dev))
-
-
-def _at(t):
-    return None if t is None else t.data_ptr()
-
-
-def _cuda(t):
-    """Index of the tensor's device."""
-    dev = t.get_device()
-    if dev < 0:
-        raise McceError("no CUDA tensor: this library has no CPU path")
-    return dev
-
-
-def _call(fn, dev, *args):
-    """Calls an entry point that uses the current device, on the current stream of the tensors' device.  These calls take
-    a few microseconds on the device, so the handle comes without a Stream object around it."""
-    if torch._C._cuda_getDevice() == dev:
-        rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
-    else:
-        with torch.cuda.device(dev):
-            rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
-    if rc:
-        _check(rc)
-
-
-# Descriptors and their workspace sizes, by shape and type alone.
-@functools.lru_cache(maxsize=1024)
-def _norm_desc(*fields):
-    n = Norm(*fields)
-    return n, C.byref(n), load().mcce_rmsnorm_backward_workspace_bytes(C.byref(n))
-
-
-@functools.lru_cache(maxsize=1024)
-def _rows_desc(*fields):
-    r = Rows(*fields)
-    return r, C.byref(r), load().mcce_dispatch_workspace_bytes(C.byref(r))
+def _on_cuda(t):
+    _need(isinstance(t, torch.Tensor) and t.is_cuda, "no CUDA tensor: this library has no CPU path")
+    return t.device
 
 
 def rmsnorm(x, weight, eps=1e-6, add=None, quant_group=None, want_out=True, out: Optional[NormOut] = None) -> NormOut:
     """h = x + add (returned as `sum` when add is given), out = h / rms(h) * weight; with quant_group (0: one scale per
     row, else 32, 64 or 128 columns per scale) also the 8-bit rows `q` and their `scales`.  x [..., d] fp32 or bf16;
     add fp32 or x's type; weight [d] fp32 or x's type.  `out` gives the result tensors (out.sum may be x); a field that
-    is None is not computed."""
-    lib, dev, shape = _lib or load(), _cuda(x), x.shape
-    _need(x.dim() >= 1 and shape[-1] >= 1, "x must have columns")
-    d = shape[-1]
-    rows = x.numel() // d
-    code = _code(x, "x")
+    is None is not computed.  Not differentiable by itself: rmsnorm_backward is its gradient."""
     if out is None:
+        dev, shape = _on_cuda(x), x.shape
+        _need(x.dim() >= 1 and shape[-1] >= 1, "x must have columns")
         q = scales = None
         if quant_group is not None:
-            cols = -(-d // quant_group) if quant_group > 0 else 1
+            cols = -(-shape[-1] // quant_group) if quant_group > 0 else 1
             q = torch.empty(shape, dtype=torch.float8_e4m3fn, device=dev)
             scales = torch.empty(shape[:-1] + (cols,), dtype=torch.float32, device=dev)
         out = NormOut(torch.empty(shape, dtype=x.dtype, device=dev) if want_out else None,
                       torch.empty(shape, dtype=x.dtype, device=dev) if add is not None else None, q, scales)
-    o, h, q, scales = out
-    for t, what in ((o, "out"), (h, "sum")):
-        _need(t is None or t.dtype == x.dtype, "%s must have the type of x" % what)
-    group = 0
-    if q is not None:
-        _need(quant_group is not None and scales is not None, "8-bit rows need quant_group and scales")
-        _need(q.dtype == torch.float8_e4m3fn, "q must be float8_e4m3fn")
-        group = quant_group
-        _dense(scales, shape[:-1] + (-(-d // group) if group > 0 else 1,), torch.float32, dev, "scales")
-    else:
-        _need(quant_group is None and scales is None, "quant_group without 8-bit rows")
-    _dense(weight, (d,), weight.dtype, dev, "weight")
-    n, ref, _ = _norm_desc(rows, d, code, code if add is None else _code(add, "add"), _code(weight, "weight"), group, eps,
-                           _ld(x, shape, dev, "x"), 0 if add is None else _ld(add, shape, dev, "add"),
-                           0 if h is None else _ld(h, shape, dev, "sum"), 0 if o is None else _ld(o, shape, dev, "out"),
-                           0 if q is None else _ld(q, shape, dev, "q"))
-    _call(lib.mcce_rmsnorm, dev, ref, x.data_ptr(), _at(add), weight.data_ptr(), _at(h), _at(o), _at(q), _at(scales))
+    (_fast or _marshal()).rmsnorm(x, weight, eps, add, quant_group, *out)
     return out
 
 
 def rmsnorm_backward(dout, h, weight, eps=1e-6, dsum=None, want_dweight=True, out=None):
     """Gradient of rmsnorm: dx (the gradient of x and of add) and dweight (fp32, None if not wanted).  h is the `sum` of the
     forward call, dsum the gradient that reaches it past the norm; `out` = (dx, dweight)."""
-    lib, dev, shape = _lib or load(), _cuda(h), h.shape
-    _need(h.dim() >= 1 and shape[-1] >= 1, "h must have columns")
-    d = shape[-1]
-    code = _code(h, "h")
     if out is None:
-        out = (torch.empty(shape, dtype=h.dtype, device=dev),
-               torch.empty(d, dtype=torch.float32, device=dev) if want_dweight else None)
-    dx, dw = out
-    for t, what in ((dout, "dout"), (dsum, "dsum"), (dx, "dx")):
-        _need(t is None or t.dtype == h.dtype, "%s must have the type of h" % what)
-    _dense(weight, (d,), weight.dtype, dev, "weight")
-    if dw is not None:
-        _dense(dw, (d,), torch.float32, dev, "dweight")
-    n, ref, nbytes = _norm_desc(h.numel() // d, d, code, code, _code(weight, "weight"), 0, eps, _ld(h, shape, dev, "h"),
-                                0 if dsum is None else _ld(dsum, shape, dev, "dsum"), _ld(dx, shape, dev, "dx"),
-                                _ld(dout, shape, dev, "dout"), 0)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if dw is not None else None
-    _call(lib.mcce_rmsnorm_backward, dev, ref, dout.data_ptr(), h.data_ptr(), _at(dsum), weight.data_ptr(), dx.data_ptr(),
-          _at(dw), _at(ws), nbytes)
+        dev = _on_cuda(h)
+        _need(h.dim() >= 1, "h must have columns")
+        out = (torch.empty(h.shape, dtype=h.dtype, device=dev),
+               torch.empty(h.shape[-1], dtype=torch.float32, device=dev) if want_dweight else None)
+    (_fast or _marshal()).rmsnorm_backward(dout, h, weight, eps, dsum, *out)
     return out
 
 
@@ -565,88 +488,39 @@ def dispatch(sel_idx, n_experts, x=None, scales=None, out: Optional[Dispatched] 
     """Sorts token rows by expert.  sel_idx [T,K] or [L,T,K] int32; x [(L,)T,d] fp32, bf16 or float8_e4m3fn; scales [(L,)T,n]
     fp32.  Returns offsets [(L,)E+1], perm [(L,)T*K], inv like sel_idx, rows [(L,)T*K,d], scales [(L,)T*K,n]; what lies
     behind the last bucket is left as it was (with `out`) or undefined."""
-    lib, dev = _lib or load(), _cuda(sel_idx)
-    _need(sel_idx.dim() in (2, 3), "sel_idx must be [T,K] or [L,T,K]")
-    head, (T, K) = sel_idx.shape[:-2], sel_idx.shape[-2:]
-    L = head[0] if head else 1
-    d, n, code = 1, 0, BF16
-    _dense(sel_idx, sel_idx.shape, torch.int32, dev, "sel_idx")
-    if x is not None:
-        _need(x.dim() == len(head) + 2, "x must have the leading sizes of sel_idx")
-        d, code = x.shape[-1], _code(x, "x")
-    if scales is not None:
-        n = scales.shape[-1]
-        _dense(scales, head + (T, n), torch.float32, dev, "scales")
     if out is None:
+        dev = _on_cuda(sel_idx)
+        _need(sel_idx.dim() in (2, 3), "sel_idx must be [T,K] or [L,T,K]")
+        _need(0 < n_experts <= 256, "n_experts must be 1 .. 256")
+        head, pairs = sel_idx.shape[:-2], sel_idx.shape[-2] * sel_idx.shape[-1]
         i32 = dict(dtype=torch.int32, device=dev)
-        out = Dispatched(torch.empty(head + (n_experts + 1,), **i32), torch.empty(head + (T * K,), **i32),
+        out = Dispatched(torch.empty(head + (n_experts + 1,), **i32), torch.empty(head + (pairs,), **i32),
                          torch.empty(sel_idx.shape, **i32),
-                         None if x is None else torch.empty(head + (T * K, d), dtype=x.dtype, device=dev),
-                         None if scales is None else torch.empty(head + (T * K, n), dtype=torch.float32, device=dev))
-    _dense(out.offsets, head + (n_experts + 1,), torch.int32, dev, "offsets")
-    _dense(out.inv, sel_idx.shape, torch.int32, dev, "inv")
-    if out.perm is not None:
-        _dense(out.perm, head + (T * K,), torch.int32, dev, "perm")
-    _need((x is None) == (out.rows is None) and (scales is None) == (out.scales is None),
-          "rows and scales are wanted exactly where x and scales are given")
-    ld_x = ld_rows = 0
-    if x is not None:
-        _need(out.rows.dtype == x.dtype, "rows must have the type of x")
-        ld_x, ld_rows = _ld(x, head + (T, d), dev, "x"), _ld(out.rows, head + (T * K, d), dev, "rows")
-    if scales is not None:
-        _dense(out.scales, head + (T * K, n), torch.float32, dev, "scales of the rows")
-    r, ref, nbytes = _rows_desc(L, T, K, n_experts, d, code, code, n, ld_x, ld_rows)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-    _call(lib.mcce_dispatch, dev, ref, sel_idx.data_ptr(), _at(x), _at(scales), out.offsets.data_ptr(), _at(out.perm),
-          out.inv.data_ptr(), _at(out.rows), _at(out.scales), _at(ws), nbytes)
+                         None if x is None else torch.empty(head + (pairs, x.shape[-1]), dtype=x.dtype, device=dev),
+                         None if scales is None else torch.empty(head + (pairs, scales.shape[-1]), dtype=torch.float32,
+                                                                 device=dev))
+    (_fast or _marshal()).dispatch(sel_idx, n_experts, x, scales, *out)
     return out
-
-
-def _pairs(rows, inv, dev):
-    """Leading sizes, L, T, K and d of sorted rows [(L,)T*K,d] with positions inv [(L,)T,K]."""
-    _need(inv.dim() in (2, 3) and rows.dim() == inv.dim(), "inv must be [T,K] or [L,T,K], rows [T*K,d] or [L,T*K,d]")
-    head, (T, K) = inv.shape[:-2], inv.shape[-2:]
-    _dense(inv, inv.shape, torch.int32, dev, "inv")
-    return head, head[0] if head else 1, T, K, rows.shape[-1]
 
 
 def combine(rows, inv, sel_w=None, add=None, out_dtype=None, out=None):
     """y[t] = add[t] + sum_k sel_w[t,k] rows[inv[t,k]] (weights 1 without sel_w: the gradient of dispatch with respect to
     x).  rows [(L,)T*K,d] fp32 or bf16, inv and sel_w [(L,)T,K]; y [(L,)T,d] in out_dtype: fp32, or the type of rows
     (the default).  `out` may be add."""
-    lib, dev = _lib or load(), _cuda(rows)
-    head, L, T, K, d = _pairs(rows, inv, dev)
     if out is None:
-        out = torch.empty(head + (T, d), dtype=out_dtype or rows.dtype, device=dev)
-    if sel_w is not None:
-        _dense(sel_w, inv.shape, torch.float32, dev, "sel_w")
-    ld_rows, ld_y = _ld(rows, head + (T * K, d), dev, "rows"), _ld(out, head + (T, d), dev, "out")
-    if add is not None:
-        _need(add.dtype == out.dtype and _ld(add, head + (T, d), dev, "add") == ld_y,
-              "add must have the type and the row stride of out")
-    r, ref, _ = _rows_desc(L, T, K, 1, d, _code(rows, "rows"), _code(out, "out"), 0, ld_y, ld_rows)
-    _call(lib.mcce_combine, dev, ref, rows.data_ptr(), inv.data_ptr(), _at(sel_w), _at(add), out.data_ptr())
+        _on_cuda(rows)
+        _need(inv.dim() in (2, 3) and rows.dim() == inv.dim(), "inv must be [T,K] or [L,T,K], rows [T*K,d] or [L,T*K,d]")
+        out = torch.empty(inv.shape[:-1] + rows.shape[-1:], dtype=out_dtype or rows.dtype, device=rows.device)
+    (_fast or _marshal()).combine(rows, inv, sel_w, add, out)
     return out
 
 
 def combine_backward(dy, rows, inv, sel_w=None, want_dw=True, out=None):
     """Gradient of combine: drows (in the type of rows; rows at positions that inv does not name are left as they were) and
     dw [(L,)T,K] fp32 (None if not wanted).  `out` = (drows, dw); drows may be rows."""
-    lib, dev = _lib or load(), _cuda(rows)
-    head, L, T, K, d = _pairs(rows, inv, dev)
     if out is None:
-        out = (torch.empty(head + (T * K, d), dtype=rows.dtype, device=dev),
-               torch.empty(inv.shape, dtype=torch.float32, device=dev) if want_dw else None)
-    drows, dw = out
-    if sel_w is not None:
-        _dense(sel_w, inv.shape, torch.float32, dev, "sel_w")
-    if dw is not None:
-        _dense(dw, inv.shape, torch.float32, dev, "dw")
-    ld_rows = _ld(rows, head + (T * K, d), dev, "rows")
-    _need(drows.dtype == rows.dtype and _ld(drows, head + (T * K, d), dev, "drows") == ld_rows,
-          "drows must have the type and the row stride of rows")
-    r, ref, _ = _rows_desc(L, T, K, 1, d, _code(rows, "rows"), _code(dy, "dy"), 0, _ld(dy, head + (T, d), dev, "dy"),
-                           ld_rows)
-    _call(lib.mcce_combine_backward, dev, ref, dy.data_ptr(), rows.data_ptr(), inv.data_ptr(), _at(sel_w), drows.data_ptr(),
-          _at(dw))
+        _on_cuda(rows)
+        out = (torch.empty_strided(rows.shape, rows.stride(), dtype=rows.dtype, device=rows.device),
+               torch.empty(inv.shape, dtype=torch.float32, device=rows.device) if want_dw else None)
+    (_fast or _marshal()).combine_backward(dy, rows, inv, sel_w, *out)
     return out

@@ -1,7 +1,8 @@
-"""Builds libmcce.so (CUDA, sm_100a only) next to this file:  python -m paper_2412_00099_b200.build"""
+"""Builds libmcce.so (CUDA, sm_100a only) and _marshal.so next to this file:  python -m paper_2412_00099_b200.build"""
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
 from concurrent.futures import ThreadPoolExecutor
@@ -11,6 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmcce.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 SOURCES = ["api.cu", "route.cu", "route_thread.cu", "route_static.cu", "route_gemm.cu", "route_gemm_res.cu", "route_fused.cu", "belady.cu", "group.cu", "ffn_simt.cu", "ffn_tc.cu", "norm.cu", "rows.cu", "gen.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC,-Wall", "-I", INCLUDE, "-I", CSRC]
@@ -24,6 +26,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
     srcs = [os.path.join(CSRC, s) for s in SOURCES]
     deps = srcs + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cuh")] + [
         os.path.join(INCLUDE, "mcce.h")]
+    marshal = build_marshal(force)
+    if verbose:
+        sys.stderr.write("%s\n" % marshal)
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest(deps):
         return LIB
     os.makedirs(OBJ, exist_ok=True)
@@ -43,6 +48,27 @@ def build(force: bool = False, verbose: bool = False) -> str:
         objs = list(ex.map(compile_one, srcs))
     subprocess.check_call([nvcc, "-shared", "-o", LIB, *objs, "-gencode", "arch=compute_100a,code=sm_100a"])
     return LIB
+
+
+def build_marshal(force: bool = False) -> str:
+    """Builds _marshal.so, the torch side of the operators' binding (host code: g++ against torch's own headers)."""
+    src, header = os.path.join(CSRC, "marshal.cpp"), os.path.join(INCLUDE, "mcce.h")
+    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= _newest([src, header]):
+        return MARSHAL
+    import sysconfig
+
+    import torch
+    home = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(shutil.which(os.environ.get("NVCC", "nvcc")))))
+    includes = [INCLUDE, os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"),
+                sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+           *[x for i in includes for x in ("-isystem" if i != INCLUDE else "-I", i)], src, "-o", MARSHAL,
+           "-L" + os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed for marshal.cpp:\n%s" % r.stderr)
+    return MARSHAL
 
 
 if __name__ == "__main__":
