@@ -125,6 +125,10 @@ int mcce_set_router(mcce_ctx* ctx, const float* Wr, const float* fixed_delta);
 int mcce_set_experts(mcce_ctx* ctx, const void* Wg, const void* Wu, const void* Wd, const void* shWg,
                      const void* shWu, const void* shWd);
 
+/* Root-mean-square norm in front of every layer's router and experts in mcce_decode_step_chained (mcce_rmsnorm's
+ * formulas).  weight: DEVICE fp32 [L,d], 16-byte aligned, borrowed; eps finite, >= 0.  NULL: no norm (the state after mcce_create). */
+int mcce_set_norm(mcce_ctx* ctx, const float* weight, float eps);
+
 /* Empties every cache, or loads an initial cache content (Sec. 4.8 "Impact of Initial Cache State"):
  * init_order HOST int32 [L,S,C], resident experts most-recently-used first, -1 padding; NULL = empty.
  * These entries count as older than anything touched later.  Counters are zeroed.  The running
@@ -165,7 +169,9 @@ int mcce_moe_forward(mcce_ctx* ctx, const void* hidden, const int32_t* sel_idx, 
 /* One token in sequential-layer mode: the layers are chained through a residual stream instead of being
  * independent, as in a real decoder (the paper changes nothing in the forward pass but the ranking, Sec. 2.2).
  * For l = 0..L-1: route layer l on its input x_l, run its experts, x_{l+1} = x_l + y_l rounded to the hidden
- * dtype (no normalisation layer: the logit scale may drift with depth, which the per-layer Delta_avg absorbs).
+ * dtype.  Without mcce_set_norm there is no normalisation layer: the logit scale may drift with depth, which the
+ * per-layer Delta_avg absorbs.  With it, layer l routes and runs its experts on mcce_rmsnorm(x_l, weight[l]), as
+ * pre-norm decoders do, and the residual stream x_l itself stays as it is.
  *   x0     DEVICE hidden_dtype [S,d]: input of layer 0        x_out DEVICE hidden_dtype [S,d]: output of layer L-1
  *   sel_idx DEVICE int32 [L,S,K], optional: the selections of every layer
  * Cache state, counters, Delta statistics and the miss trace advance exactly as with mcce_route_step.  Launches
@@ -278,9 +284,10 @@ int mcce_belady_replay(const int32_t* sel_trace, int32_t n_tokens, int32_t n_lay
 
 /* Rows for mcce_rmsnorm and its gradient.  Row strides (ld_*) are in elements, 0 means d; the columns of a row are
  * contiguous and rows of a tensor do not overlap. */
+enum { MCCE_NORM_MAX_D = 16384 };
 typedef struct {
-  int64_t rows;          /* >= 0                                                                              */
-  int32_t d;             /* columns, 1..16384                                                                 */
+  int64_t rows;          /* 0..2^31-1                                                                         */
+  int32_t d;             /* columns, 1..MCCE_NORM_MAX_D                                                                 */
   int32_t dtype;         /* x, sum, out, and the gradients: MCCE_F32 or MCCE_BF16                             */
   int32_t add_dtype;     /* MCCE_F32 (what mcce_moe_forward returns) or dtype                                 */
   int32_t weight_dtype;  /* MCCE_F32 or dtype                                                                 */

@@ -24,7 +24,7 @@ ROUTE_AUTO, ROUTE_TWO_KERNELS, ROUTE_FUSED = 0, 1, 2
 ROUTER_FP32_PIPE, ROUTER_GEMM_TAIL, ROUTER_RESIDENT_TAIL, ROUTER_FUSED = 0, 1, 2, 3
 
 EXPORTS = [
-    "mcce_workspace_bytes", "mcce_create", "mcce_destroy", "mcce_set_router", "mcce_set_experts", "mcce_reset",
+    "mcce_workspace_bytes", "mcce_create", "mcce_destroy", "mcce_set_router", "mcce_set_experts", "mcce_set_norm", "mcce_reset",
     "mcce_route_step", "mcce_moe_forward", "mcce_decode_step_host", "mcce_decode_step_chained", "mcce_pipeline_submit_host", "mcce_pipeline_submit", "mcce_pipeline_wait", "mcce_cache_stats", "mcce_calibrate_delta", "mcce_get_cache_state",
     "mcce_get_grouping", "mcce_lifetime_stats", "mcce_set_miss_trace", "mcce_belady_replay",
     "mcce_rmsnorm", "mcce_rmsnorm_backward", "mcce_rmsnorm_backward_workspace_bytes", "mcce_dispatch", "mcce_dispatch_workspace_bytes",
@@ -83,6 +83,7 @@ def load():
         lib.mcce_destroy.argtypes = [vp]
         lib.mcce_set_router.argtypes = [vp, vp, vp]
         lib.mcce_set_experts.argtypes = [vp] * 7
+        lib.mcce_set_norm.argtypes = [vp, vp, f32]
         lib.mcce_reset.argtypes = [vp, vp, C.c_int, vp, C.c_int64]
         lib.mcce_route_step.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp]
         lib.mcce_moe_forward.argtypes = [vp] * 6
@@ -197,6 +198,12 @@ class Engine:
             assert t is None or t.dtype == _tdtype(self.dtype)
         self._keep += [Wg, Wu, Wd, shWg, shWu, shWd]
         _check(self.lib.mcce_set_experts(self.ctx, *[_ptr(t) for t in (Wg, Wu, Wd, shWg, shWu, shWd)]), self.ctx)
+
+    def set_norm(self, weight: torch.Tensor | None, eps: float = 1e-6):
+        """Root-mean-square norm in front of every layer of decode_step_chained: weight [L,d] fp32, None for no norm."""
+        assert weight is None or (weight.dtype == torch.float32 and tuple(weight.shape) == (self.L, self.d))
+        _check(self.lib.mcce_set_norm(self.ctx, _ptr(weight), eps), self.ctx)
+        self._norm_weight = weight
 
     def reset(self, init_order: np.ndarray | None = None, keep_delta_stats=False, delta_sum=None, delta_count=0):
         if init_order is not None:

@@ -48,6 +48,8 @@ struct mcce_ctx {
   int pipe_ready, pipe_slot, pipe_busy[2], pipe_used[2];
   // borrowed weights
   const float *Wr, *fixed_delta;
+  const float* norm_weight;   // [L,d] of the chained step's norms, or null
+  float norm_eps;
   const void *Wg, *Wu, *Wd, *shWg, *shWu, *shWd;
   // optional per-token miss trace (caller's buffer)
   uint32_t* miss_trace;
@@ -351,6 +353,14 @@ extern "C" int mcce_set_experts(mcce_ctx* ctx, const void* Wg, const void* Wu, c
   return MCCE_OK;
 }
 
+extern "C" int mcce_set_norm(mcce_ctx* ctx, const float* weight, float eps) {
+  if (!ctx || ((uintptr_t)weight % 16)) return MCCE_EINVAL;
+  if (weight && (!(eps >= 0.f) || !isfinite(eps) || ctx->cfg.d_model > MCCE_NORM_MAX_D)) return MCCE_EINVAL;
+  ctx->norm_weight = weight;
+  ctx->norm_eps = eps;
+  return MCCE_OK;
+}
+
 extern "C" int mcce_reset(mcce_ctx* ctx, const int32_t* init_order, int keep_delta_stats, const float* delta_sum,
                           int64_t delta_count) {
   if (!ctx) return MCCE_EINVAL;
@@ -604,16 +614,34 @@ extern "C" int mcce_decode_step_chained(mcce_ctx* ctx, const void* x0, void* x_o
   const size_t S = c.n_streams, K = c.top_k, n = S * c.d_model;
   const bool bf16 = c.hidden_dtype == MCCE_BF16;
   void* buf[2] = {ctx->stage_hidden, ctx->stage_hidden2};
+  // normalised input of the current layer: behind the residual stream in its staging buffer (a single layer does not stage
+  // the residual stream)
+  char* normed = (char*)ctx->stage_hidden + (c.n_layers > 1 ? n * (bf16 ? 2 : 4) : 0);
+  mcce_norm nd{};
+  nd.rows = c.n_streams, nd.d = c.d_model, nd.dtype = c.hidden_dtype, nd.eps = ctx->norm_eps;
+  auto norm = [&](int l, const void* in, const float* add, void* sum) {
+    return mcce_rmsnorm(&nd, in, add, ctx->norm_weight + (size_t)l * c.d_model, sum, normed, nullptr, nullptr, cuda_stream);
+  };
   const void* x = x0;
+  if (ctx->norm_weight) {
+    const int rc = norm(0, x0, nullptr, nullptr);
+    if (rc != MCCE_OK) return rc;
+  }
   for (int l = 0; l < c.n_layers; ++l) {
+    const void* in = ctx->norm_weight ? normed : x;
     int32_t* sel = ctx->stage_sel + (size_t)l * S * K;
     float* w = ctx->stage_w + (size_t)l * S * K;
-    int rc = route_one_layer(ctx, l, x, sel, w, st);
+    int rc = route_one_layer(ctx, l, in, sel, w, st);
     if (rc != MCCE_OK) return rc;
-    rc = forward_layers(ctx, l, 1, x, sel, w, ctx->stage_y, st);
+    rc = forward_layers(ctx, l, 1, in, sel, w, ctx->stage_y, st);
     if (rc != MCCE_OK) return rc;
     void* nxt = l + 1 == c.n_layers ? x_out : buf[l & 1];
-    CK(launch_residual(x, ctx->stage_y, nxt, n, bf16, st));
+    if (ctx->norm_weight && l + 1 < c.n_layers) {   // x + y and its norm for the next layer in one kernel
+      rc = norm(l + 1, x, ctx->stage_y, nxt);
+      if (rc != MCCE_OK) return rc;
+    } else {
+      CK(launch_residual(x, ctx->stage_y, nxt, n, bf16, st));
+    }
     x = nxt;
   }
   if (sel_idx)

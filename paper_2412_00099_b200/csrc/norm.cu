@@ -11,7 +11,7 @@ namespace mcce {
 namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
-constexpr int kMaxNormD = 16384;
+constexpr int kMaxNormD = MCCE_NORM_MAX_D;
 constexpr float kE4m3Max = 448.f;
 constexpr uint32_t kAmaxFloor = 0x0d800000u;   // bits of 2^-100
 
@@ -703,8 +703,10 @@ GradShape grad_shape(int64_t rows, int d, Layout3 lay, int elem_bytes, bool dsum
   while (g.stages > 1 && grad_smem(g.s, g.stages, d, ragged, dsum, dweight) > kGradSmemMost / per_sm) --g.stages;
   g.smem = grad_smem(g.s, g.stages, d, ragged, dsum, dweight);
   int ctas = per_sm * kSms;
-  if (ragged) ctas = ctas / u * u;   // rows of a CTA: a multiple of u apart
+  if (ragged) ctas = ctas / u * u;   // rows of a thread: a multiple of u apart
   g.ctas = (int)(all < ctas ? all : ctas);
+  // a few rows one after the other in a single CTA take less time than the launch that adds several CTAs' parts
+  if (dweight && all <= 4 && (!ragged || rpb % u == 0)) g.ctas = 1;
   return g;
 }
 int parts_most(const mcce_norm& n) {
@@ -830,6 +832,8 @@ extern "C" int mcce_rmsnorm_backward(const mcce_norm* n, const void* dout, const
   const Layout3 lay = aligned(weight, 16) ? rule.layout() : kScalar;
   a.off = rule.off;
   const GradShape g = grad_shape(n->rows, n->d, lay, e, dsum != nullptr, dweight != nullptr);
+  const bool direct = g.ctas == 1 && aligned(dweight, 16);   // the only part is the result
+  if (direct) a.part = dweight;
   cudaError_t err;
   if (lay == kScalar) {
     if (n->dtype == MCCE_F32) rmsnorm_grad_scalar_kernel<float><<<g.ctas, kThreads, 0, st>>>(a);
@@ -838,8 +842,6 @@ extern "C" int mcce_rmsnorm_backward(const mcce_norm* n, const void* dout, const
   } else {
     err = launch_grad_types(a, n->dtype, lay == kRagged, g, st);
   }
-  if (err == cudaSuccess && dweight) {
-    err = launch_dweight(a.part, dweight, g.ctas, n->d, st);
-  }
+  if (err == cudaSuccess && dweight && !direct) err = launch_dweight(a.part, dweight, g.ctas, n->d, st);
   return err == cudaSuccess ? MCCE_OK : MCCE_ECUDA;
 }

@@ -8,92 +8,28 @@ namespace mcce {
 namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
-constexpr int kSortChunk = 1024;   // pairs per CTA of the counting sort
-
 struct SortArgs {
-  int T, K, E, P, B;
+  int T, K, E, P;
+  int chunk, B;   // tokens per chunk, chunks per layer
   const int32_t* sel;
-  int32_t *offsets, *perm, *inv, *counts;   // counts [L][B][E]
+  int32_t *offsets, *perm, *inv, *counts;   // counts [L][B][E], not used when B is 1
 };
 
-__global__ void __launch_bounds__(256) rows_count_kernel(const SortArgs a) {
-  __shared__ int hist[kMaxE];
+// Pairs of every expert in a chunk of a layer.
+__global__ void __launch_bounds__(256) rows_count_kernel(const __grid_constant__ SortArgs s) {
+  __shared__ int count[kMaxE];
   const int b = blockIdx.x, l = blockIdx.y;
-  for (int e = threadIdx.x; e < a.E; e += 256) hist[e] = 0;
+  count[threadIdx.x] = 0;
   __syncthreads();
-  for (int i = threadIdx.x; i < kSortChunk; i += 256) {
-    const int64_t q = (int64_t)b * kSortChunk + i;
-    if (q < a.P) {
-      const int e = a.sel[(size_t)l * a.P + q];
-      if ((unsigned)e < (unsigned)a.E) atomicAdd(&hist[e], 1);
-    }
+  const int32_t* sel = s.sel + (size_t)l * s.P;
+  const int end = min(s.P, (b + 1) * s.chunk * s.K);
+#pragma unroll 4
+  for (int q = b * s.chunk * s.K + threadIdx.x; q < end; q += 256) {
+    const int e = sel[q];
+    if ((unsigned)e < (unsigned)s.E) atomicAdd(&count[e], 1);
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < a.E; e += 256) a.counts[((size_t)l * a.B + b) * a.E + e] = hist[e];
-}
-
-__global__ void __launch_bounds__(kSortChunk) rows_rank_kernel(const SortArgs a) {
-  cudaGridDependencySynchronize();
-  __shared__ int total[kMaxE], before[kMaxE], warp_at[kSortChunk / 32][kMaxE];
-  const int b = blockIdx.x, l = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  if (tid < a.E) total[tid] = before[tid] = 0;
-  for (int i = tid; i < kSortChunk / 32 * kMaxE; i += kSortChunk) (&warp_at[0][0])[i] = 0;
-  __syncthreads();
-  {
-    const int n_sub = kSortChunk / a.E, e = tid % a.E, sub = tid / a.E;
-    if (sub < n_sub) {
-      int all = 0, mine = 0;
-      const int* c = a.counts + (size_t)l * a.B * a.E + e;
-#pragma unroll 8
-      for (int i = sub; i < a.B; i += n_sub) {
-        const int n = c[(size_t)i * a.E];
-        all += n;
-        if (i < b) mine += n;
-      }
-      atomicAdd(&total[e], all);
-      atomicAdd(&before[e], mine);
-    }
-  }
-  __syncthreads();
-  if (warp == 0) {   // exclusive scan over the experts
-    int run = 0;
-    for (int e0 = 0; e0 < a.E; e0 += 32) {
-      const int n = e0 + lane < a.E ? total[e0 + lane] : 0;
-      int s = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(kFull, s, o);
-        if (lane >= o) s += v;
-      }
-      if (e0 + lane < a.E) {
-        before[e0 + lane] += run + s - n;
-        if (b == 0) a.offsets[(size_t)l * (a.E + 1) + e0 + lane] = run + s - n;
-      }
-      run += __shfl_sync(kFull, s, 31);
-    }
-    if (b == 0 && lane == 0) a.offsets[(size_t)l * (a.E + 1) + a.E] = run;
-  }
-  const int64_t q = (int64_t)b * kSortChunk + tid;
-  int e = q < a.P ? a.sel[(size_t)l * a.P + q] : -1;
-  if ((unsigned)e >= (unsigned)a.E) e = -1;
-  const unsigned peers = __match_any_sync(kFull, e);
-  const int rank = __popc(peers & ((1u << lane) - 1u));
-  if (e >= 0 && rank == 0) warp_at[warp][e] = __popc(peers);
-  __syncthreads();
-  if (tid < a.E) {
-    int run = before[tid];
-    for (int w = 0; w < kSortChunk / 32; ++w) {
-      const int n = warp_at[w][tid];
-      warp_at[w][tid] = run;
-      run += n;
-    }
-  }
-  __syncthreads();
-  if (q < a.P) {
-    const int pos = e >= 0 ? warp_at[warp][e] + rank : -1;
-    a.inv[(size_t)l * a.P + q] = pos;
-    if (a.perm && pos >= 0) a.perm[(size_t)l * a.P + pos] = (int)q;
-  }
+  if ((int)threadIdx.x < s.E) s.counts[((size_t)l * s.B + b) * s.E + threadIdx.x] = count[threadIdx.x];
 }
 
 // ---- moving rows ------------------------------------------------------------------------------------------------
@@ -122,10 +58,8 @@ __device__ __forceinline__ int my_position(const Token& tk, const int32_t* inv, 
 }
 
 struct CopyArgs {
-  int64_t tokens;        // L * T
   int64_t ld_x, ld_rows; // in units
-  int T, K, P, units, scale_cols, tpt;
-  const int32_t* inv;
+  int K, units, scale_cols;
   const void* x;
   void* rows;
   const float* scales;
@@ -156,42 +90,53 @@ __device__ __forceinline__ void move_row(const CopyArgs& a, int64_t t, int64_t f
   }
 }
 
-template <typename V>
-__global__ void __launch_bounds__(256) rows_copy_kernel(const __grid_constant__ CopyArgs a) {
-  cudaGridDependencySynchronize();
-  const Token tk(a.tpt, a.tokens, a.T, a.P);
-  const int mine = my_position(tk, a.inv, a.K, a.P);
-  if (a.x) move_row<V>(a, tk.there ? tk.t : 0, tk.first, tk.u0, a.tpt, [&](int k) { return position(tk, mine, k); });
-  for (int k = 0; a.scale_cols && k < a.K; ++k) {
-    const int pos = position(tk, mine, k);
-    for (int c = tk.u0; pos >= 0 && c < a.scale_cols; c += a.tpt)
-      a.row_scales[(tk.first + pos) * a.scale_cols + c] = a.scales[tk.t * a.scale_cols + c];
-  }
-}
-
-// Few pairs per layer: one launch.  Every CTA counts all pairs of its layer (and, in the upper half of a word, those before
-// its own tokens), ranks its own and moves their rows; the counting takes the place of two more launches.
-constexpr int kFusedPairs = 64;    // pairs of a CTA at most
+// Ranks the pairs of a few tokens and moves their rows.  Where a pair goes: pairs of smaller experts (totals of all chunks), of
+// its expert in earlier chunks (both from the chunks' counts), earlier in its chunk (counted here again), earlier in this
+// CTA.  A layer of few pairs is one chunk: the CTA counts all of it, and there is no launch before this one.
+constexpr int kCtaPairs = 128;    // pairs of a CTA at most
 template <typename V>
 __global__ void __launch_bounds__(256) rows_dispatch_kernel(const __grid_constant__ SortArgs s, const __grid_constant__ CopyArgs a,
                                                             const int tokens_per_cta) {
-  __shared__ int count[kMaxE], base[kMaxE], warp_sum[8], id[kFusedPairs], place[kFusedPairs];
+  __shared__ int total[kMaxE], before[kMaxE], warp_sum[8], id[kCtaPairs], place[kCtaPairs];
   const int l = blockIdx.y, t0 = blockIdx.x * tokens_per_cta, n_tok = min(tokens_per_cta, s.T - t0);
   const int q0 = t0 * s.K, n = n_tok * s.K, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int b = t0 / s.chunk, chunk0 = b * s.chunk * s.K;
   const int32_t* sel = s.sel + (size_t)l * s.P;
-  count[tid] = 0;
+  total[tid] = before[tid] = 0;
   __syncthreads();
   if (tid < n) {
     const int e = sel[q0 + tid];
     id[tid] = (unsigned)e < (unsigned)s.E ? e : -1;
   }
+  if (s.B == 1) {   // total and, in the upper half of a word, before
 #pragma unroll 4
-  for (int q = tid; q < s.P; q += 256) {
-    const int e = sel[q];
-    if ((unsigned)e < (unsigned)s.E) atomicAdd(&count[e], q < q0 ? 0x10001 : 1);
+    for (int q = tid; q < s.P; q += 256) {
+      const int e = sel[q];
+      if ((unsigned)e < (unsigned)s.E) atomicAdd(&total[e], q < q0 ? 0x10001 : 1);
+    }
+  } else {
+#pragma unroll 4
+    for (int q = chunk0 + tid; q < q0; q += 256) {
+      const int e = sel[q];
+      if ((unsigned)e < (unsigned)s.E) atomicAdd(&before[e], 1);
+    }
+    cudaGridDependencySynchronize();
+    const int n_sub = 256 / s.E, e = tid % s.E, sub = tid / s.E;
+    if (sub < n_sub) {
+      const int32_t* c = s.counts + (size_t)l * s.B * s.E + e;
+      int all = 0, mine = 0;
+#pragma unroll 8
+      for (int i = sub; i < s.B; i += n_sub) {
+        const int v = c[(size_t)i * s.E];
+        all += v;
+        if (i < b) mine += v;
+      }
+      atomicAdd(&total[e], all);
+      atomicAdd(&before[e], mine);
+    }
   }
   __syncthreads();
-  const int c = count[tid], all = c & 0xffff;
+  const int packed = total[tid], all = s.B == 1 ? packed & 0xffff : packed;
   int run = all;   // inclusive scan over the experts
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -201,7 +146,7 @@ __global__ void __launch_bounds__(256) rows_dispatch_kernel(const __grid_constan
   if (lane == 31) warp_sum[warp] = run;
   __syncthreads();
   for (int w = 0; w < warp; ++w) run += warp_sum[w];
-  base[tid] = run - all + (c >> 16);
+  before[tid] += run - all + (s.B == 1 ? packed >> 16 : 0);
   if (blockIdx.x == 0) {
     int32_t* off = s.offsets + (size_t)l * (s.E + 1);
     if (tid < s.E) off[tid + 1] = run;
@@ -212,7 +157,7 @@ __global__ void __launch_bounds__(256) rows_dispatch_kernel(const __grid_constan
     const int e = id[tid];
     int pos = -1;
     if (e >= 0) {
-      pos = base[e];
+      pos = before[e];
       for (int j = 0; j < tid; ++j) pos += id[j] == e;
     }
     place[tid] = pos;
@@ -438,6 +383,33 @@ bool aligned(const void* p, size_t a) { return (uintptr_t)p % a == 0; }
 int elem(int dtype) { return dtype == MCCE_F32 ? 4 : dtype == MCCE_BF16 ? 2 : 1; }
 int64_t ld_or(int64_t ld, int d) { return ld ? ld : d; }
 
+// How the pairs of a layer are split: tokens per CTA (`cta`), tokens per chunk (a multiple of it) and chunks.
+struct SortShape {
+  int cta, chunk, B;
+};
+// A CTA moves up to 160 KB: 16384 tokens x 8 of 2048 bytes with scales, us, 4 / 8 tokens: 63.6 / 59; of 4096 bytes 2 / 4 / 8 tokens:
+// 106 / 109 / 111; 24 x 256 tokens x 4 of 4096 bytes 27 / 25 / 27.  Chunks of 2048 pairs: between 512 and 4096 the time changes by
+// 1 %.  A layer is one chunk -- one launch, every CTA counts the whole layer -- while that is little work: 24 x 256 tokens x 4
+// 25.0 against 27.9 with two launches, 4096 tokens x 2 of 8192 bytes 32.7 against 22.8.
+SortShape sort_shape(const mcce_rows& r) {
+  const int K = r.top_k, T = r.n_tokens;
+  const int64_t moved = (int64_t)(K + 1) * r.d * (r.dtype == MCCE_F32 ? 4 : r.dtype == MCCE_BF16 ? 2 : 1);
+  SortShape h;
+  h.cta = 1;
+  while (h.cta * 2 * K <= kCtaPairs && h.cta * 2 * moved <= 160 * 1024) h.cta *= 2;
+  const int64_t pairs = (int64_t)T * K, ctas = (int64_t)r.n_layers * ((T + h.cta - 1) / h.cta);
+  if (pairs <= 2048 || (pairs <= 8192 && ctas * pairs <= (2 << 20))) {
+    h.chunk = T, h.B = 1;
+    return h;
+  }
+  const int most = 16384 / r.n_experts < 256 ? 16384 / r.n_experts : 256;   // chunks: every CTA reads all counts
+  int chunk = 2048 / K;
+  if ((T + chunk - 1) / chunk > most) chunk = (T + most - 1) / most;
+  h.chunk = (chunk + h.cta - 1) / h.cta * h.cta;
+  h.B = (T + h.chunk - 1) / h.chunk;
+  return h;
+}
+
 CombineArgs combine_args(const mcce_rows& r) {
   CombineArgs a{};
   a.tokens = (int64_t)r.n_layers * r.n_tokens, a.ld_token = ld_or(r.ld_token, r.d), a.ld_rows = ld_or(r.ld_rows, r.d);
@@ -459,41 +431,40 @@ cudaError_t launch_tokens(K kernel, const CombineArgs& a, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-// Many tokens: a few units per thread.  Few tokens: one.
-int spread(const CombineArgs& a, int u, int units_per_thread) {
-  return threads_per_token((a.d + u - 1) / u, a.tokens * 64 < 148 * 1024 ? 1 : units_per_thread);
-}
+// With fewer tokens than this the device is not full: one unit per thread and as many threads per token as that takes.
+bool few(const CombineArgs& a) { return a.tokens * 64 < 148 * 1024; }
 
-// Rows at once x units at once and threads per token, us measured (one launch between two events, 5 us of it not the kernel's;
-// 16384 tokens of 2048 bf16 columns unless noted).  Return, K = 8: 4 x 1 on 64 threads 99 (0.93 of the copy bandwidth), 8 x 1 104,
-// 2 x 2 133; K = 2, 4099 tokens of 4096: 1 x 4 22.8, 2 x 2 24.1, 2 x 1 25.2; K = 1 of 4096: 1 x 4 47.8, 2 x 2 55.7.  Gradient, K = 8:
-// 2 x 2 on 32 threads 195 (0.89), 4 x 1 193, 1 x 2 222; K = 6: 151 / 163 / 156.
+// KC rows at once x VPT units at once, us measured back to back on rotating buffers (16384 tokens of 2048 bf16 columns unless
+// noted).  Return, K = 8: 4 x 1 on 32 threads per token 96.6 (0.95 of the copy bandwidth), 8 x 1 104, 2 x 2 133; K = 2, 4099
+// tokens of 4096: 2 x 4 22.7 (0.68), 1 x 4 24.5, 4 x 1 25; K = 1 of 4096: 1 x 4 45 (0.91), 2 x 2 56; 256 tokens, K = 8: 4 x 1 on 256 threads
+// 4.2, 4 x 2 4.7.  Gradient, K = 8: 1 x 4 on 32 threads 188 (0.92), 4 x 1 191, 2 x 2 192; K = 1 of 4096: 1 x 4 66 (0.93); 256 tokens,
+// K = 8: 4 x 1 on 256 threads 6.3, 2 x 2 8.3.
 // Units narrower than 16 bytes (odd widths, unaligned rows) keep fewer bytes in flight per register: 8192 tokens, K = 8, of 1411
-// columns: return 4 x 4 82 (0.39), 4 x 2 93; gradient 4 x 1 142 (0.42), 2 x 4 152.  Sixteen-byte loads at the next boundary, shifted
+// bf16 columns: return 4 x 4 80 (0.40), 8 x 2 88; gradient 4 x 1 143 (0.42), 2 x 4 152.  Sixteen-byte loads at the next boundary, shifted
 // into place, were no faster (74 .. 80 and 166).
 template <typename T, typename Y, int U>
 cudaError_t run_combine(CombineArgs a, cudaStream_t st) {
-  if constexpr (U * sizeof(T) == 16) {
-    a.tpt = spread(a, U, a.K <= 2 ? 8 : 4);
-    if (a.K <= 2) return launch_tokens(combine_rows_kernel<T, Y, U, 1, 4>, a, st);
+  constexpr bool kWide = U * sizeof(T) == 16;
+  a.tpt = threads_per_token((a.d + U - 1) / U, few(a) ? 1 : kWide ? 8 : 32);
+  if constexpr (kWide) {
+    if (a.K == 1) return launch_tokens(combine_rows_kernel<T, Y, U, 1, 4>, a, st);
+    if (a.K == 2) return launch_tokens(combine_rows_kernel<T, Y, U, 2, 4>, a, st);
     return launch_tokens(combine_rows_kernel<T, Y, U, 4, sizeof(T) == 4 ? 2 : 1>, a, st);
   } else {
-    a.tpt = spread(a, U, 32);
-    if (a.K <= 2) return launch_tokens(combine_rows_kernel<T, Y, U, 1, 8>, a, st);
+    if (a.K <= 2) return launch_tokens(combine_rows_kernel<T, Y, U, 2, 4>, a, st);
     return launch_tokens(combine_rows_kernel<T, Y, U, 4, 4>, a, st);
   }
 }
 template <typename T, typename Y, int U>
 cudaError_t run_combine_grad(CombineArgs a, cudaStream_t st) {
-  if constexpr (U * sizeof(T) == 16) {
-    a.tpt = spread(a, U, 8);
-    if (a.K == 1) return launch_tokens(combine_rows_grad_kernel<T, Y, U, 1, 2>, a, st);
-    return launch_tokens(combine_rows_grad_kernel<T, Y, U, 2, 2>, a, st);
+  constexpr bool kWide = U * sizeof(T) == 16;
+  a.tpt = threads_per_token((a.d + U - 1) / U, few(a) ? 1 : kWide ? 8 : a.K <= 2 ? 32 : 16);
+  if constexpr (kWide) {
+    if (!few(a)) return launch_tokens(combine_rows_grad_kernel<T, Y, U, 1, 4>, a, st);
   } else {
-    a.tpt = spread(a, U, a.K <= 2 ? 32 : 16);
     if (a.K <= 2) return launch_tokens(combine_rows_grad_kernel<T, Y, U, 2, 4>, a, st);
-    return launch_tokens(combine_rows_grad_kernel<T, Y, U, 4, 1>, a, st);
   }
+  return launch_tokens(combine_rows_grad_kernel<T, Y, U, 4, 1>, a, st);
 }
 template <typename T, typename Y>
 cudaError_t run_combine_unit(const CombineArgs& a, int u, bool grad, cudaStream_t st) {
@@ -509,38 +480,26 @@ cudaError_t run_combine_types(const mcce_rows& r, const CombineArgs& a, int u, b
 }
 
 // A launch that may begin while the kernel before it ends; the kernel waits for that one itself.
-template <typename P>
-cudaError_t launch_after(void (*kernel)(P), dim3 grid, int threads, cudaStream_t st, const std::decay_t<P>& args) {
+template <typename... P>
+cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t st, const std::decay_t<P>&... args) {
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid, cfg.blockDim = dim3(threads), cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, args);
-}
-
-// Tokens per CTA of the single launch, 0: several launches.
-int fused_tokens(const SortArgs& s) {
-  if (s.P > 8192) return 0;
-  return s.K >= 4 ? 4 : s.K >= 2 ? 8 : 16;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 template <typename V>
-cudaError_t run_dispatch(const SortArgs& s, CopyArgs c, int L, cudaStream_t st) {
-  if (const int t = fused_tokens(s)) {
-    rows_dispatch_kernel<V><<<dim3((s.T + t - 1) / t, L), 256, 0, st>>>(s, c, t);
+cudaError_t run_dispatch(const SortArgs& s, const CopyArgs& c, int L, int t, cudaStream_t st) {
+  const dim3 grid((s.T + t - 1) / t, L);
+  if (s.B == 1) {
+    rows_dispatch_kernel<V><<<grid, 256, 0, st>>>(s, c, t);
     return cudaGetLastError();
   }
-  const dim3 grid(s.B, L);
-  rows_count_kernel<<<grid, 256, 0, st>>>(s);
-  cudaError_t err = cudaGetLastError();
-  if (err == cudaSuccess) err = launch_after(rows_rank_kernel, grid, kSortChunk, st, s);
-  if (err != cudaSuccess || !(c.x || c.scale_cols)) return err;
-  c.tpt = threads_per_token(c.units, sizeof(V) == 16 ? 2 : 16);
-  if (c.tpt > 128) c.tpt = 128;
-  const int64_t ctas = (c.tokens * c.tpt + 255) / 256;
-  if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
-  return launch_after(rows_copy_kernel<V>, dim3((unsigned)ctas), 256, st, c);
+  rows_count_kernel<<<dim3(s.B, L), 256, 0, st>>>(s);
+  const cudaError_t err = cudaGetLastError();
+  return err == cudaSuccess ? launch_after(rows_dispatch_kernel<V>, grid, 256, st, s, c, t) : err;
 }
 
 }  // namespace
@@ -550,8 +509,9 @@ using namespace mcce;
 
 extern "C" size_t mcce_dispatch_workspace_bytes(const mcce_rows* r) {
   if (!dispatch_ok(r)) return 0;
-  const size_t P = (size_t)r->n_tokens * r->top_k, B = (P + kSortChunk - 1) / kSortChunk;
-  return (size_t)r->n_layers * B * r->n_experts * 4;
+  if (r->n_tokens == 0) return 0;
+  const SortShape h = sort_shape(*r);
+  return h.B == 1 ? 0 : (size_t)r->n_layers * h.B * r->n_experts * 4;
 }
 
 extern "C" int mcce_dispatch(const mcce_rows* r, const int32_t* sel_idx, const void* x, const float* scales,
@@ -572,23 +532,24 @@ extern "C" int mcce_dispatch(const mcce_rows* r, const int32_t* sel_idx, const v
   const size_t need = mcce_dispatch_workspace_bytes(r);
   if (need && (!workspace || !aligned(workspace, 16))) return MCCE_EINVAL;
   if (workspace_bytes < need) return MCCE_ENOSPC;
+  const SortShape h = sort_shape(*r);
   SortArgs s;
-  s.T = r->n_tokens, s.K = r->top_k, s.E = r->n_experts, s.P = s.T * s.K, s.B = (s.P + kSortChunk - 1) / kSortChunk;
+  s.T = r->n_tokens, s.K = r->top_k, s.E = r->n_experts, s.P = s.T * s.K, s.chunk = h.chunk, s.B = h.B;
   s.sel = sel_idx, s.offsets = offsets, s.perm = perm, s.inv = inv, s.counts = (int32_t*)workspace;
   CopyArgs c{};
-  c.tokens = (int64_t)r->n_layers * r->n_tokens, c.T = s.T, c.K = s.K, c.P = s.P, c.scale_cols = r->scale_cols;
-  c.inv = inv, c.x = x, c.rows = rows, c.scales = scales, c.row_scales = row_scales;
+  c.K = s.K, c.scale_cols = r->scale_cols;
+  c.x = x, c.rows = rows, c.scales = scales, c.row_scales = row_scales;
   // rows are moved in units of 16 bytes or the largest power of two that they are aligned to
   int64_t ld_x = ld_or(r->ld_token, r->d) * e, ld_rows = ld_or(r->ld_rows, r->d) * e, row = x ? (int64_t)r->d * e : 0;
   int v = 16;
   while (v > 1 && (row % v || ld_x % v || ld_rows % v || !aligned(x, v) || !aligned(rows, v))) v /= 2;
   c.ld_x = ld_x / v, c.ld_rows = ld_rows / v, c.units = (int)(row / v);
   cudaError_t err;
-  if (v == 16) err = run_dispatch<uint4>(s, c, r->n_layers, st);
-  else if (v == 8) err = run_dispatch<uint2>(s, c, r->n_layers, st);
-  else if (v == 4) err = run_dispatch<uint32_t>(s, c, r->n_layers, st);
-  else if (v == 2) err = run_dispatch<uint16_t>(s, c, r->n_layers, st);
-  else err = run_dispatch<uint8_t>(s, c, r->n_layers, st);
+  if (v == 16) err = run_dispatch<uint4>(s, c, r->n_layers, h.cta, st);
+  else if (v == 8) err = run_dispatch<uint2>(s, c, r->n_layers, h.cta, st);
+  else if (v == 4) err = run_dispatch<uint32_t>(s, c, r->n_layers, h.cta, st);
+  else if (v == 2) err = run_dispatch<uint16_t>(s, c, r->n_layers, h.cta, st);
+  else err = run_dispatch<uint8_t>(s, c, r->n_layers, h.cta, st);
   return err == cudaSuccess ? MCCE_OK : MCCE_ECUDA;
 }
 

@@ -204,6 +204,17 @@ def test_norm_gradient_against_differences():
         assert abs(num - (dw.double() * vw).sum()) <= (NORM_U + 1e-8) * size
 
 
+@pytest.mark.parametrize("R,d", [(1, 64), (3, 2048), (4, 1411), (16, 128), (20, 7), (33, 40)])
+def test_norm_gradient_of_few_rows_into_an_unaligned_weight_gradient(R, d):
+    gn = gen(R)
+    h, g, w = normal(gn, R, d), normal(gn, R, d), 1 + 0.1 * normal(gn, d)
+    for shift in (0, 1):
+        dw = torch.full((d + 8,), 3.0, device="cuda")
+        out = mb.rmsnorm_backward(g, h, w, out=(torch.empty_like(h), dw[shift:d + shift]))
+        check_gradient(g, h, w, 1e-6, None, *out)
+        assert (dw[:shift] == 3).all() and (dw[d + shift:] == 3).all()
+
+
 def test_norm_gradient_strides_and_no_rows():
     gn, R, d = gen(3), 29, 200
     big = [normal(gn, R, d + 8 + 2 * i, dtype=BF16) for i in range(4)]
@@ -362,6 +373,17 @@ def test_combine_strides_and_empty():
     assert z.shape == (0, d)
     dz = mb.combine_backward(z, rows[:0], inv[:0], w[:0])
     assert dz[0].shape == (0, d) and dz[1].shape == (0, K)
+
+
+def test_combine_gradient_of_rows_apart():
+    """Rows further apart than their width: a fresh drows gets the same strides."""
+    g, T, K, d = gen(12), 40, 2, 56
+    inv, _ = positions(g, 1, T, K, 0.0)
+    base = normal(g, T * K, 64)
+    rows, dy, w = base[:, :d], normal(g, T, d), torch.rand(T, K, device="cuda", generator=g)
+    drows, dw = mb.combine_backward(dy, rows, inv[0], w)
+    want = mb.combine_backward(dy, rows.contiguous(), inv[0], w)
+    assert torch.equal(drows, want[0]) and torch.equal(dw, want[1])
 
 
 def test_combine_gradient_against_differences():
@@ -566,3 +588,51 @@ def test_binding_refuses_what_does_not_fit():
         mb.combine(torch.zeros(8, 16, device="cuda"), sel, out_dtype=BF16)
     with bad:
         mb.combine_backward(x[:3], torch.zeros(8, 16, device="cuda"), sel)
+
+
+def test_chained_step_with_norms_equals_the_composition():
+    """mcce_set_norm: layer l routes and runs its experts on the norm of the residual stream, which itself stays as it is.  Against
+    single-layer engines joined by the operators (fp32-pipe experts, so every step is the same kernels: bit for bit), with
+    one layer and several, and off again."""
+    from paper_2412_00099_b200 import synth
+    import helpers as H
+    for wl in (synth.TINY.with_(L=3, S=6), synth.TINY.with_(L=1, S=5),
+               synth.QWEN.with_(L=3, S=20, E=12, K=4, C=6, d=264, I=256, n_shared=1)):
+        Wr, W = wl.router(), H.weights_for(wl)
+        Wd = {k: (None if v is None else H.to_dev(v)) for k, v in W.items()}
+        full = mb.engine_for(wl, ffn_impl=mb.FFN_SIMT)
+        full.set_router(H.to_dev(Wr))
+        full.set_experts(**Wd)
+        plain = mb.engine_for(wl, ffn_impl=mb.FFN_SIMT)
+        plain.set_router(H.to_dev(Wr))
+        plain.set_experts(**Wd)
+        singles = []
+        for l in range(wl.L):
+            e = mb.engine_for(wl.with_(L=1), ffn_impl=mb.FFN_SIMT)
+            e.set_router(H.to_dev(Wr[l:l + 1]))
+            e.set_experts(**{k: (None if v is None else v[l:l + 1].contiguous()) for k, v in Wd.items()})
+            singles.append(e)
+        nw = 1 + 0.3 * normal(gen(wl.L), wl.L, wl.d)
+        full.set_norm(nw, 1e-5)
+        for x0 in [H.to_dev(x)[0] for x in wl.with_(L=1).hidden_trace(4)]:
+            keep = x0.clone()
+            x_c, sel_c = full.decode_step_chained(x0, want_sel=True)
+            assert torch.equal(x0, keep)
+            x = x0
+            for l, e in enumerate(singles):
+                n = mb.rmsnorm(x, nw[l], 1e-5).out
+                sel, w = e.route_step(hidden=n[None, None])
+                y = e.moe_forward(n[None], sel[0], w[0])[0]
+                assert torch.equal(sel[0, 0], sel_c[l])
+                x = mb.rmsnorm(x, nw[l], 1e-5, add=y, want_out=False).sum
+            assert torch.equal(x, x_c)
+        full.set_norm(None)                          # off: the step of an engine that never had one
+        full.reset()
+        x0 = H.to_dev(next(iter(wl.with_(L=1).hidden_trace(1))))[0]
+        assert torch.equal(full.decode_step_chained(x0), plain.decode_step_chained(x0))
+        with pytest.raises(mb.McceError):
+            full.set_norm(nw, -1.0)
+        with pytest.raises(AssertionError):
+            full.set_norm(nw[:, :8])
+        for e in [full, plain, *singles]:
+            e.close()

@@ -140,6 +140,10 @@ def test_combine_refusals(lib):
     assert lib.mcce_combine_backward(None, P[0], P[1], P[2], P[3], P[4], P[5], None) == EINVAL
 
 
+def test_set_norm_needs_a_context(lib):
+    assert lib.mcce_set_norm(None, P[0], 1e-6) == EINVAL
+
+
 def test_binding_refuses_cpu_tensors():
     import torch
     with pytest.raises(mb.McceError, match="no CPU path"):
