@@ -33,29 +33,21 @@ __global__ void __launch_bounds__(256) rows_count_kernel(const __grid_constant__
 }
 
 // ---- moving rows ------------------------------------------------------------------------------------------------
-// tpt threads per token (a power of two, 16 .. 256); a token's pairs are looked at by its first top_k threads and
-// handed round the warp.
+// One warp per token, or 2, 4 or 8 that share its columns: a warp takes blocks of 32 * V units, every wpt-th block, so that the V
+// loads of a lane lie at fixed distances and only the last block of a row needs a look at its end.
 struct Token {
   int64_t t, first;   // token over all layers; first sorted row of its layer
-  int lane0;          // first lane of the token in this warp
-  int u0;             // this thread's index in the token
+  int lane, part;     // this warp's part of the token
   bool there;
-  __device__ __forceinline__ Token(int tpt, int64_t tokens, int T, int P) {
-    const int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    t = at / tpt;
-    u0 = (int)at & (tpt - 1);
-    lane0 = tpt < 32 ? (int)(threadIdx.x & 31) & ~(tpt - 1) : 0;
+  __device__ __forceinline__ Token(int wpt, int64_t tokens, int T, int P) {
+    const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    lane = threadIdx.x & 31;
+    t = w / wpt;
+    part = (int)w & (wpt - 1);
     there = t < tokens;
     first = there ? t / T * P : 0;
   }
 };
-// The position of pair k of a token, -1: none.  `mine` is the position of this lane's pair.
-__device__ __forceinline__ int position(const Token& tk, int mine, int k) { return __shfl_sync(kFull, mine, tk.lane0 + k); }
-__device__ __forceinline__ int my_position(const Token& tk, const int32_t* inv, int K, int P) {
-  const int k = (int)(threadIdx.x & 31) - tk.lane0;
-  const int pos = tk.there && k < K ? inv[tk.t * K + k] : -1;
-  return (unsigned)pos < (unsigned)P ? pos : -1;
-}
 
 struct CopyArgs {
   int64_t ld_x, ld_rows; // in units
@@ -66,26 +58,42 @@ struct CopyArgs {
   float* row_scales;
 };
 
-// The row of a token to the positions of its pairs, by `threads` threads of which this is number u0.  V units of the row are
-// read, all in flight, and written once for every pair: a token's row is read once.
+// The row of a token to the positions of its pairs, by `parts` warps of which this is number `part`: V units of the row are read, all
+// in flight, and written once for every pair, so a token's row is read once.  The warps of a row take turns every 32 units of 16
+// bytes (24 x 256 tokens x 4 of 4096 bytes: 25.3 us, with blocks of 128 units 29.6), or blocks of 256 narrower ones, whose loads and
+// stores lie at fixed distances then and need no look at the row's end (8192 x 8 of 1411 bf16: 57 us against 73).
 // position_of(k): of pair k, -1: none.
 template <typename V_, typename F>
-__device__ __forceinline__ void move_row(const CopyArgs& a, int64_t t, int64_t first, int u0, int threads, F position_of) {
-  constexpr int V = sizeof(V_) == 16 ? 4 : 8;
+__device__ __forceinline__ void move_row(const CopyArgs& a, int64_t t, int64_t first, int lane, int part, int parts, F position_of) {
+  constexpr bool kWide = sizeof(V_) == 16;
+  constexpr int V = kWide ? 4 : 8;
   const V_* x = (const V_*)a.x + t * a.ld_x;
   V_* rows = (V_*)a.rows + first * a.ld_rows;
-  for (int b = u0; b - u0 < a.units; b += threads * V) {
+  const int step = kWide ? parts * 32 : 32, u0 = kWide ? part * 32 + lane : lane;
+  for (int b = kWide ? 0 : part * 32 * V; b < a.units; b += parts * 32 * V) {
     V_ p[V];
+    if (!kWide && b + 32 * V <= a.units) {
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-      if (b + v * threads < a.units) p[v] = __ldg(x + b + v * threads);
-    for (int k = 0; k < a.K; ++k) {
-      const int pos = position_of(k);
-      if (pos < 0) continue;
-      V_* to = rows + pos * a.ld_rows + b;
+      for (int v = 0; v < V; ++v) p[v] = __ldg(x + b + lane + v * 32);
+      for (int k = 0; k < a.K; ++k) {
+        const int pos = position_of(k);
+        if (pos < 0) continue;
+        V_* to = rows + pos * a.ld_rows + b + lane;
+#pragma unroll
+        for (int v = 0; v < V; ++v) to[v * 32] = p[v];
+      }
+    } else {
 #pragma unroll
       for (int v = 0; v < V; ++v)
-        if (b + v * threads < a.units) to[v * threads] = p[v];
+        if (b + u0 + v * step < a.units) p[v] = __ldg(x + b + u0 + v * step);
+      for (int k = 0; k < a.K; ++k) {
+        const int pos = position_of(k);
+        if (pos < 0) continue;
+        V_* to = rows + pos * a.ld_rows + b + u0;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          if (b + u0 + v * step < a.units) to[v * step] = p[v];
+      }
     }
   }
 }
@@ -165,16 +173,15 @@ __global__ void __launch_bounds__(256) rows_dispatch_kernel(const __grid_constan
     if (s.perm && pos >= 0) s.perm[(size_t)l * s.P + pos] = q0 + tid;
   }
   __syncthreads();
-  // the warps of a token: one each for eight tokens or more, else the eight warps shared out
+  // one warp per token for eight tokens or more, else the eight warps shared out
   const int64_t first = (int64_t)l * s.P;
-  const int per_token = n_tok >= 8 ? 1 : n_tok >= 4 ? 2 : n_tok >= 2 ? 4 : 8, slots = 8 / per_token;
-  const int u0 = (warp & (per_token - 1)) * 32 + lane;
-  for (int t = warp / per_token; t < n_tok; t += slots) {
+  const int parts = n_tok >= 8 ? 1 : n_tok >= 4 ? 2 : n_tok >= 2 ? 4 : 8, part = warp & (parts - 1);
+  for (int t = warp / parts; t < n_tok; t += 8 / parts) {
     const int64_t token = (int64_t)l * s.T + t0 + t;
-    if (a.x) move_row<V>(a, token, first, u0, per_token * 32, [&](int k) { return place[t * s.K + k]; });
-    for (int k = 0; a.scale_cols && k < s.K; ++k) {
+    if (a.x) move_row<V>(a, token, first, lane, part, parts, [&](int k) { return place[t * s.K + k]; });
+    for (int k = part; a.scale_cols && k < s.K; k += parts) {
       const int pos = place[t * s.K + k];
-      for (int i = u0; pos >= 0 && i < a.scale_cols; i += per_token * 32)
+      for (int i = lane; pos >= 0 && i < a.scale_cols; i += 32)
         a.row_scales[(first + pos) * a.scale_cols + i] = a.scales[token * a.scale_cols + i];
     }
   }
@@ -182,7 +189,7 @@ __global__ void __launch_bounds__(256) rows_dispatch_kernel(const __grid_constan
 
 struct CombineArgs {
   int64_t tokens, ld_token, ld_rows;
-  int T, K, P, d, tpt;
+  int T, K, P, d, wpt;
   const int32_t* inv;
   const float* w;
   const void *rows, *add;
@@ -192,18 +199,48 @@ struct CombineArgs {
   float* dw;
 };
 
-// y of a token: U columns at a time, VPT such units per thread and KC rows at once, so that KC * VPT loads are in flight.
+// The pairs of a token in the lanes of its warp: position (-1: none) and weight.
+struct Pairs {
+  int pos;
+  float w;
+  __device__ __forceinline__ Pairs(const CombineArgs& a, const Token& tk) : pos(-1), w(1.f) {
+    if (tk.there && tk.lane < a.K) {
+      const int p = a.inv[tk.t * a.K + tk.lane];
+      if ((unsigned)p < (unsigned)a.P) {
+        pos = p;
+        if (a.w) w = a.w[tk.t * a.K + tk.lane];
+      }
+    }
+  }
+  // of pair k, the same in all lanes
+  __device__ __forceinline__ int position(int k, int K) const {
+    const int p = __shfl_sync(kFull, pos, k & 31);
+    return k < K ? p : -1;
+  }
+  __device__ __forceinline__ float weight(int k) const { return __shfl_sync(kFull, w, k & 31); }
+};
+
+template <int U>
+__device__ __forceinline__ void add_scaled(float2 (&s)[(U + 1) / 2], const float2 (&e)[(U + 1) / 2], float w) {
+  if constexpr (U == 1) {
+    s[0].x = fmaf(e[0].x, w, s[0].x);
+  } else {
+#pragma unroll
+    for (int j = 0; j < U / 2; ++j) s[j] = fma2(e[j], both(w), s[j]);
+  }
+}
+
+// y of a token: U columns (16 bytes of a row) at a time, VPT such units per lane and KC rows at once, so that KC * VPT loads are in flight.
 template <typename T, typename Y, int U, int KC, int VPT>
 __global__ void __launch_bounds__(256) combine_rows_kernel(const __grid_constant__ CombineArgs a) {
-  constexpr int N = (U + 1) / 2;
-  const Token tk(a.tpt, a.tokens, a.T, a.P);
-  const int mine = my_position(tk, a.inv, a.K, a.P);
-  const float my_w = mine >= 0 && a.w ? a.w[tk.t * a.K + (int)(threadIdx.x & 31) - tk.lane0] : 1.f;
+  constexpr int N = U / 2;
+  const Token tk(a.wpt, a.tokens, a.T, a.P);
+  const Pairs pairs(a, tk);
   const T* rows = (const T*)a.rows + tk.first * a.ld_rows;
   const int64_t at = tk.t * a.ld_token;
-  const int d = tk.there ? a.d : 0, step = a.tpt * U;
+  const int d = tk.there ? a.d : 0, step = a.wpt * 32 * U;
   for (int b = 0; b < a.d; b += step * VPT) {
-    const int c0 = b + tk.u0 * U;
+    const int c0 = b + (tk.part * 32 + tk.lane) * U;
     float2 s[VPT][N];
 #pragma unroll
     for (int v = 0; v < VPT; ++v)
@@ -214,8 +251,8 @@ __global__ void __launch_bounds__(256) combine_rows_kernel(const __grid_constant
       float w[KC];
 #pragma unroll
       for (int k = 0; k < KC; ++k) {
-        const int pos = k0 + k < a.K ? position(tk, mine, k0 + k) : -1;
-        w[k] = __shfl_sync(kFull, my_w, tk.lane0 + ((k0 + k) & 15));
+        const int pos = k0 + k < a.K ? __shfl_sync(kFull, pairs.pos, k0 + k) : -1;
+        w[k] = __shfl_sync(kFull, pairs.w, (k0 + k) & 15);
         const T* row = rows + pos * a.ld_rows + c0;
 #pragma unroll
         for (int v = 0; v < VPT; ++v) {
@@ -251,11 +288,88 @@ __global__ void __launch_bounds__(256) combine_rows_kernel(const __grid_constant
   }
 }
 
-// Sums of acc[k] over `lanes` lanes, k < KC.  The number of values is halved while the lanes that share one double, so KC sums
-// cost little more than one; lane l holds that of k = l / (lanes / KC) afterwards.
+// The same for narrower units (odd widths, unaligned rows), where instructions are what bounds it: blocks that lie inside the row and
+// whose pairs all have rows run without a predicate, at fixed distances.
+template <typename T, typename Y, int U, int KC, int VPT>
+__global__ void __launch_bounds__(256) combine_narrow_kernel(const __grid_constant__ CombineArgs a) {
+  constexpr int N = (U + 1) / 2, kBlock = 32 * U * VPT;
+  const Token tk(a.wpt, a.tokens, a.T, a.P);
+  const Pairs pairs(a, tk);
+  const T* rows = (const T*)a.rows + tk.first * a.ld_rows + tk.lane * U;
+  const int64_t at = tk.t * a.ld_token + tk.lane * U;
+  const int d = tk.there ? a.d : 0;
+  auto block = [&](int b, auto whole) {   // columns b .. b + kBlock, all of them inside the row or not
+    constexpr bool kWhole = decltype(whole)::value;
+    const int left = d - b - tk.lane * U;
+    float2 s[VPT][N];
+#pragma unroll
+    for (int v = 0; v < VPT; ++v)
+#pragma unroll
+      for (int j = 0; j < N; ++j) s[v][j] = both(0.f);
+    for (int k0 = 0; k0 < a.K; k0 += KC) {
+      int pos[KC], least = 0;
+      float w[KC];
+#pragma unroll
+      for (int k = 0; k < KC; ++k) {
+        pos[k] = pairs.position(k0 + k, a.K);
+        w[k] = pairs.weight(k0 + k);
+        least = min(least, pos[k]);
+      }
+      // (branches between the loads would keep them from being issued together: either none, or predicates)
+      auto rows_of = [&](auto all) {
+        constexpr bool kAll = decltype(all)::value;
+        Pack<T, U> p[KC][VPT];
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+          const T* row = rows + pos[k] * a.ld_rows + b;
+#pragma unroll
+          for (int v = 0; v < VPT; ++v) {
+            if (!kAll) p[k][v].zero();
+            if (kAll || (pos[k] >= 0 && v * 32 * U < left)) p[k][v].load_const(row + v * 32 * U);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < KC; ++k)
+#pragma unroll
+          for (int v = 0; v < VPT; ++v) {
+            float2 e[N];
+            p[k][v].get(e);
+            add_scaled<U>(s[v], e, w[k]);
+          }
+      };
+      if constexpr (kWhole) {
+        if (least == 0) rows_of(std::true_type{});
+        else rows_of(std::false_type{});
+      } else {
+        rows_of(std::false_type{});
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < VPT; ++v) {
+      if (!kWhole && v * 32 * U >= left) continue;
+      Pack<Y, U> y;
+      if (a.add) {
+        y.load((const Y*)a.add + at + b + v * 32 * U);
+        float2 e[N];
+        y.get(e);
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[v][j] = add2(s[v][j], e[j]);
+      }
+      y.set(s[v]);
+      y.store((Y*)a.y + at + b + v * 32 * U);
+    }
+  };
+  for (int b = tk.part * kBlock; b < a.d; b += a.wpt * kBlock) {
+    if (b + kBlock <= d) block(b, std::true_type{});
+    else block(b, std::false_type{});
+  }
+}
+
+// Sums of acc[k] over a warp, k < KC.  The number of values is halved while the lanes that share one double, so KC sums
+// cost little more than one; lane l holds that of k = l / (32 / KC) afterwards.
 template <int KC>
-__device__ __forceinline__ float sum_of_all(float (&acc)[KC], int lanes) {
-  int o = lanes >> 1;
+__device__ __forceinline__ float sum_of_all(float (&acc)[KC]) {
+  int o = 16;
   const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int n = KC / 2; n > 0; n >>= 1, o >>= 1) {
@@ -273,77 +387,87 @@ __device__ __forceinline__ float sum_of_all(float (&acc)[KC], int lanes) {
 // drows and dw of a token: a unit of a row is read, multiplied into the pair's sum, and replaced by w dy.  KC rows at once.
 template <typename T, typename Y, int U, int KC, int VPT>
 __global__ void __launch_bounds__(256) combine_rows_grad_kernel(const __grid_constant__ CombineArgs a) {
-  constexpr int N = (U + 1) / 2;
+  constexpr int N = (U + 1) / 2, kBlock = 32 * U * VPT;
   __shared__ float parts[8][KC];
-  const Token tk(a.tpt, a.tokens, a.T, a.P);
-  const int mine = my_position(tk, a.inv, a.K, a.P);
-  const float my_w = mine >= 0 && a.w ? a.w[tk.t * a.K + (int)(threadIdx.x & 31) - tk.lane0] : 1.f;
-  const T* rows = (const T*)a.rows;
-  T* drows = (T*)a.drows;
-  const Y* dy = (const Y*)a.dy + tk.t * a.ld_token;
-  const int d = tk.there ? a.d : 0, step = a.tpt * U;
+  const Token tk(a.wpt, a.tokens, a.T, a.P);
+  const Pairs pairs(a, tk);
+  const Y* dy = (const Y*)a.dy + tk.t * a.ld_token + tk.lane * U;
+  const int d = tk.there ? a.d : 0;
   for (int k0 = 0; k0 < a.K; k0 += KC) {
-    int64_t at[KC];   // first element of the pair's row, -1: no row
+    int64_t at[KC];   // this lane's first element of the pair's row, -1: no row
     float w[KC], acc[KC];
 #pragma unroll
     for (int k = 0; k < KC; ++k) {
-      const int pos = k0 + k < a.K ? position(tk, mine, k0 + k) : -1;
-      w[k] = __shfl_sync(kFull, my_w, tk.lane0 + ((k0 + k) & 15));
-      at[k] = pos >= 0 ? (tk.first + pos) * a.ld_rows : -1;
+      const int pos = pairs.position(k0 + k, a.K);
+      w[k] = pairs.weight(k0 + k);
+      at[k] = pos >= 0 ? (tk.first + pos) * a.ld_rows + tk.lane * U : -1;
       acc[k] = 0.f;
     }
-    for (int c = tk.u0 * U; c < d; c += step * VPT) {
+    bool all_there = true;
+#pragma unroll
+    for (int k = 0; k < KC; ++k) all_there &= at[k] >= 0;
+    auto block = [&](int b, auto all) {   // all: every pair has a row and all columns of the block lie in it
+      constexpr bool kAll = decltype(all)::value;
+      const int left = d - b - tk.lane * U;
       Pack<T, U> p[KC][VPT];
       Pack<Y, U> q[VPT];
 #pragma unroll
       for (int v = 0; v < VPT; ++v)
-        if (c + v * step < d) q[v].load_const(dy + c + v * step);
+        if (kAll || v * 32 * U < left) q[v].load_const(dy + b + v * 32 * U);
       if (a.dw) {
 #pragma unroll
-        for (int k = 0; k < KC; ++k)
+        for (int k = 0; k < KC; ++k) {
+          const T* row = (const T*)a.rows + at[k] + b;
 #pragma unroll
           for (int v = 0; v < VPT; ++v)
-            if (at[k] >= 0 && c + v * step < d) p[k][v].load(rows + at[k] + c + v * step);
-      }
-#pragma unroll
-      for (int v = 0; v < VPT; ++v) {
-        if (c + v * step >= d) continue;
-        float2 g[N];
-        q[v].get(g);
-#pragma unroll
-        for (int k = 0; k < KC; ++k) {
-          if (at[k] < 0) continue;
-          float2 e[N];
-          if (a.dw) {
-            p[k][v].get(e);
-            float2 s = both(0.f);
-#pragma unroll
-            for (int j = 0; j < N; ++j) s = fma2(e[j], g[j], s);
-            acc[k] += s.x + s.y;
-          }
-#pragma unroll
-          for (int j = 0; j < N; ++j) e[j] = mul2(g[j], both(w[k]));
-          p[k][v].set(e);
-          p[k][v].store(drows + at[k] + c + v * step);
+            if (kAll || (at[k] >= 0 && v * 32 * U < left)) p[k][v].load(row + v * 32 * U);
         }
       }
+#pragma unroll
+      for (int k = 0; k < KC; ++k) {
+        T* row = (T*)a.drows + at[k] + b;
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) {
+          if (!kAll && (at[k] < 0 || v * 32 * U >= left)) continue;
+          float2 g[N], e[N];
+          q[v].get(g);
+          if (a.dw) {
+            p[k][v].get(e);
+            if constexpr (U == 1) {
+              acc[k] = fmaf(e[0].x, g[0].x, acc[k]);
+            } else {
+              float2 s = both(0.f);
+#pragma unroll
+              for (int j = 0; j < N; ++j) s = fma2(e[j], g[j], s);
+              acc[k] += s.x + s.y;
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < N; ++j) e[j] = U == 1 ? make_float2(g[j].x * w[k], 0.f) : mul2(g[j], both(w[k]));
+          p[k][v].set(e);
+          p[k][v].store(row + v * 32 * U);
+        }
+      }
+    };
+    for (int b = tk.part * kBlock; b < d; b += a.wpt * kBlock) {
+      // (a look at the row's end costs little beside the columns of a 16-byte unit)
+      if (U * sizeof(T) < 16 && all_there && b + kBlock <= d) block(b, std::true_type{});
+      else block(b, std::false_type{});
     }
     if (!a.dw) continue;
-    const int lane = threadIdx.x & 31, lanes = min(a.tpt, 32);
-    const float s = sum_of_all(acc, lanes);
-    const int k = (lane & (lanes - 1)) / (lanes / KC);
-    const bool speaks = (lane & (lanes / KC - 1)) == 0;
-    if (a.tpt <= 32) {
-      if (speaks && tk.there && k0 + k < a.K) a.dw[tk.t * a.K + k0 + k] = s;
+    const float s = sum_of_all(acc);
+    const int k = tk.lane / (32 / KC);
+    const bool speaks = tk.lane % (32 / KC) == 0 && tk.there && k0 + k < a.K;
+    if (a.wpt == 1) {
+      if (speaks) a.dw[tk.t * a.K + k0 + k] = s;
     } else {
       __syncthreads();   // the last chunk's parts have been read
       if (speaks) parts[threadIdx.x >> 5][k] = s;
       __syncthreads();
-      if (tk.there && tk.u0 < KC && k0 + tk.u0 < a.K) {
-        const int warps = a.tpt >> 5, w0 = threadIdx.x >> 5;
+      if (speaks && tk.part == 0) {
         float v = 0.f;
-        for (int i = 0; i < warps; ++i) v += parts[w0 + i][tk.u0];
-        a.dw[tk.t * a.K + k0 + tk.u0] = v;
+        for (int i = 0; i < a.wpt; ++i) v += parts[(threadIdx.x >> 5) + i][k];
+        a.dw[tk.t * a.K + k0 + k] = v;
       }
     }
   }
@@ -387,7 +511,7 @@ int64_t ld_or(int64_t ld, int d) { return ld ? ld : d; }
 struct SortShape {
   int cta, chunk, B;
 };
-// A CTA moves up to 160 KB: 16384 tokens x 8 of 2048 bytes with scales, us, 4 / 8 tokens: 63.6 / 59; of 4096 bytes 2 / 4 / 8 tokens:
+// A CTA moves up to 150 KB: 16384 tokens x 8 of 2048 bytes with scales, us, 4 / 8 tokens: 63.6 / 59; of 4096 bytes 2 / 4 / 8 tokens:
 // 106 / 109 / 111; 24 x 256 tokens x 4 of 4096 bytes 27 / 25 / 27.  Chunks of 2048 pairs: between 512 and 4096 the time changes by
 // 1 %.  A layer is one chunk -- one launch, every CTA counts the whole layer -- while that is little work: 24 x 256 tokens x 4
 // 25.0 against 27.9 with two launches, 4096 tokens x 2 of 8192 bytes 32.7 against 22.8.
@@ -396,7 +520,7 @@ SortShape sort_shape(const mcce_rows& r) {
   const int64_t moved = (int64_t)(K + 1) * r.d * (r.dtype == MCCE_F32 ? 4 : r.dtype == MCCE_BF16 ? 2 : 1);
   SortShape h;
   h.cta = 1;
-  while (h.cta * 2 * K <= kCtaPairs && h.cta * 2 * moved <= 160 * 1024) h.cta *= 2;
+  while (h.cta * 2 * K <= kCtaPairs && h.cta * 2 * moved <= 150 * 1024) h.cta *= 2;
   const int64_t pairs = (int64_t)T * K, ctas = (int64_t)r.n_layers * ((T + h.cta - 1) / h.cta);
   if (pairs <= 2048 || (pairs <= 8192 && ctas * pairs <= (2 << 20))) {
     h.chunk = T, h.B = 1;
@@ -417,54 +541,56 @@ CombineArgs combine_args(const mcce_rows& r) {
   return a;
 }
 
-// Threads per token: a power of two that covers the row's units `per_thread` at a time, within 16 .. 256.
-int threads_per_token(int units, int per_thread) {
-  int t = 16;
-  while (t < 256 && t * per_thread < units) t *= 2;
-  return t;
+// Warps per token: a power of two that covers the row's units `per_lane` at a time, at most 8.
+int warps_per_token(int units, int per_lane) {
+  int w = 1;
+  while (w < 8 && w * 32 * per_lane < units) w *= 2;
+  return w;
 }
 template <typename K>
 cudaError_t launch_tokens(K kernel, const CombineArgs& a, cudaStream_t st) {
-  const int64_t grid = (a.tokens * a.tpt + 255) / 256;
+  const int64_t grid = (a.tokens * a.wpt + 7) / 8;
   if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
   kernel<<<(unsigned)grid, 256, 0, st>>>(a);
   return cudaGetLastError();
 }
 
-// With fewer tokens than this the device is not full: one unit per thread and as many threads per token as that takes.
+// With fewer tokens than this the device is not full: one unit per lane and as many warps per token as that takes.
 bool few(const CombineArgs& a) { return a.tokens * 64 < 148 * 1024; }
 
 // KC rows at once x VPT units at once, us measured back to back on rotating buffers (16384 tokens of 2048 bf16 columns unless
-// noted).  Return, K = 8: 4 x 1 on 32 threads per token 96.6 (0.95 of the copy bandwidth), 8 x 1 104, 2 x 2 133; K = 2, 4099
-// tokens of 4096: 2 x 4 22.7 (0.68), 1 x 4 24.5, 4 x 1 25; K = 1 of 4096: 1 x 4 45 (0.91), 2 x 2 56; 256 tokens, K = 8: 4 x 1 on 256 threads
-// 4.2, 4 x 2 4.7.  Gradient, K = 8: 1 x 4 on 32 threads 188 (0.92), 4 x 1 191, 2 x 2 192; K = 1 of 4096: 1 x 4 66 (0.93); 256 tokens,
-// K = 8: 4 x 1 on 256 threads 6.3, 2 x 2 8.3.
-// Units narrower than 16 bytes (odd widths, unaligned rows) keep fewer bytes in flight per register: 8192 tokens, K = 8, of 1411
-// bf16 columns: return 4 x 4 80 (0.40), 8 x 2 88; gradient 4 x 1 143 (0.42), 2 x 4 152.  Sixteen-byte loads at the next boundary, shifted
-// into place, were no faster (74 .. 80 and 166).
+// noted).  Return, K = 8: 4 x 1 with 2 warps per token 96.4 (0.96 of the copy bandwidth), 8 x 1 104, 2 x 2 133; K = 6 with add: 4 x 1 92.4, 3 x
+// 1 92.3, 1 x 2 94.1; K = 2, 4099 tokens of 4096: 1 x 2 22.1 (0.69), 2 x 2 22.7, 4 x 1 24.8; K = 1 of 4096: 1 x 4 45.2 (0.91); 256
+// tokens, K = 8: 4 x 1 with 8 warps 4.2, 4 x 2 4.7.  Gradient, K = 8: 1 x 4 with 2 warps 179 (0.97), 2 x 2 181, 4 x 1 191; K = 1 of 4096: 1 x 4
+// 63.6 (0.97); 256 tokens, K = 8: 4 x 1 with 8 warps 6.3, 2 x 2 8.3.
+// Units of one bf16: 8192 tokens of 1411, K = 8, return 4 x 8 with 2 warps 53 (0.60), 4 x 4 57, 1 x 8 62; of 4097, K = 2: 2 x 8 50 (0.62), 1 x 8 53;
+// gradient 4 x 4 109 (0.55), 2 x 4 117; K = 2: 2 x 4 88 (0.58).  Sixteen-byte loads at the next boundary, shifted into place: 74 and 166.
 template <typename T, typename Y, int U>
 cudaError_t run_combine(CombineArgs a, cudaStream_t st) {
-  constexpr bool kWide = U * sizeof(T) == 16;
-  a.tpt = threads_per_token((a.d + U - 1) / U, few(a) ? 1 : kWide ? 8 : 32);
-  if constexpr (kWide) {
+  const int units = (a.d + U - 1) / U;
+  if constexpr (U * sizeof(T) == 16) {
+    a.wpt = warps_per_token(units, few(a) ? 1 : 4);
     if (a.K == 1) return launch_tokens(combine_rows_kernel<T, Y, U, 1, 4>, a, st);
-    if (a.K == 2) return launch_tokens(combine_rows_kernel<T, Y, U, 2, 4>, a, st);
+    if (a.K == 2) return launch_tokens(combine_rows_kernel<T, Y, U, 1, 2>, a, st);
     return launch_tokens(combine_rows_kernel<T, Y, U, 4, sizeof(T) == 4 ? 2 : 1>, a, st);
   } else {
-    if (a.K <= 2) return launch_tokens(combine_rows_kernel<T, Y, U, 2, 4>, a, st);
-    return launch_tokens(combine_rows_kernel<T, Y, U, 4, 4>, a, st);
+    a.wpt = warps_per_token(units, few(a) ? 1 : 36);
+    if (a.K <= 2) return launch_tokens(combine_narrow_kernel<T, Y, U, 2, 8 / U>, a, st);
+    return launch_tokens(combine_narrow_kernel<T, Y, U, 4, sizeof(T) == 4 ? 4 : 8 / U>, a, st);
   }
 }
 template <typename T, typename Y, int U>
 cudaError_t run_combine_grad(CombineArgs a, cudaStream_t st) {
-  constexpr bool kWide = U * sizeof(T) == 16;
-  a.tpt = threads_per_token((a.d + U - 1) / U, few(a) ? 1 : kWide ? 8 : a.K <= 2 ? 32 : 16);
-  if constexpr (kWide) {
-    if (!few(a)) return launch_tokens(combine_rows_grad_kernel<T, Y, U, 1, 4>, a, st);
+  const int units = (a.d + U - 1) / U;
+  if constexpr (U * sizeof(T) == 16) {
+    if (few(a)) return a.wpt = warps_per_token(units, 1), launch_tokens(combine_rows_grad_kernel<T, Y, U, 4, 1>, a, st);
+    a.wpt = units > 128 ? 2 : 1;
+    return launch_tokens(combine_rows_grad_kernel<T, Y, U, 1, 4>, a, st);
   } else {
+    a.wpt = warps_per_token(units, few(a) ? 1 : 36);
     if (a.K <= 2) return launch_tokens(combine_rows_grad_kernel<T, Y, U, 2, 4>, a, st);
+    return launch_tokens(combine_rows_grad_kernel<T, Y, U, 4, 4 / U>, a, st);
   }
-  return launch_tokens(combine_rows_grad_kernel<T, Y, U, 4, 1>, a, st);
 }
 template <typename T, typename Y>
 cudaError_t run_combine_unit(const CombineArgs& a, int u, bool grad, cudaStream_t st) {
