@@ -454,27 +454,11 @@ __global__ void __launch_bounds__(512) rmsnorm_grad_kernel(const __grid_constant
   const int tensor_bytes = VPT * (int)blockDim.x * 16, stage_bytes = (a.dsum ? 3 : 2) * tensor_bytes;
   uint8_t* ring = smem + threadIdx.x * 16;
 
-  const W* weight = (const W*)a.weight;
-  float2 w[VPT][U / 2], dw[VPT][U / 2];
-#pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    Pack<W, U> p;
-    p.zero();
-    if (in[i]) {
-      if constexpr (RAGGED) p.load_part(weight + head + c0 + i * step, 0, U);   // once per CTA
-      else p.load_const(weight + c0 + i * step);
-    }
-    p.get(w[i]);
-#pragma unroll
-    for (int j = 0; j < U / 2; ++j) dw[i][j] = both(0.f);
-  }
   // single elements of a ragged row, of its first U threads: one before the units, one behind them
   const int tail = head + whole + th.t;
   const bool edges = RAGGED && th.t < U;
   const bool there[2] = {RAGGED && th.t < head, RAGGED && tail < a.d};
   const int col[2] = {th.t, tail};
-  const float we[2] = {there[0] ? wide(weight[col[0]]) : 0.f, there[1] ? wide(weight[col[1]]) : 0.f};
-  float dwe[2] = {0.f, 0.f};
   struct Edge {
     T h[2], g[2], s[2];   // as loaded: converting would wait for them
   } edge{}, next{};
@@ -512,6 +496,22 @@ __global__ void __launch_bounds__(512) rmsnorm_grad_kernel(const __grid_constant
     copies_commit();
   }
   if (edges) fetch_edge(first);
+  const W* weight = (const W*)a.weight;
+  float2 w[VPT][U / 2], dw[VPT][U / 2];
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    Pack<W, U> p;
+    p.zero();
+    if (in[i]) {
+      if constexpr (RAGGED) p.load_part(weight + head + c0 + i * step, 0, U);   // once per CTA
+      else p.load_const(weight + c0 + i * step);
+    }
+    p.get(w[i]);
+#pragma unroll
+    for (int j = 0; j < U / 2; ++j) dw[i][j] = both(0.f);
+  }
+  const float we[2] = {there[0] ? wide(weight[col[0]]) : 0.f, there[1] ? wide(weight[col[1]]) : 0.f};
+  float dwe[2] = {0.f, 0.f};
   int stage = 0, par = 0;
   for (int64_t base = (int64_t)blockIdx.x * rpb; base < a.rows; base += stride, par ^= 1) {
     const int64_t r = base + th.slot;
@@ -642,22 +642,24 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_grad_scalar_kernel(const __g
   }
 }
 
-// dweight = the sum of the parts, in a fixed order: 32 columns per CTA, a warp takes every 32nd part.
+// dweight = the sum of the parts, in a fixed order: 16 columns per CTA, 64 threads per column, each taking every 64th part.
 __global__ void __launch_bounds__(1024) dweight_kernel(const float* part, float* dweight, int parts, int d) {
-  __shared__ float sum[32][33];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  __shared__ float sum[64][17];
+  const int col = threadIdx.x & 15, group = threadIdx.x >> 4, c = blockIdx.x * 16 + col;
   float s = 0.f;
   cudaGridDependencySynchronize();   // launched before the kernel that writes the parts has ended
   if (c < d) {
-#pragma unroll 8
-    for (int p = warp; p < parts; p += 32) s += part[(int64_t)p * d + c];
+#pragma unroll 10
+    for (int p = group; p < parts; p += 64) s += part[(int64_t)p * d + c];
   }
-  sum[warp][lane] = s;
+  sum[group][col] = s;
   __syncthreads();
-  s = sum[lane][warp];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (warp >= 16) return;
+  s = sum[lane][warp] + sum[lane + 32][warp];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
-  if (lane == 0 && blockIdx.x * 32 + warp < d) dweight[blockIdx.x * 32 + warp] = s;
+  if (lane == 0 && blockIdx.x * 16 + warp < d) dweight[blockIdx.x * 16 + warp] = s;
 }
 
 cudaError_t launch_dweight(const float* part, float* dweight, int parts, int d, cudaStream_t st) {
@@ -665,7 +667,7 @@ cudaError_t launch_dweight(const float* part, float* dweight, int parts, int d, 
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((d + 31) / 32), cfg.blockDim = dim3(1024), cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
+  cfg.gridDim = dim3((d + 15) / 16), cfg.blockDim = dim3(1024), cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, dweight_kernel, part, dweight, parts, d);
 }
 
@@ -698,8 +700,12 @@ GradShape grad_shape(int64_t rows, int d, Layout3 lay, int elem_bytes, bool dsum
   g.s = shape_for(units, units <= 1024 ? 2 : elem_bytes == 4 ? 8 : 4, ragged ? u : 1);
   const int rpb = g.s.threads / g.s.tpr;
   const int64_t all = (rows + rpb - 1) / rpb;
-  const int per_sm = 512 / g.s.threads < 1 ? 1 : 512 / g.s.threads;
-  g.stages = 3;
+  // About 12 warps per SM and 48 to 72 KB of rows on their way.  CTAs per SM / stages, us (16384 rows with dsum, weight's
+  // gradient included): 2048 bf16 3 / 3 47.4, 4 / 2 47.3, 3 / 2 49.5, 4 / 3 49.6; 1024 bf16 6 / 3 27.0, 6 / 2 28.7, 8 / 3 29.6; 4096 bf16 2 /
+  // 2 85.5, 2 / 3 87.0; 4096 fp32 without dsum 1 / 3 122, 1 / 2 138.
+  const int per_sm = g.s.threads >= 384 ? 1 : g.s.threads > 192 ? 2 : 384 / g.s.threads;
+  const size_t flying = grad_smem(g.s, 1, d, false, dsum, false) * per_sm;
+  g.stages = flying >= 48 * 1024 ? 2 : 3;
   while (g.stages > 1 && grad_smem(g.s, g.stages, d, ragged, dsum, dweight) > kGradSmemMost / per_sm) --g.stages;
   g.smem = grad_smem(g.s, g.stages, d, ragged, dsum, dweight);
   int ctas = per_sm * kSms;
