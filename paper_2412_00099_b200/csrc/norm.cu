@@ -81,10 +81,17 @@ __device__ __forceinline__ void store_e4m3(uint8_t* p, const float2 (&v)[N]) {
 }
 __device__ __forceinline__ uint32_t magnitude(float n) { return __float_as_uint(fabsf(n)); }   // NaN above everything
 
+// Column of the single element that thread t of a ragged row looks after: the first U threads before the units, the next U behind.
+template <int U>
+__device__ __forceinline__ int single_column(int t, int head, int whole, int d) {
+  const int c = t < U ? t : head + whole + t - U;
+  return (t < U ? t < head : t < 2 * U && c < d) ? c : -1;
+}
+
 // A row is read once: its units stay in registers from the addition to the last output, VPT of them per thread, so
 // that a thread has all its loads in flight before the point where the threads of a row meet.
 // RAGGED: rows start anywhere.  The units are those of the memory, up to U - 1 elements before the first and behind
-// the last one are single elements of the row's first U threads.
+// the last one are single elements, one for each of the row's first 2 U threads.
 template <typename T, typename A, typename W, int VPT, bool RAGGED>
 __global__ void __launch_bounds__(512) rmsnorm_kernel(const __grid_constant__ NormArgs a) {
   constexpr int U = 16 / (int)sizeof(T);
@@ -131,19 +138,13 @@ __global__ void __launch_bounds__(512) rmsnorm_kernel(const __grid_constant__ No
       h[i].set(v);
     }
   }
-  // single elements: column t of the head, column t behind the units
-  const int tail = head + whole + th.t;
-  const bool in_head = RAGGED && th.t < head, in_tail = RAGGED && tail < d;
-  float h_head = 0.f, h_tail = 0.f;
-  if (RAGGED) {
-    auto one = [&](int c) {
-      const float v = wide(xr[c]);
-      return a.add ? wide(narrow<T>(v + wide(ar[c]))) : v;
-    };
-    if (in_head) h_head = one(th.t);
-    if (in_tail) h_tail = one(tail);
+  const int ce = RAGGED ? single_column<U>(th.t, head, whole, d) : -1;   // of this thread's single element, -1: none
+  float he = 0.f;
+  if (ce >= 0) {
+    he = wide(xr[ce]);
+    if (a.add) he = wide(narrow<T>(he + wide(ar[ce])));
   }
-  float2 ss2 = make_float2(h_head * h_head, h_tail * h_tail);
+  float2 ss2 = make_float2(he * he, 0.f);
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     float2 v[U / 2];
@@ -157,8 +158,7 @@ __global__ void __launch_bounds__(512) rmsnorm_kernel(const __grid_constant__ No
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
       if (in[i]) h[i].store(sum + head + c0 + i * step);
-    if (in_head) sum[th.t] = narrow<T>(h_head);
-    if (in_tail) sum[tail] = narrow<T>(h_tail);
+    if (ce >= 0) sum[ce] = narrow<T>(he);
   }
   if (!a.out && !a.q) return;
 
@@ -174,9 +174,9 @@ __global__ void __launch_bounds__(512) rmsnorm_kernel(const __grid_constant__ No
   };
   if constexpr (RAGGED) with_shift(weight + head, whole, weight, weight + a.d, load_weights);
   else load_weights(Int<kInPlace>{});
-  const float w_head = in_head ? wide(weight[th.t]) : 0.f, w_tail = in_tail ? wide(weight[tail]) : 0.f;
+  const float we = ce >= 0 ? wide(weight[ce]) : 0.f;
   const float inv = inv_rms(row_sum(ss, a.tpr, buf), a.inv_d, a.eps);
-  const float n_head = h_head * inv * w_head, n_tail = h_tail * inv * w_tail;
+  const float ne = he * inv * we;
   auto norm_unit = [&](int i, float2 (&n)[U / 2]) {
     float2 wv[U / 2];
     h[i].get(n);
@@ -194,8 +194,7 @@ __global__ void __launch_bounds__(512) rmsnorm_kernel(const __grid_constant__ No
       o.set(n);
       if (in[i]) o.store(out + head + c0 + i * step);
     }
-    if (in_head) out[th.t] = narrow<T>(n_head);
-    if (in_tail) out[tail] = narrow<T>(n_tail);
+    if (ce >= 0) out[ce] = narrow<T>(ne);
   }
   if (!a.q) return;
 
@@ -203,7 +202,7 @@ __global__ void __launch_bounds__(512) rmsnorm_kernel(const __grid_constant__ No
   uint8_t* q = a.q + r * a.ld_q;
   float* scales = a.scales + r * a.n_groups;
   if (a.quant == kQuantRow) {
-    uint32_t top = max(kAmaxFloor, max(magnitude(n_head), magnitude(n_tail)));
+    uint32_t top = max(kAmaxFloor, magnitude(ne));
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       float2 n[U / 2];
@@ -221,8 +220,7 @@ __global__ void __launch_bounds__(512) rmsnorm_kernel(const __grid_constant__ No
       for (int j = 0; j < U / 2; ++j) n[j] = mul2(n[j], both(back));
       if (in[i]) store_e4m3(q + head + c0 + i * step, n);
     }
-    if (in_head) q[th.t] = e4m3(n_head * back);
-    if (in_tail) q[tail] = e4m3(n_tail * back);
+    if (ce >= 0) q[ce] = e4m3(ne * back);
   } else if (!RAGGED) {
     // a group is a power of two of neighbouring lanes
     const int lanes = (1 << a.group_log2) / U;
@@ -245,8 +243,7 @@ __global__ void __launch_bounds__(512) rmsnorm_kernel(const __grid_constant__ No
   } else {
     // a unit's columns may belong to two groups
     uint32_t* m = amax + th.slot * a.n_groups;
-    if (in_head) atomicMax(m, magnitude(n_head));   // the head is shorter than a group
-    if (in_tail) atomicMax(m + (tail >> a.group_log2), magnitude(n_tail));
+    if (ce >= 0) atomicMax(m + (ce >> a.group_log2), magnitude(ne));
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       if (!in[i]) continue;
@@ -277,8 +274,7 @@ __global__ void __launch_bounds__(512) rmsnorm_kernel(const __grid_constant__ No
       for (int j = 0; j < U / 2; ++j) n[j] = mul2(n[j], make_float2(2 * j < cut ? b0 : b1, 2 * j + 1 < cut ? b0 : b1));
       store_e4m3(q + c, n);
     }
-    if (in_head) q[th.t] = e4m3(n_head * back_of(scale_of(m[0])));
-    if (in_tail) q[tail] = e4m3(n_tail * back_of(scale_of(m[tail >> a.group_log2])));
+    if (ce >= 0) q[ce] = e4m3(ne * back_of(scale_of(m[ce >> a.group_log2])));
   }
 }
 
@@ -377,8 +373,8 @@ cudaError_t launch_norm_types(const NormArgs& a, int dtype, bool ragged, const N
 // One unit per thread: 16384 x 4096 98.8, a single row of 2048 7.2 against 7.3.
 NormShape norm_shape(int64_t rows, int d, bool ragged, int elem_bytes, int group_log2) {
   const int u = 16 / elem_bytes, units = d / u;
-  // a group of columns has to fit the lanes of one unit step; a ragged row needs a thread for every single element
-  const int least = ragged ? u : group_log2 < 30 ? (1 << group_log2) / u : 1;
+  // a group of columns has to fit the lanes of one unit step; a ragged row needs 2 U threads for its single elements
+  const int least = ragged ? 2 * u : group_log2 < 30 ? (1 << group_log2) / u : 1;
   const bool two = units <= 1024 && !(ragged && rows > 4096 && units > 256);
   return shape_for(units, two ? 2 : elem_bytes == 4 ? 8 : 4, least);
 }
@@ -454,22 +450,15 @@ __global__ void __launch_bounds__(512) rmsnorm_grad_kernel(const __grid_constant
   const int tensor_bytes = VPT * (int)blockDim.x * 16, stage_bytes = (a.dsum ? 3 : 2) * tensor_bytes;
   uint8_t* ring = smem + threadIdx.x * 16;
 
-  // single elements of a ragged row, of its first U threads: one before the units, one behind them
-  const int tail = head + whole + th.t;
-  const bool edges = RAGGED && th.t < U;
-  const bool there[2] = {RAGGED && th.t < head, RAGGED && tail < a.d};
-  const int col[2] = {th.t, tail};
-  struct Edge {
-    T h[2], g[2], s[2];   // as loaded: converting would wait for them
-  } edge{}, next{};
-  auto fetch_edge = [&](int64_t r) {
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-      if (there[k] && r < a.rows) {
-        next.h[k] = ((const T*)a.h)[r * a.ld_h + col[k]];
-        next.g[k] = ((const T*)a.dout)[r * a.ld_dout + col[k]];
-        if (a.dsum) next.s[k] = ((const T*)a.dsum)[r * a.ld_dsum + col[k]];
-      }
+  const int ce = RAGGED ? single_column<U>(th.t, head, whole, a.d) : -1;   // of this thread's single element, -1: none
+  struct Single {
+    T h, g, s;   // as loaded: converting would wait for them
+  } one{}, next{};
+  auto fetch_one = [&](int64_t r) {
+    if (ce < 0 || r >= a.rows) return;
+    next.h = ((const T*)a.h)[r * a.ld_h + ce];
+    next.g = ((const T*)a.dout)[r * a.ld_dout + ce];
+    if (a.dsum) next.s = ((const T*)a.dsum)[r * a.ld_dsum + ce];
   };
   auto fetch = [&](int64_t r, int stage) {
     const bool row = r < a.rows;
@@ -495,7 +484,7 @@ __global__ void __launch_bounds__(512) rmsnorm_grad_kernel(const __grid_constant
     fetch(first + k * stride, k);
     copies_commit();
   }
-  if (edges) fetch_edge(first);
+  if (RAGGED) fetch_one(first);
   const W* weight = (const W*)a.weight;
   float2 w[VPT][U / 2], dw[VPT][U / 2];
 #pragma unroll
@@ -510,8 +499,8 @@ __global__ void __launch_bounds__(512) rmsnorm_grad_kernel(const __grid_constant
 #pragma unroll
     for (int j = 0; j < U / 2; ++j) dw[i][j] = both(0.f);
   }
-  const float we[2] = {there[0] ? wide(weight[col[0]]) : 0.f, there[1] ? wide(weight[col[1]]) : 0.f};
-  float dwe[2] = {0.f, 0.f};
+  const float we = ce >= 0 ? wide(weight[ce]) : 0.f;
+  float dwe = 0.f;
   int stage = 0, par = 0;
   for (int64_t base = (int64_t)blockIdx.x * rpb; base < a.rows; base += stride, par ^= 1) {
     const int64_t r = base + th.slot;
@@ -520,15 +509,11 @@ __global__ void __launch_bounds__(512) rmsnorm_grad_kernel(const __grid_constant
     fetch(r + (a.stages - 1) * stride, into);
     copies_commit();
     float2 sum = both(0.f);   // of h^2, of h g
-    if (edges) {
-      edge = next;
-      fetch_edge(r + stride);
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const float he = wide(edge.h[k]);
-        sum.x = fmaf(he, he, sum.x);
-        sum.y = fmaf(he, wide(edge.g[k]) * we[k], sum.y);
-      }
+    if (RAGGED) {
+      one = next;
+      fetch_one(r + stride);
+      const float he = wide(one.h);   // zero for a thread without one
+      sum = make_float2(he * he, he * (wide(one.g) * we));
     }
     if (a.stages == 1) copies_wait<0>();
     else if (a.stages == 2) copies_wait<1>();
@@ -569,14 +554,10 @@ __global__ void __launch_bounds__(512) rmsnorm_grad_kernel(const __grid_constant
       o.set(v);
       if (in[i] && r < a.rows) o.store(xr + c0 + i * step);
     }
-    if (edges && r < a.rows) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        if (!there[k]) continue;
-        const float he = wide(edge.h[k]), ge = wide(edge.g[k]);
-        xr[col[k] - head] = narrow<T>(fmaf(ge * we[k], inv, fmaf(he * inv, coef, a.dsum ? wide(edge.s[k]) : 0.f)));
-        dwe[k] = fmaf(ge, he * inv, dwe[k]);
-      }
+    if (ce >= 0 && r < a.rows) {
+      const float he = wide(one.h), ge = wide(one.g);
+      xr[ce - head] = narrow<T>(fmaf(ge * we, inv, fmaf(he * inv, coef, a.dsum ? wide(one.s) : 0.f)));
+      dwe = fmaf(ge, he * inv, dwe);
     }
     if (++stage == a.stages) stage = 0;
   }
@@ -603,9 +584,7 @@ __global__ void __launch_bounds__(512) rmsnorm_grad_kernel(const __grid_constant
         float* p = mine + head + c0 + i * step + 2 * j;
         p[0] = dw[i][j].x, p[1] = dw[i][j].y;
       }
-#pragma unroll
-  for (int k = 0; k < 2; ++k)
-    if (there[k]) mine[col[k]] = dwe[k];
+  if (ce >= 0) mine[ce] = dwe;
   __syncthreads();
   for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
     float v = 0.f;
@@ -697,7 +676,7 @@ GradShape grad_shape(int64_t rows, int d, Layout3 lay, int elem_bytes, bool dsum
   }
   const bool ragged = lay == kRagged;
   const int u = 16 / elem_bytes, units = d / u;
-  g.s = shape_for(units, units <= 1024 ? 2 : elem_bytes == 4 ? 8 : 4, ragged ? u : 1);
+  g.s = shape_for(units, units <= 1024 ? 2 : elem_bytes == 4 ? 8 : 4, ragged ? 2 * u : 1);
   const int rpb = g.s.threads / g.s.tpr;
   const int64_t all = (rows + rpb - 1) / rpb;
   // About 12 warps per SM and 48 to 72 KB of rows on their way.  CTAs per SM / stages, us (16384 rows with dsum, weight's
