@@ -307,7 +307,8 @@ typedef struct {
  *   scales DEVICE fp32 [rows, ceil(d / quant_group)] out, contiguous; given exactly when q is.  The last group of a
  *       row may be shorter.  q_j * scales_G is within 2^-4 |n_j| (or half a subnormal step) of n_j.
  * One of sum, out and q at least.  Apart from sum == x no output may overlap another tensor of the call.  A row that holds a NaN is
- * NaN throughout; the sum of squares is formed in fp32, so one beyond 3.4e38 counts as infinite (r = 0). */
+ * NaN throughout; the sum of squares is formed in fp32, so one beyond 3.4e38 counts as infinite (r = 0) and squares
+ * below 1e-45 as zero. */
 int mcce_rmsnorm(const mcce_norm* n /*HOST*/, const void* x, const void* add, const void* weight, void* sum,
                  void* out, void* q, float* scales, void* cuda_stream);
 
@@ -333,7 +334,7 @@ typedef struct {
   int32_t n_tokens;    /* >= 0                                                                            */
   int32_t top_k;       /* 1..16                                                                           */
   int32_t n_experts;   /* 1..256 (mcce_dispatch)                                                          */
-  int32_t d;           /* columns of a row, >= 1                                                          */
+  int32_t d;           /* columns of a row, 1..2^24                                                       */
   int32_t dtype;       /* sorted rows: MCCE_F32 or MCCE_BF16; MCCE_E4M3 too in mcce_dispatch              */
   int32_t token_dtype; /* y, add and dy: MCCE_F32, or dtype (mcce_combine and its gradient)               */
   int32_t scale_cols;  /* fp32 scales that travel with a row, 0: none (mcce_dispatch)                     */

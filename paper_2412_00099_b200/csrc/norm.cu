@@ -89,7 +89,9 @@ __device__ __forceinline__ int single_column(int t, int head, int whole, int d) 
 }
 
 // A row is read once: its units stay in registers from the addition to the last output, VPT of them per thread, so
-// that a thread has all its loads in flight before the point where the threads of a row meet.
+// that a thread has all its loads in flight before the point where the threads of a row meet.  fp32 arithmetic in pairs: one
+// element at a time, with its conversions, kept the scheduler busier than the memory (16384 x 4096 bf16: 98 us, now 81.5).
+// Bound: HBM, 1.0 of the copy bandwidth there (537 MB); ragged rows 0.83 (16384 x 4097 with fp32 add and 8-bit rows 135 us).
 // RAGGED: rows start anywhere.  The units are those of the memory, up to U - 1 elements before the first and behind
 // the last one are single elements, one for each of the row's first 2 U threads.
 template <typename T, typename A, typename W, int VPT, bool RAGGED>
@@ -430,9 +432,10 @@ __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_grou
 // RAGGED: the step between a thread's rows is a multiple of U (or it has one row), so that every one of its rows starts at
 // the same place in a unit.  A thread therefore has the same columns in all its rows, aligned or not, and keeps their
 // weights and its part of the weights' gradient in registers.
-// Bound: HBM for aligned rows (16384 x 2048 bf16 with dsum: 42 us = 0.97 of the copy bandwidth, with the weight's gradient and
-// the second launch 43); ragged rows issue (16384 x 4097: 120 us = 0.68).  With the row in registers instead of the ring, loaded
-// when it was needed, the first took 62 us; with columns that move from row to row and sums in shared memory the second 148.
+// Bound: HBM for aligned rows (16384 x 2048 bf16 with dsum: 40.5 us = 1.0 of the copy bandwidth, 47.4 back to back with the launch that
+// adds the parts of the weight's gradient); ragged rows add the pass over the single elements to every row's chain (16384 x 4097: 96
+// us = 0.85).  With the row in registers instead of the ring, loaded when it was needed, the first took 62 us; with columns that
+// move from row to row and sums in shared memory the second 148.
 template <typename T, typename W, int VPT, bool RAGGED>
 __global__ void __launch_bounds__(512) rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a) {
   constexpr int U = 16 / (int)sizeof(T);
@@ -461,15 +464,12 @@ __global__ void __launch_bounds__(512) rmsnorm_grad_kernel(const __grid_constant
     if (a.dsum) next.s = ((const T*)a.dsum)[r * a.ld_dsum + ce];
   };
   auto fetch = [&](int64_t r, int stage) {
-    const bool row = r < a.rows;
-    const int64_t rr = row ? r : 0;
-    const int at = RAGGED && !row ? 0 : head;   // (another row's phase would leave the address unaligned)
-    const T *hr = (const T*)a.h + rr * a.ld_h + at, *gr = (const T*)a.dout + rr * a.ld_dout + at;
-    const T* sr = (const T*)a.dsum + rr * a.ld_dsum + at;
+    const T *hr = (const T*)a.h + r * a.ld_h + head, *gr = (const T*)a.dout + r * a.ld_dout + head;
+    const T* sr = (const T*)a.dsum + r * a.ld_dsum + head;
     uint8_t* to = ring + stage * stage_bytes;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      if (!(row && in[i])) {   // what such a unit holds is never used, but has to be finite for the sums
+      if (!(r < a.rows && in[i])) {   // adds nothing to the sums
         *(uint4*)(to + i * (int)blockDim.x * 16) = *(uint4*)(to + tensor_bytes + i * (int)blockDim.x * 16) = make_uint4(0, 0, 0, 0);
         continue;
       }

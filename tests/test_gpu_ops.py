@@ -3,9 +3,10 @@ addition and 8-bit output, its gradient, rows sorted by expert, their weighted r
 
 Tolerances.  u = 2^-24 is half an fp32 step, U(T) half a step of the output type relative to the value (bf16 2^-8, fp32
 2^-24).  A fp32 sum of n terms is off by at most (n - 1) u times the sum of the terms' magnitudes, whatever its order;
-each multiplication, division, square root adds u.  The norm's sum of squares has only positive terms and no thread adds more than 64 of
-them in a row before the tree (10 levels at most), so it is off by 74 u relatively and r = 1 / sqrt(.) by
-(74 + 1 + 1) / 2 u + 2 u = 40 u; h r weight adds two: 42 u.  NORM_U = 64 u covers it with room for the division in the scales."""
+each multiplication or division adds u.  The norm's sum of squares has only positive terms and no thread adds more than 64 of
+them in a row before the tree (10 levels at most), so it is off by 74 u relatively, its mean plus eps by 3 u more (1 / d is
+rounded too) and r by half of that and the two units in the last place of the reciprocal square root (4 u): 43 u; h r weight
+adds two: 45 u.  NORM_U = 64 u covers it with room for the two factors in the scales."""
 import math
 
 import numpy as np

@@ -84,7 +84,7 @@ def test_norm_backward_buffers(lib):
     assert call(dx=P[0], n=norm(ld_sum=128)) == EINVAL and call(dx=P[2], n=norm(ld_sum=128)) == EINVAL
 
 
-BAD_ROWS = [dict(n_layers=0), dict(n_layers=65536), dict(n_tokens=-1), dict(top_k=0), dict(top_k=17), dict(d=0),
+BAD_ROWS = [dict(n_layers=0), dict(n_layers=65536), dict(n_tokens=-1), dict(top_k=0), dict(top_k=17), dict(d=0), dict(d=(1 << 24) + 1),
             dict(n_tokens=1 << 28, top_k=8), dict(ld_token=63), dict(ld_rows=1), dict(ld_rows=-64),
             dict(scale_cols=-1), dict(dtype=3), dict(dtype=-1)]
 
