@@ -432,7 +432,7 @@ __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_grou
 // RAGGED: the step between a thread's rows is a multiple of U (or it has one row), so that every one of its rows starts at
 // the same place in a unit.  A thread therefore has the same columns in all its rows, aligned or not, and keeps their
 // weights and its part of the weights' gradient in registers.
-// Bound: HBM for aligned rows (16384 x 2048 bf16 with dsum: 40.5 us = 1.0 of the copy bandwidth, 47.4 back to back with the launch that
+// Bound: HBM for aligned rows (16384 x 2048 bf16 with dsum: 40.5 us = 1.0 of the copy bandwidth, 47.6 back to back with the launch that
 // adds the parts of the weight's gradient); ragged rows add the pass over the single elements to every row's chain (16384 x 4097: 96
 // us = 0.85).  With the row in registers instead of the ring, loaded when it was needed, the first took 62 us; with columns that
 // move from row to row and sums in shared memory the second 148.
@@ -679,10 +679,14 @@ GradShape grad_shape(int64_t rows, int d, Layout3 lay, int elem_bytes, bool dsum
   g.s = shape_for(units, units <= 1024 ? 2 : elem_bytes == 4 ? 8 : 4, ragged ? 2 * u : 1);
   const int rpb = g.s.threads / g.s.tpr;
   const int64_t all = (rows + rpb - 1) / rpb;
-  // About 12 warps per SM and 48 to 72 KB of rows on their way.  CTAs per SM / stages, us (16384 rows with dsum, weight's
-  // gradient included): 2048 bf16 3 / 3 47.4, 4 / 2 47.3, 3 / 2 49.5, 4 / 3 49.6; 1024 bf16 6 / 3 27.0, 6 / 2 28.7, 8 / 3 29.6; 4096 bf16 2 /
-  // 2 85.5, 2 / 3 87.0; 4096 fp32 without dsum 1 / 3 122, 1 / 2 138.
-  const int per_sm = g.s.threads >= 384 ? 1 : g.s.threads > 192 ? 2 : 384 / g.s.threads;
+  // 12 to 16 warps per SM with about 72 to 108 KB of rows on their way.  CTAs per SM / stages, us (16384 rows with dsum,
+  // weight's gradient included; the two figures of 2048: launches apart, back to back): 2048 bf16 4 / 2 49.3 and 47.6,
+  // 3 / 3 50.2 and 47.3, 4 / 3 49.8 and 49.8, 6 / 3 54.9 and 56; 1024 bf16 6 / 3 27.0, 6 / 2 28.7, 8 / 3 29.6; 4096 bf16
+  // 2 / 2 85.5, 2 / 3 87.0; 4096 fp32 without dsum 1 / 3 122, 1 / 2 138; 1001 x 1411 fp32 2 / 2 11.3, 2 / 3 12.3.
+  int per_sm = g.s.threads <= 64 ? 6 : g.s.threads >= 384 ? 1 : g.s.threads > 192 ? 2 : 512 / g.s.threads;
+  // Two such CTAs that are left with one stage lose to one with two from 288 threads on (8192 x 9216 fp32 201 -> 155, 4096 x
+  // 10000 bf16 100 -> 71), but not below (8192 x 5120 fp32 with dsum 130 against 124).
+  if (g.s.threads > 256 && grad_smem(g.s, 2, d, ragged, dsum, dweight) > kGradSmemMost / 2) per_sm = 1;
   const size_t flying = grad_smem(g.s, 1, d, false, dsum, false) * per_sm;
   g.stages = flying >= 48 * 1024 ? 2 : 3;
   while (g.stages > 1 && grad_smem(g.s, g.stages, d, ragged, dsum, dweight) > kGradSmemMost / per_sm) --g.stages;
