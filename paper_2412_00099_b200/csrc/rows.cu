@@ -60,21 +60,18 @@ struct CopyArgs {
   float* row_scales;
 };
 
-// The row of a token to the positions of its pairs, by `parts` warps of which this is number `part`: V units of the row are read, all
-// in flight, and written once for every pair, so a token's row is read once.  The warps of a row take turns every 32 units of 16
-// bytes (24 x 256 tokens x 4 of 4096 bytes: 25.3 us, with blocks of 128 units 29.6), or blocks of 256 narrower ones, whose loads and
-// stores lie at fixed distances then and need no look at the row's end (8192 x 8 of 1411 bf16: 57 us against 73).
+// A row of units narrower than 16 bytes to the positions of its token's pairs, by `parts` warps of which this is number `part`:
+// V units of the row are read, all in flight, and written once for every pair, so a token's row is read once.  Full blocks'
+// loads and stores lie at fixed distances and need no look at the row's end (8192 x 8 of 1411 bf16: 57 us against 73).
 // position_of(k): of pair k, -1: none.
 template <typename V_, typename F>
 __device__ __forceinline__ void move_row(const CopyArgs& a, int64_t t, int64_t first, int lane, int part, int parts, F position_of) {
-  constexpr bool kWide = sizeof(V_) == 16;
-  constexpr int V = kWide ? 4 : 8;
+  constexpr int V = 8;
   const V_* x = (const V_*)a.x + t * a.ld_x;
   V_* rows = (V_*)a.rows + first * a.ld_rows;
-  const int step = kWide ? parts * 32 : 32, u0 = kWide ? part * 32 + lane : lane;
-  for (int b = kWide ? 0 : part * 32 * V; b < a.units; b += parts * 32 * V) {
+  for (int b = part * 32 * V; b < a.units; b += parts * 32 * V) {
     V_ p[V];
-    if (!kWide && b + 32 * V <= a.units) {
+    if (b + 32 * V <= a.units) {
 #pragma unroll
       for (int v = 0; v < V; ++v) p[v] = __ldg(x + b + lane + v * 32);
       for (int k = 0; k < a.K; ++k) {
@@ -87,38 +84,96 @@ __device__ __forceinline__ void move_row(const CopyArgs& a, int64_t t, int64_t f
     } else {
 #pragma unroll
       for (int v = 0; v < V; ++v)
-        if (b + u0 + v * step < a.units) p[v] = __ldg(x + b + u0 + v * step);
+        if (b + lane + v * 32 < a.units) p[v] = __ldg(x + b + lane + v * 32);
       for (int k = 0; k < a.K; ++k) {
         const int pos = position_of(k);
         if (pos < 0) continue;
-        V_* to = rows + pos * a.ld_rows + b + u0;
+        V_* to = rows + pos * a.ld_rows + b + lane;
 #pragma unroll
         for (int v = 0; v < V; ++v)
-          if (b + u0 + v * step < a.units) to[v * step] = p[v];
+          if (b + lane + v * 32 < a.units) to[v * 32] = p[v];
       }
     }
   }
 }
 
+// Rows of 16-byte units go through shared memory in pieces of kPiece units: fetched by cp.async, which needs no registers and so
+// starts before the counting, and written by one bulk copy per pair, issued by as many lanes at once.  Against loads into registers
+// and stores of 16 bytes per lane, us: 16384 x 8 rows of 2048 bytes with scales 55.0 / 58, of 4096 bytes 94.5 / 99; 24 x 256
+// tokens x 4 of 4096 bytes 24.4 / 24.8; 20000 x 8 of 1024 bytes 48.0 / 46.7 (half of a piece's lanes idle).  Pieces of 64 units, three
+// per warp: 56.2, 95.0, 24.2 and 46.1.
+constexpr int kPiece = 128, kRing = 2;
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void fetch_unit(uint4* to, const uint4* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(shared_address(to)), "l"(__cvta_generic_to_global(from)) : "memory");
+}
+__device__ __forceinline__ void bulk_store(void* to, const uint4* from, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(__cvta_generic_to_global(to)),
+               "r"(shared_address(from)), "r"(bytes)
+               : "memory");
+}
+
+// The pieces that a warp moves, one after the other: number `part` of `parts` warps that share a token.
+struct Pieces {
+  int t, b;
+  __device__ __forceinline__ Pieces(int warp, int part, int parts, int blocks, int n_tok) : t(part < blocks ? warp / parts : n_tok), b(part) {}
+  __device__ __forceinline__ void next(int part, int parts, int blocks) {
+    b += parts;
+    if (b >= blocks) b = part, t += 8 / parts;
+  }
+};
+
 // Ranks the pairs of a few tokens and moves their rows.  Where a pair goes: pairs of smaller experts (totals of all chunks), of
 // its expert in earlier chunks (both from the chunks' counts), earlier in its chunk (counted here again), earlier in this
 // CTA.  A layer of few pairs is one chunk: the CTA counts all of it, and there is no launch before this one.
-// Bound: HBM writes, once the counting is done: 16384 x 8 rows of 4096 bytes 106 us, 95.5 of them the rows (0.96 of the copy bandwidth),
-// the rest two launches and the counts; of 2048 bytes with scales 59 (0.73).
+// A pair's rank among its CTA's pairs comes from its warp's matches and the counts of the warps before.
+// Bound: HBM writes, once the counting is done: 16384 x 8 rows of 4096 bytes 94.5 us (0.89 of the copy bandwidth), of 2048 bytes with
+// scales 55 (0.79); about 8 us of each are the counting launch and the wait for the first CTAs' positions.  More CTAs per SM
+// at once are slower, not faster: 5 / 6 / 8 of them 99 / 101 / 115 with 4096 bytes (before the bulk copies).
 constexpr int kCtaPairs = 128;    // pairs of a CTA at most
 template <typename V>
 __global__ void __launch_bounds__(256) rows_dispatch_kernel(const __grid_constant__ SortArgs s, const __grid_constant__ CopyArgs a,
                                                             const int tokens_per_cta) {
-  __shared__ int total[kMaxE], before[kMaxE], warp_sum[8], id[kCtaPairs], place[kCtaPairs];
+  __shared__ int total[kMaxE], before[kMaxE], warp_sum[8], place[kCtaPairs], in_warp[4][kMaxE];
   const int l = blockIdx.y, t0 = blockIdx.x * tokens_per_cta, n_tok = min(tokens_per_cta, s.T - t0);
   const int q0 = t0 * s.K, n = n_tok * s.K, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int b = t0 / s.chunk, chunk0 = b * s.chunk * s.K;
   const int32_t* sel = s.sel + (size_t)l * s.P;
+  const int64_t first = (int64_t)l * s.P;
+  // one warp per token for eight tokens or more, else the eight warps shared out
+  const int parts = n_tok >= 8 ? 1 : n_tok >= 4 ? 2 : n_tok >= 2 ? 4 : 8, part = warp & (parts - 1);
+  constexpr bool kBulk = sizeof(V) == 16;
+  __shared__ uint4 ring[kBulk ? 8 * kRing * kPiece : 1];
+  uint4* mine = ring + (kBulk ? warp * kRing * kPiece : 0);
+  const int blocks = (a.units + kPiece - 1) / kPiece;
+  Pieces ahead(warp, part, parts, blocks, n_tok);
+  auto fetch = [&](int slot) {
+    if (ahead.t < n_tok) {
+      const uint4* x = (const uint4*)a.x + ((int64_t)l * s.T + t0 + ahead.t) * a.ld_x;
+#pragma unroll
+      for (int v = 0; v < kPiece / 32; ++v) {
+        const int u = lane + 32 * v;
+        if (ahead.b * kPiece + u < a.units) fetch_unit(mine + slot * kPiece + u, x + ahead.b * kPiece + u);
+      }
+      ahead.next(part, parts, blocks);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  int e_mine = -1, rank = 0;
+  if (tid < n) e_mine = sel[q0 + tid];
+  if ((unsigned)e_mine >= (unsigned)s.E) e_mine = -1;
+  if constexpr (kBulk) {
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) fetch(i);
+  }
   total[tid] = before[tid] = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) in_warp[w][tid] = 0;
   __syncthreads();
-  if (tid < n) {
-    const int e = sel[q0 + tid];
-    id[tid] = (unsigned)e < (unsigned)s.E ? e : -1;
+  if (warp * 32 < n) {
+    const unsigned same = __match_any_sync(kFull, e_mine);
+    rank = __popc(same & ((1u << lane) - 1));
+    if (e_mine >= 0 && rank == 0) in_warp[warp][e_mine] = __popc(same);
   }
   if (s.B == 1) {   // total and, in the upper half of a word, before
 #pragma unroll 4
@@ -166,29 +221,53 @@ __global__ void __launch_bounds__(256) rows_dispatch_kernel(const __grid_constan
   }
   __syncthreads();
   if (tid < n) {
-    const int e = id[tid];
     int pos = -1;
-    if (e >= 0) {
-      pos = before[e];
-      for (int j = 0; j < tid; ++j) pos += id[j] == e;
+    if (e_mine >= 0) {
+      pos = before[e_mine] + rank;
+      for (int w = 0; w < warp; ++w) pos += in_warp[w][e_mine];
     }
     place[tid] = pos;
     s.inv[(size_t)l * s.P + q0 + tid] = pos;
     if (s.perm && pos >= 0) s.perm[(size_t)l * s.P + pos] = q0 + tid;
   }
   __syncthreads();
-  // one warp per token for eight tokens or more, else the eight warps shared out
-  const int64_t first = (int64_t)l * s.P;
-  const int parts = n_tok >= 8 ? 1 : n_tok >= 4 ? 2 : n_tok >= 2 ? 4 : 8, part = warp & (parts - 1);
-  for (int t = warp / parts; t < n_tok; t += 8 / parts) {
-    const int64_t token = (int64_t)l * s.T + t0 + t;
-    if (a.x) move_row<V>(a, token, first, lane, part, parts, [&](int k) { return place[t * s.K + k]; });
-    for (int k = part; a.scale_cols && k < s.K; k += parts) {
-      const int pos = place[t * s.K + k];
-      for (int i = lane; pos >= 0 && i < a.scale_cols; i += 32)
-        a.row_scales[(first + pos) * a.scale_cols + i] = a.scales[token * a.scale_cols + i];
+  if constexpr (kBulk) {
+    int slot = 0;
+    for (Pieces p(warp, part, parts, blocks, n_tok); p.t < n_tok; p.next(part, parts, blocks)) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      const int pos = lane < s.K ? place[p.t * s.K + lane] : -1;
+      if (pos >= 0)
+        bulk_store((uint4*)a.rows + (first + pos) * a.ld_rows + p.b * kPiece, mine + slot * kPiece, min(kPiece, a.units - p.b * kPiece) * 16);
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+      if (ahead.t < n_tok) {
+        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
+      }
+      fetch(slot);
+      slot = slot + 1 == kRing ? 0 : slot + 1;
+    }
+  } else if (a.x) {
+    for (int t = warp / parts; t < n_tok; t += 8 / parts)
+      move_row<V>(a, (int64_t)l * s.T + t0 + t, first, lane, part, parts, [&](int k) { return place[t * s.K + k]; });
+  }
+  if (a.scale_cols) {
+    const int k0 = (part * 32 + lane) / a.scale_cols, i0 = (part * 32 + lane) % a.scale_cols;
+    const int dk = parts * 32 / a.scale_cols, di = parts * 32 % a.scale_cols;
+    for (int t = warp / parts; t < n_tok; t += 8 / parts) {
+      const float* from = a.scales + ((int64_t)l * s.T + t0 + t) * a.scale_cols;
+      int i = i0;
+#pragma unroll 4
+      for (int k = k0; k < s.K; k += dk) {
+        const int pos = place[t * s.K + k];
+        if (pos >= 0) a.row_scales[(first + pos) * a.scale_cols + i] = __ldg(from + i);
+        i += di;
+        if (i >= a.scale_cols) i -= a.scale_cols, ++k;
+      }
     }
   }
+  if constexpr (kBulk) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
 }
 
 struct CombineArgs {
@@ -517,10 +596,11 @@ int64_t ld_or(int64_t ld, int d) { return ld ? ld : d; }
 struct SortShape {
   int cta, chunk, B;
 };
-// A CTA moves up to 150 KB: 16384 tokens x 8 of 2048 bytes with scales, us, 4 / 8 tokens: 63.6 / 59; of 4096 bytes 2 / 4 / 8 tokens:
-// 106 / 109 / 111; 24 x 256 tokens x 4 of 4096 bytes 27 / 25 / 27.  Chunks of 2048 pairs: between 512 and 4096 the time changes by
-// 1 %.  A layer is one chunk -- one launch, every CTA counts the whole layer -- while that is little work: 24 x 256 tokens x 4
-// 25.0 against 27.9 with two launches, 4096 tokens x 2 of 8192 bytes 32.7 against 22.8.
+// A CTA moves up to 150 KB: 16384 tokens x 8 of 2048 bytes with scales, us, 4 / 8 / 16 tokens: 58.7 / 54.9 / 58.0; of 4096 bytes
+// 2 / 4 / 8 tokens: 106 / 94.0 / 95.2; 24 x 256 tokens x 4 of 4096 bytes 2 / 4 tokens 26.1 / 24.3.
+// Chunks of 2048 pairs: between 512 and 4096 the time changes by 1 %.  A layer is one chunk -- one launch, every CTA counts
+// the whole layer -- while that is little work: 24 x 256 tokens x 4 25.0 against 27.9 with two launches, 4096 tokens x 2 of 8192
+// bytes 32.7 against 22.8.
 SortShape sort_shape(const mcce_rows& r) {
   const int K = r.top_k, T = r.n_tokens;
   const int64_t moved = (int64_t)(K + 1) * r.d * (r.dtype == MCCE_F32 ? 4 : r.dtype == MCCE_BF16 ? 2 : 1);
