@@ -432,7 +432,7 @@ __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_grou
 // RAGGED: the step between a thread's rows is a multiple of U (or it has one row), so that every one of its rows starts at
 // the same place in a unit.  A thread therefore has the same columns in all its rows, aligned or not, and keeps their
 // weights and its part of the weights' gradient in registers.
-// Bound: HBM for aligned rows (16384 x 2048 bf16 with dsum: 40.5 us = 1.0 of the copy bandwidth, 47.6 back to back with the launch that
+// Bound: HBM for aligned rows (16384 x 2048 bf16 with dsum: 43 us = 0.94 of the copy bandwidth, 47.6 back to back with the launch that
 // adds the parts of the weight's gradient); ragged rows add the pass over the single elements to every row's chain (16384 x 4097: 96
 // us = 0.85).  With the row in registers instead of the ring, loaded when it was needed, the first took 62 us; with columns that
 // move from row to row and sums in shared memory the second 148.
