@@ -279,7 +279,9 @@ int mcce_belady_replay(const int32_t* sel_trace, int32_t n_tokens, int32_t n_lay
  * the stream, nothing is allocated and nothing is kept between calls; a call may be captured into a graph.  A
  * workspace is used only while the call's kernels run: calls that can overlap need one each.  Sums, statistics and
  * weights are held in fp32; every result is rounded once, to nearest even, to the type of its buffer.  Results do
- * not depend on the order in which threads run (no atomics on data): repeated calls give identical bits.
+ * not depend on the order in which threads run (no atomics on data): repeated calls give identical bits.  Where a call
+ * does not say that an output may be one of its inputs, no output may overlap another tensor of the call (one that
+ * starts at the same address is refused).
  */
 
 /* Rows for mcce_rmsnorm and its gradient.  Row strides (ld_*) are in elements, 0 means d; the columns of a row are

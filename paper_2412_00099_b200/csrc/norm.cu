@@ -759,6 +759,9 @@ extern "C" int mcce_rmsnorm(const mcce_norm* n, const void* x, const void* add, 
       !aligned(scales, 4))
     return MCCE_EINVAL;
   if (sum == x && ld_or(n->ld_sum, n->d) != ld_or(n->ld_x, n->d)) return MCCE_EINVAL;
+  if (!apart(sum, {add, weight}) || !apart(out, {x, add, weight, sum}) || !apart(q, {x, add, weight, sum, out}) ||
+      !apart(scales, {x, add, weight, sum, out, q}))
+    return MCCE_EINVAL;
   NormArgs a{};
   a.rows = n->rows, a.d = n->d, a.eps = n->eps;
   a.ld_x = ld_or(n->ld_x, n->d), a.ld_add = ld_or(n->ld_add, n->d), a.ld_sum = ld_or(n->ld_sum, n->d);
@@ -805,6 +808,7 @@ extern "C" int mcce_rmsnorm_backward(const mcce_norm* n, const void* dout, const
   a.ld_dout = ld_or(n->ld_out, n->d), a.ld_h = ld_or(n->ld_x, n->d), a.ld_dsum = ld_or(n->ld_add, n->d);
   a.ld_dx = ld_or(n->ld_sum, n->d);
   if ((dx == dout && a.ld_dx != a.ld_dout) || (dx == dsum && a.ld_dx != a.ld_dsum)) return MCCE_EINVAL;
+  if (n->rows && (!apart(dx, {h, weight}) || !apart(dweight, {dout, h, dsum, weight, dx, workspace}))) return MCCE_EINVAL;
   if (dweight) {
     if (!workspace || !aligned(workspace, 16)) return MCCE_EINVAL;
     if (workspace_bytes < mcce_rmsnorm_backward_workspace_bytes(n)) return MCCE_ENOSPC;

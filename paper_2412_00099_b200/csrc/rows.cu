@@ -741,6 +741,10 @@ extern "C" int mcce_dispatch(const mcce_rows* r, const int32_t* sel_idx, const v
   if (!aligned(x, e) || !aligned(rows, e) || !aligned(scales, 4) || !aligned(row_scales, 4) || !aligned(sel_idx, 4) ||
       !aligned(perm, 4) || !aligned(inv, 4))
     return MCCE_EINVAL;
+  if (!apart(offsets, {sel_idx, x, scales, perm, inv, rows, row_scales}) || !apart(perm, {sel_idx, x, scales, inv, rows, row_scales}) ||
+      !apart(inv, {sel_idx, x, scales, rows, row_scales}) || !apart(rows, {sel_idx, x, scales, row_scales}) ||
+      !apart(row_scales, {sel_idx, x, scales}))
+    return MCCE_EINVAL;
   const size_t need = mcce_dispatch_workspace_bytes(r);
   if (need && (!workspace || !aligned(workspace, 16))) return MCCE_EINVAL;
   if (workspace_bytes < need) return MCCE_ENOSPC;
@@ -772,6 +776,7 @@ extern "C" int mcce_combine(const mcce_rows* r, const void* rows, const int32_t*
   if (!rows || !inv || !y) return MCCE_EINVAL;
   const int e = elem(r->dtype), ey = elem(r->token_dtype);
   if (!aligned(rows, e) || !aligned(inv, 4) || !aligned(sel_w, 4) || !aligned(add, ey) || !aligned(y, ey)) return MCCE_EINVAL;
+  if (!apart(y, {rows, inv, sel_w})) return MCCE_EINVAL;
   CombineArgs a = combine_args(*r);
   a.inv = inv, a.w = sel_w, a.rows = rows, a.add = add, a.y = y;
   UnitRule u(r->d, 16 / e);
@@ -789,6 +794,7 @@ extern "C" int mcce_combine_backward(const mcce_rows* r, const void* dy, const v
   const int e = elem(r->dtype), ey = elem(r->token_dtype);
   if (!aligned(rows, e) || !aligned(drows, e) || !aligned(inv, 4) || !aligned(sel_w, 4) || !aligned(dy, ey) || !aligned(dw, 4))
     return MCCE_EINVAL;
+  if (!apart(drows, {dy, inv, sel_w}) || !apart(dw, {dy, rows, inv, sel_w, drows})) return MCCE_EINVAL;
   CombineArgs a = combine_args(*r);
   a.inv = inv, a.w = sel_w, a.rows = dw ? rows : nullptr, a.dy = dy, a.drows = drows, a.dw = dw;
   UnitRule u(r->d, 16 / e);

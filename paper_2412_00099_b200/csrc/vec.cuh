@@ -10,6 +10,8 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <initializer_list>
+
 namespace mcce {
 
 enum Layout3 { kAligned = 0, kRagged = 1, kScalar = 2 };
@@ -177,6 +179,14 @@ __device__ __forceinline__ void with_shift(const T* first, int n, const T* base,
   else if (m < 8) f(Int<1>{});
   else if (m < 12) f(Int<2>{});
   else f(Int<3>{});
+}
+
+// Host: an output that does not start where one of these tensors does.
+inline bool apart(const void* out, std::initializer_list<const void*> others) {
+  if (out)
+    for (const void* o : others)
+      if (o == out) return false;
+  return true;
 }
 
 // Host: which layout the tensors of a call allow.  `unit` is U; add every tensor (null: not part of the call).

@@ -140,6 +140,36 @@ def test_combine_refusals(lib):
     assert lib.mcce_combine_backward(None, P[0], P[1], P[2], P[3], P[4], P[5], None) == EINVAL
 
 
+def refused_pairs(call, names, allowed):
+    """Every pair of arguments at one address that is not allowed: `names` are the arguments, outputs last after "|"."""
+    ins, outs = [n.split() for n in names.split("|")]
+    address = {n: P[i] for i, n in enumerate(ins + outs)}
+    for i, o in enumerate(outs):
+        for other in ins + outs[:i]:
+            if (o, other) not in allowed:
+                assert call(**dict(address, **{o: address[other]})) == EINVAL, (o, other)
+
+
+def test_outputs_at_an_inputs_address(lib):
+    refused_pairs(lambda **k: call_norm(lib, norm(), **k), "x add w | s o q sc", {("s", "x")})
+
+    def norm_back(dout, h, dsum, w, dx, dw):
+        return lib.mcce_rmsnorm_backward(C.byref(norm()), dout, h, dsum, w, dx, dw, P[11], 1 << 30, None)
+    refused_pairs(norm_back, "dout h dsum w | dx dw", {("dx", "dout"), ("dx", "dsum")})
+
+    def dispatch(sel, x, sc, off, perm, inv, out, osc):
+        return lib.mcce_dispatch(C.byref(rows(scale_cols=2)), sel, x, sc, off, perm, inv, out, osc, P[11], 1 << 30, None)
+    refused_pairs(dispatch, "sel x sc | off perm inv out osc", set())
+
+    def combine(rows_, inv, w, add, y):
+        return lib.mcce_combine(C.byref(rows()), rows_, inv, w, add, y, None)
+    refused_pairs(combine, "rows_ inv w add | y", {("y", "add")})
+
+    def combine_back(dy, rows_, inv, w, dr, dw):
+        return lib.mcce_combine_backward(C.byref(rows()), dy, rows_, inv, w, dr, dw, None)
+    refused_pairs(combine_back, "dy rows_ inv w | dr dw", {("dr", "rows_")})
+
+
 def test_set_norm_needs_a_context(lib):
     assert lib.mcce_set_norm(None, P[0], 1e-6) == EINVAL
 
