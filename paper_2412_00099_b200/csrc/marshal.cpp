@@ -112,6 +112,12 @@ at::Tensor workspace(size_t bytes, const at::Tensor& like) {
   return at::empty({(int64_t)bytes}, like.options().dtype(at::kByte));
 }
 
+// A call writes its results behind torch's back: count them as changed, so that a backward pass that saved one of them says so.
+void changed(std::initializer_list<const at::Tensor*> results) {
+  for (const at::Tensor* t : results)
+    if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+
 // rmsnorm(x, weight, eps, add, quant_group, out, sum, q, scales)
 void run_rmsnorm(PyObject* const* a) {
   const at::Tensor &x = given(a[0], "x"), &w = given(a[1], "weight");
@@ -146,6 +152,7 @@ void run_rmsnorm(PyObject* const* a) {
   n.ld_sum = ld(sum, shape, dev, "sum"), n.ld_out = ld(out, shape, dev, "out");
   Where on(dev);
   done(p_rmsnorm(&n, x.data_ptr(), at_(add), w.data_ptr(), at_(sum), at_(out), at_(q), (float*)at_(scales), on.stream));
+  changed({sum, out, q, scales});
 }
 
 // rmsnorm_backward(dout, h, weight, eps, dsum, dx, dweight)
@@ -173,6 +180,7 @@ void run_rmsnorm_backward(PyObject* const* a) {
   if (bytes) ws = workspace(bytes, h);
   done(p_rmsnorm_backward(&n, g.data_ptr(), h.data_ptr(), at_(ds), w.data_ptr(), dx.data_ptr(), (float*)at_(dw),
                           bytes ? ws.data_ptr() : nullptr, bytes, on.stream));
+  changed({&dx, dw});
 }
 
 // Leading sizes of [(L,)T,K]
@@ -232,6 +240,7 @@ void run_dispatch(PyObject* const* a) {
   done(p_dispatch(&r, (const int32_t*)sel.data_ptr(), at_(x), move_scales ? (const float*)sc->data_ptr() : nullptr,
                   (int32_t*)off.data_ptr(), (int32_t*)at_(perm), (int32_t*)inv.data_ptr(), at_(rows),
                   move_scales ? (float*)osc->data_ptr() : nullptr, bytes ? ws.data_ptr() : nullptr, bytes, on.stream));
+  changed({&off, perm, &inv, rows, osc});
 }
 
 mcce_rows pairs(const Lead& n, const at::Tensor& rows, const at::Tensor& token) {
@@ -257,6 +266,7 @@ void run_combine(PyObject* const* a) {
        "add must have the type and the row stride of out");
   Where on(dev);
   done(p_combine(&r, rows.data_ptr(), (const int32_t*)inv.data_ptr(), (const float*)at_(w), at_(add), y.data_ptr(), on.stream));
+  changed({&y});
 }
 
 // combine_backward(dy, rows, inv, sel_w, drows, dw)
@@ -276,6 +286,7 @@ void run_combine_backward(PyObject* const* a) {
   Where on(dev);
   done(p_combine_backward(&r, dy.data_ptr(), rows.data_ptr(), (const int32_t*)inv.data_ptr(), (const float*)at_(w), dr.data_ptr(),
                           (float*)at_(dw), on.stream));
+  changed({&dr, dw});
 }
 
 template <void (*RUN)(PyObject* const*), int N>

@@ -282,6 +282,21 @@ def test_dispatch(L, T, K, E, d, masked):
     assert np.array_equal(alone.offsets.cpu().numpy(), off) and np.array_equal(alone.inv.cpu().numpy(), inv) and alone.rows is None
 
 
+@pytest.mark.parametrize("L,T,K,E,d,T_,cols", [(1, 70, 1, 4, 8192, F32, 100), (2, 33, 3, 9, 6152, BF16, 33), (1, 41, 16, 20, 1040, torch.float8_e4m3fn, 1),
+                                               (1, 9, 2, 3, 60000, BF16, 7), (1, 600, 5, 11, 4112, F32, 64), (1, 3, 4, 4, 2064, BF16, 300)])
+def test_dispatch_rows_of_many_pieces(L, T, K, E, d, T_, cols):
+    """Rows that a warp moves in several pieces, the last one short; scale rows narrower and wider than a warp."""
+    g = gen(d)
+    sel = routing(g, L, T, K, E, 0.2)
+    off, perm, _ = sorted_by_hand(sel, E)
+    x, scales = normal(g, L, T, d, dtype=T_), torch.rand(L, T, cols, device="cuda", generator=g)
+    r = mb.dispatch(sel, E, x, scales=scales)
+    for l in range(L):
+        n = off[l, E]
+        p = torch.from_numpy(perm[l, :n]).long().cuda() // K
+        assert torch.equal(r.rows[l, :n].view(torch.uint8), x[l].view(torch.uint8)[p]) and torch.equal(r.scales[l, :n], scales[l][p])
+
+
 def test_dispatch_unusual_ids_and_layout():
     """The same expert twice for a token, ids outside [0, E) of every kind, one layer without the leading size, rows
     further apart than their width, no perm wanted, no tokens."""
@@ -549,6 +564,23 @@ def test_streams_and_graphs(T, d):
                 gr.replay()
     torch.cuda.synchronize()
     assert same(graphs[0][2], want[2]) and same(graphs[1][2], want[1])
+
+
+def test_results_count_as_changed():
+    """A tensor that a backward pass has saved and a call then overwrites: the backward pass refuses."""
+    x, w = torch.ones(4, 64, device="cuda"), torch.ones(64, device="cuda")
+    leaf = torch.ones(4, 64, device="cuda", requires_grad=True)
+    loss = (leaf * x).sum()
+    mb.rmsnorm(x, w, add=x.clone(), out=mb.NormOut(sum=x))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    versions = dx._version, dw._version
+    mb.rmsnorm_backward(x, x, w, out=(dx, dw))
+    assert dx._version > versions[0] and dw._version > versions[1]
+    with torch.inference_mode():
+        y = mb.rmsnorm(torch.ones(4, 64, device="cuda"), w).out
+    assert torch.isfinite(y).all()
 
 
 def test_binding_refuses_what_does_not_fit():
