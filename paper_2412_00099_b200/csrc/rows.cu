@@ -99,7 +99,7 @@ __device__ __forceinline__ void move_row(const CopyArgs& a, int64_t t, int64_t f
 
 // Rows of 16-byte units go through shared memory in pieces of kPiece units: fetched by cp.async, which needs no registers and so
 // starts before the counting, and written by one bulk copy per pair, issued by as many lanes at once.  Against loads into registers
-// and stores of 16 bytes per lane, us: 16384 x 8 rows of 2048 bytes with scales 55.0 / 58, of 4096 bytes 94.5 / 99; 24 x 256
+// and stores of 16 bytes per lane, us: 16384 x 8, a tenth of the pairs dropped, rows of 2048 bytes with scales 55.0 / 58, of 4096 bytes 94.5 / 99; 24 x 256
 // tokens x 4 of 4096 bytes 24.4 / 24.8; 20000 x 8 of 1024 bytes 48.0 / 46.7 (half of a piece's lanes idle).  Pieces of 64 units, three
 // per warp: 56.2, 95.0, 24.2 and 46.1.
 constexpr int kPiece = 128, kRing = 2;
@@ -127,8 +127,8 @@ struct Pieces {
 // its expert in earlier chunks (both from the chunks' counts), earlier in its chunk (counted here again), earlier in this
 // CTA.  A layer of few pairs is one chunk: the CTA counts all of it, and there is no launch before this one.
 // A pair's rank among its CTA's pairs comes from its warp's matches and the counts of the warps before.
-// Bound: HBM writes, once the counting is done: 16384 x 8 rows of 4096 bytes 94.5 us (0.89 of the copy bandwidth), of 2048 bytes with
-// scales 55 (0.79); about 8 us of each are the counting launch and the wait for the first CTAs' positions.  More CTAs per SM
+// Bound: HBM writes, once the counting is done: 16384 x 8, a tenth dropped, rows of 4096 bytes 94.5 us (0.89 of the copy bandwidth), of
+// 2048 bytes with scales 55 (0.79); about 8 us of each are the counting launch and the wait for the first CTAs' positions.  More CTAs per SM
 // at once are slower, not faster: 5 / 6 / 8 of them 99 / 101 / 115 with 4096 bytes (before the bulk copies).
 constexpr int kCtaPairs = 128;    // pairs of a CTA at most
 template <typename V>
@@ -313,6 +313,8 @@ __device__ __forceinline__ void add_scaled(float2 (&s)[(U + 1) / 2], const float
   }
 }
 
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(__cvta_generic_to_global(p))); }
+
 // y of a token: U columns (16 bytes of a row) at a time, VPT such units per lane and KC rows at once, so that KC * VPT loads are in flight.
 template <typename T, typename Y, int U, int KC, int VPT>
 __global__ void __launch_bounds__(256) combine_rows_kernel(const __grid_constant__ CombineArgs a) {
@@ -329,6 +331,13 @@ __global__ void __launch_bounds__(256) combine_rows_kernel(const __grid_constant
     for (int v = 0; v < VPT; ++v)
 #pragma unroll
       for (int j = 0; j < N; ++j) s[v][j] = both(0.f);
+    // The sum's last term is loaded last (held meanwhile, it costs a CTA per SM), but asked for into L2 at once.  K = 6 with a tenth of
+    // the pairs dropped, us: not asked for 89.7, asked for 86.1, loaded here 95.3; K = 8: 108.4, 106.0, 119.1.  One row at a time: worse (K = 2 28.8, 36.5).
+    if constexpr (KC > 1) {
+#pragma unroll
+      for (int v = 0; v < VPT; ++v)
+        if (a.add && c0 + v * step < d) prefetch_l2((const Y*)a.add + at + c0 + v * step);
+    }
     for (int k0 = 0; k0 < a.K; k0 += KC) {
       Pack<T, U> p[KC][VPT];
       float w[KC];
@@ -596,7 +605,7 @@ int64_t ld_or(int64_t ld, int d) { return ld ? ld : d; }
 struct SortShape {
   int cta, chunk, B;
 };
-// A CTA moves up to 150 KB: 16384 tokens x 8 of 2048 bytes with scales, us, 4 / 8 / 16 tokens: 58.7 / 54.9 / 58.0; of 4096 bytes
+// A CTA moves up to 150 KB: 16384 tokens x 8, a tenth of the pairs dropped, of 2048 bytes with scales, us, 4 / 8 / 16 tokens: 58.7 / 54.9 / 58.0; of 4096 bytes
 // 2 / 4 / 8 tokens: 106 / 94.0 / 95.2; 24 x 256 tokens x 4 of 4096 bytes 2 / 4 tokens 26.1 / 24.3.
 // Chunks of 2048 pairs: between 512 and 4096 the time changes by 1 %.  A layer is one chunk -- one launch, every CTA counts
 // the whole layer -- while that is little work: 24 x 256 tokens x 4 25.0 against 27.9 with two launches, 4096 tokens x 2 of 8192
@@ -645,8 +654,8 @@ cudaError_t launch_tokens(K kernel, const CombineArgs& a, cudaStream_t st) {
 bool few(const CombineArgs& a) { return a.tokens * 64 < 148 * 1024; }
 
 // KC rows at once x VPT units at once, us measured back to back on rotating buffers (16384 tokens of 2048 bf16 columns unless
-// noted).  Return, K = 8: 4 x 1 with 2 warps per token 96.4 (0.96 of the copy bandwidth), 8 x 1 104, 2 x 2 133; K = 6 with add: 4 x 1 92.4, 3 x
-// 1 92.3, 1 x 2 94.1; K = 2, 4099 tokens of 4096: 1 x 2 22.1 (0.69), 2 x 2 22.7, 4 x 1 24.8; K = 1 of 4096: 1 x 4 45.2 (0.91); 256
+// noted).  Return, K = 8: 4 x 1 with 2 warps per token 96.4 (0.96 of the copy bandwidth), 8 x 1 104, 2 x 2 133; K = 6 with add (before it was asked for early): 4 x 1
+// 92.4, 3 x 1 92.3, 1 x 2 94.1; K = 2, 4099 tokens of 4096: 1 x 2 22.1 (0.69), 2 x 2 22.7, 4 x 1 24.8; K = 1 of 4096: 1 x 4 45.2 (0.91); 256
 // tokens, K = 8: 4 x 1 with 8 warps 4.2, 4 x 2 4.7.  Gradient, K = 8: 1 x 4 with 2 warps 179 (0.97), 2 x 2 181, 4 x 1 191; K = 1 of 4096: 1 x 4
 // 63.6 (0.97); 256 tokens, K = 8: 4 x 1 with 8 warps 6.3, 2 x 2 8.3.
 // Units of one bf16: 8192 tokens of 1411, K = 8, return 4 x 8 with 2 warps 53 (0.60), 4 x 4 57, 1 x 8 62; of 4097, K = 2: 2 x 8 50 (0.62), 1 x 8 53;
