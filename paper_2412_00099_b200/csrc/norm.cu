@@ -682,13 +682,14 @@ GradShape grad_shape(int64_t rows, int d, Layout3 lay, int elem_bytes, bool dsum
   // 12 to 16 warps per SM with about 72 to 108 KB of rows on their way.  CTAs per SM / stages, us (16384 rows with dsum,
   // weight's gradient included; the two figures of 2048: launches apart, back to back): 2048 bf16 4 / 2 49.3 and 47.6,
   // 3 / 3 50.2 and 47.3, 4 / 3 49.8 and 49.8, 6 / 3 54.9 and 56; 1024 bf16 6 / 3 27.0, 6 / 2 28.7, 8 / 3 29.6; 4096 bf16
-  // 2 / 2 85.5, 2 / 3 87.0; 4096 fp32 without dsum 1 / 3 122, 1 / 2 138; 1001 x 1411 fp32 2 / 2 11.3, 2 / 3 12.3.
+  // 2 / 2 85.5, 2 / 3 87.0; 4096 fp32 without dsum 1 / 3 122, 1 / 2 138; 1001 x 1411 fp32 2 / 2 11.4, 2 / 3 12.0
+  // (up to four turns of a CTA; other shapes of few rows show no difference).
   int per_sm = g.s.threads <= 64 ? 6 : g.s.threads >= 384 ? 1 : g.s.threads > 192 ? 2 : 512 / g.s.threads;
   // Two such CTAs that are left with one stage lose to one with two from 288 threads on (8192 x 9216 fp32 201 -> 155, 4096 x
   // 10000 bf16 100 -> 71), but not below (8192 x 5120 fp32 with dsum 130 against 124).
   if (g.s.threads > 256 && grad_smem(g.s, 2, d, ragged, dsum, dweight) > kGradSmemMost / 2) per_sm = 1;
   const size_t flying = grad_smem(g.s, 1, d, false, dsum, false) * per_sm;
-  g.stages = flying >= 48 * 1024 ? 2 : 3;
+  g.stages = flying >= 48 * 1024 || all <= 4 * per_sm * kSms ? 2 : 3;
   while (g.stages > 1 && grad_smem(g.s, g.stages, d, ragged, dsum, dweight) > kGradSmemMost / per_sm) --g.stages;
   g.smem = grad_smem(g.s, g.stages, d, ragged, dsum, dweight);
   int ctas = per_sm * kSms;
