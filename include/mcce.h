@@ -307,7 +307,8 @@ typedef struct {
  *   out DEVICE dtype [rows,d] out or NULL
  *   q   DEVICE e4m3 (one byte: 4 exponent bits, 3 mantissa bits, largest value 448) [rows,d] out or NULL
  *   scales DEVICE fp32 [rows, ceil(d / quant_group)] out, contiguous; given exactly when q is.  The last group of a
- *       row may be shorter.  q_j * scales_G is within 2^-4 |n_j| (or half a subnormal step) of n_j.
+ *       row may be shorter.  q_j * scales_G is within 2^-4 |n_j| (or half a subnormal step) of n_j.  The quotient is formed in fp32
+ *       as n_j * (448 / max), both operations rounded to nearest, from n_j in fp32.
  * One of sum, out and q at least.  Apart from sum == x no output may overlap another tensor of the call.  A row that holds a NaN is
  * NaN throughout; the sum of squares is formed in fp32, so one beyond 3.4e38 counts as infinite (r = 0) and squares
  * below 1e-45 as zero. */

@@ -65,9 +65,12 @@ struct NormArgs {
 
 // r of the norm (rsqrtf is within 2 units in the last place)
 __device__ __forceinline__ float inv_rms(float sum_sq, float inv_d, float eps) { return rsqrtf(fmaf(sum_sq, inv_d, eps)); }
-// scale of a group from the bits of its largest magnitude, and what its values are multiplied by
-__device__ __forceinline__ float scale_of(uint32_t amax) { return __uint_as_float(amax) * (1.f / kE4m3Max); }
-__device__ __forceinline__ float back_of(float scale) { return __fdividef(1.f, scale); }   // scale is in [2^-109, 2^120]
+// scale of a group from the bits of its largest magnitude, and what its values are multiplied by.  Both are one correctly rounded
+// division; the factor comes from the largest magnitude itself, not from the rounded scale, so a value is off by
+// two roundings before the one to 8 bits.  (An approximate reciprocal of a scale formed with a rounded 1 / 448 is off by up to 7, and
+// put two or three values in a million on the other side of an e4m3 tie.)
+__device__ __forceinline__ float scale_of(uint32_t amax) { return __fdiv_rn(__uint_as_float(amax), kE4m3Max); }
+__device__ __forceinline__ float back_of(uint32_t amax) { return __fdiv_rn(kE4m3Max, __uint_as_float(amax)); }
 
 __device__ __forceinline__ uint8_t e4m3(float v) { return __nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3); }
 template <int N>
@@ -212,8 +215,9 @@ __global__ void __launch_bounds__(512) rmsnorm_kernel(const __grid_constant__ No
 #pragma unroll
       for (int j = 0; j < U / 2; ++j) top = max(top, max(magnitude(n[j].x), magnitude(n[j].y)));
     }
-    const float sc = scale_of(row_max(top, a.tpr, buf_max)), back = back_of(sc);
-    if (d && th.t == 0) scales[0] = sc;
+    top = row_max(top, a.tpr, buf_max);
+    const float back = back_of(top);
+    if (d && th.t == 0) scales[0] = scale_of(top);
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       float2 n[U / 2];
@@ -224,8 +228,10 @@ __global__ void __launch_bounds__(512) rmsnorm_kernel(const __grid_constant__ No
     }
     if (ce >= 0) q[ce] = e4m3(ne * back);
   } else if (!RAGGED) {
-    // a group is a power of two of neighbouring lanes
-    const int lanes = (1 << a.group_log2) / U;
+    // A group is a power of two of neighbouring lanes, at least VPT of them: lane i does the two divisions for the group that the
+    // i-th units lie in.  In every lane, for every unit: 16384 x 4096 bf16 in groups of 32 100 us.
+    const int lanes = (1 << a.group_log2) / U, me = th.t & (lanes - 1);
+    uint32_t top = kAmaxFloor;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       float2 n[U / 2];
@@ -234,13 +240,19 @@ __global__ void __launch_bounds__(512) rmsnorm_kernel(const __grid_constant__ No
 #pragma unroll
       for (int j = 0; j < U / 2; ++j) m = max(m, max(magnitude(n[j].x), magnitude(n[j].y)));
       for (int o = lanes >> 1; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(kFull, m, o));
-      const float sc = scale_of(m), back = back_of(sc);
+      if (me == i) top = m;
+    }
+    const float back = back_of(top);
+    const int cg = c0 - me * U + me * step;   // first column of that group
+    if (me < VPT && cg < whole) scales[cg >> a.group_log2] = scale_of(top);
 #pragma unroll
-      for (int j = 0; j < U / 2; ++j) n[j] = mul2(n[j], both(back));
-      if (in[i]) {
-        store_e4m3(q + c0 + i * step, n);
-        if ((th.t & (lanes - 1)) == 0) scales[(c0 + i * step) >> a.group_log2] = sc;
-      }
+    for (int i = 0; i < VPT; ++i) {
+      float2 n[U / 2];
+      norm_unit(i, n);
+      const float b = __shfl_sync(kFull, back, ((int)threadIdx.x & 31 & ~(lanes - 1)) + i);
+#pragma unroll
+      for (int j = 0; j < U / 2; ++j) n[j] = mul2(n[j], both(b));
+      if (in[i]) store_e4m3(q + c0 + i * step, n);
     }
   } else {
     // a unit's columns may belong to two groups
@@ -264,19 +276,24 @@ __global__ void __launch_bounds__(512) rmsnorm_kernel(const __grid_constant__ No
     }
     __syncthreads();
     if (d)
-      for (int g = th.t; g < a.n_groups; g += a.tpr) scales[g] = scale_of(m[g]);
+      for (int g = th.t; g < a.n_groups; g += a.tpr) {
+        const uint32_t top = m[g];
+        scales[g] = scale_of(top);
+        m[g] = __float_as_uint(back_of(top));   // only this thread looks at it before the barrier
+      }
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       if (!in[i]) continue;
       float2 n[U / 2];
       norm_unit(i, n);
       const int c = head + c0 + i * step, g = c >> a.group_log2, cut = ((g + 1) << a.group_log2) - c;
-      const float b0 = back_of(scale_of(m[g])), b1 = cut < U ? back_of(scale_of(m[g + 1])) : b0;
+      const float b0 = __uint_as_float(m[g]), b1 = cut < U ? __uint_as_float(m[g + 1]) : b0;
 #pragma unroll
       for (int j = 0; j < U / 2; ++j) n[j] = mul2(n[j], make_float2(2 * j < cut ? b0 : b1, 2 * j + 1 < cut ? b0 : b1));
       store_e4m3(q + c, n);
     }
-    if (ce >= 0) q[ce] = e4m3(ne * back_of(scale_of(m[ce >> a.group_log2])));
+    if (ce >= 0) q[ce] = e4m3(ne * __uint_as_float(m[ce >> a.group_log2]));
   }
 }
 
@@ -318,9 +335,14 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_scalar_kernel(const __grid_c
   }
   if (!a.q) return;
   __syncthreads();
-  for (int g = threadIdx.x; g < a.n_groups; g += kThreads) a.scales[r * a.n_groups + g] = scale_of(amax[g]);
+  for (int g = threadIdx.x; g < a.n_groups; g += kThreads) {
+    const uint32_t top = amax[g];
+    a.scales[r * a.n_groups + g] = scale_of(top);
+    amax[g] = __float_as_uint(back_of(top));
+  }
+  __syncthreads();
   for (int j = threadIdx.x; j < a.d; j += kThreads)
-    a.q[r * a.ld_q + j] = e4m3(n_at(j) * back_of(scale_of(amax[j >> a.group_log2])));
+    a.q[r * a.ld_q + j] = e4m3(n_at(j) * __uint_as_float(amax[j >> a.group_log2]));
 }
 
 // How a row is laid over threads: `vpt` units for each of tpr threads.

@@ -145,6 +145,38 @@ def test_norm_small_large_and_special_rows():
         assert e.out.shape == (0, 8) and e.scales.shape == (0, 1)
 
 
+@pytest.mark.parametrize("d", [128, 4096, 1411, 16384])
+@pytest.mark.parametrize("T", [BF16, F32])
+@pytest.mark.parametrize("alike", [True, False])
+@pytest.mark.parametrize("group", [0, 32, 64, 128])
+def test_norm_to_8_bits_rounds_the_quotient(d, T, alike, group):
+    """q is the e4m3 rounding of n / scale.  With x = 1, eps = 0 (r = 1) n is the weight itself, so what stays between n and q is the
+    division that forms a group's factor and the multiplication by it: 2 u.  The weights lie a few u off the e4m3 ties of their
+    group, whose largest values are arbitrary."""
+    R, g = 3, gen(d + group)
+    cols = -(-d // group) if group else 1
+    top = 1 + torch.rand(cols, device="cuda", generator=g)
+    top = top.repeat_interleave(group or d)[:d]
+    tie = torch.randint(8, 16, (d,), device="cuda", generator=g).double() + 0.5        # halfway between two of 4 significant bits
+    tie = tie * 2.0 ** torch.randint(-2, 5, (d,), device="cuda", generator=g).double()
+    off = 1 + u * (torch.rand(d, device="cuda", generator=g).double() * 12 - 6)
+    w = (tie * off * top.double() / 448.0).float()
+    first = torch.arange(0, d, group or d, device="cuda")
+    w[first] = top[first]
+    x = torch.ones(R, d + 1, device="cuda", dtype=T)
+    x = x[:, :d].contiguous() if alike else x[:, 1:]
+    out = mb.NormOut(None, None, torch.empty(R, d, device="cuda", dtype=torch.float8_e4m3fn), torch.empty(R, cols, device="cuda"))
+    assert torch.equal(mb.rmsnorm(x, w, 0.0).out[0], w.to(T))        # r = 1
+    r = mb.rmsnorm(x, w, 0.0, quant_group=group, out=out)
+    v = w.double() * 448.0 / top.double()
+    lo, hi = e4m3(v - v.abs() * 2.01 * u), e4m3(v + v.abs() * 2.01 * u)
+    q = r.q.double()
+    bad = (q < lo) | (q > hi)
+    assert not bad.any(), "%d of %d" % (int(bad.sum()), bad.numel())
+    scale = (top.double() / 448.0)[first]
+    within(r.scales, scale.expand(R, cols), scale * 1.01 * u, "scales")
+
+
 def check_gradient(g, h, w, eps, ds, dx, dw):
     """dx and dweight against the formulas in 64 bits."""
     R = h.shape[0]
