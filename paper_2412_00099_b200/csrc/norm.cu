@@ -413,6 +413,11 @@ struct NormGradArgs {
   float* part;   // [CTAs, d], or null: the weight's gradient is not wanted
 };
 
+// dx = r g + (h r) c + dsum with c = -r^2 mean(h g), for the vector and the scalar kernel alike.  The mean takes in one r at a time: it is
+// at most as large as rms(h) rms(g), so every product on the way lies between the mean, rms(g) and c, in fp32's range where r^2 or
+// r^3 alone are not.
+__device__ __forceinline__ float grad_coef(float inv, float mean_hg) { return -(inv * (inv * mean_hg)); }
+
 // Both sums at once: the lower half of a group of lanes ends up with x, the upper half with y.
 __device__ __forceinline__ float half_sum2(float2 v, int lanes) {
   const bool upper = threadIdx.x & (lanes >> 1);
@@ -556,8 +561,7 @@ __global__ void __launch_bounds__(512) rmsnorm_grad_kernel(const __grid_constant
     }
     sum.x += hh.x + hh.y, sum.y += hg.x + hg.y;
     sum = row_sum2(sum, a.tpr, buf[par]);
-    // dx = r g - (h r) (r^2 mean(h g)) + dsum
-    const float inv = r < a.rows ? inv_rms(sum.x, a.inv_d, a.eps) : 0.f, coef = -inv * inv * (sum.y * a.inv_d);
+    const float inv = r < a.rows ? inv_rms(sum.x, a.inv_d, a.eps) : 0.f, coef = grad_coef(inv, sum.y * a.inv_d);
     T* xr = (T*)a.dx + r * a.ld_dx + head;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
@@ -632,12 +636,11 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_grad_scalar_kernel(const __g
       s.y = fmaf(hj, wide(g[j]) * get1<T>(a.weight, j, a.weight_f32), s.y);
     }
     s = row_sum2(s, kThreads, buf[par]);
-    const float inv = inv_rms(s.x, a.inv_d, a.eps), coef = inv * inv * inv * (s.y * a.inv_d);
+    const float inv = inv_rms(s.x, a.inv_d, a.eps), coef = grad_coef(inv, s.y * a.inv_d);
     for (int j = threadIdx.x; j < a.d; j += kThreads) {
       const float hj = wide(h[j]), gj = wide(g[j]);
-      float v = fmaf(inv, gj * get1<T>(a.weight, j, a.weight_f32), -hj * coef);
-      if (a.dsum) v += wide(((const T*)a.dsum)[r * a.ld_dsum + j]);
-      ((T*)a.dx)[r * a.ld_dx + j] = narrow<T>(v);
+      const float past = a.dsum ? wide(((const T*)a.dsum)[r * a.ld_dsum + j]) : 0.f;
+      ((T*)a.dx)[r * a.ld_dx + j] = narrow<T>(fmaf(gj * get1<T>(a.weight, j, a.weight_f32), inv, fmaf(hj * inv, coef, past)));
       if (part) part[j] = fmaf(gj, hj * inv, part[j]);
     }
   }

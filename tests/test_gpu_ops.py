@@ -214,6 +214,23 @@ def test_norm_gradient(R, d, T, W, with_dsum):
             assert torch.equal(mb.rmsnorm_backward(a[0], h, w, eps, dsum=a[1], out=(target, None))[0], dx)
 
 
+@pytest.mark.parametrize("T", [BF16, F32])
+@pytest.mark.parametrize("d,layout", [(64, "aligned"), (61, "ragged"), (64, "unlike")])
+@pytest.mark.parametrize("rms", [1e18, 1e15, 1e13, 1e-13, 1e-15, 3e-20])
+def test_norm_gradient_of_large_and_small_rows(T, d, layout, rms):
+    """r^2 and r^3 leave the range of fp32, the products that they stand in do not.  (The smallest squares are subnormal: each
+    rounding of them and of the mean is off by 2^-150, 13 u of their sum together, which NORM_U's room covers.)"""
+    gn, R = gen(d), 40
+    pad = 1 if layout == "unlike" else 0
+    h, g, ds = normal(gn, R, d + pad)[:, pad:], normal(gn, R, d, dtype=T), normal(gn, R, d, dtype=T) / rms
+    h = (h * rms).to(T)
+    if pad:
+        h = torch.cat([h, h], 1)[:, pad:d + pad]
+    w = 1 + 0.2 * normal(gn, d)
+    check_gradient(g, h, w, 0.0, None, *mb.rmsnorm_backward(g, h, w, 0.0))
+    check_gradient(g, h, w, 0.0, ds, *mb.rmsnorm_backward(g, h, w, 0.0, dsum=ds))
+
+
 def test_norm_gradient_against_differences():
     """<gradient, direction> against central differences of the definition in 64 bits (truncation ~1e-10)."""
     R, d, eps = 7, 96, 1e-5
