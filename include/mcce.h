@@ -126,7 +126,8 @@ int mcce_set_experts(mcce_ctx* ctx, const void* Wg, const void* Wu, const void* 
                      const void* shWu, const void* shWd);
 
 /* Root-mean-square norm in front of every layer's router and experts in mcce_decode_step_chained (mcce_rmsnorm's
- * formulas).  weight: DEVICE fp32 [L,d], 16-byte aligned, borrowed; eps finite, >= 0.  NULL: no norm (the state after mcce_create). */
+ * formulas).  weight: DEVICE fp32 [L,d], 16-byte aligned, borrowed; eps finite, >= 0; d at most
+ * MCCE_NORM_MAX_D.  NULL: no norm (the state after mcce_create). */
 int mcce_set_norm(mcce_ctx* ctx, const float* weight, float eps);
 
 /* Empties every cache, or loads an initial cache content (Sec. 4.8 "Impact of Initial Cache State"):

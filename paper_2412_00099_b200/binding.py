@@ -200,10 +200,13 @@ class Engine:
         _check(self.lib.mcce_set_experts(self.ctx, *[_ptr(t) for t in (Wg, Wu, Wd, shWg, shWu, shWd)]), self.ctx)
 
     def set_norm(self, weight: torch.Tensor | None, eps: float = 1e-6):
-        """Root-mean-square norm in front of every layer of decode_step_chained: weight [L,d] fp32, None for no norm."""
+        """Root-mean-square norm in front of every layer of decode_step_chained: weight [L,d] fp32 on the engine's device, kept
+        with the engine like its other weights (steps under way may still read an earlier one); None for no norm."""
         assert weight is None or (weight.dtype == torch.float32 and tuple(weight.shape) == (self.L, self.d))
+        _need(weight is None or weight.device == self.device, "the norm's weight must be on %s" % self.device)
         _check(self.lib.mcce_set_norm(self.ctx, _ptr(weight), eps), self.ctx)
-        self._norm_weight = weight
+        if weight is not None and not any(t is weight for t in self._keep):
+            self._keep.append(weight)
 
     def reset(self, init_order: np.ndarray | None = None, keep_delta_stats=False, delta_sum=None, delta_count=0):
         if init_order is not None:

@@ -718,3 +718,18 @@ def test_chained_step_with_norms_equals_the_composition():
             full.set_norm(nw[:, :8])
         for e in [full, plain, *singles]:
             e.close()
+
+
+def test_norm_weights_live_as_long_as_the_engine():
+    """Steps under way read the weight that was set when they were queued: replacing it frees nothing."""
+    import weakref
+    from paper_2412_00099_b200 import synth
+    eng = mb.engine_for(synth.TINY)
+    weights = [torch.ones(synth.TINY.L, synth.TINY.d, device="cuda") for _ in range(2)]
+    alive = [weakref.ref(w) for w in weights]
+    for w in weights:
+        eng.set_norm(w)
+    eng.set_norm(None)
+    del weights, w
+    assert all(a() is not None for a in alive)
+    eng.close()

@@ -174,6 +174,25 @@ def test_set_norm_needs_a_context(lib):
     assert lib.mcce_set_norm(None, P[0], 1e-6) == EINVAL
 
 
+def test_set_norm_refuses_weights_that_are_not_on_its_device():
+    """The kernels would read the address: an error on the host instead, before the library hears of it."""
+    import torch
+    calls = []
+
+    class Lib:
+        def mcce_set_norm(self, *a):
+            calls.append(a)
+            return 0
+    eng = object.__new__(mb.Engine)
+    eng.L, eng.d, eng.device, eng.lib, eng.ctx, eng._keep = 2, 16, torch.device("cuda", 0), Lib(), C.c_void_p(), []
+    for weight in (torch.ones(2, 16), torch.ones(2, 16, device="meta")):
+        with pytest.raises(mb.McceError, match="cuda:0"):
+            eng.set_norm(weight)
+    assert not calls and not eng._keep
+    eng.set_norm(None)
+    assert len(calls) == 1
+
+
 def test_binding_refuses_cpu_tensors():
     import torch
     with pytest.raises(mb.McceError, match="no CPU path"):
