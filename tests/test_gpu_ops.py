@@ -733,3 +733,39 @@ def test_norm_weights_live_as_long_as_the_engine():
     del weights, w
     assert all(a() is not None for a in alive)
     eng.close()
+
+
+@pytest.mark.parametrize("S,d,n_shared", [(72, 256, 0), (130, 512, 1)])
+def test_chained_step_with_norms_on_the_tensor_path(S, d, n_shared):
+    """The normalised buffer as the tensor-core experts and the router GEMM read it, several layers and one: against single-layer
+    engines joined by the operators (deterministic contexts add in a fixed order: bit for bit)."""
+    from paper_2412_00099_b200 import synth
+    import helpers as H
+    for L in (3, 1):
+        wl = synth.QWEN.with_(L=L, S=S, E=12, K=4, C=6, d=d, I=256, n_shared=n_shared)
+        Wr, W = wl.router(), H.weights_for(wl)
+        Wd = {k: (None if v is None else H.to_dev(v)) for k, v in W.items()}
+
+        def engine(layers, wr, we):
+            e = mb.engine_for(wl.with_(L=layers), ffn_impl=mb.FFN_TENSOR, deterministic=True)
+            e.set_router(wr)
+            e.set_experts(**we)
+            assert e.uses_tensor_path()
+            return e
+        full = engine(L, H.to_dev(Wr), Wd)
+        singles = [engine(1, H.to_dev(Wr[l:l + 1]), {k: (None if v is None else v[l:l + 1].contiguous()) for k, v in Wd.items()})
+                   for l in range(L)]
+        nw = 1 + 0.3 * normal(gen(L), L, d)
+        full.set_norm(nw, 1e-5)
+        for x0 in [H.to_dev(x)[0] for x in wl.with_(L=1).hidden_trace(4)]:
+            x_c, sel_c = full.decode_step_chained(x0, want_sel=True)
+            x = x0
+            for l, e in enumerate(singles):
+                n = mb.rmsnorm(x, nw[l], 1e-5).out
+                sel, w = e.route_step(hidden=n[None, None])
+                y = e.moe_forward(n[None], sel[0], w[0])[0]
+                assert torch.equal(sel[0, 0], sel_c[l])
+                x = mb.rmsnorm(x, nw[l], 1e-5, add=y, want_out=False).sum
+            assert torch.equal(x, x_c)
+        for e in [full, *singles]:
+            e.close()
