@@ -281,8 +281,8 @@ int mcce_belady_replay(const int32_t* sel_trace, int32_t n_tokens, int32_t n_lay
  * workspace is used only while the call's kernels run: calls that can overlap need one each.  Sums, statistics and
  * weights are held in fp32; every result is rounded once, to nearest even, to the type of its buffer.  Results do
  * not depend on the order in which threads run (no atomics on data): repeated calls give identical bits.  Where a call
- * does not say that an output may be one of its inputs, no output may overlap another tensor of the call (one that
- * starts at the same address is refused).
+ * does not say that an output may be one of its inputs, no output and no workspace may share memory with another tensor of the
+ * call: refused, from the addresses, sizes and strides.  (Columns of one buffer, side by side, share none.)
  */
 
 /* Rows for mcce_rmsnorm and its gradient.  Row strides (ld_*) are in elements, 0 means d; the columns of a row are

@@ -765,7 +765,7 @@ bool norm_ok(const mcce_norm* n) {
 
 bool aligned(const void* p, size_t a) { return (uintptr_t)p % a == 0; }
 int elem(int dtype) { return dtype == MCCE_F32 ? 4 : 2; }
-int64_t ld_or(int64_t ld, int d) { return ld ? ld : d; }
+int64_t ld_or(int64_t ld, int64_t d) { return ld ? ld : d; }
 
 }  // namespace
 }  // namespace mcce
@@ -784,9 +784,13 @@ extern "C" int mcce_rmsnorm(const mcce_norm* n, const void* x, const void* add, 
   if (!aligned(x, e) || !aligned(sum, e) || !aligned(out, e) || !aligned(weight, ew) || (add && !aligned(add, ea)) ||
       !aligned(scales, 4))
     return MCCE_EINVAL;
-  if (sum == x && ld_or(n->ld_sum, n->d) != ld_or(n->ld_x, n->d)) return MCCE_EINVAL;
-  if (!apart(sum, {add, weight}) || !apart(out, {x, add, weight, sum}) || !apart(q, {x, add, weight, sum, out}) ||
-      !apart(scales, {x, add, weight, sum, out, q}))
+  const int64_t R = n->rows, d = n->d;
+  const Span sx = row_span(x, R, ld_or(n->ld_x, d), d, e), sadd = row_span(add, R, ld_or(n->ld_add, d), d, ea);
+  const Span sw = flat_span(weight, d * ew), ssum = row_span(sum, R, ld_or(n->ld_sum, d), d, e);
+  const Span sout = row_span(out, R, ld_or(n->ld_out, d), d, e), sq = row_span(q, R, ld_or(n->ld_q, d), d, 1);
+  const Span sscales = flat_span(scales, R * (g ? (d + g - 1) / g : 1), 4);
+  if (!same_or_apart(ssum, sx) || !apart(ssum, {&sadd, &sw}) || !apart(sout, {&sx, &sadd, &sw, &ssum}) ||
+      !apart(sq, {&sx, &sadd, &sw, &ssum, &sout}) || !apart(sscales, {&sx, &sadd, &sw, &ssum, &sout, &sq}))
     return MCCE_EINVAL;
   NormArgs a{};
   a.rows = n->rows, a.d = n->d, a.eps = n->eps;
@@ -833,12 +837,17 @@ extern "C" int mcce_rmsnorm_backward(const mcce_norm* n, const void* dout, const
   a.rows = n->rows, a.d = n->d, a.eps = n->eps, a.weight_f32 = n->weight_dtype == MCCE_F32, a.inv_d = 1.f / (float)n->d;
   a.ld_dout = ld_or(n->ld_out, n->d), a.ld_h = ld_or(n->ld_x, n->d), a.ld_dsum = ld_or(n->ld_add, n->d);
   a.ld_dx = ld_or(n->ld_sum, n->d);
-  if ((dx == dout && a.ld_dx != a.ld_dout) || (dx == dsum && a.ld_dx != a.ld_dsum)) return MCCE_EINVAL;
-  if (n->rows && (!apart(dx, {h, weight}) || !apart(dweight, {dout, h, dsum, weight, dx, workspace}))) return MCCE_EINVAL;
   if (dweight) {
     if (!workspace || !aligned(workspace, 16)) return MCCE_EINVAL;
     if (workspace_bytes < mcce_rmsnorm_backward_workspace_bytes(n)) return MCCE_ENOSPC;
   }
+  const int64_t R = n->rows, d = n->d;
+  const Span sg = row_span(dout, R, a.ld_dout, d, e), sh = row_span(h, R, a.ld_h, d, e), sds = row_span(dsum, R, a.ld_dsum, d, e);
+  const Span sw = flat_span(weight, d * elem(n->weight_dtype)), sdx = row_span(dx, R, a.ld_dx, d, e), sdw = flat_span(dweight, d * 4);
+  const Span sws = flat_span(dweight ? workspace : nullptr, mcce_rmsnorm_backward_workspace_bytes(n));
+  if (R && (!same_or_apart(sdx, sg) || !same_or_apart(sdx, sds) || !apart(sdx, {&sh, &sw}) || !apart(sdw, {&sg, &sh, &sds, &sw, &sdx}) ||
+            !apart(sws, {&sg, &sh, &sds, &sw, &sdx, &sdw})))
+    return MCCE_EINVAL;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   if (n->rows == 0)
     return !dweight || cudaMemsetAsync(dweight, 0, (size_t)n->d * 4, st) == cudaSuccess ? MCCE_OK : MCCE_ECUDA;

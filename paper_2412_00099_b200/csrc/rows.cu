@@ -750,13 +750,19 @@ extern "C" int mcce_dispatch(const mcce_rows* r, const int32_t* sel_idx, const v
   if (!aligned(x, e) || !aligned(rows, e) || !aligned(scales, 4) || !aligned(row_scales, 4) || !aligned(sel_idx, 4) ||
       !aligned(perm, 4) || !aligned(inv, 4))
     return MCCE_EINVAL;
-  if (!apart(offsets, {sel_idx, x, scales, perm, inv, rows, row_scales}) || !apart(perm, {sel_idx, x, scales, inv, rows, row_scales}) ||
-      !apart(inv, {sel_idx, x, scales, rows, row_scales}) || !apart(rows, {sel_idx, x, scales, row_scales}) ||
-      !apart(row_scales, {sel_idx, x, scales}))
-    return MCCE_EINVAL;
   const size_t need = mcce_dispatch_workspace_bytes(r);
   if (need && (!workspace || !aligned(workspace, 16))) return MCCE_EINVAL;
   if (workspace_bytes < need) return MCCE_ENOSPC;
+  const int64_t tokens = (int64_t)r->n_layers * r->n_tokens, pairs = tokens * r->top_k;
+  const Span ssel = flat_span(sel_idx, pairs * 4), sx = row_span(x, tokens, ld_or(r->ld_token, r->d), r->d, e);
+  const Span ssc = flat_span(scales, tokens, 4ll * r->scale_cols), soff = flat_span(offsets, (int64_t)r->n_layers * (r->n_experts + 1) * 4);
+  const Span sperm = flat_span(perm, pairs * 4), sinv = flat_span(inv, pairs * 4);
+  const Span srows = row_span(rows, pairs, ld_or(r->ld_rows, r->d), r->d, e), sosc = flat_span(row_scales, pairs, 4ll * r->scale_cols);
+  const Span sws = flat_span(need ? workspace : nullptr, need);
+  if (!apart(soff, {&ssel, &sx, &ssc, &sperm, &sinv, &srows, &sosc}) || !apart(sperm, {&ssel, &sx, &ssc, &sinv, &srows, &sosc}) ||
+      !apart(sinv, {&ssel, &sx, &ssc, &srows, &sosc}) || !apart(srows, {&ssel, &sx, &ssc, &sosc}) || !apart(sosc, {&ssel, &sx, &ssc}) ||
+      !apart(sws, {&ssel, &sx, &ssc, &soff, &sperm, &sinv, &srows, &sosc}))
+    return MCCE_EINVAL;
   const SortShape h = sort_shape(*r);
   SortArgs s;
   s.T = r->n_tokens, s.K = r->top_k, s.E = r->n_experts, s.P = s.T * s.K, s.chunk = h.chunk, s.B = h.B;
@@ -785,8 +791,11 @@ extern "C" int mcce_combine(const mcce_rows* r, const void* rows, const int32_t*
   if (!rows || !inv || !y) return MCCE_EINVAL;
   const int e = elem(r->dtype), ey = elem(r->token_dtype);
   if (!aligned(rows, e) || !aligned(inv, 4) || !aligned(sel_w, 4) || !aligned(add, ey) || !aligned(y, ey)) return MCCE_EINVAL;
-  if (!apart(y, {rows, inv, sel_w})) return MCCE_EINVAL;
   CombineArgs a = combine_args(*r);
+  const int64_t pairs = a.tokens * a.K;
+  const Span sy = row_span(y, a.tokens, a.ld_token, a.d, ey), sadd = row_span(add, a.tokens, a.ld_token, a.d, ey);
+  const Span srows = row_span(rows, pairs, a.ld_rows, a.d, e), sinv = flat_span(inv, pairs * 4), sw = flat_span(sel_w, pairs * 4);
+  if (!same_or_apart(sy, sadd) || !apart(sy, {&srows, &sinv, &sw})) return MCCE_EINVAL;
   a.inv = inv, a.w = sel_w, a.rows = rows, a.add = add, a.y = y;
   UnitRule u(r->d, 16 / e);
   u.tensor(rows, a.ld_rows, e);
@@ -803,8 +812,13 @@ extern "C" int mcce_combine_backward(const mcce_rows* r, const void* dy, const v
   const int e = elem(r->dtype), ey = elem(r->token_dtype);
   if (!aligned(rows, e) || !aligned(drows, e) || !aligned(inv, 4) || !aligned(sel_w, 4) || !aligned(dy, ey) || !aligned(dw, 4))
     return MCCE_EINVAL;
-  if (!apart(drows, {dy, inv, sel_w}) || !apart(dw, {dy, rows, inv, sel_w, drows})) return MCCE_EINVAL;
   CombineArgs a = combine_args(*r);
+  const int64_t pairs = a.tokens * a.K;
+  const Span sdy = row_span(dy, a.tokens, a.ld_token, a.d, ey), srows = row_span(dw ? rows : nullptr, pairs, a.ld_rows, a.d, e);
+  const Span sinv = flat_span(inv, pairs * 4), sw = flat_span(sel_w, pairs * 4), sdr = row_span(drows, pairs, a.ld_rows, a.d, e);
+  const Span sdw = flat_span(dw, pairs * 4);
+  if (!same_or_apart(sdr, srows) || !apart(sdr, {&sdy, &sinv, &sw}) || !apart(sdw, {&sdy, &srows, &sinv, &sw, &sdr}))
+    return MCCE_EINVAL;
   a.inv = inv, a.w = sel_w, a.rows = dw ? rows : nullptr, a.dy = dy, a.drows = drows, a.dw = dw;
   UnitRule u(r->d, 16 / e);
   u.tensor(a.rows, a.ld_rows, e);

@@ -10,7 +10,7 @@
 #include <stdint.h>
 #include <string.h>
 
-#include <initializer_list>
+#include "span.h"
 
 namespace mcce {
 
@@ -179,14 +179,6 @@ __device__ __forceinline__ void with_shift(const T* first, int n, const T* base,
   else if (m < 8) f(Int<1>{});
   else if (m < 12) f(Int<2>{});
   else f(Int<3>{});
-}
-
-// Host: an output that does not start where one of these tensors does.
-inline bool apart(const void* out, std::initializer_list<const void*> others) {
-  if (out)
-    for (const void* o : others)
-      if (o == out) return false;
-  return true;
 }
 
 // Host: which layout the tensors of a call allow.  `unit` is U; add every tensor (null: not part of the call).

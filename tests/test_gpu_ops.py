@@ -769,3 +769,39 @@ def test_chained_step_with_norms_on_the_tensor_path(S, d, n_shared):
             assert torch.equal(x, x_c)
         for e in [full, *singles]:
             e.close()
+
+
+def test_columns_of_one_buffer_and_overlaps():
+    """Tensors that are columns of one buffer share no memory and are taken; outputs that reach into an input are refused."""
+    g, R, d = gen(31), 21, 64
+    buf = normal(g, R, 4 * d, dtype=BF16)
+    x, add, w = buf[:, :d], buf[:, d:2 * d], 1 + 0.1 * normal(g, d)
+    want = mb.rmsnorm(x.clone(), w, 1e-6, add=add.clone())
+    r = mb.rmsnorm(x, w, 1e-6, add=add, out=mb.NormOut(buf[:, 2 * d:3 * d], buf[:, 3 * d:]))
+    assert torch.equal(r.out, want.out) and torch.equal(r.sum, want.sum)
+    dx, dw = mb.rmsnorm_backward(x.clone(), add.clone(), w, dsum=x.clone())
+    got = mb.rmsnorm_backward(x, add, w, dsum=x, out=(buf[:, 2 * d:3 * d], torch.empty_like(dw)))
+    assert torch.equal(got[0], dx) and torch.equal(got[1], dw)
+    with pytest.raises(mb.McceError):                # the sum one row late in x
+        mb.rmsnorm(x[:-1], w, 1e-6, add=add[:-1], out=mb.NormOut(None, x[1:]))
+    with pytest.raises(mb.McceError):
+        mb.rmsnorm(x[:8], w, 1e-6, out=mb.NormOut(buf[4:12, d // 2:d // 2 + d]))
+    T, K = 7, 3
+    rows, inv = buf[:, :d], torch.randperm(T * K, device="cuda", generator=g).to(torch.int32).view(T, K)
+    y = mb.combine(rows.clone(), inv)
+    got = mb.combine(rows, inv, out=buf[:T, d:2 * d])
+    assert torch.equal(got, y)
+    with pytest.raises(mb.McceError):
+        mb.combine(rows, inv, out=rows[2:2 + T])
+    dy = normal(g, T, d, dtype=BF16)
+    drows, dw = mb.combine_backward(dy, rows.clone(), inv)
+    got = mb.combine_backward(dy, rows, inv, out=(buf[:, 2 * d:3 * d], torch.empty_like(dw)))
+    assert torch.equal(got[0], drows) and torch.equal(got[1], dw)
+    sel = torch.randint(0, 4, (R, 1), device="cuda", generator=g).to(torch.int32)
+    want = mb.dispatch(sel, 4, rows.clone())
+    out = want._replace(rows=buf[:, d:2 * d])
+    assert torch.equal(mb.dispatch(sel, 4, rows, out=out).rows, mb.dispatch(sel, 4, rows.clone()).rows)
+    with pytest.raises(mb.McceError):
+        mb.dispatch(sel, 4, rows, out=want._replace(inv=want.perm.view(R, 1)))
+    with pytest.raises(mb.McceError):
+        mb.dispatch(sel, 4, rows, out=want._replace(rows=rows))

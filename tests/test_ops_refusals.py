@@ -170,6 +170,93 @@ def test_outputs_at_an_inputs_address(lib):
     refused_pairs(combine_back, "dy rows_ inv w | dr dw", {("dr", "rows_")})
 
 
+def at(p, nbytes):
+    return C.c_void_p(p.value + nbytes)
+
+
+def test_outputs_that_reach_into_another_tensor(lib):
+    """An output that starts one row into another tensor, or whose last row is another's first: refused like one at its address."""
+    n = norm()                                       # 4 rows of 64: x 512 bytes (bf16), add 1024 (fp32), weight 256, q 256, scales 32
+    row = dict(x=128, add=256, w=64, s=128, o=128, q=64, sc=8)
+    size = dict(x=512, add=1024, w=256, s=512, o=512, q=256, sc=32)
+    names = ["x", "add", "w", "s", "o", "q", "sc"]
+    for i, out in enumerate(names):
+        for other in names[:i]:
+            if i >= 3:
+                for place in (at(P[names.index(other)], size[other] - row[other]), at(P[names.index(other)], row[out] - size[out])):
+                    assert call_norm(lib, n, **{out: place}) == EINVAL, (out, other)
+    assert call_norm(lib, norm(rows=2, ld_x=256, ld_sum=192), s=at(P[0], 128)) == EINVAL      # row 1 of the sum is inside row 1 of x
+    assert call_norm(lib, norm(rows=2), s=at(P[0], 128)) == EINVAL                             # in place, one row late
+
+    def norm_back(dout=P[0], h=P[1], dsum=P[2], w=P[3], dx=P[4], dw=P[5], ws=P[6]):
+        return lib.mcce_rmsnorm_backward(C.byref(n), dout, h, dsum, w, dx, dw, ws, 1 << 30, None)
+    for i in range(4):
+        step = 64 if i == 3 else 128
+        assert norm_back(dx=at(P[i], step)) == EINVAL and norm_back(dx=at(P[i], -384)) == EINVAL
+        assert norm_back(dw=at(P[i], step)) == EINVAL and norm_back(ws=at(P[i], 16)) == EINVAL and norm_back(ws=at(P[i], -16)) == EINVAL
+    assert norm_back(dw=at(P[4], 256)) == EINVAL and norm_back(ws=at(P[4], 16)) == EINVAL and norm_back(ws=at(P[5], 16)) == EINVAL
+    assert norm_back(ws=at(P[5], -1008)) == EINVAL
+
+    def dispatch(place=(), **kw):                    # 2 layers of 10 tokens x 4, rows of 128 bytes, 2 scales
+        r = rows(**dict(dict(scale_cols=2), **kw))
+        a = dict(sel=P[0], x=P[1], sc=P[2], off=P[3], perm=P[4], inv=P[5], out=P[6], osc=P[7], ws=P[8])
+        a.update(place)
+        return lib.mcce_dispatch(C.byref(r), a["sel"], a["x"], a["sc"], a["off"], a["perm"], a["inv"], a["out"], a["osc"], a["ws"], 1 << 30, None)
+    names = ["sel", "x", "sc", "off", "perm", "inv", "out", "osc"]
+    for i, out in enumerate(names):
+        for j, other in enumerate(names[:i]):
+            if i >= 3:
+                assert dispatch({out: at(P[j], 16)}) == EINVAL and dispatch({out: at(P[j], -16)}) == EINVAL, (out, other)
+    # with a workspace: 4096 tokens, tensors 64 MB apart
+    far = {n: C.c_void_p((i + 1) << 26) for i, n in enumerate(names + ["ws"])}
+    for n_ in names:
+        assert dispatch(dict(far, ws=at(far[n_], 16)), n_tokens=4096) == EINVAL, n_
+
+    def combine(rows_=P[0], inv=P[1], w=P[2], add=P[3], y=P[4], **kw):
+        return lib.mcce_combine(C.byref(rows(**kw)), rows_, inv, w, add, y, None)
+    for i in range(4):
+        assert combine(y=at(P[i], 16)) == EINVAL and combine(y=at(P[i], -16)) == EINVAL
+
+    def combine_back(dy=P[0], rows_=P[1], inv=P[2], w=P[3], dr=P[4], dw=P[5]):
+        return lib.mcce_combine_backward(C.byref(rows()), dy, rows_, inv, w, dr, dw, None)
+    for i in range(4):
+        for d in (16, -16):
+            assert combine_back(dr=at(P[i], d)) == EINVAL and combine_back(dw=at(P[i], d)) == EINVAL
+    assert combine_back(dw=at(P[4], 16)) == EINVAL and combine_back(dw=at(P[4], -16)) == EINVAL
+
+
+def test_shared_memory_is_found_exactly(tmp_path):
+    """The check itself (span.h, compiled here) against sets of bytes: rows side by side, between one another, with equal and
+    unequal strides; sizes that would overflow 64 bits."""
+    import os
+    import random
+    import subprocess
+    src = tmp_path / "span.cpp"
+    src.write_text('#include "span.h"\nextern "C" int apart3(long long p, long long r, long long s, long long w, long long p2, long long r2, '
+                   'long long s2, long long w2) { return mcce::disjoint(mcce::span((void*)p, r, s, w), mcce::span((void*)p2, r2, s2, w2)); }\n'
+                   'extern "C" int huge(long long n) { return mcce::disjoint(mcce::row_span((void*)4096, n, n, 64, 4), mcce::row_span((void*)8192, 3, n, 64, 4)); }\n')
+    subprocess.run(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-I", mbuild.CSRC, str(src), "-o", str(tmp_path / "span.so")], check=True)
+    so = C.CDLL(os.path.join(str(tmp_path), "span.so"))
+    so.apart3.argtypes = [C.c_longlong] * 8
+    so.huge.argtypes = [C.c_longlong]
+    rng = random.Random(3)
+
+    def touched(p, rows, step, width):
+        return {p + i * step + j for i in range(rows) for j in range(width)}
+    seen = [0, 0]
+    for _ in range(20000):
+        a, b = [(rng.randint(100, 160), rng.randint(1, 9), 0, rng.randint(1, 9)) for _ in range(2)]
+        sa = a[3] + rng.randint(0, 12)
+        sb = sa if rng.random() < 0.4 and sa >= b[3] else b[3] + rng.randint(0, 12)
+        a, b = (a[0], a[1], sa, a[3]), (b[0], b[1], sb, b[3])
+        want = not (touched(*a) & touched(*b))
+        seen[want] += 1
+        assert bool(so.apart3(*a, *b)) == want, (a, b)
+    assert min(seen) > 4000
+    for n in (1 << 62, (1 << 63) - 1):
+        assert so.huge(n) in (0, 1)
+
+
 def test_set_norm_needs_a_context(lib):
     assert lib.mcce_set_norm(None, P[0], 1e-6) == EINVAL
 
