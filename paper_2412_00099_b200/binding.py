@@ -428,7 +428,14 @@ def _marshal():
         path = os.path.join(_HERE, "_marshal.so")
         if not os.path.exists(path):
             raise McceError("_marshal.so is missing: build it with `python -m paper_2412_00099_b200.build`")
-        from . import _marshal as m
+        try:
+            from . import _marshal as m
+        except ImportError as e:
+            raise McceError("_marshal.so does not load (%s): build it again with `python -m paper_2412_00099_b200.build --force`" % e)
+        from .build import marshal_target
+        if getattr(m, "built_for", None) != marshal_target():
+            raise McceError("_marshal.so was built for %s, this is %s: build it again with `python -m paper_2412_00099_b200.build --force`"
+                            % (getattr(m, "built_for", "another version"), marshal_target()))
         m.connect(McceError, *[C.cast(getattr(lib, n), C.c_void_p).value for n in (
             "mcce_rmsnorm", "mcce_rmsnorm_backward_workspace_bytes", "mcce_rmsnorm_backward", "mcce_dispatch_workspace_bytes",
             "mcce_dispatch", "mcce_combine", "mcce_combine_backward", "mcce_strerror")])

@@ -338,4 +338,12 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Marshalling of torch t
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__marshal(void) { return PyModule_Create(&module); }
+// built_for: the torch and Python that this file was compiled against, for the binding to compare
+PyMODINIT_FUNC PyInit__marshal(void) {
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "built_for", MCCE_BUILT_FOR) < 0) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}
