@@ -417,6 +417,9 @@ def belady_replay(sel_trace: torch.Tensor, n_experts: int, capacities) -> torch.
 
 
 # -- operators around the experts ------------------------------------------------------------------------------
+# They record nothing for autograd.  In training each belongs inside a torch.autograd.Function whose backward makes the call that
+# is named as its gradient; a tensor that requires grad is refused while autograd is recording (in a Function's forward
+# and backward, and under torch.no_grad(), it is not).
 _fast = None
 
 
@@ -474,7 +477,7 @@ def rmsnorm(x, weight, eps=1e-6, add=None, quant_group=None, want_out=True, out:
     """h = x + add (returned as `sum` when add is given), out = h / rms(h) * weight; with quant_group (0: one scale per
     row, else 32, 64 or 128 columns per scale) also the 8-bit rows `q` and their `scales`.  x [..., d] fp32 or bf16;
     add fp32 or x's type; weight [d] fp32 or x's type.  `out` gives the result tensors (out.sum may be x); a field that
-    is None is not computed.  Not differentiable by itself: rmsnorm_backward is its gradient."""
+    is None is not computed.  Records no gradient (see below): rmsnorm_backward is its gradient."""
     if out is None:
         dev, shape = _on_cuda(x), x.shape
         _need(x.dim() >= 1 and shape[-1] >= 1, "x must have columns")
@@ -504,7 +507,8 @@ def rmsnorm_backward(dout, h, weight, eps=1e-6, dsum=None, want_dweight=True, ou
 def dispatch(sel_idx, n_experts, x=None, scales=None, out: Optional[Dispatched] = None) -> Dispatched:
     """Sorts token rows by expert.  sel_idx [T,K] or [L,T,K] int32; x [(L,)T,d] fp32, bf16 or float8_e4m3fn; scales [(L,)T,n]
     fp32.  Returns offsets [(L,)E+1], perm [(L,)T*K], inv like sel_idx, rows [(L,)T*K,d], scales [(L,)T*K,n]; what lies
-    behind the last bucket is left as it was (with `out`) or undefined."""
+    behind the last bucket is left as it was (with `out`) or undefined.  Records no gradient: combine without sel_w is the gradient of
+    rows with respect to x."""
     if out is None:
         dev = _on_cuda(sel_idx)
         _need(sel_idx.dim() in (2, 3), "sel_idx must be [T,K] or [L,T,K]")
@@ -523,7 +527,7 @@ def dispatch(sel_idx, n_experts, x=None, scales=None, out: Optional[Dispatched] 
 def combine(rows, inv, sel_w=None, add=None, out_dtype=None, out=None):
     """y[t] = add[t] + sum_k sel_w[t,k] rows[inv[t,k]] (weights 1 without sel_w: the gradient of dispatch with respect to
     x).  rows [(L,)T*K,d] fp32 or bf16, inv and sel_w [(L,)T,K]; y [(L,)T,d] in out_dtype: fp32, or the type of rows
-    (the default).  `out` may be add."""
+    (the default).  `out` may be add.  Records no gradient: combine_backward is its gradient (that of add is dy)."""
     if out is None:
         _on_cuda(rows)
         _need(inv.dim() in (2, 3) and rows.dim() == inv.dim(), "inv must be [T,K] or [L,T,K], rows [T*K,d] or [L,T*K,d]")
@@ -533,8 +537,8 @@ def combine(rows, inv, sel_w=None, add=None, out_dtype=None, out=None):
 
 
 def combine_backward(dy, rows, inv, sel_w=None, want_dw=True, out=None):
-    """Gradient of combine: drows (in the type of rows; rows at positions that inv does not name are left as they were) and
-    dw [(L,)T,K] fp32 (None if not wanted).  `out` = (drows, dw); drows may be rows."""
+    """Gradient of combine: drows (in the type of rows; rows at positions that inv does not name are left as they were with `out`,
+    undefined without) and dw [(L,)T,K] fp32 (None if not wanted).  `out` = (drows, dw); drows may be rows."""
     if out is None:
         _on_cuda(rows)
         out = (torch.empty_strided(rows.shape, rows.stride(), dtype=rows.dtype, device=rows.device),

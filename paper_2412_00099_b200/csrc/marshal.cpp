@@ -4,6 +4,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -38,11 +39,16 @@ void done(int rc) {
   if (rc != MCCE_OK) refuse("mcce error " + std::to_string(rc) + ": " + p_strerror(rc));
 }
 
-// A tensor argument; null for None.
+// A tensor argument; null for None.  The calls record nothing for autograd, so where it is recording a tensor that needs a gradient is
+// refused rather than cut off in silence.
 const at::Tensor* tensor(PyObject* o, const char* what) {
   if (o == Py_None) return nullptr;
   if (!THPVariable_Check(o)) refuse(std::string(what) + " must be a tensor");
-  return &THPVariable_Unpack(o);
+  const at::Tensor* t = &THPVariable_Unpack(o);
+  if (at::GradMode::is_enabled() && t->requires_grad())
+    refuse(std::string(what) + " requires grad, and this call records no gradient: call it inside a torch.autograd.Function "
+           "whose backward makes the gradient call, or under torch.no_grad()");
+  return t;
 }
 const at::Tensor& given(PyObject* o, const char* what) {
   const at::Tensor* t = tensor(o, what);

@@ -805,3 +805,25 @@ def test_columns_of_one_buffer_and_overlaps():
         mb.dispatch(sel, 4, rows, out=want._replace(inv=want.perm.view(R, 1)))
     with pytest.raises(mb.McceError):
         mb.dispatch(sel, 4, rows, out=want._replace(rows=rows))
+
+
+def test_inside_an_autograd_function():
+    """The way to train with them: a Function of the two calls, parameters that require grad handed straight in."""
+    class Norm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w):
+            ctx.save_for_backward(x, w)
+            return mb.rmsnorm(x, w, 1e-6).out
+
+        @staticmethod
+        def backward(ctx, g):
+            x, w = ctx.saved_tensors
+            return mb.rmsnorm_backward(g, x, w, 1e-6)
+    gn = gen(40)
+    x, w, g = normal(gn, 9, 96).requires_grad_(), (1 + 0.1 * normal(gn, 96)).requires_grad_(), normal(gn, 9, 96)
+    Norm.apply(x, w).backward(g)
+    check_gradient(g, x.detach(), w.detach(), 1e-6, None, x.grad, w.grad)
+    with pytest.raises(mb.McceError, match="requires grad"):
+        mb.rmsnorm(x, w)
+    with torch.no_grad():
+        assert torch.equal(mb.rmsnorm(x, w).out, Norm.apply(x, w))

@@ -292,3 +292,29 @@ def test_binding_refuses_cpu_tensors():
         mb.combine(torch.zeros(4, 8), torch.zeros(2, 2, dtype=torch.int32))
     with pytest.raises(mb.McceError, match="no CPU path"):
         mb.combine_backward(torch.zeros(2, 8), torch.zeros(4, 8), torch.zeros(2, 2, dtype=torch.int32))
+
+
+def test_binding_refuses_to_lose_a_gradient():
+    """The calls record nothing for autograd: a tensor that needs a gradient is refused while autograd is recording.  (CPU tensors: what
+    is not refused for its gradient is refused for its device.)"""
+    import torch
+
+    def leaf(*shape):
+        return torch.zeros(*shape, requires_grad=True)
+    x, w, i = torch.zeros(4, 8), torch.ones(8), torch.zeros(2, 2, dtype=torch.int32)
+    pair = torch.zeros(2, 2)
+    y, sorted_ = mb.NormOut(torch.zeros(4, 8), torch.zeros(4, 8)), mb.Dispatched(torch.zeros(5, dtype=torch.int32), None, i, x, x)
+    calls = [(lambda x, w, a: mb.rmsnorm(x, w, add=a, out=y), (x, w, x)),
+             (lambda g, h, w, s: mb.rmsnorm_backward(g, h, w, dsum=s, out=(x, w)), (x, x, w, x)),
+             (lambda x, s: mb.dispatch(i, 4, x, scales=s, out=sorted_), (x[:2], x[:2])),
+             (lambda r, w, a: mb.combine(r, i, w, add=a, out=x[:2]), (x, pair, x[:2])),
+             (lambda g, r, w: mb.combine_backward(g, r, i, w, out=(x, pair)), (x[:2], x, pair))]
+    for call, args in calls:
+        for k, a in enumerate(args):
+            some = [leaf(*b.shape) if j == k else b for j, b in enumerate(args)]
+            with pytest.raises(mb.McceError, match="requires grad"):
+                call(*some)
+            with torch.no_grad(), pytest.raises(mb.McceError, match="CUDA"):
+                call(*some)
+    with pytest.raises(mb.McceError, match="requires grad"):                  # a result that needs one
+        mb.rmsnorm(x, w, out=mb.NormOut(leaf(4, 8)))
