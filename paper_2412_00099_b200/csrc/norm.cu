@@ -704,17 +704,24 @@ GradShape grad_shape(int64_t rows, int d, Layout3 lay, int elem_bytes, bool dsum
   g.s = shape_for(units, units <= 1024 ? 2 : elem_bytes == 4 ? 8 : 4, ragged ? 2 * u : 1);
   const int rpb = g.s.threads / g.s.tpr;
   const int64_t all = (rows + rpb - 1) / rpb;
-  // 12 to 16 warps per SM with about 72 to 108 KB of rows on their way.  CTAs per SM / stages, us (16384 rows with dsum,
-  // weight's gradient included; the two figures of 2048: launches apart, back to back): 2048 bf16 4 / 2 49.3 and 47.6,
-  // 3 / 3 50.2 and 47.3, 4 / 3 49.8 and 49.8, 6 / 3 54.9 and 56; 1024 bf16 6 / 3 27.0, 6 / 2 28.7, 8 / 3 29.6; 4096 bf16
-  // 2 / 2 85.5, 2 / 3 87.0; 4096 fp32 without dsum 1 / 3 122, 1 / 2 138; 1001 x 1411 fp32 2 / 2 11.4, 2 / 3 12.0
-  // (up to four turns of a CTA; other shapes of few rows show no difference).
+  // CTAs per SM / stages, us (16384 rows with dsum, weight's gradient included): 2048 bf16 4 / 2 47.6, 3 / 3 47.3, 4 / 3 49.8, 6 / 3 56;
+  // 1024 bf16 6 / 3 27.0, 6 / 2 28.7, 8 / 3 29.6; 4096 bf16 2 / 2 85.5, 2 / 3 87.0.
   int per_sm = g.s.threads <= 64 ? 6 : g.s.threads >= 384 ? 1 : g.s.threads > 192 ? 2 : 512 / g.s.threads;
   // Two such CTAs that are left with one stage lose to one with two from 288 threads on (8192 x 9216 fp32 201 -> 155, 4096 x
   // 10000 bf16 100 -> 71), but not below (8192 x 5120 fp32 with dsum 130 against 124).
   if (g.s.threads > 256 && grad_smem(g.s, 2, d, ragged, dsum, dweight) > kGradSmemMost / 2) per_sm = 1;
+  // A third stage is worth its longer start where less than 48 KB of rows per SM are under way without it, the rows are aligned and a
+  // CTA has more than eight turns.  Two stages against three, us (calls in a graph), by turns of a CTA:
+  //                             2             4             8             16            32
+  //   1024 bf16 with dsum    7.5 / 7.7     9.5 / 9.7   14.7 / 15.0   23.6 / 22.9   40.9 / 39.6
+  //   2048 bf16              9.1 / 9.3   11.6 / 12.0   17.0 / 17.6   26.7 / 26.7   45.3 / 44.7
+  //   2048 fp32              6.5 / 6.8     8.7 / 8.9   14.6 / 14.8   23.6 / 22.7   41.7 / 38.9
+  //   4096 fp32              6.3 / 6.5     8.8 / 9.0   14.9 / 14.9   24.3 / 23.0   43.0 / 39.1
+  //   1411 bf16, ragged      9.7 / 9.9   11.6 / 11.9   16.6 / 17.2   25.3 / 25.9   41.7 / 42.4
+  //   1411 fp32, ragged      7.7 / 8.1     9.5 / 9.7   15.1 / 15.4   23.7 / 24.1   40.2 / 40.5
+  //   515 fp32 with dsum, r. 8.1 / 8.2     9.1 / 9.5   13.8 / 14.5   20.7 / 21.3   34.3 / 34.9
   const size_t flying = grad_smem(g.s, 1, d, false, dsum, false) * per_sm;
-  g.stages = flying >= 48 * 1024 || all <= 4 * per_sm * kSms ? 2 : 3;
+  g.stages = ragged || flying >= 48 * 1024 || all <= 8 * per_sm * kSms ? 2 : 3;
   while (g.stages > 1 && grad_smem(g.s, g.stages, d, ragged, dsum, dweight) > kGradSmemMost / per_sm) --g.stages;
   g.smem = grad_smem(g.s, g.stages, d, ragged, dsum, dweight);
   int ctas = per_sm * kSms;

@@ -214,6 +214,31 @@ def test_norm_gradient(R, d, T, W, with_dsum):
             assert torch.equal(mb.rmsnorm_backward(a[0], h, w, eps, dsum=a[1], out=(target, None))[0], dx)
 
 
+# rows for several turns of every CTA: three stages of the ring (aligned, more than eight turns), ragged rows whose threads keep their
+# columns from row to row, with one to six CTAs per SM, the last turn with and without rows for every CTA
+@pytest.mark.parametrize("R,d,T,W", [(5000, 2048, BF16, BF16), (7500, 1024, BF16, F32), (60000, 256, BF16, BF16), (1500, 4096, F32, F32),
+                                     (2500, 2048, F32, F32), (9000, 520, F32, F32), (1001, 1411, F32, F32), (2500, 1411, BF16, BF16),
+                                     (700, 4097, BF16, F32), (701, 2049, F32, F32), (3001, 515, F32, F32), (400, 9217, F32, F32),
+                                     (451, 10003, BF16, BF16), (9000, 100, BF16, BF16), (1300, 8192, BF16, F32)])
+@pytest.mark.parametrize("with_dsum", [True, False])
+def test_norm_gradient_of_batches(R, d, T, W, with_dsum):
+    gn = gen(R + d)
+    h, g = normal(gn, R, d, dtype=T) * 2, normal(gn, R, d, dtype=T)
+    w = (1 + 0.2 * normal(gn, d)).to(W)
+    ds = normal(gn, R, d, dtype=T) if with_dsum else None
+    dx, dw = mb.rmsnorm_backward(g, h, w, 1e-5, dsum=ds)
+    check_gradient(g, h, w, 1e-5, ds, dx, dw)
+    alone, none = mb.rmsnorm_backward(g, h, w, 1e-5, dsum=ds, want_dweight=False)
+    assert none is None and torch.equal(alone, dx)
+    if with_dsum:                                    # in place of what other rows are still to be fetched from
+        t = ds.clone()
+        got = mb.rmsnorm_backward(g, h, w, 1e-5, dsum=t, out=(t, torch.empty_like(dw)))
+        assert torch.equal(t, dx) and torch.equal(got[1], dw)
+    t = g.clone()
+    got = mb.rmsnorm_backward(t, h, w, 1e-5, dsum=ds, out=(t, torch.empty_like(dw)))
+    assert torch.equal(t, dx) and torch.equal(got[1], dw)
+
+
 @pytest.mark.parametrize("T", [BF16, F32])
 @pytest.mark.parametrize("d,layout", [(64, "aligned"), (61, "ragged"), (64, "unlike")])
 @pytest.mark.parametrize("rms", [1e18, 1e15, 1e13, 1e-13, 1e-15, 3e-20])
