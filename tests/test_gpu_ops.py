@@ -852,3 +852,45 @@ def test_inside_an_autograd_function():
         mb.rmsnorm(x, w)
     with torch.no_grad():
         assert torch.equal(mb.rmsnorm(x, w).out, Norm.apply(x, w))
+
+
+# the layouts of batches: more tokens than fill the device with one unit per lane (2368), 16-byte units, two elements and one, one pair
+# per token, two and more, rows of one warp and of several, both sides of the limit
+@pytest.mark.parametrize("L,T,K,d", [(1, 2500, 8, 256), (1, 2367, 5, 256), (1, 2368, 5, 256), (3, 1200, 1, 520), (1, 3000, 2, 1032), (2, 1300, 3, 2048),
+                                     (1, 2600, 6, 250), (1, 2600, 2, 250), (2, 1250, 4, 141), (1, 2500, 1, 333), (1, 2400, 3, 2050),
+                                     (1, 2400, 2, 2307), (1, 5000, 16, 24)])
+@pytest.mark.parametrize("R,Y", [(BF16, BF16), (BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("masked", [0.0, 0.3])
+def test_combine_and_gradient_of_batches(L, T, K, d, R, Y, masked):
+    g = gen(T * 7 + d)
+    inv, kept = positions(g, L, T, K, masked)
+    P = T * K
+    rows = normal(g, L, P, d, dtype=R)
+    named = torch.zeros(L, P, dtype=torch.bool, device="cuda")
+    for l in range(L):
+        named[l, inv[l][kept[l]].long()] = True
+    rows[~named] = float("nan")
+    w = torch.softmax(normal(g, L, T, K), -1)
+    w_ = torch.where(kept, w, torch.full_like(w, float("nan")))
+    add, dy = normal(g, L, T, d, dtype=Y), normal(g, L, T, d, dtype=Y)
+    at = inv.long().clamp(0, P - 1)
+    picked = torch.where(kept[..., None], torch.stack([rows[l][at[l]] for l in range(L)]).double(), torch.zeros((), dtype=torch.float64, device="cuda"))
+    for weight, a in ((w_, add), (None, None)):
+        wk = torch.where(kept, w.double() if weight is not None else torch.ones_like(w).double(), torch.zeros_like(w).double())[..., None]
+        want = (wk * picked).sum(2) + (a.double() if a is not None else 0)
+        size = (wk * picked).abs().sum(2) + (a.double().abs() if a is not None else 0)
+        y = mb.combine(rows, inv, weight, add=a, out_dtype=Y)
+        within(y, want, want.abs() * U(Y) + (K + 2) * u * size * (1 + U(Y)), "y")
+        drows = torch.full((L, P, d), 5.0, device="cuda", dtype=R)
+        _, dw = mb.combine_backward(dy, rows, inv, weight, out=(drows, torch.full((L, T, K), 8.0, device="cuda")))
+        terms = picked * dy.double()[:, :, None]
+        within(dw, terms.sum(3), (d + 8) * u * terms.abs().sum(3), "dw")
+        assert (dw[~kept] == 0).all() and (drows[~named] == 5).all()
+        for l in range(L):
+            wantd = (wk[l] * dy[l].double()[:, None])[kept[l]]
+            within(drows[l][inv[l][kept[l]].long()], wantd, wantd.abs() * (U(R) + 2 * u), "drows")
+        alone, _ = mb.combine_backward(dy, rows, inv, weight, want_dw=False, out=(torch.full_like(drows, 5.0), None))
+        assert torch.equal(alone, drows)
+        mine = rows.clone()
+        got, dw2 = mb.combine_backward(dy, mine, inv, weight, out=(mine, torch.empty_like(dw)))
+        assert torch.equal(dw2, dw) and torch.equal(got[named], drows[named]) and got[~named].isnan().all()
