@@ -94,7 +94,8 @@ __device__ __forceinline__ int single_column(int t, int head, int whole, int d) 
 // A row is read once: its units stay in registers from the addition to the last output, VPT of them per thread, so
 // that a thread has all its loads in flight before the point where the threads of a row meet.  fp32 arithmetic in pairs: one
 // element at a time, with its conversions, kept the scheduler busier than the memory (16384 x 4096 bf16: 98 us, now 81.5).
-// Bound: HBM, 1.0 of the copy bandwidth there (537 MB); ragged rows 0.83 (16384 x 4097 with fp32 add and 8-bit rows 135 us).
+// Bound: HBM, 1.0 of the copy bandwidth there (537 MB); ragged rows 0.91 (16384 x 4097 bf16: 90 us; with fp32 add and 8-bit rows 148, 0.76)
+// and rows aligned unlike each other, in the kernel below, 0.39 (16384 x 4096: 209 us).
 // RAGGED: rows start anywhere.  The units are those of the memory, up to U - 1 elements before the first and behind
 // the last one are single elements, one for each of the row's first 2 U threads.
 template <typename T, typename A, typename W, int VPT, bool RAGGED>
@@ -229,7 +230,8 @@ __global__ void __launch_bounds__(512) rmsnorm_kernel(const __grid_constant__ No
     if (ce >= 0) q[ce] = e4m3(ne * back);
   } else if (!RAGGED) {
     // A group is a power of two of neighbouring lanes, at least VPT of them: lane i does the two divisions for the group that the
-    // i-th units lie in.  In every lane, for every unit: 16384 x 4096 bf16 in groups of 32 100 us.
+    // i-th units lie in.  In every lane, for every unit, 16384 x 4096 bf16 in groups of 32 takes
+    // 100 us, so 93.
     const int lanes = (1 << a.group_log2) / U, me = th.t & (lanes - 1);
     uint32_t top = kAmaxFloor;
 #pragma unroll
@@ -390,11 +392,12 @@ cudaError_t launch_norm_types(const NormArgs& a, int dtype, bool ragged, const N
 }
 
 // Two units per thread; 64 bytes of every tensor per thread (4 units of bf16, 8 of fp32) where two would need more than 512
-// threads for a row, and for many wide ragged rows, whose single elements and shifted weights cost a thread the
-// same for two units as for four.  Measured with the residual's addition, us, two / wide: 16384 x 4096 bf16 83.9 / 85.0
-// (0.98 of the copy bandwidth), with 8-bit rows 16384 x 2048 60.9 / 62.7, 131072 x 64 13.2 / 17.2; ragged 16384 x 4097 with 8-bit
-// rows 152 / 150, 16384 x 4098 101 / 99, 16384 x 4097 fp32 191 / 184 (between two events: 5 us are not the kernel's).
-// One unit per thread: 16384 x 4096 98.8, a single row of 2048 7.2 against 7.3.
+// threads for a row, and for many wide ragged rows, whose single elements and shifted weights cost a thread the same for two units
+// as for four.  us with the residual's addition (calls back to back on three sets of inputs in turn, as all figures of this file), two
+// / wide: 16384 x 4096 bf16 81.5 / 82.1 (1.00 of the copy bandwidth), 16384 x 2048 with 8-bit rows 58.9 / 59.6, 131072 x 64 14.0 /
+// 15.2, with 8-bit rows 20.6 / 30.8; ragged 16384 x 4098 bf16 92.9 / 90.2, 16384 x 4097 fp32 178 / 160, 4097 bf16 with fp32 add and only
+// 8-bit rows 125 / 118, with out and fp32 weights beside them 143 / 148 (106 registers: the one that loses).  One unit per thread: 16384
+// x 4096 84.0, 16384 x 2048 with 8-bit rows 63.6, ragged 16384 x 4098 137.
 NormShape norm_shape(int64_t rows, int d, bool ragged, int elem_bytes, int group_log2) {
   const int u = 16 / elem_bytes, units = d / u;
   // a group of columns has to fit the lanes of one unit step; a ragged row needs 2 U threads for its single elements
@@ -416,7 +419,7 @@ struct NormGradArgs {
 // dx = r g + (h r) c + dsum with c = -r^2 mean(h g), for the vector and the scalar kernel alike.  The mean takes in one r at a time: it is
 // at most as large as rms(h) rms(g), so every product on the way lies between the mean, rms(g) and c, in fp32's range where r^2 or
 // r^3 alone are not.
-__device__ __forceinline__ float grad_coef(float inv, float mean_hg) { return -(inv * (inv * mean_hg)); }
+__device__ __forceinline__ float grad_coef(float inv, float mean_hg) { return -inv * (inv * mean_hg); }
 
 // Both sums at once: the lower half of a group of lanes ends up with x, the upper half with y.
 __device__ __forceinline__ float half_sum2(float2 v, int lanes) {
@@ -459,10 +462,12 @@ __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_grou
 // RAGGED: the step between a thread's rows is a multiple of U (or it has one row), so that every one of its rows starts at
 // the same place in a unit.  A thread therefore has the same columns in all its rows, aligned or not, and keeps their
 // weights and its part of the weights' gradient in registers.
-// Bound: HBM for aligned rows (16384 x 2048 bf16 with dsum: 43 us = 0.94 of the copy bandwidth, 47.6 back to back with the launch that
+// Bound: HBM for aligned rows (16384 x 2048 bf16 with dsum: 43.0 us = 0.95 of the copy bandwidth, 47.6 with the launch that
 // adds the parts of the weight's gradient); ragged rows add the pass over the single elements to every row's chain (16384 x 4097: 96
 // us = 0.85).  With the row in registers instead of the ring, loaded when it was needed, the first took 62 us; with columns that
-// move from row to row and sums in shared memory the second 148.
+// move from row to row and sums in shared memory the second 148.  62 to 102 registers with two units per thread; the wide forms hold
+// 128 and the aligned ones of them spill (20 bytes for bf16 above 8192 columns, 56 for fp32 above 4096: 16384 x 8192 bf16 164 us = 1.00,
+// 16384 x 5120 fp32 224 us = 0.91).
 template <typename T, typename W, int VPT, bool RAGGED>
 __global__ void __launch_bounds__(512) rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a) {
   constexpr int U = 16 / (int)sizeof(T);
@@ -619,7 +624,8 @@ __global__ void __launch_bounds__(512) rmsnorm_grad_kernel(const __grid_constant
   }
 }
 
-// Tensors whose rows are not aligned alike: element by element, twice over a row.
+// Tensors whose rows are not aligned alike: element by element, twice over a row.  16384 x 2048 bf16 with dsum 207 us (0.20 of the
+// copy bandwidth): one element per thread and load, and one row of a CTA after the other.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) rmsnorm_grad_scalar_kernel(const __grid_constant__ NormGradArgs a) {
   __shared__ float buf[2][32];
@@ -651,7 +657,7 @@ __global__ void __launch_bounds__(1024) dweight_kernel(const float* part, float*
   __shared__ float sum[64][17];
   const int col = threadIdx.x & 15, group = threadIdx.x >> 4, c = blockIdx.x * 16 + col;
   float s = 0.f;
-  cudaGridDependencySynchronize();   // launched before the kernel that writes the parts has ended
+  cudaGridDependencySynchronize();   // starts as the last CTAs of the kernel that writes the parts end, before its memory is flushed
   if (c < d) {
 #pragma unroll 10
     for (int p = group; p < parts; p += 64) s += part[(int64_t)p * d + c];
@@ -707,8 +713,8 @@ GradShape grad_shape(int64_t rows, int d, Layout3 lay, int elem_bytes, bool dsum
   // CTAs per SM / stages, us (16384 rows with dsum, weight's gradient included): 2048 bf16 4 / 2 47.6, 3 / 3 47.3, 4 / 3 49.8, 6 / 3 56;
   // 1024 bf16 6 / 3 27.0, 6 / 2 28.7, 8 / 3 29.6; 4096 bf16 2 / 2 85.5, 2 / 3 87.0.
   int per_sm = g.s.threads <= 64 ? 6 : g.s.threads >= 384 ? 1 : g.s.threads > 192 ? 2 : 512 / g.s.threads;
-  // Two such CTAs that are left with one stage lose to one with two from 288 threads on (8192 x 9216 fp32 201 -> 155, 4096 x
-  // 10000 bf16 100 -> 71), but not below (8192 x 5120 fp32 with dsum 130 against 124).
+  // Two such CTAs that are left with one stage lose to one with two from 288 threads on: 8192 x 9216 fp32 197 us against 152, with
+  // dsum 4096 x 10000 bf16 96 against 67, 10001 113 against 80, 8192 x 8200 fp32 213 against 194.
   if (g.s.threads > 256 && grad_smem(g.s, 2, d, ragged, dsum, dweight) > kGradSmemMost / 2) per_sm = 1;
   // A third stage is worth its longer start where less than 48 KB of rows per SM are under way without it, the rows are aligned and a
   // CTA has more than eight turns.  Two stages against three, us (calls in a graph), by turns of a CTA:

@@ -62,7 +62,9 @@ struct CopyArgs {
 
 // A row of units narrower than 16 bytes to the positions of its token's pairs, by `parts` warps of which this is number `part`:
 // V units of the row are read, all in flight, and written once for every pair, so a token's row is read once.  Full blocks'
-// loads and stores lie at fixed distances and need no look at the row's end (8192 x 8 of 1411 bf16: 57 us against 73).
+// loads and stores lie at fixed distances and need no look at the row's end (8192 x 8 of 1411 bf16: 56 us against
+// 73).  What bounds it is the units: 0.57 of the copy bandwidth there with 2 bytes per load and store, 0.78 with 4 (1411 fp32, 81 us), 0.32 with one
+// (1411 e4m3, 50 us).
 // position_of(k): of pair k, -1: none.
 template <typename V_, typename F>
 __device__ __forceinline__ void move_row(const CopyArgs& a, int64_t t, int64_t first, int lane, int part, int parts, F position_of) {
@@ -99,8 +101,8 @@ __device__ __forceinline__ void move_row(const CopyArgs& a, int64_t t, int64_t f
 
 // Rows of 16-byte units go through shared memory in pieces of kPiece units: fetched by cp.async, which needs no registers and so
 // starts before the counting, and written by one bulk copy per pair, issued by as many lanes at once.  Against loads into registers
-// and stores of 16 bytes per lane, us: 16384 x 8, a tenth of the pairs dropped, rows of 2048 bytes with scales 55.0 / 58, of 4096 bytes 94.5 / 99; 24 x 256
-// tokens x 4 of 4096 bytes 24.4 / 24.8; 20000 x 8 of 1024 bytes 48.0 / 46.7 (half of a piece's lanes idle).  Pieces of 64 units, three
+// and stores of 16 bytes per lane, us: 16384 x 8, a tenth of the pairs dropped, rows of 2048 bytes with scales 54.8 / 58, of 4096 bytes 94.3 / 99; 24 x 256
+// tokens x 4 of 4096 bytes 24.4 / 24.8; 20000 x 8 of 1024 bytes to 256 experts 48.1 / 46.7 (half of a piece's lanes idle).  Pieces of 64 units, three
 // per warp: 56.2, 95.0, 24.2 and 46.1.
 constexpr int kPiece = 128, kRing = 2;
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -127,7 +129,7 @@ struct Pieces {
 // its expert in earlier chunks (both from the chunks' counts), earlier in its chunk (counted here again), earlier in this
 // CTA.  A layer of few pairs is one chunk: the CTA counts all of it, and there is no launch before this one.
 // A pair's rank among its CTA's pairs comes from its warp's matches and the counts of the warps before.
-// Bound: HBM writes, once the counting is done: 16384 x 8, a tenth dropped, rows of 4096 bytes 94.5 us (0.89 of the copy bandwidth), of
+// Bound: HBM writes, once the counting is done: 16384 x 8, a tenth dropped, rows of 4096 bytes 94.3 us (0.89 of the copy bandwidth), of
 // 2048 bytes with scales 55 (0.79); about 8 us of each are the counting launch and the wait for the first CTAs' positions.  More CTAs per SM
 // at once are slower, not faster: 5 / 6 / 8 of them 99 / 101 / 115 with 4096 bytes (before the bulk copies).
 constexpr int kCtaPairs = 128;    // pairs of a CTA at most
@@ -332,7 +334,7 @@ __global__ void __launch_bounds__(256) combine_rows_kernel(const __grid_constant
 #pragma unroll
       for (int j = 0; j < N; ++j) s[v][j] = both(0.f);
     // The sum's last term is loaded last (held meanwhile, it costs a CTA per SM), but asked for into L2 at once.  K = 6 with a tenth of
-    // the pairs dropped, us: not asked for 89.7, asked for 86.1, loaded here 95.3; K = 8: 108.4, 106.0, 119.1.  One row at a time: worse (K = 2 28.8, 36.5).
+    // the pairs dropped, us: not asked for 89.7, asked for 86.0, loaded here 95.3; K = 8, none dropped: 108.4, 105.3, 119.1.  One row at a time: worse (K = 2 28.8, 36.5).
     if constexpr (KC > 1) {
 #pragma unroll
       for (int v = 0; v < VPT; ++v)
@@ -477,7 +479,7 @@ __device__ __forceinline__ float sum_of_all(float (&acc)[KC]) {
 }
 
 // drows and dw of a token: a unit of a row is read, multiplied into the pair's sum, and replaced by w dy.  KC rows at once.
-// Bound: HBM (0.97 of the copy bandwidth on 16384 x 8 rows of 2048 bf16, half of it writes).
+// Bound: HBM (0.98 of the copy bandwidth on 16384 x 8 rows of 2048 bf16, half of it writes).
 template <typename T, typename Y, int U, int KC, int VPT>
 __global__ void __launch_bounds__(256) combine_rows_grad_kernel(const __grid_constant__ CombineArgs a) {
   constexpr int N = (U + 1) / 2, kBlock = 32 * U * VPT;
@@ -654,12 +656,13 @@ cudaError_t launch_tokens(K kernel, const CombineArgs& a, cudaStream_t st) {
 bool few(const CombineArgs& a) { return a.tokens * 64 < 148 * 1024; }
 
 // KC rows at once x VPT units at once, us measured back to back on rotating buffers (16384 tokens of 2048 bf16 columns unless
-// noted).  Return, K = 8: 4 x 1 with 2 warps per token 96.4 (0.96 of the copy bandwidth), 8 x 1 104, 2 x 2 133; K = 6 with add (before it was asked for early): 4 x 1
-// 92.4, 3 x 1 92.3, 1 x 2 94.1; K = 2, 4099 tokens of 4096: 1 x 2 22.1 (0.69), 2 x 2 22.7, 4 x 1 24.8; K = 1 of 4096: 1 x 4 45.2 (0.91); 256
-// tokens, K = 8: 4 x 1 with 8 warps 4.2, 4 x 2 4.7.  Gradient, K = 8: 1 x 4 with 2 warps 179 (0.97), 2 x 2 181, 4 x 1 191; K = 1 of 4096: 1 x 4
+// noted).  Return, K = 8: 4 x 1 with 2 warps per token 94.6 (0.98 of the copy bandwidth), 8 x 1 104, 2 x 2 133; K = 6 with add (before it was asked for early): 4 x 1
+// 92.4, 3 x 1 92.3, 1 x 2 94.1; K = 2, 4099 tokens of 4096: 1 x 2 22.1 (0.69), 2 x 2 22.7, 4 x 1 24.8; K = 1 of 4096: 1 x 4 49.2 (0.83); 256
+// tokens, K = 8: 4 x 1 with 8 warps 4.2, 4 x 2 4.7.  Gradient, K = 8: 1 x 4 with 2 warps 177 (0.98), 2 x 2 181, 4 x 1 191; K = 1 of 4096: 1 x 4
 // 63.6 (0.97); 256 tokens, K = 8: 4 x 1 with 8 warps 6.3, 2 x 2 8.3.
-// Units of one bf16: 8192 tokens of 1411, K = 8, return 4 x 8 with 2 warps 53 (0.60), 4 x 4 57, 1 x 8 62; of 4097, K = 2: 2 x 8 50 (0.62), 1 x 8 53;
-// gradient 4 x 4 109 (0.55), 2 x 4 117; K = 2: 2 x 4 88 (0.58).  Sixteen-byte loads at the next boundary, shifted into place: 74 and 166.
+// Units of one bf16: 8192 tokens of 1411, K = 8, return 4 x 8 with 2 warps 51.4 (0.62), 4 x 4 57, 1 x 8 62; of 4097, K = 2: 2 x 8 49.2 (0.62), 1 x 8 53;
+// gradient 4 x 4 106 (0.57), 2 x 4 117; K = 2: 2 x 4 86 (0.59).  Sixteen-byte loads at the next boundary, shifted into place: 74 and 166.
+// A width that 4 divides but not 8 has units of two bf16: 16384 x 8 of 1004 55 (0.82) and 123 (0.70), of 1000 52 and 97.
 template <typename T, typename Y, int U>
 cudaError_t run_combine(CombineArgs a, cudaStream_t st) {
   const int units = (a.d + U - 1) / U;
@@ -700,7 +703,8 @@ cudaError_t run_combine_types(const mcce_rows& r, const CombineArgs& a, int u, b
   return run_combine_unit<__nv_bfloat16, __nv_bfloat16>(a, u, grad, st);
 }
 
-// A launch that may begin while the kernel before it ends; the kernel waits for that one itself.
+// A launch that follows the kernel before it at once: it starts when that one's last CTAs end, without the time between two launches, and waits
+// for its memory itself.  (No kernel here lets its dependents start sooner.)
 template <typename... P>
 cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t st, const std::decay_t<P>&... args) {
   cudaLaunchAttribute attr;
