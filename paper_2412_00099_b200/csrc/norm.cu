@@ -67,8 +67,9 @@ struct NormArgs {
 __device__ __forceinline__ float inv_rms(float sum_sq, float inv_d, float eps) { return rsqrtf(fmaf(sum_sq, inv_d, eps)); }
 // scale of a group from the bits of its largest magnitude, and what its values are multiplied by.  Both are one correctly rounded
 // division; the factor comes from the largest magnitude itself, not from the rounded scale, so a value is off by
-// two roundings before the one to 8 bits.  (An approximate reciprocal of a scale formed with a rounded 1 / 448 is off by up to 7, and
-// put two or three values in a million on the other side of an e4m3 tie.)
+// two roundings before the one to 8 bits.  (With an approximate reciprocal of a scale formed with a rounded 1 / 448 it was up to 7.)
+// Codes that differ from the quotient in 64 bits: 12 of 8.4 million in groups of 128 (the plain form in fp32: 9), fp32 in groups of 32
+// 49 of 67 million (56).
 __device__ __forceinline__ float scale_of(uint32_t amax) { return __fdiv_rn(__uint_as_float(amax), kE4m3Max); }
 __device__ __forceinline__ float back_of(uint32_t amax) { return __fdiv_rn(kE4m3Max, __uint_as_float(amax)); }
 
