@@ -378,6 +378,86 @@ int mcce_combine(const mcce_rows* r /*HOST*/, const void* rows, const int32_t* i
 int mcce_combine_backward(const mcce_rows* r /*HOST*/, const void* dy, const void* rows, const int32_t* inv,
                           const float* sel_w, void* drows, float* dw, void* cuda_stream);
 
+/* The experts' products on sorted rows, for mcce_expert_linear and its gradients.  Group g = l * n_experts + e holds rows
+ * offsets[l][e] .. offsets[l][e+1] of layer l (ascending, as mcce_dispatch writes them; what reaches outside [0, rows] is cut
+ * off) and uses weights number g.  One expert with offsets {0, rows} is a plain layer.  Rows behind a layer's last group are neither read for a
+ * result nor written. */
+enum { MCCE_ACT_NONE = 0, MCCE_ACT_SILU = 1, MCCE_ACT_GELU = 2 /* z P(z), P the normal distribution */ };
+enum { MCCE_LINEAR_MAX_GROUPS = 4096, MCCE_LINEAR_MAX_WIDTH = 1 << 20 };
+typedef struct {
+  int32_t n_layers, n_experts; /* >= 1, at most MCCE_LINEAR_MAX_GROUPS groups                                 */
+  int64_t rows;                /* per layer, >= 0; n_layers * rows <= 2^31-1                                  */
+  int32_t n, k;                /* outputs and inputs of one weight matrix [n,k], 1..MCCE_LINEAR_MAX_WIDTH     */
+  int32_t dtype;               /* rows, weights and what is saved of them: MCCE_F32 or MCCE_BF16              */
+  int32_t out_dtype;           /* out and add (mcce_expert_linear), dw and db (mcce_expert_linear_dweight): MCCE_F32 or dtype */
+  int32_t bias_dtype;          /* MCCE_F32 or dtype                                                           */
+  int32_t saved_dtype;         /* dtype, or MCCE_E4M3: blocks of 32 columns with a scale, as mcce_checkpoint_pack makes them */
+  int32_t act;                 /* MCCE_ACT_*                                                                  */
+  int32_t gated;               /* 1: two weight matrices per expert                                           */
+  int32_t below;               /* mcce_expert_linear_backward: columns of `saved` in units of k, 0 (none), 1, 2 (gated) */
+  int64_t ld_x, ld_y, ld_add, ld_saved, ld_h; /* row strides in elements, 0: the width.  x: rows of k (dx with below == 2: of 2 k);
+                                  y: out (rows of n), dout (rows of n, gated: of 2 n)                         */
+  int64_t ld_w, step_w;        /* weights: stride of a row (0: k) and from one matrix to the next (0: n * ld_w).  Both matrices of a
+                                  gated layer, dw and what is added to it have the same                       */
+} mcce_linear;
+
+/* One layer of every expert:  z = x W_g^T + bias_g;  out = act(z) + add, or gated  out = act(z) z_up + add  with
+ * z_up = x W_up_g^T + bias_up_g.
+ *   x DEVICE dtype [L,rows,k];  offsets DEVICE int32 [L,E+1];  w, w_up DEVICE dtype [L,E,n,k] (w_up NULL unless gated)
+ *   bias, bias_up DEVICE bias_dtype [L,E,n], contiguous, or NULL
+ *   add DEVICE out_dtype [L,rows,n] or NULL;    out DEVICE out_dtype [L,rows,n] out, may be add itself (same stride)
+ *   saved DEVICE saved_dtype [L,rows,n] (gated: [L,rows,2n], z then z_up) out or NULL: what the backward pass needs;
+ *   scales DEVICE bytes (e8m0) [L,rows,ceil(n/32)] (gated: twice that, those of z first), contiguous; given exactly when saved is and holds
+ *       8 bits.  Blocks do not reach from z into z_up.
+ * bf16 rows and weights meet on the tensor cores, whose fp32 accumulation truncates: a sum of k products is within 2^-24 k / 8 of its
+ * terms' magnitudes. */
+int mcce_expert_linear(const mcce_linear* p /*HOST*/, const void* x, const int32_t* offsets, const void* w, const void* w_up,
+                       const void* bias, const void* bias_up, const void* add, void* out, void* saved, void* scales,
+                       void* cuda_stream);
+
+/* Its gradient with respect to the rows:  t = dout W_g  (gated: dout = [d | d_up], t = d W_g + d_up W_up_g), and
+ *   below == 0:  dx = t + add
+ *   below == 1:  dx = t act'(z),  h = act(z)            where z = saved is what the layer below kept, whose act(z) was this layer's input
+ *   below == 2:  dx = [t z_up act'(z) | t act(z)],  h = act(z) z_up,  saved = [z | z_up]
+ * so one call takes the gradient through a product and the activation in front of it; h is the input again, for the weight gradient.
+ * (The gradient of the forward call's add is dout.)  act belongs to the layer below; MCCE_ACT_NONE when there is none.
+ *   dout DEVICE dtype [L,rows,n] (gated: [L,rows,2n]), stride ld_y;    add DEVICE dtype [L,rows,k] or NULL (below == 0 only)
+ *   saved DEVICE saved_dtype [L,rows,below*k], scales [L,rows,below*ceil(k/32)] with 8 bits; NULL where below == 0
+ *   dx DEVICE dtype [L,rows,k] (below == 2: [L,rows,2k]) out, stride ld_x; may be add, or saved in dtype, itself (same stride)
+ *   h  DEVICE dtype [L,rows,k] out, stride ld_h, or NULL */
+int mcce_expert_linear_backward(const mcce_linear* p /*HOST*/, const void* dout, const int32_t* offsets, const void* w,
+                                const void* w_up, const void* add, const void* saved, const void* scales, void* dx, void* h,
+                                void* cuda_stream);
+
+/* Its gradient with respect to weights and bias:  dw_g = add_dw_g + sum over the group's rows of dout_r^T x_r,
+ * db_g = add_db_g + sum of dout_r; gated: dw_up and db_up from the second half of dout's columns.  A group without rows gets what is added, or 0.
+ *   dout as above;    x DEVICE dtype [L,rows,k], or with scales (bytes, [L,rows,ceil(k/32)]) e4m3, stride ld_x
+ *   dw, dw_up DEVICE out_dtype [L,E,n,k] out (dw_up exactly when gated);    db, db_up DEVICE out_dtype [L,E,n] out, contiguous, or NULL
+ *   add_dw, add_dw_up, add_db, add_db_up: like dw .. db_up, or NULL; each may be that output itself
+ *   workspace DEVICE, 16-byte aligned, mcce_expert_linear_dweight_workspace_bytes(p) bytes with 8-bit x (0 otherwise: it may be NULL then):
+ *       x in dtype, which is exact for scales of 2^-117 and more. */
+size_t mcce_expert_linear_dweight_workspace_bytes(const mcce_linear* p /*HOST*/);
+int mcce_expert_linear_dweight(const mcce_linear* p /*HOST*/, const void* dout, const void* x, const void* scales,
+                               const int32_t* offsets, const void* add_dw, const void* add_dw_up, const void* add_db,
+                               const void* add_db_up, void* dw, void* dw_up, void* db, void* db_up, void* workspace,
+                               size_t workspace_bytes, void* cuda_stream);
+
+/* MCCE_ETIMEOUT if a bounded wait in one of the three calls above gave up on the current device since the last call (the launch it
+ * happened in is incomplete, the CUDA context stays usable), else MCCE_OK.  Synchronises the stream. */
+int mcce_expert_linear_status(void* cuda_stream);
+
+/* Rows into 8 bits and back, for what a backward pass needs again.  For every block of 32 columns (the last may be shorter)
+ *   scale = the smallest power of two, 2^-127 at least, with max |x_j| <= 448 scale;    q_j = e4m3(x_j / scale)
+ * and back x_j = q_j scale.  Division and product are exact, so a value is rounded once, to within 2^-4 of itself (or half a subnormal
+ * step, 2^-10 scale).  A block that holds a NaN or an infinity becomes NaN.  scale is stored as its exponent (e8m0: byte b
+ * stands for 2^(b-127), 255 for NaN).
+ *   x DEVICE dtype (MCCE_F32 or MCCE_BF16) [rows,d], stride ld_x (0: d);  q DEVICE e4m3 [rows,d], stride ld_q (0: d)
+ *   scales DEVICE bytes [rows,ceil(d/32)], contiguous.    0 <= rows <= 2^31-1, 1 <= d <= MCCE_LINEAR_MAX_WIDTH */
+int mcce_checkpoint_pack(const void* x, int32_t dtype, int64_t rows, int32_t d, int64_t ld_x, int64_t ld_q, void* q, void* scales,
+                         void* cuda_stream);
+int mcce_checkpoint_unpack(const void* q, const void* scales, int32_t dtype, int64_t rows, int32_t d, int64_t ld_x, int64_t ld_q,
+                           void* x, void* cuda_stream);
+
 /* Seeded synthetic inputs (counter-based: Philox4x32-10 keyed by (seed, 0), counter = (element
  * block, t, tensor_id), Box-Muller with fixed-order fp32 series); no counterpart in the paper, whose
  * inputs are text corpora.  out DEVICE, dtype MCCE_F32/MCCE_BF16; elements [start, start+count) of the

@@ -28,7 +28,8 @@ EXPORTS = [
     "mcce_route_step", "mcce_moe_forward", "mcce_decode_step_host", "mcce_decode_step_chained", "mcce_pipeline_submit_host", "mcce_pipeline_submit", "mcce_pipeline_wait", "mcce_cache_stats", "mcce_calibrate_delta", "mcce_get_cache_state",
     "mcce_get_grouping", "mcce_lifetime_stats", "mcce_set_miss_trace", "mcce_belady_replay",
     "mcce_rmsnorm", "mcce_rmsnorm_backward", "mcce_rmsnorm_backward_workspace_bytes", "mcce_dispatch", "mcce_dispatch_workspace_bytes",
-    "mcce_combine", "mcce_combine_backward", "mcce_profile", "mcce_profile_read", "mcce_uses_tensor_path", "mcce_router_kernel_kind", "mcce_selftest_wait_timeout", "mcce_route_trace_static",
+    "mcce_combine", "mcce_combine_backward", "mcce_expert_linear", "mcce_expert_linear_backward", "mcce_expert_linear_dweight",
+    "mcce_expert_linear_dweight_workspace_bytes", "mcce_expert_linear_status", "mcce_checkpoint_pack", "mcce_checkpoint_unpack", "mcce_profile", "mcce_profile_read", "mcce_uses_tensor_path", "mcce_router_kernel_kind", "mcce_selftest_wait_timeout", "mcce_route_trace_static",
     "mcce_route_trace_static_limit", "mcce_gen_normal", "mcce_gen_hidden_step", "mcce_gen_philox_words", "mcce_strerror",
     "mcce_last_cuda_error",
 ]
@@ -60,6 +61,12 @@ class Norm(C.Structure):
 class Rows(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_tokens", "top_k", "n_experts", "d", "dtype", "token_dtype",
                                          "scale_cols")] + [(n, C.c_int64) for n in ("ld_token", "ld_rows")]
+
+
+class Linear(C.Structure):
+    _fields_ = [("n_layers", C.c_int32), ("n_experts", C.c_int32), ("rows", C.c_int64)] + [
+        (n, C.c_int32) for n in ("n", "k", "dtype", "out_dtype", "bias_dtype", "saved_dtype", "act", "gated", "below")] + [
+        (n, C.c_int64) for n in ("ld_x", "ld_y", "ld_add", "ld_saved", "ld_h", "ld_w", "step_w")]
 
 
 class McceError(RuntimeError):
@@ -118,6 +125,14 @@ def load():
         lib.mcce_dispatch.argtypes = [vp] * 10 + [C.c_size_t, vp]
         lib.mcce_combine.argtypes = [vp] * 7
         lib.mcce_combine_backward.argtypes = [vp] * 8
+        lib.mcce_expert_linear.argtypes = [vp] * 12
+        lib.mcce_expert_linear_backward.argtypes = [vp] * 11
+        lib.mcce_expert_linear_dweight_workspace_bytes.restype = C.c_size_t
+        lib.mcce_expert_linear_dweight_workspace_bytes.argtypes = [vp]
+        lib.mcce_expert_linear_dweight.argtypes = [vp] * 14 + [C.c_size_t, vp]
+        lib.mcce_expert_linear_status.argtypes = [vp]
+        lib.mcce_checkpoint_pack.argtypes = [vp, i32, C.c_int64, i32, C.c_int64, C.c_int64, vp, vp, vp]
+        lib.mcce_checkpoint_unpack.argtypes = [vp, vp, i32, C.c_int64, i32, C.c_int64, C.c_int64, vp, vp]
         lib.mcce_strerror.restype = C.c_char_p
         lib.mcce_strerror.argtypes = [C.c_int]
         lib.mcce_last_cuda_error.argtypes = [vp]
@@ -441,7 +456,9 @@ def _marshal():
                             % (getattr(m, "built_for", "another version"), marshal_target()))
         m.connect(McceError, *[C.cast(getattr(lib, n), C.c_void_p).value for n in (
             "mcce_rmsnorm", "mcce_rmsnorm_backward_workspace_bytes", "mcce_rmsnorm_backward", "mcce_dispatch_workspace_bytes",
-            "mcce_dispatch", "mcce_combine", "mcce_combine_backward", "mcce_strerror")])
+            "mcce_dispatch", "mcce_combine", "mcce_combine_backward", "mcce_expert_linear", "mcce_expert_linear_backward",
+            "mcce_expert_linear_dweight_workspace_bytes", "mcce_expert_linear_dweight", "mcce_checkpoint_pack", "mcce_checkpoint_unpack",
+            "mcce_strerror")])
         _fast = m
     return _fast
 
@@ -544,4 +561,131 @@ def combine_backward(dy, rows, inv, sel_w=None, want_dw=True, out=None):
         out = (torch.empty_strided(rows.shape, rows.stride(), dtype=rows.dtype, device=rows.device),
                torch.empty(inv.shape, dtype=torch.float32, device=rows.device) if want_dw else None)
     (_fast or _marshal()).combine_backward(dy, rows, inv, sel_w, *out)
+    return out
+
+
+# -- the experts' products on sorted rows ----------------------------------------------------------------------
+# x, dout and everything else that has a row per (token, slot) pair lies as dispatch sorts it: offsets [(L,)E+1] int32 says where every
+# expert's rows begin.  Rows behind the last expert's are neither read for a result nor written.  They record nothing for autograd either.
+ACTS = {None: 0, "silu": 1, "gelu": 2}
+E8M0 = torch.float8_e8m0fnu
+
+
+class LinearOut(NamedTuple):
+    """Results of expert_linear: `saved` [(L,)R,n] or, gated, [(L,)R,2n] is what the backward pass needs, `scales` belong to 8-bit `saved`."""
+    out: torch.Tensor
+    saved: Optional[torch.Tensor] = None
+    scales: Optional[torch.Tensor] = None
+
+
+class LinearGrad(NamedTuple):
+    """Results of expert_linear_backward."""
+    dx: torch.Tensor
+    h: Optional[torch.Tensor] = None
+
+
+class WeightGrad(NamedTuple):
+    """Results of expert_linear_dweight (and what it adds to); *_up for gated layers, db* where the bias's gradient is wanted."""
+    dw: torch.Tensor
+    dw_up: Optional[torch.Tensor] = None
+    db: Optional[torch.Tensor] = None
+    db_up: Optional[torch.Tensor] = None
+
+
+class Checkpoint(NamedTuple):
+    """Rows in 8 bits: `q` float8_e4m3fn, `scales` float8_e8m0fnu per block of 32 columns."""
+    q: torch.Tensor
+    scales: torch.Tensor
+
+
+def _act_code(act):
+    _need(act in ACTS, "act must be None, 'silu' or 'gelu'")
+    return ACTS[act]
+
+
+def _weights(w):
+    _on_cuda(w)
+    _need(w.dim() in (3, 4), "weights must be [E,n,k] or [L,E,n,k]")
+    return w.shape[-2], w.shape[-1]
+
+
+def expert_linear(x, offsets, w, w_up=None, bias=None, bias_up=None, act=None, add=None, save=None, out_dtype=None,
+                  out: Optional[LinearOut] = None) -> LinearOut:
+    """One layer of every expert on its rows: act(x w^T + bias) + add, or with w_up the gated layer act(x w^T + bias) * (x w_up^T + bias_up) +
+    add.  x [(L,)R,k] fp32 or bf16, w and w_up [(L,)E,n,k] in its type, bias [(L,)E,n] fp32 or its type, act None, "silu" or "gelu"; add
+    and the result in out_dtype: fp32, or the type of x (the default).  save keeps the pre-activations for the backward pass: "same" in
+    the type of x, "e4m3" in 8 bits.  `out` gives the result tensors (out.out may be add).  Records no gradient:
+    expert_linear_backward and expert_linear_dweight are its gradients (that of add is dout)."""
+    if out is None:
+        (n, _), dev = _weights(w), _on_cuda(x)
+        _need(x.dim() == w.dim() - 1, "x must be [R,k], or [L,R,k] with weights [L,E,n,k]")
+        _need(save in (None, "same", "e4m3"), "save must be None, 'same' or 'e4m3'")
+        halves, head, saved, scales = 1 if w_up is None else 2, x.shape[:-1], None, None
+        if save is not None:
+            saved = torch.empty(head + (halves * n,), dtype=x.dtype if save == "same" else torch.float8_e4m3fn, device=dev)
+        if save == "e4m3":
+            scales = torch.empty(head + (halves * -(-n // 32),), dtype=E8M0, device=dev)
+        out = LinearOut(torch.empty(head + (n,), dtype=out_dtype or x.dtype, device=dev), saved, scales)
+    (_fast or _marshal()).expert_linear(x, offsets, w, w_up, bias, bias_up, _act_code(act), add, *out)
+    return out
+
+
+def expert_linear_backward(dout, offsets, w, w_up=None, saved=None, scales=None, act=None, add=None, want_h=True,
+                           out: Optional[LinearGrad] = None) -> LinearGrad:
+    """Gradient of expert_linear with respect to its rows, t = dout w (gated: dout [(L,)R,2n] holds the gradients of both products).  Without
+    `saved` dx = t + add.  With `saved`, what the layer below kept (k columns, or 2k of a gated layer; 8-bit with scales), the gradient
+    goes on through its activation `act`: dx is the gradient of its pre-activations, in the shape of `saved`, and h its output formed
+    again for expert_linear_dweight.  `out` gives the result tensors: dx may be add, or `saved` in the type of dout; h None is not
+    computed."""
+    if out is None:
+        (_, k), dev = _weights(w), _on_cuda(dout)
+        _need(dout.dim() == w.dim() - 1, "dout must be [R,n], or [L,R,n] with weights [L,E,n,k]")
+        head = dout.shape[:-1]
+        out = LinearGrad(torch.empty(head + (k if saved is None else saved.shape[-1],), dtype=dout.dtype, device=dev),
+                         torch.empty(head + (k,), dtype=dout.dtype, device=dev) if saved is not None and want_h else None)
+    (_fast or _marshal()).expert_linear_backward(dout, offsets, w, w_up, _act_code(act), add, saved, scales, *out)
+    return out
+
+
+def expert_linear_dweight(dout, x, offsets, scales=None, gated=False, want_db=False, add: Optional[WeightGrad] = None, out_dtype=None,
+                          out: Optional[WeightGrad] = None) -> WeightGrad:
+    """Gradient of expert_linear with respect to its weights [(L,)E,n,k] and, with want_db, its bias: dout^T x and the sums of dout, expert by
+    expert, in out_dtype: fp32, or the type of dout (the default).  gated: dout [(L,)R,2n] holds both products' gradients.  x in the
+    type of dout, or float8_e4m3fn with scales.  `add` is what earlier batches left (accumulation: the same tensors as `out`)."""
+    if out is None:
+        dev = _on_cuda(dout)
+        _need(dout.dim() in (2, 3) and offsets.dim() == dout.dim() - 1 and x.dim() == dout.dim(), "dout and x must be [R,columns] with offsets "
+              "[E+1], or [L,R,columns] with offsets [L,E+1]")
+        n, kind = dout.shape[-1] // (2 if gated else 1), dict(dtype=out_dtype or dout.dtype, device=dev)
+        shape = offsets.shape[:-1] + (offsets.shape[-1] - 1, n)
+        w = [torch.empty(shape + (x.shape[-1],), **kind) for _ in range(2 if gated else 1)] + [None]
+        b = [torch.empty(shape, **kind) for _ in range(2 if gated else 1)] + [None] if want_db else [None, None]
+        out = WeightGrad(w[0], w[1], b[0], b[1])
+    (_fast or _marshal()).expert_linear_dweight(dout, x, scales, offsets, *(add or (None, None, None, None)), *out)
+    return out
+
+
+def expert_linear_status():
+    """Raises McceError if a bounded wait inside one of these products' kernels gave up on the current device since the last call.
+    Synchronises the current stream."""
+    _check(load().mcce_expert_linear_status(_stream()))
+
+
+def checkpoint_pack(x, out: Optional[Checkpoint] = None) -> Checkpoint:
+    """Rows x [..., d] (fp32 or bf16) in 8 bits: e4m3 values and a power-of-two scale for every 32 columns."""
+    if out is None:
+        dev = _on_cuda(x)
+        _need(x.dim() >= 1 and x.shape[-1] >= 1, "x must have columns")
+        out = Checkpoint(torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=dev),
+                         torch.empty(x.shape[:-1] + (-(-x.shape[-1] // 32),), dtype=E8M0, device=dev))
+    (_fast or _marshal()).checkpoint_pack(x, *out)
+    return out
+
+
+def checkpoint_unpack(q, scales, dtype=torch.bfloat16, out=None):
+    """The rows that checkpoint_pack or expert_linear kept, in fp32 or bf16."""
+    if out is None:
+        _on_cuda(q)
+        out = torch.empty(q.shape, dtype=dtype, device=q.device)
+    (_fast or _marshal()).checkpoint_unpack(q, scales, out)
     return out

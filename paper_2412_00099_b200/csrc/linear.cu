@@ -1,0 +1,461 @@
+// The experts' products on sorted rows: entry points, and the kernels that take any size, stride, alignment and type.
+#include "linear.cuh"
+
+#include "span.h"
+#include "tc_common.cuh"
+
+namespace mcce {
+namespace linear {
+namespace {
+
+// ---- products of any shape -----------------------------------------------------------------------------------
+// Tiles of 64 x 64 results, 16 products deep, 4 x 4 results per thread, in fp32.  The results go through shared memory so that a warp
+// ends up with 32 neighbouring columns of a row.
+constexpr int kTile = 64, kDeep = 16, kPad = kTile + 4;
+
+template <Kind KIND, typename T, bool GATED>
+__global__ void __launch_bounds__(256) general_kernel(const Problem p) {
+  constexpr int kSets = KIND == kForward && GATED ? 2 : 1;   // sums per result: a gated forward pass has two
+  extern __shared__ __align__(16) float smem[];
+  float* As = smem;                          // [kDeep][kPad]
+  float* Bs = As + kDeep * kPad;             // [kSets][kDeep][kPad]
+  float* Cs = smem;                          // [kSets][64][65], after the products
+  int* before = (int*)(smem + kSets * kTile * 65);
+  int* scratch = before + p.groups.G + 1;
+  const int t = threadIdx.x, tx = t % 16, ty = t / 16;
+
+  const int cols = KIND == kForward ? p.n : p.k;
+  const int JT = (cols + kTile - 1) / kTile;
+  int64_t items;
+  const int IT = (p.n + kTile - 1) / kTile;               // kDweight: tiles of dout's columns
+  constexpr int kHalves = KIND == kDweight && GATED ? 2 : 1;
+  if (KIND == kDweight) {
+    items = (int64_t)p.groups.G * kHalves * IT * JT;
+  } else {
+    count_tiles(p.groups, kTile, before, scratch);
+    items = (int64_t)before[p.groups.G] * JT;
+  }
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    int g, i0, j0 = (int)(item % JT) * kTile, half = 0;
+    if (KIND == kDweight) {
+      int64_t r = item / JT;
+      i0 = (int)(r % IT) * kTile, r /= IT;
+      half = (int)(r % kHalves), g = (int)(r / kHalves);
+    } else {
+      const int tile = (int)(item / JT);
+      g = find_group(before, p.groups.G, tile);
+      i0 = 0;
+      if (tile >= before[g]) i0 = (tile - before[g]) * kTile;
+    }
+    const GroupRows gr = group_rows(p.groups, g);
+    const int64_t row0 = gr.first + (KIND == kDweight ? 0 : i0);
+    const int I = KIND == kDweight ? min(kTile, p.n - i0) : (int)min((int64_t)kTile, gr.m - i0);
+    const int J = min(kTile, cols - j0);
+    const int64_t red = KIND == kForward ? p.k : KIND == kBackward ? p.n : gr.m;
+    constexpr int kParts = KIND == kBackward && GATED ? 2 : 1;
+    float c[kSets][4][4] = {};
+    for (int part = 0; part < kParts; ++part)
+      for (int64_t d0 = 0; d0 < red; d0 += kDeep) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          // operand with the reduction along its rows: 16 neighbours of a row; across them: 64 neighbours
+          const int ka = t % kDeep, ma = t / kDeep + 16 * i, kb = t / kTile + 4 * i, mb = t % kTile;
+          if (KIND == kDweight) {
+            const bool in = d0 + kb < red;
+            const int64_t r = gr.first + d0 + kb;
+            As[kb * kPad + mb] = in && mb < I ? load_as_float((const T*)p.y + r * p.ld_y + half * p.n + i0 + mb) : 0.f;
+            Bs[kb * kPad + mb] = in && mb < J ? load_as_float((const T*)p.x + r * p.ld_x + j0 + mb) : 0.f;
+          } else if (KIND == kForward) {
+            const bool in = d0 + ka < red;
+            As[ka * kPad + ma] = in && ma < I ? load_as_float((const T*)p.x + (row0 + ma) * p.ld_x + d0 + ka) : 0.f;
+            const int64_t at = g * p.step_w + (int64_t)(j0 + ma) * p.ld_w + d0 + ka;
+            Bs[ka * kPad + ma] = in && ma < J ? load_as_float((const T*)p.w + at) : 0.f;
+            if (kSets == 2) Bs[(kDeep + ka) * kPad + ma] = in && ma < J ? load_as_float((const T*)p.w_up + at) : 0.f;
+          } else {
+            As[ka * kPad + ma] =
+                d0 + ka < red && ma < I ? load_as_float((const T*)p.y + (row0 + ma) * p.ld_y + (int64_t)part * p.n + d0 + ka) : 0.f;
+            Bs[kb * kPad + mb] = d0 + kb < red && mb < J ? load_as_float((const T*)(part ? p.w_up : p.w) + g * p.step_w + (d0 + kb) * p.ld_w + j0 + mb)
+                                                         : 0.f;
+          }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int d = 0; d < kDeep; ++d) {
+          const float4 a = *(const float4*)(As + d * kPad + 4 * ty);
+          const float av[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+          for (int s = 0; s < kSets; ++s) {
+            const float4 b = *(const float4*)(Bs + (s * kDeep + d) * kPad + 4 * tx);
+            const float bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) c[s][i][j] = fmaf(av[i], bv[j], c[s][i][j]);
+          }
+        }
+        __syncthreads();
+      }
+#pragma unroll
+    for (int s = 0; s < kSets; ++s)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) Cs[(s * kTile + 4 * ty + i) * 65 + 4 * tx + j] = c[s][i][j];
+    __syncthreads();
+    const int warp = t / 32, lane = t % 32;
+    for (int jj = 0; jj < J; jj += 32) {
+      const float* col = Cs + jj + lane;
+      if (KIND == kDweight) {
+        const void* add = half ? p.add_dw_up : p.add_dw;
+        void* dw = half ? p.dw_up : p.dw;
+        const int j = jj + lane;
+        for (int i = warp; i < I; i += 8) {
+          if (j >= J) continue;
+          const int64_t at = g * p.step_w + (int64_t)(i0 + i) * p.ld_w + j0 + j;
+          float v = col[i * 65];
+          if (p.dw_f32) {
+            if (add) v += ((const float*)add)[at];
+            ((float*)dw)[at] = v;
+          } else {
+            if (add) v += load_as_float((const T*)add + at);
+            store_as((T*)dw + at, v);
+          }
+        }
+      } else if (KIND == kForward) {
+        const Forward<T, GATED> e(p.fwd, g, j0 + jj + lane);
+        for (int i = warp; i < I; i += 8) e.store(row0 + i, col[i * 65], kSets == 2 ? col[(kTile + i) * 65] : 0.f, e.load(row0 + i));
+      } else {
+        const Backward<T> e(p.bwd, g, j0 + jj + lane);
+        for (int i = warp; i < I; i += 8) e.store(row0 + i, col[i * 65], 0.f, e.load(row0 + i));
+      }
+    }
+    __syncthreads();
+  }
+}
+
+template <Kind KIND, typename T, bool GATED>
+cudaError_t launch_general(const Problem& p, cudaStream_t st) {
+  static int cache[64] = {0};
+  constexpr int kSets = KIND == kForward && GATED ? 2 : 1;
+  const size_t fixed = (size_t)kSets * kTile * 65 * 4;
+  int sms = 0;
+  const cudaError_t e =
+      tc::sm_count_and_smem_optin(general_kernel<KIND, T, GATED>, fixed + (MCCE_LINEAR_MAX_GROUPS + 1 + 33) * 4, cache, &sms);
+  if (e != cudaSuccess) return e;
+  const int64_t jt = ((KIND == kForward ? p.n : p.k) + kTile - 1) / kTile;
+  const int64_t most = KIND == kDweight ? (int64_t)p.groups.G * 2 * ((p.n + kTile - 1) / kTile) * jt
+                                        : ((p.L * p.groups.R) / kTile + p.groups.G) * jt;
+  const int64_t grid = most < 4 * sms ? most : 4 * sms;
+  general_kernel<KIND, T, GATED><<<(unsigned)grid, 256, fixed + (size_t)(p.groups.G + 1 + 33) * 4, st>>>(p);
+  return cudaGetLastError();
+}
+
+// ---- sums of dout's columns per group (the bias's gradient) ----------------------------------------------------
+struct BiasArgs {
+  Groups groups;
+  int32_t n, gated, f32;
+  int64_t ld_y;
+  const void *y, *add, *add_up;
+  void *db, *db_up;
+};
+// A CTA sums 32 columns of one group: 32 warps take rows in turn, four under way each, and their sums are added in a fixed order.
+template <typename T>
+__global__ void __launch_bounds__(1024) bias_kernel(const BiasArgs a) {
+  __shared__ float part[32][33];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = blockIdx.y, half = blockIdx.z;
+  const int j = blockIdx.x * 32 + lane;
+  const GroupRows gr = group_rows(a.groups, g);
+  const T* y = (const T*)a.y + gr.first * a.ld_y + (int64_t)half * a.n + j;
+  float s[4] = {};
+  if (j < a.n)
+    for (int64_t r = warp; r < gr.m; r += 128) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (r + 32 * u < gr.m) s[u] += load_as_float(y + (r + 32 * u) * a.ld_y);
+    }
+  part[warp][lane] = (s[0] + s[1]) + (s[2] + s[3]);
+  __syncthreads();
+  float v = part[lane][warp];   // column `warp`, part `lane`
+  for (int d = 16; d; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
+  const int col = blockIdx.x * 32 + warp;
+  if (lane == 0 && col < a.n) {
+    const int64_t at = (int64_t)g * a.n + col;
+    const void* add = half ? a.add_up : a.add;
+    void* db = half ? a.db_up : a.db;
+    if (a.f32) ((float*)db)[at] = v + (add ? ((const float*)add)[at] : 0.f);
+    else store_as((T*)db + at, v + (add ? load_as_float((const T*)add + at) : 0.f));
+  }
+}
+
+// ---- 8-bit checkpoints ------------------------------------------------------------------------------------------
+// One block of 32 columns per warp at a time.
+template <typename T>
+__global__ void __launch_bounds__(256) pack_kernel(const T* x, uint8_t* q, uint8_t* scales, int64_t blocks, int per_row, int d, int64_t ld_x,
+                                                   int64_t ld_q) {
+  const int lane = threadIdx.x & 31;
+  for (int64_t b = blockIdx.x * 8ll + (threadIdx.x >> 5); b < blocks; b += gridDim.x * 8ll) {
+    const int64_t row = b / per_row;
+    const int j = (int)(b % per_row) * 32 + lane;
+    const float v = j < d ? load_as_float(x + row * ld_x + j) : 0.f;
+    const uint32_t s = warp_block_scale(v);
+    if (j < d) q[row * ld_q + j] = to_e4m3(v, s);
+    if (lane == 0) scales[b] = (uint8_t)s;
+  }
+}
+template <typename T>
+__global__ void __launch_bounds__(256) unpack_kernel(const uint8_t* q, const uint8_t* scales, T* x, int64_t blocks, int per_row, int d,
+                                                     int64_t ld_x, int64_t ld_q) {
+  const int lane = threadIdx.x & 31;
+  for (int64_t b = blockIdx.x * 8ll + (threadIdx.x >> 5); b < blocks; b += gridDim.x * 8ll) {
+    const int64_t row = b / per_row;
+    const int j = (int)(b % per_row) * 32 + lane;
+    if (j < d) store_as(x + row * ld_x + j, e4m3_value(q[row * ld_q + j]) * scale_value(scales[b]));
+  }
+}
+
+}  // namespace
+
+cudaError_t run_general(Kind kind, const Problem& p, int32_t dtype, cudaStream_t st) {
+  const bool g = p.gated;
+  if (dtype == MCCE_F32) {
+    if (kind == kForward) return g ? launch_general<kForward, float, true>(p, st) : launch_general<kForward, float, false>(p, st);
+    if (kind == kBackward) return g ? launch_general<kBackward, float, true>(p, st) : launch_general<kBackward, float, false>(p, st);
+    return g ? launch_general<kDweight, float, true>(p, st) : launch_general<kDweight, float, false>(p, st);
+  }
+  typedef __nv_bfloat16 B;
+  if (kind == kForward) return g ? launch_general<kForward, B, true>(p, st) : launch_general<kForward, B, false>(p, st);
+  if (kind == kBackward) return g ? launch_general<kBackward, B, true>(p, st) : launch_general<kBackward, B, false>(p, st);
+  return g ? launch_general<kDweight, B, true>(p, st) : launch_general<kDweight, B, false>(p, st);
+}
+
+cudaError_t run_bias_sums(const Problem& p, int32_t dtype, const void* add, const void* add_up, void* db, void* db_up, cudaStream_t st) {
+  const BiasArgs a{p.groups, p.n, p.gated, p.dw_f32, p.ld_y, p.y, add, add_up, db, db_up};
+  const dim3 grid((p.n + 31) / 32, p.groups.G, p.gated ? 2 : 1);
+  if (dtype == MCCE_F32) bias_kernel<float><<<grid, 1024, 0, st>>>(a);
+  else bias_kernel<__nv_bfloat16><<<grid, 1024, 0, st>>>(a);
+  return cudaGetLastError();
+}
+
+cudaError_t run_pack(const void* x, int32_t dtype, int64_t rows, int32_t d, int64_t ld_x, int64_t ld_q, uint8_t* q, uint8_t* scales,
+                     cudaStream_t st) {
+  const int per_row = (d + 31) / 32;
+  const int64_t blocks = rows * per_row, grid = (blocks + 7) / 8 < 148 * 16 ? (blocks + 7) / 8 : 148 * 16;
+  if (dtype == MCCE_F32) pack_kernel<<<(unsigned)grid, 256, 0, st>>>((const float*)x, q, scales, blocks, per_row, d, ld_x, ld_q);
+  else pack_kernel<<<(unsigned)grid, 256, 0, st>>>((const __nv_bfloat16*)x, q, scales, blocks, per_row, d, ld_x, ld_q);
+  return cudaGetLastError();
+}
+cudaError_t run_unpack(const uint8_t* q, const uint8_t* scales, int32_t dtype, int64_t rows, int32_t d, int64_t ld_x, int64_t ld_q, void* x,
+                       cudaStream_t st) {
+  const int per_row = (d + 31) / 32;
+  const int64_t blocks = rows * per_row, grid = (blocks + 7) / 8 < 148 * 16 ? (blocks + 7) / 8 : 148 * 16;
+  if (dtype == MCCE_F32) unpack_kernel<<<(unsigned)grid, 256, 0, st>>>(q, scales, (float*)x, blocks, per_row, d, ld_x, ld_q);
+  else unpack_kernel<<<(unsigned)grid, 256, 0, st>>>(q, scales, (__nv_bfloat16*)x, blocks, per_row, d, ld_x, ld_q);
+  return cudaGetLastError();
+}
+
+// ---- checks --------------------------------------------------------------------------------------------------------
+namespace {
+
+bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+int elem(int32_t dtype) { return dtype == MCCE_F32 ? 4 : dtype == MCCE_BF16 ? 2 : 1; }
+bool plain_type(int32_t t) { return t == MCCE_F32 || t == MCCE_BF16; }
+int64_t ld_or(int64_t ld, int64_t d) { return ld ? ld : d; }
+bool stride_ok(int64_t ld, int64_t d) { return ld == 0 || ld >= d; }
+
+bool sizes_ok(const mcce_linear* p) {
+  if (!p || p->n_layers < 1 || p->n_experts < 1 || (int64_t)p->n_layers * p->n_experts > MCCE_LINEAR_MAX_GROUPS) return false;
+  if (p->rows < 0 || p->rows > 0x7fffffffll || p->n_layers * p->rows > 0x7fffffffll) return false;
+  if (p->n < 1 || p->k < 1 || p->n > MCCE_LINEAR_MAX_WIDTH || p->k > MCCE_LINEAR_MAX_WIDTH) return false;
+  if (!plain_type(p->dtype) || (p->gated != 0 && p->gated != 1)) return false;
+  if (!stride_ok(p->ld_w, p->k)) return false;
+  const int64_t ld_w = ld_or(p->ld_w, p->k);
+  if (ld_w > (1ll << 40) || (p->step_w != 0 && p->step_w < (p->n - 1) * ld_w + p->k) || p->step_w > (1ll << 48)) return false;
+  return true;
+}
+bool act_ok(int32_t act) { return act == MCCE_ACT_NONE || act == MCCE_ACT_SILU || act == MCCE_ACT_GELU; }
+
+// All rows of the weights as one tensor for the comparison of addresses; matrices further apart than their rows count as solid.
+Span weight_span(const mcce_linear& p, const void* w, int e) {
+  const int64_t ld = ld_or(p.ld_w, p.k), step = p.step_w ? p.step_w : p.n * ld, G = (int64_t)p.n_layers * p.n_experts;
+  if (step == p.n * ld || G == 1) return row_span(w, G * p.n, ld, p.k, e);
+  if (ld == p.k) return row_span(w, G, step, p.n * ld, e);
+  return flat_span(w, (G - 1) * step + (p.n - 1) * ld + p.k, e);
+}
+Problem problem(const mcce_linear& p, const int32_t* offsets) {
+  Problem q{};
+  q.groups = {offsets, p.n_experts, p.n_layers * p.n_experts, p.rows};
+  q.n = p.n, q.k = p.k, q.gated = p.gated, q.L = p.n_layers;
+  q.ld_w = ld_or(p.ld_w, p.k), q.step_w = p.step_w ? p.step_w : p.n * q.ld_w;
+  return q;
+}
+int blocks_of(int64_t cols) { return (int)((cols + 31) / 32); }
+int code(cudaError_t e) { return e == cudaSuccess ? MCCE_OK : MCCE_ECUDA; }
+
+}  // namespace
+}  // namespace linear
+}  // namespace mcce
+
+using namespace mcce;
+using namespace mcce::linear;
+
+extern "C" int mcce_expert_linear(const mcce_linear* p, const void* x, const int32_t* offsets, const void* w, const void* w_up,
+                                  const void* bias, const void* bias_up, const void* add, void* out, void* saved, void* scales,
+                                  void* cuda_stream) {
+  if (!sizes_ok(p) || !act_ok(p->act)) return MCCE_EINVAL;
+  const int64_t width = (int64_t)p->n * (1 + p->gated), rows = p->n_layers * p->rows;
+  if (p->out_dtype != MCCE_F32 && p->out_dtype != p->dtype) return MCCE_EINVAL;
+  if (bias && p->bias_dtype != MCCE_F32 && p->bias_dtype != p->dtype) return MCCE_EINVAL;
+  if (saved && p->saved_dtype != p->dtype && p->saved_dtype != MCCE_E4M3) return MCCE_EINVAL;
+  const bool bytes = saved && p->saved_dtype == MCCE_E4M3;
+  if (!stride_ok(p->ld_x, p->k) || !stride_ok(p->ld_y, p->n) || (add && !stride_ok(p->ld_add, p->n)) ||
+      (saved && !stride_ok(p->ld_saved, width)))
+    return MCCE_EINVAL;
+  if ((w_up != nullptr) != (p->gated == 1) || (bias_up != nullptr) != (bias != nullptr && p->gated) || (scales != nullptr) != bytes)
+    return MCCE_EINVAL;
+  if (rows == 0) return MCCE_OK;
+  if (!x || !offsets || !w || !out) return MCCE_EINVAL;
+  const int e = elem(p->dtype), eo = elem(p->out_dtype), eb = elem(p->bias_dtype), es = bytes ? 1 : e;
+  if (!aligned(x, e) || !aligned(offsets, 4) || !aligned(w, e) || !aligned(w_up, e) || (bias && (!aligned(bias, eb) || !aligned(bias_up, eb))) ||
+      !aligned(add, eo) || !aligned(out, eo) || !aligned(saved, es))
+    return MCCE_EINVAL;
+  Problem q = problem(*p, offsets);
+  q.x = x, q.w = w, q.w_up = w_up;
+  q.ld_x = ld_or(p->ld_x, p->k);
+  ForwardArgs& f = q.fwd;
+  f.bias = bias, f.bias_up = bias_up, f.add = add, f.out = out, f.saved = saved, f.scales = (uint8_t*)scales;
+  f.ld_add = ld_or(p->ld_add, p->n), f.ld_out = ld_or(p->ld_y, p->n), f.ld_saved = ld_or(p->ld_saved, width);
+  f.bias_f32 = p->bias_dtype == MCCE_F32, f.out_f32 = p->out_dtype == MCCE_F32, f.act = p->act, f.n = p->n, f.blocks = blocks_of(p->n);
+  const int64_t G = q.groups.G;
+  const Span sx = row_span(x, rows, q.ld_x, p->k, e), soff = flat_span(offsets, (int64_t)p->n_layers * (p->n_experts + 1), 4);
+  const Span sw = weight_span(*p, w, e), swu = weight_span(*p, w_up, e);
+  const Span sb = flat_span(bias, G * p->n, eb), sbu = flat_span(bias_up, G * p->n, eb);
+  const Span sadd = row_span(add, rows, f.ld_add, p->n, eo), sout = row_span(out, rows, f.ld_out, p->n, eo);
+  const Span ssv = row_span(saved, rows, f.ld_saved, width, es), ssc = flat_span(scales, rows, (1 + p->gated) * (int64_t)f.blocks);
+  if (!same_or_apart(sout, sadd) || !apart(sout, {&sx, &soff, &sw, &swu, &sb, &sbu, &ssv, &ssc}) ||
+      !apart(ssv, {&sx, &soff, &sw, &swu, &sb, &sbu, &sadd, &ssc}) || !apart(ssc, {&sx, &soff, &sw, &swu, &sb, &sbu, &sadd}))
+    return MCCE_EINVAL;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  if (tensor_applicable(kForward, q, p->dtype)) return code(run_tensor(kForward, q, st));
+  return code(run_general(kForward, q, p->dtype, st));
+}
+
+extern "C" int mcce_expert_linear_backward(const mcce_linear* p, const void* dout, const int32_t* offsets, const void* w,
+                                           const void* w_up, const void* add, const void* saved, const void* scales, void* dx, void* h,
+                                           void* cuda_stream) {
+  if (!sizes_ok(p) || !act_ok(p->act) || p->below < 0 || p->below > 2) return MCCE_EINVAL;
+  const int64_t width = (int64_t)p->n * (1 + p->gated), wide = p->below == 2 ? 2ll * p->k : p->k, rows = p->n_layers * p->rows;
+  if (saved && p->saved_dtype != p->dtype && p->saved_dtype != MCCE_E4M3) return MCCE_EINVAL;
+  const bool bytes = saved && p->saved_dtype == MCCE_E4M3;
+  if (!stride_ok(p->ld_y, width) || !stride_ok(p->ld_x, wide) || (add && !stride_ok(p->ld_add, p->k)) ||
+      (saved && !stride_ok(p->ld_saved, wide)) || (h && !stride_ok(p->ld_h, p->k)))
+    return MCCE_EINVAL;
+  if ((w_up != nullptr) != (p->gated == 1) || (saved != nullptr) != (p->below > 0) || (scales != nullptr) != bytes) return MCCE_EINVAL;
+  if (p->below ? add != nullptr : (h != nullptr || p->act != MCCE_ACT_NONE)) return MCCE_EINVAL;
+  if (rows == 0) return MCCE_OK;
+  if (!dout || !offsets || !w || !dx) return MCCE_EINVAL;
+  const int e = elem(p->dtype), es = bytes ? 1 : e;
+  if (!aligned(dout, e) || !aligned(offsets, 4) || !aligned(w, e) || !aligned(w_up, e) || !aligned(add, e) || !aligned(saved, es) ||
+      !aligned(dx, e) || !aligned(h, e))
+    return MCCE_EINVAL;
+  Problem q = problem(*p, offsets);
+  q.y = dout, q.w = w, q.w_up = w_up;
+  q.ld_y = ld_or(p->ld_y, width);
+  BackwardArgs& b = q.bwd;
+  b.add = add, b.saved = saved, b.scales = (const uint8_t*)scales, b.dx = dx, b.h = h;
+  b.ld_add = ld_or(p->ld_add, p->k), b.ld_saved = ld_or(p->ld_saved, wide), b.ld_dx = ld_or(p->ld_x, wide), b.ld_h = ld_or(p->ld_h, p->k);
+  b.below = p->below, b.act = p->act, b.k = p->k, b.blocks = blocks_of(p->k);
+  const Span sy = row_span(dout, rows, q.ld_y, width, e), soff = flat_span(offsets, (int64_t)p->n_layers * (p->n_experts + 1), 4);
+  const Span sw = weight_span(*p, w, e), swu = weight_span(*p, w_up, e), sadd = row_span(add, rows, b.ld_add, p->k, e);
+  const Span ssv = row_span(saved, rows, b.ld_saved, wide, es);
+  const Span ssc = flat_span(scales, rows, (p->below == 2 ? 2 : 1) * (int64_t)b.blocks);
+  const Span sdx = row_span(dx, rows, b.ld_dx, wide, e), sh = row_span(h, rows, b.ld_h, p->k, e);
+  if (!same_or_apart(sdx, sadd) || !(bytes ? apart(sdx, {&ssv}) : same_or_apart(sdx, ssv)) || !apart(sdx, {&sy, &soff, &sw, &swu, &ssc, &sh}) ||
+      !apart(sh, {&sy, &soff, &sw, &swu, &sadd, &ssv, &ssc}))
+    return MCCE_EINVAL;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  if (tensor_applicable(kBackward, q, p->dtype)) return code(run_tensor(kBackward, q, st));
+  return code(run_general(kBackward, q, p->dtype, st));
+}
+
+extern "C" size_t mcce_expert_linear_dweight_workspace_bytes(const mcce_linear* p) {
+  if (!sizes_ok(p) || p->saved_dtype != MCCE_E4M3) return 0;
+  const int64_t ld = (p->k + 7) & ~7ll;
+  return (size_t)(p->n_layers * p->rows) * ld * elem(p->dtype);
+}
+
+extern "C" int mcce_expert_linear_dweight(const mcce_linear* p, const void* dout, const void* x, const void* scales,
+                                          const int32_t* offsets, const void* add_dw, const void* add_dw_up, const void* add_db,
+                                          const void* add_db_up, void* dw, void* dw_up, void* db, void* db_up, void* workspace,
+                                          size_t workspace_bytes, void* cuda_stream) {
+  if (!sizes_ok(p)) return MCCE_EINVAL;
+  const bool bytes = p->saved_dtype == MCCE_E4M3;
+  if (!bytes && p->saved_dtype != p->dtype) return MCCE_EINVAL;
+  const int64_t width = (int64_t)p->n * (1 + p->gated), rows = p->n_layers * p->rows;
+  if (p->out_dtype != MCCE_F32 && p->out_dtype != p->dtype) return MCCE_EINVAL;
+  if (!stride_ok(p->ld_y, width) || !stride_ok(p->ld_x, p->k)) return MCCE_EINVAL;
+  if (!dw || !offsets || (dw_up != nullptr) != (p->gated == 1) || (db_up != nullptr) != (db != nullptr && p->gated) ||
+      (scales != nullptr) != (bytes && rows > 0))
+    return MCCE_EINVAL;
+  if ((add_dw_up != nullptr) != (add_dw != nullptr && p->gated) || (add_db_up != nullptr) != (add_db != nullptr && p->gated) || (add_db && !db))
+    return MCCE_EINVAL;
+  if (rows && (!dout || !x)) return MCCE_EINVAL;
+  const int e = elem(p->dtype), eo = elem(p->out_dtype), ex = bytes ? 1 : e;
+  if (!aligned(dout, e) || !aligned(x, ex) || !aligned(offsets, 4) || !aligned(add_dw, eo) || !aligned(add_dw_up, eo) || !aligned(add_db, eo) ||
+      !aligned(add_db_up, eo) || !aligned(dw, eo) || !aligned(dw_up, eo) || !aligned(db, eo) || !aligned(db_up, eo))
+    return MCCE_EINVAL;
+  const size_t need = mcce_expert_linear_dweight_workspace_bytes(p);
+  if (need && (!workspace || !aligned(workspace, 16))) return MCCE_EINVAL;
+  if (workspace_bytes < need) return MCCE_ENOSPC;
+  Problem q = problem(*p, offsets);
+  const int64_t G = q.groups.G;
+  q.y = dout, q.x = x, q.ld_y = ld_or(p->ld_y, width), q.ld_x = ld_or(p->ld_x, p->k);
+  q.dw = dw, q.dw_up = dw_up, q.add_dw = add_dw, q.add_dw_up = add_dw_up, q.dw_f32 = p->out_dtype == MCCE_F32;
+  q.dw_wide = aligned(dw, 16) && aligned(dw_up, 16) && aligned(add_dw, 16) && aligned(add_dw_up, 16) && q.ld_w * eo % 16 == 0 && q.step_w * eo % 16 == 0;
+  const Span sy = row_span(dout, rows, q.ld_y, width, e), sx = row_span(x, rows, q.ld_x, p->k, ex);
+  const Span ssc = flat_span(scales, rows, blocks_of(p->k)), soff = flat_span(offsets, (int64_t)p->n_layers * (p->n_experts + 1), 4);
+  const Span saw = weight_span(*p, add_dw, eo), sawu = weight_span(*p, add_dw_up, eo), sab = flat_span(add_db, G * p->n, eo);
+  const Span sabu = flat_span(add_db_up, G * p->n, eo), sdw = weight_span(*p, dw, eo), sdwu = weight_span(*p, dw_up, eo);
+  const Span sdb = flat_span(db, G * p->n, eo), sdbu = flat_span(db_up, G * p->n, eo), sws = flat_span(need ? workspace : nullptr, need);
+  if (!same_or_apart(sdw, saw) || !same_or_apart(sdwu, sawu) || !same_or_apart(sdb, sab) || !same_or_apart(sdbu, sabu) ||
+      !apart(sdw, {&sy, &sx, &ssc, &soff, &sawu, &sab, &sabu, &sdwu, &sdb, &sdbu}) ||
+      !apart(sdwu, {&sy, &sx, &ssc, &soff, &saw, &sab, &sabu, &sdb, &sdbu}) || !apart(sdb, {&sy, &sx, &ssc, &soff, &saw, &sawu, &sabu, &sdbu}) ||
+      !apart(sdbu, {&sy, &sx, &ssc, &soff, &saw, &sawu, &sab}) ||
+      !apart(sws, {&sy, &sx, &ssc, &soff, &saw, &sawu, &sab, &sabu, &sdw, &sdwu, &sdb, &sdbu}))
+    return MCCE_EINVAL;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  if (bytes && rows) {
+    const int64_t ld = (p->k + 7) & ~7ll;
+    const cudaError_t err = run_unpack((const uint8_t*)x, (const uint8_t*)scales, p->dtype, rows, p->k, ld, q.ld_x, workspace, st);
+    if (err != cudaSuccess) return MCCE_ECUDA;
+    q.x = workspace, q.ld_x = ld;
+  }
+  cudaError_t err = tensor_applicable(kDweight, q, p->dtype) ? run_tensor(kDweight, q, st) : run_general(kDweight, q, p->dtype, st);
+  if (err == cudaSuccess && db) err = run_bias_sums(q, p->dtype, add_db, add_db_up, db, db_up, st);
+  return code(err);
+}
+
+static bool checkpoint_ok(const void* x, int32_t dtype, int64_t rows, int32_t d, int64_t ld_x, int64_t ld_q, const void* q, const void* scales) {
+  if (!plain_type(dtype) || rows < 0 || rows > 0x7fffffffll || d < 1 || d > MCCE_LINEAR_MAX_WIDTH || !stride_ok(ld_x, d) || !stride_ok(ld_q, d))
+    return false;
+  return rows == 0 || (x && q && scales && aligned(x, elem(dtype)));
+}
+
+extern "C" int mcce_checkpoint_pack(const void* x, int32_t dtype, int64_t rows, int32_t d, int64_t ld_x, int64_t ld_q, void* q, void* scales,
+                                    void* cuda_stream) {
+  if (!checkpoint_ok(x, dtype, rows, d, ld_x, ld_q, q, scales)) return MCCE_EINVAL;
+  if (rows == 0) return MCCE_OK;
+  const Span sx = row_span(x, rows, ld_or(ld_x, d), d, elem(dtype)), sq = row_span(q, rows, ld_or(ld_q, d), d, 1);
+  const Span ssc = flat_span(scales, rows, blocks_of(d));
+  if (!apart(sq, {&sx, &ssc}) || !apart(ssc, {&sx})) return MCCE_EINVAL;
+  return code(run_pack(x, dtype, rows, d, ld_or(ld_x, d), ld_or(ld_q, d), (uint8_t*)q, (uint8_t*)scales, (cudaStream_t)cuda_stream));
+}
+
+extern "C" int mcce_checkpoint_unpack(const void* q, const void* scales, int32_t dtype, int64_t rows, int32_t d, int64_t ld_x, int64_t ld_q,
+                                      void* x, void* cuda_stream) {
+  if (!checkpoint_ok(x, dtype, rows, d, ld_x, ld_q, q, scales)) return MCCE_EINVAL;
+  if (rows == 0) return MCCE_OK;
+  const Span sx = row_span(x, rows, ld_or(ld_x, d), d, elem(dtype)), sq = row_span(q, rows, ld_or(ld_q, d), d, 1);
+  const Span ssc = flat_span(scales, rows, blocks_of(d));
+  if (!apart(sx, {&sq, &ssc})) return MCCE_EINVAL;
+  return code(run_unpack((const uint8_t*)q, (const uint8_t*)scales, dtype, rows, d, ld_or(ld_x, d), ld_or(ld_q, d), x, (cudaStream_t)cuda_stream));
+}

@@ -13,6 +13,8 @@
 
 #include <stdexcept>
 #include <string>
+#include <tuple>
+#include <utility>
 
 #include "mcce.h"
 
@@ -25,6 +27,12 @@ decltype(&mcce_dispatch_workspace_bytes) p_dispatch_workspace_bytes;
 decltype(&mcce_dispatch) p_dispatch;
 decltype(&mcce_combine) p_combine;
 decltype(&mcce_combine_backward) p_combine_backward;
+decltype(&mcce_expert_linear) p_expert_linear;
+decltype(&mcce_expert_linear_backward) p_expert_linear_backward;
+decltype(&mcce_expert_linear_dweight_workspace_bytes) p_expert_linear_dweight_workspace_bytes;
+decltype(&mcce_expert_linear_dweight) p_expert_linear_dweight;
+decltype(&mcce_checkpoint_pack) p_checkpoint_pack;
+decltype(&mcce_checkpoint_unpack) p_checkpoint_unpack;
 decltype(&mcce_strerror) p_strerror;
 PyObject* error_class = nullptr;
 
@@ -295,6 +303,194 @@ void run_combine_backward(PyObject* const* a) {
   changed({&dr, dw});
 }
 
+// Sizes of the experts' products: weights [(L,)E,n,k] with evenly spaced matrices and rows
+struct Experts {
+  int64_t L, E, R, n, k;
+  bool layers;
+  int dev;
+  Experts(const at::Tensor& w, const at::Tensor& rows, const at::Tensor& offsets, const char* what) : dev(cuda_device(w)) {
+    if (w.dim() != 3 && w.dim() != 4) refuse(std::string(what) + " must be [E,n,k] or [L,E,n,k]");
+    layers = w.dim() == 4, L = layers ? w.size(0) : 1, E = w.size(-3), n = w.size(-2), k = w.size(-1);
+    need(L >= 1 && E >= 1 && n >= 1 && k >= 1, "weights without elements");
+    if (rows.dim() != w.dim() - 1) refuse(std::string("rows must be [R,columns], or [L,R,columns] where ") + what + " has layers");
+    R = rows.size(-2);
+    dense(&offsets, layers ? at::IntArrayRef{L, E + 1} : at::IntArrayRef{E + 1}, at::kInt, dev, "offsets");
+  }
+  c10::SmallVector<int64_t, 3> rows(int64_t cols) const {
+    if (layers) return {L, R, cols};
+    return {R, cols};
+  }
+  c10::SmallVector<int64_t, 4> weights() const {
+    if (layers) return {L, E, n, k};
+    return {E, n, k};
+  }
+  c10::SmallVector<int64_t, 3> biases() const {
+    if (layers) return {L, E, n};
+    return {E, n};
+  }
+  mcce_linear describe(int32_t type) const {
+    mcce_linear p{};
+    p.n_layers = i32(L, "L"), p.n_experts = i32(E, "E"), p.rows = R, p.n = i32(n, "n"), p.k = i32(k, "k");
+    p.dtype = p.out_dtype = p.bias_dtype = p.saved_dtype = type;
+    return p;
+  }
+  // strides of a row and of a matrix
+  std::pair<int64_t, int64_t> strides(const at::Tensor& t, const char* what) const {
+    placed(t, weights(), dev, what);
+    const int64_t d = t.dim();
+    if (k > 1 && t.stride(d - 1) != 1) refuse(std::string(what) + ": the columns of a row must be contiguous");
+    const int64_t ld = n > 1 ? t.stride(d - 2) : k;
+    const int64_t step = E > 1 ? t.stride(d - 3) : L > 1 ? t.stride(0) : n * ld;
+    if (L > 1 && E > 1 && t.stride(0) != E * step) refuse(std::string(what) + ": matrices must be evenly spaced");
+    if (ld < k || step < (n - 1) * ld + k) refuse(std::string(what) + ": rows or matrices overlap");
+    return {ld, step};
+  }
+  void alike(const at::Tensor* t, const at::Tensor& first, const char* what) const {
+    if (!t) return;
+    if (t->scalar_type() != first.scalar_type() || strides(*t, what) != strides(first, what))
+      refuse(std::string(what) + ": both matrices of a layer, and what is added to gradients, must have the same type and strides");
+  }
+};
+int64_t blocks(int64_t cols) { return ceil_div(cols, 32); }
+// What is kept for the backward pass and, where it holds 8 bits, its scales; `halves` of `cols` columns
+int32_t saved_type(const at::Tensor& saved, const at::Tensor* scales, const at::Tensor& like, const Experts& s, int64_t halves, int64_t cols,
+                   const char* what) {
+  if (saved.scalar_type() == at::kFloat8_e4m3fn) {
+    if (!scales) refuse(std::string(what) + " in 8 bits needs scales");
+    dense(scales, s.rows(halves * blocks(cols)), at::kFloat8_e8m0fnu, s.dev, "scales");
+    return MCCE_E4M3;
+  }
+  if (scales || saved.scalar_type() != like.scalar_type())
+    refuse(std::string(what) + " must have the type of the rows, or be float8_e4m3fn with scales");
+  return code(saved, what);
+}
+int32_t number(PyObject* o) {
+  const long v = PyLong_AsLong(o);
+  if (PyErr_Occurred()) throw python_error();
+  return i32(v, "act");
+}
+
+// expert_linear(x, offsets, w, w_up, bias, bias_up, act, add, out, saved, scales)
+void run_expert_linear(PyObject* const* a) {
+  const at::Tensor &x = given(a[0], "x"), &off = given(a[1], "offsets"), &w = given(a[2], "w"), &out = given(a[8], "out");
+  const at::Tensor *wu = tensor(a[3], "w_up"), *b = tensor(a[4], "bias"), *bu = tensor(a[5], "bias_up"), *add = tensor(a[7], "add");
+  const at::Tensor *saved = tensor(a[9], "saved"), *scales = tensor(a[10], "scales");
+  const Experts s(w, x, off, "w");
+  mcce_linear p = s.describe(code(x, "x"));
+  p.gated = wu != nullptr, p.act = number(a[6]);
+  need(w.scalar_type() == x.scalar_type(), "w must have the type of x");
+  s.alike(wu, w, "w_up");
+  std::tie(p.ld_w, p.step_w) = s.strides(w, "w");
+  p.ld_x = ld(&x, s.rows(s.k), s.dev, "x"), p.ld_y = ld(&out, s.rows(s.n), s.dev, "out");
+  p.out_dtype = code(out, "out");
+  if (b) {
+    p.bias_dtype = code(*b, "bias");
+    dense(b, s.biases(), b->scalar_type(), s.dev, "bias");
+    dense(bu, s.biases(), b->scalar_type(), s.dev, "bias_up");
+  } else {
+    need(!bu, "bias_up without bias");
+  }
+  if (add) {
+    need(add->scalar_type() == out.scalar_type(), "add must have the type of out");
+    p.ld_add = ld(add, s.rows(s.n), s.dev, "add");
+  }
+  if (saved) {
+    p.saved_dtype = saved_type(*saved, scales, x, s, 1 + p.gated, s.n, "saved");
+    p.ld_saved = ld(saved, s.rows((1 + p.gated) * s.n), s.dev, "saved");
+  } else {
+    need(!scales, "scales without saved");
+  }
+  Where on(s.dev);
+  done(p_expert_linear(&p, x.data_ptr(), (const int32_t*)off.data_ptr(), w.data_ptr(), at_(wu), at_(b), at_(bu), at_(add), out.data_ptr(),
+                       at_(saved), at_(scales), on.stream));
+  changed({&out, saved, scales});
+}
+
+// expert_linear_backward(dout, offsets, w, w_up, act, add, saved, scales, dx, h)
+void run_expert_linear_backward(PyObject* const* a) {
+  const at::Tensor &g = given(a[0], "dout"), &off = given(a[1], "offsets"), &w = given(a[2], "w"), &dx = given(a[8], "dx");
+  const at::Tensor *wu = tensor(a[3], "w_up"), *add = tensor(a[5], "add"), *saved = tensor(a[6], "saved"), *scales = tensor(a[7], "scales"),
+                   *h = tensor(a[9], "h");
+  const Experts s(w, g, off, "w");
+  mcce_linear p = s.describe(code(g, "dout"));
+  p.gated = wu != nullptr, p.act = number(a[4]);
+  need(w.scalar_type() == g.scalar_type() && dx.scalar_type() == g.scalar_type() && (!add || add->scalar_type() == g.scalar_type()) &&
+           (!h || h->scalar_type() == g.scalar_type()),
+       "w, add, dx and h must have the type of dout");
+  s.alike(wu, w, "w_up");
+  std::tie(p.ld_w, p.step_w) = s.strides(w, "w");
+  p.ld_y = ld(&g, s.rows((1 + p.gated) * s.n), s.dev, "dout");
+  if (saved) {
+    need(saved->dim() >= 1 && (saved->size(-1) == s.k || saved->size(-1) == 2 * s.k), "saved must have the columns of the input, or twice as many");
+    p.below = (int32_t)(saved->size(-1) / s.k);
+    p.saved_dtype = saved_type(*saved, scales, g, s, p.below, s.k, "saved");
+    p.ld_saved = ld(saved, s.rows(p.below * s.k), s.dev, "saved");
+  } else {
+    need(!scales, "scales without saved");
+  }
+  p.ld_add = ld(add, s.rows(s.k), s.dev, "add"), p.ld_h = ld(h, s.rows(s.k), s.dev, "h");
+  p.ld_x = ld(&dx, s.rows(p.below == 2 ? 2 * s.k : s.k), s.dev, "dx");
+  Where on(s.dev);
+  done(p_expert_linear_backward(&p, g.data_ptr(), (const int32_t*)off.data_ptr(), w.data_ptr(), at_(wu), at_(add), at_(saved), at_(scales),
+                                dx.data_ptr(), at_(h), on.stream));
+  changed({&dx, h});
+}
+
+// expert_linear_dweight(dout, x, scales, offsets, add_dw, add_dw_up, add_db, add_db_up, dw, dw_up, db, db_up)
+void run_expert_linear_dweight(PyObject* const* a) {
+  const at::Tensor &g = given(a[0], "dout"), &x = given(a[1], "x"), &off = given(a[3], "offsets"), &dw = given(a[8], "dw");
+  const at::Tensor *scales = tensor(a[2], "scales"), *adw = tensor(a[4], "add.dw"), *adwu = tensor(a[5], "add.dw_up"),
+                   *adb = tensor(a[6], "add.db"), *adbu = tensor(a[7], "add.db_up"), *dwu = tensor(a[9], "dw_up"), *db = tensor(a[10], "db"),
+                   *dbu = tensor(a[11], "db_up");
+  const Experts s(dw, g, off, "dw");
+  mcce_linear p = s.describe(code(g, "dout"));
+  p.gated = dwu != nullptr, p.out_dtype = code(dw, "dw");
+  s.alike(dwu, dw, "dw_up"), s.alike(adw, dw, "add.dw"), s.alike(adwu, dw, "add.dw_up");
+  std::tie(p.ld_w, p.step_w) = s.strides(dw, "dw");
+  for (const at::Tensor* t : {db, dbu, adb, adbu}) dense(t, s.biases(), dw.scalar_type(), s.dev, "db");
+  p.ld_y = ld(&g, s.rows((1 + p.gated) * s.n), s.dev, "dout"), p.ld_x = ld(&x, s.rows(s.k), s.dev, "x");
+  p.saved_dtype = saved_type(x, scales, g, s, 1, s.k, "x");
+  Where on(s.dev);
+  at::Tensor ws;
+  const size_t bytes = p_expert_linear_dweight_workspace_bytes(&p);
+  if (bytes) ws = workspace(bytes, g);
+  done(p_expert_linear_dweight(&p, g.data_ptr(), x.data_ptr(), s.R ? at_(scales) : nullptr, (const int32_t*)off.data_ptr(), at_(adw), at_(adwu),
+                               at_(adb), at_(adbu), dw.data_ptr(), at_(dwu), at_(db), at_(dbu), bytes ? ws.data_ptr() : nullptr, bytes,
+                               on.stream));
+  changed({&dw, dwu, db, dbu});
+}
+
+struct Flat {
+  int64_t rows, d, ld_x, ld_q;
+  int dev;
+  int32_t type;
+  Flat(const at::Tensor& x, const at::Tensor& q, const at::Tensor& scales) : dev(cuda_device(x)), type(code(x, "x")) {
+    need(x.dim() >= 1 && x.size(-1) >= 1, "x must have columns");
+    d = x.size(-1), rows = x.numel() / d;
+    need(q.scalar_type() == at::kFloat8_e4m3fn, "q must be float8_e4m3fn");
+    auto shape = x.sizes().vec();
+    ld_x = ld(&x, x.sizes(), dev, "x"), ld_q = ld(&q, x.sizes(), dev, "q");
+    shape.back() = blocks(d);
+    dense(&scales, shape, at::kFloat8_e8m0fnu, dev, "scales");
+  }
+};
+// checkpoint_pack(x, q, scales)
+void run_checkpoint_pack(PyObject* const* a) {
+  const at::Tensor &x = given(a[0], "x"), &q = given(a[1], "q"), &scales = given(a[2], "scales");
+  const Flat f(x, q, scales);
+  Where on(f.dev);
+  done(p_checkpoint_pack(x.data_ptr(), f.type, f.rows, i32(f.d, "the width"), f.ld_x, f.ld_q, q.data_ptr(), scales.data_ptr(), on.stream));
+  changed({&q, &scales});
+}
+// checkpoint_unpack(q, scales, x)
+void run_checkpoint_unpack(PyObject* const* a) {
+  const at::Tensor &q = given(a[0], "q"), &scales = given(a[1], "scales"), &x = given(a[2], "x");
+  const Flat f(x, q, scales);
+  Where on(f.dev);
+  done(p_checkpoint_unpack(q.data_ptr(), scales.data_ptr(), f.type, f.rows, i32(f.d, "the width"), f.ld_x, f.ld_q, x.data_ptr(), on.stream));
+  changed({&x});
+}
+
 template <void (*RUN)(PyObject* const*), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -312,16 +508,18 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// connect(error class, addresses of the eight functions above in their order)
+// connect(error class, addresses of the functions above in their order)
 PyObject* connect(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  void** const to[8] = {(void**)&p_rmsnorm, (void**)&p_rmsnorm_backward_workspace_bytes, (void**)&p_rmsnorm_backward,
-                        (void**)&p_dispatch_workspace_bytes, (void**)&p_dispatch, (void**)&p_combine, (void**)&p_combine_backward,
-                        (void**)&p_strerror};
-  if (n != 9) {
+  void** const to[] = {(void**)&p_rmsnorm, (void**)&p_rmsnorm_backward_workspace_bytes, (void**)&p_rmsnorm_backward,
+                       (void**)&p_dispatch_workspace_bytes, (void**)&p_dispatch, (void**)&p_combine, (void**)&p_combine_backward,
+                       (void**)&p_expert_linear, (void**)&p_expert_linear_backward, (void**)&p_expert_linear_dweight_workspace_bytes,
+                       (void**)&p_expert_linear_dweight, (void**)&p_checkpoint_pack, (void**)&p_checkpoint_unpack, (void**)&p_strerror};
+  constexpr int kFunctions = sizeof(to) / sizeof(to[0]);
+  if (n != 1 + kFunctions) {
     PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
     return nullptr;
   }
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < kFunctions; ++i) {
     *to[i] = PyLong_AsVoidPtr(args[1 + i]);
     if (PyErr_Occurred()) return nullptr;
   }
@@ -338,6 +536,13 @@ PyMethodDef methods[] = {
     {"dispatch", FAST((entry<run_dispatch, 9>)), "dispatch(sel_idx, n_experts, x, scales, offsets, perm, inv, rows, row_scales)"},
     {"combine", FAST((entry<run_combine, 5>)), "combine(rows, inv, sel_w, add, out)"},
     {"combine_backward", FAST((entry<run_combine_backward, 6>)), "combine_backward(dy, rows, inv, sel_w, drows, dw)"},
+    {"expert_linear", FAST((entry<run_expert_linear, 11>)), "expert_linear(x, offsets, w, w_up, bias, bias_up, act, add, out, saved, scales)"},
+    {"expert_linear_backward", FAST((entry<run_expert_linear_backward, 10>)),
+     "expert_linear_backward(dout, offsets, w, w_up, act, add, saved, scales, dx, h)"},
+    {"expert_linear_dweight", FAST((entry<run_expert_linear_dweight, 12>)),
+     "expert_linear_dweight(dout, x, scales, offsets, add_dw, add_dw_up, add_db, add_db_up, dw, dw_up, db, db_up)"},
+    {"checkpoint_pack", FAST((entry<run_checkpoint_pack, 3>)), "checkpoint_pack(x, q, scales)"},
+    {"checkpoint_unpack", FAST((entry<run_checkpoint_unpack, 3>)), "checkpoint_unpack(q, scales, x)"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Marshalling of torch tensors to the C ABI of mcce.h", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
