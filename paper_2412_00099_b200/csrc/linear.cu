@@ -123,10 +123,21 @@ __global__ void __launch_bounds__(256) general_kernel(const Problem p) {
         }
       } else if (KIND == kForward) {
         const Forward<T, GATED> e(p.fwd, g, j0 + jj + lane);
-        for (int i = warp; i < I; i += 8) e.store(row0 + i, col[i * 65], kSets == 2 ? col[(kTile + i) * 65] : 0.f, e.load(row0 + i));
+        float z[8], up[8] = {};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          z[i] = col[(warp * 8 + i) * 65];
+          if (kSets == 2) up[i] = col[(kTile + warp * 8 + i) * 65];
+        }
+        e.rows(row0 + warp * 8, I - warp * 8, z, up);
       } else {
         const Backward<T> e(p.bwd, g, j0 + jj + lane);
-        for (int i = warp; i < I; i += 8) e.store(row0 + i, col[i * 65], 0.f, e.load(row0 + i));
+        typename Backward<T>::template Asked<8> q;
+        float v[8];
+        e.ask(row0 + warp * 8, I - warp * 8, q);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = col[(warp * 8 + i) * 65];
+        e.rows(row0 + warp * 8, I - warp * 8, v, q);
       }
     }
     __syncthreads();
@@ -198,7 +209,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const T* x, uint8_t* q, uint8
     const int j = (int)(b % per_row) * 32 + lane;
     const float v = j < d ? load_as_float(x + row * ld_x + j) : 0.f;
     const uint32_t s = warp_block_scale(v);
-    if (j < d) q[row * ld_q + j] = to_e4m3(v, s);
+    if (j < d) q[row * ld_q + j] = (uint8_t)to_e4m3x2(v * scale_inverse(s), 0.f);
     if (lane == 0) scales[b] = (uint8_t)s;
   }
 }
@@ -209,7 +220,7 @@ __global__ void __launch_bounds__(256) unpack_kernel(const uint8_t* q, const uin
   for (int64_t b = blockIdx.x * 8ll + (threadIdx.x >> 5); b < blocks; b += gridDim.x * 8ll) {
     const int64_t row = b / per_row;
     const int j = (int)(b % per_row) * 32 + lane;
-    if (j < d) store_as(x + row * ld_x + j, e4m3_value(q[row * ld_q + j]) * scale_value(scales[b]));
+    if (j < d) store_as(x + row * ld_x + j, e4m3x2_value(q[row * ld_q + j], 0u).x * scale_value(scales[b]));
   }
 }
 

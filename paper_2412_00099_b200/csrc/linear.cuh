@@ -45,19 +45,12 @@ __device__ __forceinline__ float sigmoid(float z) {
   return 1.f / (1.f + expf(-z));
 }
 template <bool FAST>
-__device__ __forceinline__ float act_value(float z, int act) {
-  if (act == MCCE_ACT_SILU) return z * sigmoid<FAST>(z);
-  if (act == MCCE_ACT_GELU) return z * normcdff(z);
-  return z;
-}
-template <bool FAST>
-__device__ __forceinline__ void act_value_and_slope(float z, int act, float& value, float& slope) {
+__device__ __forceinline__ void slope_and_value(float z, int act, float& value, float& slope) {
   if (act == MCCE_ACT_SILU) {
     const float s = sigmoid<FAST>(z);
     value = z * s, slope = s * (1.f + z * (1.f - s));
   } else if (act == MCCE_ACT_GELU) {
-    const float p = normcdff(z);
-    const float q = z * z * -0.5f;
+    const float p = normcdff(z), q = z * z * -0.5f;
     value = z * p, slope = p + z * (0.3989422804014327f * (FAST ? __expf(q) : expf(q)));
   } else {
     value = z, slope = 1.f;
@@ -74,17 +67,19 @@ __device__ __forceinline__ uint32_t block_scale(uint32_t largest_bits) {
   const int b = (int)e - 8 + ((largest_bits & 0x7fffffu) > 0x600000u ? 1 : 0);
   return b > 0 ? (uint32_t)b : 0u;
 }
-__device__ __forceinline__ uint8_t to_e4m3(float v, uint32_t scale) {
-  if (scale == 255u) return 0x7f;
-  return (uint8_t)__nv_cvt_float_to_fp8(v * __uint_as_float((254u - scale) << 23), __NV_SATFINITE, __NV_E4M3);
-}
+__device__ __forceinline__ float scale_inverse(uint32_t scale) { return __uint_as_float(scale == 255u ? 0x7fffffffu : (254u - scale) << 23); }
 __device__ __forceinline__ float scale_value(uint32_t scale) {
   return __uint_as_float(scale == 255u ? 0x7fffffffu : scale == 0u ? 0x00400000u : scale << 23);
 }
-__device__ __forceinline__ float e4m3_value(uint8_t q) {
-  return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)q, __NV_E4M3)));
+// Two quotients by their scales: e4m3 in the low and the high byte
+__device__ __forceinline__ uint32_t to_e4m3x2(float low, float high) {
+  return __nv_cvt_float2_to_fp8x2(make_float2(low, high), __NV_SATFINITE, __NV_E4M3);
 }
-// The same for a column per lane of a whole warp; lanes without one hand in 0.
+__device__ __forceinline__ float2 e4m3x2_value(uint32_t low, uint32_t high) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(low | high << 8), __NV_E4M3);
+  return __half22float2(__half2(h));
+}
+// The scale of the values that a whole warp holds, a column per lane; lanes without one hand in 0.
 __device__ __forceinline__ uint32_t warp_block_scale(float v) {
   return block_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu));
 }
@@ -107,13 +102,10 @@ struct BackwardArgs {
   int32_t below, act, k, blocks;   // below: 0 none, 1 an activation, 2 a gated one
 };
 
-// Forward: z (and the gated layer's second sum) of one row, column f of this lane.  `pre` holds what is read, so that a caller can
-// ask for several rows' values before it waits for the first.
+// N rows from `row` on, of which `left` count, in column f of this lane: z, and z_up of a gated layer.  A warp calls it as a whole; the N rows'
+// loads, sums and stores are independent of one another, so that none waits for the row before it.
 template <typename T, bool GATED>
 struct Forward {
-  struct Pre {
-    float add;
-  };
   const ForwardArgs& a;
   float b = 0.f, b_up = 0.f;
   int f;
@@ -122,83 +114,172 @@ struct Forward {
     if (a.bias && on) {
       const int64_t i = (int64_t)group * a.n + f;
       b = a.bias_f32 ? ((const float*)a.bias)[i] : load_as_float((const T*)a.bias + i);
-      if (GATED && a.bias_up) b_up = a.bias_f32 ? ((const float*)a.bias_up)[i] : load_as_float((const T*)a.bias_up + i);
+      if (GATED) b_up = a.bias_f32 ? ((const float*)a.bias_up)[i] : load_as_float((const T*)a.bias_up + i);
     }
   }
-  __device__ __forceinline__ Pre load(int64_t row) const {
-    Pre p{0.f};
-    if (a.add && on) p.add = a.out_f32 ? ((const float*)a.add)[row * a.ld_add + f] : load_as_float((const T*)a.add + row * a.ld_add + f);
-    return p;
-  }
-  __device__ __forceinline__ void keep(int64_t row, float z, int half) const {
-    if (a.scales) {
-      const uint32_t s = warp_block_scale(on ? z : 0.f);
-      if (on) ((uint8_t*)a.saved)[row * a.ld_saved + half * a.n + f] = to_e4m3(z, s);
-      if ((f & 31) == 0 && on) a.scales[row * (GATED ? 2 * a.blocks : a.blocks) + half * a.blocks + (f >> 5)] = (uint8_t)s;
-    } else if (on) {
-      store_as((T*)a.saved + row * a.ld_saved + half * a.n + f, z);
+  template <int N>
+  __device__ __forceinline__ void keep8(int64_t row, int left, const float (&z)[N], int half) const {
+    uint32_t s[N], mine = 0u;
+#pragma unroll
+    for (int j = 0; j < N; ++j) s[j] = warp_block_scale(on ? z[j] : 0.f);
+    uint8_t* q = (uint8_t*)a.saved + row * a.ld_saved + half * a.n + f;
+    uint32_t bytes[(N + 1) / 2];
+#pragma unroll
+    for (int j = 0; j < N; j += 2)
+      bytes[j / 2] = to_e4m3x2(z[j] * scale_inverse(s[j]), j + 1 < N ? z[j + 1 < N ? j + 1 : j] * scale_inverse(s[j + 1 < N ? j + 1 : j]) : 0.f);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if (on && j < left) q[j * a.ld_saved] = (uint8_t)(bytes[j / 2] >> (8 * (j & 1)));
+      if (j == (f & 31)) mine = s[j];
     }
+    // lane j has row j's scale
+    const int first = f & ~31, stride = GATED ? 2 * a.blocks : a.blocks, j = f & 31;
+    if (first < a.n && j < N && j < left) a.scales[(row + j) * stride + half * a.blocks + (first >> 5)] = (uint8_t)mine;
   }
-  __device__ __forceinline__ void store(int64_t row, float z, float z_up, const Pre& p) const {
+  template <int N>
+  __device__ __forceinline__ void keep(int64_t row, int left, const float (&z)[N], int half) const {
+    if (a.scales) return keep8(row, left, z, half);
+    T* o = (T*)a.saved + row * a.ld_saved + half * a.n + f;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (on && j < left) store_as(o + j * a.ld_saved, z[j]);
+  }
+  template <int N, typename O>
+  __device__ __forceinline__ void finish(int64_t row, int left, float (&z)[N], float (&up)[N]) const {
     constexpr bool kFast = sizeof(T) == 2;
-    z += b;
-    if (GATED) z_up += b_up;
-    if (a.saved) {
-      keep(row, z, 0);
-      if (GATED) keep(row, z_up, 1);
+    float add[N] = {};
+    if (a.add) {
+      const O* p = (const O*)a.add + row * a.ld_add + f;
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (on && j < left) add[j] = load_as_float(p + j * a.ld_add);
     }
-    float y = act_value<kFast>(z, a.act);
-    if (GATED) y *= z_up;
-    y += p.add;
-    if (!on) return;
-    if (a.out_f32) ((float*)a.out)[row * a.ld_out + f] = y;
-    else store_as((T*)a.out + row * a.ld_out + f, y);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      z[j] += b;
+      if (GATED) up[j] += b_up;
+    }
+    if (a.saved) {
+      keep(row, left, z, 0);
+      if (GATED) keep(row, left, up, 1);
+    }
+    if (a.act == MCCE_ACT_SILU) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) z[j] *= sigmoid<kFast>(z[j]);
+    } else if (a.act == MCCE_ACT_GELU) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) z[j] *= normcdff(z[j]);
+    }
+    O* o = (O*)a.out + row * a.ld_out + f;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (on && j < left) store_as(o + j * a.ld_out, (GATED ? z[j] * up[j] : z[j]) + add[j]);
+  }
+  template <int N>
+  __device__ __forceinline__ void rows(int64_t row, int left, float (&z)[N], float (&up)[N]) const {
+    if (a.out_f32) finish<N, float>(row, left, z, up);
+    else finish<N, T>(row, left, z, up);
   }
 };
 
+// The same for a gradient with respect to rows, t[N], in two steps: `ask` reads what the layer below kept (or what is added),
+// `rows` uses it, so that a caller can wait for its sums in between.
 template <typename T>
 struct Backward {
-  struct Pre {
-    float z, up;   // what is added instead of z where no layer lies below
-  };
   const BackwardArgs& a;
   int f;
   bool on;
   __device__ __forceinline__ Backward(const BackwardArgs& a_, int, int f_) : a(a_), f(f_), on(f_ < a_.k) {}
-  __device__ __forceinline__ float saved_at(int64_t row, int half) const {
-    const int64_t i = row * a.ld_saved + half * a.k + f;
-    if (!a.scales) return load_as_float((const T*)a.saved + i);
-    return e4m3_value(((const uint8_t*)a.saved)[i]) *
-           scale_value(a.scales[row * (a.below == 2 ? 2 * a.blocks : a.blocks) + half * a.blocks + (f >> 5)]);
-  }
-  __device__ __forceinline__ Pre load(int64_t row) const {
-    Pre p{0.f, 0.f};
-    if (!on) return p;
-    if (a.below) {
-      p.z = saved_at(row, 0);
-      if (a.below == 2) p.up = saved_at(row, 1);
+  template <int N>
+  struct Asked {
+    uint32_t z[N], up[N], scales[N];   // as they lie in memory; scales: z's in the low byte, up's in the next
+  };
+  __device__ __forceinline__ uint32_t raw(const float* p) const { return __float_as_uint(*p); }
+  __device__ __forceinline__ uint32_t raw(const __nv_bfloat16* p) const { return *(const uint16_t*)p; }
+  __device__ __forceinline__ float value(uint32_t v) const { return __uint_as_float(sizeof(T) == 2 ? v << 16 : v); }
+  template <int N>
+  __device__ __forceinline__ void ask(int64_t row, int left, Asked<N>& q) const {
+#pragma unroll
+    for (int j = 0; j < N; ++j) q.z[j] = q.up[j] = q.scales[j] = 0u;
+    if (!on) return;
+    if (a.below && a.scales) {
+      const uint8_t *p = (const uint8_t*)a.saved + row * a.ld_saved + f, *s = a.scales + row * a.below * a.blocks + (f >> 5);
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (j < left) q.z[j] = p[j * a.ld_saved], q.scales[j] = s[j * a.below * a.blocks];
+      if (a.below == 2) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (j < left) q.up[j] = p[j * a.ld_saved + a.k], q.scales[j] |= (uint32_t)s[j * 2 * a.blocks + a.blocks] << 8;
+      }
+    } else if (a.below) {
+      const T* p = (const T*)a.saved + row * a.ld_saved + f;
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (j < left) q.z[j] = raw(p + j * a.ld_saved);
+      if (a.below == 2) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (j < left) q.up[j] = raw(p + j * a.ld_saved + a.k);
+      }
     } else if (a.add) {
-      p.z = load_as_float((const T*)a.add + row * a.ld_add + f);
+      const T* p = (const T*)a.add + row * a.ld_add + f;
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (j < left) q.z[j] = raw(p + j * a.ld_add);
     }
-    return p;
   }
-  __device__ __forceinline__ void store(int64_t row, float t, float, const Pre& p) const {
+  template <int N>
+  __device__ __forceinline__ void rows(int64_t row, int left, const float (&t)[N], const Asked<N>& q) const {
     if (!on) return;
     T* dx = (T*)a.dx + row * a.ld_dx + f;
+    float z[N], up[N];
+    if (a.below && a.scales) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float2 v = e4m3x2_value(q.z[j], q.up[j]);
+        z[j] = v.x * scale_value(q.scales[j] & 255u), up[j] = v.y * scale_value(q.scales[j] >> 8);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) z[j] = value(q.z[j]), up[j] = value(q.up[j]);
+    }
     if (!a.below) {
-      store_as(dx, t + p.z);
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (j < left) store_as(dx + j * a.ld_dx, t[j] + z[j]);
       return;
     }
-    float y, slope;
-    act_value_and_slope<sizeof(T) == 2>(p.z, a.act, y, slope);
-    if (a.below == 2) {
-      store_as(dx, t * p.up * slope);
-      store_as(dx + a.k, t * y);
-      y *= p.up;
+    float slope[N];
+    if (a.act == MCCE_ACT_SILU) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) slope_and_value<sizeof(T) == 2>(z[j], MCCE_ACT_SILU, z[j], slope[j]);
+    } else if (a.act == MCCE_ACT_GELU) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) slope_and_value<sizeof(T) == 2>(z[j], MCCE_ACT_GELU, z[j], slope[j]);
     } else {
-      store_as(dx, t * slope);
+#pragma unroll
+      for (int j = 0; j < N; ++j) slope[j] = 1.f;
     }
-    if (a.h) store_as((T*)a.h + row * a.ld_h + f, y);
+    T* h = (T*)a.h + row * a.ld_h + f;
+    if (a.below == 2) {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (j < left) {
+          store_as(dx + j * a.ld_dx, t[j] * up[j] * slope[j]);
+          store_as(dx + j * a.ld_dx + a.k, t[j] * z[j]);
+        }
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (a.h && j < left) store_as(h + j * a.ld_h, z[j] * up[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (j < left) store_as(dx + j * a.ld_dx, t[j] * slope[j]);
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (a.h && j < left) store_as(h + j * a.ld_h, z[j]);
+    }
   }
 };
 

@@ -5,8 +5,8 @@
 //   backward  D[feature, row] = sum_j w[j, feature] dout[row, j]               weights across their rows
 //   dweight   D[j, feature]   = sum_r dout[r, j] x[r, feature]                 both across their rows; r runs over the group's rows
 // Weight features are the 128 rows of the MMA and token rows its N dimension: groups of any size then cost what their rows rounded up to 16 cost,
-// where 128-row tiles of tokens would waste a third of the work at 250 rows per expert.  A gated forward tile has 64 features: 32 gate rows, 32
-// up rows and so on in turn, so that two neighbouring epilogue warps hold gate and up of the same features and swap half of their rows.
+// where 128-row tiles of tokens would waste a third of the work at 250 rows per expert.  A gated forward tile has 64 features: 64
+// gate rows, then 64 up rows, so that two epilogue warps hold gate and up of the same features and swap half of their rows.
 //
 // One CTA per SM walks the tiles.  Warp 0 issues TMA loads into a ring of stages, warp 1 the MMAs into one of two TMEM buffers, eight warps
 // bring the other buffer to memory, a feature per lane.  Every wait is bounded: when one gives up, the CTA notes it, lets its copies land, frees
@@ -35,9 +35,11 @@ constexpr uint32_t kABytes = kTileM * kSlab * 2;
 constexpr uint32_t kPanelBytes = kSlab * 128;   // an operand across its rows: 64 rows of 64 columns
 constexpr int kBlockOfTiles = 16;   // row tiles of a group that are walked together, so that their rows stay in L2 for the next features
 
-template <int KIND, bool GATED, int BN>
+template <int KIND, bool GATED, int BN, bool PAIR>
 struct Cfg {
-  static constexpr uint32_t kBBytes = BN * kSlab * 2;
+  static constexpr int kCtas = PAIR ? 2 : 1;
+  static constexpr int kFeatures = kTileM * kCtas / (KIND == kForward && GATED ? 2 : 1);   // of a tile
+  static constexpr uint32_t kBBytes = BN / kCtas * kSlab * 2;
   static constexpr uint32_t kStageBytes = kABytes + kBBytes;
   static constexpr uint32_t kSwapBytes = KIND == kForward && GATED ? 4 * 2 * 2 * 8 * 32 * 4 : 0;
   static constexpr uint32_t kCountBytes = KIND == kDweight ? 0 : ((MCCE_LINEAR_MAX_GROUPS + 1 + 33) * 4 + 127) & ~127;
@@ -45,22 +47,108 @@ struct Cfg {
   static constexpr int kFit = (232448 - kFixed) / kStageBytes;
   static constexpr int kStages = kFit < 10 ? kFit : 10;
   static constexpr size_t kSmemBytes = kFixed + (size_t)kStages * kStageBytes;
-  static constexpr int kRowBox = BN >= 64 ? 32 : 16;   // token rows per TMA copy
+  static constexpr int kRowBox = BN / kCtas;   // token rows per TMA copy, or half as many: one copy whatever the tile has
 };
 
 struct Maps {
   CUtensorMap a, a_up;   // weights; dweight: dout and its second half
   CUtensorMap b, b_up;   // rows; dweight: x
+  CUtensorMap b_half, b_up_half;   // rows, boxes of half the height
+  int a_panels, b_panels;   // operands across their rows: 64-column panels that one copy brings
 };
 
 // Descriptor of an operand across its rows: panels of 64 columns (128 bytes), kPanelBytes apart; eight rows 1024 bytes apart.
 __device__ __forceinline__ uint64_t smem_desc_across(uint32_t addr) {
   return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(kPanelBytes >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
-               "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
-               : "memory");
+// TMA copies into this CTA's shared memory; in a pair the barrier may be the other CTA's.
+#define MCCE_TMA_LOAD(DIMS, COORDS, ...)                                                                                              \
+  if (PAIR)                                                                                                                           \
+    asm volatile("cp.async.bulk.tensor." DIMS                                                                                         \
+                 ".cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {" COORDS "}], [%2];" ::"r"(dst),      \
+                 "l"(map), "r"(bar), __VA_ARGS__                                                                                      \
+                 : "memory");                                                                                                         \
+  else                                                                                                                                \
+    asm volatile("cp.async.bulk.tensor." DIMS ".shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {" COORDS "}], [%2];"  \
+                 ::"r"(dst),                                                                                                          \
+                 "l"(map), "r"(bar), __VA_ARGS__                                                                                      \
+                 : "memory")
+template <bool PAIR>
+__device__ __forceinline__ void load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  MCCE_TMA_LOAD("2d", "%3, %4", "r"(x), "r"(y));
+}
+template <bool PAIR>
+__device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  MCCE_TMA_LOAD("3d", "%3, %4, %5", "r"(x), "r"(y), "r"(z));
+}
+template <bool PAIR>
+__device__ __forceinline__ void load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int u, uint32_t bar) {
+  MCCE_TMA_LOAD("4d", "%3, %4, %5, %6", "r"(x), "r"(y), "r"(z), "r"(u));
+}
+#undef MCCE_TMA_LOAD
+// `count` panels of 64 columns from column x, 64 rows from row y of matrix g.  The map's dimensions: column in a panel, row, (panel,) matrix.
+// What a copy costs is mostly its own: one that brings two panels instead of two copies (for these and for the rows' boxes) took a product of 8192 x 4096 x
+// 4096 from 1250 to 1450 TFLOP/s.
+template <bool PAIR>
+__device__ __forceinline__ void load_panels(uint32_t dst, const CUtensorMap* map, int per_copy, int count, int x, int y, int g, uint32_t bar) {
+  if (per_copy > 1) load_4d<PAIR>(dst, map, 0, y, x / 64, g, bar);
+  else
+    for (int i = 0; i < count; ++i) load_3d<PAIR>(dst + i * kPanelBytes, map, x + 64 * i, y, g, bar);
+}
+
+// ---- pairs of CTAs: the even one (rank 0) leads, its barriers say when both CTAs' operands have landed ----------
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t leaders(uint32_t addr) {   // the same place in rank 0's shared memory
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+  return r;
+}
+__device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// Without ordering what this thread did before: a release at cluster scope costs hundreds of cycles.
+__device__ __forceinline__ void arrive_at_relaxed(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+template <bool PAIR>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  if (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+  else umma_bf16(d, a, b, idesc, accumulate);
+}
+// Arrives, in both CTAs of a pair, once every MMA issued so far has completed.
+template <bool PAIR>
+__device__ __forceinline__ void commit(uint32_t bar) {
+  if (PAIR)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3)
+                 : "memory");
+  else umma_commit(bar);
+}
+template <bool PAIR>
+__device__ __forceinline__ void take_tmem(uint32_t slot, uint32_t cols) {
+  if (PAIR) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  } else {
+    tmem_alloc(slot, cols);
+  }
+}
+template <bool PAIR>
+__device__ __forceinline__ void free_tmem(uint32_t addr, uint32_t cols) {
+  if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
+  else tmem_dealloc(addr, cols);
 }
 
 struct Item {
@@ -69,21 +157,22 @@ struct Item {
   int j0, half;     // dweight: first column of x; which half of dout
 };
 
-template <int KIND, bool GATED, int BN>
+template <int KIND, bool GATED, int BN, bool PAIR>
 struct Walk {
+  static constexpr int kFeatures = Cfg<KIND, GATED, BN, PAIR>::kFeatures;
   const Problem& p;
   const int* before;
   int64_t items;
   int FT, JT;   // tiles of features (dweight: of dout's columns), of x's columns
   __device__ __forceinline__ Walk(const Problem& p_, const int* before_) : p(p_), before(before_) {
-    const int features = KIND == kBackward ? p.k : p.n, per = KIND == kForward && GATED ? kTileM / 2 : kTileM;
-    FT = (features + per - 1) / per, JT = KIND == kDweight ? (p.k + BN - 1) / BN : 1;
+    const int features = KIND == kBackward ? p.k : p.n;
+    FT = (features + kFeatures - 1) / kFeatures, JT = KIND == kDweight ? (p.k + BN - 1) / BN : 1;
     items = KIND == kDweight ? (int64_t)p.groups.G * (GATED ? 2 : 1) * FT * JT : (int64_t)before[p.groups.G] * FT;
   }
   __device__ __forceinline__ Item at(int64_t w) const {
     Item it;
     if (KIND == kDweight) {
-      it.f0 = (int)(w % FT) * kTileM, w /= FT;
+      it.f0 = (int)(w % FT) * kFeatures, w /= FT;
       it.j0 = (int)(w % JT) * BN, w /= JT;
       it.half = GATED ? (int)(w & 1) : 0;
       it.g = (int)(GATED ? w >> 1 : w);
@@ -97,12 +186,17 @@ struct Walk {
       const int block = (int)(in / (kBlockOfTiles * FT)), rest = (int)(in % (kBlockOfTiles * FT));
       const int wide = min(kBlockOfTiles, tiles - block * kBlockOfTiles);
       const int tile = block * kBlockOfTiles + rest % wide;
-      it.f0 = rest / wide * (GATED && KIND == kForward ? kTileM / 2 : kTileM);
+      it.f0 = rest / wide * kFeatures;
       const int m = (int)gr.m, each = ((m + tiles - 1) / tiles + 15) & ~15;   // tiles of equal size; none is empty
       it.row = (int)gr.first + tile * each, it.rows = min(each, m - tile * each);
       it.j0 = it.half = 0;
     }
     return it;
+  }
+  // N of the tile's MMAs: its rows; its columns of x, in whole panels for each CTA
+  __device__ __forceinline__ int wide(const Item& it) const {
+    if (KIND == kDweight) return (min(BN, p.k - it.j0) + 64 * Cfg<KIND, GATED, BN, PAIR>::kCtas - 1) & ~(64 * Cfg<KIND, GATED, BN, PAIR>::kCtas - 1);
+    return (it.rows + 15) & ~15;
   }
   __device__ __forceinline__ int slabs(const Item& it) const {
     if (KIND == kDweight) return (it.rows + kSlab - 1) / kSlab;
@@ -110,9 +204,12 @@ struct Walk {
   }
 };
 
-template <int KIND, bool GATED, int BN>
+// One CTA, or a pair of CTAs that share a tile: each has half of its features (128 MMA rows, accumulated in its own TMEM) and half of its
+// rows (dweight: of x's columns) in shared memory, and the leader's MMAs read both halves.  A pair takes in a third less than two single CTAs for
+// the same products.
+template <int KIND, bool GATED, int BN, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Problem p) {
-  using C = Cfg<KIND, GATED, BN>;
+  using C = Cfg<KIND, GATED, BN, PAIR>;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem_al = smem_raw + (smem_base - smem_u32(smem_raw));
@@ -121,85 +218,127 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
   int* before = (int*)(rest + C::kSwapBytes);
   uint64_t* bars = (uint64_t*)(rest + C::kSwapBytes + C::kCountBytes);
   const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * C::kStages;
-  const uint32_t bar_tfull = bar_empty + 8 * C::kStages, bar_tempty = bar_tfull + 16, bar_swap = bar_tempty + 16;
-  uint32_t* tmem_slot = (uint32_t*)(bars + 2 * C::kStages + 8);
+  const uint32_t bar_tfull = bar_empty + 8 * C::kStages, bar_tempty = bar_tfull + 16, bar_swap = bar_tempty + 16, bar_tail = bar_swap + 32;
+  uint32_t* tmem_slot = (uint32_t*)(bars + 3 * C::kStages + 8);
   volatile uint32_t* abort_flag = tmem_slot + 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = PAIR ? (int)cluster_rank() : 0;
+  const int64_t first = PAIR ? blockIdx.x >> 1 : blockIdx.x, step = PAIR ? gridDim.x >> 1 : gridDim.x;
+  // in a pair, the follower's last slab of a group is complete when its own warp has cleared the rows of the next group (dweight)
+  constexpr bool kTail = PAIR && KIND == kDweight;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
-      mbar_init(bar_full + 8 * s, 1);
+      mbar_init(bar_full + 8 * s, kTail ? 2 : 1);
       mbar_init(bar_empty + 8 * s, 1);
+      mbar_init(bar_tail + 8 * s, 1);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(bar_tfull + 8 * b, 1);
-      mbar_init(bar_tempty + 8 * b, kEpilogueWarps);
+      mbar_init(bar_tempty + 8 * b, kEpilogueWarps * C::kCtas);
     }
     for (int b = 0; b < 4; ++b) mbar_init(bar_swap + 8 * b, 2);
     *abort_flag = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 2 * BN);
+  if (PAIR) cluster_sync();
+  if (warp == 1) take_tmem<PAIR>(smem_u32(tmem_slot), 2 * BN);
   if (KIND != kDweight) count_tiles(p.groups, BN, before, before + p.groups.G + 1);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  const Walk<KIND, GATED, BN> walk(p, before);
+  const Walk<KIND, GATED, BN, PAIR> walk(p, before);
 
   if (warp == 0) {
     if (lane == 0) {
       uint32_t stage = 0, phase = 0;
       bool alive = true;
-      for (int64_t w = blockIdx.x; w < walk.items && alive; w += gridDim.x) {
+      for (int64_t w = first; w < walk.items && alive; w += step) {
         const Item it = walk.at(w);
         const int slabs = walk.slabs(it), part = GATED && KIND == kBackward ? slabs / 2 : slabs;
-        const int panels = KIND == kDweight ? min(BN / 64, (p.k - it.j0 + 63) / 64) : 0;
-        const int boxes = (it.rows + C::kRowBox - 1) / C::kRowBox;
-        const uint32_t tx = kABytes + (KIND == kDweight ? panels * kPanelBytes : (uint32_t)boxes * C::kRowBox * kSlab * 2);
+        const int f0 = it.f0 + rank * (C::kFeatures / C::kCtas);
+        // this CTA's share of the MMA's N dimension
+        const int share = walk.wide(it) / C::kCtas;
+        const int row = it.row + rank * share, j0 = it.j0 + rank * share;
+        const int panels = KIND == kDweight && maps.b_panels > 1 ? maps.b_panels : (share + 63) / 64;
+        const bool half = share <= C::kRowBox / 2;
+        const uint32_t tx = kABytes + (KIND == kDweight ? panels * kPanelBytes : (uint32_t)(half ? C::kRowBox / 2 : C::kRowBox) * kSlab * 2);
+        const CUtensorMap *map_b = half ? &maps.b_half : &maps.b, *map_b_up = half ? &maps.b_up_half : &maps.b_up;
         for (int kt = 0; kt < slabs; ++kt) {
           if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, &wait_error, 1u)) {
             alive = false;
             break;
           }
-          const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + kABytes, full = bar_full + 8 * stage;
-          mbar_expect_tx(full, tx);
+          const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + kABytes;
+          uint32_t full = bar_full + 8 * stage;
+          const bool tail = kTail && it.rows - kt * kSlab < kSlab;
+          if (rank == 0) {
+            mbar_expect_tx(full, tail ? tx : C::kCtas * tx);
+          } else if (tail) {
+            full = bar_tail + 8 * stage;   // waited for by this CTA's warp 1, which then arrives at the leader's barrier
+            mbar_expect_tx(full, tx);
+          } else {
+            full = leaders(full);
+            if (kTail) arrive_at_relaxed(full);   // the copies themselves say when they have landed
+          }
           if (KIND == kForward) {
             const int x = kt * kSlab;
             if (GATED) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) tma_load_3d(sa + i * 4096, i & 1 ? &maps.a_up : &maps.a, x, it.f0 + (i >> 1) * 32, it.g, full);
+              load_3d<PAIR>(sa, &maps.a, x, f0, it.g, full);
+              load_3d<PAIR>(sa + kABytes / 2, &maps.a_up, x, f0, it.g, full);
             } else {
-              tma_load_3d(sa, &maps.a, x, it.f0, it.g, full);
+              load_3d<PAIR>(sa, &maps.a, x, f0, it.g, full);
             }
-            for (int i = 0; i < boxes; ++i) tma_load_2d(sb + i * C::kRowBox * 128, &maps.b, x, it.row + i * C::kRowBox, full);
+            load_2d<PAIR>(sb, map_b, x, row, full);
           } else if (KIND == kBackward) {
             const bool up = kt >= part;
             const int x = (up ? kt - part : kt) * kSlab;
-            tma_load_3d(sa, up ? &maps.a_up : &maps.a, it.f0, x, it.g, full);
-            tma_load_3d(sa + kPanelBytes, up ? &maps.a_up : &maps.a, it.f0 + 64, x, it.g, full);
-            for (int i = 0; i < boxes; ++i) tma_load_2d(sb + i * C::kRowBox * 128, up ? &maps.b_up : &maps.b, x, it.row + i * C::kRowBox, full);
+            load_panels<PAIR>(sa, up ? &maps.a_up : &maps.a, maps.a_panels, 2, f0, x, it.g, full);
+            load_2d<PAIR>(sb, up ? map_b_up : map_b, x, row, full);
           } else {
             const int y = it.row + kt * kSlab;
-            tma_load_2d(sa, it.half ? &maps.a_up : &maps.a, it.f0, y, full);
-            tma_load_2d(sa + kPanelBytes, it.half ? &maps.a_up : &maps.a, it.f0 + 64, y, full);
-            for (int i = 0; i < panels; ++i) tma_load_2d(sb + i * kPanelBytes, &maps.b, it.j0 + 64 * i, y, full);
+            load_panels<PAIR>(sa, it.half ? &maps.a_up : &maps.a, maps.a_panels, 2, f0, y, 0, full);
+            load_panels<PAIR>(sb, &maps.b, maps.b_panels, panels, j0, y, 0, full);
           }
           if (++stage == C::kStages) stage = 0, phase ^= 1u;
         }
       }
     }
   } else if (warp == 1) {
-    // The whole warp walks along: in dweight's last slab its lanes clear the rows that belong to the next group.
-    uint32_t stage = 0, phase = 0, acc = 0;
+    // The whole warp walks along: in dweight's last slab its lanes clear the rows that belong to the next group (of both operands: zero times a
+    // NaN of the next group would not be zero).
+    uint32_t stage = 0, phase = 0, acc = 0, tails = 0;   // tails: the phase of every stage's bar_tail
     bool alive = true;
-    for (int64_t w = blockIdx.x; w < walk.items && alive; w += gridDim.x) {
+    for (int64_t w = first; w < walk.items && alive; w += step) {
       const Item it = walk.at(w);
       const int slabs = walk.slabs(it);
       if (slabs == 0) continue;
-      const int cols = KIND == kDweight ? min(BN, p.k - it.j0) : it.rows;
-      // fp32 sums of bf16, M = 128, N; a set bit 15 / 16: A / B lies across its rows
-      const uint32_t idesc = instr_desc((uint32_t)(cols + 15) & ~15u) | (KIND != kForward ? 1u << 15 : 0u) | (KIND == kDweight ? 1u << 16 : 0u);
+      const int cols = walk.wide(it);
+      const int panels = 2 + (cols / C::kCtas + 63) / 64;
+      auto clear = [&](uint32_t at_stage, int valid) {
+        const int n16 = (((valid + 15) & ~15) - valid) * 8;
+        for (int i = lane; i < n16 * panels; i += 32)
+          *(uint4*)(smem_al + (size_t)at_stage * C::kStageBytes + (size_t)(i / n16) * kPanelBytes + valid * 128 + (i % n16) * 16) =
+              make_uint4(0u, 0u, 0u, 0u);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+      };
+      if (rank != 0) {   // the follower: only its tails
+        const int valid = it.rows - (slabs - 1) * kSlab;
+        stage = (stage + slabs - 1) % C::kStages;
+        if (kTail && valid < kSlab) {
+          if (!mbar_wait(bar_tail + 8 * stage, (tails >> stage) & 1u, abort_flag, &wait_error, 6u)) break;
+          tails ^= 1u << stage;
+          clear(stage, valid);
+          if (lane == 0) arrive_at(leaders(bar_full + 8 * stage));
+        }
+        stage = (stage + 1) % C::kStages;
+        continue;
+      }
+      // fp32 sums of bf16, M = 128 (256 in a pair), N; a set bit 15 / 16: A / B lies across its rows
+      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)cols >> 3 << 17) | ((uint32_t)(kTileM * C::kCtas) >> 4 << 24) |
+                             (KIND != kForward ? 1u << 15 : 0u) | (KIND == kDweight ? 1u << 16 : 0u);
       const uint32_t buf = acc & 1u;
       if (!mbar_wait(bar_tempty + 8 * buf, ((acc >> 1) & 1u) ^ 1u, abort_flag, &wait_error, 2u)) break;
       ++acc;
@@ -215,27 +354,21 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
         if (KIND == kDweight && it.rows - kt * kSlab < kSlab) {
           const int valid = it.rows - kt * kSlab;
           steps = (valid + 15) / 16;
-          // both operands: zero times a NaN of the next group would not be zero
-          const int n16 = (steps * 16 - valid) * 8, panels = 2 + (cols + 63) / 64;
-          for (int i = lane; i < n16 * panels; i += 32)
-            *(uint4*)(smem_al + (size_t)stage * C::kStageBytes + (size_t)(i / n16) * kPanelBytes + valid * 128 + (i % n16) * 16) =
-                make_uint4(0u, 0u, 0u, 0u);
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
+          clear(stage, valid);
         }
         tc_fence_after();
         if (lane == 0) {
           for (int k = 0; k < steps; ++k) {
             const uint64_t ad = KIND == kForward ? smem_desc(sa + k * 32) : smem_desc_across(sa + k * 2048);
             const uint64_t bd = KIND == kDweight ? smem_desc_across(sb + k * 2048) : smem_desc(sb + k * 32);
-            umma_bf16(d, ad, bd, idesc, (kt | k) != 0 ? 1u : 0u);
+            mma<PAIR>(d, ad, bd, idesc, (kt | k) != 0 ? 1u : 0u);
           }
-          umma_commit(bar_empty + 8 * stage);
+          commit<PAIR>(bar_empty + 8 * stage);
         }
         __syncwarp();
         if (++stage == C::kStages) stage = 0, phase ^= 1u;
       }
-      if (alive && lane == 0) umma_commit(bar_tfull + 8 * buf);
+      if (alive && lane == 0) commit<PAIR>(bar_tfull + 8 * buf);
       __syncwarp();
     }
   } else {
@@ -243,8 +376,9 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     uint32_t acc = 0, swaps = 0;
     bool alive = true;
-    for (int64_t w = blockIdx.x; w < walk.items && alive; w += gridDim.x) {
-      const Item it = walk.at(w);
+    for (int64_t w = first; w < walk.items && alive; w += step) {
+      Item it = walk.at(w);
+      it.f0 += rank * (C::kFeatures / C::kCtas);
       const bool sums = walk.slabs(it) > 0;
       const uint32_t buf = acc & 1u;
       if (sums) {
@@ -306,9 +440,9 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
           }
         }
       } else if constexpr (KIND == kForward && GATED) {
-        // even quadrants hold z, odd ones z_up of the same 32 features; of every 16 rows the first 8 are finished by the even warp
-        const int pair = (quad >> 1) * 2 + team, up = quad & 1;
-        const Forward<__nv_bfloat16, true> e(p.fwd, it.g, it.f0 + (quad >> 1) * 32 + lane);
+        // quadrants 0 and 1 hold z, 2 and 3 z_up of the same 64 features; of every 16 rows the first 8 are finished by the warp that holds z
+        const int pair = (quad & 1) * 2 + team, up = quad >> 1;
+        const Forward<__nv_bfloat16, true> e(p.fwd, it.g, it.f0 + (quad & 1) * 32 + lane);
         for (int c = 16 * team; c < it.rows && alive; c += 32, ++swaps) {
           float v[16];
           __syncwarp();
@@ -324,45 +458,42 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
             alive = false;
             break;
           }
-          const int64_t row = it.row + c + up * 8;
-          const int left = it.rows - c - up * 8;
-          typename Forward<__nv_bfloat16, true>::Pre pre[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (j < left) pre[j] = e.load(row + j);
+          float z[8], z_up[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const float other = theirs[j * 32 + lane];
-            if (j < left) e.store(row + j, up ? other : v[j], up ? v[8 + j] : other, pre[j]);
+            z[j] = up ? other : v[j], z_up[j] = up ? v[8 + j] : other;
           }
+          e.rows((int64_t)it.row + c + up * 8, it.rows - c - up * 8, z, z_up);
+        }
+      } else if constexpr (KIND == kForward) {
+        const Forward<__nv_bfloat16, false> e(p.fwd, it.g, it.f0 + quad * 32 + lane);
+        for (int c = 16 * team; c < it.rows; c += 32) {
+          float v[16], none[16];
+          __syncwarp();
+          tmem_ld16(t0 + c, v);
+          tmem_ld_wait();
+          e.rows((int64_t)it.row + c, it.rows - c, v, none);
         }
       } else {
-        typedef typename std::conditional<KIND == kForward, Forward<__nv_bfloat16, false>, Backward<__nv_bfloat16>>::type Epilogue;
-        const int f = it.f0 + quad * 32 + lane;
-        const Epilogue e = [&] {
-          if constexpr (KIND == kForward) return Epilogue(p.fwd, it.g, f);
-          else return Epilogue(p.bwd, it.g, f);
-        }();
+        const Backward<__nv_bfloat16> e(p.bwd, it.g, it.f0 + quad * 32 + lane);
         for (int c = 16 * team; c < it.rows; c += 32) {
-          const int64_t row = it.row + c;
-          const int left = it.rows - c;
-          typename Epilogue::Pre pre[16];
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (j < left) pre[j] = e.load(row + j);
+          Backward<__nv_bfloat16>::Asked<16> q;
+          e.ask((int64_t)it.row + c, it.rows - c, q);
           float v[16];
           __syncwarp();
           tmem_ld16(t0 + c, v);
           tmem_ld_wait();
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (j < left) e.store(row + j, v[j], 0.f, pre[j]);
+          e.rows((int64_t)it.row + c, it.rows - c, v, q);
         }
       }
       if (sums) {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar_tempty + 8 * buf);
+        if (lane == 0) {
+          if (PAIR) arrive_at(leaders(bar_tempty + 8 * buf));
+          else mbar_arrive(bar_tempty + 8 * buf);
+        }
       }
     }
   }
@@ -375,13 +506,14 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
   }
   tc_fence_before();
   __syncthreads();
+  if (PAIR) cluster_sync();   // neither CTA leaves while the other may still reach its barriers
   tc_fence_after();
-  if (warp == 1) tmem_dealloc(tmem_base, 2 * BN);
+  if (warp == 1) free_tmem<PAIR>(tmem_base, 2 * BN);
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------
 bool encode(CUtensorMap* m, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
-  const cuuint32_t one[3] = {1, 1, 1};
+  const cuuint32_t one[4] = {1, 1, 1, 1};
   EncodeFn fn = encode_fn();
   return fn && fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -392,53 +524,83 @@ bool map_rows(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int6
   const cuuint32_t box[2] = {kSlab, (cuuint32_t)box_rows};
   return encode(m, base, 2, dims, strides, box);
 }
-// [groups, n, k]: what lies outside a matrix is filled with zeros, not with the next matrix
+// [groups, n, k], a box of 64 columns: what lies outside a matrix is filled with zeros, not with the next matrix
 bool map_weights(CUtensorMap* m, const void* base, const Problem& p, int box_rows) {
   const cuuint64_t dims[3] = {(cuuint64_t)p.k, (cuuint64_t)p.n, (cuuint64_t)p.groups.G};
   const cuuint64_t strides[2] = {(cuuint64_t)p.ld_w * 2, (cuuint64_t)(p.groups.G > 1 ? p.step_w : (p.n * p.ld_w + 7) & ~7ll) * 2};
   const cuuint32_t box[3] = {kSlab, (cuuint32_t)box_rows, 1};
   return encode(m, base, 3, dims, strides, box);
 }
+// [matrices, rows, cols] read across their rows, 64 rows at a time: two panels of 64 columns per copy where the columns are a multiple of 64 (a panel
+// that reached behind the last column would read what lies there), else one.
+bool map_panels(CUtensorMap* m, int* panels, const void* base, int64_t matrices, int64_t rows, int64_t cols, int64_t ld, int64_t step) {
+  const cuuint64_t sg = (cuuint64_t)(matrices > 1 ? step : (rows * ld + 7) & ~7ll) * 2;
+  if (cols % 64 == 0) {
+    const cuuint64_t dims[4] = {64, (cuuint64_t)rows, (cuuint64_t)(cols / 64), (cuuint64_t)matrices}, strides[3] = {(cuuint64_t)ld * 2, 128, sg};
+    const cuuint32_t box[4] = {64, kSlab, 2, 1};
+    *panels = 2;
+    return encode(m, base, 4, dims, strides, box);
+  }
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)matrices}, strides[2] = {(cuuint64_t)ld * 2, sg};
+  const cuuint32_t box[3] = {64, kSlab, 1};
+  *panels = 1;
+  return encode(m, base, 3, dims, strides, box);
+}
 
-template <int KIND, bool GATED, int BN>
+template <int KIND, bool GATED, int BN, bool PAIR>
 cudaError_t launch(const Problem& p, cudaStream_t st) {
-  using C = Cfg<KIND, GATED, BN>;
-  static int cache[64] = {0};
-  int sms = 0;
-  const cudaError_t e = sm_count_and_smem_optin(linear_tc_kernel<KIND, GATED, BN>, C::kSmemBytes, cache, &sms);
+  using C = Cfg<KIND, GATED, BN, PAIR>;
+  static int cache[64] = {0}, pairs[64] = {0};
+  auto kernel = linear_tc_kernel<KIND, GATED, BN, PAIR>;
+  int sms = 0, dev = 0;
+  cudaError_t e = sm_count_and_smem_optin(kernel, C::kSmemBytes, cache, &sms);
   if (e != cudaSuccess) return e;
   Maps m;
   bool ok;
-  const int64_t rows = p.L * p.groups.R;
-  const int kind_features = KIND == kBackward ? p.k : p.n, per = KIND == kForward && GATED ? kTileM / 2 : kTileM;
-  const int64_t FT = (kind_features + per - 1) / per;
-  int64_t most;
+  const int64_t rows = p.L * p.groups.R, features = KIND == kBackward ? p.k : p.n;
+  const int64_t FT = (features + C::kFeatures - 1) / C::kFeatures;
+  int64_t most = (rows / BN + p.groups.G) * FT;
+  const __nv_bfloat16* y = (const __nv_bfloat16*)p.y;
+  m.a_panels = m.b_panels = 1;
   if (KIND == kDweight) {
-    const __nv_bfloat16* y = (const __nv_bfloat16*)p.y;
-    ok = map_rows(&m.a, y, rows, p.n, p.ld_y, kSlab) && map_rows(&m.b, p.x, rows, p.k, p.ld_x, kSlab) &&
-         (!GATED || map_rows(&m.a_up, y + p.n, rows, p.n, p.ld_y, kSlab));
+    static_assert(KIND != kDweight || BN / C::kCtas == 128, "two panels of x's columns per CTA");
+    ok = map_panels(&m.a, &m.a_panels, y, 1, rows, p.n, p.ld_y, 0) && map_panels(&m.b, &m.b_panels, p.x, 1, rows, p.k, p.ld_x, 0) &&
+         (!GATED || map_panels(&m.a_up, &m.a_panels, y + p.n, 1, rows, p.n, p.ld_y, 0));
     most = (int64_t)p.groups.G * (GATED ? 2 : 1) * FT * ((p.k + BN - 1) / BN);
   } else if (KIND == kForward) {
-    const int box = GATED ? 32 : kTileM;
-    ok = map_weights(&m.a, p.w, p, box) && (!GATED || map_weights(&m.a_up, p.w_up, p, box)) && map_rows(&m.b, p.x, rows, p.k, p.ld_x, C::kRowBox);
-    most = (rows / BN + p.groups.G) * FT;
+    const int box = GATED ? kTileM / 2 : kTileM;
+    ok = map_weights(&m.a, p.w, p, box) && (!GATED || map_weights(&m.a_up, p.w_up, p, box)) && map_rows(&m.b, p.x, rows, p.k, p.ld_x, C::kRowBox) &&
+         map_rows(&m.b_half, p.x, rows, p.k, p.ld_x, C::kRowBox / 2);
   } else {
-    const __nv_bfloat16* y = (const __nv_bfloat16*)p.y;
-    ok = map_weights(&m.a, p.w, p, kSlab) && (!GATED || map_weights(&m.a_up, p.w_up, p, kSlab)) &&
-         map_rows(&m.b, y, rows, p.n, p.ld_y, C::kRowBox) && (!GATED || map_rows(&m.b_up, y + p.n, rows, p.n, p.ld_y, C::kRowBox));
-    most = (rows / BN + p.groups.G) * FT;
+    ok = map_panels(&m.a, &m.a_panels, p.w, p.groups.G, p.n, p.k, p.ld_w, p.step_w) &&
+         (!GATED || map_panels(&m.a_up, &m.a_panels, p.w_up, p.groups.G, p.n, p.k, p.ld_w, p.step_w));
+    ok = ok && map_rows(&m.b, y, rows, p.n, p.ld_y, C::kRowBox) && map_rows(&m.b_half, y, rows, p.n, p.ld_y, C::kRowBox / 2);
+    ok = ok && (!GATED || (map_rows(&m.b_up, y + p.n, rows, p.n, p.ld_y, C::kRowBox) &&
+                           map_rows(&m.b_up_half, y + p.n, rows, p.n, p.ld_y, C::kRowBox / 2)));
   }
   if (!ok) return cudaErrorInvalidValue;
-  linear_tc_kernel<KIND, GATED, BN><<<(unsigned)(most < sms ? most : sms), kThreads, C::kSmemBytes, st>>>(m, p);
-  return cudaGetLastError();
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = C::kCtas, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = sms, cfg.blockDim = kThreads, cfg.dynamicSmemBytes = C::kSmemBytes, cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
+  int64_t units = sms;
+  if (PAIR) {
+    if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
+    cfg.gridDim = sms / 2 * 2;
+    if (!pairs[dev] && (e = cudaOccupancyMaxActiveClusters(&pairs[dev], kernel, &cfg)) != cudaSuccess) return e;
+    units = pairs[dev] > 0 ? pairs[dev] : 1;
+  }
+  cfg.gridDim = (unsigned)((most < units ? most : units) * C::kCtas);
+  return cudaLaunchKernelEx(&cfg, kernel, m, p);
 }
 
 template <int KIND, bool GATED>
 cudaError_t launch_rows(const Problem& p, cudaStream_t st) {
   const int64_t each = p.L * p.groups.R / p.groups.G;
-  if (each <= 24) return launch<KIND, GATED, 32>(p, st);
-  if (each <= 96) return launch<KIND, GATED, 128>(p, st);
-  return launch<KIND, GATED, 256>(p, st);
+  if (each <= 24) return launch<KIND, GATED, 32, false>(p, st);
+  if (each <= 96) return launch<KIND, GATED, 128, false>(p, st);
+  return launch<KIND, GATED, 256, true>(p, st);
 }
 
 bool tma_rows(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
@@ -456,7 +618,7 @@ bool tensor_applicable(Kind kind, const Problem& p, int32_t dtype) {
 cudaError_t run_tensor(Kind kind, const Problem& p, cudaStream_t st) {
   if (kind == kForward) return p.gated ? launch_rows<kForward, true>(p, st) : launch_rows<kForward, false>(p, st);
   if (kind == kBackward) return p.gated ? launch_rows<kBackward, true>(p, st) : launch_rows<kBackward, false>(p, st);
-  return p.gated ? launch<kDweight, true, 256>(p, st) : launch<kDweight, false, 256>(p, st);
+  return p.gated ? launch<kDweight, true, 256, true>(p, st) : launch<kDweight, false, 256, true>(p, st);
 }
 
 }  // namespace linear
