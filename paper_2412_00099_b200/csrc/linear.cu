@@ -19,8 +19,8 @@ __global__ void __launch_bounds__(256) general_kernel(const Problem p) {
   extern __shared__ __align__(16) float smem[];
   float* As = smem;                          // [kDeep][kPad]
   float* Bs = As + kDeep * kPad;             // [kSets][kDeep][kPad]
-  float* Cs = smem;                          // [kSets][64][65], after the products
-  int* before = (int*)(smem + kSets * kTile * 65);
+  float* Cs = smem;                          // [kSets][64][kPad], after the products
+  int* before = (int*)(smem + kSets * kTile * kPad);
   int* scratch = before + p.groups.G + 1;
   const int t = threadIdx.x, tx = t % 16, ty = t / 16;
 
@@ -100,11 +100,10 @@ __global__ void __launch_bounds__(256) general_kernel(const Problem p) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) Cs[(s * kTile + 4 * ty + i) * 65 + 4 * tx + j] = c[s][i][j];
+        for (int j = 0; j < 4; ++j) Cs[(s * kTile + 4 * ty + i) * kPad + 4 * tx + j] = c[s][i][j];
     __syncthreads();
     const int warp = t / 32, lane = t % 32;
     for (int jj = 0; jj < J; jj += 32) {
-      const float* col = Cs + jj + lane;
       if (KIND == kDweight) {
         const void* add = half ? p.add_dw_up : p.add_dw;
         void* dw = half ? p.dw_up : p.dw;
@@ -112,7 +111,7 @@ __global__ void __launch_bounds__(256) general_kernel(const Problem p) {
         for (int i = warp; i < I; i += 8) {
           if (j >= J) continue;
           const int64_t at = g * p.step_w + (int64_t)(i0 + i) * p.ld_w + j0 + j;
-          float v = col[i * 65];
+          float v = Cs[i * kPad + j];
           if (p.dw_f32) {
             if (add) v += ((const float*)add)[at];
             ((float*)dw)[at] = v;
@@ -121,23 +120,23 @@ __global__ void __launch_bounds__(256) general_kernel(const Problem p) {
             store_as((T*)dw + at, v);
           }
         }
-      } else if (KIND == kForward) {
-        const Forward<T, GATED> e(p.fwd, g, j0 + jj + lane);
-        float z[8], up[8] = {};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          z[i] = col[(warp * 8 + i) * 65];
-          if (kSets == 2) up[i] = col[(kTile + warp * 8 + i) * 65];
-        }
-        e.rows(row0 + warp * 8, I - warp * 8, z, up);
       } else {
-        const Backward<T> e(p.bwd, g, j0 + jj + lane);
-        typename Backward<T>::template Asked<8> q;
-        float v[8];
-        e.ask(row0 + warp * 8, I - warp * 8, q);
+        const int i = warp * 8 + lane / 4, j = jj + 8 * (lane % 4);
+        float z[1][8], up[1][8] = {};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = col[(warp * 8 + i) * 65];
-        e.rows(row0 + warp * 8, I - warp * 8, v, q);
+        for (int u = 0; u < 8; ++u) {
+          z[0][u] = Cs[i * kPad + j + u];
+          if (kSets == 2) up[0][u] = Cs[(kTile + i) * kPad + j + u];
+        }
+        if constexpr (KIND == kForward) {
+          const Forward<T, GATED> e(p.fwd, g, j0 + j);
+          e.rows(row0 + warp * 8, I - warp * 8, z, up);
+        } else {
+          const Backward<T> e(p.bwd, g, j0 + j);
+          typename Backward<T>::template Asked<1> q;
+          e.ask(row0 + warp * 8, I - warp * 8, q);
+          e.rows(row0 + warp * 8, I - warp * 8, z, q);
+        }
       }
     }
     __syncthreads();
@@ -148,7 +147,7 @@ template <Kind KIND, typename T, bool GATED>
 cudaError_t launch_general(const Problem& p, cudaStream_t st) {
   static int cache[64] = {0};
   constexpr int kSets = KIND == kForward && GATED ? 2 : 1;
-  const size_t fixed = (size_t)kSets * kTile * 65 * 4;
+  const size_t fixed = (size_t)kSets * kTile * kPad * 4;
   int sms = 0;
   const cudaError_t e =
       tc::sm_count_and_smem_optin(general_kernel<KIND, T, GATED>, fixed + (MCCE_LINEAR_MAX_GROUPS + 1 + 33) * 4, cache, &sms);
@@ -199,29 +198,38 @@ __global__ void __launch_bounds__(1024) bias_kernel(const BiasArgs a) {
 }
 
 // ---- 8-bit checkpoints ------------------------------------------------------------------------------------------
-// One block of 32 columns per warp at a time.
+// Four lanes have a block of 32 columns.  `wide`: eight columns are aligned as a whole in both tensors.
 template <typename T>
 __global__ void __launch_bounds__(256) pack_kernel(const T* x, uint8_t* q, uint8_t* scales, int64_t blocks, int per_row, int d, int64_t ld_x,
-                                                   int64_t ld_q) {
-  const int lane = threadIdx.x & 31;
-  for (int64_t b = blockIdx.x * 8ll + (threadIdx.x >> 5); b < blocks; b += gridDim.x * 8ll) {
-    const int64_t row = b / per_row;
-    const int j = (int)(b % per_row) * 32 + lane;
-    const float v = j < d ? load_as_float(x + row * ld_x + j) : 0.f;
-    const uint32_t s = warp_block_scale(v);
-    if (j < d) q[row * ld_q + j] = (uint8_t)to_e4m3x2(v * scale_inverse(s), 0.f);
-    if (lane == 0) scales[b] = (uint8_t)s;
-  }
+                                                   int64_t ld_q, bool wide) {
+  const int64_t b = (blockIdx.x * 256ll + threadIdx.x) / 4;
+  const bool on = b < blocks;
+  const int64_t row = on ? b / per_row : 0;
+  const int j = (int)(on ? b % per_row : 0) * 32 + 8 * (threadIdx.x & 3), count = on ? min(max(d - j, 0), 8) : 0;
+  uint32_t raw[2 * sizeof(T)] = {}, w[2];
+  float v[8];
+  if (count) load_8(x + row * ld_x + j, wide, count, raw);
+  floats_of(raw, v);
+  const uint32_t s = pack_8(v, w);
+  if (count) store_words_8(q + row * ld_q + j, wide, count, w);
+  if (on && (threadIdx.x & 3) == 0) scales[b] = (uint8_t)s;
 }
 template <typename T>
 __global__ void __launch_bounds__(256) unpack_kernel(const uint8_t* q, const uint8_t* scales, T* x, int64_t blocks, int per_row, int d,
-                                                     int64_t ld_x, int64_t ld_q) {
-  const int lane = threadIdx.x & 31;
-  for (int64_t b = blockIdx.x * 8ll + (threadIdx.x >> 5); b < blocks; b += gridDim.x * 8ll) {
-    const int64_t row = b / per_row;
-    const int j = (int)(b % per_row) * 32 + lane;
-    if (j < d) store_as(x + row * ld_x + j, e4m3x2_value(q[row * ld_q + j], 0u).x * scale_value(scales[b]));
-  }
+                                                     int64_t ld_x, int64_t ld_q, bool wide) {
+  const int64_t b = (blockIdx.x * 256ll + threadIdx.x) / 4;
+  if (b >= blocks) return;
+  const int64_t row = b / per_row;
+  const int j = (int)(b % per_row) * 32 + 8 * (threadIdx.x & 3), count = min(max(d - j, 0), 8);
+  if (!count) return;
+  uint32_t w[2];
+  float v[8];
+  load_8(q + row * ld_q + j, wide, count, w);
+  const float s = scale_value(scales[b]);
+  floats_of(w, v);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] *= s;
+  store_8(x + row * ld_x + j, wide, count, v);
 }
 
 }  // namespace
@@ -247,20 +255,29 @@ cudaError_t run_bias_sums(const Problem& p, int32_t dtype, const void* add, cons
   return cudaGetLastError();
 }
 
+namespace {
+// Eight columns of every row start at a multiple of what they take, 16 bytes at most.
+bool wide_rows(const void* p, int64_t ld, int e) { return !p || (((uintptr_t)p | (uintptr_t)(ld * e)) & (e == 1 ? 7 : 15)) == 0; }
+}  // namespace
+
 cudaError_t run_pack(const void* x, int32_t dtype, int64_t rows, int32_t d, int64_t ld_x, int64_t ld_q, uint8_t* q, uint8_t* scales,
                      cudaStream_t st) {
   const int per_row = (d + 31) / 32;
-  const int64_t blocks = rows * per_row, grid = (blocks + 7) / 8 < 148 * 16 ? (blocks + 7) / 8 : 148 * 16;
-  if (dtype == MCCE_F32) pack_kernel<<<(unsigned)grid, 256, 0, st>>>((const float*)x, q, scales, blocks, per_row, d, ld_x, ld_q);
-  else pack_kernel<<<(unsigned)grid, 256, 0, st>>>((const __nv_bfloat16*)x, q, scales, blocks, per_row, d, ld_x, ld_q);
+  const int64_t blocks = rows * per_row, grid = (blocks + 63) / 64;
+  if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
+  const bool wide = wide_rows(x, ld_x, dtype == MCCE_F32 ? 4 : 2) && wide_rows(q, ld_q, 1);
+  if (dtype == MCCE_F32) pack_kernel<<<(unsigned)grid, 256, 0, st>>>((const float*)x, q, scales, blocks, per_row, d, ld_x, ld_q, wide);
+  else pack_kernel<<<(unsigned)grid, 256, 0, st>>>((const __nv_bfloat16*)x, q, scales, blocks, per_row, d, ld_x, ld_q, wide);
   return cudaGetLastError();
 }
 cudaError_t run_unpack(const uint8_t* q, const uint8_t* scales, int32_t dtype, int64_t rows, int32_t d, int64_t ld_x, int64_t ld_q, void* x,
                        cudaStream_t st) {
   const int per_row = (d + 31) / 32;
-  const int64_t blocks = rows * per_row, grid = (blocks + 7) / 8 < 148 * 16 ? (blocks + 7) / 8 : 148 * 16;
-  if (dtype == MCCE_F32) unpack_kernel<<<(unsigned)grid, 256, 0, st>>>(q, scales, (float*)x, blocks, per_row, d, ld_x, ld_q);
-  else unpack_kernel<<<(unsigned)grid, 256, 0, st>>>(q, scales, (__nv_bfloat16*)x, blocks, per_row, d, ld_x, ld_q);
+  const int64_t blocks = rows * per_row, grid = (blocks + 63) / 64;
+  if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
+  const bool wide = wide_rows(x, ld_x, dtype == MCCE_F32 ? 4 : 2) && wide_rows(q, ld_q, 1);
+  if (dtype == MCCE_F32) unpack_kernel<<<(unsigned)grid, 256, 0, st>>>(q, scales, (float*)x, blocks, per_row, d, ld_x, ld_q, wide);
+  else unpack_kernel<<<(unsigned)grid, 256, 0, st>>>(q, scales, (__nv_bfloat16*)x, blocks, per_row, d, ld_x, ld_q, wide);
   return cudaGetLastError();
 }
 
@@ -336,6 +353,7 @@ extern "C" int mcce_expert_linear(const mcce_linear* p, const void* x, const int
   f.bias = bias, f.bias_up = bias_up, f.add = add, f.out = out, f.saved = saved, f.scales = (uint8_t*)scales;
   f.ld_add = ld_or(p->ld_add, p->n), f.ld_out = ld_or(p->ld_y, p->n), f.ld_saved = ld_or(p->ld_saved, width);
   f.bias_f32 = p->bias_dtype == MCCE_F32, f.out_f32 = p->out_dtype == MCCE_F32, f.act = p->act, f.n = p->n, f.blocks = blocks_of(p->n);
+  f.wide = wide_rows(add, f.ld_add, eo) && wide_rows(out, f.ld_out, eo) && wide_rows(saved, f.ld_saved, es);
   const int64_t G = q.groups.G;
   const Span sx = row_span(x, rows, q.ld_x, p->k, e), soff = flat_span(offsets, (int64_t)p->n_layers * (p->n_experts + 1), 4);
   const Span sw = weight_span(*p, w, e), swu = weight_span(*p, w_up, e);
@@ -375,6 +393,7 @@ extern "C" int mcce_expert_linear_backward(const mcce_linear* p, const void* dou
   b.add = add, b.saved = saved, b.scales = (const uint8_t*)scales, b.dx = dx, b.h = h;
   b.ld_add = ld_or(p->ld_add, p->k), b.ld_saved = ld_or(p->ld_saved, wide), b.ld_dx = ld_or(p->ld_x, wide), b.ld_h = ld_or(p->ld_h, p->k);
   b.below = p->below, b.act = p->act, b.k = p->k, b.blocks = blocks_of(p->k);
+  b.wide = wide_rows(add, b.ld_add, e) && wide_rows(saved, b.ld_saved, es) && wide_rows(dx, b.ld_dx, e) && wide_rows(h, b.ld_h, e);
   const Span sy = row_span(dout, rows, q.ld_y, width, e), soff = flat_span(offsets, (int64_t)p->n_layers * (p->n_experts + 1), 4);
   const Span sw = weight_span(*p, w, e), swu = weight_span(*p, w_up, e), sadd = row_span(add, rows, b.ld_add, p->k, e);
   const Span ssv = row_span(saved, rows, b.ld_saved, wide, es);
@@ -421,7 +440,7 @@ extern "C" int mcce_expert_linear_dweight(const mcce_linear* p, const void* dout
   const int64_t G = q.groups.G;
   q.y = dout, q.x = x, q.ld_y = ld_or(p->ld_y, width), q.ld_x = ld_or(p->ld_x, p->k);
   q.dw = dw, q.dw_up = dw_up, q.add_dw = add_dw, q.add_dw_up = add_dw_up, q.dw_f32 = p->out_dtype == MCCE_F32;
-  q.dw_wide = aligned(dw, 16) && aligned(dw_up, 16) && aligned(add_dw, 16) && aligned(add_dw_up, 16) && q.ld_w * eo % 16 == 0 && q.step_w * eo % 16 == 0;
+  q.dw_wide = aligned(dw, 32) && aligned(dw_up, 32) && aligned(add_dw, 32) && aligned(add_dw_up, 32) && q.ld_w * eo % 32 == 0 && q.step_w * eo % 32 == 0;
   const Span sy = row_span(dout, rows, q.ld_y, width, e), sx = row_span(x, rows, q.ld_x, p->k, ex);
   const Span ssc = flat_span(scales, rows, blocks_of(p->k)), soff = flat_span(offsets, (int64_t)p->n_layers * (p->n_experts + 1), 4);
   const Span saw = weight_span(*p, add_dw, eo), sawu = weight_span(*p, add_dw_up, eo), sab = flat_span(add_db, G * p->n, eo);

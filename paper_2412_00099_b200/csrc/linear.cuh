@@ -1,5 +1,5 @@
 // What the kernels of the experts' products share: the groups of rows, the activations, the 8-bit blocks, and what happens to a
-// value once its sum is formed.  All of them end with a warp that holds 32 neighbouring columns of one row, a column per lane.
+// value once its sum is formed.  All of them end with a warp that holds 32 neighbouring columns of several rows: four lanes have a row's, eight each.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
@@ -71,17 +71,103 @@ __device__ __forceinline__ float scale_inverse(uint32_t scale) { return __uint_a
 __device__ __forceinline__ float scale_value(uint32_t scale) {
   return __uint_as_float(scale == 255u ? 0x7fffffffu : scale == 0u ? 0x00400000u : scale << 23);
 }
-// Two quotients by their scales: e4m3 in the low and the high byte
 __device__ __forceinline__ uint32_t to_e4m3x2(float low, float high) {
   return __nv_cvt_float2_to_fp8x2(make_float2(low, high), __NV_SATFINITE, __NV_E4M3);
 }
-__device__ __forceinline__ float2 e4m3x2_value(uint32_t low, uint32_t high) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(low | high << 8), __NV_E4M3);
-  return __half22float2(__half2(h));
+__device__ __forceinline__ float2 e4m3x2_value(uint32_t pair) {
+  return __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)pair, __NV_E4M3)));
 }
-// The scale of the values that a whole warp holds, a column per lane; lanes without one hand in 0.
-__device__ __forceinline__ uint32_t warp_block_scale(float v) {
-  return block_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu));
+
+// ---- eight neighbouring columns of a row in a lane ----------------------------------------------------------------
+// As they lie in memory, `count` of them (1 .. 8; the rest reads as 0), in one or two accesses where `wide` says that they are aligned to it.
+template <typename E>
+__device__ __forceinline__ void load_8(const E* p, bool wide, int count, uint32_t (&w)[2 * sizeof(E)]) {
+  if (wide && count == 8) {
+    if constexpr (sizeof(E) == 1) {
+      const uint2 v = *(const uint2*)p;
+      w[0] = v.x, w[1] = v.y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(E) / 2; ++i) {
+        const uint4 v = ((const uint4*)p)[i];
+        w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 2 * (int)sizeof(E); ++i) w[i] = 0u;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (j < count) {
+      if constexpr (sizeof(E) == 4) w[j] = __float_as_uint(p[j]);
+      else if constexpr (sizeof(E) == 2) w[j / 2] |= (uint32_t)((const uint16_t*)p)[j] << (16 * (j & 1));
+      else w[j / 4] |= (uint32_t)p[j] << (8 * (j & 3));
+    }
+}
+__device__ __forceinline__ void floats_of(const uint32_t (&w)[8], float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j]);
+}
+__device__ __forceinline__ void floats_of(const uint32_t (&w)[4], float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[2 * j] = __uint_as_float(w[j] << 16), v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+}
+__device__ __forceinline__ void floats_of(const uint32_t (&w)[2], float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 f = e4m3x2_value(w[j / 2] >> (16 * (j & 1)) & 0xffffu);
+    v[2 * j] = f.x, v[2 * j + 1] = f.y;
+  }
+}
+template <typename E>
+__device__ __forceinline__ void store_words_8(E* p, bool wide, int count, const uint32_t (&w)[2 * sizeof(E)]) {
+  if (wide && count == 8) {
+    if constexpr (sizeof(E) == 1) {
+      *(uint2*)p = make_uint2(w[0], w[1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(E) / 2; ++i) ((uint4*)p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (j < count) {
+      if constexpr (sizeof(E) == 4) p[j] = __uint_as_float(w[j]);
+      else if constexpr (sizeof(E) == 2) ((uint16_t*)p)[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
+      else p[j] = (uint8_t)(w[j / 4] >> (8 * (j & 3)));
+    }
+}
+__device__ __forceinline__ void store_8(float* p, bool wide, int count, const float (&v)[8]) {
+  uint32_t w[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[j]);
+  store_words_8(p, wide, count, w);
+}
+__device__ __forceinline__ void store_8(__nv_bfloat16* p, bool wide, int count, const float (&v)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+    w[j] = *(const uint32_t*)&h;
+  }
+  store_words_8(p, wide, count, w);
+}
+// The same in 8 bits, and the scale of the 32 columns that this lane and its three neighbours hold; values behind the last
+// column are 0.  Every lane of the warp calls it.
+__device__ __forceinline__ uint32_t pack_8(const float (&v)[8], uint32_t (&w)[2]) {
+  uint32_t bits = 0u;   // of the largest magnitude: ordered like the magnitudes, infinity and NaN last
+#pragma unroll
+  for (int j = 0; j < 8; ++j) bits = max(bits, __float_as_uint(v[j]) & 0x7fffffffu);
+  bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 1));
+  bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 2));
+  const uint32_t s = block_scale(bits);
+  const float f = scale_inverse(s);
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    w[i] = to_e4m3x2(v[4 * i] * f, v[4 * i + 1] * f) | to_e4m3x2(v[4 * i + 2] * f, v[4 * i + 3] * f) << 16;
+  return s;
 }
 
 // ---- what becomes of a sum -----------------------------------------------------------------------------------
@@ -93,192 +179,201 @@ struct ForwardArgs {
   uint8_t* scales;              // [rows, blocks (2 blocks gated)] with e4m3
   int64_t ld_add, ld_out, ld_saved;
   int32_t bias_f32, out_f32, act, n, blocks;
+  int32_t wide;                 // eight columns of every tensor's rows are aligned as a whole (16 bytes at most)
 };
 struct BackwardArgs {
   const void *add, *saved;      // saved: [rows, k (2 k below == 2)] T or e4m3
   const uint8_t* scales;
   void *dx, *h;
   int64_t ld_add, ld_saved, ld_dx, ld_h;
-  int32_t below, act, k, blocks;   // below: 0 none, 1 an activation, 2 a gated one
+  int32_t below, act, k, blocks, wide;   // below: 0 none, 1 an activation, 2 a gated one
 };
 
-// N rows from `row` on, of which `left` count, in column f of this lane: z, and z_up of a gated layer.  A warp calls it as a whole; the N rows'
-// loads, sums and stores are independent of one another, so that none waits for the row before it.
+// P times eight rows from `row` on, of which the first `left` count: lane l has rows l / 4, 8 + l / 4 .., columns f .. f + 7 with f the tile's
+// first + 8 (l % 4): z, and z_up of a gated layer.  A warp calls it as a whole, with the same rows.  (With a column per lane and a row after the other the
+// gradient through a gated layer took five times as many instructions.)  What is read is read without a condition (behind the last row that counts, that
+// row again: a branch around every load made the loads wait for one another).
 template <typename T, bool GATED>
 struct Forward {
   const ForwardArgs& a;
-  float b = 0.f, b_up = 0.f;
-  int f;
-  bool on;
-  __device__ __forceinline__ Forward(const ForwardArgs& a_, int group, int f_) : a(a_), f(f_), on(f_ < a_.n) {
-    if (a.bias && on) {
-      const int64_t i = (int64_t)group * a.n + f;
-      b = a.bias_f32 ? ((const float*)a.bias)[i] : load_as_float((const T*)a.bias + i);
-      if (GATED) b_up = a.bias_f32 ? ((const float*)a.bias_up)[i] : load_as_float((const T*)a.bias_up + i);
+  float b[8] = {}, b_up[8] = {};
+  int f, count;   // columns that exist
+  __device__ __forceinline__ void bias_of(const void* p, int64_t at, float (&v)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < count) v[j] = a.bias_f32 ? ((const float*)p)[at + j] : load_as_float((const T*)p + at + j);
+  }
+  __device__ __forceinline__ Forward(const ForwardArgs& a_, int group, int f_) : a(a_), f(f_), count(min(max(a_.n - f_, 0), 8)) {
+    if (!a.bias) return;
+    bias_of(a.bias, (int64_t)group * a.n + f, b);
+    if (GATED) bias_of(a.bias_up, (int64_t)group * a.n + f, b_up);
+  }
+  __device__ __forceinline__ void keep(int64_t row, bool on, const float (&v)[8], int half) const {
+    if (a.scales) {
+      float z[8];
+      uint32_t w[2];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z[j] = j < count ? v[j] : 0.f;
+      const uint32_t s = pack_8(z, w);
+      if (!on || count == 0) return;
+      store_words_8((uint8_t*)a.saved + row * a.ld_saved + half * a.n + f, a.wide && (!half || a.n % 8 == 0), count, w);
+      if ((f & 31) == 0) a.scales[row * (GATED ? 2 * a.blocks : a.blocks) + half * a.blocks + (f >> 5)] = (uint8_t)s;
+    } else if (on && count) {
+      store_8((T*)a.saved + row * a.ld_saved + half * a.n + f, a.wide && (!half || a.n % 8 == 0), count, v);
     }
   }
-  template <int N>
-  __device__ __forceinline__ void keep8(int64_t row, int left, const float (&z)[N], int half) const {
-    uint32_t s[N], mine = 0u;
-#pragma unroll
-    for (int j = 0; j < N; ++j) s[j] = warp_block_scale(on ? z[j] : 0.f);
-    uint8_t* q = (uint8_t*)a.saved + row * a.ld_saved + half * a.n + f;
-    uint32_t bytes[(N + 1) / 2];
-#pragma unroll
-    for (int j = 0; j < N; j += 2)
-      bytes[j / 2] = to_e4m3x2(z[j] * scale_inverse(s[j]), j + 1 < N ? z[j + 1 < N ? j + 1 : j] * scale_inverse(s[j + 1 < N ? j + 1 : j]) : 0.f);
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      if (on && j < left) q[j * a.ld_saved] = (uint8_t)(bytes[j / 2] >> (8 * (j & 1)));
-      if (j == (f & 31)) mine = s[j];
-    }
-    // lane j has row j's scale
-    const int first = f & ~31, stride = GATED ? 2 * a.blocks : a.blocks, j = f & 31;
-    if (first < a.n && j < N && j < left) a.scales[(row + j) * stride + half * a.blocks + (first >> 5)] = (uint8_t)mine;
-  }
-  template <int N>
-  __device__ __forceinline__ void keep(int64_t row, int left, const float (&z)[N], int half) const {
-    if (a.scales) return keep8(row, left, z, half);
-    T* o = (T*)a.saved + row * a.ld_saved + half * a.n + f;
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (on && j < left) store_as(o + j * a.ld_saved, z[j]);
-  }
-  template <int N, typename O>
-  __device__ __forceinline__ void finish(int64_t row, int left, float (&z)[N], float (&up)[N]) const {
+  template <typename O, int P>
+  __device__ __forceinline__ void finish(int64_t row, int left, float (&z)[P][8], float (&up)[P][8]) const {
     constexpr bool kFast = sizeof(T) == 2;
-    float add[N] = {};
-    if (a.add) {
-      const O* p = (const O*)a.add + row * a.ld_add + f;
+    const int r = (threadIdx.x & 31) >> 2;
+    uint32_t add[P][2 * sizeof(O)] = {};
+    if (a.add && count) {
 #pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (on && j < left) add[j] = load_as_float(p + j * a.ld_add);
+      for (int i = 0; i < P; ++i) load_8((const O*)a.add + (row + min(r + 8 * i, left - 1)) * a.ld_add + f, a.wide, count, add[i]);
     }
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      z[j] += b;
-      if (GATED) up[j] += b_up;
-    }
+    for (int i = 0; i < P; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        z[i][j] += b[j];
+        if (GATED) up[i][j] += b_up[j];
+      }
     if (a.saved) {
-      keep(row, left, z, 0);
-      if (GATED) keep(row, left, up, 1);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        keep(row + r + 8 * i, r + 8 * i < left, z[i], 0);
+        if (GATED) keep(row + r + 8 * i, r + 8 * i < left, up[i], 1);
+      }
     }
     if (a.act == MCCE_ACT_SILU) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) z[j] *= sigmoid<kFast>(z[j]);
+      for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[i][j] *= sigmoid<kFast>(z[i][j]);
     } else if (a.act == MCCE_ACT_GELU) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) z[j] *= normcdff(z[j]);
-    }
-    O* o = (O*)a.out + row * a.ld_out + f;
+      for (int i = 0; i < P; ++i)
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (on && j < left) store_as(o + j * a.ld_out, (GATED ? z[j] * up[j] : z[j]) + add[j]);
+        for (int j = 0; j < 8; ++j) z[i][j] *= normcdff(z[i][j]);
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      float y[8];
+      floats_of(add[i], y);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] += GATED ? z[i][j] * up[i][j] : z[i][j];
+      if (r + 8 * i < left && count) store_8((O*)a.out + (row + r + 8 * i) * a.ld_out + f, a.wide, count, y);
+    }
   }
-  template <int N>
-  __device__ __forceinline__ void rows(int64_t row, int left, float (&z)[N], float (&up)[N]) const {
-    if (a.out_f32) finish<N, float>(row, left, z, up);
-    else finish<N, T>(row, left, z, up);
+  template <int P>
+  __device__ __forceinline__ void rows(int64_t row, int left, float (&z)[P][8], float (&up)[P][8]) const {
+    if (left <= 0) return;
+    if (a.out_f32) finish<float, P>(row, left, z, up);
+    else finish<T, P>(row, left, z, up);
   }
 };
 
-// The same for a gradient with respect to rows, t[N], in two steps: `ask` reads what the layer below kept (or what is added),
-// `rows` uses it, so that a caller can wait for its sums in between.
+// The same for a gradient with respect to rows, t, in two steps: `ask` reads what the layer below kept (or what is added), `rows` uses it, so
+// that a caller can wait for its sums in between.
 template <typename T>
 struct Backward {
   const BackwardArgs& a;
-  int f;
-  bool on;
-  __device__ __forceinline__ Backward(const BackwardArgs& a_, int, int f_) : a(a_), f(f_), on(f_ < a_.k) {}
-  template <int N>
+  int f, count;
+  bool wide_up;   // the second half of the columns too
+  __device__ __forceinline__ Backward(const BackwardArgs& a_, int, int f_)
+      : a(a_), f(f_), count(min(max(a_.k - f_, 0), 8)), wide_up(a_.wide && a_.k % 8 == 0) {}
+  template <int P>
   struct Asked {
-    uint32_t z[N], up[N], scales[N];   // as they lie in memory; scales: z's in the low byte, up's in the next
+    uint32_t z[P][2 * sizeof(T)], up[P][2 * sizeof(T)], scales[P];   // as they lie in memory; scales: z's in the low byte, up's in the next
   };
-  __device__ __forceinline__ uint32_t raw(const float* p) const { return __float_as_uint(*p); }
-  __device__ __forceinline__ uint32_t raw(const __nv_bfloat16* p) const { return *(const uint16_t*)p; }
-  __device__ __forceinline__ float value(uint32_t v) const { return __uint_as_float(sizeof(T) == 2 ? v << 16 : v); }
-  template <int N>
-  __device__ __forceinline__ void ask(int64_t row, int left, Asked<N>& q) const {
+  template <int P>
+  __device__ __forceinline__ void ask(int64_t row, int left, Asked<P>& q) const {
 #pragma unroll
-    for (int j = 0; j < N; ++j) q.z[j] = q.up[j] = q.scales[j] = 0u;
-    if (!on) return;
+    for (int i = 0; i < P; ++i) {
+      q.scales[i] = 0u;
+#pragma unroll
+      for (int j = 0; j < 2 * (int)sizeof(T); ++j) q.z[i][j] = q.up[i][j] = 0u;
+    }
+    if (!count || left <= 0) return;
+    const int r = (threadIdx.x & 31) >> 2;
     if (a.below && a.scales) {
-      const uint8_t *p = (const uint8_t*)a.saved + row * a.ld_saved + f, *s = a.scales + row * a.below * a.blocks + (f >> 5);
+      uint32_t su[P] = {};
 #pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (j < left) q.z[j] = p[j * a.ld_saved], q.scales[j] = s[j * a.below * a.blocks];
-      if (a.below == 2) {
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-          if (j < left) q.up[j] = p[j * a.ld_saved + a.k], q.scales[j] |= (uint32_t)s[j * 2 * a.blocks + a.blocks] << 8;
+      for (int i = 0; i < P; ++i) {
+        const int64_t at = row + min(r + 8 * i, left - 1);
+        const uint8_t *p = (const uint8_t*)a.saved + at * a.ld_saved + f, *s = a.scales + at * a.below * a.blocks + (f >> 5);
+        uint32_t w[2];
+        load_8(p, a.wide, count, w);
+        q.z[i][0] = w[0], q.z[i][1] = w[1], q.scales[i] = s[0];
+        if (a.below == 2) {
+          load_8(p + a.k, wide_up, count, w);
+          q.up[i][0] = w[0], q.up[i][1] = w[1], su[i] = s[a.blocks];
+        }
       }
-    } else if (a.below) {
-      const T* p = (const T*)a.saved + row * a.ld_saved + f;
 #pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (j < left) q.z[j] = raw(p + j * a.ld_saved);
-      if (a.below == 2) {
+      for (int i = 0; i < P; ++i) q.scales[i] |= su[i] << 8;
+    } else if (a.below || a.add) {
+      const T* p = (const T*)(a.below ? a.saved : a.add) + f;
+      const int64_t ld = a.below ? a.ld_saved : a.ld_add;
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-          if (j < left) q.up[j] = raw(p + j * a.ld_saved + a.k);
+      for (int i = 0; i < P; ++i) {
+        const T* at = p + (row + min(r + 8 * i, left - 1)) * ld;
+        load_8(at, a.wide, count, q.z[i]);
+        if (a.below == 2) load_8(at + a.k, wide_up, count, q.up[i]);
       }
-    } else if (a.add) {
-      const T* p = (const T*)a.add + row * a.ld_add + f;
-#pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (j < left) q.z[j] = raw(p + j * a.ld_add);
     }
   }
-  template <int N>
-  __device__ __forceinline__ void rows(int64_t row, int left, const float (&t)[N], const Asked<N>& q) const {
-    if (!on) return;
-    T* dx = (T*)a.dx + row * a.ld_dx + f;
-    float z[N], up[N];
-    if (a.below && a.scales) {
+  template <int P>
+  __device__ __forceinline__ void rows(int64_t row, int left, const float (&t)[P][8], const Asked<P>& q) const {
+    if (!count || left <= 0) return;
+    const int r = (threadIdx.x & 31) >> 2;
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float2 v = e4m3x2_value(q.z[j], q.up[j]);
-        z[j] = v.x * scale_value(q.scales[j] & 255u), up[j] = v.y * scale_value(q.scales[j] >> 8);
+    for (int i = 0; i < P; ++i) {
+      const bool on = r + 8 * i < left;
+      T* dx = (T*)a.dx + (row + r + 8 * i) * a.ld_dx + f;
+      float z[8], up[8], slope[8], v[8];
+      if (a.below && a.scales) {
+        const uint32_t wz[2] = {q.z[i][0], q.z[i][1]}, wu[2] = {q.up[i][0], q.up[i][1]};
+        const float sz = scale_value(q.scales[i] & 255u), su = scale_value(q.scales[i] >> 8);
+        floats_of(wz, z), floats_of(wu, up);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] *= sz, up[j] *= su;
+      } else {
+        floats_of(q.z[i], z), floats_of(q.up[i], up);
       }
-    } else {
+      if (!a.below) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) z[j] = value(q.z[j]), up[j] = value(q.up[j]);
-    }
-    if (!a.below) {
+        for (int j = 0; j < 8; ++j) v[j] = t[i][j] + z[j];
+        if (on) store_8(dx, a.wide, count, v);
+        continue;
+      }
+      if (a.act == MCCE_ACT_SILU) {
 #pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (j < left) store_as(dx + j * a.ld_dx, t[j] + z[j]);
-      return;
-    }
-    float slope[N];
-    if (a.act == MCCE_ACT_SILU) {
+        for (int j = 0; j < 8; ++j) slope_and_value<sizeof(T) == 2>(z[j], MCCE_ACT_SILU, z[j], slope[j]);
+      } else if (a.act == MCCE_ACT_GELU) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) slope_and_value<sizeof(T) == 2>(z[j], MCCE_ACT_SILU, z[j], slope[j]);
-    } else if (a.act == MCCE_ACT_GELU) {
+        for (int j = 0; j < 8; ++j) slope_and_value<sizeof(T) == 2>(z[j], MCCE_ACT_GELU, z[j], slope[j]);
+      } else {
 #pragma unroll
-      for (int j = 0; j < N; ++j) slope_and_value<sizeof(T) == 2>(z[j], MCCE_ACT_GELU, z[j], slope[j]);
-    } else {
+        for (int j = 0; j < 8; ++j) slope[j] = 1.f;
+      }
+      T* h = (T*)a.h + (row + r + 8 * i) * a.ld_h + f;
+      if (a.below == 2) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) slope[j] = 1.f;
-    }
-    T* h = (T*)a.h + row * a.ld_h + f;
-    if (a.below == 2) {
+        for (int j = 0; j < 8; ++j) v[j] = t[i][j] * up[j] * slope[j];
+        if (on) store_8(dx, a.wide, count, v);
 #pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (j < left) {
-          store_as(dx + j * a.ld_dx, t[j] * up[j] * slope[j]);
-          store_as(dx + j * a.ld_dx + a.k, t[j] * z[j]);
-        }
+        for (int j = 0; j < 8; ++j) v[j] = t[i][j] * z[j];
+        if (on) store_8(dx + a.k, wide_up, count, v);
 #pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (a.h && j < left) store_as(h + j * a.ld_h, z[j] * up[j]);
-    } else {
+        for (int j = 0; j < 8; ++j) v[j] = z[j] * up[j];
+        if (on && a.h) store_8(h, a.wide, count, v);
+      } else {
 #pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (j < left) store_as(dx + j * a.ld_dx, t[j] * slope[j]);
-#pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (a.h && j < left) store_as(h + j * a.ld_h, z[j]);
+        for (int j = 0; j < 8; ++j) v[j] = t[i][j] * slope[j];
+        if (on) store_8(dx, a.wide, count, v);
+        if (on && a.h) store_8(h, a.wide, count, z);
+      }
     }
   }
 };
@@ -291,7 +386,7 @@ struct Problem {
   const void *x, *y, *w, *w_up;    // forward: x, w; backward: y, w; dweight: y, x
   void *dw, *dw_up;                // dweight
   const void *add_dw, *add_dw_up;
-  int32_t dw_f32, dw_wide;   // dw_wide: its rows (and those added) start at multiples of 16 bytes
+  int32_t dw_f32, dw_wide;   // dw_wide: its rows (and those added) start at multiples of 32 bytes
   ForwardArgs fwd;
   BackwardArgs bwd;
 };

@@ -30,6 +30,7 @@ __device__ uint32_t wait_error;   // set when a bounded wait gives up; read and 
 constexpr int kTileM = 128;    // MMA rows
 constexpr int kSlab = 64;      // reduction per stage: 64 bf16 = one 128-byte swizzled row
 constexpr int kEpilogueWarps = 8;
+constexpr int kSwapStride = 36;   // floats of a row: reading eight columns per lane, four lanes a row, then meets every bank once
 constexpr int kThreads = 64 + 32 * kEpilogueWarps;
 constexpr uint32_t kABytes = kTileM * kSlab * 2;
 constexpr uint32_t kPanelBytes = kSlab * 128;   // an operand across its rows: 64 rows of 64 columns
@@ -41,7 +42,8 @@ struct Cfg {
   static constexpr int kFeatures = kTileM * kCtas / (KIND == kForward && GATED ? 2 : 1);   // of a tile
   static constexpr uint32_t kBBytes = BN / kCtas * kSlab * 2;
   static constexpr uint32_t kStageBytes = kABytes + kBBytes;
-  static constexpr uint32_t kSwapBytes = KIND == kForward && GATED ? 4 * 2 * 2 * 8 * 32 * 4 : 0;
+  // sums of 16 rows x 32 features per epilogue warp, on their way from a feature per lane to a row per four lanes; gated: two buffers
+  static constexpr uint32_t kSwapBytes = KIND == kDweight ? 0 : kEpilogueWarps * 16 * kSwapStride * 4 * (KIND == kForward && GATED ? 2 : 1);
   static constexpr uint32_t kCountBytes = KIND == kDweight ? 0 : ((MCCE_LINEAR_MAX_GROUPS + 1 + 33) * 4 + 127) & ~127;
   static constexpr uint32_t kFixed = 1024 + 512 + kSwapBytes + kCountBytes;
   static constexpr int kFit = (232448 - kFixed) / kStageBytes;
@@ -151,6 +153,57 @@ __device__ __forceinline__ void free_tmem(uint32_t addr, uint32_t cols) {
   else tmem_dealloc(addr, cols);
 }
 
+// 16 neighbouring sums of a row, added to what is there, 32 bytes at a time (whole sectors) where rows are aligned to it.
+__device__ __forceinline__ void load_32(const void* p, uint32_t (&v)[8]) {
+  asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+               : "l"(p));
+}
+__device__ __forceinline__ void store_32(void* p, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]),
+               "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+template <typename O>
+__device__ __forceinline__ void store_16(O* o, const O* add, float (&v)[16], int left, bool wide) {
+  if (!wide || left < 16) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      if (j < left) store_as(o + j, v[j] + (add ? load_as_float(add + j) : 0.f));
+    return;
+  }
+  constexpr int kParts = sizeof(O) / 2;
+  uint32_t q[kParts][8];
+  if (add) {
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) load_32((const uint8_t*)add + 32 * i, q[i]);
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      v[j] += sizeof(O) == 4 ? __uint_as_float(q[j / 8 * (kParts - 1)][j % 8])
+                             : __uint_as_float(j & 1 ? q[0][j / 2] & 0xffff0000u : q[0][j / 2] << 16);
+  }
+  if (sizeof(O) == 4) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) q[j / 8 * (kParts - 1)][j % 8] = __float_as_uint(v[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+      q[0][j] = *(const uint32_t*)&h;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kParts; ++i) store_32((uint8_t*)o + 32 * i, q[i]);
+}
+
+// This lane's eight columns of its row among eight
+__device__ __forceinline__ void row_of(const float* buffer, int first, float (&v)[8]) {
+  const int lane = threadIdx.x & 31;
+  const float4* p = (const float4*)(buffer + (first + (lane >> 2)) * kSwapStride + 8 * (lane & 3));
+  const float4 a = p[0], b = p[1];
+  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+
 struct Item {
   int g, f0;        // group, first feature (dweight: first column of dout)
   int row, rows;    // first row among all, rows of the tile (dweight: the group's)
@@ -214,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem_al = smem_raw + (smem_base - smem_u32(smem_raw));
   uint8_t* rest = smem_al + (size_t)C::kStages * C::kStageBytes;
-  float* swap = (float*)rest;   // [pair of warps][buffer][direction][8 rows][32 lanes]
+  float* swap = (float*)rest;
   int* before = (int*)(rest + C::kSwapBytes);
   uint64_t* bars = (uint64_t*)(rest + C::kSwapBytes + C::kCountBytes);
   const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * C::kStages;
@@ -402,89 +455,56 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
           }
           if (!on) continue;
           const int left = min(16, cols - c);
-          if (p.dw_f32) {
-            float* o = (float*)dw + at + c;
-            const float* a = add ? (const float*)add + at + c : nullptr;
-            if (p.dw_wide && left == 16) {
-#pragma unroll
-              for (int j = 0; j < 16; j += 4) {
-                float4 q = a ? *(const float4*)(a + j) : make_float4(0.f, 0.f, 0.f, 0.f);
-                q.x += v[j], q.y += v[j + 1], q.z += v[j + 2], q.w += v[j + 3];
-                *(float4*)(o + j) = q;
-              }
-            } else {
-#pragma unroll
-              for (int j = 0; j < 16; ++j)
-                if (j < left) o[j] = v[j] + (a ? a[j] : 0.f);
-            }
-          } else {
-            __nv_bfloat16* o = (__nv_bfloat16*)dw + at + c;
-            const __nv_bfloat16* a = add ? (const __nv_bfloat16*)add + at + c : nullptr;
-            if (p.dw_wide && left == 16) {
-#pragma unroll
-              for (int j = 0; j < 16; j += 8) {
-                uint4 q = a ? *(const uint4*)(a + j) : make_uint4(0u, 0u, 0u, 0u);
-                __nv_bfloat162* h = (__nv_bfloat162*)&q;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                  const float2 f = __bfloat1622float2(h[u]);
-                  h[u] = __floats2bfloat162_rn(f.x + v[j + 2 * u], f.y + v[j + 2 * u + 1]);
-                }
-                *(uint4*)(o + j) = q;
-              }
-            } else {
-#pragma unroll
-              for (int j = 0; j < 16; ++j)
-                if (j < left) store_as(o + j, v[j] + (a ? load_as_float(a + j) : 0.f));
-            }
-          }
+          if (p.dw_f32) store_16((float*)dw + at + c, add ? (const float*)add + at + c : nullptr, v, min(16, cols - c), p.dw_wide);
+          else store_16((__nv_bfloat16*)dw + at + c, add ? (const __nv_bfloat16*)add + at + c : nullptr, v, min(16, cols - c), p.dw_wide);
         }
       } else if constexpr (KIND == kForward && GATED) {
         // quadrants 0 and 1 hold z, 2 and 3 z_up of the same 64 features; of every 16 rows the first 8 are finished by the warp that holds z
         const int pair = (quad & 1) * 2 + team, up = quad >> 1;
-        const Forward<__nv_bfloat16, true> e(p.fwd, it.g, it.f0 + (quad & 1) * 32 + lane);
-        for (int c = 16 * team; c < it.rows && alive; c += 32, ++swaps) {
-          float v[16];
+        const Forward<__nv_bfloat16, true> e(p.fwd, it.g, it.f0 + (quad & 1) * 32 + 8 * (lane & 3));
+        for (int c = 16 * team; c < it.rows; c += 32, ++swaps) {
+          float v[16], z[1][8], z_up[1][8];
           __syncwarp();
           tmem_ld16(t0 + c, v);
           tmem_ld_wait();
-          float* mine = swap + (pair * 2 + (swaps & 1)) * 512 + up * 256;
-          const float* theirs = swap + (pair * 2 + (swaps & 1)) * 512 + (up ^ 1) * 256;
+          float* both = swap + (pair * 2 + (swaps & 1)) * 2 * 16 * kSwapStride;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) mine[j * 32 + lane] = up ? v[j] : v[8 + j];
+          for (int j = 0; j < 16; ++j) both[(up * 16 + j) * kSwapStride + lane] = v[j];
           __syncwarp();
           if (lane == 0) mbar_arrive(bar_swap + 8 * pair);
           if (!mbar_wait(bar_swap + 8 * pair, swaps & 1u, abort_flag, &wait_error, 5u)) {
             alive = false;
             break;
           }
-          float z[8], z_up[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float other = theirs[j * 32 + lane];
-            z[j] = up ? other : v[j], z_up[j] = up ? v[8 + j] : other;
-          }
+          row_of(both, up * 8, z[0]);
+          row_of(both + 16 * kSwapStride, up * 8, z_up[0]);
           e.rows((int64_t)it.row + c + up * 8, it.rows - c - up * 8, z, z_up);
         }
-      } else if constexpr (KIND == kForward) {
-        const Forward<__nv_bfloat16, false> e(p.fwd, it.g, it.f0 + quad * 32 + lane);
-        for (int c = 16 * team; c < it.rows; c += 32) {
-          float v[16], none[16];
-          __syncwarp();
-          tmem_ld16(t0 + c, v);
-          tmem_ld_wait();
-          e.rows((int64_t)it.row + c, it.rows - c, v, none);
-        }
       } else {
-        const Backward<__nv_bfloat16> e(p.bwd, it.g, it.f0 + quad * 32 + lane);
+        typedef typename std::conditional<KIND == kForward, Forward<__nv_bfloat16, false>, Backward<__nv_bfloat16>>::type Epilogue;
+        typename std::conditional<KIND == kForward, const ForwardArgs&, const BackwardArgs&>::type args = [&]() -> auto& {
+          if constexpr (KIND == kForward) return p.fwd;
+          else return p.bwd;
+        }();
+        const Epilogue e(args, it.g, it.f0 + quad * 32 + 8 * (lane & 3));
+        float* mine = swap + (warp - 2) * 16 * kSwapStride;
         for (int c = 16 * team; c < it.rows; c += 32) {
-          Backward<__nv_bfloat16>::Asked<16> q;
-          e.ask((int64_t)it.row + c, it.rows - c, q);
-          float v[16];
+          float v[16], t[2][8];
+          Backward<__nv_bfloat16>::Asked<2> q;
+          if constexpr (KIND == kBackward) e.ask((int64_t)it.row + c, it.rows - c, q);
           __syncwarp();
           tmem_ld16(t0 + c, v);
           tmem_ld_wait();
-          e.rows((int64_t)it.row + c, it.rows - c, v, q);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) mine[j * kSwapStride + lane] = v[j];
+          __syncwarp();
+          row_of(mine, 0, t[0]), row_of(mine, 8, t[1]);
+          if constexpr (KIND == kBackward) {
+            e.rows((int64_t)it.row + c, it.rows - c, t, q);
+          } else {
+            float none[2][8];
+            e.rows((int64_t)it.row + c, it.rows - c, t, none);
+          }
         }
       }
       if (sums) {
