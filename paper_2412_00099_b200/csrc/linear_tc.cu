@@ -49,13 +49,12 @@ struct Cfg {
   static constexpr int kFit = (232448 - kFixed) / kStageBytes;
   static constexpr int kStages = kFit < 10 ? kFit : 10;
   static constexpr size_t kSmemBytes = kFixed + (size_t)kStages * kStageBytes;
-  static constexpr int kRowBox = BN / kCtas;   // token rows per TMA copy, or half as many: one copy whatever the tile has
+  static constexpr int kRowBox = BN / kCtas;   // most rows per TMA copy
 };
 
 struct Maps {
   CUtensorMap a, a_up;   // weights; dweight: dout and its second half
-  CUtensorMap b, b_up;   // rows; dweight: x
-  CUtensorMap b_half, b_up_half;   // rows, boxes of half the height
+  CUtensorMap b[4], b_up[4];   // rows, boxes of 1/4, 2/4, 3/4 and 4/4 of a CTA's most; dweight: x (the first)
   int a_panels, b_panels;   // operands across their rows: 64-column panels that one copy brings
 };
 
@@ -215,28 +214,29 @@ struct Walk {
   static constexpr int kFeatures = Cfg<KIND, GATED, BN, PAIR>::kFeatures;
   const Problem& p;
   const int* before;
-  int64_t items;
+  int first, step, items;   // this CTA's (pair's) tiles: first, first + step ..
   int FT, JT;   // tiles of features (dweight: of dout's columns), of x's columns
   __device__ __forceinline__ Walk(const Problem& p_, const int* before_) : p(p_), before(before_) {
     const int features = KIND == kBackward ? p.k : p.n;
+    first = PAIR ? blockIdx.x >> 1 : blockIdx.x, step = PAIR ? gridDim.x >> 1 : gridDim.x;
     FT = (features + kFeatures - 1) / kFeatures, JT = KIND == kDweight ? (p.k + BN - 1) / BN : 1;
-    items = KIND == kDweight ? (int64_t)p.groups.G * (GATED ? 2 : 1) * FT * JT : (int64_t)before[p.groups.G] * FT;
+    items = KIND == kDweight ? p.groups.G * (GATED ? 2 : 1) * FT * JT : before[p.groups.G] * FT;   // fits: the launch sees to it
   }
-  __device__ __forceinline__ Item at(int64_t w) const {
+  __device__ __forceinline__ Item decode(int w) const {
     Item it;
     if (KIND == kDweight) {
-      it.f0 = (int)(w % FT) * kFeatures, w /= FT;
-      it.j0 = (int)(w % JT) * BN, w /= JT;
-      it.half = GATED ? (int)(w & 1) : 0;
-      it.g = (int)(GATED ? w >> 1 : w);
+      it.f0 = w % FT * kFeatures, w /= FT;
+      it.j0 = w % JT * BN, w /= JT;
+      it.half = GATED ? w & 1 : 0;
+      it.g = GATED ? w >> 1 : w;
       const GroupRows gr = group_rows(p.groups, it.g);
       it.row = (int)gr.first, it.rows = (int)gr.m;
     } else {
-      it.g = find_group(before, p.groups.G, (int)(w / FT));
+      it.g = find_group(before, p.groups.G, w / FT);
       const GroupRows gr = group_rows(p.groups, it.g);
       const int tiles = before[it.g + 1] - before[it.g];
-      const int64_t in = w - (int64_t)before[it.g] * FT;
-      const int block = (int)(in / (kBlockOfTiles * FT)), rest = (int)(in % (kBlockOfTiles * FT));
+      const int in = w - before[it.g] * FT;
+      const int block = in / (kBlockOfTiles * FT), rest = in % (kBlockOfTiles * FT);
       const int wide = min(kBlockOfTiles, tiles - block * kBlockOfTiles);
       const int tile = block * kBlockOfTiles + rest % wide;
       it.f0 = rest / wide * kFeatures;
@@ -245,6 +245,23 @@ struct Walk {
       it.j0 = it.half = 0;
     }
     return it;
+  }
+  // The i-th tile, by a whole warp: its lanes work out 32 tiles at a time (divisions and loads of offsets are paid once for them), `mine` is
+  // the lane's.  False behind the last one.
+  __device__ __forceinline__ bool at(int i, Item& mine, Item& it) const {
+    const int64_t w = first + (int64_t)i * step;
+    if (w >= items) return false;
+    const int lane = threadIdx.x & 31;
+    if ((i & 31) == 0) {
+      const int64_t own = w + (int64_t)lane * step;
+      mine = decode(own < items ? (int)own : items - 1);
+    }
+    const int from = i & 31;
+    it.g = __shfl_sync(0xffffffffu, mine.g, from), it.f0 = __shfl_sync(0xffffffffu, mine.f0, from);
+    it.row = __shfl_sync(0xffffffffu, mine.row, from), it.rows = __shfl_sync(0xffffffffu, mine.rows, from);
+    it.j0 = KIND == kDweight ? __shfl_sync(0xffffffffu, mine.j0, from) : 0;
+    it.half = KIND == kDweight && GATED ? __shfl_sync(0xffffffffu, mine.half, from) : 0;
+    return true;
   }
   // N of the tile's MMAs: its rows; its columns of x, in whole panels for each CTA
   __device__ __forceinline__ int wide(const Item& it) const {
@@ -276,7 +293,6 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
   volatile uint32_t* abort_flag = tmem_slot + 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = PAIR ? (int)cluster_rank() : 0;
-  const int64_t first = PAIR ? blockIdx.x >> 1 : blockIdx.x, step = PAIR ? gridDim.x >> 1 : gridDim.x;
   // in a pair, the follower's last slab of a group is complete when its own warp has cleared the rows of the next group (dweight)
   constexpr bool kTail = PAIR && KIND == kDweight;
 
@@ -303,21 +319,22 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
   const uint32_t tmem_base = *tmem_slot;
   const Walk<KIND, GATED, BN, PAIR> walk(p, before);
 
+  Item it, mine;
   if (warp == 0) {
-    if (lane == 0) {
-      uint32_t stage = 0, phase = 0;
-      bool alive = true;
-      for (int64_t w = first; w < walk.items && alive; w += step) {
-        const Item it = walk.at(w);
+    uint32_t stage = 0, phase = 0;
+    bool alive = true;
+    for (int i = 0; alive && walk.at(i, mine, it); ++i) {
+      if (lane == 0) {
         const int slabs = walk.slabs(it), part = GATED && KIND == kBackward ? slabs / 2 : slabs;
         const int f0 = it.f0 + rank * (C::kFeatures / C::kCtas);
         // this CTA's share of the MMA's N dimension
         const int share = walk.wide(it) / C::kCtas;
         const int row = it.row + rank * share, j0 = it.j0 + rank * share;
         const int panels = KIND == kDweight && maps.b_panels > 1 ? maps.b_panels : (share + 63) / 64;
-        const bool half = share <= C::kRowBox / 2;
-        const uint32_t tx = kABytes + (KIND == kDweight ? panels * kPanelBytes : (uint32_t)(half ? C::kRowBox / 2 : C::kRowBox) * kSlab * 2);
-        const CUtensorMap *map_b = half ? &maps.b_half : &maps.b, *map_b_up = half ? &maps.b_up_half : &maps.b_up;
+        // a CTA's rows come in one copy of the lowest box that has them: a second copy costs more than the rows that it saves
+        constexpr int kQuarter = C::kRowBox / 4;
+        const int quarters = (share + kQuarter - 1) / kQuarter;
+        const uint32_t tx = kABytes + (KIND == kDweight ? panels * kPanelBytes : (uint32_t)(quarters * kQuarter) * kSlab * 2);
         for (int kt = 0; kt < slabs; ++kt) {
           if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, &wait_error, 1u)) {
             alive = false;
@@ -343,28 +360,28 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
             } else {
               load_3d<PAIR>(sa, &maps.a, x, f0, it.g, full);
             }
-            load_2d<PAIR>(sb, map_b, x, row, full);
+            load_2d<PAIR>(sb, &maps.b[quarters - 1], x, row, full);
           } else if (KIND == kBackward) {
             const bool up = kt >= part;
             const int x = (up ? kt - part : kt) * kSlab;
             load_panels<PAIR>(sa, up ? &maps.a_up : &maps.a, maps.a_panels, 2, f0, x, it.g, full);
-            load_2d<PAIR>(sb, up ? map_b_up : map_b, x, row, full);
+            load_2d<PAIR>(sb, up ? &maps.b_up[quarters - 1] : &maps.b[quarters - 1], x, row, full);
           } else {
             const int y = it.row + kt * kSlab;
             load_panels<PAIR>(sa, it.half ? &maps.a_up : &maps.a, maps.a_panels, 2, f0, y, 0, full);
-            load_panels<PAIR>(sb, &maps.b, maps.b_panels, panels, j0, y, 0, full);
+            load_panels<PAIR>(sb, &maps.b[0], maps.b_panels, panels, j0, y, 0, full);
           }
           if (++stage == C::kStages) stage = 0, phase ^= 1u;
         }
       }
+      alive = __shfl_sync(0xffffffffu, alive, 0);
     }
   } else if (warp == 1) {
     // The whole warp walks along: in dweight's last slab its lanes clear the rows that belong to the next group (of both operands: zero times a
     // NaN of the next group would not be zero).
     uint32_t stage = 0, phase = 0, acc = 0, tails = 0;   // tails: the phase of every stage's bar_tail
     bool alive = true;
-    for (int64_t w = first; w < walk.items && alive; w += step) {
-      const Item it = walk.at(w);
+    for (int i = 0; alive && walk.at(i, mine, it); ++i) {
       const int slabs = walk.slabs(it);
       if (slabs == 0) continue;
       const int cols = walk.wide(it);
@@ -429,8 +446,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     uint32_t acc = 0, swaps = 0;
     bool alive = true;
-    for (int64_t w = first; w < walk.items && alive; w += step) {
-      Item it = walk.at(w);
+    for (int i = 0; alive && walk.at(i, mine, it); ++i) {
       it.f0 += rank * (C::kFeatures / C::kCtas);
       const bool sums = walk.slabs(it) > 0;
       const uint32_t buf = acc & 1u;
@@ -538,11 +554,14 @@ bool encode(CUtensorMap* m, const void* base, int rank, const cuuint64_t* dims, 
   return fn && fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// [rows, cols], a box of 64 columns
-bool map_rows(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+// [rows, cols], boxes of 64 columns and 1/4 .. 4/4 of `most` rows
+bool map_boxes(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t ld, int most) {
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
-  const cuuint32_t box[2] = {kSlab, (cuuint32_t)box_rows};
-  return encode(m, base, 2, dims, strides, box);
+  for (int i = 0; i < 4; ++i) {
+    const cuuint32_t box[2] = {kSlab, (cuuint32_t)(most / 4 * (i + 1))};
+    if (!encode(m + i, base, 2, dims, strides, box)) return false;
+  }
+  return true;
 }
 // [groups, n, k], a box of 64 columns: what lies outside a matrix is filled with zeros, not with the next matrix
 bool map_weights(CUtensorMap* m, const void* base, const Problem& p, int box_rows) {
@@ -584,21 +603,18 @@ cudaError_t launch(const Problem& p, cudaStream_t st) {
   m.a_panels = m.b_panels = 1;
   if (KIND == kDweight) {
     static_assert(KIND != kDweight || BN / C::kCtas == 128, "two panels of x's columns per CTA");
-    ok = map_panels(&m.a, &m.a_panels, y, 1, rows, p.n, p.ld_y, 0) && map_panels(&m.b, &m.b_panels, p.x, 1, rows, p.k, p.ld_x, 0) &&
+    ok = map_panels(&m.a, &m.a_panels, y, 1, rows, p.n, p.ld_y, 0) && map_panels(&m.b[0], &m.b_panels, p.x, 1, rows, p.k, p.ld_x, 0) &&
          (!GATED || map_panels(&m.a_up, &m.a_panels, y + p.n, 1, rows, p.n, p.ld_y, 0));
     most = (int64_t)p.groups.G * (GATED ? 2 : 1) * FT * ((p.k + BN - 1) / BN);
   } else if (KIND == kForward) {
     const int box = GATED ? kTileM / 2 : kTileM;
-    ok = map_weights(&m.a, p.w, p, box) && (!GATED || map_weights(&m.a_up, p.w_up, p, box)) && map_rows(&m.b, p.x, rows, p.k, p.ld_x, C::kRowBox) &&
-         map_rows(&m.b_half, p.x, rows, p.k, p.ld_x, C::kRowBox / 2);
+    ok = map_weights(&m.a, p.w, p, box) && (!GATED || map_weights(&m.a_up, p.w_up, p, box)) && map_boxes(m.b, p.x, rows, p.k, p.ld_x, C::kRowBox);
   } else {
     ok = map_panels(&m.a, &m.a_panels, p.w, p.groups.G, p.n, p.k, p.ld_w, p.step_w) &&
          (!GATED || map_panels(&m.a_up, &m.a_panels, p.w_up, p.groups.G, p.n, p.k, p.ld_w, p.step_w));
-    ok = ok && map_rows(&m.b, y, rows, p.n, p.ld_y, C::kRowBox) && map_rows(&m.b_half, y, rows, p.n, p.ld_y, C::kRowBox / 2);
-    ok = ok && (!GATED || (map_rows(&m.b_up, y + p.n, rows, p.n, p.ld_y, C::kRowBox) &&
-                           map_rows(&m.b_up_half, y + p.n, rows, p.n, p.ld_y, C::kRowBox / 2)));
+    ok = ok && map_boxes(m.b, y, rows, p.n, p.ld_y, C::kRowBox) && (!GATED || map_boxes(m.b_up, y + p.n, rows, p.n, p.ld_y, C::kRowBox));
   }
-  if (!ok) return cudaErrorInvalidValue;
+  if (!ok || most > 0x7fffffffll) return cudaErrorInvalidValue;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
   attr.val.clusterDim.x = C::kCtas, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
