@@ -28,18 +28,19 @@ namespace {
 __device__ uint32_t wait_error;   // set when a bounded wait gives up; read and cleared by mcce_expert_linear_status
 
 constexpr int kTileM = 128;    // MMA rows
-constexpr int kSlab = 64;      // reduction per stage: 64 bf16 = one 128-byte swizzled row
 constexpr int kEpilogueWarps = 8;
 constexpr int kSwapStride = 36;   // floats of a row: reading eight columns per lane, four lanes a row, then meets every bank once
 constexpr int kThreads = 64 + 32 * kEpilogueWarps;
-constexpr uint32_t kABytes = kTileM * kSlab * 2;
-constexpr uint32_t kPanelBytes = kSlab * 128;   // an operand across its rows: 64 rows of 64 columns
 constexpr int kBlockOfTiles = 16;   // row tiles of a group that are walked together, so that their rows stay in L2 for the next features
 
 template <int KIND, bool GATED, int BN, bool PAIR>
 struct Cfg {
   static constexpr int kCtas = PAIR ? 2 : 1;
   static constexpr int kFeatures = kTileM * kCtas / (KIND == kForward && GATED ? 2 : 1);   // of a tile
+  // Reduction per stage.  Along an operand's rows 64 bf16 are a swizzled row of 128 bytes; dweight's operands lie across their rows, and the fewer copies of
+  // 128 rows win (8192 x 4096 x 4096: 193 us, with 64 rows 220).
+  static constexpr int kSlab = KIND == kDweight ? 128 : 64;
+  static constexpr uint32_t kABytes = kTileM * kSlab * 2;
   static constexpr uint32_t kBBytes = BN / kCtas * kSlab * 2;
   static constexpr uint32_t kStageBytes = kABytes + kBBytes;
   // sums of 16 rows x 32 features per epilogue warp, on their way from a feature per lane to a row per four lanes; gated: two buffers
@@ -53,14 +54,15 @@ struct Cfg {
 };
 
 struct Maps {
-  CUtensorMap a, a_up;   // weights; dweight: dout and its second half
-  CUtensorMap b[4], b_up[4];   // rows, boxes of 1/4, 2/4, 3/4 and 4/4 of a CTA's most; dweight: x (the first)
-  int a_panels, b_panels;   // operands across their rows: 64-column panels that one copy brings
+  CUtensorMap a[2], a_up[2];   // weights; dweight: dout and its second half, 128 and 64 rows at a time
+  CUtensorMap b[4], b_up[4];   // rows, boxes of 1/4, 2/4, 3/4 and 4/4 of a CTA's most; dweight: x, 128 and 64 rows at a time
+  int a_whole, b_whole;   // operands across their rows: one copy brings both panels of 64 columns; forward: all matrices in one map of their rows
+  int a_step;             // forward, then: rows from one matrix to the next
 };
 
-// Descriptor of an operand across its rows: panels of 64 columns (128 bytes), kPanelBytes apart; eight rows 1024 bytes apart.
-__device__ __forceinline__ uint64_t smem_desc_across(uint32_t addr) {
-  return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(kPanelBytes >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+// Descriptor of an operand across its rows: panels of 64 columns (128 bytes), `panel` bytes apart; eight rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t smem_desc_across(uint32_t addr, uint32_t panel) {
+  return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(panel >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
 // TMA copies into this CTA's shared memory; in a pair the barrier may be the other CTA's.
 #define MCCE_TMA_LOAD(DIMS, COORDS, ...)                                                                                              \
@@ -87,14 +89,13 @@ __device__ __forceinline__ void load_4d(uint32_t dst, const CUtensorMap* map, in
   MCCE_TMA_LOAD("4d", "%3, %4, %5, %6", "r"(x), "r"(y), "r"(z), "r"(u));
 }
 #undef MCCE_TMA_LOAD
-// `count` panels of 64 columns from column x, 64 rows from row y of matrix g.  The map's dimensions: column in a panel, row, (panel,) matrix.
-// What a copy costs is mostly its own: one that brings two panels instead of two copies (for these and for the rows' boxes) took a product of 8192 x 4096 x
-// 4096 from 1250 to 1450 TFLOP/s.
+// `count` panels of 64 columns from column x, `panel` bytes each, rows from y on, of matrix g.  The map's dimensions: column in a panel, row, (panel,) matrix.
 template <bool PAIR>
-__device__ __forceinline__ void load_panels(uint32_t dst, const CUtensorMap* map, int per_copy, int count, int x, int y, int g, uint32_t bar) {
-  if (per_copy > 1) load_4d<PAIR>(dst, map, 0, y, x / 64, g, bar);
+__device__ __forceinline__ void load_panels(uint32_t dst, const CUtensorMap* map, bool whole, int count, uint32_t panel, int x, int y, int g,
+                                            uint32_t bar) {
+  if (whole) load_4d<PAIR>(dst, map, 0, y, x / 64, g, bar);
   else
-    for (int i = 0; i < count; ++i) load_3d<PAIR>(dst + i * kPanelBytes, map, x + 64 * i, y, g, bar);
+    for (int i = 0; i < count; ++i) load_3d<PAIR>(dst + i * panel, map, x + 64 * i, y, g, bar);
 }
 
 // ---- pairs of CTAs: the even one (rank 0) leads, its barriers say when both CTAs' operands have landed ----------
@@ -269,6 +270,7 @@ struct Walk {
     return (it.rows + 15) & ~15;
   }
   __device__ __forceinline__ int slabs(const Item& it) const {
+    constexpr int kSlab = Cfg<KIND, GATED, BN, PAIR>::kSlab;
     if (KIND == kDweight) return (it.rows + kSlab - 1) / kSlab;
     return KIND == kForward ? (p.k + kSlab - 1) / kSlab : (GATED ? 2 : 1) * ((p.n + kSlab - 1) / kSlab);
   }
@@ -330,19 +332,23 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
         // this CTA's share of the MMA's N dimension
         const int share = walk.wide(it) / C::kCtas;
         const int row = it.row + rank * share, j0 = it.j0 + rank * share;
-        const int panels = KIND == kDweight && maps.b_panels > 1 ? maps.b_panels : (share + 63) / 64;
+        const int panels = KIND == kDweight && maps.b_whole ? 2 : (share + 63) / 64;
         // a CTA's rows come in one copy of the lowest box that has them: a second copy costs more than the rows that it saves
         constexpr int kQuarter = C::kRowBox / 4;
         const int quarters = (share + kQuarter - 1) / kQuarter;
-        const uint32_t tx = kABytes + (KIND == kDweight ? panels * kPanelBytes : (uint32_t)(quarters * kQuarter) * kSlab * 2);
+        const uint32_t part_b = quarters * kQuarter * 128;
         for (int kt = 0; kt < slabs; ++kt) {
           if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, &wait_error, 1u)) {
             alive = false;
             break;
           }
-          const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + kABytes;
+          const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + C::kABytes;
+          const int left = it.rows - kt * C::kSlab;             // dweight: rows of the group from here on
+          const int low = KIND == kDweight && left <= 64;       // they come in the lower box
+          const uint32_t panel = (low ? 64 : C::kSlab) * 128;   // of an operand across its rows
+          const uint32_t tx = KIND == kDweight ? (2 + panels) * panel : C::kABytes + part_b;
           uint32_t full = bar_full + 8 * stage;
-          const bool tail = kTail && it.rows - kt * kSlab < kSlab;
+          const bool tail = kTail && left < C::kSlab;
           if (rank == 0) {
             mbar_expect_tx(full, tail ? tx : C::kCtas * tx);
           } else if (tail) {
@@ -353,23 +359,25 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
             if (kTail) arrive_at_relaxed(full);   // the copies themselves say when they have landed
           }
           if (KIND == kForward) {
-            const int x = kt * kSlab;
-            if (GATED) {
-              load_3d<PAIR>(sa, &maps.a, x, f0, it.g, full);
-              load_3d<PAIR>(sa + kABytes / 2, &maps.a_up, x, f0, it.g, full);
+            const int x = kt * C::kSlab;
+            if (maps.a_whole) {
+              const int y = it.g * maps.a_step + f0;
+              load_2d<PAIR>(sa, &maps.a[0], x, y, full);
+              if (GATED) load_2d<PAIR>(sa + C::kABytes / 2, &maps.a_up[0], x, y, full);
             } else {
-              load_3d<PAIR>(sa, &maps.a, x, f0, it.g, full);
+              load_3d<PAIR>(sa, &maps.a[0], x, f0, it.g, full);
+              if (GATED) load_3d<PAIR>(sa + C::kABytes / 2, &maps.a_up[0], x, f0, it.g, full);
             }
             load_2d<PAIR>(sb, &maps.b[quarters - 1], x, row, full);
           } else if (KIND == kBackward) {
             const bool up = kt >= part;
-            const int x = (up ? kt - part : kt) * kSlab;
-            load_panels<PAIR>(sa, up ? &maps.a_up : &maps.a, maps.a_panels, 2, f0, x, it.g, full);
+            const int x = (up ? kt - part : kt) * C::kSlab;
+            load_panels<PAIR>(sa, up ? &maps.a_up[0] : &maps.a[0], maps.a_whole, 2, panel, f0, x, it.g, full);
             load_2d<PAIR>(sb, up ? &maps.b_up[quarters - 1] : &maps.b[quarters - 1], x, row, full);
           } else {
-            const int y = it.row + kt * kSlab;
-            load_panels<PAIR>(sa, it.half ? &maps.a_up : &maps.a, maps.a_panels, 2, f0, y, 0, full);
-            load_panels<PAIR>(sb, &maps.b[0], maps.b_panels, panels, j0, y, 0, full);
+            const int y = it.row + kt * C::kSlab;
+            load_panels<PAIR>(sa, it.half ? &maps.a_up[low] : &maps.a[low], maps.a_whole, 2, panel, f0, y, 0, full);
+            load_panels<PAIR>(sb, &maps.b[low], maps.b_whole, panels, panel, j0, y, 0, full);
           }
           if (++stage == C::kStages) stage = 0, phase ^= 1u;
         }
@@ -379,6 +387,8 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
   } else if (warp == 1) {
     // The whole warp walks along: in dweight's last slab its lanes clear the rows that belong to the next group (of both operands: zero times a
     // NaN of the next group would not be zero).
+    const uint64_t a_first = KIND == kForward ? smem_desc(smem_base) : smem_desc_across(smem_base, C::kSlab * 128);
+    const uint64_t b_first = KIND == kDweight ? smem_desc_across(smem_base + C::kABytes, C::kSlab * 128) : smem_desc(smem_base + C::kABytes);
     uint32_t stage = 0, phase = 0, acc = 0, tails = 0;   // tails: the phase of every stage's bar_tail
     bool alive = true;
     for (int i = 0; alive && walk.at(i, mine, it); ++i) {
@@ -387,17 +397,19 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
       const int cols = walk.wide(it);
       const int panels = 2 + (cols / C::kCtas + 63) / 64;
       auto clear = [&](uint32_t at_stage, int valid) {
-        const int n16 = (((valid + 15) & ~15) - valid) * 8;
-        for (int i = lane; i < n16 * panels; i += 32)
-          *(uint4*)(smem_al + (size_t)at_stage * C::kStageBytes + (size_t)(i / n16) * kPanelBytes + valid * 128 + (i % n16) * 16) =
-              make_uint4(0u, 0u, 0u, 0u);
+        const int n16 = (((valid + 15) & ~15) - valid) * 8, panel = (valid <= 64 ? 64 : C::kSlab) * 128;
+        for (int i = lane; i < n16 * panels; i += 32) {
+          const int which = i / n16;   // dout's panels, then x's
+          *(uint4*)(smem_al + (size_t)at_stage * C::kStageBytes + (which < 2 ? which * panel : C::kABytes + (which - 2) * panel) + valid * 128 +
+                    (i % n16) * 16) = make_uint4(0u, 0u, 0u, 0u);
+        }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
       };
       if (rank != 0) {   // the follower: only its tails
-        const int valid = it.rows - (slabs - 1) * kSlab;
+        const int valid = it.rows - (slabs - 1) * C::kSlab;
         stage = (stage + slabs - 1) % C::kStages;
-        if (kTail && valid < kSlab) {
+        if (kTail && valid < C::kSlab) {
           if (!mbar_wait(bar_tail + 8 * stage, (tails >> stage) & 1u, abort_flag, &wait_error, 6u)) break;
           tails ^= 1u << stage;
           clear(stage, valid);
@@ -419,19 +431,19 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
           alive = false;
           break;
         }
-        const uint32_t sa = smem_base + stage * C::kStageBytes, sb = sa + kABytes;
-        int steps = kSlab / 16;
-        if (KIND == kDweight && it.rows - kt * kSlab < kSlab) {
-          const int valid = it.rows - kt * kSlab;
-          steps = (valid + 15) / 16;
-          clear(stage, valid);
-        }
+        const int left = KIND == kDweight ? it.rows - kt * C::kSlab : C::kSlab;
+        if (KIND == kDweight && left < C::kSlab) clear(stage, left);
         tc_fence_after();
         if (lane == 0) {
-          for (int k = 0; k < steps; ++k) {
-            const uint64_t ad = KIND == kForward ? smem_desc(sa + k * 32) : smem_desc_across(sa + k * 2048);
-            const uint64_t bd = KIND == kDweight ? smem_desc_across(sb + k * 2048) : smem_desc(sb + k * 32);
-            mma<PAIR>(d, ad, bd, idesc, (kt | k) != 0 ? 1u : 0u);
+          const uint64_t ad = a_first + stage * (C::kStageBytes >> 4), bd = b_first + stage * (C::kStageBytes >> 4);
+          // from one 16 of the reduction to the next: 32 bytes along a swizzled row, 16 rows across
+          constexpr uint32_t kStepA = (KIND == kForward ? 32 : 2048) >> 4, kStepB = (KIND == kDweight ? 2048 : 32) >> 4;
+          if (left >= C::kSlab) {
+#pragma unroll
+            for (int k = 0; k < C::kSlab / 16; ++k) mma<PAIR>(d, ad + k * kStepA, bd + k * kStepB, idesc, (kt | k) != 0 ? 1u : 0u);
+          } else {
+            const uint64_t low = left <= 64 ? (uint64_t)(64 * 128 >> 4) << 16 : 0;   // panels half as far apart
+            for (int k = 0; k < (left + 15) / 16; ++k) mma<PAIR>(d, ad - low + k * kStepA, bd - low + k * kStepB, idesc, (kt | k) != 0 ? 1u : 0u);
           }
           commit<PAIR>(bar_empty + 8 * stage);
         }
@@ -476,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
         }
       } else if constexpr (KIND == kForward && GATED) {
         // quadrants 0 and 1 hold z, 2 and 3 z_up of the same 64 features; of every 16 rows the first 8 are finished by the warp that holds z
-        const int pair = (quad & 1) * 2 + team, up = quad >> 1;
+        const int pair = (quad & 1) * 2 + team, up = (quad >> 1);
         const Forward<__nv_bfloat16, true> e(p.fwd, it.g, it.f0 + (quad & 1) * 32 + 8 * (lane & 3));
         for (int c = 16 * team; c < it.rows; c += 32, ++swaps) {
           float v[16], z[1][8], z_up[1][8];
@@ -554,35 +566,42 @@ bool encode(CUtensorMap* m, const void* base, int rank, const cuuint64_t* dims, 
   return fn && fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// [rows, cols], boxes of 64 columns and 1/4 .. 4/4 of `most` rows
-bool map_boxes(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t ld, int most) {
+// [rows, cols] read along its rows: boxes of 64 columns and 1/4 .. 4/4 of `most` rows
+bool map_rows(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
-  for (int i = 0; i < 4; ++i) {
-    const cuuint32_t box[2] = {kSlab, (cuuint32_t)(most / 4 * (i + 1))};
-    if (!encode(m + i, base, 2, dims, strides, box)) return false;
-  }
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+  return encode(m, base, 2, dims, strides, box);
+}
+bool map_boxes(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t ld, int most) {
+  for (int i = 0; i < 4; ++i)
+    if (!map_rows(m + i, base, rows, cols, ld, most / 4 * (i + 1))) return false;
   return true;
 }
-// [groups, n, k], a box of 64 columns: what lies outside a matrix is filled with zeros, not with the next matrix
-bool map_weights(CUtensorMap* m, const void* base, const Problem& p, int box_rows) {
+cuuint64_t matrix_step(int64_t matrices, int64_t rows, int64_t ld, int64_t step) {   // one matrix: any multiple of 16 bytes
+  return (cuuint64_t)(matrices > 1 ? step : (rows * ld + 7) & ~7ll) * 2;
+}
+// [groups, n, k] read along its rows.  Rows behind a matrix's last may come from the next one: they are features that nobody stores.
+bool map_weights(CUtensorMap* m, const void* base, const Problem& p, int box_rows, int* whole, int* step) {
+  const int64_t apart = p.groups.G > 1 ? p.step_w / p.ld_w : p.n, rows = (p.groups.G - 1) * apart + p.n;
+  *whole = (p.groups.G == 1 || p.step_w % p.ld_w == 0) && rows <= 0x7fffffffll;
+  *step = (int)apart;
+  if (*whole) return map_rows(m, base, rows, p.k, p.ld_w, box_rows);
   const cuuint64_t dims[3] = {(cuuint64_t)p.k, (cuuint64_t)p.n, (cuuint64_t)p.groups.G};
-  const cuuint64_t strides[2] = {(cuuint64_t)p.ld_w * 2, (cuuint64_t)(p.groups.G > 1 ? p.step_w : (p.n * p.ld_w + 7) & ~7ll) * 2};
-  const cuuint32_t box[3] = {kSlab, (cuuint32_t)box_rows, 1};
+  const cuuint64_t strides[2] = {(cuuint64_t)p.ld_w * 2, matrix_step(p.groups.G, p.n, p.ld_w, p.step_w)};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
   return encode(m, base, 3, dims, strides, box);
 }
-// [matrices, rows, cols] read across their rows, 64 rows at a time: two panels of 64 columns per copy where the columns are a multiple of 64 (a panel
-// that reached behind the last column would read what lies there), else one.
-bool map_panels(CUtensorMap* m, int* panels, const void* base, int64_t matrices, int64_t rows, int64_t cols, int64_t ld, int64_t step) {
-  const cuuint64_t sg = (cuuint64_t)(matrices > 1 ? step : (rows * ld + 7) & ~7ll) * 2;
-  if (cols % 64 == 0) {
+bool whole(int64_t cols) { return cols % 64 == 0; }
+// [matrices, rows, cols] read across its rows, `box_rows` at a time
+bool map_panels(CUtensorMap* m, const void* base, int64_t matrices, int64_t rows, int64_t cols, int64_t ld, int64_t step, int box_rows) {
+  const cuuint64_t sg = matrix_step(matrices, rows, ld, step);
+  if (whole(cols)) {
     const cuuint64_t dims[4] = {64, (cuuint64_t)rows, (cuuint64_t)(cols / 64), (cuuint64_t)matrices}, strides[3] = {(cuuint64_t)ld * 2, 128, sg};
-    const cuuint32_t box[4] = {64, kSlab, 2, 1};
-    *panels = 2;
+    const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 2, 1};
     return encode(m, base, 4, dims, strides, box);
   }
   const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)matrices}, strides[2] = {(cuuint64_t)ld * 2, sg};
-  const cuuint32_t box[3] = {64, kSlab, 1};
-  *panels = 1;
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
   return encode(m, base, 3, dims, strides, box);
 }
 
@@ -600,18 +619,23 @@ cudaError_t launch(const Problem& p, cudaStream_t st) {
   const int64_t FT = (features + C::kFeatures - 1) / C::kFeatures;
   int64_t most = (rows / BN + p.groups.G) * FT;
   const __nv_bfloat16* y = (const __nv_bfloat16*)p.y;
-  m.a_panels = m.b_panels = 1;
+  m.a_whole = m.b_whole = m.a_step = 0;
   if (KIND == kDweight) {
     static_assert(KIND != kDweight || BN / C::kCtas == 128, "two panels of x's columns per CTA");
-    ok = map_panels(&m.a, &m.a_panels, y, 1, rows, p.n, p.ld_y, 0) && map_panels(&m.b[0], &m.b_panels, p.x, 1, rows, p.k, p.ld_x, 0) &&
-         (!GATED || map_panels(&m.a_up, &m.a_panels, y + p.n, 1, rows, p.n, p.ld_y, 0));
+    m.a_whole = whole(p.n), m.b_whole = whole(p.k);
+    ok = true;
+    for (int i = 0; i < 2; ++i)
+      ok = ok && map_panels(&m.a[i], y, 1, rows, p.n, p.ld_y, 0, 128 >> i) && map_panels(&m.b[i], p.x, 1, rows, p.k, p.ld_x, 0, 128 >> i) &&
+           (!GATED || map_panels(&m.a_up[i], y + p.n, 1, rows, p.n, p.ld_y, 0, 128 >> i));
     most = (int64_t)p.groups.G * (GATED ? 2 : 1) * FT * ((p.k + BN - 1) / BN);
   } else if (KIND == kForward) {
     const int box = GATED ? kTileM / 2 : kTileM;
-    ok = map_weights(&m.a, p.w, p, box) && (!GATED || map_weights(&m.a_up, p.w_up, p, box)) && map_boxes(m.b, p.x, rows, p.k, p.ld_x, C::kRowBox);
+    ok = map_weights(&m.a[0], p.w, p, box, &m.a_whole, &m.a_step) && (!GATED || map_weights(&m.a_up[0], p.w_up, p, box, &m.a_whole, &m.a_step)) &&
+         map_boxes(m.b, p.x, rows, p.k, p.ld_x, C::kRowBox);
   } else {
-    ok = map_panels(&m.a, &m.a_panels, p.w, p.groups.G, p.n, p.k, p.ld_w, p.step_w) &&
-         (!GATED || map_panels(&m.a_up, &m.a_panels, p.w_up, p.groups.G, p.n, p.k, p.ld_w, p.step_w));
+    m.a_whole = whole(p.k);
+    ok = map_panels(&m.a[0], p.w, p.groups.G, p.n, p.k, p.ld_w, p.step_w, C::kSlab) &&
+         (!GATED || map_panels(&m.a_up[0], p.w_up, p.groups.G, p.n, p.k, p.ld_w, p.step_w, C::kSlab));
     ok = ok && map_boxes(m.b, y, rows, p.n, p.ld_y, C::kRowBox) && (!GATED || map_boxes(m.b_up, y + p.n, rows, p.n, p.ld_y, C::kRowBox));
   }
   if (!ok || most > 0x7fffffffll) return cudaErrorInvalidValue;
