@@ -30,7 +30,7 @@ __device__ uint32_t wait_error;   // set when a bounded wait gives up; read and 
 constexpr int kTileM = 128;    // MMA rows
 constexpr int kEpilogueWarps = 8;
 constexpr int kSwapStride = 36;   // floats of a row: reading eight columns per lane, four lanes a row, then meets every bank once
-constexpr int kThreads = 64 + 32 * kEpilogueWarps;
+constexpr int kClearWarp = 2 + kEpilogueWarps;   // dweight only
 constexpr int kBlockOfTiles = 16;   // row tiles of a group that are walked together, so that their rows stay in L2 for the next features
 
 template <int KIND, bool GATED, int BN, bool PAIR>
@@ -49,6 +49,7 @@ struct Cfg {
   static constexpr uint32_t kFixed = 1024 + 512 + kSwapBytes + kCountBytes;
   static constexpr int kFit = (232448 - kFixed) / kStageBytes;
   static constexpr int kStages = kFit < 10 ? kFit : 10;
+  static constexpr int kThreads = 32 * (2 + kEpilogueWarps + (KIND == kDweight ? 1 : 0));
   static constexpr size_t kSmemBytes = kFixed + (size_t)kStages * kStageBytes;
   static constexpr int kRowBox = BN / kCtas;   // most rows per TMA copy
 };
@@ -112,7 +113,7 @@ __device__ __forceinline__ uint32_t leaders(uint32_t addr) {   // the same place
 __device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-// Without ordering what this thread did before: a release at cluster scope costs hundreds of cycles.
+// Without ordering what this thread did before: a release at cluster scope waits for all of its stores.
 __device__ __forceinline__ void arrive_at_relaxed(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
@@ -280,7 +281,7 @@ struct Walk {
 // rows (dweight: of x's columns) in shared memory, and the leader's MMAs read both halves.  A pair takes in a third less than two single CTAs for
 // the same products.
 template <int KIND, bool GATED, int BN, bool PAIR>
-__global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Problem p) {
+__global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linear_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Problem p) {
   using C = Cfg<KIND, GATED, BN, PAIR>;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -295,12 +296,12 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
   volatile uint32_t* abort_flag = tmem_slot + 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = PAIR ? (int)cluster_rank() : 0;
-  // in a pair, the follower's last slab of a group is complete when its own warp has cleared the rows of the next group (dweight)
-  constexpr bool kTail = PAIR && KIND == kDweight;
+  // dweight: a group's last slab is complete when a warp of its own has cleared the rows of the next group in it, in each CTA
+  constexpr bool kTail = KIND == kDweight;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
-      mbar_init(bar_full + 8 * s, kTail ? 2 : 1);
+      mbar_init(bar_full + 8 * s, kTail ? C::kCtas : 1);
       mbar_init(bar_empty + 8 * s, 1);
       mbar_init(bar_tail + 8 * s, 1);
     }
@@ -349,11 +350,11 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
           const uint32_t tx = KIND == kDweight ? (2 + panels) * panel : C::kABytes + part_b;
           uint32_t full = bar_full + 8 * stage;
           const bool tail = kTail && left < C::kSlab;
-          if (rank == 0) {
-            mbar_expect_tx(full, tail ? tx : C::kCtas * tx);
-          } else if (tail) {
-            full = bar_tail + 8 * stage;   // waited for by this CTA's warp 1, which then arrives at the leader's barrier
+          if (tail) {
+            full = bar_tail + 8 * stage;   // waited for by this CTA's clearing warp, which then arrives at the leader's barrier
             mbar_expect_tx(full, tx);
+          } else if (rank == 0) {
+            mbar_expect_tx(full, C::kCtas * tx);
           } else {
             full = leaders(full);
             if (kTail) arrive_at_relaxed(full);   // the copies themselves say when they have landed
@@ -385,39 +386,14 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
       alive = __shfl_sync(0xffffffffu, alive, 0);
     }
   } else if (warp == 1) {
-    // The whole warp walks along: in dweight's last slab its lanes clear the rows that belong to the next group (of both operands: zero times a
-    // NaN of the next group would not be zero).
     const uint64_t a_first = KIND == kForward ? smem_desc(smem_base) : smem_desc_across(smem_base, C::kSlab * 128);
     const uint64_t b_first = KIND == kDweight ? smem_desc_across(smem_base + C::kABytes, C::kSlab * 128) : smem_desc(smem_base + C::kABytes);
-    uint32_t stage = 0, phase = 0, acc = 0, tails = 0;   // tails: the phase of every stage's bar_tail
-    bool alive = true;
+    uint32_t stage = 0, phase = 0, acc = 0;
+    bool alive = rank == 0;   // the leader's MMAs are the pair's
     for (int i = 0; alive && walk.at(i, mine, it); ++i) {
       const int slabs = walk.slabs(it);
       if (slabs == 0) continue;
       const int cols = walk.wide(it);
-      const int panels = 2 + (cols / C::kCtas + 63) / 64;
-      auto clear = [&](uint32_t at_stage, int valid) {
-        const int n16 = (((valid + 15) & ~15) - valid) * 8, panel = (valid <= 64 ? 64 : C::kSlab) * 128;
-        for (int i = lane; i < n16 * panels; i += 32) {
-          const int which = i / n16;   // dout's panels, then x's
-          *(uint4*)(smem_al + (size_t)at_stage * C::kStageBytes + (which < 2 ? which * panel : C::kABytes + (which - 2) * panel) + valid * 128 +
-                    (i % n16) * 16) = make_uint4(0u, 0u, 0u, 0u);
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-      };
-      if (rank != 0) {   // the follower: only its tails
-        const int valid = it.rows - (slabs - 1) * C::kSlab;
-        stage = (stage + slabs - 1) % C::kStages;
-        if (kTail && valid < C::kSlab) {
-          if (!mbar_wait(bar_tail + 8 * stage, (tails >> stage) & 1u, abort_flag, &wait_error, 6u)) break;
-          tails ^= 1u << stage;
-          clear(stage, valid);
-          if (lane == 0) arrive_at(leaders(bar_full + 8 * stage));
-        }
-        stage = (stage + 1) % C::kStages;
-        continue;
-      }
       // fp32 sums of bf16, M = 128 (256 in a pair), N; a set bit 15 / 16: A / B lies across its rows
       const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)cols >> 3 << 17) | ((uint32_t)(kTileM * C::kCtas) >> 4 << 24) |
                              (KIND != kForward ? 1u << 15 : 0u) | (KIND == kDweight ? 1u << 16 : 0u);
@@ -432,7 +408,6 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
           break;
         }
         const int left = KIND == kDweight ? it.rows - kt * C::kSlab : C::kSlab;
-        if (KIND == kDweight && left < C::kSlab) clear(stage, left);
         tc_fence_after();
         if (lane == 0) {
           const uint64_t ad = a_first + stage * (C::kStageBytes >> 4), bd = b_first + stage * (C::kStageBytes >> 4);
@@ -452,6 +427,33 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
       }
       if (alive && lane == 0) commit<PAIR>(bar_tfull + 8 * buf);
       __syncwarp();
+    }
+  } else if (kTail && warp == kClearWarp) {
+    // Clears, in a group's last slab, the rows of the next group up to the next multiple of 16 (the MMAs go no further), of both operands: zero times
+    // a NaN of the next group would not be zero.  In the MMAs' own warp this cost the 8 slabs of a group of 500 rows 20 us of 300.
+    uint32_t stage = 0, tails = 0;   // tails: the phase of every stage's bar_tail
+    for (int i = 0; walk.at(i, mine, it); ++i) {
+      const int slabs = walk.slabs(it), valid = it.rows - (slabs - 1) * C::kSlab;
+      if (slabs == 0) continue;
+      stage = (stage + slabs - 1) % C::kStages;
+      if (valid < C::kSlab) {
+        if (!mbar_wait(bar_tail + 8 * stage, (tails >> stage) & 1u, abort_flag, &wait_error, 6u)) break;
+        tails ^= 1u << stage;
+        const int panels = 2 + (walk.wide(it) / C::kCtas + 63) / 64;
+        const int n16 = (((valid + 15) & ~15) - valid) * 8, panel = (valid <= 64 ? 64 : C::kSlab) * 128;
+        for (int u = lane; u < n16 * panels; u += 32) {
+          const int which = u / n16;   // dout's panels, then x's
+          *(uint4*)(smem_al + (size_t)stage * C::kStageBytes + (which < 2 ? which * panel : C::kABytes + (which - 2) * panel) + valid * 128 +
+                    (u % n16) * 16) = make_uint4(0u, 0u, 0u, 0u);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          if (PAIR) arrive_at(leaders(bar_full + 8 * stage));
+          else mbar_arrive(bar_full + 8 * stage);
+        }
+      }
+      stage = (stage + 1) % C::kStages;
     }
   } else {
     const int quad = warp & 3, team = (warp - 2) >> 2;   // TMEM lanes this warp may read; which half of the chunks it takes
@@ -539,7 +541,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tc_kernel(const __grid_con
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          if (PAIR) arrive_at(leaders(bar_tempty + 8 * buf));
+          if (PAIR) arrive_at_relaxed(leaders(bar_tempty + 8 * buf));   // the sums are in registers; the stores need not have landed
           else mbar_arrive(bar_tempty + 8 * buf);
         }
       }
@@ -643,7 +645,7 @@ cudaError_t launch(const Problem& p, cudaStream_t st) {
   attr.id = cudaLaunchAttributeClusterDimension;
   attr.val.clusterDim.x = C::kCtas, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = sms, cfg.blockDim = kThreads, cfg.dynamicSmemBytes = C::kSmemBytes, cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
+  cfg.gridDim = sms, cfg.blockDim = C::kThreads, cfg.dynamicSmemBytes = C::kSmemBytes, cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
   int64_t units = sms;
   if (PAIR) {
     if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
