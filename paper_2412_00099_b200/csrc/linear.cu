@@ -440,7 +440,7 @@ extern "C" int mcce_expert_linear_dweight(const mcce_linear* p, const void* dout
   const int64_t G = q.groups.G;
   q.y = dout, q.x = x, q.ld_y = ld_or(p->ld_y, width), q.ld_x = ld_or(p->ld_x, p->k);
   q.dw = dw, q.dw_up = dw_up, q.add_dw = add_dw, q.add_dw_up = add_dw_up, q.dw_f32 = p->out_dtype == MCCE_F32;
-  q.dw_wide = aligned(dw, 32) && aligned(dw_up, 32) && aligned(add_dw, 32) && aligned(add_dw_up, 32) && q.ld_w * eo % 32 == 0 && q.step_w * eo % 32 == 0;
+  q.dw_wide = aligned(dw, 4 * eo) && aligned(dw_up, 4 * eo) && aligned(add_dw, 4 * eo) && aligned(add_dw_up, 4 * eo) && q.ld_w % 4 == 0 && q.step_w % 4 == 0;
   const Span sy = row_span(dout, rows, q.ld_y, width, e), sx = row_span(x, rows, q.ld_x, p->k, ex);
   const Span ssc = flat_span(scales, rows, blocks_of(p->k)), soff = flat_span(offsets, (int64_t)p->n_layers * (p->n_experts + 1), 4);
   const Span saw = weight_span(*p, add_dw, eo), sawu = weight_span(*p, add_dw_up, eo), sab = flat_span(add_db, G * p->n, eo);

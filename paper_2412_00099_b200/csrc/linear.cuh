@@ -386,7 +386,7 @@ struct Problem {
   const void *x, *y, *w, *w_up;    // forward: x, w; backward: y, w; dweight: y, x
   void *dw, *dw_up;                // dweight
   const void *add_dw, *add_dw_up;
-  int32_t dw_f32, dw_wide;   // dw_wide: its rows (and those added) start at multiples of 32 bytes
+  int32_t dw_f32, dw_wide;   // dw_wide: four columns of its rows (and of those added) are aligned as a whole
   ForwardArgs fwd;
   BackwardArgs bwd;
 };

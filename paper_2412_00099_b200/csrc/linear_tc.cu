@@ -44,7 +44,8 @@ struct Cfg {
   static constexpr uint32_t kBBytes = BN / kCtas * kSlab * 2;
   static constexpr uint32_t kStageBytes = kABytes + kBBytes;
   // sums of 16 rows x 32 features per epilogue warp, on their way from a feature per lane to a row per four lanes; gated: two buffers
-  static constexpr uint32_t kSwapBytes = KIND == kDweight ? 0 : kEpilogueWarps * 16 * kSwapStride * 4 * (KIND == kForward && GATED ? 2 : 1);
+  // (dweight: 32 x 32)
+  static constexpr uint32_t kSwapBytes = KIND == kDweight ? kEpilogueWarps * 4096 : kEpilogueWarps * 16 * kSwapStride * 4 * (KIND == kForward && GATED ? 2 : 1);
   static constexpr uint32_t kCountBytes = KIND == kDweight ? 0 : ((MCCE_LINEAR_MAX_GROUPS + 1 + 33) * 4 + 127) & ~127;
   static constexpr uint32_t kFixed = 1024 + 512 + kSwapBytes + kCountBytes;
   static constexpr int kFit = (232448 - kFixed) / kStageBytes;
@@ -65,6 +66,22 @@ struct Maps {
 __device__ __forceinline__ uint64_t smem_desc_across(uint32_t addr, uint32_t panel) {
   return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(panel >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
+// 32 consecutive fp32 columns of this thread's TMEM lane
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,"
+      "%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+        "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
 // TMA copies into this CTA's shared memory; in a pair the barrier may be the other CTA's.
 #define MCCE_TMA_LOAD(DIMS, COORDS, ...)                                                                                              \
   if (PAIR)                                                                                                                           \
@@ -154,47 +171,49 @@ __device__ __forceinline__ void free_tmem(uint32_t addr, uint32_t cols) {
   else tmem_dealloc(addr, cols);
 }
 
-// 16 neighbouring sums of a row, added to what is there, 32 bytes at a time (whole sectors) where rows are aligned to it.
-__device__ __forceinline__ void load_32(const void* p, uint32_t (&v)[8]) {
-  asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
-               : "l"(p));
-}
-__device__ __forceinline__ void store_32(void* p, const uint32_t (&v)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]),
-               "r"(v[6]), "r"(v[7])
-               : "memory");
-}
+// 32 rows x 32 columns of sums, a row per lane, brought to memory (added to what is there) with four columns per lane, a row per eight lanes: whole
+// sectors of 64 (bf16) or 128 neighbouring bytes, where a row per lane wrote 32 rows with every instruction.  They turn in shared memory, 16 bytes
+// at a time, a row's units rotated by its number so that neither side meets a bank twice.
 template <typename O>
-__device__ __forceinline__ void store_16(O* o, const O* add, float (&v)[16], int left, bool wide) {
-  if (!wide || left < 16) {
+__device__ __forceinline__ void store_block(uint8_t* buffer, const float (&v)[32], O* o, const O* add, int64_t ld, int rows, int cols, bool wide) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
-      if (j < left) store_as(o + j, v[j] + (add ? load_as_float(add + j) : 0.f));
+  for (int i = 0; i < 8; ++i)
+    *(float4*)(buffer + lane * 128 + ((i ^ (lane & 7)) << 4)) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+  __syncwarp();
+  const int unit = lane & 7, count = min(4, cols - 4 * unit), r0 = lane >> 3;
+  if (count <= 0) return;
+  if (!wide || count < 4) {
+    for (int r = r0; r < min(32, rows); r += 4)
+      for (int j = 0; j < count; ++j)
+        store_as(o + r * ld + 4 * unit + j, ((const float*)(buffer + r * 128 + ((unit ^ (r & 7)) << 4)))[j] +
+                                                (add ? load_as_float(add + r * ld + 4 * unit + j) : 0.f));
     return;
   }
-  constexpr int kParts = sizeof(O) / 2;
-  uint32_t q[kParts][8];
-  if (add) {
+  float4 x[8];
+  typedef typename std::conditional<sizeof(O) == 4, float4, uint2>::type Four;
+  Four a[8];
 #pragma unroll
-    for (int i = 0; i < kParts; ++i) load_32((const uint8_t*)add + 32 * i, q[i]);
-#pragma unroll
-    for (int j = 0; j < 16; ++j)
-      v[j] += sizeof(O) == 4 ? __uint_as_float(q[j / 8 * (kParts - 1)][j % 8])
-                             : __uint_as_float(j & 1 ? q[0][j / 2] & 0xffff0000u : q[0][j / 2] << 16);
+  for (int i = 0; i < 8; ++i) {
+    a[i] = Four{};
+    if (add) a[i] = *(const Four*)(add + min(r0 + 4 * i, rows - 1) * ld + 4 * unit);
   }
-  if (sizeof(O) == 4) {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) q[j / 8 * (kParts - 1)][j % 8] = __float_as_uint(v[j]);
-  } else {
+  for (int i = 0; i < 8; ++i) x[i] = *(const float4*)(buffer + (r0 + 4 * i) * 128 + ((unit ^ ((r0 + 4 * i) & 7)) << 4));
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
-      q[0][j] = *(const uint32_t*)&h;
+  for (int i = 0; i < 8; ++i) {
+    O* to = o + (r0 + 4 * i) * ld + 4 * unit;
+    Four v;
+    if constexpr (sizeof(O) == 4) {
+      v = make_float4(x[i].x + a[i].x, x[i].y + a[i].y, x[i].z + a[i].z, x[i].w + a[i].w);
+    } else {
+      const __nv_bfloat162 lo = __floats2bfloat162_rn(x[i].x + __uint_as_float(a[i].x << 16), x[i].y + __uint_as_float(a[i].x & 0xffff0000u));
+      const __nv_bfloat162 hi = __floats2bfloat162_rn(x[i].z + __uint_as_float(a[i].y << 16), x[i].w + __uint_as_float(a[i].y & 0xffff0000u));
+      v = make_uint2(*(const uint32_t*)&lo, *(const uint32_t*)&hi);
     }
+    if (r0 + 4 * i < rows) *(Four*)to = v;
   }
-#pragma unroll
-  for (int i = 0; i < kParts; ++i) store_32((uint8_t*)o + 32 * i, q[i]);
 }
 
 // This lane's eight columns of its row among eight
@@ -439,13 +458,10 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
       if (valid < C::kSlab) {
         if (!mbar_wait(bar_tail + 8 * stage, (tails >> stage) & 1u, abort_flag, &wait_error, 6u)) break;
         tails ^= 1u << stage;
-        const int panels = 2 + (walk.wide(it) / C::kCtas + 63) / 64;
-        const int n16 = (((valid + 15) & ~15) - valid) * 8, panel = (valid <= 64 ? 64 : C::kSlab) * 128;
-        for (int u = lane; u < n16 * panels; u += 32) {
-          const int which = u / n16;   // dout's panels, then x's
-          *(uint4*)(smem_al + (size_t)stage * C::kStageBytes + (which < 2 ? which * panel : C::kABytes + (which - 2) * panel) + valid * 128 +
-                    (u % n16) * 16) = make_uint4(0u, 0u, 0u, 0u);
-        }
+        // a row's 128 bytes in two panels of dout and two of x at a time
+        const int panel = (valid <= 64 ? 64 : C::kSlab) * 128;
+        uint8_t* at = smem_al + (size_t)stage * C::kStageBytes + (lane >> 4) * C::kABytes + (lane >> 3 & 1) * panel + (lane & 7) * 16;
+        for (int r = valid; r & 15; ++r) *(uint4*)(at + r * 128) = make_uint4(0u, 0u, 0u, 0u);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) {
@@ -471,22 +487,23 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
       }
       const uint32_t t0 = tmem_base + lane_addr + buf * BN;
       if constexpr (KIND == kDweight) {
-        const int cols = min(BN, p.k - it.j0), i = it.f0 + quad * 32 + lane;
+        const int cols = min(BN, p.k - it.j0), first_row = it.f0 + quad * 32;
         const void* add = it.half ? p.add_dw_up : p.add_dw;
         void* dw = it.half ? p.dw_up : p.dw;
-        const int64_t at = it.g * p.step_w + (int64_t)i * p.ld_w + it.j0;
-        const bool on = i < p.n;
-        for (int c = 16 * team; c < cols; c += 32) {
-          float v[16] = {};
+        const int64_t at = it.g * p.step_w + (int64_t)first_row * p.ld_w + it.j0;
+        for (int c = 32 * team; c < cols && first_row < p.n; c += 64) {
+          float v[32] = {};
           __syncwarp();   // the loads from TMEM take the whole warp
           if (sums) {
-            tmem_ld16(t0 + c, v);
+            tmem_ld32(t0 + c, v);
             tmem_ld_wait();
           }
-          if (!on) continue;
-          const int left = min(16, cols - c);
-          if (p.dw_f32) store_16((float*)dw + at + c, add ? (const float*)add + at + c : nullptr, v, min(16, cols - c), p.dw_wide);
-          else store_16((__nv_bfloat16*)dw + at + c, add ? (const __nv_bfloat16*)add + at + c : nullptr, v, min(16, cols - c), p.dw_wide);
+          uint8_t* buffer = (uint8_t*)swap + (warp - 2) * 4096;
+          if (p.dw_f32)
+            store_block(buffer, v, (float*)dw + at + c, add ? (const float*)add + at + c : nullptr, p.ld_w, p.n - first_row, cols - c, p.dw_wide);
+          else
+            store_block(buffer, v, (__nv_bfloat16*)dw + at + c, add ? (const __nv_bfloat16*)add + at + c : nullptr, p.ld_w, p.n - first_row, cols - c,
+                        p.dw_wide);
         }
       } else if constexpr (KIND == kForward && GATED) {
         // quadrants 0 and 1 hold z, 2 and 3 z_up of the same 64 features; of every 16 rows the first 8 are finished by the warp that holds z
