@@ -9,98 +9,132 @@ namespace linear {
 namespace {
 
 // ---- products of any shape -----------------------------------------------------------------------------------
-// Tiles of 64 x 64 results, 16 products deep, 4 x 4 results per thread, in fp32.  The results go through shared memory so that a warp
-// ends up with 32 neighbouring columns of a row.
+// Tiles of TI x 64 results (TI 64, or 32 where 64 would leave SMs without a tile), 16 products deep, 4 x 4 results per thread, in fp32.  The
+// next step's operands are on their way to registers while this one's are multiplied (without that every step waited for memory: 900 x 1002 x 515 fp32
+// 95 us).  The results go through shared memory so that a warp ends up with 32 neighbouring columns of a row.
 constexpr int kTile = 64, kDeep = 16, kPad = kTile + 4;
 
-template <Kind KIND, typename T, bool GATED>
-__global__ void __launch_bounds__(256) general_kernel(const Problem p) {
+template <Kind KIND, typename T, bool GATED, int TI>
+__global__ void __launch_bounds__(TI * 4) general_kernel(const Problem p) {
   constexpr int kSets = KIND == kForward && GATED ? 2 : 1;   // sums per result: a gated forward pass has two
   extern __shared__ __align__(16) float smem[];
-  float* As = smem;                          // [kDeep][kPad]
-  float* Bs = As + kDeep * kPad;             // [kSets][kDeep][kPad]
-  float* Cs = smem;                          // [kSets][64][kPad], after the products
-  int* before = (int*)(smem + kSets * kTile * kPad);
+  constexpr int kThreads = TI * 4, kBuffer = (1 + kSets) * kDeep * kPad;
+  float* Cs = smem;                          // [kSets][TI][kPad], after the products; before: two buffers of [kDeep][kPad] of either operand
+  constexpr int kFloats = kSets * TI * kPad > 2 * kBuffer ? kSets * TI * kPad : 2 * kBuffer;
+  int* before = (int*)(smem + kFloats);
   int* scratch = before + p.groups.G + 1;
   const int t = threadIdx.x, tx = t % 16, ty = t / 16;
 
   const int cols = KIND == kForward ? p.n : p.k;
   const int JT = (cols + kTile - 1) / kTile;
   int64_t items;
-  const int IT = (p.n + kTile - 1) / kTile;               // kDweight: tiles of dout's columns
+  const int IT = (p.n + TI - 1) / TI;               // kDweight: tiles of dout's columns
   constexpr int kHalves = KIND == kDweight && GATED ? 2 : 1;
   if (KIND == kDweight) {
     items = (int64_t)p.groups.G * kHalves * IT * JT;
   } else {
-    count_tiles(p.groups, kTile, before, scratch);
+    count_tiles(p.groups, TI, before, scratch);
     items = (int64_t)before[p.groups.G] * JT;
   }
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     int g, i0, j0 = (int)(item % JT) * kTile, half = 0;
     if (KIND == kDweight) {
       int64_t r = item / JT;
-      i0 = (int)(r % IT) * kTile, r /= IT;
+      i0 = (int)(r % IT) * TI, r /= IT;
       half = (int)(r % kHalves), g = (int)(r / kHalves);
     } else {
       const int tile = (int)(item / JT);
       g = find_group(before, p.groups.G, tile);
-      i0 = 0;
-      if (tile >= before[g]) i0 = (tile - before[g]) * kTile;
+      i0 = (tile - before[g]) * TI;
     }
     const GroupRows gr = group_rows(p.groups, g);
     const int64_t row0 = gr.first + (KIND == kDweight ? 0 : i0);
-    const int I = KIND == kDweight ? min(kTile, p.n - i0) : (int)min((int64_t)kTile, gr.m - i0);
+    const int I = KIND == kDweight ? min(TI, p.n - i0) : (int)min((int64_t)TI, gr.m - i0);
     const int J = min(kTile, cols - j0);
     const int64_t red = KIND == kForward ? p.k : KIND == kBackward ? p.n : gr.m;
-    constexpr int kParts = KIND == kBackward && GATED ? 2 : 1;
+    constexpr int kHalvesRed = KIND == kBackward && GATED ? 2 : 1;
+    const int64_t steps = (red + kDeep - 1) / kDeep, all = steps * kHalvesRed;
     float c[kSets][4][4] = {};
-    for (int part = 0; part < kParts; ++part)
-      for (int64_t d0 = 0; d0 < red; d0 += kDeep) {
+    // this thread's elements of a step, as fp32
+    constexpr int kA = TI * kDeep / kThreads, kB = kTile * kDeep / kThreads;
+    float ra[kA], rb[kSets][kB];
+    auto fetch = [&](int64_t step) {
+      const int part = step >= steps ? 1 : 0;
+      const int64_t d0 = (step - part * steps) * kDeep;
+      // operand with the reduction along its rows: 16 neighbours of a row; across them: neighbours of a row of the operand
+      if (KIND == kDweight) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          // operand with the reduction along its rows: 16 neighbours of a row; across them: 64 neighbours
-          const int ka = t % kDeep, ma = t / kDeep + 16 * i, kb = t / kTile + 4 * i, mb = t % kTile;
-          if (KIND == kDweight) {
-            const bool in = d0 + kb < red;
-            const int64_t r = gr.first + d0 + kb;
-            As[kb * kPad + mb] = in && mb < I ? load_as_float((const T*)p.y + r * p.ld_y + half * p.n + i0 + mb) : 0.f;
-            Bs[kb * kPad + mb] = in && mb < J ? load_as_float((const T*)p.x + r * p.ld_x + j0 + mb) : 0.f;
-          } else if (KIND == kForward) {
-            const bool in = d0 + ka < red;
-            As[ka * kPad + ma] = in && ma < I ? load_as_float((const T*)p.x + (row0 + ma) * p.ld_x + d0 + ka) : 0.f;
-            const int64_t at = g * p.step_w + (int64_t)(j0 + ma) * p.ld_w + d0 + ka;
-            Bs[ka * kPad + ma] = in && ma < J ? load_as_float((const T*)p.w + at) : 0.f;
-            if (kSets == 2) Bs[(kDeep + ka) * kPad + ma] = in && ma < J ? load_as_float((const T*)p.w_up + at) : 0.f;
-          } else {
-            As[ka * kPad + ma] =
-                d0 + ka < red && ma < I ? load_as_float((const T*)p.y + (row0 + ma) * p.ld_y + (int64_t)part * p.n + d0 + ka) : 0.f;
-            Bs[kb * kPad + mb] = d0 + kb < red && mb < J ? load_as_float((const T*)(part ? p.w_up : p.w) + g * p.step_w + (d0 + kb) * p.ld_w + j0 + mb)
-                                                         : 0.f;
-          }
+        for (int i = 0; i < kA; ++i) {
+          const int d = t / TI + kThreads / TI * i, m = t % TI;
+          ra[i] = d0 + d < red && m < I ? load_as_float((const T*)p.y + (gr.first + d0 + d) * p.ld_y + half * p.n + i0 + m) : 0.f;
         }
-        __syncthreads();
+      } else {
 #pragma unroll
-        for (int d = 0; d < kDeep; ++d) {
-          const float4 a = *(const float4*)(As + d * kPad + 4 * ty);
-          const float av[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-          for (int s = 0; s < kSets; ++s) {
-            const float4 b = *(const float4*)(Bs + (s * kDeep + d) * kPad + 4 * tx);
-            const float bv[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int j = 0; j < 4; ++j) c[s][i][j] = fmaf(av[i], bv[j], c[s][i][j]);
-          }
+        for (int i = 0; i < kA; ++i) {
+          const int d = t % kDeep, m = t / kDeep + kThreads / kDeep * i;
+          const T* a = KIND == kForward ? (const T*)p.x + (row0 + m) * p.ld_x : (const T*)p.y + (row0 + m) * p.ld_y + (int64_t)part * p.n;
+          ra[i] = d0 + d < red && m < I ? load_as_float(a + d0 + d) : 0.f;
         }
-        __syncthreads();
       }
+#pragma unroll
+      for (int i = 0; i < kB; ++i) {
+        if (KIND == kForward) {
+          const int d = t % kDeep, m = t / kDeep + kThreads / kDeep * i;
+          const bool in = d0 + d < red && m < J;
+          const int64_t at = g * p.step_w + (int64_t)(j0 + m) * p.ld_w + d0 + d;
+          rb[0][i] = in ? load_as_float((const T*)p.w + at) : 0.f;
+          if (kSets == 2) rb[kSets - 1][i] = in ? load_as_float((const T*)p.w_up + at) : 0.f;
+        } else {
+          const int d = t / kTile + kThreads / kTile * i, m = t % kTile;
+          const bool in = d0 + d < red && m < J;
+          if (KIND == kDweight) rb[0][i] = in ? load_as_float((const T*)p.x + (gr.first + d0 + d) * p.ld_x + j0 + m) : 0.f;
+          else rb[0][i] = in ? load_as_float((const T*)(part ? p.w_up : p.w) + g * p.step_w + (d0 + d) * p.ld_w + j0 + m) : 0.f;
+        }
+      }
+    };
+    auto put = [&](float* buffer) {
+#pragma unroll
+      for (int i = 0; i < kA; ++i) {
+        if (KIND == kDweight) buffer[(t / TI + kThreads / TI * i) * kPad + t % TI] = ra[i];
+        else buffer[(t % kDeep) * kPad + t / kDeep + kThreads / kDeep * i] = ra[i];
+      }
+#pragma unroll
+      for (int s = 0; s < kSets; ++s)
+#pragma unroll
+        for (int i = 0; i < kB; ++i) {
+          float* b = buffer + (1 + s) * kDeep * kPad;
+          if (KIND == kForward) b[(t % kDeep) * kPad + t / kDeep + kThreads / kDeep * i] = rb[s][i];
+          else b[(t / kTile + kThreads / kTile * i) * kPad + t % kTile] = rb[s][i];
+        }
+    };
+    if (all) fetch(0), put(smem);
+    __syncthreads();
+    for (int64_t step = 0; step < all; ++step) {
+      const float* buffer = smem + (step & 1) * kBuffer;
+      if (step + 1 < all) fetch(step + 1);
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d) {
+        const float4 a = *(const float4*)(buffer + d * kPad + 4 * ty);
+        const float av[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int s = 0; s < kSets; ++s) {
+          const float4 b = *(const float4*)(buffer + ((1 + s) * kDeep + d) * kPad + 4 * tx);
+          const float bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) c[s][i][j] = fmaf(av[i], bv[j], c[s][i][j]);
+        }
+      }
+      if (step + 1 < all) put(smem + ((step + 1) & 1) * kBuffer);
+      __syncthreads();
+    }
 #pragma unroll
     for (int s = 0; s < kSets; ++s)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) Cs[(s * kTile + 4 * ty + i) * kPad + 4 * tx + j] = c[s][i][j];
+        for (int j = 0; j < 4; ++j) Cs[(s * TI + 4 * ty + i) * kPad + 4 * tx + j] = c[s][i][j];
     __syncthreads();
     const int warp = t / 32, lane = t % 32;
     for (int jj = 0; jj < J; jj += 32) {
@@ -108,7 +142,7 @@ __global__ void __launch_bounds__(256) general_kernel(const Problem p) {
         const void* add = half ? p.add_dw_up : p.add_dw;
         void* dw = half ? p.dw_up : p.dw;
         const int j = jj + lane;
-        for (int i = warp; i < I; i += 8) {
+        for (int i = warp; i < I; i += kThreads / 32) {
           if (j >= J) continue;
           const int64_t at = g * p.step_w + (int64_t)(i0 + i) * p.ld_w + j0 + j;
           float v = Cs[i * kPad + j];
@@ -126,7 +160,7 @@ __global__ void __launch_bounds__(256) general_kernel(const Problem p) {
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
           z[0][u] = Cs[i * kPad + j + u];
-          if (kSets == 2) up[0][u] = Cs[(kTile + i) * kPad + j + u];
+          if (kSets == 2) up[0][u] = Cs[(TI + i) * kPad + j + u];
         }
         if constexpr (KIND == kForward) {
           const Forward<T, GATED> e(p.fwd, g, j0 + j);
@@ -143,93 +177,188 @@ __global__ void __launch_bounds__(256) general_kernel(const Problem p) {
   }
 }
 
-template <Kind KIND, typename T, bool GATED>
-cudaError_t launch_general(const Problem& p, cudaStream_t st) {
+template <Kind KIND, typename T, bool GATED, int TI>
+cudaError_t launch_tiles(const Problem& p, int64_t tiles, int sms, cudaStream_t st) {
   static int cache[64] = {0};
   constexpr int kSets = KIND == kForward && GATED ? 2 : 1;
-  const size_t fixed = (size_t)kSets * kTile * kPad * 4;
-  int sms = 0;
+  constexpr size_t kFloats = kSets * TI * kPad > 2 * (1 + kSets) * kDeep * kPad ? kSets * TI * kPad : 2 * (1 + kSets) * kDeep * kPad;
   const cudaError_t e =
-      tc::sm_count_and_smem_optin(general_kernel<KIND, T, GATED>, fixed + (MCCE_LINEAR_MAX_GROUPS + 1 + 33) * 4, cache, &sms);
+      tc::sm_count_and_smem_optin(general_kernel<KIND, T, GATED, TI>, kFloats * 4 + (MCCE_LINEAR_MAX_GROUPS + 1 + 33) * 4, cache, &sms);
   if (e != cudaSuccess) return e;
-  const int64_t jt = ((KIND == kForward ? p.n : p.k) + kTile - 1) / kTile;
-  const int64_t most = KIND == kDweight ? (int64_t)p.groups.G * 2 * ((p.n + kTile - 1) / kTile) * jt
-                                        : ((p.L * p.groups.R) / kTile + p.groups.G) * jt;
-  const int64_t grid = most < 4 * sms ? most : 4 * sms;
-  general_kernel<KIND, T, GATED><<<(unsigned)grid, 256, fixed + (size_t)(p.groups.G + 1 + 33) * 4, st>>>(p);
+  const int64_t most = (TI == 64 ? 6 : 12) * sms;
+  general_kernel<KIND, T, GATED, TI>
+      <<<(unsigned)(tiles < most ? tiles : most), TI * 4, kFloats * 4 + (size_t)(p.groups.G + 1 + 33) * 4, st>>>(p);
   return cudaGetLastError();
+}
+template <Kind KIND, typename T, bool GATED>
+cudaError_t launch_general(const Problem& p, cudaStream_t st) {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return cudaErrorInvalidDevice;
+  const int64_t jt = ((KIND == kForward ? p.n : p.k) + kTile - 1) / kTile;
+  auto tiles = [&](int ti) {
+    return KIND == kDweight ? (int64_t)p.groups.G * (GATED ? 2 : 1) * ((p.n + ti - 1) / ti) * jt : (p.L * p.groups.R / ti + p.groups.G) * jt;
+  };
+  if (tiles(64) < 4 * sms) return launch_tiles<KIND, T, GATED, 32>(p, tiles(32), sms, st);
+  return launch_tiles<KIND, T, GATED, 64>(p, tiles(64), sms, st);
 }
 
 // ---- sums of dout's columns per group (the bias's gradient) ----------------------------------------------------
 struct BiasArgs {
   Groups groups;
-  int32_t n, gated, f32;
+  int32_t n, gated, f32, wide, chunks;
   int64_t ld_y;
   const void *y, *add, *add_up;
   void *db, *db_up;
+  float* parts;   // [chunks][halves][G][n], null with one chunk
 };
-// A CTA sums 32 columns of one group: 32 warps take rows in turn, four under way each, and their sums are added in a fixed order.
 template <typename T>
-__global__ void __launch_bounds__(1024) bias_kernel(const BiasArgs a) {
-  __shared__ float part[32][33];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = blockIdx.y, half = blockIdx.z;
-  const int j = blockIdx.x * 32 + lane;
+__device__ __forceinline__ void bias_store(const BiasArgs& a, int half, int64_t at, float v) {
+  const void* add = half ? a.add_up : a.add;
+  void* db = half ? a.db_up : a.db;
+  if (a.f32) ((float*)db)[at] = v + (add ? ((const float*)add)[at] : 0.f);
+  else store_as((T*)db + at, v + (add ? load_as_float((const T*)add + at) : 0.f));
+}
+// A CTA of 8 warps sums 256 columns (eight per lane) of one group, or of one chunk of its rows; a warp takes every eighth row, four under way.  Parts
+// are added in a fixed order.
+template <typename T>
+__global__ void __launch_bounds__(256) bias_kernel(const BiasArgs a) {
+  __shared__ float part[8][256 + 8];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = blockIdx.y, half = blockIdx.z % (a.gated + 1), chunk = blockIdx.z / (a.gated + 1);
+  const int j = blockIdx.x * 256 + 8 * lane, count = min(max(a.n - j, 0), 8);
   const GroupRows gr = group_rows(a.groups, g);
+  const int64_t each = (gr.m + a.chunks - 1) / a.chunks, lo = min(chunk * each, gr.m), hi = min(lo + each, gr.m);
   const T* y = (const T*)a.y + gr.first * a.ld_y + (int64_t)half * a.n + j;
-  float s[4] = {};
-  if (j < a.n)
-    for (int64_t r = warp; r < gr.m; r += 128) {
+  float s[8] = {};
+  if (count)
+    for (int64_t r = lo + warp; r < hi; r += 32) {
+      uint32_t w[4][2 * sizeof(T)];
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (r + 32 * u < gr.m) s[u] += load_as_float(y + (r + 32 * u) * a.ld_y);
+      for (int u = 0; u < 4; ++u) load_8(y + min(r + 8 * u, hi - 1) * a.ld_y, a.wide, count, w[u]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        float v[8];
+        floats_of(w[u], v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] += r + 8 * u < hi ? v[i] : 0.f;
+      }
     }
-  part[warp][lane] = (s[0] + s[1]) + (s[2] + s[3]);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) part[warp][8 * lane + i] = s[i];
   __syncthreads();
-  float v = part[lane][warp];   // column `warp`, part `lane`
-  for (int d = 16; d; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
-  const int col = blockIdx.x * 32 + warp;
-  if (lane == 0 && col < a.n) {
-    const int64_t at = (int64_t)g * a.n + col;
-    const void* add = half ? a.add_up : a.add;
-    void* db = half ? a.db_up : a.db;
-    if (a.f32) ((float*)db)[at] = v + (add ? ((const float*)add)[at] : 0.f);
-    else store_as((T*)db + at, v + (add ? load_as_float((const T*)add + at) : 0.f));
+  float v = 0.f;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) v += part[w][threadIdx.x];
+  const int col = blockIdx.x * 256 + threadIdx.x;
+  if (col >= a.n) return;
+  const int64_t at = (int64_t)g * a.n + col;
+  if (a.parts) {
+    a.parts[(int64_t)(chunk * (a.gated + 1) + half) * a.groups.G * a.n + at] = v;
+    return;
   }
+  bias_store<T>(a, half, at, v);
+}
+template <typename T>
+__global__ void __launch_bounds__(256) bias_parts_kernel(const BiasArgs a) {
+  const int64_t at = blockIdx.x * 256ll + threadIdx.x, all = (int64_t)a.groups.G * a.n;
+  if (at >= all) return;
+  float v = 0.f;
+  for (int c = 0; c < a.chunks; ++c) v += a.parts[(int64_t)(c * (a.gated + 1) + blockIdx.y) * all + at];
+  bias_store<T>(a, blockIdx.y, at, v);
 }
 
 // ---- 8-bit checkpoints ------------------------------------------------------------------------------------------
-// Four lanes have a block of 32 columns.  `wide`: eight columns are aligned as a whole in both tensors.
-template <typename T>
+// Rows whose columns are aligned eight at a time: four lanes have a block of 32 columns, and a lane has U blocks, kStride blocks apart, under way.
+// 16384 x 4096 bf16: one block per lane 50 us.
+template <typename T, int U>
 __global__ void __launch_bounds__(256) pack_kernel(const T* x, uint8_t* q, uint8_t* scales, int64_t blocks, int per_row, int d, int64_t ld_x,
-                                                   int64_t ld_q, bool wide) {
-  const int64_t b = (blockIdx.x * 256ll + threadIdx.x) / 4;
-  const bool on = b < blocks;
-  const int64_t row = on ? b / per_row : 0;
-  const int j = (int)(on ? b % per_row : 0) * 32 + 8 * (threadIdx.x & 3), count = on ? min(max(d - j, 0), 8) : 0;
-  uint32_t raw[2 * sizeof(T)] = {}, w[2];
+                                                   int64_t ld_q) {
+  const int64_t first = (int64_t)blockIdx.x * (64 * U) + threadIdx.x / 4;
+  uint32_t raw[U][2 * sizeof(T)];
+  int count[U], col[U];
+  int64_t row[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t b = min(first + 64 * u, blocks - 1);
+    row[u] = (uint32_t)(b >> 32) ? b / per_row : (uint32_t)b / (uint32_t)per_row;
+    col[u] = (int)(b - row[u] * per_row) * 32 + 8 * (threadIdx.x & 3), count[u] = min(max(d - col[u], 0), 8);
+#pragma unroll
+    for (int i = 0; i < 2 * (int)sizeof(T); ++i) raw[u][i] = 0u;
+    if (count[u]) load_8(x + row[u] * ld_x + col[u], true, count[u], raw[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float v[8];
+    uint32_t w[2];
+    floats_of(raw[u], v);
+    const uint32_t s = pack_8(v, w);
+    const int64_t b = first + 64 * u;
+    if (b >= blocks) continue;
+    if (count[u]) store_words_8(q + row[u] * ld_q + col[u], true, count[u], w);
+    if ((threadIdx.x & 3) == 0) scales[b] = (uint8_t)s;
+  }
+}
+template <typename T, int U>
+__global__ void __launch_bounds__(256) unpack_kernel(const uint8_t* q, const uint8_t* scales, T* x, int64_t blocks, int per_row, int d,
+                                                     int64_t ld_x, int64_t ld_q) {
+  const int64_t first = (int64_t)blockIdx.x * (64 * U) + threadIdx.x / 4;
+  uint32_t w[U][2], s[U];
+  int count[U], col[U];
+  int64_t row[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t b = min(first + 64 * u, blocks - 1);
+    row[u] = (uint32_t)(b >> 32) ? b / per_row : (uint32_t)b / (uint32_t)per_row;
+    col[u] = (int)(b - row[u] * per_row) * 32 + 8 * (threadIdx.x & 3), count[u] = first + 64 * u < blocks ? min(max(d - col[u], 0), 8) : 0;
+    w[u][0] = w[u][1] = 0u;
+    if (count[u]) load_8(q + row[u] * ld_q + col[u], true, count[u], w[u]);
+    s[u] = scales[b];
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float v[8];
+    floats_of(w[u], v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= scale_value(s[u]);
+    if (count[u]) store_8(x + row[u] * ld_x + col[u], true, count[u], v);
+  }
+}
+// Any other rows: a column per lane, a warp takes eight blocks of a row at a time.
+template <typename T>
+__global__ void __launch_bounds__(256) pack_odd_kernel(const T* x, uint8_t* q, uint8_t* scales, int64_t rows, int per_row, int d, int64_t ld_x,
+                                                       int64_t ld_q) {
+  const int lane = threadIdx.x & 31, parts = (per_row + 7) / 8;
+  const int64_t w = blockIdx.x * 8ll + (threadIdx.x >> 5), row = w / parts;
+  if (row >= rows) return;
+  const int b0 = (int)(w - row * parts) * 8;
   float v[8];
-  if (count) load_8(x + row * ld_x + j, wide, count, raw);
-  floats_of(raw, v);
-  const uint32_t s = pack_8(v, w);
-  if (count) store_words_8(q + row * ld_q + j, wide, count, w);
-  if (on && (threadIdx.x & 3) == 0) scales[b] = (uint8_t)s;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (b0 + i) * 32 + lane < d ? load_as_float(x + row * ld_x + (b0 + i) * 32 + lane) : 0.f;
+  uint32_t mine = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t s = warp_block_scale(v[i]);
+    if ((b0 + i) * 32 + lane < d) q[row * ld_q + (b0 + i) * 32 + lane] = (uint8_t)to_e4m3x2(v[i] * scale_inverse(s), 0.f);
+    if (lane == i) mine = s;
+  }
+  if (lane < 8 && b0 + lane < per_row) scales[row * per_row + b0 + lane] = (uint8_t)mine;
 }
 template <typename T>
-__global__ void __launch_bounds__(256) unpack_kernel(const uint8_t* q, const uint8_t* scales, T* x, int64_t blocks, int per_row, int d,
-                                                     int64_t ld_x, int64_t ld_q, bool wide) {
-  const int64_t b = (blockIdx.x * 256ll + threadIdx.x) / 4;
-  if (b >= blocks) return;
-  const int64_t row = b / per_row;
-  const int j = (int)(b % per_row) * 32 + 8 * (threadIdx.x & 3), count = min(max(d - j, 0), 8);
-  if (!count) return;
-  uint32_t w[2];
-  float v[8];
-  load_8(q + row * ld_q + j, wide, count, w);
-  const float s = scale_value(scales[b]);
-  floats_of(w, v);
+__global__ void __launch_bounds__(256) unpack_odd_kernel(const uint8_t* q, const uint8_t* scales, T* x, int64_t rows, int per_row, int d,
+                                                         int64_t ld_x, int64_t ld_q) {
+  const int lane = threadIdx.x & 31, parts = (per_row + 7) / 8;
+  const int64_t w = blockIdx.x * 8ll + (threadIdx.x >> 5), row = w / parts;
+  if (row >= rows) return;
+  const int b0 = (int)(w - row * parts) * 8;
+  uint32_t v[8];
+  const uint32_t s = b0 + (lane & 7) < per_row ? scales[row * per_row + b0 + (lane & 7)] : 0u;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] *= s;
-  store_8(x + row * ld_x + j, wide, count, v);
+  for (int i = 0; i < 8; ++i) v[i] = (b0 + i) * 32 + lane < d ? q[row * ld_q + (b0 + i) * 32 + lane] : 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float f = e4m3x2_value(v[i]).x * scale_value(__shfl_sync(0xffffffffu, s, i));
+    if ((b0 + i) * 32 + lane < d) store_as(x + row * ld_x + (b0 + i) * 32 + lane, f);
+  }
 }
 
 }  // namespace
@@ -247,38 +376,67 @@ cudaError_t run_general(Kind kind, const Problem& p, int32_t dtype, cudaStream_t
   return g ? launch_general<kDweight, B, true>(p, st) : launch_general<kDweight, B, false>(p, st);
 }
 
-cudaError_t run_bias_sums(const Problem& p, int32_t dtype, const void* add, const void* add_up, void* db, void* db_up, cudaStream_t st) {
-  const BiasArgs a{p.groups, p.n, p.gated, p.dw_f32, p.ld_y, p.y, add, add_up, db, db_up};
-  const dim3 grid((p.n + 31) / 32, p.groups.G, p.gated ? 2 : 1);
-  if (dtype == MCCE_F32) bias_kernel<float><<<grid, 1024, 0, st>>>(a);
-  else bias_kernel<__nv_bfloat16><<<grid, 1024, 0, st>>>(a);
-  return cudaGetLastError();
-}
-
 namespace {
 // Eight columns of every row start at a multiple of what they take, 16 bytes at most.
 bool wide_rows(const void* p, int64_t ld, int e) { return !p || (((uintptr_t)p | (uintptr_t)(ld * e)) & (e == 1 ? 7 : 15)) == 0; }
 }  // namespace
 
+// Chunks of a group's rows: one unless the groups are few and long.
+int bias_chunks(int64_t rows, int32_t G, int32_t n) {
+  const int64_t ctas = (int64_t)G * ((n + 255) / 256), each = rows / G / 512;
+  if (each < 2 || ctas >= 592) return 1;
+  const int64_t want = 592 / ctas;
+  return (int)(each < want ? each : want < 64 ? want : 64);
+}
+cudaError_t run_bias_sums(const Problem& p, int32_t dtype, const void* add, const void* add_up, void* db, void* db_up, float* parts,
+                          cudaStream_t st) {
+  const int halves = p.gated ? 2 : 1, e = dtype == MCCE_F32 ? 4 : 2, chunks = bias_chunks(p.L * p.groups.R, p.groups.G, p.n);
+  const bool wide = wide_rows(p.y, p.ld_y, e) && (!p.gated || p.n * e % 16 == 0);
+  const BiasArgs a{p.groups, p.n, p.gated, p.dw_f32, wide, chunks, p.ld_y, p.y, add, add_up, db, db_up, chunks > 1 ? parts : nullptr};
+  const dim3 grid((p.n + 255) / 256, p.groups.G, halves * chunks), all((unsigned)(((int64_t)p.groups.G * p.n + 255) / 256), halves);
+  if (dtype == MCCE_F32) bias_kernel<float><<<grid, 256, 0, st>>>(a);
+  else bias_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(a);
+  cudaError_t err = cudaGetLastError();
+  if (err != cudaSuccess || chunks == 1) return err;
+  if (dtype == MCCE_F32) bias_parts_kernel<float><<<all, 256, 0, st>>>(a);
+  else bias_parts_kernel<__nv_bfloat16><<<all, 256, 0, st>>>(a);
+  return cudaGetLastError();
+}
+
+namespace {
+template <typename T>
+cudaError_t pack_as(bool pack, const void* x, void* to, const uint8_t* q_in, uint8_t* q, const uint8_t* s_in, uint8_t* scales, int64_t rows, int32_t d,
+                    int64_t ld_x, int64_t ld_q, cudaStream_t st) {
+  const int per_row = (d + 31) / 32;
+  const bool wide = pack ? wide_rows(x, ld_x, sizeof(T)) && wide_rows(q, ld_q, 1) : wide_rows(to, ld_x, sizeof(T)) && wide_rows(q_in, ld_q, 1);
+  const int64_t blocks = rows * per_row;
+  constexpr int kU = sizeof(T) == 2 ? 4 : 2;
+  const bool many = blocks >= 148 * 8 * 64 * kU;   // else one block per lane: more CTAs
+  const int64_t grid = !wide ? (rows * ((per_row + 7) / 8) + 7) / 8 : many ? (blocks + 64 * kU - 1) / (64 * kU) : (blocks + 63) / 64;
+  if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
+  const unsigned n = (unsigned)grid;
+  if (pack) {
+    if (!wide) pack_odd_kernel<T><<<n, 256, 0, st>>>((const T*)x, q, scales, rows, per_row, d, ld_x, ld_q);
+    else if (many) pack_kernel<T, kU><<<n, 256, 0, st>>>((const T*)x, q, scales, blocks, per_row, d, ld_x, ld_q);
+    else pack_kernel<T, 1><<<n, 256, 0, st>>>((const T*)x, q, scales, blocks, per_row, d, ld_x, ld_q);
+  } else {
+    if (!wide) unpack_odd_kernel<T><<<n, 256, 0, st>>>(q_in, s_in, (T*)to, rows, per_row, d, ld_x, ld_q);
+    else if (many) unpack_kernel<T, kU><<<n, 256, 0, st>>>(q_in, s_in, (T*)to, blocks, per_row, d, ld_x, ld_q);
+    else unpack_kernel<T, 1><<<n, 256, 0, st>>>(q_in, s_in, (T*)to, blocks, per_row, d, ld_x, ld_q);
+  }
+  return cudaGetLastError();
+}
+}  // namespace
+
 cudaError_t run_pack(const void* x, int32_t dtype, int64_t rows, int32_t d, int64_t ld_x, int64_t ld_q, uint8_t* q, uint8_t* scales,
                      cudaStream_t st) {
-  const int per_row = (d + 31) / 32;
-  const int64_t blocks = rows * per_row, grid = (blocks + 63) / 64;
-  if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
-  const bool wide = wide_rows(x, ld_x, dtype == MCCE_F32 ? 4 : 2) && wide_rows(q, ld_q, 1);
-  if (dtype == MCCE_F32) pack_kernel<<<(unsigned)grid, 256, 0, st>>>((const float*)x, q, scales, blocks, per_row, d, ld_x, ld_q, wide);
-  else pack_kernel<<<(unsigned)grid, 256, 0, st>>>((const __nv_bfloat16*)x, q, scales, blocks, per_row, d, ld_x, ld_q, wide);
-  return cudaGetLastError();
+  return dtype == MCCE_F32 ? pack_as<float>(true, x, nullptr, nullptr, q, nullptr, scales, rows, d, ld_x, ld_q, st)
+                           : pack_as<__nv_bfloat16>(true, x, nullptr, nullptr, q, nullptr, scales, rows, d, ld_x, ld_q, st);
 }
 cudaError_t run_unpack(const uint8_t* q, const uint8_t* scales, int32_t dtype, int64_t rows, int32_t d, int64_t ld_x, int64_t ld_q, void* x,
                        cudaStream_t st) {
-  const int per_row = (d + 31) / 32;
-  const int64_t blocks = rows * per_row, grid = (blocks + 63) / 64;
-  if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
-  const bool wide = wide_rows(x, ld_x, dtype == MCCE_F32 ? 4 : 2) && wide_rows(q, ld_q, 1);
-  if (dtype == MCCE_F32) unpack_kernel<<<(unsigned)grid, 256, 0, st>>>(q, scales, (float*)x, blocks, per_row, d, ld_x, ld_q, wide);
-  else unpack_kernel<<<(unsigned)grid, 256, 0, st>>>(q, scales, (__nv_bfloat16*)x, blocks, per_row, d, ld_x, ld_q, wide);
-  return cudaGetLastError();
+  return dtype == MCCE_F32 ? pack_as<float>(false, nullptr, x, q, nullptr, scales, nullptr, rows, d, ld_x, ld_q, st)
+                           : pack_as<__nv_bfloat16>(false, nullptr, x, q, nullptr, scales, nullptr, rows, d, ld_x, ld_q, st);
 }
 
 // ---- checks --------------------------------------------------------------------------------------------------------
@@ -318,6 +476,18 @@ Problem problem(const mcce_linear& p, const int32_t* offsets) {
 }
 int blocks_of(int64_t cols) { return (int)((cols + 31) / 32); }
 int code(cudaError_t e) { return e == cudaSuccess ? MCCE_OK : MCCE_ECUDA; }
+
+// Workspace of the weight gradient: 8-bit rows in the type of dout, then the parts of the bias's gradient.
+size_t unpacked_bytes(const mcce_linear& p) {
+  if (p.saved_dtype != MCCE_E4M3) return 0;
+  const int64_t ld = (p.k + 7) & ~7ll;
+  return ((size_t)(p.n_layers * p.rows) * ld * elem(p.dtype) + 15) & ~(size_t)15;
+}
+size_t bias_bytes(const mcce_linear& p) {
+  const int32_t G = p.n_layers * p.n_experts;
+  const int chunks = bias_chunks(p.n_layers * p.rows, G, p.n);
+  return chunks > 1 ? (size_t)chunks * (1 + p.gated) * G * p.n * 4 : 0;
+}
 
 }  // namespace
 }  // namespace linear
@@ -408,9 +578,8 @@ extern "C" int mcce_expert_linear_backward(const mcce_linear* p, const void* dou
 }
 
 extern "C" size_t mcce_expert_linear_dweight_workspace_bytes(const mcce_linear* p) {
-  if (!sizes_ok(p) || p->saved_dtype != MCCE_E4M3) return 0;
-  const int64_t ld = (p->k + 7) & ~7ll;
-  return (size_t)(p->n_layers * p->rows) * ld * elem(p->dtype);
+  if (!sizes_ok(p)) return 0;
+  return unpacked_bytes(*p) + bias_bytes(*p);
 }
 
 extern "C" int mcce_expert_linear_dweight(const mcce_linear* p, const void* dout, const void* x, const void* scales,
@@ -460,7 +629,8 @@ extern "C" int mcce_expert_linear_dweight(const mcce_linear* p, const void* dout
     q.x = workspace, q.ld_x = ld;
   }
   cudaError_t err = tensor_applicable(kDweight, q, p->dtype) ? run_tensor(kDweight, q, st) : run_general(kDweight, q, p->dtype, st);
-  if (err == cudaSuccess && db) err = run_bias_sums(q, p->dtype, add_db, add_db_up, db, db_up, st);
+  if (err == cudaSuccess && db) 
+    err = run_bias_sums(q, p->dtype, add_db, add_db_up, db, db_up, (float*)((uint8_t*)workspace + unpacked_bytes(*p)), st);
   return code(err);
 }
 

@@ -78,6 +78,11 @@ __device__ __forceinline__ float2 e4m3x2_value(uint32_t pair) {
   return __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)pair, __NV_E4M3)));
 }
 
+// The scale of the values that a whole warp holds, a column per lane; lanes without one hand in 0.
+__device__ __forceinline__ uint32_t warp_block_scale(float v) {
+  return block_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu));
+}
+
 // ---- eight neighbouring columns of a row in a lane ----------------------------------------------------------------
 // As they lie in memory, `count` of them (1 .. 8; the rest reads as 0), in one or two accesses where `wide` says that they are aligned to it.
 template <typename E>
@@ -434,7 +439,9 @@ __device__ __forceinline__ void count_tiles(const Groups& g, int rows_per_tile, 
 cudaError_t run_general(Kind kind, const Problem& p, int32_t dtype, cudaStream_t st);   // any size, stride and alignment
 bool tensor_applicable(Kind kind, const Problem& p, int32_t dtype);
 cudaError_t run_tensor(Kind kind, const Problem& p, cudaStream_t st);
-cudaError_t run_bias_sums(const Problem& p, int32_t dtype, const void* add, const void* add_up, void* db, void* db_up, cudaStream_t st);
+int bias_chunks(int64_t rows, int32_t G, int32_t n);   // more than one: run_bias_sums needs `parts`
+cudaError_t run_bias_sums(const Problem& p, int32_t dtype, const void* add, const void* add_up, void* db, void* db_up, float* parts,
+                          cudaStream_t st);
 cudaError_t run_pack(const void* x, int32_t dtype, int64_t rows, int32_t d, int64_t ld_x, int64_t ld_q, uint8_t* q, uint8_t* scales,
                      cudaStream_t st);
 cudaError_t run_unpack(const uint8_t* q, const uint8_t* scales, int32_t dtype, int64_t rows, int32_t d, int64_t ld_x, int64_t ld_q, void* x,

@@ -480,6 +480,10 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
       it.f0 += rank * (C::kFeatures / C::kCtas);
       const bool sums = walk.slabs(it) > 0;
       const uint32_t buf = acc & 1u;
+      // what the layer below kept is asked for a chunk ahead, the first before the sums are there
+      Backward<__nv_bfloat16>::Asked<2> asked;
+      if constexpr (KIND == kBackward)
+        Backward<__nv_bfloat16>(p.bwd, it.g, it.f0 + quad * 32 + 8 * (lane & 3)).ask((int64_t)it.row + 16 * team, it.rows - 16 * team, asked);
       if (sums) {
         if (!mbar_wait(bar_tfull + 8 * buf, (acc >> 1) & 1u, abort_flag, &wait_error, 4u)) break;
         ++acc;
@@ -534,18 +538,18 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
           else return p.bwd;
         }();
         const Epilogue e(args, it.g, it.f0 + quad * 32 + 8 * (lane & 3));
-        float* mine = swap + (warp - 2) * 16 * kSwapStride;
+        float* turn = swap + (warp - 2) * 16 * kSwapStride;
         for (int c = 16 * team; c < it.rows; c += 32) {
           float v[16], t[2][8];
-          Backward<__nv_bfloat16>::Asked<2> q;
-          if constexpr (KIND == kBackward) e.ask((int64_t)it.row + c, it.rows - c, q);
+          const Backward<__nv_bfloat16>::Asked<2> q = asked;
+          if constexpr (KIND == kBackward) e.ask((int64_t)it.row + c + 32, it.rows - c - 32, asked);
           __syncwarp();
           tmem_ld16(t0 + c, v);
           tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 16; ++j) mine[j * kSwapStride + lane] = v[j];
+          for (int j = 0; j < 16; ++j) turn[j * kSwapStride + lane] = v[j];
           __syncwarp();
-          row_of(mine, 0, t[0]), row_of(mine, 8, t[1]);
+          row_of(turn, 0, t[0]), row_of(turn, 8, t[1]);
           if constexpr (KIND == kBackward) {
             e.rows((int64_t)it.row + c, it.rows - c, t, q);
           } else {
