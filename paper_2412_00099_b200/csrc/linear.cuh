@@ -41,14 +41,14 @@ __device__ __forceinline__ void store_as(__nv_bfloat16* p, float v) { *p = __flo
 // FAST: bf16 results, whose rounding (2^-9) hides the few 2^-22 of the fast exponential and division.
 template <bool FAST>
 __device__ __forceinline__ float sigmoid(float z) {
-  if (FAST) return __fdividef(1.f, 1.f + __expf(-fmaxf(z, -80.f)));
+  if (FAST) return __fdividef(1.f, 1.f + __expf(-z));   // 0 from about z = -87 on
   return 1.f / (1.f + expf(-z));
 }
 template <bool FAST>
 __device__ __forceinline__ void slope_and_value(float z, int act, float& value, float& slope) {
   if (act == MCCE_ACT_SILU) {
     const float s = sigmoid<FAST>(z);
-    value = z * s, slope = s * (1.f + z * (1.f - s));
+    value = z * s, slope = fmaf(value, 1.f - s, s);
   } else if (act == MCCE_ACT_GELU) {
     const float p = normcdff(z), q = z * z * -0.5f;
     value = z * p, slope = p + z * (0.3989422804014327f * (FAST ? __expf(q) : expf(q)));

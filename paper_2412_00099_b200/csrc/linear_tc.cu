@@ -28,9 +28,7 @@ namespace {
 __device__ uint32_t wait_error;   // set when a bounded wait gives up; read and cleared by mcce_expert_linear_status
 
 constexpr int kTileM = 128;    // MMA rows
-constexpr int kEpilogueWarps = 8;
 constexpr int kSwapStride = 36;   // floats of a row: reading eight columns per lane, four lanes a row, then meets every bank once
-constexpr int kClearWarp = 2 + kEpilogueWarps;   // dweight only
 constexpr int kBlockOfTiles = 16;   // row tiles of a group that are walked together, so that their rows stay in L2 for the next features
 
 template <int KIND, bool GATED, int BN, bool PAIR>
@@ -43,9 +41,14 @@ struct Cfg {
   static constexpr uint32_t kABytes = kTileM * kSlab * 2;
   static constexpr uint32_t kBBytes = BN / kCtas * kSlab * 2;
   static constexpr uint32_t kStageBytes = kABytes + kBBytes;
-  // sums of 16 rows x 32 features per epilogue warp, on their way from a feature per lane to a row per four lanes; gated: two buffers
-  // (dweight: 32 x 32)
-  static constexpr uint32_t kSwapBytes = KIND == kDweight ? kEpilogueWarps * 4096 : kEpilogueWarps * 16 * kSwapStride * 4 * (KIND == kForward && GATED ? 2 : 1);
+  // Epilogue warps, four teams (a gated layer and dweight: two) of a warp per TMEM quadrant.  They have few instructions that do not wait for another:
+  // 16 of them take a gated layer's gradient through in 2/3 of the time of 8.
+  static constexpr int kTeams = KIND == kDweight || (KIND == kForward && GATED) ? 2 : 4;
+  static constexpr int kEpilogueWarps = 4 * kTeams, kClearWarp = 2 + kEpilogueWarps;
+  // Sums of 8 (gated: 16) rows x 32 features per epilogue warp, on their way from a feature per lane to a row per four lanes; gated: two buffers;
+  // dweight: 32 x 32.
+  static constexpr uint32_t kSwapBytes =
+      kEpilogueWarps * (KIND == kDweight ? 4096 : 8 * kSwapStride * 4 * (KIND == kForward && GATED ? 4 : 1));
   static constexpr uint32_t kCountBytes = KIND == kDweight ? 0 : ((MCCE_LINEAR_MAX_GROUPS + 1 + 33) * 4 + 127) & ~127;
   static constexpr uint32_t kFixed = 1024 + 512 + kSwapBytes + kCountBytes;
   static constexpr int kFit = (232448 - kFixed) / kStageBytes;
@@ -66,7 +69,16 @@ struct Maps {
 __device__ __forceinline__ uint64_t smem_desc_across(uint32_t addr, uint32_t panel) {
   return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(panel >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
-// 32 consecutive fp32 columns of this thread's TMEM lane
+// 8 and 32 consecutive fp32 columns of this thread's TMEM lane
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float (&v)[8]) {
+  uint32_t r[8];
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
   uint32_t r[32];
   asm volatile(
@@ -326,7 +338,7 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(bar_tfull + 8 * b, 1);
-      mbar_init(bar_tempty + 8 * b, kEpilogueWarps * C::kCtas);
+      mbar_init(bar_tempty + 8 * b, C::kEpilogueWarps * C::kCtas);
     }
     for (int b = 0; b < 4; ++b) mbar_init(bar_swap + 8 * b, 2);
     *abort_flag = 0u;
@@ -447,7 +459,7 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
       if (alive && lane == 0) commit<PAIR>(bar_tfull + 8 * buf);
       __syncwarp();
     }
-  } else if (kTail && warp == kClearWarp) {
+  } else if (kTail && warp == C::kClearWarp) {
     // Clears, in a group's last slab, the rows of the next group up to the next multiple of 16 (the MMAs go no further), of both operands: zero times
     // a NaN of the next group would not be zero.  In the MMAs' own warp this cost the 8 slabs of a group of 500 rows 20 us of 300.
     uint32_t stage = 0, tails = 0;   // tails: the phase of every stage's bar_tail
@@ -472,7 +484,7 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
       stage = (stage + 1) % C::kStages;
     }
   } else {
-    const int quad = warp & 3, team = (warp - 2) >> 2;   // TMEM lanes this warp may read; which half of the chunks it takes
+    const int quad = warp & 3, team = (warp - 2) >> 2;   // TMEM lanes this warp may read; which chunks it takes
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     uint32_t acc = 0, swaps = 0;
     bool alive = true;
@@ -481,9 +493,9 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
       const bool sums = walk.slabs(it) > 0;
       const uint32_t buf = acc & 1u;
       // what the layer below kept is asked for a chunk ahead, the first before the sums are there
-      Backward<__nv_bfloat16>::Asked<2> asked;
+      Backward<__nv_bfloat16>::Asked<1> asked;
       if constexpr (KIND == kBackward)
-        Backward<__nv_bfloat16>(p.bwd, it.g, it.f0 + quad * 32 + 8 * (lane & 3)).ask((int64_t)it.row + 16 * team, it.rows - 16 * team, asked);
+        Backward<__nv_bfloat16>(p.bwd, it.g, it.f0 + quad * 32 + 8 * (lane & 3)).ask((int64_t)it.row + 8 * team, it.rows - 8 * team, asked);
       if (sums) {
         if (!mbar_wait(bar_tfull + 8 * buf, (acc >> 1) & 1u, abort_flag, &wait_error, 4u)) break;
         ++acc;
@@ -538,22 +550,22 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
           else return p.bwd;
         }();
         const Epilogue e(args, it.g, it.f0 + quad * 32 + 8 * (lane & 3));
-        float* turn = swap + (warp - 2) * 16 * kSwapStride;
-        for (int c = 16 * team; c < it.rows; c += 32) {
-          float v[16], t[2][8];
-          const Backward<__nv_bfloat16>::Asked<2> q = asked;
-          if constexpr (KIND == kBackward) e.ask((int64_t)it.row + c + 32, it.rows - c - 32, asked);
+        float* turn = swap + (warp - 2) * 8 * kSwapStride;
+        for (int c = 8 * team; c < it.rows; c += 8 * C::kTeams) {
+          float v[8], t[1][8];
+          const Backward<__nv_bfloat16>::Asked<1> q = asked;
+          if constexpr (KIND == kBackward) e.ask((int64_t)it.row + c + 8 * C::kTeams, it.rows - c - 8 * C::kTeams, asked);
           __syncwarp();
-          tmem_ld16(t0 + c, v);
+          tmem_ld8(t0 + c, v);
           tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 16; ++j) turn[j * kSwapStride + lane] = v[j];
+          for (int j = 0; j < 8; ++j) turn[j * kSwapStride + lane] = v[j];
           __syncwarp();
-          row_of(turn, 0, t[0]), row_of(turn, 8, t[1]);
+          row_of(turn, 0, t[0]);
           if constexpr (KIND == kBackward) {
             e.rows((int64_t)it.row + c, it.rows - c, t, q);
           } else {
-            float none[2][8];
+            float none[1][8];
             e.rows((int64_t)it.row + c, it.rows - c, t, none);
           }
         }
