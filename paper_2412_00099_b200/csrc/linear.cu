@@ -534,6 +534,7 @@ extern "C" int mcce_expert_linear(const mcce_linear* p, const void* x, const int
       !apart(ssv, {&sx, &soff, &sw, &swu, &sb, &sbu, &sadd, &ssc}) || !apart(ssc, {&sx, &soff, &sw, &swu, &sb, &sbu, &sadd}))
     return MCCE_EINVAL;
   cudaStream_t st = (cudaStream_t)cuda_stream;
+  if (few_applicable(q, p->dtype)) return code(run_few(q, st));
   if (tensor_applicable(kForward, q, p->dtype)) return code(run_tensor(kForward, q, st));
   return code(run_general(kForward, q, p->dtype, st));
 }

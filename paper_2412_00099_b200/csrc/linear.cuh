@@ -409,8 +409,9 @@ __device__ __forceinline__ int find_group(const int* before, int G, int tile) {
 // before[0 .. G]: every thread of the block calls it; ends with a barrier.  scratch: 33 ints.
 __device__ __forceinline__ void count_tiles(const Groups& g, int rows_per_tile, int* before, int* scratch) {
   const int t = threadIdx.x, nt = blockDim.x, each = (g.G + nt - 1) / nt;
+  auto tiles = [&](int i) { return (int)((group_rows(g, i).m + rows_per_tile - 1) / rows_per_tile); };
   int sum = 0;
-  for (int i = t * each; i < min((t + 1) * each, g.G); ++i) sum += (int)((group_rows(g, i).m + rows_per_tile - 1) / rows_per_tile);
+  for (int i = t * each; i < min((t + 1) * each, g.G); ++i) sum += tiles(i);
   int run = sum;
   for (int d = 1; d < 32; d *= 2) {
     const int o = __shfl_up_sync(0xffffffffu, run, d);
@@ -418,25 +419,22 @@ __device__ __forceinline__ void count_tiles(const Groups& g, int rows_per_tile, 
   }
   if ((t & 31) == 31) scratch[t >> 5] = run;
   __syncthreads();
-  if (t < 32) {
-    int w = t < (nt >> 5) ? scratch[t] : 0;
-    for (int d = 1; d < 32; d *= 2) {
-      const int o = __shfl_up_sync(0xffffffffu, w, d);
-      if (t >= d) w += o;
-    }
-    scratch[t] = w;
-  }
-  __syncthreads();
-  run += (t >> 5 ? scratch[(t >> 5) - 1] : 0) - sum;   // tiles before this thread's groups
-  if (t == 0) before[g.G] = scratch[(nt >> 5) - 1];
-  for (int i = t * each; i < min((t + 1) * each, g.G); ++i) {
-    before[i] = run;
-    run += (int)((group_rows(g, i).m + rows_per_tile - 1) / rows_per_tile);
+  // tiles of the warps before this one, and of all
+  int w = (t & 31) < (nt >> 5) ? scratch[t & 31] : 0, all = w, less = (t & 31) < (t >> 5) ? w : 0;
+  all = __reduce_add_sync(0xffffffffu, all), less = __reduce_add_sync(0xffffffffu, less);
+  run += less - sum;
+  if (t == 0) before[g.G] = all;
+  if (each == 1) {
+    if (t < g.G) before[t] = run;
+  } else {
+    for (int i = t * each; i < min((t + 1) * each, g.G); ++i) before[i] = run, run += tiles(i);
   }
   __syncthreads();
 }
 
 cudaError_t run_general(Kind kind, const Problem& p, int32_t dtype, cudaStream_t st);   // any size, stride and alignment
+bool few_applicable(const Problem& p, int32_t dtype);   // forward, a few rows in all
+cudaError_t run_few(const Problem& p, cudaStream_t st);
 bool tensor_applicable(Kind kind, const Problem& p, int32_t dtype);
 cudaError_t run_tensor(Kind kind, const Problem& p, cudaStream_t st);
 int bias_chunks(int64_t rows, int32_t G, int32_t n);   // more than one: run_bias_sums needs `parts`

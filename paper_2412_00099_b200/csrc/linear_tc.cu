@@ -31,8 +31,13 @@ constexpr int kTileM = 128;    // MMA rows
 constexpr int kSwapStride = 36;   // floats of a row: reading eight columns per lane, four lanes a row, then meets every bank once
 constexpr int kBlockOfTiles = 16;   // row tiles of a group that are walked together, so that their rows stay in L2 for the next features
 
-template <int KIND, bool GATED, int BN, bool PAIR>
+// How CTAs of a cluster work together: each for itself; a pair on one tile; several on parts of one tile's reduction.
+enum Share { kAlone = 0, kPair = 1, kSplit = 2 };
+constexpr int most_parts(int bn) { return bn <= 64 ? 4 : 2; }   // CTAs on one reduction: what rank 0 has room for
+
+template <int KIND, bool GATED, int BN, int SHARE>
 struct Cfg {
+  static constexpr bool PAIR = SHARE == kPair;
   static constexpr int kCtas = PAIR ? 2 : 1;
   static constexpr int kFeatures = kTileM * kCtas / (KIND == kForward && GATED ? 2 : 1);   // of a tile
   // Reduction per stage.  Along an operand's rows 64 bf16 are a swizzled row of 128 bytes; dweight's operands lie across their rows, and the fewer copies of
@@ -50,7 +55,8 @@ struct Cfg {
   static constexpr uint32_t kSwapBytes =
       kEpilogueWarps * (KIND == kDweight ? 4096 : 8 * kSwapStride * 4 * (KIND == kForward && GATED ? 4 : 1));
   static constexpr uint32_t kCountBytes = KIND == kDweight ? 0 : ((MCCE_LINEAR_MAX_GROUPS + 1 + 33) * 4 + 127) & ~127;
-  static constexpr uint32_t kFixed = 1024 + 512 + kSwapBytes + kCountBytes;
+  static constexpr uint32_t kPartBytes = SHARE == kSplit ? (most_parts(BN) - 1) * BN * kTileM * 4 : 0;   // the other CTAs' sums, in rank 0's
+  static constexpr uint32_t kFixed = 1024 + 512 + kSwapBytes + kCountBytes + kPartBytes;
   static constexpr int kFit = (232448 - kFixed) / kStageBytes;
   static constexpr int kStages = kFit < 10 ? kFit : 10;
   static constexpr int kThreads = 32 * (2 + kEpilogueWarps + (KIND == kDweight ? 1 : 0));
@@ -134,6 +140,11 @@ __device__ __forceinline__ uint32_t cluster_rank() {
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(r));
+  return r;
+}
 __device__ __forceinline__ uint32_t leaders(uint32_t addr) {   // the same place in rank 0's shared memory
   uint32_t r;
   asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
@@ -141,6 +152,12 @@ __device__ __forceinline__ uint32_t leaders(uint32_t addr) {   // the same place
 }
 __device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// mbar_wait for what other CTAs of the cluster wrote
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* err, uint32_t code) {
+  const bool ok = mbar_wait(bar, parity, abort_flag, err, code);
+  asm volatile("fence.acq_rel.cluster;" ::: "memory");
+  return ok;
 }
 // Without ordering what this thread did before: a release at cluster scope waits for all of its stores.
 __device__ __forceinline__ void arrive_at_relaxed(uint32_t cluster_addr) {
@@ -242,16 +259,17 @@ struct Item {
   int j0, half;     // dweight: first column of x; which half of dout
 };
 
-template <int KIND, bool GATED, int BN, bool PAIR>
+template <int KIND, bool GATED, int BN, int SHARE>
 struct Walk {
-  static constexpr int kFeatures = Cfg<KIND, GATED, BN, PAIR>::kFeatures;
+  static constexpr int kFeatures = Cfg<KIND, GATED, BN, SHARE>::kFeatures;
   const Problem& p;
   const int* before;
-  int first, step, items;   // this CTA's (pair's) tiles: first, first + step ..
+  int first, step, items;   // this CTA's (cluster's) tiles: first, first + step ..
   int FT, JT;   // tiles of features (dweight: of dout's columns), of x's columns
   __device__ __forceinline__ Walk(const Problem& p_, const int* before_) : p(p_), before(before_) {
     const int features = KIND == kBackward ? p.k : p.n;
-    first = PAIR ? blockIdx.x >> 1 : blockIdx.x, step = PAIR ? gridDim.x >> 1 : gridDim.x;
+    const int ctas = SHARE == kAlone ? 1 : cluster_size();
+    first = blockIdx.x / ctas, step = gridDim.x / ctas;
     FT = (features + kFeatures - 1) / kFeatures, JT = KIND == kDweight ? (p.k + BN - 1) / BN : 1;
     items = KIND == kDweight ? p.groups.G * (GATED ? 2 : 1) * FT * JT : before[p.groups.G] * FT;   // fits: the launch sees to it
   }
@@ -298,11 +316,18 @@ struct Walk {
   }
   // N of the tile's MMAs: its rows; its columns of x, in whole panels for each CTA
   __device__ __forceinline__ int wide(const Item& it) const {
-    if (KIND == kDweight) return (min(BN, p.k - it.j0) + 64 * Cfg<KIND, GATED, BN, PAIR>::kCtas - 1) & ~(64 * Cfg<KIND, GATED, BN, PAIR>::kCtas - 1);
+    if (KIND == kDweight) return (min(BN, p.k - it.j0) + 64 * Cfg<KIND, GATED, BN, SHARE>::kCtas - 1) & ~(64 * Cfg<KIND, GATED, BN, SHARE>::kCtas - 1);
     return (it.rows + 15) & ~15;
   }
+  // The slabs of a tile that this CTA multiplies: all, or (several CTAs on its reduction) its share of them
+  __device__ __forceinline__ void range(const Item& it, int place, int& from, int& to) const {
+    from = 0, to = slabs(it);
+    if (SHARE != kSplit) return;
+    const int each = (to + (int)cluster_size() - 1) / (int)cluster_size();
+    from = min(place * each, to), to = min(from + each, to);
+  }
   __device__ __forceinline__ int slabs(const Item& it) const {
-    constexpr int kSlab = Cfg<KIND, GATED, BN, PAIR>::kSlab;
+    constexpr int kSlab = Cfg<KIND, GATED, BN, SHARE>::kSlab;
     if (KIND == kDweight) return (it.rows + kSlab - 1) / kSlab;
     return KIND == kForward ? (p.k + kSlab - 1) / kSlab : (GATED ? 2 : 1) * ((p.n + kSlab - 1) / kSlab);
   }
@@ -311,9 +336,9 @@ struct Walk {
 // One CTA, or a pair of CTAs that share a tile: each has half of its features (128 MMA rows, accumulated in its own TMEM) and half of its
 // rows (dweight: of x's columns) in shared memory, and the leader's MMAs read both halves.  A pair takes in a third less than two single CTAs for
 // the same products.
-template <int KIND, bool GATED, int BN, bool PAIR>
-__global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linear_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Problem p) {
-  using C = Cfg<KIND, GATED, BN, PAIR>;
+template <int KIND, bool GATED, int BN, int SHARE>
+__global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) linear_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Problem p) {
+  using C = Cfg<KIND, GATED, BN, SHARE>;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem_al = smem_raw + (smem_base - smem_u32(smem_raw));
@@ -323,10 +348,13 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
   uint64_t* bars = (uint64_t*)(rest + C::kSwapBytes + C::kCountBytes);
   const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * C::kStages;
   const uint32_t bar_tfull = bar_empty + 8 * C::kStages, bar_tempty = bar_tfull + 16, bar_swap = bar_tempty + 16, bar_tail = bar_swap + 32;
-  uint32_t* tmem_slot = (uint32_t*)(bars + 3 * C::kStages + 8);
+  const uint32_t bar_parts = bar_tail + 8 * C::kStages;
+  uint32_t* tmem_slot = (uint32_t*)(bars + 3 * C::kStages + 9);
+  float* parts = (float*)(rest + C::kSwapBytes + C::kCountBytes + 512);   // [rank - 1][row][feature]
   volatile uint32_t* abort_flag = tmem_slot + 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = PAIR ? (int)cluster_rank() : 0;
+  constexpr bool PAIR = C::PAIR;
+  const int place = SHARE == kAlone ? 0 : (int)cluster_rank(), rank = PAIR ? place : 0;
   // dweight: a group's last slab is complete when a warp of its own has cleared the rows of the next group in it, in each CTA
   constexpr bool kTail = KIND == kDweight;
 
@@ -341,17 +369,18 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
       mbar_init(bar_tempty + 8 * b, C::kEpilogueWarps * C::kCtas);
     }
     for (int b = 0; b < 4; ++b) mbar_init(bar_swap + 8 * b, 2);
+    mbar_init(bar_parts, SHARE == kSplit ? (cluster_size() - 1) * C::kEpilogueWarps : 1);
     *abort_flag = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (PAIR) cluster_sync();
+  if (SHARE != kAlone) cluster_sync();
   if (warp == 1) take_tmem<PAIR>(smem_u32(tmem_slot), 2 * BN);
   if (KIND != kDweight) count_tiles(p.groups, BN, before, before + p.groups.G + 1);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  const Walk<KIND, GATED, BN, PAIR> walk(p, before);
+  const Walk<KIND, GATED, BN, SHARE> walk(p, before);
 
   Item it, mine;
   if (warp == 0) {
@@ -369,7 +398,9 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
         constexpr int kQuarter = C::kRowBox / 4;
         const int quarters = (share + kQuarter - 1) / kQuarter;
         const uint32_t part_b = quarters * kQuarter * 128;
-        for (int kt = 0; kt < slabs; ++kt) {
+        int from, to;
+        walk.range(it, place, from, to);
+        for (int kt = from; kt < to; ++kt) {
           if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1u, abort_flag, &wait_error, 1u)) {
             alive = false;
             break;
@@ -422,8 +453,9 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
     uint32_t stage = 0, phase = 0, acc = 0;
     bool alive = rank == 0;   // the leader's MMAs are the pair's
     for (int i = 0; alive && walk.at(i, mine, it); ++i) {
-      const int slabs = walk.slabs(it);
-      if (slabs == 0) continue;
+      int from, to;
+      walk.range(it, place, from, to);
+      if (from == to) continue;
       const int cols = walk.wide(it);
       // fp32 sums of bf16, M = 128 (256 in a pair), N; a set bit 15 / 16: A / B lies across its rows
       const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)cols >> 3 << 17) | ((uint32_t)(kTileM * C::kCtas) >> 4 << 24) |
@@ -433,7 +465,7 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
       ++acc;
       tc_fence_after();
       const uint32_t d = tmem_base + buf * BN;
-      for (int kt = 0; kt < slabs; ++kt) {
+      for (int kt = from; kt < to; ++kt) {
         if (!mbar_wait(bar_full + 8 * stage, phase, abort_flag, &wait_error, 3u)) {
           alive = false;
           break;
@@ -446,10 +478,10 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
           constexpr uint32_t kStepA = (KIND == kForward ? 32 : 2048) >> 4, kStepB = (KIND == kDweight ? 2048 : 32) >> 4;
           if (left >= C::kSlab) {
 #pragma unroll
-            for (int k = 0; k < C::kSlab / 16; ++k) mma<PAIR>(d, ad + k * kStepA, bd + k * kStepB, idesc, (kt | k) != 0 ? 1u : 0u);
+            for (int k = 0; k < C::kSlab / 16; ++k) mma<PAIR>(d, ad + k * kStepA, bd + k * kStepB, idesc, ((kt - from) | k) != 0 ? 1u : 0u);
           } else {
             const uint64_t low = left <= 64 ? (uint64_t)(64 * 128 >> 4) << 16 : 0;   // panels half as far apart
-            for (int k = 0; k < (left + 15) / 16; ++k) mma<PAIR>(d, ad - low + k * kStepA, bd - low + k * kStepB, idesc, (kt | k) != 0 ? 1u : 0u);
+            for (int k = 0; k < (left + 15) / 16; ++k) mma<PAIR>(d, ad - low + k * kStepA, bd - low + k * kStepB, idesc, ((kt - from) | k) != 0 ? 1u : 0u);
           }
           commit<PAIR>(bar_empty + 8 * stage);
         }
@@ -490,7 +522,9 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
     bool alive = true;
     for (int i = 0; alive && walk.at(i, mine, it); ++i) {
       it.f0 += rank * (C::kFeatures / C::kCtas);
-      const bool sums = walk.slabs(it) > 0;
+      int from, to;
+      walk.range(it, place, from, to);
+      const bool sums = to > from;
       const uint32_t buf = acc & 1u;
       // what the layer below kept is asked for a chunk ahead, the first before the sums are there
       Backward<__nv_bfloat16>::Asked<1> asked;
@@ -502,6 +536,34 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
         tc_fence_after();
       }
       const uint32_t t0 = tmem_base + lane_addr + buf * BN;
+      if constexpr (SHARE == kSplit) {
+        // At most one tile per cluster.  The others hand their sums to rank 0, which adds them in the order of their ranks.
+        if (place != 0) {
+          const uint32_t to0 = leaders(smem_u32(parts + (size_t)(place - 1) * BN * kTileM + quad * 32 + lane));
+          for (int c = 8 * team; c < walk.wide(it); c += 8 * C::kTeams) {
+            float v[8] = {};
+            __syncwarp();
+            if (sums) {
+              tmem_ld8(t0 + c, v);
+              tmem_ld_wait();
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to0 + (uint32_t)((c + j) * kTileM * 4)), "f"(v[j]) : "memory");
+          }
+          __syncwarp();
+          if (lane == 0) arrive_at(leaders(bar_parts));
+          break;
+        }
+        if (cluster_size() > 1 && !mbar_wait_cluster(bar_parts, 0u, abort_flag, &wait_error, 7u)) break;
+      }
+      auto add_parts = [&](auto& v, int c) {
+        if constexpr (SHARE == kSplit) {
+          for (int r = 1; r < (int)cluster_size(); ++r)
+#pragma unroll
+            for (int j = 0; j < (int)(sizeof(v) / 4); ++j) v[j] += parts[((size_t)(r - 1) * BN + c + j) * kTileM + quad * 32 + lane];
+        }
+      };
       if constexpr (KIND == kDweight) {
         const int cols = min(BN, p.k - it.j0), first_row = it.f0 + quad * 32;
         const void* add = it.half ? p.add_dw_up : p.add_dw;
@@ -530,6 +592,7 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
           __syncwarp();
           tmem_ld16(t0 + c, v);
           tmem_ld_wait();
+          add_parts(v, c);
           float* both = swap + (pair * 2 + (swaps & 1)) * 2 * 16 * kSwapStride;
 #pragma unroll
           for (int j = 0; j < 16; ++j) both[(up * 16 + j) * kSwapStride + lane] = v[j];
@@ -558,6 +621,7 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
           __syncwarp();
           tmem_ld8(t0 + c, v);
           tmem_ld_wait();
+          add_parts(v, c);
 #pragma unroll
           for (int j = 0; j < 8; ++j) turn[j * kSwapStride + lane] = v[j];
           __syncwarp();
@@ -589,7 +653,7 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, PAIR>::kThreads, 1) linea
   }
   tc_fence_before();
   __syncthreads();
-  if (PAIR) cluster_sync();   // neither CTA leaves while the other may still reach its barriers
+  if (SHARE != kAlone) cluster_sync();   // no CTA leaves while another may still reach its shared memory
   tc_fence_after();
   if (warp == 1) free_tmem<PAIR>(tmem_base, 2 * BN);
 }
@@ -640,19 +704,33 @@ bool map_panels(CUtensorMap* m, const void* base, int64_t matrices, int64_t rows
   return encode(m, base, 3, dims, strides, box);
 }
 
-template <int KIND, bool GATED, int BN, bool PAIR>
+// Tiles of a product, at most
+template <int KIND, bool GATED, int BN, int SHARE>
+int64_t most_tiles(const Problem& p) {
+  using C = Cfg<KIND, GATED, BN, SHARE>;
+  const int64_t rows = p.L * p.groups.R, FT = ((KIND == kBackward ? p.k : p.n) + C::kFeatures - 1) / C::kFeatures;
+  if (KIND == kDweight) return (int64_t)p.groups.G * (GATED ? 2 : 1) * FT * ((p.k + BN - 1) / BN);
+  return (p.groups.G == 1 ? (rows + BN - 1) / BN : rows / BN + p.groups.G) * FT;
+}
+// CTAs per tile: as many as leave every cluster one tile and every CTA eight slabs.
+int split_of(const Problem& p, int kind, int64_t tiles, int bn, int sms) {
+  const int64_t slabs = (int64_t)((kind == kBackward ? p.n : p.k) + 63) / 64 * (kind == kBackward && p.gated ? 2 : 1);
+  int s = most_parts(bn);
+  while (s > 1 && (tiles * s > sms || slabs < 8 * s)) s /= 2;
+  return s;
+}
+
+template <int KIND, bool GATED, int BN, int SHARE>
 cudaError_t launch(const Problem& p, cudaStream_t st) {
-  using C = Cfg<KIND, GATED, BN, PAIR>;
+  using C = Cfg<KIND, GATED, BN, SHARE>;
   static int cache[64] = {0}, pairs[64] = {0};
-  auto kernel = linear_tc_kernel<KIND, GATED, BN, PAIR>;
+  auto kernel = linear_tc_kernel<KIND, GATED, BN, SHARE>;
   int sms = 0, dev = 0;
   cudaError_t e = sm_count_and_smem_optin(kernel, C::kSmemBytes, cache, &sms);
   if (e != cudaSuccess) return e;
   Maps m;
   bool ok;
-  const int64_t rows = p.L * p.groups.R, features = KIND == kBackward ? p.k : p.n;
-  const int64_t FT = (features + C::kFeatures - 1) / C::kFeatures;
-  int64_t most = (rows / BN + p.groups.G) * FT;
+  const int64_t rows = p.L * p.groups.R, most = most_tiles<KIND, GATED, BN, SHARE>(p);
   const __nv_bfloat16* y = (const __nv_bfloat16*)p.y;
   m.a_whole = m.b_whole = m.a_step = 0;
   if (KIND == kDweight) {
@@ -662,7 +740,6 @@ cudaError_t launch(const Problem& p, cudaStream_t st) {
     for (int i = 0; i < 2; ++i)
       ok = ok && map_panels(&m.a[i], y, 1, rows, p.n, p.ld_y, 0, 128 >> i) && map_panels(&m.b[i], p.x, 1, rows, p.k, p.ld_x, 0, 128 >> i) &&
            (!GATED || map_panels(&m.a_up[i], y + p.n, 1, rows, p.n, p.ld_y, 0, 128 >> i));
-    most = (int64_t)p.groups.G * (GATED ? 2 : 1) * FT * ((p.k + BN - 1) / BN);
   } else if (KIND == kForward) {
     const int box = GATED ? kTileM / 2 : kTileM;
     ok = map_weights(&m.a[0], p.w, p, box, &m.a_whole, &m.a_step) && (!GATED || map_weights(&m.a_up[0], p.w_up, p, box, &m.a_whole, &m.a_step)) &&
@@ -674,28 +751,37 @@ cudaError_t launch(const Problem& p, cudaStream_t st) {
     ok = ok && map_boxes(m.b, y, rows, p.n, p.ld_y, C::kRowBox) && (!GATED || map_boxes(m.b_up, y + p.n, rows, p.n, p.ld_y, C::kRowBox));
   }
   if (!ok || most > 0x7fffffffll) return cudaErrorInvalidValue;
+  int ctas = C::kCtas;
+  if (SHARE == kSplit) ctas = split_of(p, KIND, most, BN, sms);
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = C::kCtas, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  attr.val.clusterDim.x = ctas, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = sms, cfg.blockDim = C::kThreads, cfg.dynamicSmemBytes = C::kSmemBytes, cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
+  cfg.gridDim = sms / ctas * ctas, cfg.blockDim = C::kThreads, cfg.dynamicSmemBytes = C::kSmemBytes, cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
   int64_t units = sms;
-  if (PAIR) {
+  if (SHARE == kPair) {
     if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
-    cfg.gridDim = sms / 2 * 2;
     if (!pairs[dev] && (e = cudaOccupancyMaxActiveClusters(&pairs[dev], kernel, &cfg)) != cudaSuccess) return e;
     units = pairs[dev] > 0 ? pairs[dev] : 1;
   }
-  cfg.gridDim = (unsigned)((most < units ? most : units) * C::kCtas);
+  // several CTAs on a reduction: a cluster per tile
+  cfg.gridDim = (unsigned)((SHARE == kSplit || most < units ? most : units) * ctas);
   return cudaLaunchKernelEx(&cfg, kernel, m, p);
 }
 
+// Rows per tile by the rows that a group has on average.  Where all tiles together leave half of the SMs idle, up to four CTAs share a tile's reduction (16 rows
+// x 14336 x 4096, 32 tiles: 70 us alone, 29 shared); a pair of CTAs wants more rows than one (below 96 its tiles would be mostly empty).
 template <int KIND, bool GATED>
-cudaError_t launch_rows(const Problem& p, cudaStream_t st) {
+cudaError_t launch_rows(const Problem& p, int sms, cudaStream_t st) {
   const int64_t each = p.L * p.groups.R / p.groups.G;
-  if (each <= 24) return launch<KIND, GATED, 32, false>(p, st);
-  if (each <= 96) return launch<KIND, GATED, 128, false>(p, st);
-  return launch<KIND, GATED, 256, true>(p, st);
+  if (each <= 32 && split_of(p, KIND, most_tiles<KIND, GATED, 32, kSplit>(p), 32, sms) > 1) return launch<KIND, GATED, 32, kSplit>(p, st);
+  if (each > 32 && each <= 64 && split_of(p, KIND, most_tiles<KIND, GATED, 64, kSplit>(p), 64, sms) > 1)
+    return launch<KIND, GATED, 64, kSplit>(p, st);
+  if (each > 64 && each <= 256 && split_of(p, KIND, most_tiles<KIND, GATED, 128, kSplit>(p), 128, sms) > 1)
+    return launch<KIND, GATED, 128, kSplit>(p, st);
+  if (each <= 24) return launch<KIND, GATED, 32, kAlone>(p, st);
+  if (each <= 96) return launch<KIND, GATED, 128, kAlone>(p, st);
+  return launch<KIND, GATED, 256, kPair>(p, st);
 }
 
 bool tma_rows(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
@@ -711,9 +797,12 @@ bool tensor_applicable(Kind kind, const Problem& p, int32_t dtype) {
 }
 
 cudaError_t run_tensor(Kind kind, const Problem& p, cudaStream_t st) {
-  if (kind == kForward) return p.gated ? launch_rows<kForward, true>(p, st) : launch_rows<kForward, false>(p, st);
-  if (kind == kBackward) return p.gated ? launch_rows<kBackward, true>(p, st) : launch_rows<kBackward, false>(p, st);
-  return p.gated ? launch<kDweight, true, 256, true>(p, st) : launch<kDweight, false, 256, true>(p, st);
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return cudaErrorInvalidDevice;
+  if (kind == kForward) return p.gated ? launch_rows<kForward, true>(p, sms, st) : launch_rows<kForward, false>(p, sms, st);
+  if (kind == kBackward) return p.gated ? launch_rows<kBackward, true>(p, sms, st) : launch_rows<kBackward, false>(p, sms, st);
+  return p.gated ? launch<kDweight, true, 256, kPair>(p, st) : launch<kDweight, false, 256, kPair>(p, st);
 }
 
 }  // namespace linear

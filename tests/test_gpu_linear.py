@@ -150,7 +150,8 @@ def some_counts(L, E, R, g, full=True):
 # (L, E, R, n, k): the tensor path needs strides that are multiples of 8 and starts of 16 bytes; the others take any
 SHAPES = [(1, 1, 1, 1, 1), (1, 1, 1, 8, 8), (1, 4, 4, 64, 64), (1, 3, 40, 64, 128), (2, 5, 37, 72, 200), (1, 7, 300, 136, 264),
           (1, 2, 700, 320, 64), (1, 60, 64, 128, 256), (3, 4, 130, 40, 96), (1, 1, 517, 515, 259), (1, 6, 77, 33, 31),
-          (1, 4, 1100, 192, 512), (1, 300, 500, 16, 24), (1, 1, 257, 1000, 1002)]
+          (1, 4, 1100, 192, 512), (1, 300, 500, 16, 24), (1, 1, 257, 1000, 1002), (1, 1, 16, 264, 4096), (1, 2, 40, 136, 2048), (1, 1, 60, 192, 1024),
+          (1, 1, 3, 100, 2056), (2, 3, 5, 72, 520), (1, 2, 600, 520, 192), (1, 1, 30, 4096, 264), (1, 3, 65, 2048, 136)]
 
 
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
