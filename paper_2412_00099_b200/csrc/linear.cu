@@ -9,24 +9,97 @@ namespace linear {
 namespace {
 
 // ---- products of any shape -----------------------------------------------------------------------------------
-// Tiles of TI x 64 results (TI 64, or 32 where 64 would leave SMs without a tile), 16 products deep, 4 x 4 results per thread, in fp32.  The
-// next step's operands are on their way to registers while this one's are multiplied (without that every step waited for memory: 900 x 1002 x 515 fp32
-// 95 us).  The results go through shared memory so that a warp ends up with 32 neighbouring columns of a row.
-constexpr int kTile = 64, kDeep = 16, kPad = kTile + 4;
+// fp32 sums on the fp32 pipe: tiles of 32 x 64, 4 x 4 results per thread, 16 products deep per step.  An operand lies in shared memory as it lies in memory: with
+// the reduction along its rows ([row][16], read four products at a time) or across them ([16][row], read four rows at a time); either way 8 16-byte loads
+// feed 32 packed multiply-adds.  fp32 operands of the next three steps are on their way by cp.async, 16, 8 or 4 bytes at a time as the alignment allows; bf16
+// elements of the next step in registers.  The results go through shared memory so that a warp ends up with 32 neighbouring columns of a row.
+// 30 to 36 TFLOP/s (16 groups of 256 rows x 2048 x 512 fp32: 283 us; its gradients 262 and 240), bound by the loads from shared memory and the
+// instructions around them; 64 x 64 and 128 x 128 tiles with 8 x 8 results per thread left more SMs idle than they saved (340 and 490 us).
+// 900 x 1002 x 515 (two elements per copy): 69 us, one step behind the other 95.
+constexpr int kDeep = 16;
 
-template <Kind KIND, typename T, bool GATED, int TI>
-__global__ void __launch_bounds__(TI * 4) general_kernel(const Problem p) {
-  constexpr int kSets = KIND == kForward && GATED ? 2 : 1;   // sums per result: a gated forward pass has two
+template <Kind KIND, typename T, bool GATED>
+struct General {
+  static constexpr int kSets = KIND == kForward && GATED ? 2 : 1;   // sums per result: a gated forward pass has two
+  static constexpr int kThreads = 128, TI = 32, TJ = 64;
+  static constexpr int kLanesJ = 16, kLanesI = kThreads / kLanesJ, RI = TI / kLanesI, RJ = TJ / kLanesJ;   // results of a thread
+  static constexpr bool kAlongA = KIND != kDweight, kAlongB = KIND == kForward;    // reduction along the operand's rows
+  static constexpr int kStrideA = kAlongA ? kDeep + 4 : TI + 4, kStrideB = kAlongB ? kDeep + 4 : TJ + 4;
+  static constexpr int kFloatsA = kAlongA ? TI * kStrideA : kDeep * kStrideA, kFloatsB = kAlongB ? TJ * kStrideB : kDeep * kStrideB;
+  static constexpr int kBuffer = kFloatsA + kSets * kFloatsB, kBuffers = sizeof(T) == 4 ? 4 : 2, kPad = TJ + 4;
+  static constexpr int kFloats = kSets * TI * kPad > kBuffers * kBuffer ? kSets * TI * kPad : kBuffers * kBuffer;
+  // row (column) i of a thread: every kLanesI-th (kLanesJ-th) along, four neighbours at a time across
+  static __device__ __forceinline__ int row(int ty, int i) { return kAlongA ? ty + kLanesI * i : 4 * ty + 4 * kLanesI * (i / 4) + i % 4; }
+  static __device__ __forceinline__ int col(int tx, int j) { return kAlongB ? tx + kLanesJ * j : 4 * tx + 4 * kLanesJ * (j / 4) + j % 4; }
+};
+
+__device__ __forceinline__ float2 fma_2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(*(uint64_t*)&r) : "l"(*(const uint64_t*)&a), "l"(*(const uint64_t*)&b), "l"(*(const uint64_t*)&c));
+  return r;
+}
+// `count` floats (0 .. V) from memory, zeros behind them.
+template <int V>
+__device__ __forceinline__ void copy_floats(float* to, const float* from, int count) {
+  if (V == 4) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_u32(to)), "l"(from), "r"(4 * count) : "memory");
+  else if (V == 2) asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(tc::smem_u32(to)), "l"(from), "r"(4 * count) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(tc::smem_u32(to)), "l"(from), "r"(4 * count) : "memory");
+}
+
+// One thread's units (V elements each) of an operand's steps: ROWS of it, the reduction along (ALONG) or across its rows.  Its units have one column and
+// every kRows-th row of the buffer, so that an address is an addition.
+template <typename T, int ROWS, bool ALONG, int STRIDE, int THREADS, int V>
+struct Part {
+  static constexpr int kAcross = (ALONG ? kDeep : ROWS) / V, kRows = THREADS / kAcross, kEach = (ALONG ? ROWS : kDeep) / kRows;
+  static_assert(THREADS % kAcross == 0 && kEach * kRows == (ALONG ? ROWS : kDeep), "whole units");
+  const T* from;         // first unit of the next step
+  int64_t ld, step;
+  int r, c, rows;        // row and column of the first unit; rows (along) or columns (across) that exist
+  // base: first row (along) or first of the reduction (across) of the tile, first column
+  __device__ __forceinline__ Part(const T* base, int64_t ld_, int rows_) : ld(ld_), step(ALONG ? kDeep : kDeep * ld_), rows(rows_) {
+    r = threadIdx.x / kAcross, c = threadIdx.x % kAcross * V;
+    from = base + r * ld + c;
+  }
+  // elements of unit i that exist, `left` of the reduction being left
+  __device__ __forceinline__ int count(int i, int left) const {
+    const int a = ALONG ? left - c : rows - c, n = a < 0 ? 0 : a < V ? a : V;
+    return r + i * kRows < (ALONG ? rows : left) ? n : 0;
+  }
+  __device__ __forceinline__ void copy(float* buffer, int left, const T* any) {
+    float* to = buffer + r * STRIDE + c;
+    const T* p = from;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i, p += kRows * ld) {
+      const int n = count(i, left);
+      copy_floats<V>(to + i * kRows * STRIDE, n ? p : any, n);
+    }
+    from += step;
+  }
+  __device__ __forceinline__ void fetch(float (&v)[kEach], int left) {
+    const T* p = from;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i, p += kRows * ld) v[i] = count(i, left) ? load_as_float(p) : 0.f;
+    from += step;
+  }
+  __device__ __forceinline__ void put(float* buffer, const float (&v)[kEach]) const {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) buffer[(r + i * kRows) * STRIDE + c] = v[i];
+  }
+};
+
+template <Kind KIND, typename T, bool GATED, int V>
+__global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads) general_kernel(const Problem p) {
+  typedef General<KIND, T, GATED> C;
+  constexpr int kSets = C::kSets, kThreads = C::kThreads, TI = C::TI, TJ = C::TJ, kPad = C::kPad;
   extern __shared__ __align__(16) float smem[];
-  constexpr int kThreads = TI * 4, kBuffer = (1 + kSets) * kDeep * kPad;
-  float* Cs = smem;                          // [kSets][TI][kPad], after the products; before: two buffers of [kDeep][kPad] of either operand
-  constexpr int kFloats = kSets * TI * kPad > 2 * kBuffer ? kSets * TI * kPad : 2 * kBuffer;
-  int* before = (int*)(smem + kFloats);
+  after_previous();
+  float* Cs = smem;   // [kSets][TI][kPad], after the products
+  int* before = (int*)(smem + C::kFloats);
   int* scratch = before + p.groups.G + 1;
-  const int t = threadIdx.x, tx = t % 16, ty = t / 16;
+  const int t = threadIdx.x, tx = t % C::kLanesJ, ty = t / C::kLanesJ;
 
   const int cols = KIND == kForward ? p.n : p.k;
-  const int JT = (cols + kTile - 1) / kTile;
+  const int JT = (cols + TJ - 1) / TJ;
   int64_t items;
   const int IT = (p.n + TI - 1) / TI;               // kDweight: tiles of dout's columns
   constexpr int kHalves = KIND == kDweight && GATED ? 2 : 1;
@@ -37,7 +110,7 @@ __global__ void __launch_bounds__(TI * 4) general_kernel(const Problem p) {
     items = (int64_t)before[p.groups.G] * JT;
   }
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    int g, i0, j0 = (int)(item % JT) * kTile, half = 0;
+    int g, i0, j0 = (int)(item % JT) * TJ, half = 0;
     if (KIND == kDweight) {
       int64_t r = item / JT;
       i0 = (int)(r % IT) * TI, r /= IT;
@@ -50,91 +123,108 @@ __global__ void __launch_bounds__(TI * 4) general_kernel(const Problem p) {
     const GroupRows gr = group_rows(p.groups, g);
     const int64_t row0 = gr.first + (KIND == kDweight ? 0 : i0);
     const int I = KIND == kDweight ? min(TI, p.n - i0) : (int)min((int64_t)TI, gr.m - i0);
-    const int J = min(kTile, cols - j0);
+    const int J = min(TJ, cols - j0);
     const int64_t red = KIND == kForward ? p.k : KIND == kBackward ? p.n : gr.m;
-    constexpr int kHalvesRed = KIND == kBackward && GATED ? 2 : 1;
-    const int64_t steps = (red + kDeep - 1) / kDeep, all = steps * kHalvesRed;
-    float c[kSets][4][4] = {};
-    // this thread's elements of a step, as fp32
-    constexpr int kA = TI * kDeep / kThreads, kB = kTile * kDeep / kThreads;
-    float ra[kA], rb[kSets][kB];
-    auto fetch = [&](int64_t step) {
-      const int part = step >= steps ? 1 : 0;
-      const int64_t d0 = (step - part * steps) * kDeep;
-      // operand with the reduction along its rows: 16 neighbours of a row; across them: neighbours of a row of the operand
-      if (KIND == kDweight) {
+    const int64_t steps = (red + kDeep - 1) / kDeep;
+    // Sums in pairs for the packed multiply-add: of the even and the odd products where both operands lie along, else of two neighbouring columns
+    constexpr bool kByProduct = C::kAlongA && C::kAlongB;
+    constexpr int kPairs = kByProduct ? C::RJ : C::RJ / 2;
+    float2 c[kSets][C::RI][kPairs] = {};
+    auto multiply = [&](const float* A) {
+      const float* B = A + C::kFloatsA;
 #pragma unroll
-        for (int i = 0; i < kA; ++i) {
-          const int d = t / TI + kThreads / TI * i, m = t % TI;
-          ra[i] = d0 + d < red && m < I ? load_as_float((const T*)p.y + (gr.first + d0 + d) * p.ld_y + half * p.n + i0 + m) : 0.f;
+      for (int d = 0; d < kDeep; d += 4) {
+        float a[C::RI][4];   // [row][product]
+#pragma unroll
+        for (int i = 0; i < C::RI; ++i) {
+          const float4 v = *(const float4*)(C::kAlongA ? A + C::row(ty, i) * C::kStrideA + d : A + (d + i) * C::kStrideA + C::row(ty, 0));
+          if (C::kAlongA) a[i][0] = v.x, a[i][1] = v.y, a[i][2] = v.z, a[i][3] = v.w;
+          else a[0][i] = v.x, a[1][i] = v.y, a[2][i] = v.z, a[3][i] = v.w;
         }
+#pragma unroll
+        for (int s = 0; s < kSets; ++s)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {   // along: column q; across: product d + q
+            const float4 b = *(const float4*)(B + s * C::kFloatsB + (C::kAlongB ? C::col(tx, q) * C::kStrideB + d : (d + q) * C::kStrideB + C::col(tx, 0)));
+#pragma unroll
+            for (int i = 0; i < C::RI; ++i) {
+              if (kByProduct) {
+                c[s][i][q] = fma_2(make_float2(a[i][0], a[i][1]), make_float2(b.x, b.y), c[s][i][q]);
+                c[s][i][q] = fma_2(make_float2(a[i][2], a[i][3]), make_float2(b.z, b.w), c[s][i][q]);
+              } else {
+                const float2 twice = make_float2(a[i][q], a[i][q]);
+                c[s][i][0] = fma_2(twice, make_float2(b.x, b.y), c[s][i][0]);
+                c[s][i][1] = fma_2(twice, make_float2(b.z, b.w), c[s][i][1]);
+              }
+            }
+          }
+      }
+    };
+    for (int part = 0; part < (KIND == kBackward && GATED ? 2 : 1); ++part) {
+      const T *base_a, *base_b, *base_b2 = nullptr;
+      int64_t ld_a, ld_b;
+      if (KIND == kForward) {
+        base_a = (const T*)p.x + row0 * p.ld_x, ld_a = p.ld_x;
+        const int64_t at = g * p.step_w + (int64_t)j0 * p.ld_w;
+        base_b = (const T*)p.w + at, ld_b = p.ld_w;
+        if (kSets == 2) base_b2 = (const T*)p.w_up + at;
+      } else if (KIND == kBackward) {
+        base_a = (const T*)p.y + row0 * p.ld_y + (int64_t)part * p.n, ld_a = p.ld_y;
+        base_b = (const T*)(part ? p.w_up : p.w) + g * p.step_w + j0, ld_b = p.ld_w;
       } else {
-#pragma unroll
-        for (int i = 0; i < kA; ++i) {
-          const int d = t % kDeep, m = t / kDeep + kThreads / kDeep * i;
-          const T* a = KIND == kForward ? (const T*)p.x + (row0 + m) * p.ld_x : (const T*)p.y + (row0 + m) * p.ld_y + (int64_t)part * p.n;
-          ra[i] = d0 + d < red && m < I ? load_as_float(a + d0 + d) : 0.f;
+        base_a = (const T*)p.y + gr.first * p.ld_y + (int64_t)half * p.n + i0, ld_a = p.ld_y;
+        base_b = (const T*)p.x + gr.first * p.ld_x + j0, ld_b = p.ld_x;
+      }
+      Part<T, TI, C::kAlongA, C::kStrideA, kThreads, V> pa(base_a, ld_a, I);
+      typedef Part<T, TJ, C::kAlongB, C::kStrideB, kThreads, V> PartB;
+      auto left_of = [&](int64_t step) { return (int)min(red - step * kDeep, (int64_t)kDeep); };
+      PartB pb(base_b, ld_b, J), pb2(kSets == 2 ? base_b2 : base_b, ld_b, J);
+      if constexpr (sizeof(T) == 4) {
+        auto ask = [&](int64_t step) {
+          if (step < steps) {
+            float* buffer = smem + step % C::kBuffers * C::kBuffer;
+            pa.copy(buffer, left_of(step), base_a), pb.copy(buffer + C::kFloatsA, left_of(step), base_a);
+            if (kSets == 2) pb2.copy(buffer + C::kFloatsA + C::kFloatsB, left_of(step), base_a);
+          }
+          asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        for (int i = 0; i < C::kBuffers - 1; ++i) ask(i);
+        for (int64_t step = 0; step < steps; ++step) {
+          asm volatile("cp.async.wait_group %0;" ::"n"(C::kBuffers - 2) : "memory");
+          __syncthreads();   // everybody's copies of this step are there, and nobody reads the buffer that the next copies go to
+          ask(step + C::kBuffers - 1);
+          multiply(smem + step % C::kBuffers * C::kBuffer);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();
+      } else {
+        float ra[decltype(pa)::kEach], rb[kSets][PartB::kEach];
+        auto fetch = [&](int64_t step) {
+          pa.fetch(ra, left_of(step)), pb.fetch(rb[0], left_of(step));
+          if (kSets == 2) pb2.fetch(rb[kSets - 1], left_of(step));
+        };
+        auto put = [&](int64_t step) {
+          float* buffer = smem + step % C::kBuffers * C::kBuffer;
+          pa.put(buffer, ra), pb.put(buffer + C::kFloatsA, rb[0]);
+          if (kSets == 2) pb2.put(buffer + C::kFloatsA + C::kFloatsB, rb[kSets - 1]);
+        };
+        if (steps) fetch(0), put(0);
+        __syncthreads();
+        for (int64_t step = 0; step < steps; ++step) {
+          if (step + 1 < steps) fetch(step + 1);
+          multiply(smem + step % C::kBuffers * C::kBuffer);
+          if (step + 1 < steps) put(step + 1);
+          __syncthreads();
         }
       }
-#pragma unroll
-      for (int i = 0; i < kB; ++i) {
-        if (KIND == kForward) {
-          const int d = t % kDeep, m = t / kDeep + kThreads / kDeep * i;
-          const bool in = d0 + d < red && m < J;
-          const int64_t at = g * p.step_w + (int64_t)(j0 + m) * p.ld_w + d0 + d;
-          rb[0][i] = in ? load_as_float((const T*)p.w + at) : 0.f;
-          if (kSets == 2) rb[kSets - 1][i] = in ? load_as_float((const T*)p.w_up + at) : 0.f;
-        } else {
-          const int d = t / kTile + kThreads / kTile * i, m = t % kTile;
-          const bool in = d0 + d < red && m < J;
-          if (KIND == kDweight) rb[0][i] = in ? load_as_float((const T*)p.x + (gr.first + d0 + d) * p.ld_x + j0 + m) : 0.f;
-          else rb[0][i] = in ? load_as_float((const T*)(part ? p.w_up : p.w) + g * p.step_w + (d0 + d) * p.ld_w + j0 + m) : 0.f;
-        }
-      }
-    };
-    auto put = [&](float* buffer) {
-#pragma unroll
-      for (int i = 0; i < kA; ++i) {
-        if (KIND == kDweight) buffer[(t / TI + kThreads / TI * i) * kPad + t % TI] = ra[i];
-        else buffer[(t % kDeep) * kPad + t / kDeep + kThreads / kDeep * i] = ra[i];
-      }
-#pragma unroll
-      for (int s = 0; s < kSets; ++s)
-#pragma unroll
-        for (int i = 0; i < kB; ++i) {
-          float* b = buffer + (1 + s) * kDeep * kPad;
-          if (KIND == kForward) b[(t % kDeep) * kPad + t / kDeep + kThreads / kDeep * i] = rb[s][i];
-          else b[(t / kTile + kThreads / kTile * i) * kPad + t % kTile] = rb[s][i];
-        }
-    };
-    if (all) fetch(0), put(smem);
-    __syncthreads();
-    for (int64_t step = 0; step < all; ++step) {
-      const float* buffer = smem + (step & 1) * kBuffer;
-      if (step + 1 < all) fetch(step + 1);
-#pragma unroll
-      for (int d = 0; d < kDeep; ++d) {
-        const float4 a = *(const float4*)(buffer + d * kPad + 4 * ty);
-        const float av[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int s = 0; s < kSets; ++s) {
-          const float4 b = *(const float4*)(buffer + ((1 + s) * kDeep + d) * kPad + 4 * tx);
-          const float bv[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) c[s][i][j] = fmaf(av[i], bv[j], c[s][i][j]);
-        }
-      }
-      if (step + 1 < all) put(smem + ((step + 1) & 1) * kBuffer);
-      __syncthreads();
     }
 #pragma unroll
     for (int s = 0; s < kSets; ++s)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < C::RI; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) Cs[(s * TI + 4 * ty + i) * kPad + 4 * tx + j] = c[s][i][j];
+        for (int j = 0; j < C::RJ; ++j)
+          Cs[(s * TI + C::row(ty, i)) * kPad + C::col(tx, j)] = kByProduct ? c[s][i][j].x + c[s][i][j].y : j & 1 ? c[s][i][j / 2].y : c[s][i][j / 2].x;
     __syncthreads();
     const int warp = t / 32, lane = t % 32;
     for (int jj = 0; jj < J; jj += 32) {
@@ -155,21 +245,24 @@ __global__ void __launch_bounds__(TI * 4) general_kernel(const Problem p) {
           }
         }
       } else {
-        const int i = warp * 8 + lane / 4, j = jj + 8 * (lane % 4);
-        float z[1][8], up[1][8] = {};
+        const int j = jj + 8 * (lane % 4);
+        for (int i0w = warp * 8; i0w < I; i0w += kThreads / 4) {
+          const int i = i0w + lane / 4;
+          float z[1][8], up[1][8] = {};
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          z[0][u] = Cs[i * kPad + j + u];
-          if (kSets == 2) up[0][u] = Cs[(TI + i) * kPad + j + u];
-        }
-        if constexpr (KIND == kForward) {
-          const Forward<T, GATED> e(p.fwd, g, j0 + j);
-          e.rows(row0 + warp * 8, I - warp * 8, z, up);
-        } else {
-          const Backward<T> e(p.bwd, g, j0 + j);
-          typename Backward<T>::template Asked<1> q;
-          e.ask(row0 + warp * 8, I - warp * 8, q);
-          e.rows(row0 + warp * 8, I - warp * 8, z, q);
+          for (int u = 0; u < 8; ++u) {
+            z[0][u] = Cs[i * kPad + j + u];
+            if (kSets == 2) up[0][u] = Cs[(TI + i) * kPad + j + u];
+          }
+          if constexpr (KIND == kForward) {
+            const Forward<T, GATED> e(p.fwd, g, j0 + j);
+            e.rows(row0 + i0w, I - i0w, z, up);
+          } else {
+            const Backward<T> e(p.bwd, g, j0 + j);
+            typename Backward<T>::template Asked<1> q;
+            e.ask(row0 + i0w, I - i0w, q);
+            e.rows(row0 + i0w, I - i0w, z, q);
+          }
         }
       }
     }
@@ -177,30 +270,41 @@ __global__ void __launch_bounds__(TI * 4) general_kernel(const Problem p) {
   }
 }
 
-template <Kind KIND, typename T, bool GATED, int TI>
+template <Kind KIND, typename T, bool GATED, int V>
 cudaError_t launch_tiles(const Problem& p, int64_t tiles, int sms, cudaStream_t st) {
   static int cache[64] = {0};
-  constexpr int kSets = KIND == kForward && GATED ? 2 : 1;
-  constexpr size_t kFloats = kSets * TI * kPad > 2 * (1 + kSets) * kDeep * kPad ? kSets * TI * kPad : 2 * (1 + kSets) * kDeep * kPad;
-  const cudaError_t e =
-      tc::sm_count_and_smem_optin(general_kernel<KIND, T, GATED, TI>, kFloats * 4 + (MCCE_LINEAR_MAX_GROUPS + 1 + 33) * 4, cache, &sms);
+  constexpr size_t kBytes = General<KIND, T, GATED>::kFloats * 4;
+  const cudaError_t e = tc::sm_count_and_smem_optin(general_kernel<KIND, T, GATED, V>, kBytes + (MCCE_LINEAR_MAX_GROUPS + 1 + 33) * 4, cache, &sms);
   if (e != cudaSuccess) return e;
-  const int64_t most = (TI == 64 ? 6 : 12) * sms;
-  general_kernel<KIND, T, GATED, TI>
-      <<<(unsigned)(tiles < most ? tiles : most), TI * 4, kFloats * 4 + (size_t)(p.groups.G + 1 + 33) * 4, st>>>(p);
-  return cudaGetLastError();
+  const int64_t most = 8 * sms;
+  return launch_close(general_kernel<KIND, T, GATED, V>, dim3((unsigned)(tiles < most ? tiles : most)), General<KIND, T, GATED>::kThreads,
+                      kBytes + (size_t)(p.groups.G + 1 + 33) * 4, st, p);
 }
-template <Kind KIND, typename T, bool GATED>
+template <Kind KIND, typename T, bool GATED, int V>
 cudaError_t launch_general(const Problem& p, cudaStream_t st) {
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return cudaErrorInvalidDevice;
-  const int64_t jt = ((KIND == kForward ? p.n : p.k) + kTile - 1) / kTile;
-  auto tiles = [&](int ti) {
-    return KIND == kDweight ? (int64_t)p.groups.G * (GATED ? 2 : 1) * ((p.n + ti - 1) / ti) * jt : (p.L * p.groups.R / ti + p.groups.G) * jt;
+  typedef General<KIND, T, GATED> C;
+  const int64_t jt = ((KIND == kForward ? p.n : p.k) + C::TJ - 1) / C::TJ;
+  const int64_t tiles =
+      KIND == kDweight ? (int64_t)p.groups.G * (GATED ? 2 : 1) * ((p.n + C::TI - 1) / C::TI) * jt : (p.L * p.groups.R / C::TI + p.groups.G) * jt;
+  return launch_tiles<KIND, T, GATED, V>(p, tiles, sms, st);
+}
+template <Kind KIND, typename T, int V>
+cudaError_t launch_general_gated(const Problem& p, cudaStream_t st) {
+  return p.gated ? launch_general<KIND, T, true, V>(p, st) : launch_general<KIND, T, false, V>(p, st);
+}
+template <Kind KIND>
+cudaError_t launch_general_types(const Problem& p, int32_t dtype, cudaStream_t st) {
+  if (dtype == MCCE_BF16) return launch_general_gated<KIND, __nv_bfloat16, 1>(p, st);
+  auto aligned_to = [&](int v) {   // v columns of what this product reads: x and the weights, dout and the weights, dout and x
+    auto one = [&](const void* a, int64_t ld) { return !a || (((uintptr_t)a | (uintptr_t)(ld * 4)) & (4 * v - 1)) == 0; };
+    return (KIND == kBackward || one(p.x, p.ld_x)) && (KIND == kForward || (one(p.y, p.ld_y) && (!p.gated || p.n % v == 0))) &&
+           (KIND == kDweight || (one(p.w, p.ld_w) && one(p.w_up, p.ld_w) && (p.groups.G == 1 || p.step_w % v == 0)));
   };
-  if (tiles(64) < 4 * sms) return launch_tiles<KIND, T, GATED, 32>(p, tiles(32), sms, st);
-  return launch_tiles<KIND, T, GATED, 64>(p, tiles(64), sms, st);
+  if (aligned_to(4)) return launch_general_gated<KIND, float, 4>(p, st);
+  return aligned_to(2) ? launch_general_gated<KIND, float, 2>(p, st) : launch_general_gated<KIND, float, 1>(p, st);
 }
 
 // ---- sums of dout's columns per group (the bias's gradient) ----------------------------------------------------
@@ -224,6 +328,7 @@ __device__ __forceinline__ void bias_store(const BiasArgs& a, int half, int64_t 
 template <typename T>
 __global__ void __launch_bounds__(256) bias_kernel(const BiasArgs a) {
   __shared__ float part[8][256 + 8];
+  after_previous();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = blockIdx.y, half = blockIdx.z % (a.gated + 1), chunk = blockIdx.z / (a.gated + 1);
   const int j = blockIdx.x * 256 + 8 * lane, count = min(max(a.n - j, 0), 8);
   const GroupRows gr = group_rows(a.groups, g);
@@ -261,6 +366,7 @@ __global__ void __launch_bounds__(256) bias_kernel(const BiasArgs a) {
 template <typename T>
 __global__ void __launch_bounds__(256) bias_parts_kernel(const BiasArgs a) {
   const int64_t at = blockIdx.x * 256ll + threadIdx.x, all = (int64_t)a.groups.G * a.n;
+  after_previous();
   if (at >= all) return;
   float v = 0.f;
   for (int c = 0; c < a.chunks; ++c) v += a.parts[(int64_t)(c * (a.gated + 1) + blockIdx.y) * all + at];
@@ -274,6 +380,7 @@ template <typename T, int U>
 __global__ void __launch_bounds__(256) pack_kernel(const T* x, uint8_t* q, uint8_t* scales, int64_t blocks, int per_row, int d, int64_t ld_x,
                                                    int64_t ld_q) {
   const int64_t first = (int64_t)blockIdx.x * (64 * U) + threadIdx.x / 4;
+  after_previous();
   uint32_t raw[U][2 * sizeof(T)];
   int count[U], col[U];
   int64_t row[U];
@@ -302,6 +409,7 @@ template <typename T, int U>
 __global__ void __launch_bounds__(256) unpack_kernel(const uint8_t* q, const uint8_t* scales, T* x, int64_t blocks, int per_row, int d,
                                                      int64_t ld_x, int64_t ld_q) {
   const int64_t first = (int64_t)blockIdx.x * (64 * U) + threadIdx.x / 4;
+  after_previous();
   uint32_t w[U][2], s[U];
   int count[U], col[U];
   int64_t row[U];
@@ -328,6 +436,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) pack_odd_kernel(const T* x, uint8_t* q, uint8_t* scales, int64_t rows, int per_row, int d, int64_t ld_x,
                                                        int64_t ld_q) {
   const int lane = threadIdx.x & 31, parts = (per_row + 7) / 8;
+  after_previous();
   const int64_t w = blockIdx.x * 8ll + (threadIdx.x >> 5), row = w / parts;
   if (row >= rows) return;
   const int b0 = (int)(w - row * parts) * 8;
@@ -347,6 +456,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) unpack_odd_kernel(const uint8_t* q, const uint8_t* scales, T* x, int64_t rows, int per_row, int d,
                                                          int64_t ld_x, int64_t ld_q) {
   const int lane = threadIdx.x & 31, parts = (per_row + 7) / 8;
+  after_previous();
   const int64_t w = blockIdx.x * 8ll + (threadIdx.x >> 5), row = w / parts;
   if (row >= rows) return;
   const int b0 = (int)(w - row * parts) * 8;
@@ -364,16 +474,8 @@ __global__ void __launch_bounds__(256) unpack_odd_kernel(const uint8_t* q, const
 }  // namespace
 
 cudaError_t run_general(Kind kind, const Problem& p, int32_t dtype, cudaStream_t st) {
-  const bool g = p.gated;
-  if (dtype == MCCE_F32) {
-    if (kind == kForward) return g ? launch_general<kForward, float, true>(p, st) : launch_general<kForward, float, false>(p, st);
-    if (kind == kBackward) return g ? launch_general<kBackward, float, true>(p, st) : launch_general<kBackward, float, false>(p, st);
-    return g ? launch_general<kDweight, float, true>(p, st) : launch_general<kDweight, float, false>(p, st);
-  }
-  typedef __nv_bfloat16 B;
-  if (kind == kForward) return g ? launch_general<kForward, B, true>(p, st) : launch_general<kForward, B, false>(p, st);
-  if (kind == kBackward) return g ? launch_general<kBackward, B, true>(p, st) : launch_general<kBackward, B, false>(p, st);
-  return g ? launch_general<kDweight, B, true>(p, st) : launch_general<kDweight, B, false>(p, st);
+  if (kind == kForward) return launch_general_types<kForward>(p, dtype, st);
+  return kind == kBackward ? launch_general_types<kBackward>(p, dtype, st) : launch_general_types<kDweight>(p, dtype, st);
 }
 
 namespace {
@@ -394,13 +496,11 @@ cudaError_t run_bias_sums(const Problem& p, int32_t dtype, const void* add, cons
   const bool wide = wide_rows(p.y, p.ld_y, e) && (!p.gated || p.n * e % 16 == 0);
   const BiasArgs a{p.groups, p.n, p.gated, p.dw_f32, wide, chunks, p.ld_y, p.y, add, add_up, db, db_up, chunks > 1 ? parts : nullptr};
   const dim3 grid((p.n + 255) / 256, p.groups.G, halves * chunks), all((unsigned)(((int64_t)p.groups.G * p.n + 255) / 256), halves);
-  if (dtype == MCCE_F32) bias_kernel<float><<<grid, 256, 0, st>>>(a);
-  else bias_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(a);
-  cudaError_t err = cudaGetLastError();
+  const cudaError_t err = dtype == MCCE_F32 ? launch_close(bias_kernel<float>, grid, 256, 0, st, a)
+                                            : launch_close(bias_kernel<__nv_bfloat16>, grid, 256, 0, st, a);
   if (err != cudaSuccess || chunks == 1) return err;
-  if (dtype == MCCE_F32) bias_parts_kernel<float><<<all, 256, 0, st>>>(a);
-  else bias_parts_kernel<__nv_bfloat16><<<all, 256, 0, st>>>(a);
-  return cudaGetLastError();
+  return dtype == MCCE_F32 ? launch_close(bias_parts_kernel<float>, all, 256, 0, st, a)
+                           : launch_close(bias_parts_kernel<__nv_bfloat16>, all, 256, 0, st, a);
 }
 
 namespace {
@@ -414,17 +514,14 @@ cudaError_t pack_as(bool pack, const void* x, void* to, const uint8_t* q_in, uin
   const bool many = blocks >= 148 * 8 * 64 * kU;   // else one block per lane: more CTAs
   const int64_t grid = !wide ? (rows * ((per_row + 7) / 8) + 7) / 8 : many ? (blocks + 64 * kU - 1) / (64 * kU) : (blocks + 63) / 64;
   if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
-  const unsigned n = (unsigned)grid;
+  const dim3 n((unsigned)grid);
   if (pack) {
-    if (!wide) pack_odd_kernel<T><<<n, 256, 0, st>>>((const T*)x, q, scales, rows, per_row, d, ld_x, ld_q);
-    else if (many) pack_kernel<T, kU><<<n, 256, 0, st>>>((const T*)x, q, scales, blocks, per_row, d, ld_x, ld_q);
-    else pack_kernel<T, 1><<<n, 256, 0, st>>>((const T*)x, q, scales, blocks, per_row, d, ld_x, ld_q);
-  } else {
-    if (!wide) unpack_odd_kernel<T><<<n, 256, 0, st>>>(q_in, s_in, (T*)to, rows, per_row, d, ld_x, ld_q);
-    else if (many) unpack_kernel<T, kU><<<n, 256, 0, st>>>(q_in, s_in, (T*)to, blocks, per_row, d, ld_x, ld_q);
-    else unpack_kernel<T, 1><<<n, 256, 0, st>>>(q_in, s_in, (T*)to, blocks, per_row, d, ld_x, ld_q);
+    const T* from = (const T*)x;
+    if (!wide) return launch_close(pack_odd_kernel<T>, n, 256, 0, st, from, q, scales, rows, per_row, d, ld_x, ld_q);
+    return launch_close(many ? pack_kernel<T, kU> : pack_kernel<T, 1>, n, 256, 0, st, from, q, scales, blocks, per_row, d, ld_x, ld_q);
   }
-  return cudaGetLastError();
+  if (!wide) return launch_close(unpack_odd_kernel<T>, n, 256, 0, st, q_in, s_in, (T*)to, rows, per_row, d, ld_x, ld_q);
+  return launch_close(many ? unpack_kernel<T, kU> : unpack_kernel<T, 1>, n, 256, 0, st, q_in, s_in, (T*)to, blocks, per_row, d, ld_x, ld_q);
 }
 }  // namespace
 

@@ -6,10 +6,27 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "mcce.h"
 
 namespace mcce {
 namespace linear {
+
+// Every kernel here is launched so that it may take its place while the kernel before it still runs, and waits for that one's memory before it touches any;
+// and lets the next one do so.  (A launch that does not ask for it is not affected.)
+__device__ __forceinline__ void after_previous() {
+  asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
+}
+template <typename... P>
+cudaError_t launch_close(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const std::decay_t<P>&... args) {
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid, cfg.blockDim = dim3(threads), cfg.dynamicSmemBytes = smem, cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
 
 enum Kind { kForward = 0, kBackward = 1, kDweight = 2 };
 

@@ -89,6 +89,7 @@ __device__ __forceinline__ void few_rows(const Problem& p, int g, int64_t row, i
 template <bool GATED, int M>
 __global__ void __launch_bounds__(256, M == 1 ? 3 : 2) few_kernel(const __grid_constant__ Problem p) {
   extern __shared__ int before[];
+  after_previous();
   count_tiles(p.groups, M, before, before + p.groups.G + 1);
   const int FT = GATED ? p.n : (p.n + 1) / 2;
   const int64_t items = (int64_t)before[p.groups.G] * FT;
@@ -109,8 +110,7 @@ template <bool GATED, int M>
 cudaError_t launch_few(const Problem& p, int sms, cudaStream_t st) {
   const int64_t rows = p.L * p.groups.R, tiles = rows < p.groups.G ? rows : rows / M + p.groups.G;
   const int64_t want = (tiles * (GATED ? p.n : (p.n + 1) / 2) + 7) / 8, most = (M == 1 ? 3 : 2) * sms;
-  few_kernel<GATED, M><<<(unsigned)(want < most ? want : most), 256, (size_t)(p.groups.G + 1 + 33) * 4, st>>>(p);
-  return cudaGetLastError();
+  return launch_close(few_kernel<GATED, M>, dim3((unsigned)(want < most ? want : most)), 256, (size_t)(p.groups.G + 1 + 33) * 4, st, p);
 }
 
 }  // namespace

@@ -375,6 +375,7 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
   }
   if (SHARE != kAlone) cluster_sync();
   if (warp == 1) take_tmem<PAIR>(smem_u32(tmem_slot), 2 * BN);
+  after_previous();
   if (KIND != kDweight) count_tiles(p.groups, BN, before, before + p.groups.G + 1);
   tc_fence_before();
   __syncthreads();
@@ -753,11 +754,13 @@ cudaError_t launch(const Problem& p, cudaStream_t st) {
   if (!ok || most > 0x7fffffffll) return cudaErrorInvalidValue;
   int ctas = C::kCtas;
   if (SHARE == kSplit) ctas = split_of(p, KIND, most, BN, sms);
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = ctas, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = ctas, attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = sms / ctas * ctas, cfg.blockDim = C::kThreads, cfg.dynamicSmemBytes = C::kSmemBytes, cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
+  cfg.gridDim = sms / ctas * ctas, cfg.blockDim = C::kThreads, cfg.dynamicSmemBytes = C::kSmemBytes, cfg.stream = st, cfg.attrs = attr, cfg.numAttrs = 2;
   int64_t units = sms;
   if (SHARE == kPair) {
     if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
