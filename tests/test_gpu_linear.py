@@ -335,3 +335,223 @@ def test_checkpoint_special_blocks():
         bad[0, :32] = bad[1, 32:64] = bad[2, 64:] = True
         assert back[bad].isnan().all() and back[~bad].isfinite().all()
         assert (back[0, 32:] == 1).all() and abs(float(back[3, 0]) / 3e38 - 1) <= 2.0 ** -4
+
+
+# ---- strides, places, streams, graphs --------------------------------------------------------------------------
+def padded(t, right, left=0, fill=9.0):
+    """The same values as columns of a wider buffer, and the buffer."""
+    full = torch.full(t.shape[:-1] + (left + t.shape[-1] + right,), fill, device="cuda").to(t.dtype)
+    view = full[..., left:left + t.shape[-1]]
+    view.copy_(t)
+    return view, full
+
+
+@pytest.mark.parametrize("T", [BF16, F32])
+@pytest.mark.parametrize("left,right", [(8, 24), (0, 8), (1, 2), (4, 4)])
+def test_strides(T, left, right):
+    """Every tensor another stride and start (aligned to what the copies want, or not): the results of contiguous ones, nothing beside them touched."""
+    g, R, n, k, E = gen(7), 210, 72, 136, 3
+    off = offsets_of([[100, 0, 90]])[0]
+    x, w, wu, add = normal(g, R, k, dtype=T), normal(g, E, n, k, dtype=T, std=0.1), normal(g, E, n, k, dtype=T, std=0.1), normal(g, R, n, dtype=T)
+    want = mb.expert_linear(x, off, w, w_up=wu, act="silu", add=add, save="same")
+    xs, ws, wus, adds = padded(x, right, left)[0], padded(w, right, left)[0], padded(wu, right, left)[0], padded(add, right + 1, left)[0]
+    out, full = padded(torch.zeros(R, n, device="cuda", dtype=T), right + 8, left)
+    saved, full_saved = padded(torch.zeros(R, 2 * n, device="cuda", dtype=T), right + 16, left)
+    r = mb.expert_linear(xs, off, ws, w_up=wus, act="silu", add=adds, out=mb.LinearOut(out, saved))
+    tol = (k + 16) * u * 10 * (1 if T == F32 else 0) + (2 * U(T) if T == BF16 else 0)      # other kernels, other orders of summation
+    close = lambda a, b: (a.double() - b.double()).abs().max() <= tol * b.double().abs().max()
+    assert close(r.out[:190], want.out[:190]) and close(r.saved[:190], want.saved[:190])
+    assert (full[:, :left] == 9).all() and (full[:, left + n:] == 9).all() and (full_saved[:, left + 2 * n:] == 9).all() and (out[190:] == 0).all()
+    # gradients: both matrices in one buffer, dx over the kept values, dw into columns of a wider buffer, added in place
+    both = torch.cat([w, wu], 1)
+    dout = normal(g, R, 2 * n, dtype=T)
+    z = normal(g, R, 2 * k, dtype=T)
+    ref = mb.expert_linear_backward(dout, off, w, w_up=wu, saved=z, act="gelu")
+    zs = padded(z, right, left)[0]
+    got = mb.expert_linear_backward(padded(dout, right, left)[0], off, both[:, :n], w_up=both[:, n:], saved=zs, act="gelu",
+                                    out=mb.LinearGrad(zs, torch.empty(R, k, device="cuda", dtype=T)))
+    assert close(got.dx[:190], ref.dx[:190]) and close(got.h[:190], ref.h[:190]) and torch.equal(zs[190:], z[190:])
+    dw = [padded(torch.ones(E, n, k, device="cuda", dtype=T), right, left) for _ in range(2)]
+    ref = mb.expert_linear_dweight(dout, x, off, gated=True)
+    into = mb.WeightGrad(dw[0][0], dw[1][0])
+    got = mb.expert_linear_dweight(padded(dout, right, left)[0], xs, off, gated=True, add=into, out=into)
+    for a, b, (_, whole) in zip(got[:2], ref[:2], dw):
+        assert close(a, b + 1) and (whole[..., :left] == 9).all() and (whole[..., left + k:] == 9).all()
+
+
+def test_rows_far_apart():
+    """Offsets beyond 2^32 elements: rows, weights and results with strides of 2^27 and more."""
+    g, R, n, k = gen(3), 36, 64, 64
+    big = torch.empty(R * (1 << 27) + 4096, device="cuda", dtype=BF16)
+    for T in (BF16, F32):
+        buf = big if T == BF16 else big.view(F32)
+        step = (1 << 27) if T == BF16 else (1 << 26)
+        x, w, dout = normal(g, R, k, dtype=T), normal(g, 1, n, k, dtype=T), normal(g, R, n, dtype=T)
+        off = offsets_of([[R]])[0]
+        place = lambda at, cols: torch.as_strided(buf, (R, cols), (step, 1), at)
+        xs, outs = place(0, k), place(1024, n)
+        xs.copy_(x)
+        want = mb.expert_linear(x, off, w).out
+        r = mb.expert_linear(xs, off, w, out=mb.LinearOut(outs))
+        assert torch.equal(r.out, want)
+        xs.copy_(x)
+        assert torch.equal(mb.expert_linear_dweight(dout, xs, off).dw, mb.expert_linear_dweight(dout, x, off).dw)
+        c = mb.checkpoint_pack(x)
+        assert torch.equal(mb.checkpoint_unpack(c.q, c.scales, out=outs), mb.checkpoint_unpack(c.q, c.scales, dtype=T))
+    ws = torch.as_strided(big, (R, 16, 64), (1 << 27, 64, 1))
+    ws.copy_(normal(g, R, 16, 64, dtype=BF16))
+    off = offsets_of([[1] * R])[0]
+    x = normal(g, R, 64, dtype=BF16)
+    assert torch.equal(mb.expert_linear(x, off, ws).out, mb.expert_linear(x, off, ws.contiguous()).out)
+
+
+@pytest.mark.parametrize("T", [BF16, F32])
+@pytest.mark.parametrize("R,E", [(7, 3), (300, 4), (900, 2)])
+def test_offsets_that_are_no_offsets(T, R, E):
+    """What reaches outside [0, R] is cut off, a group that ends before it begins is empty: nothing outside the rows is touched."""
+    g, n, k = gen(5), 72, 64
+    buf = torch.full((R + 200, n), 7.0, device="cuda", dtype=T)
+    x, w = normal(g, R, k, dtype=T), normal(g, E, n, k, dtype=T)
+    for o in ([-5] + [R // 2] * (E - 1) + [R + 100000], [2 ** 31 - 1] * (E + 1), [-2 ** 31] * E + [3], [R] + [0] * E):
+        off = torch.tensor(o, dtype=torch.int32, device="cuda")
+        mb.expert_linear(x, off, w, out=mb.LinearOut(buf[100:100 + R]))
+        mb.expert_linear_backward(buf[100:100 + R], off, w)
+        mb.expert_linear_dweight(buf[100:100 + R], x, off, want_db=True)
+        assert (buf[:100] == 7).all() and (buf[100 + R:] == 7).all()
+    mb.expert_linear_status()
+
+
+@pytest.mark.parametrize("T", [BF16, F32])
+def test_one_experts_nan_stays_its_own(T):
+    g, n, k, counts = gen(6), 136, 72, [37, 100, 0, 64, 300]
+    off, E, R = offsets_of([counts])[0], 5, 501
+    x, w, dout = normal(g, R, k, dtype=T), normal(g, E, n, k, dtype=T), normal(g, R, n, dtype=T)
+    x[40], dout[41], w[1, 3] = float("nan"), float("inf"), float("-inf")
+    bad = torch.zeros(R, dtype=torch.bool, device="cuda")
+    bad[37:137] = True
+    out = mb.expert_linear(x, off, w, act="silu").out
+    assert out[~bad].isfinite().all() and not out[40].isfinite().any()
+    dx = mb.expert_linear_backward(dout, off, w).dx
+    assert dx[~bad].isfinite().all()
+    r = mb.expert_linear_dweight(dout, x, off, want_db=True)
+    others = [0, 2, 3, 4]
+    assert r.dw[others].isfinite().all() and r.db[others].isfinite().all() and not r.dw[1].isfinite().all() and not r.db[1].isfinite().all()
+    assert (r.dw[2] == 0).all() and (r.db[2] == 0).all()
+
+
+def test_streams_and_graphs():
+    """On a stream of the caller's, captured and replayed on new values: the same bits as in order."""
+    g = gen(9)
+    L, E, R, n, k = 1, 6, 600, 192, 256
+    off = offsets_of(some_counts(L, E, R, g))
+    x, w, wu = normal(g, L, R, k, dtype=BF16), normal(g, L, E, n, k, dtype=BF16, std=0.1), normal(g, L, E, n, k, dtype=BF16, std=0.1)
+    wd, dy = normal(g, L, E, k, n, dtype=BF16, std=0.1), normal(g, L, R, k, dtype=BF16)
+    few = normal(g, 2, k, dtype=BF16)
+    off_few = offsets_of([[1, 0, 0, 1, 0, 0]])[0]
+
+    def step():
+        a = mb.expert_linear(x, off, w, w_up=wu, act="silu", save="e4m3")
+        y = mb.expert_linear(a.out, off, wd, add=x).out
+        d = mb.expert_linear_backward(dy, off, wd, saved=a.saved, scales=a.scales, act="silu")
+        dx = mb.expert_linear_backward(d.dx, off, w, w_up=wu, add=dy).dx
+        c = mb.checkpoint_pack(x)
+        dw = mb.expert_linear_dweight(d.dx, c.q, off, scales=c.scales, gated=True, want_db=True)
+        dwd = mb.expert_linear_dweight(dy, d.h, off)
+        return [a.out, y, d.dx, d.h, dx, *dw, dwd.dw, mb.expert_linear(few, off_few, w[0]).out]
+    side = torch.cuda.Stream()
+    want = step()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            got = step()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        held = step()
+    for seed in (1, 2):
+        x.copy_(normal(gen(seed), L, R, k, dtype=BF16))
+        off.copy_(offsets_of(some_counts(L, E, R, gen(seed))))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, step()))
+    mb.expert_linear_status()
+
+
+def test_two_calls_at_once():
+    """Two streams with calls that wait inside for their own copies: each one's own results."""
+    g = gen(10)
+    off = offsets_of([[700, 300, 500, 548]])[0]
+    data = [(normal(g, 2048, 512, dtype=BF16), normal(g, 4, 768, 512, dtype=BF16, std=0.05)) for _ in range(2)]
+    want = [mb.expert_linear(x, off, w, act="gelu").out for x, w in data]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(mb.expert_linear(data[i][0], off, data[i][1], act="gelu").out)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want[i]) for i in range(2) for o in got[i])
+    mb.expert_linear_status()
+
+
+# ---- a layer, forwards and backwards -----------------------------------------------------------------------------
+@pytest.mark.parametrize("T", [F32, BF16])
+@pytest.mark.parametrize("tokens,d,f", [(37, 64, 96), (150, 72, 40)])
+def test_layer_and_its_gradients(T, tokens, d, f):
+    """Norm, sort, gated experts, down projection with bias, weighted return onto the residual stream, and back to the gradients of everything; against the
+    formulas in 64 bits (their gradients by autograd, and by differences).  Every value on the way is a sum of at most 2 f products or of d terms: 8 stages
+    of (2 f + 8) u each, tenfold for cancellation, relative to the largest gradient of a tensor; in bf16 8 stages of a rounding each, tenfold too."""
+    E, K = 5, 2
+    g = gen(tokens)
+    x, wn = normal(g, tokens, d, dtype=T), 1 + 0.1 * normal(g, d)
+    wg, wu, wd = (normal(g, E, *s, dtype=T, std=s[1] ** -0.5) for s in ((f, d), (f, d), (d, f)))
+    bd = normal(g, E, d, std=0.1).to(T)
+    sel = torch.stack([torch.randperm(E, generator=g, device="cuda")[:K] for _ in range(tokens)]).to(torch.int32)
+    sel[3, 1] = -1                                        # a dropped pair
+    sw = torch.softmax(normal(g, tokens, K), -1)
+    dy = normal(g, tokens, d, dtype=T)
+
+    def ours():
+        h = mb.rmsnorm(x, wn, 1e-6).out
+        s = mb.dispatch(sel, E, h)
+        a = mb.expert_linear(s.rows, s.offsets, wg, w_up=wu, act="silu", save="same")
+        o = mb.expert_linear(a.out, s.offsets, wd, bias=bd).out
+        y = mb.combine(o, s.inv, sw, add=x)
+        do, dsw = mb.combine_backward(dy, o, s.inv, sw)
+        da = mb.expert_linear_backward(do, s.offsets, wd, saved=a.saved, act="silu")
+        gd = mb.expert_linear_dweight(do, da.h, s.offsets, want_db=True)
+        drows = mb.expert_linear_backward(da.dx, s.offsets, wg, w_up=wu).dx
+        gu = mb.expert_linear_dweight(da.dx, s.rows, s.offsets, gated=True)
+        dh = mb.combine(drows, s.inv)
+        dx, dwn = mb.rmsnorm_backward(dh, x, wn, 1e-6, dsum=dy)
+        return y, dict(x=dx, wn=dwn, wg=gu.dw, wu=gu.dw_up, wd=gd.dw, bd=gd.db, sw=dsw)
+    y, grads = ours()
+    leaves = {k: v.double().requires_grad_() for k, v in dict(x=x, wn=wn, wg=wg, wu=wu, wd=wd, bd=bd, sw=sw).items()}
+
+    def formula(v):
+        h = v["x"] / (v["x"].square().mean(-1, keepdim=True) + 1e-6).sqrt() * v["wn"]
+        out = v["x"]
+        for k in range(K):
+            e, on = sel[:, k].long().clamp_min(0), (sel[:, k] >= 0).double()
+            gate, up = torch.einsum("td,tfd->tf", h, v["wg"][e]), torch.einsum("td,tfd->tf", h, v["wu"][e])
+            r = torch.einsum("tf,tdf->td", act(gate, "silu") * up, v["wd"][e]) + v["bd"][e]
+            out = out + (v["sw"][:, k] * on)[:, None] * r
+        return out
+    want = formula(leaves)
+    loss = (want * dy.double()).sum()
+    loss.backward()
+    tol = 8 * 10 * ((2 * f + 8) * u + (U(T) if T == BF16 else 0))
+    assert (y.double() - want).abs().max() <= tol * want.abs().max()
+    for k, v in grads.items():
+        ref = leaves[k].grad
+        assert (v.double() - ref).abs().max() <= tol * ref.abs().max(), k
+        # a difference of the formula along a random direction
+        step = normal(gen(1), *ref.shape).double()
+        eps = 1e-5
+        moved = [dict({n: t.detach() for n, t in leaves.items()}, **{k: leaves[k].detach() + s * eps * step}) for s in (1, -1)]
+        diff = sum(s * (formula(m) * dy.double()).sum() for s, m in zip((1, -1), moved)) / (2 * eps)
+        assert abs(float(diff - (v.double() * step).sum())) <= tol * float((ref.abs() * step.abs()).sum()) + 1e-6 * float(diff.abs())
+    again_y, again = ours()
+    assert torch.equal(again_y, y) and all(torch.equal(again[k], grads[k]) for k in grads)
