@@ -29,7 +29,7 @@ __device__ uint32_t wait_error;   // set when a bounded wait gives up; read and 
 
 constexpr int kTileM = 128;    // MMA rows
 constexpr int kSwapStride = 36;   // floats of a row: reading eight columns per lane, four lanes a row, then meets every bank once
-constexpr int kBlockOfTiles = 16;   // row tiles of a group that are walked together, so that their rows stay in L2 for the next features
+constexpr int kBlockOfTiles = 8;  // row tiles of a group that are walked together, so that their rows stay in L2 for the next features
 
 // How CTAs of a cluster work together: each for itself; a pair on one tile; several on parts of one tile's reduction.
 enum Share { kAlone = 0, kPair = 1, kSplit = 2 };
@@ -67,6 +67,8 @@ struct Cfg {
 struct Maps {
   CUtensorMap a[2], a_up[2];   // weights; dweight: dout and its second half, 128 and 64 rows at a time
   CUtensorMap b[4], b_up[4];   // rows, boxes of 1/4, 2/4, 3/4 and 4/4 of a CTA's most; dweight: x, 128 and 64 rows at a time
+  CUtensorMap d, d_up;    // dweight: dw, where it is written by copies
+  int d_copies;
   int a_whole, b_whole;   // operands across their rows: one copy brings both panels of 64 columns; forward: all matrices in one map of their rows
   int a_step;             // forward, then: rows from one matrix to the next
 };
@@ -570,6 +572,48 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
         const void* add = it.half ? p.add_dw_up : p.add_dw;
         void* dw = it.half ? p.dw_up : p.dw;
         const int64_t at = it.g * p.step_w + (int64_t)first_row * p.ld_w + it.j0;
+        uint8_t* buffer = (uint8_t*)swap + (warp - 2) * 4096;
+        if (maps.d_copies && first_row < p.n) {
+          // whole lines, written by copies of 32 rows x 128 bytes from shared memory, which cut off what lies outside the matrix
+          const CUtensorMap* map = it.half ? &maps.d_up : &maps.d;
+          const int per = p.dw_f32 ? 32 : 64;
+          for (int c = per * team; c < cols; c += 2 * per) {
+            float v[32] = {};
+            uint32_t w[32];
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            __syncwarp();
+            if (sums) {
+              tmem_ld32(t0 + c, v);
+              tmem_ld_wait();
+            }
+            if (p.dw_f32) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) w[j] = __float_as_uint(v[j]);
+            } else {
+              float u[32] = {};
+              if (sums && c + 32 < BN) {
+                tmem_ld32(t0 + c + 32, u);
+                tmem_ld_wait();
+              }
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                const __nv_bfloat162 a = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]), b = __floats2bfloat162_rn(u[2 * j], u[2 * j + 1]);
+                w[j] = *(const uint32_t*)&a, w[16 + j] = *(const uint32_t*)&b;
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              *(uint4*)(buffer + lane * 128 + ((i ^ (lane & 7)) << 4)) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+              asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(smem_u32(buffer)),
+                           "r"(it.j0 + c), "r"(first_row), "r"(it.g)
+                           : "memory");
+              asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+          }
+        } else
         for (int c = 32 * team; c < cols && first_row < p.n; c += 64) {
           float v[32] = {};
           __syncwarp();   // the loads from TMEM take the whole warp
@@ -577,7 +621,6 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
             tmem_ld32(t0 + c, v);
             tmem_ld_wait();
           }
-          uint8_t* buffer = (uint8_t*)swap + (warp - 2) * 4096;
           if (p.dw_f32)
             store_block(buffer, v, (float*)dw + at + c, add ? (const float*)add + at + c : nullptr, p.ld_w, p.n - first_row, cols - c, p.dw_wide);
           else
@@ -646,6 +689,7 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
     }
   }
 
+  if (KIND == kDweight && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   __syncwarp();
   if (*abort_flag) {
     // copies and MMAs still in flight land before shared memory and TMEM are released
@@ -660,10 +704,11 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------
-bool encode(CUtensorMap* m, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+bool encode(CUtensorMap* m, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
+            CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16) {
   const cuuint32_t one[4] = {1, 1, 1, 1};
   EncodeFn fn = encode_fn();
-  return fn && fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  return fn && fn(m, type, rank, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // [rows, cols] read along its rows: boxes of 64 columns and 1/4 .. 4/4 of `most` rows
@@ -705,6 +750,15 @@ bool map_panels(CUtensorMap* m, const void* base, int64_t matrices, int64_t rows
   return encode(m, base, 3, dims, strides, box);
 }
 
+// dw [groups, n, k], boxes of 32 rows x 128 bytes; false where its rows are not aligned to 16 bytes
+bool map_dw(CUtensorMap* m, const void* base, const Problem& p) {
+  const int e = p.dw_f32 ? 4 : 2;
+  const cuuint64_t sg = p.groups.G > 1 ? (cuuint64_t)p.step_w * e : ((cuuint64_t)p.n * p.ld_w * e + 15) & ~(cuuint64_t)15;
+  if (((uintptr_t)base | (uintptr_t)(p.ld_w * e) | (uintptr_t)sg) & 15) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)p.k, (cuuint64_t)p.n, (cuuint64_t)p.groups.G}, strides[2] = {(cuuint64_t)p.ld_w * e, sg};
+  const cuuint32_t box[3] = {(cuuint32_t)(128 / e), 32, 1};
+  return encode(m, base, 3, dims, strides, box, p.dw_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16);
+}
 // Tiles of a product, at most
 template <int KIND, bool GATED, int BN, int SHARE>
 int64_t most_tiles(const Problem& p) {
@@ -733,10 +787,11 @@ cudaError_t launch(const Problem& p, cudaStream_t st) {
   bool ok;
   const int64_t rows = p.L * p.groups.R, most = most_tiles<KIND, GATED, BN, SHARE>(p);
   const __nv_bfloat16* y = (const __nv_bfloat16*)p.y;
-  m.a_whole = m.b_whole = m.a_step = 0;
+  m.a_whole = m.b_whole = m.a_step = m.d_copies = 0;
   if (KIND == kDweight) {
     static_assert(KIND != kDweight || BN / C::kCtas == 128, "two panels of x's columns per CTA");
     m.a_whole = whole(p.n), m.b_whole = whole(p.k);
+    m.d_copies = !p.add_dw && map_dw(&m.d, p.dw, p) && (!GATED || map_dw(&m.d_up, p.dw_up, p));
     ok = true;
     for (int i = 0; i < 2; ++i)
       ok = ok && map_panels(&m.a[i], y, 1, rows, p.n, p.ld_y, 0, 128 >> i) && map_panels(&m.b[i], p.x, 1, rows, p.k, p.ld_x, 0, 128 >> i) &&
