@@ -38,6 +38,26 @@ __device__ __forceinline__ float2 fma_2(float2 a, float2 b, float2 c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(*(uint64_t*)&r) : "l"(*(const uint64_t*)&a), "l"(*(const uint64_t*)&b), "l"(*(const uint64_t*)&c));
   return r;
 }
+__device__ __forceinline__ uint32_t cluster_ctas() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_place() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Eight floats at the place of `at` in another CTA's shared memory
+__device__ __forceinline__ void load_of_cta(const float* at, int rank, float (&v)[8]) {
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(tc::smem_u32(at)), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(a) : "memory");
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "r"(a + 16) : "memory");
+}
 // `count` floats (0 .. V) from memory, zeros behind them.
 template <int V>
 __device__ __forceinline__ void copy_floats(float* to, const float* from, int count) {
@@ -109,7 +129,8 @@ __global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads) general_ker
     count_tiles(p.groups, TI, before, scratch);
     items = (int64_t)before[p.groups.G] * JT;
   }
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+  const int ctas = (int)cluster_ctas(), place = (int)cluster_place();   // several CTAs on one tile share its reduction
+  for (int64_t item = blockIdx.x / ctas; item < items; item += gridDim.x / ctas) {
     int g, i0, j0 = (int)(item % JT) * TJ, half = 0;
     if (KIND == kDweight) {
       int64_t r = item / JT;
@@ -124,8 +145,9 @@ __global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads) general_ker
     const int64_t row0 = gr.first + (KIND == kDweight ? 0 : i0);
     const int I = KIND == kDweight ? min(TI, p.n - i0) : (int)min((int64_t)TI, gr.m - i0);
     const int J = min(TJ, cols - j0);
-    const int64_t red = KIND == kForward ? p.k : KIND == kBackward ? p.n : gr.m;
-    const int64_t steps = (red + kDeep - 1) / kDeep;
+    const int red = KIND == kForward ? p.k : KIND == kBackward ? p.n : (int)gr.m;
+    const int all_steps = red / kDeep + (red % kDeep != 0), each = (all_steps + ctas - 1) / ctas;
+    const int first = min(place * each, all_steps), steps = min(first + each, all_steps) - first;   // this CTA's
     // Sums in pairs for the packed multiply-add: of the even and the odd products where both operands lie along, else of two neighbouring columns
     constexpr bool kByProduct = C::kAlongA && C::kAlongB;
     constexpr int kPairs = kByProduct ? C::RJ : C::RJ / 2;
@@ -175,12 +197,15 @@ __global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads) general_ker
         base_a = (const T*)p.y + gr.first * p.ld_y + (int64_t)half * p.n + i0, ld_a = p.ld_y;
         base_b = (const T*)p.x + gr.first * p.ld_x + j0, ld_b = p.ld_x;
       }
-      Part<T, TI, C::kAlongA, C::kStrideA, kThreads, V> pa(base_a, ld_a, I);
+      const int64_t skip = (int64_t)first * kDeep;
+      const int mine = red - first * kDeep;
+      Part<T, TI, C::kAlongA, C::kStrideA, kThreads, V> pa(base_a + skip * (C::kAlongA ? 1 : ld_a), ld_a, I);
       typedef Part<T, TJ, C::kAlongB, C::kStrideB, kThreads, V> PartB;
-      auto left_of = [&](int64_t step) { return (int)min(red - step * kDeep, (int64_t)kDeep); };
-      PartB pb(base_b, ld_b, J), pb2(kSets == 2 ? base_b2 : base_b, ld_b, J);
+      auto left_of = [&](int step) { return min(mine - step * kDeep, kDeep); };
+      const int64_t skip_b = skip * (C::kAlongB ? 1 : ld_b);
+      PartB pb(base_b + skip_b, ld_b, J), pb2((kSets == 2 ? base_b2 : base_b) + skip_b, ld_b, J);
       if constexpr (sizeof(T) == 4) {
-        auto ask = [&](int64_t step) {
+        auto ask = [&](int step) {
           if (step < steps) {
             float* buffer = smem + step % C::kBuffers * C::kBuffer;
             pa.copy(buffer, left_of(step), base_a), pb.copy(buffer + C::kFloatsA, left_of(step), base_a);
@@ -189,7 +214,7 @@ __global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads) general_ker
           asm volatile("cp.async.commit_group;" ::: "memory");
         };
         for (int i = 0; i < C::kBuffers - 1; ++i) ask(i);
-        for (int64_t step = 0; step < steps; ++step) {
+        for (int step = 0; step < steps; ++step) {
           asm volatile("cp.async.wait_group %0;" ::"n"(C::kBuffers - 2) : "memory");
           __syncthreads();   // everybody's copies of this step are there, and nobody reads the buffer that the next copies go to
           ask(step + C::kBuffers - 1);
@@ -199,18 +224,18 @@ __global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads) general_ker
         __syncthreads();
       } else {
         float ra[decltype(pa)::kEach], rb[kSets][PartB::kEach];
-        auto fetch = [&](int64_t step) {
+        auto fetch = [&](int step) {
           pa.fetch(ra, left_of(step)), pb.fetch(rb[0], left_of(step));
           if (kSets == 2) pb2.fetch(rb[kSets - 1], left_of(step));
         };
-        auto put = [&](int64_t step) {
+        auto put = [&](int step) {
           float* buffer = smem + step % C::kBuffers * C::kBuffer;
           pa.put(buffer, ra), pb.put(buffer + C::kFloatsA, rb[0]);
           if (kSets == 2) pb2.put(buffer + C::kFloatsA + C::kFloatsB, rb[kSets - 1]);
         };
         if (steps) fetch(0), put(0);
         __syncthreads();
-        for (int64_t step = 0; step < steps; ++step) {
+        for (int step = 0; step < steps; ++step) {
           if (step + 1 < steps) fetch(step + 1);
           multiply(smem + step % C::kBuffers * C::kBuffer);
           if (step + 1 < steps) put(step + 1);
@@ -225,48 +250,64 @@ __global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads) general_ker
 #pragma unroll
         for (int j = 0; j < C::RJ; ++j)
           Cs[(s * TI + C::row(ty, i)) * kPad + C::col(tx, j)] = kByProduct ? c[s][i][j].x + c[s][i][j].y : j & 1 ? c[s][i][j / 2].y : c[s][i][j / 2].x;
-    __syncthreads();
-    const int warp = t / 32, lane = t % 32;
-    for (int jj = 0; jj < J; jj += 32) {
-      if (KIND == kDweight) {
+    if (ctas > 1) cluster_wait();
+    else __syncthreads();
+    // Blocks of 8 rows x 32 columns, dealt to the warps of all CTAs of the tile.  What the CTAs hold of a result is added in the order of their ranks.
+    auto sums_at = [&](int s, int i, int j, float (&v)[8]) {
+      const float* at = Cs + (s * TI + i) * kPad + j;
+      if (ctas == 1) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = at[u];
+        return;
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = 0.f;
+      for (int r = 0; r < ctas; ++r) {
+        float w[8];
+        load_of_cta(at, r, w);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] += w[u];
+      }
+    };
+    const int lane = t % 32;
+    for (int block = place + ctas * (t / 32); block < TI / 8 * (TJ / 32); block += ctas * (kThreads / 32)) {
+      const int jj = block % (TJ / 32) * 32, ii = block / (TJ / 32) * 8;
+      if (jj >= J || ii >= I) continue;
+      const int i = ii + lane / 4, j = jj + 8 * (lane % 4);
+      float z[1][8], up[1][8] = {};
+      sums_at(0, i, j, z[0]);
+      if (kSets == 2) sums_at(1, i, j, up[0]);
+      if constexpr (KIND == kDweight) {
+        const int count = i < I ? min(max(J - j, 0), 8) : 0;
         const void* add = half ? p.add_dw_up : p.add_dw;
         void* dw = half ? p.dw_up : p.dw;
-        const int j = jj + lane;
-        for (int i = warp; i < I; i += kThreads / 32) {
-          if (j >= J) continue;
-          const int64_t at = g * p.step_w + (int64_t)(i0 + i) * p.ld_w + j0 + j;
-          float v = Cs[i * kPad + j];
-          if (p.dw_f32) {
-            if (add) v += ((const float*)add)[at];
-            ((float*)dw)[at] = v;
-          } else {
-            if (add) v += load_as_float((const T*)add + at);
-            store_as((T*)dw + at, v);
-          }
-        }
-      } else {
-        const int j = jj + 8 * (lane % 4);
-        for (int i0w = warp * 8; i0w < I; i0w += kThreads / 4) {
-          const int i = i0w + lane / 4;
-          float z[1][8], up[1][8] = {};
+        const int64_t at = g * p.step_w + (int64_t)(i0 + i) * p.ld_w + j0 + j;
+        auto finish = [&](auto* o, const auto* from) {
+          if (!count) return;
+          if (from) {
+            uint32_t w[2 * sizeof(*o)];
+            float v[8];
+            load_8(from, p.dw_wide == 2, count, w);
+            floats_of(w, v);
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            z[0][u] = Cs[i * kPad + j + u];
-            if (kSets == 2) up[0][u] = Cs[(TI + i) * kPad + j + u];
+            for (int u = 0; u < 8; ++u) z[0][u] += v[u];
           }
-          if constexpr (KIND == kForward) {
-            const Forward<T, GATED> e(p.fwd, g, j0 + j);
-            e.rows(row0 + i0w, I - i0w, z, up);
-          } else {
-            const Backward<T> e(p.bwd, g, j0 + j);
-            typename Backward<T>::template Asked<1> q;
-            e.ask(row0 + i0w, I - i0w, q);
-            e.rows(row0 + i0w, I - i0w, z, q);
-          }
-        }
+          store_8(o, p.dw_wide == 2, count, z[0]);
+        };
+        if (p.dw_f32) finish((float*)dw + at, add ? (const float*)add + at : nullptr);
+        else finish((T*)dw + at, add ? (const T*)add + at : nullptr);
+      } else if constexpr (KIND == kForward) {
+        const Forward<T, GATED> e(p.fwd, g, j0 + j);
+        e.rows(row0 + ii, I - ii, z, up);
+      } else {
+        const Backward<T> e(p.bwd, g, j0 + j);
+        typename Backward<T>::template Asked<1> q;
+        e.ask(row0 + ii, I - ii, q);
+        e.rows(row0 + ii, I - ii, z, q);
       }
     }
-    __syncthreads();
+    if (ctas > 1) cluster_wait();
+    else __syncthreads();
   }
 }
 
@@ -276,9 +317,13 @@ cudaError_t launch_tiles(const Problem& p, int64_t tiles, int sms, cudaStream_t 
   constexpr size_t kBytes = General<KIND, T, GATED>::kFloats * 4;
   const cudaError_t e = tc::sm_count_and_smem_optin(general_kernel<KIND, T, GATED, V>, kBytes + (MCCE_LINEAR_MAX_GROUPS + 1 + 33) * 4, cache, &sms);
   if (e != cudaSuccess) return e;
-  const int64_t most = 8 * sms;
-  return launch_close(general_kernel<KIND, T, GATED, V>, dim3((unsigned)(tiles < most ? tiles : most)), General<KIND, T, GATED>::kThreads,
-                      kBytes + (size_t)(p.groups.G + 1 + 33) * 4, st, p);
+  // CTAs per tile: as many as a full device has room for four times over and as leave each of them eight steps (4 rows x 2034 x 64 fp32: 62 us alone)
+  const int64_t red = KIND == kForward ? p.k : KIND == kBackward ? p.n : p.L * p.groups.R / p.groups.G;
+  int ctas = 8;
+  while (ctas > 1 && (tiles * ctas > 4 * sms || red < 8 * kDeep * ctas)) ctas /= 2;
+  const int64_t most = 8 * sms / ctas;
+  return launch_close(general_kernel<KIND, T, GATED, V>, dim3((unsigned)((tiles < most ? tiles : most) * ctas)), General<KIND, T, GATED>::kThreads,
+                      kBytes + (size_t)(p.groups.G + 1 + 33) * 4, st, ctas, p);
 }
 template <Kind KIND, typename T, bool GATED, int V>
 cudaError_t launch_general(const Problem& p, cudaStream_t st) {
@@ -496,11 +541,11 @@ cudaError_t run_bias_sums(const Problem& p, int32_t dtype, const void* add, cons
   const bool wide = wide_rows(p.y, p.ld_y, e) && (!p.gated || p.n * e % 16 == 0);
   const BiasArgs a{p.groups, p.n, p.gated, p.dw_f32, wide, chunks, p.ld_y, p.y, add, add_up, db, db_up, chunks > 1 ? parts : nullptr};
   const dim3 grid((p.n + 255) / 256, p.groups.G, halves * chunks), all((unsigned)(((int64_t)p.groups.G * p.n + 255) / 256), halves);
-  const cudaError_t err = dtype == MCCE_F32 ? launch_close(bias_kernel<float>, grid, 256, 0, st, a)
-                                            : launch_close(bias_kernel<__nv_bfloat16>, grid, 256, 0, st, a);
+  const cudaError_t err = dtype == MCCE_F32 ? launch_close(bias_kernel<float>, grid, 256, 0, st, 1, a)
+                                            : launch_close(bias_kernel<__nv_bfloat16>, grid, 256, 0, st, 1, a);
   if (err != cudaSuccess || chunks == 1) return err;
-  return dtype == MCCE_F32 ? launch_close(bias_parts_kernel<float>, all, 256, 0, st, a)
-                           : launch_close(bias_parts_kernel<__nv_bfloat16>, all, 256, 0, st, a);
+  return dtype == MCCE_F32 ? launch_close(bias_parts_kernel<float>, all, 256, 0, st, 1, a)
+                           : launch_close(bias_parts_kernel<__nv_bfloat16>, all, 256, 0, st, 1, a);
 }
 
 namespace {
@@ -517,11 +562,11 @@ cudaError_t pack_as(bool pack, const void* x, void* to, const uint8_t* q_in, uin
   const dim3 n((unsigned)grid);
   if (pack) {
     const T* from = (const T*)x;
-    if (!wide) return launch_close(pack_odd_kernel<T>, n, 256, 0, st, from, q, scales, rows, per_row, d, ld_x, ld_q);
-    return launch_close(many ? pack_kernel<T, kU> : pack_kernel<T, 1>, n, 256, 0, st, from, q, scales, blocks, per_row, d, ld_x, ld_q);
+    if (!wide) return launch_close(pack_odd_kernel<T>, n, 256, 0, st, 1, from, q, scales, rows, per_row, d, ld_x, ld_q);
+    return launch_close(many ? pack_kernel<T, kU> : pack_kernel<T, 1>, n, 256, 0, st, 1, from, q, scales, blocks, per_row, d, ld_x, ld_q);
   }
-  if (!wide) return launch_close(unpack_odd_kernel<T>, n, 256, 0, st, q_in, s_in, (T*)to, rows, per_row, d, ld_x, ld_q);
-  return launch_close(many ? unpack_kernel<T, kU> : unpack_kernel<T, 1>, n, 256, 0, st, q_in, s_in, (T*)to, blocks, per_row, d, ld_x, ld_q);
+  if (!wide) return launch_close(unpack_odd_kernel<T>, n, 256, 0, st, 1, q_in, s_in, (T*)to, rows, per_row, d, ld_x, ld_q);
+  return launch_close(many ? unpack_kernel<T, kU> : unpack_kernel<T, 1>, n, 256, 0, st, 1, q_in, s_in, (T*)to, blocks, per_row, d, ld_x, ld_q);
 }
 }  // namespace
 
@@ -707,7 +752,10 @@ extern "C" int mcce_expert_linear_dweight(const mcce_linear* p, const void* dout
   const int64_t G = q.groups.G;
   q.y = dout, q.x = x, q.ld_y = ld_or(p->ld_y, width), q.ld_x = ld_or(p->ld_x, p->k);
   q.dw = dw, q.dw_up = dw_up, q.add_dw = add_dw, q.add_dw_up = add_dw_up, q.dw_f32 = p->out_dtype == MCCE_F32;
-  q.dw_wide = aligned(dw, 4 * eo) && aligned(dw_up, 4 * eo) && aligned(add_dw, 4 * eo) && aligned(add_dw_up, 4 * eo) && q.ld_w % 4 == 0 && q.step_w % 4 == 0;
+  auto dw_aligned = [&](int64_t bytes) {
+    return aligned(dw, bytes) && aligned(dw_up, bytes) && aligned(add_dw, bytes) && aligned(add_dw_up, bytes) && q.ld_w * eo % bytes == 0 && q.step_w * eo % bytes == 0;
+  };
+  q.dw_wide = dw_aligned(16) ? 2 : dw_aligned(4 * eo) ? 1 : 0;
   const Span sy = row_span(dout, rows, q.ld_y, width, e), sx = row_span(x, rows, q.ld_x, p->k, ex);
   const Span ssc = flat_span(scales, rows, blocks_of(p->k)), soff = flat_span(offsets, (int64_t)p->n_layers * (p->n_experts + 1), 4);
   const Span saw = weight_span(*p, add_dw, eo), sawu = weight_span(*p, add_dw_up, eo), sab = flat_span(add_db, G * p->n, eo);

@@ -19,12 +19,14 @@ __device__ __forceinline__ void after_previous() {
   asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
 }
 template <typename... P>
-cudaError_t launch_close(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const std::decay_t<P>&... args) {
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
+cudaError_t launch_close(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster, const std::decay_t<P>&... args) {
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid, cfg.blockDim = dim3(threads), cfg.dynamicSmemBytes = smem, cfg.stream = st, cfg.attrs = &attr, cfg.numAttrs = 1;
+  cfg.gridDim = grid, cfg.blockDim = dim3(threads), cfg.dynamicSmemBytes = smem, cfg.stream = st, cfg.attrs = attr, cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
@@ -408,7 +410,7 @@ struct Problem {
   const void *x, *y, *w, *w_up;    // forward: x, w; backward: y, w; dweight: y, x
   void *dw, *dw_up;                // dweight
   const void *add_dw, *add_dw_up;
-  int32_t dw_f32, dw_wide;   // dw_wide: four columns of its rows (and of those added) are aligned as a whole
+  int32_t dw_f32, dw_wide;   // dw_wide: of its rows (and of those added) four columns (1), also 16 bytes (2), are aligned as a whole
   ForwardArgs fwd;
   BackwardArgs bwd;
 };

@@ -110,7 +110,7 @@ template <bool GATED, int M>
 cudaError_t launch_few(const Problem& p, int sms, cudaStream_t st) {
   const int64_t rows = p.L * p.groups.R, tiles = rows < p.groups.G ? rows : rows / M + p.groups.G;
   const int64_t want = (tiles * (GATED ? p.n : (p.n + 1) / 2) + 7) / 8, most = (M == 1 ? 3 : 2) * sms;
-  return launch_close(few_kernel<GATED, M>, dim3((unsigned)(want < most ? want : most)), 256, (size_t)(p.groups.G + 1 + 33) * 4, st, p);
+  return launch_close(few_kernel<GATED, M>, dim3((unsigned)(want < most ? want : most)), 256, (size_t)(p.groups.G + 1 + 33) * 4, st, 1, p);
 }
 
 }  // namespace

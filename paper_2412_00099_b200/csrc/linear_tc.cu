@@ -534,7 +534,8 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
       if constexpr (KIND == kBackward)
         Backward<__nv_bfloat16>(p.bwd, it.g, it.f0 + quad * 32 + 8 * (lane & 3)).ask((int64_t)it.row + 8 * team, it.rows - 8 * team, asked);
       if (sums) {
-        if (!mbar_wait(bar_tfull + 8 * buf, (acc >> 1) & 1u, abort_flag, &wait_error, 4u)) break;
+        // a tile's sums may take long: 20 us per slab more than any other wait
+        if (!mbar_wait(bar_tfull + 8 * buf, (acc >> 1) & 1u, abort_flag, &wait_error, 4u, kWaitLimitNs + 20000ull * (to - from))) break;
         ++acc;
         tc_fence_after();
       }
@@ -703,6 +704,8 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
   if (warp == 1) free_tmem<PAIR>(tmem_base, 2 * BN);
 }
 
+constexpr int64_t kMostStride = 1ll << 38;   // elements: a tensor map's strides are below 2^40 bytes
+
 // ---- host ---------------------------------------------------------------------------------------------------------
 bool encode(CUtensorMap* m, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
             CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16) {
@@ -754,7 +757,7 @@ bool map_panels(CUtensorMap* m, const void* base, int64_t matrices, int64_t rows
 bool map_dw(CUtensorMap* m, const void* base, const Problem& p) {
   const int e = p.dw_f32 ? 4 : 2;
   const cuuint64_t sg = p.groups.G > 1 ? (cuuint64_t)p.step_w * e : ((cuuint64_t)p.n * p.ld_w * e + 15) & ~(cuuint64_t)15;
-  if (((uintptr_t)base | (uintptr_t)(p.ld_w * e) | (uintptr_t)sg) & 15) return false;
+  if (((uintptr_t)base | (uintptr_t)(p.ld_w * e) | (uintptr_t)sg) & 15 || p.ld_w >= kMostStride / 2 || sg >= (1ull << 40)) return false;
   const cuuint64_t dims[3] = {(cuuint64_t)p.k, (cuuint64_t)p.n, (cuuint64_t)p.groups.G}, strides[2] = {(cuuint64_t)p.ld_w * e, sg};
   const cuuint32_t box[3] = {(cuuint32_t)(128 / e), 32, 1};
   return encode(m, base, 3, dims, strides, box, p.dw_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16);
@@ -842,14 +845,14 @@ cudaError_t launch_rows(const Problem& p, int sms, cudaStream_t st) {
   return launch<KIND, GATED, 256, kPair>(p, st);
 }
 
-bool tma_rows(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
+bool tma_rows(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld < kMostStride; }
 
 }  // namespace
 
 bool tensor_applicable(Kind kind, const Problem& p, int32_t dtype) {
   if (dtype != MCCE_BF16) return false;
   if (kind == kDweight) return p.L * p.groups.R > 0 && tma_rows(p.y, p.ld_y) && tma_rows(p.x, p.ld_x) && (!p.gated || p.n % 8 == 0);
-  if (!tma_rows(p.w, p.ld_w) || !tma_rows(p.w_up, p.ld_w) || (p.groups.G > 1 && p.step_w % 8)) return false;
+  if (!tma_rows(p.w, p.ld_w) || !tma_rows(p.w_up, p.ld_w) || (p.groups.G > 1 && (p.step_w % 8 || p.step_w >= kMostStride))) return false;
   if (kind == kForward) return tma_rows(p.x, p.ld_x);
   return tma_rows(p.y, p.ld_y) && (!p.gated || p.n % 8 == 0);
 }

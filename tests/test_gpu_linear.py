@@ -439,6 +439,27 @@ def test_one_experts_nan_stays_its_own(T):
     assert (r.dw[2] == 0).all() and (r.db[2] == 0).all()
 
 
+@pytest.mark.parametrize("T", [BF16, F32])
+def test_nothing(T):
+    """No rows at all, and rows that belong to nobody: nothing is read or written but the weights' gradients, 0 or what is added."""
+    g, E, n, k = gen(2), 3, 40, 64
+    w = normal(g, E, n, k, dtype=T)
+    for R in (0, 50):
+        off = torch.zeros(E + 1, dtype=torch.int32, device="cuda")
+        x, dout = normal(g, R, k, dtype=T), normal(g, R, n, dtype=T)
+        out = torch.full((R, n), 7.0, device="cuda", dtype=T)
+        assert (mb.expert_linear(x, off, w, out=mb.LinearOut(out)).out == 7).all()
+        dx = torch.full((R, k), 7.0, device="cuda", dtype=T)
+        assert (mb.expert_linear_backward(dout, off, w, out=mb.LinearGrad(dx)).dx == 7).all()
+        before = mb.WeightGrad(normal(g, E, n, k, dtype=T), None, normal(g, E, n, dtype=T))
+        for eight in (False, True):
+            rows = mb.checkpoint_pack(x) if eight else (x, None)
+            r = mb.expert_linear_dweight(dout, rows[0], off, scales=rows[1], want_db=True)
+            assert (r.dw == 0).all() and (r.db == 0).all()
+            r = mb.expert_linear_dweight(dout, rows[0], off, scales=rows[1], want_db=True, add=before)
+            assert torch.equal(r.dw, before.dw) and torch.equal(r.db, before.db)
+
+
 def test_streams_and_graphs():
     """On a stream of the caller's, captured and replayed on new values: the same bits as in order."""
     g = gen(9)
