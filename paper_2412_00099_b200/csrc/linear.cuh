@@ -178,12 +178,29 @@ __device__ __forceinline__ void store_8(__nv_bfloat16* p, bool wide, int count, 
   }
   store_words_8(p, wide, count, w);
 }
-// The same in 8 bits, and the scale of the 32 columns that this lane and its three neighbours hold; values behind the last
-// column are 0.  Every lane of the warp calls it.
-__device__ __forceinline__ uint32_t pack_8(const float (&v)[8], uint32_t (&w)[2]) {
-  uint32_t bits = 0u;   // of the largest magnitude: ordered like the magnitudes, infinity and NaN last
+// Bits of the largest magnitude, ordered like the magnitudes, infinity and NaN last
+__device__ __forceinline__ uint32_t largest_bits(const float (&v)[8]) {
+  uint32_t bits = 0u;
 #pragma unroll
   for (int j = 0; j < 8; ++j) bits = max(bits, __float_as_uint(v[j]) & 0x7fffffffu);
+  return bits;
+}
+__device__ __forceinline__ uint32_t largest_bits(const uint32_t (&w)[8]) {
+  uint32_t bits = 0u;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) bits = max(bits, w[j] & 0x7fffffffu);
+  return bits;
+}
+__device__ __forceinline__ uint32_t largest_bits(const uint32_t (&w)[4]) {   // bf16, two at a time
+  __nv_bfloat162 m = __habs2(*(const __nv_bfloat162*)&w[0]);
+#pragma unroll
+  for (int j = 1; j < 4; ++j) m = __hmax2_nan(m, __habs2(*(const __nv_bfloat162*)&w[j]));
+  const uint32_t b = *(const uint32_t*)&m;
+  return max(b << 16, b & 0xffff0000u);
+}
+// The same in 8 bits, and the scale of the 32 columns that this lane and its three neighbours hold, `bits` being this lane's largest; values behind the last
+// column are 0.  Every lane of the warp calls it.
+__device__ __forceinline__ uint32_t pack_8(const float (&v)[8], uint32_t bits, uint32_t (&w)[2]) {
   bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 1));
   bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 2));
   const uint32_t s = block_scale(bits);
@@ -238,7 +255,7 @@ struct Forward {
       uint32_t w[2];
 #pragma unroll
       for (int j = 0; j < 8; ++j) z[j] = j < count ? v[j] : 0.f;
-      const uint32_t s = pack_8(z, w);
+      const uint32_t s = pack_8(z, largest_bits(z), w);
       if (!on || count == 0) return;
       store_words_8((uint8_t*)a.saved + row * a.ld_saved + half * a.n + f, a.wide && (!half || a.n % 8 == 0), count, w);
       if ((f & 31) == 0) a.scales[row * (GATED ? 2 * a.blocks : a.blocks) + half * a.blocks + (f >> 5)] = (uint8_t)s;
