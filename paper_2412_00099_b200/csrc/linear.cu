@@ -13,9 +13,9 @@ namespace {
 // the reduction along its rows ([row][16], read four products at a time) or across them ([16][row], read four rows at a time); either way 8 16-byte loads
 // feed 32 packed multiply-adds.  fp32 operands of the next three steps are on their way by cp.async, 16, 8 or 4 bytes at a time as the alignment allows; bf16
 // elements of the next step in registers.  The results go through shared memory so that a warp ends up with 32 neighbouring columns of a row.
-// 30 to 36 TFLOP/s (16 groups of 256 rows x 2048 x 512 fp32: 283 us; its gradients 262 and 240), bound by the loads from shared memory and the
+// 31 to 37 TFLOP/s (16 groups of 256 rows x 2048 x 512 fp32: 274 us; its gradients 258 and 233), bound by the loads from shared memory and the
 // instructions around them; 64 x 64 and 128 x 128 tiles with 8 x 8 results per thread left more SMs idle than they saved (340 and 490 us).
-// 900 x 1002 x 515 (two elements per copy): 69 us, one step behind the other 95.
+// Where tiles are few, the CTAs of a cluster share a tile's reduction.  900 x 1002 x 515 (two elements per copy): 53 us; one step behind the other, alone, 95.
 constexpr int kDeep = 16;
 
 template <Kind KIND, typename T, bool GATED>
@@ -108,7 +108,7 @@ struct Part {
 };
 
 template <Kind KIND, typename T, bool GATED, int V>
-__global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads) general_kernel(const Problem p) {
+__global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads, KIND == kForward ? 1 : 5) general_kernel(const Problem p) {
   typedef General<KIND, T, GATED> C;
   constexpr int kSets = C::kSets, kThreads = C::kThreads, TI = C::TI, TJ = C::TJ, kPad = C::kPad;
   extern __shared__ __align__(16) float smem[];
@@ -317,10 +317,11 @@ cudaError_t launch_tiles(const Problem& p, int64_t tiles, int sms, cudaStream_t 
   constexpr size_t kBytes = General<KIND, T, GATED>::kFloats * 4;
   const cudaError_t e = tc::sm_count_and_smem_optin(general_kernel<KIND, T, GATED, V>, kBytes + (MCCE_LINEAR_MAX_GROUPS + 1 + 33) * 4, cache, &sms);
   if (e != cudaSuccess) return e;
-  // CTAs per tile: as many as a full device has room for four times over and as leave each of them eight steps (4 rows x 2034 x 64 fp32: 62 us alone)
+  // CTAs per tile: as many as a full device has room for at once and as leave each of them eight steps (4 rows x 2034 x 64 fp32: 62 us alone, 13 shared;
+  // 900 x 1002 x 515, 270 tiles: 70 and 53)
   const int64_t red = KIND == kForward ? p.k : KIND == kBackward ? p.n : p.L * p.groups.R / p.groups.G;
   int ctas = 8;
-  while (ctas > 1 && (tiles * ctas > 4 * sms || red < 8 * kDeep * ctas)) ctas /= 2;
+  while (ctas > 1 && (tiles * ctas > 6 * sms || red < 8 * kDeep * ctas)) ctas /= 2;
   const int64_t most = 8 * sms / ctas;
   return launch_close(general_kernel<KIND, T, GATED, V>, dim3((unsigned)((tiles < most ? tiles : most) * ctas)), General<KIND, T, GATED>::kThreads,
                       kBytes + (size_t)(p.groups.G + 1 + 33) * 4, st, ctas, p);
