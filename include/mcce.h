@@ -409,11 +409,14 @@ typedef struct {
  *   saved DEVICE saved_dtype [L,rows,n] (gated: [L,rows,2n], z then z_up) out or NULL: what the backward pass needs;
  *   scales DEVICE bytes (e8m0) [L,rows,ceil(n/32)] (gated: twice that, those of z first), contiguous; given exactly when saved is and holds
  *       8 bits.  Blocks do not reach from z into z_up.
+ *   workspace DEVICE, 16-byte aligned, as many bytes as the call of that name answers for these addresses, which it only looks at (0 is usual: it may
+ *       be NULL then).  It takes copies of bf16 rows and weights whose starts or strides are no multiples of 16 bytes, where that pays.
  * bf16 rows and weights meet on the tensor cores, whose fp32 accumulation truncates: a sum of k products is within 2^-24 k / 8 of its
  * terms' magnitudes. */
+size_t mcce_expert_linear_workspace_bytes(const mcce_linear* p /*HOST*/, const void* x, const void* w, const void* w_up);
 int mcce_expert_linear(const mcce_linear* p /*HOST*/, const void* x, const int32_t* offsets, const void* w, const void* w_up,
                        const void* bias, const void* bias_up, const void* add, void* out, void* saved, void* scales,
-                       void* cuda_stream);
+                       void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /* Its gradient with respect to the rows:  t = dout W_g  (gated: dout = [d | d_up], t = d W_g + d_up W_up_g), and
  *   below == 0:  dx = t + add
@@ -425,18 +428,18 @@ int mcce_expert_linear(const mcce_linear* p /*HOST*/, const void* x, const int32
  *   saved DEVICE saved_dtype [L,rows,below*k], scales [L,rows,below*ceil(k/32)] with 8 bits; NULL where below == 0
  *   dx DEVICE dtype [L,rows,k] (below == 2: [L,rows,2k]) out, stride ld_x; may be add, or saved in dtype, itself (same stride)
  *   h  DEVICE dtype [L,rows,k] out, stride ld_h, or NULL */
+size_t mcce_expert_linear_backward_workspace_bytes(const mcce_linear* p /*HOST*/, const void* dout, const void* w, const void* w_up);
 int mcce_expert_linear_backward(const mcce_linear* p /*HOST*/, const void* dout, const int32_t* offsets, const void* w,
                                 const void* w_up, const void* add, const void* saved, const void* scales, void* dx, void* h,
-                                void* cuda_stream);
+                                void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /* Its gradient with respect to weights and bias:  dw_g = add_dw_g + sum over the group's rows of dout_r^T x_r,
  * db_g = add_db_g + sum of dout_r; gated: dw_up and db_up from the second half of dout's columns.  A group without rows gets what is added, or 0.
  *   dout as above;    x DEVICE dtype [L,rows,k], or with scales (bytes, [L,rows,ceil(k/32)]) e4m3, stride ld_x
  *   dw, dw_up DEVICE out_dtype [L,E,n,k] out (dw_up exactly when gated);    db, db_up DEVICE out_dtype [L,E,n] out, contiguous, or NULL
  *   add_dw, add_dw_up, add_db, add_db_up: like dw .. db_up, or NULL; each may be that output itself
- *   workspace DEVICE, 16-byte aligned, mcce_expert_linear_dweight_workspace_bytes(p) bytes with 8-bit x (0 otherwise: it may be NULL then):
- *       x in dtype, which is exact for scales of 2^-117 and more. */
-size_t mcce_expert_linear_dweight_workspace_bytes(const mcce_linear* p /*HOST*/);
+ * 8-bit x is brought to dtype in the workspace, which is exact for scales of 2^-117 and more. */
+size_t mcce_expert_linear_dweight_workspace_bytes(const mcce_linear* p /*HOST*/, const void* dout, const void* x);
 int mcce_expert_linear_dweight(const mcce_linear* p /*HOST*/, const void* dout, const void* x, const void* scales,
                                const int32_t* offsets, const void* add_dw, const void* add_dw_up, const void* add_db,
                                const void* add_db_up, void* dw, void* dw_up, void* db, void* db_up, void* workspace,

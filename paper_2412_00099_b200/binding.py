@@ -29,6 +29,7 @@ EXPORTS = [
     "mcce_get_grouping", "mcce_lifetime_stats", "mcce_set_miss_trace", "mcce_belady_replay",
     "mcce_rmsnorm", "mcce_rmsnorm_backward", "mcce_rmsnorm_backward_workspace_bytes", "mcce_dispatch", "mcce_dispatch_workspace_bytes",
     "mcce_combine", "mcce_combine_backward", "mcce_expert_linear", "mcce_expert_linear_backward", "mcce_expert_linear_dweight",
+    "mcce_expert_linear_workspace_bytes", "mcce_expert_linear_backward_workspace_bytes",
     "mcce_expert_linear_dweight_workspace_bytes", "mcce_expert_linear_status", "mcce_checkpoint_pack", "mcce_checkpoint_unpack", "mcce_profile", "mcce_profile_read", "mcce_uses_tensor_path", "mcce_router_kernel_kind", "mcce_selftest_wait_timeout", "mcce_route_trace_static",
     "mcce_route_trace_static_limit", "mcce_gen_normal", "mcce_gen_hidden_step", "mcce_gen_philox_words", "mcce_strerror",
     "mcce_last_cuda_error",
@@ -125,10 +126,11 @@ def load():
         lib.mcce_dispatch.argtypes = [vp] * 10 + [C.c_size_t, vp]
         lib.mcce_combine.argtypes = [vp] * 7
         lib.mcce_combine_backward.argtypes = [vp] * 8
-        lib.mcce_expert_linear.argtypes = [vp] * 12
-        lib.mcce_expert_linear_backward.argtypes = [vp] * 11
-        lib.mcce_expert_linear_dweight_workspace_bytes.restype = C.c_size_t
-        lib.mcce_expert_linear_dweight_workspace_bytes.argtypes = [vp]
+        lib.mcce_expert_linear.argtypes = [vp] * 12 + [C.c_size_t, vp]
+        lib.mcce_expert_linear_backward.argtypes = [vp] * 11 + [C.c_size_t, vp]
+        for name, n in (("", 4), ("_backward", 4), ("_dweight", 3)):
+            size = getattr(lib, "mcce_expert_linear%s_workspace_bytes" % name)
+            size.restype, size.argtypes = C.c_size_t, [vp] * n
         lib.mcce_expert_linear_dweight.argtypes = [vp] * 14 + [C.c_size_t, vp]
         lib.mcce_expert_linear_status.argtypes = [vp]
         lib.mcce_checkpoint_pack.argtypes = [vp, i32, C.c_int64, i32, C.c_int64, C.c_int64, vp, vp, vp]
@@ -456,8 +458,8 @@ def _marshal():
                             % (getattr(m, "built_for", "another version"), marshal_target()))
         m.connect(McceError, *[C.cast(getattr(lib, n), C.c_void_p).value for n in (
             "mcce_rmsnorm", "mcce_rmsnorm_backward_workspace_bytes", "mcce_rmsnorm_backward", "mcce_dispatch_workspace_bytes",
-            "mcce_dispatch", "mcce_combine", "mcce_combine_backward", "mcce_expert_linear", "mcce_expert_linear_backward",
-            "mcce_expert_linear_dweight_workspace_bytes", "mcce_expert_linear_dweight", "mcce_checkpoint_pack", "mcce_checkpoint_unpack",
+            "mcce_dispatch", "mcce_combine", "mcce_combine_backward", "mcce_expert_linear_workspace_bytes", "mcce_expert_linear",
+            "mcce_expert_linear_backward_workspace_bytes", "mcce_expert_linear_backward", "mcce_expert_linear_dweight_workspace_bytes", "mcce_expert_linear_dweight", "mcce_checkpoint_pack", "mcce_checkpoint_unpack",
             "mcce_strerror")])
         _fast = m
     return _fast

@@ -108,7 +108,7 @@ struct Part {
 };
 
 template <Kind KIND, typename T, bool GATED, int V>
-__global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads, KIND == kForward ? 1 : 5) general_kernel(const Problem p) {
+__global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads, KIND != kForward ? 5 : GATED ? 3 : 4) general_kernel(const Problem p) {
   typedef General<KIND, T, GATED> C;
   constexpr int kSets = C::kSets, kThreads = C::kThreads, TI = C::TI, TJ = C::TJ, kPad = C::kPad;
   extern __shared__ __align__(16) float smem[];
@@ -191,10 +191,10 @@ __global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads, KIND == kFo
         base_b = (const T*)p.w + at, ld_b = p.ld_w;
         if (kSets == 2) base_b2 = (const T*)p.w_up + at;
       } else if (KIND == kBackward) {
-        base_a = (const T*)p.y + row0 * p.ld_y + (int64_t)part * p.n, ld_a = p.ld_y;
+        base_a = (const T*)p.y + row0 * p.ld_y + part * p.half_y, ld_a = p.ld_y;
         base_b = (const T*)(part ? p.w_up : p.w) + g * p.step_w + j0, ld_b = p.ld_w;
       } else {
-        base_a = (const T*)p.y + gr.first * p.ld_y + (int64_t)half * p.n + i0, ld_a = p.ld_y;
+        base_a = (const T*)p.y + gr.first * p.ld_y + half * p.half_y + i0, ld_a = p.ld_y;
         base_b = (const T*)p.x + gr.first * p.ld_x + j0, ld_b = p.ld_x;
       }
       const int64_t skip = (int64_t)first * kDeep;
@@ -346,7 +346,7 @@ cudaError_t launch_general_types(const Problem& p, int32_t dtype, cudaStream_t s
   if (dtype == MCCE_BF16) return launch_general_gated<KIND, __nv_bfloat16, 1>(p, st);
   auto aligned_to = [&](int v) {   // v columns of what this product reads: x and the weights, dout and the weights, dout and x
     auto one = [&](const void* a, int64_t ld) { return !a || (((uintptr_t)a | (uintptr_t)(ld * 4)) & (4 * v - 1)) == 0; };
-    return (KIND == kBackward || one(p.x, p.ld_x)) && (KIND == kForward || (one(p.y, p.ld_y) && (!p.gated || p.n % v == 0))) &&
+    return (KIND == kBackward || one(p.x, p.ld_x)) && (KIND == kForward || (one(p.y, p.ld_y) && (!p.gated || p.half_y % v == 0))) &&
            (KIND == kDweight || (one(p.w, p.ld_w) && one(p.w_up, p.ld_w) && (p.groups.G == 1 || p.step_w % v == 0)));
   };
   if (aligned_to(4)) return launch_general_gated<KIND, float, 4>(p, st);
@@ -357,7 +357,7 @@ cudaError_t launch_general_types(const Problem& p, int32_t dtype, cudaStream_t s
 struct BiasArgs {
   Groups groups;
   int32_t n, gated, f32, wide, chunks;
-  int64_t ld_y;
+  int64_t ld_y, half_y;
   const void *y, *add, *add_up;
   void *db, *db_up;
   float* parts;   // [chunks][halves][G][n], null with one chunk
@@ -379,7 +379,7 @@ __global__ void __launch_bounds__(256) bias_kernel(const BiasArgs a) {
   const int j = blockIdx.x * 256 + 8 * lane, count = min(max(a.n - j, 0), 8);
   const GroupRows gr = group_rows(a.groups, g);
   const int64_t each = (gr.m + a.chunks - 1) / a.chunks, lo = min(chunk * each, gr.m), hi = min(lo + each, gr.m);
-  const T* y = (const T*)a.y + gr.first * a.ld_y + (int64_t)half * a.n + j;
+  const T* y = (const T*)a.y + gr.first * a.ld_y + half * a.half_y + j;
   float s[8] = {};
   if (count)
     for (int64_t r = lo + warp; r < hi; r += 32) {
@@ -539,8 +539,8 @@ int bias_chunks(int64_t rows, int32_t G, int32_t n) {
 cudaError_t run_bias_sums(const Problem& p, int32_t dtype, const void* add, const void* add_up, void* db, void* db_up, float* parts,
                           cudaStream_t st) {
   const int halves = p.gated ? 2 : 1, e = dtype == MCCE_F32 ? 4 : 2, chunks = bias_chunks(p.L * p.groups.R, p.groups.G, p.n);
-  const bool wide = wide_rows(p.y, p.ld_y, e) && (!p.gated || p.n * e % 16 == 0);
-  const BiasArgs a{p.groups, p.n, p.gated, p.dw_f32, wide, chunks, p.ld_y, p.y, add, add_up, db, db_up, chunks > 1 ? parts : nullptr};
+  const bool wide = wide_rows(p.y, p.ld_y, e) && (!p.gated || p.half_y * e % 16 == 0);
+  const BiasArgs a{p.groups, p.n, p.gated, p.dw_f32, wide, chunks, p.ld_y, p.half_y, p.y, add, add_up, db, db_up, chunks > 1 ? parts : nullptr};
   const dim3 grid((p.n + 255) / 256, p.groups.G, halves * chunks), all((unsigned)(((int64_t)p.groups.G * p.n + 255) / 256), halves);
   const cudaError_t err = dtype == MCCE_F32 ? launch_close(bias_kernel<float>, grid, 256, 0, st, 1, a)
                                             : launch_close(bias_kernel<__nv_bfloat16>, grid, 256, 0, st, 1, a);
@@ -582,6 +582,45 @@ cudaError_t run_unpack(const uint8_t* q, const uint8_t* scales, int32_t dtype, i
                            : pack_as<__nv_bfloat16>(false, nullptr, x, q, nullptr, scales, nullptr, rows, d, ld_x, ld_q, st);
 }
 
+// ---- bf16 rows to strides and starts of 16 bytes ------------------------------------------------------------------
+namespace {
+// Eight elements per lane, read as words (of a start between two words: five, shifted), the last of a row one by one.  Row r is row r % per of matrix r / per.
+__global__ void __launch_bounds__(256) align_kernel(const uint16_t* from, int64_t units, int64_t per, int cols, int across, int64_t ld, int64_t step,
+                                                    uint16_t* to, int64_t ld_to) {
+  after_previous();
+  const int64_t u = blockIdx.x * 256ll + threadIdx.x;
+  if (u >= units) return;
+  const int64_t row = u / across;
+  const int c = (int)(u - row * across) * 8;
+  const uint16_t* p = from + row / per * step + row % per * ld + c;
+  uint32_t w[4] = {};
+  if (c + 9 <= cols) {
+    const uint32_t* a = (const uint32_t*)((uintptr_t)p & ~(uintptr_t)3);
+    if ((uintptr_t)p & 2) {
+      uint32_t v[5];
+#pragma unroll
+      for (int i = 0; i < 5; ++i) v[i] = a[i];   // the element before the eight and the one behind them are the row's or, before its first, its word's
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(v[i], v[i + 1], 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = a[i];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i < cols) w[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
+  }
+  *(uint4*)(to + row * ld_to + c) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+}  // namespace
+cudaError_t run_align(const void* from, int64_t rows, int64_t per, int32_t cols, int64_t ld, int64_t step, void* to, int64_t ld_to, cudaStream_t st) {
+  const int across = (cols + 7) / 8;
+  const int64_t units = rows * across, grid = (units + 255) / 256;
+  if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
+  return launch_close(align_kernel, dim3((unsigned)grid), 256, 0, st, 1, (const uint16_t*)from, units, per, cols, across, ld, step, (uint16_t*)to, ld_to);
+}
+
 // ---- checks --------------------------------------------------------------------------------------------------------
 namespace {
 
@@ -613,23 +652,90 @@ Span weight_span(const mcce_linear& p, const void* w, int e) {
 Problem problem(const mcce_linear& p, const int32_t* offsets) {
   Problem q{};
   q.groups = {offsets, p.n_experts, p.n_layers * p.n_experts, p.rows};
-  q.n = p.n, q.k = p.k, q.gated = p.gated, q.L = p.n_layers;
+  q.n = p.n, q.k = p.k, q.gated = p.gated, q.L = p.n_layers, q.half_y = p.n;
   q.ld_w = ld_or(p.ld_w, p.k), q.step_w = p.step_w ? p.step_w : p.n * q.ld_w;
   return q;
 }
 int blocks_of(int64_t cols) { return (int)((cols + 31) / 32); }
 int code(cudaError_t e) { return e == cudaSuccess ? MCCE_OK : MCCE_ECUDA; }
 
+// bf16 rows that the tensor cores' copies cannot take (a stride or start that is no multiple of 16 bytes) are brought to one that is, where that pays: on the fp32
+// pipe a product runs at some 25 TFLOP/s (4096 x 2047 x 511, gated: 800 us), the copies at some 4 TB/s.
+struct Copies {
+  bool x, y, w;
+  size_t x_bytes, y_bytes, w_bytes;   // w: of one matrix of every group
+  size_t bytes(bool gated) const { return x_bytes + y_bytes + (gated ? 2 : 1) * w_bytes; }
+};
+int64_t whole_8(int64_t cols) { return (cols + 7) & ~7ll; }
+Copies copies_for(Kind kind, const Problem& q, int32_t dtype) {
+  Copies c{};
+  if (dtype != MCCE_BF16 || tensor_applicable(kind, q, dtype)) return c;
+  auto fits = [](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; };
+  const int64_t rows = q.L * q.groups.R, G = q.groups.G;
+  const int two = q.gated ? 2 : 1;
+  c.x = kind != kBackward && !fits(q.x, q.ld_x);
+  c.y = kind != kForward && !(fits(q.y, q.ld_y) && (!q.gated || q.half_y % 8 == 0));
+  c.w = kind != kDweight && !(fits(q.w, q.ld_w) && fits(q.w_up, q.ld_w) && (G == 1 || q.step_w % 8 == 0));
+  auto size = [](int64_t r, int64_t cols) { return ((size_t)r * cols * 2 + 255) & ~(size_t)255; };
+  if (c.x) c.x_bytes = size(rows, whole_8(q.k));
+  if (c.y) c.y_bytes = size(rows, two * whole_8(q.n));
+  if (c.w) c.w_bytes = size(G * q.n, whole_8(q.k));
+  const double pipe = 2.0 * rows * q.n * q.k * two / 25e12, copied = c.bytes(q.gated) * 2.0 / 4e12 + 10e-6;
+  if (rows == 0 || pipe < 2 * copied) c = Copies{};
+  return c;
+}
+// Copies in front of a product: q then names them.
+cudaError_t run_copies(const Copies& c, Problem& q, void* workspace, cudaStream_t st) {
+  uint8_t* to = (uint8_t*)workspace;
+  const int64_t rows = q.L * q.groups.R, k8 = whole_8(q.k), n8 = whole_8(q.n);
+  cudaError_t err = cudaSuccess;
+  if (c.x) {
+    err = run_align(q.x, rows, rows, q.k, q.ld_x, 0, to, k8, st);
+    q.x = to, q.ld_x = k8, to += c.x_bytes;
+  }
+  if (c.y) {
+    for (int h = 0; h < (q.gated ? 2 : 1) && err == cudaSuccess; ++h)
+      err = run_align((const __nv_bfloat16*)q.y + h * q.half_y, rows, rows, q.n, q.ld_y, 0, (__nv_bfloat16*)to + h * n8, (q.gated ? 2 : 1) * n8, st);
+    q.y = to, q.ld_y = (q.gated ? 2 : 1) * n8, q.half_y = n8, to += c.y_bytes;
+  }
+  if (c.w) {
+    for (int h = 0; h < (q.gated ? 2 : 1) && err == cudaSuccess; ++h) {
+      const void*& w = h ? q.w_up : q.w;
+      err = run_align(w, (int64_t)q.groups.G * q.n, q.n, q.k, q.ld_w, q.step_w, to, k8, st);
+      w = to, to += c.w_bytes;
+    }
+    q.ld_w = k8, q.step_w = (int64_t)q.n * k8;
+  }
+  return err;
+}
+cudaError_t run_product(Kind kind, Problem& q, int32_t dtype, void* workspace, cudaStream_t st) {
+  const Copies c = copies_for(kind, q, dtype);
+  if (c.bytes(q.gated)) {
+    const cudaError_t err = run_copies(c, q, workspace, st);
+    if (err != cudaSuccess) return err;
+  }
+  if (kind == kForward && few_applicable(q, dtype)) return run_few(q, st);
+  return tensor_applicable(kind, q, dtype) ? run_tensor(kind, q, st) : run_general(kind, q, dtype, st);
+}
+
 // Workspace of the weight gradient: 8-bit rows in the type of dout, then the parts of the bias's gradient.
 size_t unpacked_bytes(const mcce_linear& p) {
   if (p.saved_dtype != MCCE_E4M3) return 0;
   const int64_t ld = (p.k + 7) & ~7ll;
-  return ((size_t)(p.n_layers * p.rows) * ld * elem(p.dtype) + 15) & ~(size_t)15;
+  return ((size_t)(p.n_layers * p.rows) * ld * elem(p.dtype) + 255) & ~(size_t)255;
 }
 size_t bias_bytes(const mcce_linear& p) {
   const int32_t G = p.n_layers * p.n_experts;
   const int chunks = bias_chunks(p.n_layers * p.rows, G, p.n);
-  return chunks > 1 ? (size_t)chunks * (1 + p.gated) * G * p.n * 4 : 0;
+  return chunks > 1 ? ((size_t)chunks * (1 + p.gated) * G * p.n * 4 + 255) & ~(size_t)255 : 0;
+}
+
+// dout and x as the products see them: 8-bit x is unpacked to rows of whole 16 bytes first
+Problem dweight_problem(const mcce_linear& p, const void* dout, const void* x) {
+  Problem q = problem(p, nullptr);
+  q.y = dout, q.ld_y = ld_or(p.ld_y, (int64_t)p.n * (1 + p.gated)), q.x = x, q.ld_x = ld_or(p.ld_x, p.k);
+  if (p.saved_dtype == MCCE_E4M3) q.x = nullptr, q.ld_x = whole_8(p.k);
+  return q;
 }
 
 }  // namespace
@@ -641,7 +747,7 @@ using namespace mcce::linear;
 
 extern "C" int mcce_expert_linear(const mcce_linear* p, const void* x, const int32_t* offsets, const void* w, const void* w_up,
                                   const void* bias, const void* bias_up, const void* add, void* out, void* saved, void* scales,
-                                  void* cuda_stream) {
+                                  void* workspace, size_t workspace_bytes, void* cuda_stream) {
   if (!sizes_ok(p) || !act_ok(p->act)) return MCCE_EINVAL;
   const int64_t width = (int64_t)p->n * (1 + p->gated), rows = p->n_layers * p->rows;
   if (p->out_dtype != MCCE_F32 && p->out_dtype != p->dtype) return MCCE_EINVAL;
@@ -673,18 +779,21 @@ extern "C" int mcce_expert_linear(const mcce_linear* p, const void* x, const int
   const Span sb = flat_span(bias, G * p->n, eb), sbu = flat_span(bias_up, G * p->n, eb);
   const Span sadd = row_span(add, rows, f.ld_add, p->n, eo), sout = row_span(out, rows, f.ld_out, p->n, eo);
   const Span ssv = row_span(saved, rows, f.ld_saved, width, es), ssc = flat_span(scales, rows, (1 + p->gated) * (int64_t)f.blocks);
+  const size_t need = copies_for(kForward, q, p->dtype).bytes(q.gated);
+  if (need && (!workspace || !aligned(workspace, 16))) return MCCE_EINVAL;
+  if (workspace_bytes < need) return MCCE_ENOSPC;
+  const Span sws = flat_span(need ? workspace : nullptr, need);
   if (!same_or_apart(sout, sadd) || !apart(sout, {&sx, &soff, &sw, &swu, &sb, &sbu, &ssv, &ssc}) ||
-      !apart(ssv, {&sx, &soff, &sw, &swu, &sb, &sbu, &sadd, &ssc}) || !apart(ssc, {&sx, &soff, &sw, &swu, &sb, &sbu, &sadd}))
+      !apart(ssv, {&sx, &soff, &sw, &swu, &sb, &sbu, &sadd, &ssc}) || !apart(ssc, {&sx, &soff, &sw, &swu, &sb, &sbu, &sadd}) ||
+      !apart(sws, {&sx, &soff, &sw, &swu, &sb, &sbu, &sadd, &sout, &ssv, &ssc}))
     return MCCE_EINVAL;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  if (few_applicable(q, p->dtype)) return code(run_few(q, st));
-  if (tensor_applicable(kForward, q, p->dtype)) return code(run_tensor(kForward, q, st));
-  return code(run_general(kForward, q, p->dtype, st));
+  return code(run_product(kForward, q, p->dtype, workspace, st));
 }
 
 extern "C" int mcce_expert_linear_backward(const mcce_linear* p, const void* dout, const int32_t* offsets, const void* w,
                                            const void* w_up, const void* add, const void* saved, const void* scales, void* dx, void* h,
-                                           void* cuda_stream) {
+                                           void* workspace, size_t workspace_bytes, void* cuda_stream) {
   if (!sizes_ok(p) || !act_ok(p->act) || p->below < 0 || p->below > 2) return MCCE_EINVAL;
   const int64_t width = (int64_t)p->n * (1 + p->gated), wide = p->below == 2 ? 2ll * p->k : p->k, rows = p->n_layers * p->rows;
   if (saved && p->saved_dtype != p->dtype && p->saved_dtype != MCCE_E4M3) return MCCE_EINVAL;
@@ -713,17 +822,32 @@ extern "C" int mcce_expert_linear_backward(const mcce_linear* p, const void* dou
   const Span ssv = row_span(saved, rows, b.ld_saved, wide, es);
   const Span ssc = flat_span(scales, rows, (p->below == 2 ? 2 : 1) * (int64_t)b.blocks);
   const Span sdx = row_span(dx, rows, b.ld_dx, wide, e), sh = row_span(h, rows, b.ld_h, p->k, e);
-  if (!same_or_apart(sdx, sadd) || !(bytes ? apart(sdx, {&ssv}) : same_or_apart(sdx, ssv)) || !apart(sdx, {&sy, &soff, &sw, &swu, &ssc, &sh}) ||
+  const size_t need = copies_for(kBackward, q, p->dtype).bytes(q.gated);
+  if (need && (!workspace || !aligned(workspace, 16))) return MCCE_EINVAL;
+  if (workspace_bytes < need) return MCCE_ENOSPC;
+  const Span sws = flat_span(need ? workspace : nullptr, need);
+  if (!apart(sws, {&sy, &soff, &sw, &swu, &sadd, &ssv, &ssc, &sdx, &sh}) || !same_or_apart(sdx, sadd) || !(bytes ? apart(sdx, {&ssv}) : same_or_apart(sdx, ssv)) || !apart(sdx, {&sy, &soff, &sw, &swu, &ssc, &sh}) ||
       !apart(sh, {&sy, &soff, &sw, &swu, &sadd, &ssv, &ssc}))
     return MCCE_EINVAL;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  if (tensor_applicable(kBackward, q, p->dtype)) return code(run_tensor(kBackward, q, st));
-  return code(run_general(kBackward, q, p->dtype, st));
+  return code(run_product(kBackward, q, p->dtype, workspace, st));
 }
 
-extern "C" size_t mcce_expert_linear_dweight_workspace_bytes(const mcce_linear* p) {
+extern "C" size_t mcce_expert_linear_workspace_bytes(const mcce_linear* p, const void* x, const void* w, const void* w_up) {
   if (!sizes_ok(p)) return 0;
-  return unpacked_bytes(*p) + bias_bytes(*p);
+  Problem q = problem(*p, nullptr);
+  q.x = x, q.w = w, q.w_up = w_up, q.ld_x = ld_or(p->ld_x, p->k);
+  return copies_for(kForward, q, p->dtype).bytes(q.gated);
+}
+extern "C" size_t mcce_expert_linear_backward_workspace_bytes(const mcce_linear* p, const void* dout, const void* w, const void* w_up) {
+  if (!sizes_ok(p)) return 0;
+  Problem q = problem(*p, nullptr);
+  q.y = dout, q.w = w, q.w_up = w_up, q.ld_y = ld_or(p->ld_y, (int64_t)p->n * (1 + p->gated));
+  return copies_for(kBackward, q, p->dtype).bytes(q.gated);
+}
+extern "C" size_t mcce_expert_linear_dweight_workspace_bytes(const mcce_linear* p, const void* dout, const void* x) {
+  if (!sizes_ok(p)) return 0;
+  return unpacked_bytes(*p) + bias_bytes(*p) + copies_for(kDweight, dweight_problem(*p, dout, x), p->dtype).bytes(p->gated);
 }
 
 extern "C" int mcce_expert_linear_dweight(const mcce_linear* p, const void* dout, const void* x, const void* scales,
@@ -746,7 +870,7 @@ extern "C" int mcce_expert_linear_dweight(const mcce_linear* p, const void* dout
   if (!aligned(dout, e) || !aligned(x, ex) || !aligned(offsets, 4) || !aligned(add_dw, eo) || !aligned(add_dw_up, eo) || !aligned(add_db, eo) ||
       !aligned(add_db_up, eo) || !aligned(dw, eo) || !aligned(dw_up, eo) || !aligned(db, eo) || !aligned(db_up, eo))
     return MCCE_EINVAL;
-  const size_t need = mcce_expert_linear_dweight_workspace_bytes(p);
+  const size_t need = mcce_expert_linear_dweight_workspace_bytes(p, dout, x);
   if (need && (!workspace || !aligned(workspace, 16))) return MCCE_EINVAL;
   if (workspace_bytes < need) return MCCE_ENOSPC;
   Problem q = problem(*p, offsets);
@@ -775,9 +899,10 @@ extern "C" int mcce_expert_linear_dweight(const mcce_linear* p, const void* dout
     if (err != cudaSuccess) return MCCE_ECUDA;
     q.x = workspace, q.ld_x = ld;
   }
-  cudaError_t err = tensor_applicable(kDweight, q, p->dtype) ? run_tensor(kDweight, q, st) : run_general(kDweight, q, p->dtype, st);
+  const Problem given = q;   // the bias's gradient reads dout where it is
+  cudaError_t err = run_product(kDweight, q, p->dtype, (uint8_t*)workspace + unpacked_bytes(*p) + bias_bytes(*p), st);
   if (err == cudaSuccess && db) 
-    err = run_bias_sums(q, p->dtype, add_db, add_db_up, db, db_up, (float*)((uint8_t*)workspace + unpacked_bytes(*p)), st);
+    err = run_bias_sums(given, p->dtype, add_db, add_db_up, db, db_up, (float*)((uint8_t*)workspace + unpacked_bytes(*p)), st);
   return code(err);
 }
 

@@ -422,7 +422,7 @@ struct Backward {
 struct Problem {
   Groups groups;
   int32_t n, k, gated;             // sizes of the weights [n, k]; two of them when gated
-  int64_t L, ld_x, ld_y, ld_w, step_w;   // y: out (forward), dout (the gradients)
+  int64_t L, ld_x, ld_y, ld_w, step_w, half_y;   // y: dout (the gradients), its second half half_y columns on
   const void *x, *y, *w, *w_up;    // forward: x, w; backward: y, w; dweight: y, x
   void *dw, *dw_up;                // dweight
   const void *add_dw, *add_dw_up;
@@ -475,6 +475,7 @@ cudaError_t run_tensor(Kind kind, const Problem& p, cudaStream_t st);
 int bias_chunks(int64_t rows, int32_t G, int32_t n);   // more than one: run_bias_sums needs `parts`
 cudaError_t run_bias_sums(const Problem& p, int32_t dtype, const void* add, const void* add_up, void* db, void* db_up, float* parts,
                           cudaStream_t st);
+cudaError_t run_align(const void* from, int64_t rows, int64_t per, int32_t cols, int64_t ld, int64_t step, void* to, int64_t ld_to, cudaStream_t st);
 cudaError_t run_pack(const void* x, int32_t dtype, int64_t rows, int32_t d, int64_t ld_x, int64_t ld_q, uint8_t* q, uint8_t* scales,
                      cudaStream_t st);
 cudaError_t run_unpack(const uint8_t* q, const uint8_t* scales, int32_t dtype, int64_t rows, int32_t d, int64_t ld_x, int64_t ld_q, void* x,

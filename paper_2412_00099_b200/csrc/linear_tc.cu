@@ -798,7 +798,7 @@ cudaError_t launch(const Problem& p, cudaStream_t st) {
     ok = true;
     for (int i = 0; i < 2; ++i)
       ok = ok && map_panels(&m.a[i], y, 1, rows, p.n, p.ld_y, 0, 128 >> i) && map_panels(&m.b[i], p.x, 1, rows, p.k, p.ld_x, 0, 128 >> i) &&
-           (!GATED || map_panels(&m.a_up[i], y + p.n, 1, rows, p.n, p.ld_y, 0, 128 >> i));
+           (!GATED || map_panels(&m.a_up[i], y + p.half_y, 1, rows, p.n, p.ld_y, 0, 128 >> i));
   } else if (KIND == kForward) {
     const int box = GATED ? kTileM / 2 : kTileM;
     ok = map_weights(&m.a[0], p.w, p, box, &m.a_whole, &m.a_step) && (!GATED || map_weights(&m.a_up[0], p.w_up, p, box, &m.a_whole, &m.a_step)) &&
@@ -807,7 +807,7 @@ cudaError_t launch(const Problem& p, cudaStream_t st) {
     m.a_whole = whole(p.k);
     ok = map_panels(&m.a[0], p.w, p.groups.G, p.n, p.k, p.ld_w, p.step_w, C::kSlab) &&
          (!GATED || map_panels(&m.a_up[0], p.w_up, p.groups.G, p.n, p.k, p.ld_w, p.step_w, C::kSlab));
-    ok = ok && map_boxes(m.b, y, rows, p.n, p.ld_y, C::kRowBox) && (!GATED || map_boxes(m.b_up, y + p.n, rows, p.n, p.ld_y, C::kRowBox));
+    ok = ok && map_boxes(m.b, y, rows, p.n, p.ld_y, C::kRowBox) && (!GATED || map_boxes(m.b_up, y + p.half_y, rows, p.n, p.ld_y, C::kRowBox));
   }
   if (!ok || most > 0x7fffffffll) return cudaErrorInvalidValue;
   int ctas = C::kCtas;
@@ -851,10 +851,10 @@ bool tma_rows(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld
 
 bool tensor_applicable(Kind kind, const Problem& p, int32_t dtype) {
   if (dtype != MCCE_BF16) return false;
-  if (kind == kDweight) return p.L * p.groups.R > 0 && tma_rows(p.y, p.ld_y) && tma_rows(p.x, p.ld_x) && (!p.gated || p.n % 8 == 0);
+  if (kind == kDweight) return p.L * p.groups.R > 0 && tma_rows(p.y, p.ld_y) && tma_rows(p.x, p.ld_x) && (!p.gated || p.half_y % 8 == 0);
   if (!tma_rows(p.w, p.ld_w) || !tma_rows(p.w_up, p.ld_w) || (p.groups.G > 1 && (p.step_w % 8 || p.step_w >= kMostStride))) return false;
   if (kind == kForward) return tma_rows(p.x, p.ld_x);
-  return tma_rows(p.y, p.ld_y) && (!p.gated || p.n % 8 == 0);
+  return tma_rows(p.y, p.ld_y) && (!p.gated || p.half_y % 8 == 0);
 }
 
 cudaError_t run_tensor(Kind kind, const Problem& p, cudaStream_t st) {

@@ -27,7 +27,9 @@ decltype(&mcce_dispatch_workspace_bytes) p_dispatch_workspace_bytes;
 decltype(&mcce_dispatch) p_dispatch;
 decltype(&mcce_combine) p_combine;
 decltype(&mcce_combine_backward) p_combine_backward;
+decltype(&mcce_expert_linear_workspace_bytes) p_expert_linear_workspace_bytes;
 decltype(&mcce_expert_linear) p_expert_linear;
+decltype(&mcce_expert_linear_backward_workspace_bytes) p_expert_linear_backward_workspace_bytes;
 decltype(&mcce_expert_linear_backward) p_expert_linear_backward;
 decltype(&mcce_expert_linear_dweight_workspace_bytes) p_expert_linear_dweight_workspace_bytes;
 decltype(&mcce_expert_linear_dweight) p_expert_linear_dweight;
@@ -401,8 +403,11 @@ void run_expert_linear(PyObject* const* a) {
     need(!scales, "scales without saved");
   }
   Where on(s.dev);
+  at::Tensor ws;
+  const size_t bytes = p_expert_linear_workspace_bytes(&p, x.data_ptr(), w.data_ptr(), at_(wu));
+  if (bytes) ws = workspace(bytes, x);
   done(p_expert_linear(&p, x.data_ptr(), (const int32_t*)off.data_ptr(), w.data_ptr(), at_(wu), at_(b), at_(bu), at_(add), out.data_ptr(),
-                       at_(saved), at_(scales), on.stream));
+                       at_(saved), at_(scales), bytes ? ws.data_ptr() : nullptr, bytes, on.stream));
   changed({&out, saved, scales});
 }
 
@@ -431,8 +436,11 @@ void run_expert_linear_backward(PyObject* const* a) {
   p.ld_add = ld(add, s.rows(s.k), s.dev, "add"), p.ld_h = ld(h, s.rows(s.k), s.dev, "h");
   p.ld_x = ld(&dx, s.rows(p.below == 2 ? 2 * s.k : s.k), s.dev, "dx");
   Where on(s.dev);
+  at::Tensor ws;
+  const size_t bytes = p_expert_linear_backward_workspace_bytes(&p, g.data_ptr(), w.data_ptr(), at_(wu));
+  if (bytes) ws = workspace(bytes, g);
   done(p_expert_linear_backward(&p, g.data_ptr(), (const int32_t*)off.data_ptr(), w.data_ptr(), at_(wu), at_(add), at_(saved), at_(scales),
-                                dx.data_ptr(), at_(h), on.stream));
+                                dx.data_ptr(), at_(h), bytes ? ws.data_ptr() : nullptr, bytes, on.stream));
   changed({&dx, h});
 }
 
@@ -452,7 +460,7 @@ void run_expert_linear_dweight(PyObject* const* a) {
   p.saved_dtype = saved_type(x, scales, g, s, 1, s.k, "x");
   Where on(s.dev);
   at::Tensor ws;
-  const size_t bytes = p_expert_linear_dweight_workspace_bytes(&p);
+  const size_t bytes = p_expert_linear_dweight_workspace_bytes(&p, g.data_ptr(), x.data_ptr());
   if (bytes) ws = workspace(bytes, g);
   done(p_expert_linear_dweight(&p, g.data_ptr(), x.data_ptr(), s.R ? at_(scales) : nullptr, (const int32_t*)off.data_ptr(), at_(adw), at_(adwu),
                                at_(adb), at_(adbu), dw.data_ptr(), at_(dwu), at_(db), at_(dbu), bytes ? ws.data_ptr() : nullptr, bytes,
@@ -512,7 +520,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyObject* connect(PyObject*, PyObject* const* args, Py_ssize_t n) {
   void** const to[] = {(void**)&p_rmsnorm, (void**)&p_rmsnorm_backward_workspace_bytes, (void**)&p_rmsnorm_backward,
                        (void**)&p_dispatch_workspace_bytes, (void**)&p_dispatch, (void**)&p_combine, (void**)&p_combine_backward,
-                       (void**)&p_expert_linear, (void**)&p_expert_linear_backward, (void**)&p_expert_linear_dweight_workspace_bytes,
+                       (void**)&p_expert_linear_workspace_bytes, (void**)&p_expert_linear, (void**)&p_expert_linear_backward_workspace_bytes,
+                       (void**)&p_expert_linear_backward, (void**)&p_expert_linear_dweight_workspace_bytes,
                        (void**)&p_expert_linear_dweight, (void**)&p_checkpoint_pack, (void**)&p_checkpoint_unpack, (void**)&p_strerror};
   constexpr int kFunctions = sizeof(to) / sizeof(to[0]);
   if (n != 1 + kFunctions) {

@@ -151,7 +151,7 @@ def some_counts(L, E, R, g, full=True):
 SHAPES = [(1, 1, 1, 1, 1), (1, 1, 1, 8, 8), (1, 4, 4, 64, 64), (1, 3, 40, 64, 128), (2, 5, 37, 72, 200), (1, 7, 300, 136, 264),
           (1, 2, 700, 320, 64), (1, 60, 64, 128, 256), (3, 4, 130, 40, 96), (1, 1, 517, 515, 259), (1, 6, 77, 33, 31),
           (1, 4, 1100, 192, 512), (1, 300, 500, 16, 24), (1, 1, 257, 1000, 1002), (1, 1, 16, 264, 4096), (1, 2, 40, 136, 2048), (1, 1, 60, 192, 1024),
-          (1, 1, 3, 100, 2056), (2, 3, 5, 72, 520), (1, 2, 600, 520, 192), (1, 1, 30, 4096, 264), (1, 3, 65, 2048, 136)]
+          (1, 1, 3, 100, 2056), (2, 3, 5, 72, 520), (1, 2, 600, 520, 192), (1, 1, 30, 4096, 264), (1, 3, 65, 2048, 136), (1, 4, 1500, 515, 1003), (2, 2, 900, 777, 1026), (1, 3, 2100, 1001, 520)]
 
 
 @pytest.mark.parametrize("shape", SHAPES, ids=str)

@@ -30,14 +30,14 @@ def lin(**kw):
     return mb.Linear(**f)
 
 
-def forward(lib, p=None, x=P[0], off=P[1], w=P[2], wu=P[3], b=P[4], bu=P[5], add=P[6], out=P[7], saved=P[8], sc=P[9]):
+def forward(lib, p=None, x=P[0], off=P[1], w=P[2], wu=P[3], b=P[4], bu=P[5], add=P[6], out=P[7], saved=P[8], sc=P[9], ws=None, nbytes=0):
     p = lin() if p is None else p
-    return lib.mcce_expert_linear(C.byref(p), x, off, w, wu, b, bu, add, out, saved, sc, None)
+    return lib.mcce_expert_linear(C.byref(p), x, off, w, wu, b, bu, add, out, saved, sc, ws, nbytes, None)
 
 
-def backward(lib, p=None, g=P[0], off=P[1], w=P[2], wu=P[3], add=None, saved=P[4], sc=P[5], dx=P[6], h=P[7]):
+def backward(lib, p=None, g=P[0], off=P[1], w=P[2], wu=P[3], add=None, saved=P[4], sc=P[5], dx=P[6], h=P[7], ws=None, nbytes=0):
     p = lin() if p is None else p
-    return lib.mcce_expert_linear_backward(C.byref(p), g, off, w, wu, add, saved, sc, dx, h, None)
+    return lib.mcce_expert_linear_backward(C.byref(p), g, off, w, wu, add, saved, sc, dx, h, ws, nbytes, None)
 
 
 def dweight(lib, p=None, g=P[0], x=P[1], sc=P[2], off=P[3], aw=P[4], awu=P[5], ab=P[6], abu=P[7], dw=P[8], dwu=P[9], db=P[10], dbu=P[11],
@@ -58,7 +58,7 @@ def test_descriptor(lib, bad):
     p.below, p.act = (1, 1)                                                       # ld_x: rows of dx
     assert backward(lib, p) == EINVAL
     if "ld_x" not in bad:
-        assert lib.mcce_expert_linear_dweight_workspace_bytes(C.byref(p)) == 0
+        assert lib.mcce_expert_linear_dweight_workspace_bytes(C.byref(p), P[0], P[1]) == 0
 
 
 def test_types_and_strides(lib):
@@ -72,8 +72,8 @@ def test_types_and_strides(lib):
 
 
 def test_missing_and_misaligned(lib):
-    assert lib.mcce_expert_linear(None, *P[:11]) == EINVAL and lib.mcce_expert_linear_backward(None, *P[:10]) == EINVAL
-    assert lib.mcce_expert_linear_dweight_workspace_bytes(None) == 0
+    assert lib.mcce_expert_linear(None, *P[:11], 0, None) == EINVAL and lib.mcce_expert_linear_backward(None, *P[:10], 0, None) == EINVAL
+    assert lib.mcce_expert_linear_dweight_workspace_bytes(None, None, None) == 0
     for name in ("x", "off", "w", "wu", "bu", "out", "sc"):
         assert forward(lib, **{name: None}) == EINVAL, name
     assert forward(lib, saved=None) == EINVAL                                     # scales without anything kept
@@ -95,11 +95,36 @@ def test_missing_and_misaligned(lib):
     assert dweight(lib, db=None, dbu=None) == EINVAL                              # something to add to a bias that is not wanted
     for name in ("g", "off", "aw", "awu", "ab", "abu", "dw", "dwu", "db", "dbu", "ws"):
         assert dweight(lib, **{name: ODD}) == EINVAL, name
-    need = lib.mcce_expert_linear_dweight_workspace_bytes(C.byref(lin()))
+    need = lib.mcce_expert_linear_dweight_workspace_bytes(C.byref(lin()), P[0], P[1])
     assert need == 2 * 10 * 32 * 2 and dweight(lib, nbytes=need - 1) == ENOSPC
-    assert lib.mcce_expert_linear_dweight_workspace_bytes(C.byref(lin(saved_dtype=mb.BF16))) == 0
+    assert lib.mcce_expert_linear_dweight_workspace_bytes(C.byref(lin(saved_dtype=mb.BF16)), P[0], P[1]) == 0
     long = lin(n_layers=1, n_experts=1, rows=100000, saved_dtype=mb.BF16)
-    assert lib.mcce_expert_linear_dweight_workspace_bytes(C.byref(long)) % (2 * 64 * 4) == 0     # parts of the bias's gradient
+    assert lib.mcce_expert_linear_dweight_workspace_bytes(C.byref(long), P[0], P[1]) % (2 * 64 * 4) == 0     # parts of the bias's gradient
+
+
+def test_workspace_for_copies(lib):
+    """bf16 rows that are not aligned to 16 bytes need a workspace where copying them pays, and only there."""
+    big = dict(n_layers=1, n_experts=2, rows=4096, gated=0, below=0, act=0, saved_dtype=mb.BF16)
+    fwd, bwd, dw = lib.mcce_expert_linear_workspace_bytes, lib.mcce_expert_linear_backward_workspace_bytes, lib.mcce_expert_linear_dweight_workspace_bytes
+    even, odd, small = lin(n=512, k=512, **big), lin(n=511, k=515, **big), lin(n=511, k=515, **dict(big, rows=16))
+    bias = 4 * 2 * 512 * 4                               # parts of the bias's gradient: four chunks of rows
+    for p in (even, small):
+        assert fwd(C.byref(p), P[0], P[1], None) == bwd(C.byref(p), P[0], P[1], None) == 0 and dw(C.byref(p), P[0], P[1]) == (bias if p is even else 0)
+    rows_x, rows_y, weights = 4096 * 520 * 2, 4096 * 512 * 2, (2 * 511 * 520 * 2 + 255) // 256 * 256
+    assert fwd(C.byref(odd), P[0], P[1], None) == rows_x + weights and dw(C.byref(odd), P[0], P[1]) == rows_x + rows_y + bias
+    assert bwd(C.byref(odd), P[0], P[1], None) == rows_y + weights
+    assert fwd(C.byref(even), at(P[0], 2), P[1], None) == 4096 * 512 * 2 and fwd(C.byref(lin(n=511, k=515, **dict(big, dtype=mb.F32, saved_dtype=mb.F32))), P[0], P[1], None) == 0
+    assert fwd(None, P[0], P[1], None) == bwd(None, P[0], P[1], None) == 0
+    need = rows_x + weights
+    a = dict(wu=None, b=None, bu=None, add=None, saved=None, sc=None)
+    assert forward(lib, odd, ws=None, nbytes=need, **a) == EINVAL and forward(lib, odd, ws=at(P[15], 8), nbytes=need, **a) == EINVAL
+    assert forward(lib, odd, ws=P[15], nbytes=need - 1, **a) == ENOSPC
+    for other in (P[0], P[2], P[7]):
+        assert forward(lib, odd, ws=at(other, 16), nbytes=need, **a) == EINVAL
+    a = dict(wu=None, saved=None, sc=None, h=None)
+    assert backward(lib, odd, ws=P[15], nbytes=rows_y + weights - 1, **a) == ENOSPC and backward(lib, odd, nbytes=1 << 30, **a) == EINVAL
+    for other in (P[0], P[2], P[6]):
+        assert backward(lib, odd, ws=at(other, 16), nbytes=need, **a) == EINVAL
 
 
 def test_nothing_to_do(lib):
