@@ -1,6 +1,6 @@
 // The experts' products on sorted rows on the 5th-generation tensor cores (bf16 rows and weights, fp32 sums).
 //
-// All three are products whose reduction lies along K-slabs of 64:
+// All three are products whose reduction lies along slabs of 64 (dweight: 128):
 //   forward   D[feature, row] = sum_k w[feature, k] x[row, k]                  both operands with k along their rows
 //   backward  D[feature, row] = sum_j w[j, feature] dout[row, j]               weights across their rows
 //   dweight   D[j, feature]   = sum_r dout[r, j] x[r, feature]                 both across their rows; r runs over the group's rows
@@ -8,9 +8,9 @@
 // where 128-row tiles of tokens would waste a third of the work at 250 rows per expert.  A gated forward tile has 64 features: 64
 // gate rows, then 64 up rows, so that two epilogue warps hold gate and up of the same features and swap half of their rows.
 //
-// One CTA per SM walks the tiles.  Warp 0 issues TMA loads into a ring of stages, warp 1 the MMAs into one of two TMEM buffers, eight warps
-// bring the other buffer to memory, a feature per lane.  Every wait is bounded: when one gives up, the CTA notes it, lets its copies land, frees
-// its TMEM and returns.
+// One CTA per SM, or a pair on two, walks the tiles.  Warp 0 issues TMA loads into a ring of stages, warp 1 the MMAs into one of two TMEM buffers, 8 or 16
+// warps bring the other buffer to memory: from a feature per lane, as TMEM gives it, through shared memory to eight columns of a row per lane.
+// Every wait is bounded: when one gives up, the CTA notes it, lets its copies land, frees its TMEM and returns.
 #include <cuda.h>
 
 #include <type_traits>
@@ -41,7 +41,7 @@ struct Cfg {
   static constexpr int kCtas = PAIR ? 2 : 1;
   static constexpr int kFeatures = kTileM * kCtas / (KIND == kForward && GATED ? 2 : 1);   // of a tile
   // Reduction per stage.  Along an operand's rows 64 bf16 are a swizzled row of 128 bytes; dweight's operands lie across their rows, and the fewer copies of
-  // 128 rows win (8192 x 4096 x 4096: 193 us, with 64 rows 220).
+  // 128 rows win (8192 x 4096 x 4096: 197 us, with 64 rows 203).
   static constexpr int kSlab = KIND == kDweight ? 128 : 64;
   static constexpr uint32_t kABytes = kTileM * kSlab * 2;
   static constexpr uint32_t kBBytes = BN / kCtas * kSlab * 2;
@@ -155,9 +155,14 @@ __device__ __forceinline__ uint32_t leaders(uint32_t addr) {   // the same place
 __device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-// mbar_wait for what other CTAs of the cluster wrote
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* err, uint32_t code) {
-  const bool ok = mbar_wait(bar, parity, abort_flag, err, code);
+// mbar_wait by a whole warp, with one answer: lanes that went on while another gives up would wait for it without a limit
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* err, uint32_t code,
+                                          unsigned long long limit_ns = kWaitLimitNs) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, err, code, limit_ns));
+}
+// The same for what other CTAs of the cluster wrote
+__device__ __forceinline__ bool warp_wait_cluster(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* err, uint32_t code) {
+  const bool ok = warp_wait(bar, parity, abort_flag, err, code);
   asm volatile("fence.acq_rel.cluster;" ::: "memory");
   return ok;
 }
@@ -464,18 +469,16 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
       const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)cols >> 3 << 17) | ((uint32_t)(kTileM * C::kCtas) >> 4 << 24) |
                              (KIND != kForward ? 1u << 15 : 0u) | (KIND == kDweight ? 1u << 16 : 0u);
       const uint32_t buf = acc & 1u;
-      if (!mbar_wait(bar_tempty + 8 * buf, ((acc >> 1) & 1u) ^ 1u, abort_flag, &wait_error, 2u)) break;
+      if (!warp_wait(bar_tempty + 8 * buf, ((acc >> 1) & 1u) ^ 1u, abort_flag, &wait_error, 2u)) break;
       ++acc;
       tc_fence_after();
       const uint32_t d = tmem_base + buf * BN;
+      bool ok = true;   // one answer per tile, as in warp_wait (asked for every slab it cost a large product 2 %); after a "no" the slabs pass idly
       for (int kt = from; kt < to; ++kt) {
-        if (!mbar_wait(bar_full + 8 * stage, phase, abort_flag, &wait_error, 3u)) {
-          alive = false;
-          break;
-        }
+        ok = ok && mbar_wait(bar_full + 8 * stage, phase, abort_flag, &wait_error, 3u);
         const int left = KIND == kDweight ? it.rows - kt * C::kSlab : C::kSlab;
         tc_fence_after();
-        if (lane == 0) {
+        if (lane == 0 && ok) {
           const uint64_t ad = a_first + stage * (C::kStageBytes >> 4), bd = b_first + stage * (C::kStageBytes >> 4);
           // from one 16 of the reduction to the next: 32 bytes along a swizzled row, 16 rows across
           constexpr uint32_t kStepA = (KIND == kForward ? 32 : 2048) >> 4, kStepB = (KIND == kDweight ? 2048 : 32) >> 4;
@@ -491,6 +494,7 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
         __syncwarp();
         if (++stage == C::kStages) stage = 0, phase ^= 1u;
       }
+      alive = __all_sync(0xffffffffu, ok);
       if (alive && lane == 0) commit<PAIR>(bar_tfull + 8 * buf);
       __syncwarp();
     }
@@ -503,7 +507,7 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
       if (slabs == 0) continue;
       stage = (stage + slabs - 1) % C::kStages;
       if (valid < C::kSlab) {
-        if (!mbar_wait(bar_tail + 8 * stage, (tails >> stage) & 1u, abort_flag, &wait_error, 6u)) break;
+        if (!warp_wait(bar_tail + 8 * stage, (tails >> stage) & 1u, abort_flag, &wait_error, 6u)) break;
         tails ^= 1u << stage;
         // a row's 128 bytes in two panels of dout and two of x at a time
         const int panel = (valid <= 64 ? 64 : C::kSlab) * 128;
@@ -535,7 +539,7 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
         Backward<__nv_bfloat16>(p.bwd, it.g, it.f0 + quad * 32 + 8 * (lane & 3)).ask((int64_t)it.row + 8 * team, it.rows - 8 * team, asked);
       if (sums) {
         // a tile's sums may take long: 20 us per slab more than any other wait
-        if (!mbar_wait(bar_tfull + 8 * buf, (acc >> 1) & 1u, abort_flag, &wait_error, 4u, kWaitLimitNs + 20000ull * (to - from))) break;
+        if (!warp_wait(bar_tfull + 8 * buf, (acc >> 1) & 1u, abort_flag, &wait_error, 4u, kWaitLimitNs + 20000ull * (to - from))) break;
         ++acc;
         tc_fence_after();
       }
@@ -559,7 +563,7 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
           if (lane == 0) arrive_at(leaders(bar_parts));
           break;
         }
-        if (cluster_size() > 1 && !mbar_wait_cluster(bar_parts, 0u, abort_flag, &wait_error, 7u)) break;
+        if (cluster_size() > 1 && !warp_wait_cluster(bar_parts, 0u, abort_flag, &wait_error, 7u)) break;
       }
       auto add_parts = [&](auto& v, int c) {
         if constexpr (SHARE == kSplit) {
@@ -614,19 +618,19 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
               asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             }
           }
-        } else
-        for (int c = 32 * team; c < cols && first_row < p.n; c += 64) {
-          float v[32] = {};
-          __syncwarp();   // the loads from TMEM take the whole warp
-          if (sums) {
-            tmem_ld32(t0 + c, v);
-            tmem_ld_wait();
+        } else if (first_row < p.n) {
+          for (int c = 32 * team; c < cols; c += 64) {
+            float v[32] = {};
+            __syncwarp();   // the loads from TMEM take the whole warp
+            if (sums) {
+              tmem_ld32(t0 + c, v);
+              tmem_ld_wait();
+            }
+            typedef __nv_bfloat16 B;
+            const int rows = p.n - first_row;
+            if (p.dw_f32) store_block(buffer, v, (float*)dw + at + c, add ? (const float*)add + at + c : nullptr, p.ld_w, rows, cols - c, p.dw_wide);
+            else store_block(buffer, v, (B*)dw + at + c, add ? (const B*)add + at + c : nullptr, p.ld_w, rows, cols - c, p.dw_wide);
           }
-          if (p.dw_f32)
-            store_block(buffer, v, (float*)dw + at + c, add ? (const float*)add + at + c : nullptr, p.ld_w, p.n - first_row, cols - c, p.dw_wide);
-          else
-            store_block(buffer, v, (__nv_bfloat16*)dw + at + c, add ? (const __nv_bfloat16*)add + at + c : nullptr, p.ld_w, p.n - first_row, cols - c,
-                        p.dw_wide);
         }
       } else if constexpr (KIND == kForward && GATED) {
         // quadrants 0 and 1 hold z, 2 and 3 z_up of the same 64 features; of every 16 rows the first 8 are finished by the warp that holds z
@@ -643,7 +647,7 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
           for (int j = 0; j < 16; ++j) both[(up * 16 + j) * kSwapStride + lane] = v[j];
           __syncwarp();
           if (lane == 0) mbar_arrive(bar_swap + 8 * pair);
-          if (!mbar_wait(bar_swap + 8 * pair, swaps & 1u, abort_flag, &wait_error, 5u)) {
+          if (!warp_wait(bar_swap + 8 * pair, swaps & 1u, abort_flag, &wait_error, 5u)) {
             alive = false;
             break;
           }
