@@ -411,7 +411,7 @@ typedef struct {
  *       8 bits.  Blocks do not reach from z into z_up.
  *   workspace DEVICE, 16-byte aligned, as many bytes as the call of that name answers for these addresses, which it only looks at (0 is usual: it may
  *       be NULL then).  It takes copies of bf16 rows and weights whose starts or strides are no multiples of 16 bytes, where that pays.
- * bf16 rows and weights meet on the tensor cores, whose fp32 accumulation truncates: a sum of k products is within 2^-24 k / 8 of its
+ * bf16 rows and weights meet on the tensor cores, whose fp32 accumulation truncates: a sum of k products is within (k + 8) 2^-24 of its
  * terms' magnitudes. */
 size_t mcce_expert_linear_workspace_bytes(const mcce_linear* p /*HOST*/, const void* x, const void* w, const void* w_up);
 int mcce_expert_linear(const mcce_linear* p /*HOST*/, const void* x, const int32_t* offsets, const void* w, const void* w_up,
@@ -435,7 +435,7 @@ int mcce_expert_linear_backward(const mcce_linear* p /*HOST*/, const void* dout,
 
 /* Its gradient with respect to weights and bias:  dw_g = add_dw_g + sum over the group's rows of dout_r^T x_r,
  * db_g = add_db_g + sum of dout_r; gated: dw_up and db_up from the second half of dout's columns.  A group without rows gets what is added, or 0.
- *   dout as above;    x DEVICE dtype [L,rows,k], or with scales (bytes, [L,rows,ceil(k/32)]) e4m3, stride ld_x
+ *   dout as above;    x DEVICE saved_dtype [L,rows,k], stride ld_x: dtype, or e4m3 with scales (bytes, [L,rows,ceil(k/32)])
  *   dw, dw_up DEVICE out_dtype [L,E,n,k] out (dw_up exactly when gated);    db, db_up DEVICE out_dtype [L,E,n] out, contiguous, or NULL
  *   add_dw, add_dw_up, add_db, add_db_up: like dw .. db_up, or NULL; each may be that output itself
  * 8-bit x is brought to dtype in the workspace, which is exact for scales of 2^-117 and more. */

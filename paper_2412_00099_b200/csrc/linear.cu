@@ -311,17 +311,22 @@ __global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads, KIND != kFo
   }
 }
 
+// CTAs per tile: as many as a full device has room for at once and as leave each of them eight steps (4 rows x 2034 x 64 fp32: 62 us alone, 13 shared;
+// 900 x 1002 x 515, 270 tiles: 70 and 53).
+int64_t reduction(Kind kind, const Problem& p) { return kind == kForward ? p.k : kind == kBackward ? p.n : p.L * p.groups.R / p.groups.G; }
+int general_ctas(Kind kind, const Problem& p, int64_t tiles, int sms) {
+  int ctas = 8;
+  while (ctas > 1 && (tiles * ctas > 6 * sms || reduction(kind, p) < 8 * kDeep * ctas)) ctas /= 2;
+  return ctas;
+}
+
 template <Kind KIND, typename T, bool GATED, int V>
 cudaError_t launch_tiles(const Problem& p, int64_t tiles, int sms, cudaStream_t st) {
   static int cache[64] = {0};
   constexpr size_t kBytes = General<KIND, T, GATED>::kFloats * 4;
   const cudaError_t e = tc::sm_count_and_smem_optin(general_kernel<KIND, T, GATED, V>, kBytes + (MCCE_LINEAR_MAX_GROUPS + 1 + 33) * 4, cache, &sms);
   if (e != cudaSuccess) return e;
-  // CTAs per tile: as many as a full device has room for at once and as leave each of them eight steps (4 rows x 2034 x 64 fp32: 62 us alone, 13 shared;
-  // 900 x 1002 x 515, 270 tiles: 70 and 53)
-  const int64_t red = KIND == kForward ? p.k : KIND == kBackward ? p.n : p.L * p.groups.R / p.groups.G;
-  int ctas = 8;
-  while (ctas > 1 && (tiles * ctas > 6 * sms || red < 8 * kDeep * ctas)) ctas /= 2;
+  const int ctas = general_ctas(KIND, p, tiles, sms);
   const int64_t most = 8 * sms / ctas;
   return launch_close(general_kernel<KIND, T, GATED, V>, dim3((unsigned)((tiles < most ? tiles : most) * ctas)), General<KIND, T, GATED>::kThreads,
                       kBytes + (size_t)(p.groups.G + 1 + 33) * 4, st, ctas, p);
@@ -660,7 +665,7 @@ int blocks_of(int64_t cols) { return (int)((cols + 31) / 32); }
 int code(cudaError_t e) { return e == cudaSuccess ? MCCE_OK : MCCE_ECUDA; }
 
 // bf16 rows that the tensor cores' copies cannot take (a stride or start that is no multiple of 16 bytes) are brought to one that is, where that pays: on the fp32
-// pipe a product runs at some 25 TFLOP/s (4096 x 2047 x 511, gated: 800 us), the copies at some 4 TB/s.
+// pipe bf16 products run at 10 to 20 TFLOP/s (4096 x 2047 x 511, gated: 800 us, copied 74), the copies at some 4 TB/s.
 struct Copies {
   bool x, y, w;
   size_t x_bytes, y_bytes, w_bytes;   // w: of one matrix of every group
@@ -680,9 +685,12 @@ Copies copies_for(Kind kind, const Problem& q, int32_t dtype) {
   if (c.x) c.x_bytes = size(rows, whole_8(q.k));
   if (c.y) c.y_bytes = size(rows, two * whole_8(q.n));
   if (c.w) c.w_bytes = size(G * q.n, whole_8(q.k));
-  const double pipe = 2.0 * rows * q.n * q.k * two / 25e12, copied = c.bytes(q.gated) * 2.0 / 4e12 + 10e-6;
-  if (rows == 0 || pipe < 2 * copied) c = Copies{};
-  return c;
+  if (rows == 0) return Copies{};
+  // the fp32 pipe: its rate, and 0.4 us for every step of a CTA; the tensor cores: the copies, and their launches with the product's shortest time
+  const int64_t tiles = (rows / 32 + G) * (((kind == kForward ? q.n : q.k) + 63) / 64);
+  const double steps = (double)reduction(kind, q) / kDeep / general_ctas(kind, q, tiles, 148);
+  const double pipe = 2.0 * rows * q.n * q.k * two / 12e12 + steps * 0.4e-6, tensor = c.bytes(q.gated) * 2.0 / 4e12 + 22e-6;
+  return pipe > tensor ? c : Copies{};
 }
 // Copies in front of a product: q then names them.
 cudaError_t run_copies(const Copies& c, Problem& q, void* workspace, cudaStream_t st) {
