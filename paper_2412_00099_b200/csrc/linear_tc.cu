@@ -516,7 +516,9 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) {
-          if (PAIR) arrive_at(leaders(bar_full + 8 * stage));
+          // The leader's MMAs read this CTA's rows, so rank 1 arrives with a cluster-wide release: 20 us of 254 at 64 groups of 500 rows, but a
+          // relaxed arrival would leave the clearing unordered.  Copies of 16 rows and of one, zeros from behind the operand's end, took 353.
+          if (rank != 0) arrive_at(leaders(bar_full + 8 * stage));
           else mbar_arrive(bar_full + 8 * stage);
         }
       }

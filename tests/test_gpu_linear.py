@@ -439,6 +439,29 @@ def test_one_experts_nan_stays_its_own(T):
     assert (r.dw[2] == 0).all() and (r.db[2] == 0).all()
 
 
+@pytest.mark.parametrize("n,k", [(192, 136), (72, 320), (256, 256)])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("T", [BF16, F32])
+def test_dweight_of_every_number_of_rows(T, gated, n, k):
+    """Groups of 0 to 140 rows, every third full of NaN.  Small integers: the sums (below 9 * 140) are exact in fp32."""
+    g = gen(n + k)
+    counts = torch.randperm(141, generator=torch.Generator().manual_seed(k)).tolist()
+    two, R, off = 1 + gated, sum(counts), offsets_of([counts])[0]
+    dout = torch.randint(-3, 4, (R, two * n), device="cuda", generator=g).to(T)
+    x = torch.randint(-3, 4, (R, k), device="cuda", generator=g).to(T)
+    want = [torch.stack([dout[a:b, i * n:(i + 1) * n].double().T @ x[a:b].double() for a, b in zip(off.tolist(), off.tolist()[1:])]) for i in range(two)]
+    bad = [e for e in range(141) if e % 3 == 1 and counts[e]]
+    for e in bad:
+        dout[off[e]:off[e + 1]], x[off[e]:off[e + 1]] = float("nan"), float("inf")
+    ours = [e for e in range(141) if e not in bad]
+    for O in ([F32, BF16] if T == BF16 else [F32]):
+        r = mb.expert_linear_dweight(dout, x, off, gated=gated, out_dtype=O)
+        for i in range(two):
+            assert torch.equal(r[i][ours].double(), want[i][ours].to(O).double())
+            assert r[i][bad].isnan().all()
+    mb.expert_linear_status()
+
+
 @pytest.mark.parametrize("T", [BF16, F32])
 def test_nothing(T):
     """No rows at all, and rows that belong to nobody: nothing is read or written but the weights' gradients, 0 or what is added."""
