@@ -909,7 +909,7 @@ extern "C" int mcce_expert_linear_dweight(const mcce_linear* p, const void* dout
   }
   const Problem given = q;   // the bias's gradient reads dout where it is
   cudaError_t err = run_product(kDweight, q, p->dtype, (uint8_t*)workspace + unpacked_bytes(*p) + bias_bytes(*p), st);
-  if (err == cudaSuccess && db) 
+  if (err == cudaSuccess && db)
     err = run_bias_sums(given, p->dtype, add_db, add_db_up, db, db_up, (float*)((uint8_t*)workspace + unpacked_bytes(*p)), st);
   return code(err);
 }
