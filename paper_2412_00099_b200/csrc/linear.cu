@@ -13,7 +13,7 @@ namespace {
 // the reduction along its rows ([row][16], read four products at a time) or across them ([16][row], read four rows at a time); either way 8 16-byte loads
 // feed 32 packed multiply-adds.  fp32 operands of the next three steps are on their way by cp.async, 16, 8 or 4 bytes at a time as the alignment allows; bf16
 // elements of the next step in registers.  The results go through shared memory so that a warp ends up with 32 neighbouring columns of a row.
-// 32 to 41 TFLOP/s (16 groups of 256 rows x 2048 x 512 fp32: 248 us; its gradients 249 and 207), bound by the loads from shared memory and the
+// 32 to 42 TFLOP/s (16 groups of 256 rows x 2048 x 512 fp32: 248 us; its gradients 247 and 203), bound by the loads from shared memory and the
 // instructions around them; 64 x 64 and 128 x 128 tiles with 8 x 8 results per thread left more SMs idle than they saved (340 and 490 us).
 // Where tiles are few, the CTAs of a cluster share a tile's reduction.  900 x 1002 x 515 (two elements per copy): 47 us.
 constexpr int kDeep = 16;
@@ -108,7 +108,7 @@ struct Part {
 };
 
 template <Kind KIND, typename T, bool GATED, int V>
-__global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads, KIND != kForward ? 5 : GATED ? 3 : 4) general_kernel(const Problem p) {
+__global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads, KIND == kForward && GATED ? 3 : 4) general_kernel(const Problem p) {
   typedef General<KIND, T, GATED> C;
   constexpr int kSets = C::kSets, kThreads = C::kThreads, TI = C::TI, TJ = C::TJ, kPad = C::kPad;
   extern __shared__ __align__(16) float smem[];
@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads, KIND != kFo
   int* scratch = before + p.groups.G + 1;
   // A warp has 8 x 4 of the threads' places, and neighbouring lanes differ in both, so that any few lanes share what they read of either operand: 16-byte loads
   // from shared memory are served some lanes at a time.  16 groups of 256 rows x 2048 x 512: 264 -> 248 us, row gradient 258 -> 249, weight gradient
-  // 232 -> 207; the same 8 x 4 without neighbours in both gained nothing.
+  // 232 -> 207 (five CTAs per SM, now four); the same 8 x 4 without neighbours in both gained nothing.
   const int t = threadIdx.x, tx = t / 2 % 8 + t / 32 % 2 * 8, ty = t % 2 + t / 16 % 2 * 2 + t / 64 * 4;
   static_assert(C::kLanesJ == 16 && C::kLanesI == 8, "the places of 128 threads");
 
