@@ -32,6 +32,8 @@ cudaError_t launch_close(void (*kernel)(P...), dim3 grid, int threads, size_t sm
 enum Kind { kForward = 0, kBackward = 1, kDweight = 2 };
 
 // Rows sorted by group g = layer * E + expert.  Whatever the offsets hold, no row outside its layer is touched.
+// They are read by plain loads: the kernel may be running while the one that writes them still is, and a load through the read-only path (__ldg, .nc)
+// promises that nobody writes them while it runs, so that it might move up before the wait.
 struct Groups {
   const int32_t* offsets;   // [L, E + 1]
   int32_t E, G;             // experts per layer, groups L * E
@@ -44,8 +46,8 @@ struct GroupRows {
 __device__ __forceinline__ GroupRows group_rows(const Groups& g, int i) {
   const int l = i / g.E;
   const int32_t* o = g.offsets + i + l;
-  const int64_t lo = min(max((int64_t)__ldg(o), (int64_t)0), g.R);
-  const int64_t hi = min(max((int64_t)__ldg(o + 1), lo), g.R);
+  const int64_t lo = min(max((int64_t)*o, (int64_t)0), g.R);
+  const int64_t hi = min(max((int64_t)o[1], lo), g.R);
   return {l * g.R + lo, hi - lo};
 }
 

@@ -11,9 +11,10 @@ constexpr int kStep = 256;    // reduction per step of a warp: 8 bf16 per lane
 constexpr int kAhead = 4;     // steps under way.  With one row and 3 CTAs per SM, us for 4 x 2 x 1408 x 2048 / 1 x 14336 x 4096: 12.7 / 24.2; 8 steps, 2 CTAs: 14.7 / 22.2;
                               // 3 steps, 4 CTAs: 14.9 / 25.1
 
-__device__ __forceinline__ uint4 read_once(const __nv_bfloat16* p) {   // weights: no reuse, past L1
+// Weights: no reuse, past L1.  Not through the read-only path: an optimiser's kernel may still be writing them when this one takes its place.
+__device__ __forceinline__ uint4 read_once(const __nv_bfloat16* p) {
   uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
   return v;
 }
 __device__ __forceinline__ void dot_8(const uint4& a, const uint4& b, float& s) {
