@@ -161,8 +161,9 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, err, code, limit_ns));
 }
 // The same for what other CTAs of the cluster wrote
-__device__ __forceinline__ bool warp_wait_cluster(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* err, uint32_t code) {
-  const bool ok = warp_wait(bar, parity, abort_flag, err, code);
+__device__ __forceinline__ bool warp_wait_cluster(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* err, uint32_t code,
+                                                  unsigned long long limit_ns) {
+  const bool ok = warp_wait(bar, parity, abort_flag, err, code, limit_ns);
   asm volatile("fence.acq_rel.cluster;" ::: "memory");
   return ok;
 }
@@ -502,12 +503,15 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
     // Clears, in a group's last slab, the rows of the next group up to the next multiple of 16 (the MMAs go no further), of both operands: zero times
     // a NaN of the next group would not be zero.  In the MMAs' own warp this cost the 8 slabs of a group of 500 rows 20 us of 300.
     uint32_t stage = 0, tails = 0;   // tails: the phase of every stage's bar_tail
+    int64_t since = 0;               // slabs multiplied since this warp last had one to clear
     for (int i = 0; walk.at(i, mine, it); ++i) {
       const int slabs = walk.slabs(it), valid = it.rows - (slabs - 1) * C::kSlab;
       if (slabs == 0) continue;
+      since += slabs;
       stage = (stage + slabs - 1) % C::kStages;
       if (valid < C::kSlab) {
-        if (!warp_wait(bar_tail + 8 * stage, (tails >> stage) & 1u, abort_flag, &wait_error, 6u)) break;
+        if (!warp_wait(bar_tail + 8 * stage, (tails >> stage) & 1u, abort_flag, &wait_error, 6u, reduction_limit_ns(since))) break;
+        since = 0;
         tails ^= 1u << stage;
         // a row's 128 bytes in two panels of dout and two of x at a time
         const int panel = (valid <= 64 ? 64 : C::kSlab) * 128;
@@ -540,8 +544,7 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
       if constexpr (KIND == kBackward)
         Backward<__nv_bfloat16>(p.bwd, it.g, it.f0 + quad * 32 + 8 * (lane & 3)).ask((int64_t)it.row + 8 * team, it.rows - 8 * team, asked);
       if (sums) {
-        // a tile's sums may take long: 20 us per slab more than any other wait
-        if (!warp_wait(bar_tfull + 8 * buf, (acc >> 1) & 1u, abort_flag, &wait_error, 4u, kWaitLimitNs + 20000ull * (to - from))) break;
+        if (!warp_wait(bar_tfull + 8 * buf, (acc >> 1) & 1u, abort_flag, &wait_error, 4u, reduction_limit_ns(to - from))) break;
         ++acc;
         tc_fence_after();
       }
@@ -565,7 +568,7 @@ __global__ void __launch_bounds__(Cfg<KIND, GATED, BN, SHARE>::kThreads, 1) line
           if (lane == 0) arrive_at(leaders(bar_parts));
           break;
         }
-        if (cluster_size() > 1 && !warp_wait_cluster(bar_parts, 0u, abort_flag, &wait_error, 7u)) break;
+        if (cluster_size() > 1 && !warp_wait_cluster(bar_parts, 0u, abort_flag, &wait_error, 7u, reduction_limit_ns(to - from))) break;
       }
       auto add_parts = [&](auto& v, int c) {
         if constexpr (SHARE == kSplit) {
