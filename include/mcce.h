@@ -381,7 +381,8 @@ int mcce_combine_backward(const mcce_rows* r /*HOST*/, const void* dy, const voi
 /* The experts' products on sorted rows, for mcce_expert_linear and its gradients.  Group g = l * n_experts + e holds rows
  * offsets[l][e] .. offsets[l][e+1] of layer l (ascending, as mcce_dispatch writes them; what reaches outside [0, rows] is cut
  * off) and uses weights number g.  One expert with offsets {0, rows} is a plain layer.  Rows behind a layer's last group are neither read for a
- * result nor written. */
+ * result nor written.  Offsets that descend and so give a row to two groups are not looked for (they are on the device): results of such rows are
+ * unspecified, everything else about the call is as always.  The gradient of the weights sums such a row for both. */
 enum { MCCE_ACT_NONE = 0, MCCE_ACT_SILU = 1, MCCE_ACT_GELU = 2 /* z P(z), P the normal distribution */ };
 enum { MCCE_LINEAR_MAX_GROUPS = 4096, MCCE_LINEAR_MAX_WIDTH = 1 << 20 };
 typedef struct {

@@ -280,6 +280,8 @@ struct Walk {
     first = blockIdx.x / ctas, step = gridDim.x / ctas;
     FT = (features + kFeatures - 1) / kFeatures, JT = KIND == kDweight ? (p.k + BN - 1) / BN : 1;
     items = KIND == kDweight ? p.groups.G * (GATED ? 2 : 1) * FT * JT : before[p.groups.G] * FT;   // fits: the launch sees to it
+    // A cluster with one reduction takes one tile, and there are as many clusters as tiles; more tiles can only be rows that descending offsets name twice.
+    if (SHARE == kSplit) items = min(items, step);
   }
   __device__ __forceinline__ Item decode(int w) const {
     Item it;
