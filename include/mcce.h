@@ -449,6 +449,9 @@ int mcce_expert_linear_dweight(const mcce_linear* p /*HOST*/, const void* dout, 
 /* MCCE_ETIMEOUT if a bounded wait in one of the three calls above gave up on the current device since the last call (the launch it
  * happened in is incomplete, the CUDA context stays usable), else MCCE_OK.  Synchronises the stream. */
 int mcce_expert_linear_status(void* cuda_stream);
+/* Self-test of that report: launches a one-CTA kernel that waits, as those kernels do, on a barrier nothing ever arrives at, with a limit of limit_ns
+ * (1..1e9), and gives up.  The next mcce_expert_linear_status on the stream answers MCCE_ETIMEOUT, the one after it MCCE_OK. */
+int mcce_selftest_expert_linear_timeout(uint64_t limit_ns, void* cuda_stream);
 
 /* Rows into 8 bits and back, for what a backward pass needs again.  For every block of 32 columns (the last may be shorter)
  *   scale = the smallest power of two, 2^-127 at least, with max |x_j| <= 448 scale;    q_j = e4m3(x_j / scale)

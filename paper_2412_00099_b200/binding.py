@@ -30,7 +30,7 @@ EXPORTS = [
     "mcce_rmsnorm", "mcce_rmsnorm_backward", "mcce_rmsnorm_backward_workspace_bytes", "mcce_dispatch", "mcce_dispatch_workspace_bytes",
     "mcce_combine", "mcce_combine_backward", "mcce_expert_linear", "mcce_expert_linear_backward", "mcce_expert_linear_dweight",
     "mcce_expert_linear_workspace_bytes", "mcce_expert_linear_backward_workspace_bytes",
-    "mcce_expert_linear_dweight_workspace_bytes", "mcce_expert_linear_status", "mcce_checkpoint_pack", "mcce_checkpoint_unpack", "mcce_profile", "mcce_profile_read", "mcce_uses_tensor_path", "mcce_router_kernel_kind", "mcce_selftest_wait_timeout", "mcce_route_trace_static",
+    "mcce_expert_linear_dweight_workspace_bytes", "mcce_expert_linear_status", "mcce_selftest_expert_linear_timeout", "mcce_checkpoint_pack", "mcce_checkpoint_unpack", "mcce_profile", "mcce_profile_read", "mcce_uses_tensor_path", "mcce_router_kernel_kind", "mcce_selftest_wait_timeout", "mcce_route_trace_static",
     "mcce_route_trace_static_limit", "mcce_gen_normal", "mcce_gen_hidden_step", "mcce_gen_philox_words", "mcce_strerror",
     "mcce_last_cuda_error",
 ]
@@ -133,6 +133,7 @@ def load():
             size.restype, size.argtypes = C.c_size_t, [vp] * n
         lib.mcce_expert_linear_dweight.argtypes = [vp] * 14 + [C.c_size_t, vp]
         lib.mcce_expert_linear_status.argtypes = [vp]
+        lib.mcce_selftest_expert_linear_timeout.argtypes = [C.c_uint64, vp]
         lib.mcce_checkpoint_pack.argtypes = [vp, i32, C.c_int64, i32, C.c_int64, C.c_int64, vp, vp, vp]
         lib.mcce_checkpoint_unpack.argtypes = [vp, vp, i32, C.c_int64, i32, C.c_int64, C.c_int64, vp, vp]
         lib.mcce_strerror.restype = C.c_char_p

@@ -858,6 +858,19 @@ cudaError_t launch_rows(const Problem& p, int sms, cudaStream_t st) {
 
 bool tma_rows(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld < kMostStride; }
 
+// Waits, as the kernels' warps do, on a barrier that nothing arrives at; the wait gives up after limit_ns and is noted as theirs are.
+__global__ void wait_selftest_kernel(unsigned long long limit_ns) {
+  __shared__ uint64_t bar;
+  __shared__ uint32_t abort_flag;
+  if (threadIdx.x == 0) {
+    mbar_init(smem_u32(&bar), 1);
+    abort_flag = 0u;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  warp_wait(smem_u32(&bar), 0u, &abort_flag, &wait_error, 99u, limit_ns);
+}
+
 }  // namespace
 
 bool tensor_applicable(Kind kind, const Problem& p, int32_t dtype) {
@@ -892,4 +905,10 @@ extern "C" int mcce_expert_linear_status(void* cuda_stream) {
       cudaStreamSynchronize(st) != cudaSuccess)
     return MCCE_ECUDA;
   return MCCE_ETIMEOUT;
+}
+
+extern "C" int mcce_selftest_expert_linear_timeout(uint64_t limit_ns, void* cuda_stream) {
+  if (limit_ns == 0 || limit_ns > 1000000000ull) return MCCE_EINVAL;
+  mcce::linear::wait_selftest_kernel<<<1, 64, 0, (cudaStream_t)cuda_stream>>>(limit_ns);
+  return cudaGetLastError() == cudaSuccess ? MCCE_OK : MCCE_ECUDA;
 }

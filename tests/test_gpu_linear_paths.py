@@ -38,3 +38,20 @@ def test_offsets_that_give_a_row_twice(T, E, R, n, k, gated):
             within(r[i][e], on * dw, on * ((R + 8) * u * S + dw.abs() * 2 * u), "dw")
             within(r[2 + i][e], on * db, on * ((R + 8) * u * Sb + db.abs() * 2 * u), "db")
     mb.expert_linear_status()
+
+
+def test_a_wait_that_gives_up_is_reported_once():
+    """On the stream it happened on and on another, and the calls after it are whole."""
+    g, R, n, k = gen(4), 300, 136, 72
+    off, x, w = offsets_of([[100, 200]])[0], normal(g, R, k, dtype=BF16), normal(g, 2, n, k, dtype=BF16)
+    want = mb.expert_linear(x, off, w).out
+    mb.expert_linear_status()
+    lib, side = mb.load(), torch.cuda.Stream()
+    for stream in (torch.cuda.current_stream(), side):
+        with torch.cuda.stream(stream):
+            assert lib.mcce_selftest_expert_linear_timeout(1_000_000, stream.cuda_stream) == 0     # 1 ms
+            with pytest.raises(mb.McceError, match="bounded wait"):
+                mb.expert_linear_status()
+            mb.expert_linear_status()
+        assert torch.equal(mb.expert_linear(x, off, w).out, want)
+        mb.expert_linear_status()
