@@ -75,7 +75,9 @@ __device__ __forceinline__ void few_rows(const Problem& p, int g, int64_t row, i
     store_as((T*)e.saved + row * e.ld_saved + f, z);
     if (GATED) store_as((T*)e.saved + row * e.ld_saved + p.n + f, up);
   }
-  float y = e.act == MCCE_ACT_SILU ? z * sigmoid<true>(z) : e.act == MCCE_ACT_GELU ? z * normcdff(z) : z;
+  float y = z;
+  if (e.act == MCCE_ACT_SILU) y *= e.out_f32 ? sigmoid_wide(z) : sigmoid<true>(z);
+  else if (e.act == MCCE_ACT_GELU) y *= normcdff(z);
   if (GATED) y *= up;
   if (e.out_f32) {
     if (e.add) y += ((const float*)e.add)[row * e.ld_add + f];

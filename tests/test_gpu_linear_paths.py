@@ -55,3 +55,24 @@ def test_a_wait_that_gives_up_is_reported_once():
             mb.expert_linear_status()
         assert torch.equal(mb.expert_linear(x, off, w).out, want)
         mb.expert_linear_status()
+
+
+@pytest.mark.parametrize("T", [BF16, F32])
+@pytest.mark.parametrize("E,R,n,k", [(1, 1, 200, 64), (2, 7, 200, 64), (1, 30, 200, 4096), (4, 160, 136, 2048), (1, 200, 136, 2048), (6, 120, 200, 64), (6, 360, 200, 64),
+                                     (2, 900, 200, 64), (2, 100, 51, 33)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_silu_in_fp32(T, E, R, n, k, gated):
+    """fp32 results of bf16 rows are those of an fp32 activation.  A row of x has a single 1, so that z is a weight, exactly, from -80 to 80.  silu(z) = z / (1 + e^-z):
+    two steps (4 u) each of the exponential and the division (what CUDA states for expf and, between 2^-126 and 2^126, __fdividef), a rounding (u) each of the sum
+    and the product, one more times z_up: 11 u, 12 with their products."""
+    g = gen(R + n)
+    off = offsets_of(some_counts(1, E, R, g))[0]
+    col = torch.randint(k, (R,), device="cuda", generator=g)
+    x = torch.zeros(R, k, device="cuda", dtype=T)
+    x[torch.arange(R, device="cuda"), col] = 1
+    w, wu = (160 * torch.rand(E, n, k, device="cuda", generator=g) - 80).to(T), normal(g, E, n, k, dtype=T) if gated else None
+    out = mb.expert_linear(x, off, w, w_up=wu, act="silu", out_dtype=F32).out
+    owner = torch.bucketize(torch.arange(R, device="cuda"), off[1:].long(), right=True)
+    z = w[owner, :, col].double()
+    want = z * torch.sigmoid(z) * (wu[owner, :, col].double() if gated else 1)
+    within(out, want, 12 * u * want.abs() + 2.0 ** -149, "silu")
