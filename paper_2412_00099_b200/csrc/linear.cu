@@ -651,12 +651,12 @@ bool sizes_ok(const mcce_linear* p) {
 }
 bool act_ok(int32_t act) { return act == MCCE_ACT_NONE || act == MCCE_ACT_SILU || act == MCCE_ACT_GELU; }
 
-// All rows of the weights as one tensor for the comparison of addresses; matrices further apart than their rows count as solid.
+// All rows of the weights for the comparison of addresses
 Span weight_span(const mcce_linear& p, const void* w, int e) {
   const int64_t ld = ld_or(p.ld_w, p.k), step = p.step_w ? p.step_w : p.n * ld, G = (int64_t)p.n_layers * p.n_experts;
   if (step == p.n * ld || G == 1) return row_span(w, G * p.n, ld, p.k, e);
   if (ld == p.k) return row_span(w, G, step, p.n * ld, e);
-  return flat_span(w, (G - 1) * step + (p.n - 1) * ld + p.k, e);
+  return stack_span(w, G, step, p.n, ld, p.k, e);
 }
 Problem problem(const mcce_linear& p, const int32_t* offsets) {
   Problem q{};

@@ -6,11 +6,12 @@
 
 namespace mcce {
 
-// `rows` rows of `width` bytes, `step` bytes apart (step >= width), in [lo, hi).  Strides and counts that a caller got wrong
-// are cut to what fits.  No address: not part of the call.
+// `rows` rows of `width` bytes, `step` bytes apart (step >= width), in [lo, hi); or `count` such blocks, `far` bytes apart (no less than a block
+// takes).  Strides and counts that a caller got wrong are cut to what fits.  No address: not part of the call.
 struct Span {
   uintptr_t lo, hi;
   int64_t rows, step, width;
+  int64_t count = 1, far = 0;
 };
 inline int64_t bytes_of(int64_t n, int64_t each) {
   int64_t r;
@@ -26,6 +27,15 @@ inline Span span(const void* p, int64_t rows, int64_t step, int64_t width) {
 }
 inline Span row_span(const void* p, int64_t rows, int64_t ld, int64_t d, int elem_bytes) {
   return span(p, rows, bytes_of(rows > 1 ? ld : d, elem_bytes), d * elem_bytes);
+}
+// `count` matrices of `rows` rows
+inline Span stack_span(const void* p, int64_t count, int64_t step, int64_t rows, int64_t ld, int64_t d, int elem_bytes) {
+  Span s = row_span(p, rows, ld, d, elem_bytes);
+  if (!p || count <= 1) return s;
+  s.count = count, s.far = bytes_of(step, elem_bytes);
+  const unsigned __int128 end = (unsigned __int128)s.hi + (unsigned __int128)(count - 1) * (uint64_t)s.far;
+  s.hi = end > UINTPTR_MAX ? UINTPTR_MAX : (uintptr_t)end;
+  return s;
 }
 inline Span flat_span(const void* p, int64_t n, int64_t each = 1) { return span(p, 1, bytes_of(n, each), bytes_of(n, each)); }
 
@@ -60,7 +70,22 @@ inline bool rows_disjoint(const Span& a, const Span& b) {
     if (meets(i)) return false;
   return true;
 }
-inline bool disjoint(const Span& a, const Span& b) { return a.lo >= b.hi || b.lo >= a.hi || rows_disjoint(a, b); }
+// Block i of a span of several
+inline Span block_of(const Span& s, int64_t i) {
+  return span((const void*)(s.lo + (uintptr_t)i * (uintptr_t)s.far), s.rows, s.step, s.width);
+}
+inline bool disjoint(const Span& a, const Span& b) {
+  if (a.lo >= b.hi || b.lo >= a.hi) return true;
+  if (a.count == 1 && b.count == 1) return rows_disjoint(a, b);
+  // Blocks of either lie one behind the other, so that walking both in the order of their addresses meets every pair that overlaps.
+  for (int64_t i = 0, j = 0; i < a.count && j < b.count;) {
+    const Span x = block_of(a, i), y = block_of(b, j);
+    if (x.lo < y.hi && y.lo < x.hi && !rows_disjoint(x, y)) return false;
+    if (x.hi <= y.hi) ++i;
+    else ++j;
+  }
+  return true;
+}
 
 // An output that shares no byte with these tensors.
 inline bool apart(const Span& out, std::initializer_list<const Span*> others) {
@@ -70,7 +95,8 @@ inline bool apart(const Span& out, std::initializer_list<const Span*> others) {
 }
 // The same for an output that may be this input: row for row the same addresses, or none.
 inline bool same_or_apart(const Span& out, const Span& in) {
-  return (out.lo == in.lo && out.rows == in.rows && out.step == in.step && out.width == in.width) || disjoint(out, in);
+  return (out.lo == in.lo && out.rows == in.rows && out.step == in.step && out.width == in.width && out.count == in.count && out.far == in.far) ||
+         disjoint(out, in);
 }
 
 }  // namespace mcce

@@ -76,3 +76,29 @@ def test_silu_in_fp32(T, E, R, n, k, gated):
     z = w[owner, :, col].double()
     want = z * torch.sigmoid(z) * (wu[owner, :, col].double() if gated else 1)
     within(out, want, 12 * u * want.abs() + 2.0 ** -149, "silu")
+
+
+@pytest.mark.parametrize("T,O", [(BF16, BF16), (BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("pad", [0, 8, 3])
+@pytest.mark.parametrize("add", [False, True])
+def test_gradients_into_one_buffer(T, O, pad, add):
+    """dw and dw_up as the two halves of one buffer [E,2n,k] with padded rows (as a fused gate and up weight lies): those of separate tensors, bit for bit where the
+    kernel is the same, nothing else touched; and the products that read weights from such a buffer."""
+    g, E, R, n, k = gen(8), 5, 700, 72, 136
+    off = offsets_of([[100, 0, 333, 17, 250]])[0]
+    x, dout = normal(g, R, k, dtype=T), normal(g, R, 2 * n, dtype=T)
+    buf = torch.full((E, 2 * n, k + pad), 9.0, device="cuda", dtype=O)
+    halves = mb.WeightGrad(buf[:, :n, :k], buf[:, n:, :k])
+    before = mb.WeightGrad(*[normal(g, E, n, k, dtype=O) for _ in range(2)]) if add else None
+    if add:
+        halves.dw.copy_(before.dw), halves.dw_up.copy_(before.dw_up)
+    want = mb.expert_linear_dweight(dout, x, off, gated=True, add=before, out_dtype=O)
+    mb.expert_linear_dweight(dout, x, off, gated=True, add=halves if add else None, out=halves)
+    assert torch.equal(halves.dw, want.dw) and torch.equal(halves.dw_up, want.dw_up) and (buf[:, :, k:] == 9).all()
+    w = buf.to(T)
+    w, wu = w[:, :n, :k], w[:, n:, :k]
+    for a, b in ((mb.expert_linear(x, off, w, w_up=wu, act="silu").out, mb.expert_linear(x, off, w.contiguous(), w_up=wu.contiguous(), act="silu").out),
+                 (mb.expert_linear_backward(dout, off, w, w_up=wu).dx, mb.expert_linear_backward(dout, off, w.contiguous(), w_up=wu.contiguous()).dx)):
+        # a start or stride that is no multiple of 16 bytes may take another kernel: two sums of at most 2 n or k products, and a rounding, per element
+        assert torch.equal(a, b) or (pad == 3 and ((a.double() - b.double()).abs() <= 2 * (2 * n + k + 8) * u * 40 * b.double().abs().max() + 2 * U(T) * b.double().abs()).all())
+    mb.expert_linear_status()
