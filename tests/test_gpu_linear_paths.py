@@ -4,6 +4,7 @@ magnitudes S."""
 import pytest
 import torch
 
+import test_gpu_linear as base
 from test_gpu_linear import BF16, F32, U, act, gen, inside, normal, offsets_of, slope, some_counts, sums, u, within
 
 pytestmark = pytest.mark.gpu
@@ -101,4 +102,66 @@ def test_gradients_into_one_buffer(T, O, pad, add):
                  (mb.expert_linear_backward(dout, off, w, w_up=wu).dx, mb.expert_linear_backward(dout, off, w.contiguous(), w_up=wu.contiguous()).dx)):
         # a start or stride that is no multiple of 16 bytes may take another kernel: two sums of at most 2 n or k products, and a rounding, per element
         assert torch.equal(a, b) or (pad == 3 and ((a.double() - b.double()).abs() <= 2 * (2 * n + k + 8) * u * 40 * b.double().abs().max() + 2 * U(T) * b.double().abs()).all())
+    mb.expert_linear_status()
+
+
+# Ways of sharing a reduction that tiles of 32, 64 and 128 rows have: two or four CTAs (rows per group, slabs of 64 products and tiles decide)
+SPLIT_FORWARD = [(1, 1, 100, 136, 2048), (1, 4, 400, 136, 1040), (2, 1, 200, 264, 1024),        # 128 rows
+                 (1, 1, 60, 136, 2048), (1, 3, 120, 72, 1024),                                  # 64 rows: four, two
+                 (1, 2, 60, 520, 4096), (1, 1, 16, 136, 1024), (1, 2, 40, 72, 1088)]            # 32 rows: four, two
+SPLIT_BACKWARD = [(1, 1, 100, 1024, 136), (1, 4, 400, 1040, 136), (2, 1, 200, 1088, 264), (1, 1, 60, 2048, 136), (1, 3, 120, 1024, 72), (1, 2, 100, 520, 136),
+                  (1, 2, 60, 4096, 520), (1, 1, 16, 1024, 136), (1, 2, 40, 1088, 72), (1, 1, 16, 512, 136)]
+
+
+@pytest.mark.parametrize("shape", SPLIT_FORWARD, ids=str)
+@pytest.mark.parametrize("O", [BF16, F32])
+@pytest.mark.parametrize("gated", [False, True])
+def test_shared_reductions(shape, O, gated):
+    base.test_linear(shape, BF16, O, gated)
+
+
+@pytest.mark.parametrize("shape", SPLIT_BACKWARD, ids=str)
+@pytest.mark.parametrize("gated", [False, True])
+def test_shared_reductions_backward(shape, gated):
+    base.test_linear_backward(shape, BF16, gated)
+
+
+@pytest.mark.parametrize("L,E,R", [(1, 3, 7), (1, 3, 30), (1, 3, 150), (1, 3, 500), (2, 2, 700), (1, 1, 90)])
+@pytest.mark.parametrize("n,k", [(136, 72), (200, 1088), (1088, 192)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_weights_whose_step_is_no_multiple_of_a_row(L, E, R, n, k, gated):
+    """Matrices of padded rows with something between them, so that they are not rows of one tall matrix: the same bits as packed ones, whatever lies between."""
+    g, ld = gen(n + R), k + 8
+    off = offsets_of(some_counts(L, E, R, g))
+    x, dout = normal(g, L, R, k, dtype=BF16), normal(g, L, R, (1 + gated) * n, dtype=BF16)
+    packed = [normal(g, L, E, n, k, dtype=BF16, std=k ** -0.5) for _ in range(1 + gated)] + [None] * (1 - gated)
+    apart = []
+    for w in packed:
+        step = n * ld + 24
+        buf = torch.full((L * E * step,), float("nan"), device="cuda", dtype=BF16)
+        apart.append(w if w is None else torch.as_strided(buf, (L, E, n, k), (E * step, step, ld, 1)).copy_(w))
+    there = inside(off, R)
+    a, b = (mb.expert_linear(x, off, w, w_up=wu, act="gelu", save="same") for w, wu in (apart, packed))
+    assert torch.equal(a.out[there], b.out[there]) and torch.equal(a.saved[there], b.saved[there]) and a.out[there].isfinite().all()
+    a, b = (mb.expert_linear_backward(dout, off, w, w_up=wu).dx for w, wu in (apart, packed))
+    assert torch.equal(a[there], b[there]) and a[there].isfinite().all()
+    mb.expert_linear_status()
+
+
+@pytest.mark.parametrize("pad,between", [(8, 0), (8, 32), (0, 64), (2, 0)])
+@pytest.mark.parametrize("T,O", [(BF16, BF16), (BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("n,k", [(72, 136), (300, 264), (130, 520)])
+def test_gradients_into_rows_further_apart(T, O, pad, between, n, k):
+    """dw with padded rows and something between the matrices, without anything added (written by copies from shared memory where 16 bytes allow it)."""
+    g, L, E, R = gen(n + pad), 2, 3, 333
+    off = offsets_of([[100, 0, 200], [7, 128, 64]])
+    x, dout = normal(g, L, R, k, dtype=T), normal(g, L, R, n, dtype=T)
+    step = n * (k + pad) + between
+    buf = torch.full((L * E * step,), 9.0, device="cuda", dtype=O)
+    dw = torch.as_strided(buf, (L, E, n, k), (E * step, step, k + pad, 1))
+    want = mb.expert_linear_dweight(dout, x, off, out_dtype=O).dw
+    mb.expert_linear_dweight(dout, x, off, out=mb.WeightGrad(dw))
+    assert torch.equal(dw, want)
+    dw.fill_(9.0)
+    assert (buf == 9).all()
     mb.expert_linear_status()
