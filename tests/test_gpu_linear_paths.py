@@ -165,3 +165,67 @@ def test_gradients_into_rows_further_apart(T, O, pad, between, n, k):
     dw.fill_(9.0)
     assert (buf == 9).all()
     mb.expert_linear_status()
+
+
+@pytest.mark.parametrize("save", ["same", "e4m3"])
+@pytest.mark.parametrize("tokens,d,f", [(37, 64, 96), (150, 72, 40), (500, 128, 192), (900, 256, 136)])
+def test_layer_and_its_gradients_in_bf16(tokens, d, f, save):
+    """Norm, sort, gated experts, down projection with bias, weighted return onto the residual stream, and back, in bf16, against 64 bits, every tensor by its relative
+    2-norm, which a missing or wrong part of a few percent exceeds.  A rounding is off by at most U = 2^-8 of a value, evenly spread, so U / sqrt(3) in the root mean
+    square; at most 8 of them lie one behind the other, independent of one another: sqrt(8 / 3) U.  Products of random matrices keep relative norms,
+    slopes and sums move them by less than 2: 2 sqrt(8 / 3) U = 0.0128.  What was kept in 8 bits (2^-4) is taken from what the forward call kept, one stage more
+    of the 64-bit formula: the same tolerance."""
+    E, K, T = 5, 2, BF16
+    g = gen(tokens)
+    x, wn = normal(g, tokens, d, dtype=T), 1 + 0.1 * normal(g, d)
+    wg, wu, wd = (normal(g, E, *s, dtype=T, std=s[1] ** -0.5) for s in ((f, d), (f, d), (d, f)))
+    bd = normal(g, E, d, std=0.1).to(T)
+    sel = torch.stack([torch.randperm(E, generator=g, device="cuda")[:K] for _ in range(tokens)]).to(torch.int32)
+    sel[3, 1] = -1
+    sw, dy = torch.softmax(normal(g, tokens, K), -1), normal(g, tokens, d, dtype=T)
+    h = mb.rmsnorm(x, wn, 1e-6).out
+    s = mb.dispatch(sel, E, h)
+    a = mb.expert_linear(s.rows, s.offsets, wg, w_up=wu, act="silu", save=save)
+    o = mb.expert_linear(a.out, s.offsets, wd, bias=bd).out
+    y = mb.combine(o, s.inv, sw, add=x)
+    do, dsw = mb.combine_backward(dy, o, s.inv, sw)
+    da = mb.expert_linear_backward(do, s.offsets, wd, saved=a.saved, scales=a.scales, act="silu")
+    gd = mb.expert_linear_dweight(do, da.h, s.offsets, want_db=True)
+    drows = mb.expert_linear_backward(da.dx, s.offsets, wg, w_up=wu).dx
+    gu = mb.expert_linear_dweight(da.dx, s.rows, s.offsets, gated=True)
+    dh = mb.combine(drows, s.inv)
+    dx, dwn = mb.rmsnorm_backward(dh, x, wn, 1e-6, dsum=dy)
+
+    # 64 bits, with the pre-activations that the backward pass gets where they were kept in 8 bits
+    X, N, W = x.double(), wn.double(), [w.double() for w in (wg, wu, wd)]
+    r = (X.square().mean(-1, keepdim=True) + 1e-6).rsqrt()
+    H = X * r * N
+    Y, dH = X.clone(), torch.zeros_like(X)
+    G = dict(wg=torch.zeros_like(W[0]), wu=torch.zeros_like(W[1]), wd=torch.zeros_like(W[2]), bd=torch.zeros_like(bd.double()), sw=torch.zeros_like(sw.double()))
+    kept = None if save == "same" else base.unpacked(a.saved, a.scales, 2)
+    for k in range(K):
+        for e in range(E):
+            t = (sel[:, k] == e).nonzero()[:, 0]
+            z, up = H[t] @ W[0][e].T, H[t] @ W[1][e].T
+            out = (act(z, "silu") * up) @ W[2][e].T + bd[e].double()
+            Y[t] += sw[t, k, None].double() * out
+            G["sw"][t, k] = (out * dy[t].double()).sum(-1)
+            D = sw[t, k, None].double() * dy[t].double()
+            if kept is not None:
+                z, up = kept[s.inv[t, k].long()].chunk(2, -1)
+            hidden = act(z, "silu") * up
+            G["wd"][e] += D.T @ hidden
+            G["bd"][e] += D.sum(0)
+            back = D @ W[2][e]
+            dz, du = back * up * slope(z, "silu"), back * act(z, "silu")
+            G["wg"][e] += dz.T @ H[t]
+            G["wu"][e] += du.T @ H[t]
+            dH[t] += dz @ W[0][e] + du @ W[1][e]
+    v = dH * N
+    G["x"] = dy.double() + r * v - X * r ** 3 * (v * X).mean(-1, keepdim=True)
+    G["wn"] = (dH * X * r).sum(0)
+    ours = dict(x=dx, wn=dwn, wg=gu.dw, wu=gu.dw_up, wd=gd.dw, bd=gd.db, sw=dsw)
+    for name, got, want in [("y", y, Y)] + [(n, ours[n], G[n]) for n in ours]:
+        off = float((got.double() - want).norm() / want.norm())
+        assert off <= 2 * (8 / 3) ** 0.5 * U(T), (name, off)
+    mb.expert_linear_status()
