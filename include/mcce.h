@@ -413,7 +413,7 @@ typedef struct {
  *   workspace DEVICE, 16-byte aligned, as many bytes as the call of that name answers for these addresses, which it only looks at (0 is usual: it may
  *       be NULL then).  It takes copies of bf16 rows and weights whose starts or strides are no multiples of 16 bytes, where that pays.
  * bf16 rows and weights meet on the tensor cores, whose fp32 accumulation truncates: a sum of k products is within (k + 8) 2^-24 of its
- * terms' magnitudes. */
+ * terms' magnitudes.  An fp32 result's activation is computed in fp32 throughout; a bf16 result's exponential is off by up to (2 + |z|) 2^-22 of itself. */
 size_t mcce_expert_linear_workspace_bytes(const mcce_linear* p /*HOST*/, const void* x, const void* w, const void* w_up);
 int mcce_expert_linear(const mcce_linear* p /*HOST*/, const void* x, const int32_t* offsets, const void* w, const void* w_up,
                        const void* bias, const void* bias_up, const void* add, void* out, void* saved, void* scales,

@@ -13,9 +13,9 @@ namespace {
 // the reduction along its rows ([row][16], read four products at a time) or across them ([16][row], read four rows at a time); either way 8 16-byte loads
 // feed 32 packed multiply-adds.  fp32 operands of the next three steps are on their way by cp.async, 16, 8 or 4 bytes at a time as the alignment allows; bf16
 // elements of the next step in registers.  The results go through shared memory so that a warp ends up with 32 neighbouring columns of a row.
-// 32 to 42 TFLOP/s (16 groups of 256 rows x 2048 x 512 fp32: 248 us; its gradients 247 and 203), bound by the loads from shared memory and the
+// 32 to 42 TFLOP/s (16 groups of 256 rows x 2048 x 512 fp32: 245 us; its gradients 247 and 202), bound by the loads from shared memory and the
 // instructions around them; 64 x 64 and 128 x 128 tiles with 8 x 8 results per thread left more SMs idle than they saved (340 and 490 us).
-// Where tiles are few, the CTAs of a cluster share a tile's reduction.  900 x 1002 x 515 (two elements per copy): 47 us.
+// Where tiles are few, the CTAs of a cluster share a tile's reduction.  900 rows of 10 groups x 1002 x 515 (two elements per copy): 46 to 52 us.
 constexpr int kDeep = 16;
 
 template <Kind KIND, typename T, bool GATED>
@@ -315,8 +315,11 @@ __global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads, KIND == kFo
   }
 }
 
-// CTAs per tile: as many as a full device has room for at once and as leave each of them eight steps (4 rows x 2034 x 64 fp32: 62 us alone, 13 shared;
-// 900 x 1002 x 515, 270 tiles: 70 and 53).
+// CTAs per tile: as many as make six CTAs per SM in all and leave each of them eight steps.  Four (a gated forward pass: three) are on an SM at once; the others
+// take the places of those that are done, where a limit of three or four often leaves whole SMs without a second one.  fp32, rows / groups x k x n, us with one CTA
+// per tile / up to three / four / six / eight per SM:
+//   900/10 x 1002 x 515: 58 / 58 / 58 / 50 / 50     2000/16 x 640 x 256: 34 / 34 / 34 / 25 / 25     1024/4 x 1024 x 512: 36 / 36 / 37 / 37 / 39
+//   4/30 x 2034 x 64: 50 / 10 / 10 / 10 / 10        512/8 x 2048 x 512: 67 / 53 / 53 / 45 / 45     64/8 x 2048 x 512, gated: 77 / 37 / 37 / 43 / 43
 int64_t reduction(Kind kind, const Problem& p) { return kind == kForward ? p.k : kind == kBackward ? p.n : p.L * p.groups.R / p.groups.G; }
 int general_ctas(Kind kind, const Problem& p, int64_t tiles, int sms) {
   int ctas = 8;
@@ -538,11 +541,13 @@ namespace {
 bool wide_rows(const void* p, int64_t ld, int e) { return !p || (((uintptr_t)p | (uintptr_t)(ld * e)) & (e == 1 ? 7 : 15)) == 0; }
 }  // namespace
 
-// Chunks of a group's rows: one unless the groups are few and long.
+// Chunks of a group's rows: one unless the groups are few and long; up to four CTAs for each of a B200's 148 SMs, each with 512 rows or more.  (The workspace
+// is asked for without a device, so that this goes by the SMs that the library is built for; so do the copies below and the blocks per lane of a checkpoint.)
 int bias_chunks(int64_t rows, int32_t G, int32_t n) {
+  constexpr int64_t kMost = 4 * 148;
   const int64_t ctas = (int64_t)G * ((n + 255) / 256), each = rows / G / 512;
-  if (each < 2 || ctas >= 592) return 1;
-  const int64_t want = 592 / ctas;
+  if (each < 2 || ctas >= kMost) return 1;
+  const int64_t want = kMost / ctas;
   return (int)(each < want ? each : want < 64 ? want : 64);
 }
 cudaError_t run_bias_sums(const Problem& p, int32_t dtype, const void* add, const void* add_up, void* db, void* db_up, float* parts,
@@ -670,6 +675,10 @@ int code(cudaError_t e) { return e == cudaSuccess ? MCCE_OK : MCCE_ECUDA; }
 
 // bf16 rows that the tensor cores' copies cannot take (a stride or start that is no multiple of 16 bytes) are brought to one that is, where that pays: on the fp32
 // pipe bf16 products run at 10 to 20 TFLOP/s (4096 x 2047 x 511, gated: 800 us, copied 74), the copies at some 4 TB/s.
+// Both ways were timed over 396 products (forward, row and weight gradient, gated and not, 64 to 65536 rows of 1 to 64 groups, widths 65 to 2050): the estimate takes
+// the slower one by more than 12 % in 40 of them, and 5 % more than the faster ones in the mean.  Where it copies in vain that costs up to 9 us (weight gradient of
+// 1024 rows x 255 x 255, gated: 15 -> 24); where it does not copy, gated row gradients of few rows lose most (64 rows x 255 x 255: 18 -> 73 us; they
+// run at a quarter of the others' rate).  With the time of a weight gradient's slabs, which a pair of CTAs takes one after the other, in the estimate it was 48 of 396.
 struct Copies {
   bool x, y, w;
   size_t x_bytes, y_bytes, w_bytes;   // w: of one matrix of every group

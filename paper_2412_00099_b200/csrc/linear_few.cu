@@ -118,8 +118,12 @@ cudaError_t launch_few(const Problem& p, int sms, cudaStream_t st) {
 
 }  // namespace
 
-// Up to four rows per expert on average, and too few tiles for the tensor-core kernel to occupy the SMs (256 weight tiles of 128 rows: 23 us there, 25 here; 128: 16 and
-// 14.6; four rows of one expert, 32 tiles: 70 and 51).
+// Up to four rows per expert on average, and too few tiles for the tensor-core kernel to occupy the SMs, alone or sharing a reduction.  us here / there, rows x k x n of
+// one expert, and gated layers 2048 -> 1408 (222 tiles: 10 touched experts):
+//   1 x 2048 x 4096: 6 / 10      1 x 14336 x 4096: 22 / 27     1 x 4096 x 16384: 24 / 27      1 token x 4 experts: 10.9 / 14.5
+//   4 x 2048 x 4096: 7 / 10      4 x 14336 x 4096: 30 / 27     4 x 4096 x 16384: 36 / 27      2 tokens: 17.0 / 25.5
+//   2 x 14336 x 4096: 23 / 27    3 x 14336 x 4096: 26 / 27     2 x 4096 x 16384: 28 / 27      4 tokens (too many tiles): 31.3 / 30.6
+// So three or four rows of one wide expert would be better off there (up to 9 us); the rule does not look at rows and width together.
 bool few_applicable(const Problem& p, int32_t dtype) {
   const uintptr_t all = (uintptr_t)p.x | (uintptr_t)p.w | (uintptr_t)p.w_up | (uintptr_t)(p.ld_x * 2) | (uintptr_t)(p.ld_w * 2) |
                         (uintptr_t)(p.groups.G > 1 ? p.step_w * 2 : 0);

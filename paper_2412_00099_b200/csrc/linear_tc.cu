@@ -842,7 +842,10 @@ cudaError_t launch(const Problem& p, cudaStream_t st) {
 }
 
 // Rows per tile by the rows that a group has on average.  Where all tiles together leave half of the SMs idle, up to four CTAs share a tile's reduction (16 rows
-// x 14336 x 4096, 32 tiles: 70 us alone, 29 shared); a pair of CTAs wants more rows than one (below 96 its tiles would be mostly empty).
+// x 14336 x 4096, 32 tiles: 70 us alone, 27 shared); a pair of CTAs wants more rows than one (below 96 its tiles would be mostly empty).
+// Tiles of 32 rows read fewer rows that belong to another group, tiles of 128 read the weights once; 60 groups, 2048 -> 1408, us with 32 / with 128, forward,
+// gated forward, row gradient:    8 rows each 61 / 62, 104 / 108, 61 / 60    16: 61 / 63, 110 / 111, 61 / 61    24: 64 / 65, 123 / 113, 73 / 63
+// 28: 73 / 65, 128 / 113, 74 / 65    40: 78 / 66, 155 / 121, 96 / 67.  (24 is the forward pass's border; gradients would take 16.)
 template <int KIND, bool GATED>
 cudaError_t launch_rows(const Problem& p, int sms, cudaStream_t st) {
   const int64_t each = p.L * p.groups.R / p.groups.G;
