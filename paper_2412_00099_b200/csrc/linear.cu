@@ -315,12 +315,19 @@ __global__ void __launch_bounds__(General<KIND, T, GATED>::kThreads, KIND == kFo
   }
 }
 
+// Tiles of a product, at most
+constexpr int kTileI = 32, kTileJ = 64;
+int64_t general_tiles(Kind kind, const Problem& p) {
+  const int64_t across = ((kind == kForward ? p.n : p.k) + kTileJ - 1) / kTileJ;
+  if (kind == kDweight) return (int64_t)p.groups.G * (p.gated ? 2 : 1) * ((p.n + kTileI - 1) / kTileI) * across;
+  return (p.L * p.groups.R / kTileI + p.groups.G) * across;
+}
+int64_t reduction(Kind kind, const Problem& p) { return kind == kForward ? p.k : kind == kBackward ? p.n : p.L * p.groups.R / p.groups.G; }
 // CTAs per tile: as many as make six CTAs per SM in all and leave each of them eight steps.  Four (a gated forward pass: three) are on an SM at once; the others
 // take the places of those that are done, where a limit of three or four often leaves whole SMs without a second one.  fp32, rows / groups x k x n, us with one CTA
 // per tile / up to three / four / six / eight per SM:
 //   900/10 x 1002 x 515: 58 / 58 / 58 / 50 / 50     2000/16 x 640 x 256: 34 / 34 / 34 / 25 / 25     1024/4 x 1024 x 512: 36 / 36 / 37 / 37 / 39
 //   4/30 x 2034 x 64: 50 / 10 / 10 / 10 / 10        512/8 x 2048 x 512: 67 / 53 / 53 / 45 / 45     64/8 x 2048 x 512, gated: 77 / 37 / 37 / 43 / 43
-int64_t reduction(Kind kind, const Problem& p) { return kind == kForward ? p.k : kind == kBackward ? p.n : p.L * p.groups.R / p.groups.G; }
 int general_ctas(Kind kind, const Problem& p, int64_t tiles, int sms) {
   int ctas = 8;
   while (ctas > 1 && (tiles * ctas > 6 * sms || reduction(kind, p) < 8 * kDeep * ctas)) ctas /= 2;
@@ -343,11 +350,8 @@ cudaError_t launch_general(const Problem& p, cudaStream_t st) {
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return cudaErrorInvalidDevice;
-  typedef General<KIND, T, GATED> C;
-  const int64_t jt = ((KIND == kForward ? p.n : p.k) + C::TJ - 1) / C::TJ;
-  const int64_t tiles =
-      KIND == kDweight ? (int64_t)p.groups.G * (GATED ? 2 : 1) * ((p.n + C::TI - 1) / C::TI) * jt : (p.L * p.groups.R / C::TI + p.groups.G) * jt;
-  return launch_tiles<KIND, T, GATED, V>(p, tiles, sms, st);
+  static_assert(General<KIND, T, GATED>::TI == kTileI && General<KIND, T, GATED>::TJ == kTileJ, "the tiles that are counted");
+  return launch_tiles<KIND, T, GATED, V>(p, general_tiles(KIND, p), sms, st);
 }
 template <Kind KIND, typename T, int V>
 cudaError_t launch_general_gated(const Problem& p, cudaStream_t st) {
@@ -700,8 +704,7 @@ Copies copies_for(Kind kind, const Problem& q, int32_t dtype) {
   if (c.w) c.w_bytes = size(G * q.n, whole_8(q.k));
   if (rows == 0) return Copies{};
   // the fp32 pipe: its rate, and 0.4 us for every step of a CTA; the tensor cores: the copies, and their launches with the product's shortest time
-  const int64_t tiles = (rows / 32 + G) * (((kind == kForward ? q.n : q.k) + 63) / 64);
-  const double steps = (double)reduction(kind, q) / kDeep / general_ctas(kind, q, tiles, 148);
+  const double steps = (double)reduction(kind, q) / kDeep / general_ctas(kind, q, general_tiles(kind, q), 148);
   const double pipe = 2.0 * rows * q.n * q.k * two / 12e12 + steps * 0.4e-6, tensor = c.bytes(q.gated) * 2.0 / 4e12 + 22e-6;
   return pipe > tensor ? c : Copies{};
 }
