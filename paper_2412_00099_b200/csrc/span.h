@@ -77,6 +77,16 @@ inline Span block_of(const Span& s, int64_t i) {
 inline bool disjoint(const Span& a, const Span& b) {
   if (a.lo >= b.hi || b.lo >= a.hi) return true;
   if (a.count == 1 && b.count == 1) return rows_disjoint(a, b);
+  if (a.count > 1 && b.count > 1 && a.far == b.far) {   // only how many blocks apart two are matters, and three such differences are near enough
+    typedef __int128 Wide;
+    const Wide near = ((Wide)a.lo - (Wide)b.lo) / a.far;
+    for (Wide d = near - 1; d <= near + 1; ++d) {       // block i + d of b
+      const Wide i = d < 0 ? -d : 0;
+      if (i >= a.count || i + d >= b.count) continue;
+      if (!disjoint(block_of(a, (int64_t)i), block_of(b, (int64_t)(i + d)))) return false;
+    }
+    return true;
+  }
   // Blocks of either lie one behind the other, so that walking both in the order of their addresses meets every pair that overlaps.
   for (int64_t i = 0, j = 0; i < a.count && j < b.count;) {
     const Span x = block_of(a, i), y = block_of(b, j);
