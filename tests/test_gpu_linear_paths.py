@@ -229,3 +229,74 @@ def test_layer_and_its_gradients_in_bf16(tokens, d, f, save):
         off = float((got.double() - want).norm() / want.norm())
         assert off <= 2 * (8 / 3) ** 0.5 * U(T), (name, off)
     mb.expert_linear_status()
+
+
+IN_PLACE = [(1, 2, 3, 40, 64), (1, 3, 40, 72, 136), (1, 1, 30, 1088, 264), (1, 1, 60, 2048, 136), (1, 1, 100, 1024, 264), (1, 4, 200, 200, 136), (2, 3, 700, 136, 200), (1, 3, 300, 51, 77)]
+
+
+@pytest.mark.parametrize("T", [BF16, F32])
+@pytest.mark.parametrize("shape", IN_PLACE, ids=str)
+@pytest.mark.parametrize("gated", [False, True])
+def test_results_in_place_of_inputs(T, shape, gated):
+    """out over add, dx over add and over the kept values, dw over what it is added to: the bits of results of their own, whatever shares the work."""
+    L, E, R, n, k = shape
+    g, two = gen(R + k), 1 + gated
+    off = offsets_of(some_counts(L, E, R, g, full=False))
+    x, dout = normal(g, L, R, k, dtype=T), normal(g, L, R, two * n, dtype=T)
+    w = [normal(g, L, E, n, k, dtype=T, std=k ** -0.5) for _ in range(two)] + [None] * (2 - two)
+    there = inside(off, R)
+
+    def same(got, want, before):
+        assert torch.equal(got[there], want[there]) and torch.equal(got[~there], before[~there])
+    add = normal(g, L, R, n, dtype=T)
+    want, got = mb.expert_linear(x, off, w[0], w_up=w[1], act="gelu", add=add).out, add.clone()
+    mb.expert_linear(x, off, w[0], w_up=w[1], act="gelu", add=got, out=mb.LinearOut(got))
+    same(got, want, add)
+    add = normal(g, L, R, k, dtype=T)
+    want, got = mb.expert_linear_backward(dout, off, w[0], w_up=w[1], add=add).dx, add.clone()
+    mb.expert_linear_backward(dout, off, w[0], w_up=w[1], add=got, out=mb.LinearGrad(got))
+    same(got, want, add)
+    for below in (1, 2):
+        z = normal(g, L, R, below * k, dtype=T)
+        want, got = mb.expert_linear_backward(dout, off, w[0], w_up=w[1], saved=z, act="silu"), z.clone()
+        r = mb.expert_linear_backward(dout, off, w[0], w_up=w[1], saved=got, act="silu", out=mb.LinearGrad(got, torch.empty_like(x)))
+        same(got, want.dx, z)
+        assert torch.equal(r.h[there], want.h[there])
+    before = mb.WeightGrad(*[None if i >= two else normal(g, L, E, n, k, dtype=T) for i in range(2)], *[None if i >= two else normal(g, L, E, n, dtype=T) for i in range(2)])
+    want = mb.expert_linear_dweight(dout, x, off, gated=gated, want_db=True, add=before)
+    mb.expert_linear_dweight(dout, x, off, gated=gated, add=before, out=before)
+    assert all(a is None or torch.equal(a, b) for a, b in zip(before, want))
+    mb.expert_linear_status()
+
+
+@pytest.mark.parametrize("T", [BF16, F32])
+@pytest.mark.parametrize("E,R", [(4096, 3000), (4096, 30000), (700, 5), (1000, 40000), (577, 100000)])
+def test_many_groups(T, E, R):
+    """More groups than threads in any kernel's block, up to the limit; a third of them empty.  Small integers: every sum is exact."""
+    g, n, k = gen(E + R), 16, 24
+    c = torch.rand(E, device="cuda", generator=g) * (torch.rand(E, device="cuda", generator=g) > 0.33)
+    c = (c / c.sum() * R).long()
+    first = torch.randint(3, 90, (1,), generator=torch.Generator().manual_seed(E)).item() if R > 100 else 0        # rows in front of the first group are nobody's either
+    c[E // 2] += (R - first - int(c.sum())) // 2
+    off = torch.cat([torch.full((1,), first, device="cuda"), first + c.cumsum(0)]).to(torch.int32)
+    end = int(off[-1])
+    assert 0 <= first <= end <= R
+    whole = lambda *s: torch.randint(-3, 4, s, device="cuda", generator=g).to(T)
+    x, dout, w, wu = whole(R, k), whole(R, 2 * n), whole(E, n, k), whole(E, n, k)
+    for t in (x, dout):
+        t[:first], t[end:] = float("nan"), float("inf")
+    owner = torch.bucketize(torch.arange(first, end, device="cuda"), off[1:].long(), right=True)
+    xs, ds = x[first:end].double(), dout[first:end].double()
+    out = torch.full((R, n), 7.0, device="cuda", dtype=F32)
+    mb.expert_linear(x, off, w, out=mb.LinearOut(out))
+    assert torch.equal(out[first:end].double(), torch.einsum("rk,rnk->rn", xs, w[owner].double())) and (out[:first] == 7).all() and (out[end:] == 7).all()
+    dx = torch.full((R, k), 7.0, device="cuda", dtype=T)
+    mb.expert_linear_backward(dout, off, w, w_up=wu, out=mb.LinearGrad(dx))
+    want = torch.einsum("rn,rnk->rk", ds[:, :n], w[owner].double()) + torch.einsum("rn,rnk->rk", ds[:, n:], wu[owner].double())
+    assert torch.equal(dx[first:end].double(), want.to(T).double()) and (dx[:first] == 7).all() and (dx[end:] == 7).all()
+    r = mb.expert_linear_dweight(dout, x, off, gated=True, want_db=True, out_dtype=F32)
+    for i in range(2):
+        d = ds[:, i * n:(i + 1) * n]
+        dw = torch.zeros(E, n, k, dtype=torch.float64, device="cuda").index_add_(0, owner, torch.einsum("rn,rk->rnk", d, xs))
+        assert torch.equal(r[i].double(), dw) and torch.equal(r[2 + i].double(), torch.zeros(E, n, dtype=torch.float64, device="cuda").index_add_(0, owner, d))
+    mb.expert_linear_status()
